@@ -108,7 +108,8 @@ int eqat_device_status(int* h_status, int* h_detail);
  * normally.  This call enqueues one warp that waits, with a limit of 1 ms, on a
  * barrier that nothing ever signals, through the very wait routine of the GEMM
  * kernels (which = 0), of the streaming kernels (1), of the matrix-vector forward
- * (2), of the forward on weight-row tiles (3) or on pairs of them (4); afterwards
+ * (2), of the forward on weight-row tiles (3) or on pairs of them (4), or of the
+ * attention over the cache (5); afterwards
  * eqat_device_status() must report EQAT_ERR_TIMEOUT once and EQAT_OK from then
  * on.  It touches no tensor. */
 int eqat_selftest_wait_expiry(int which, void* stream);
@@ -306,6 +307,116 @@ int qlinear_packed_bwd_dx(const eqat_desc* desc, const eqat_bf16* dY, const uint
 int qlinear_packed_bwd_ds(const eqat_desc* desc, const eqat_bf16* X, const eqat_bf16* dY,
                           const uint8_t* Wq_packed, const void* z, const eqat_fp16* s16,
                           float* ds, float* dz, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------ key/value cache */
+
+/* The keys and values of the tokens before, held in 4 bits and in pages, and the
+ * attention over them (no counterpart in the paper, which quantises weights only:
+ * a block whose linears run through qlinear_packed_fwd spends its memory and its
+ * decoding time on them).  The quantiser is that of Eqs. 1-2 with the parameters
+ * of each group's range, as in eqat_minmax_init, except that the zero point is the
+ * real number -m/s: a group of a cache need not contain 0.  A group x_1..x_g of
+ * bf16 numbers (consecutive elements of a head of one token) with the minimum m
+ * and the maximum M is held as
+ *     s   = bf16((M - m) * (1/15)), 0 where that is below 2^-126,
+ *     q_i = clamp(round((x_i - m) * (1/s)), 0, 15), 0 where s = 0,
+ * evaluated in binary32 (1/15 and 1/s rounded to it; half to even), and stands
+ * for q_i * s + m.  m is exact.  A group with a NaN, an infinity or a range
+ * beyond binary32 stands for NaN.
+ *
+ * A pool holds `pages` pages, each `page_size` tokens of every key/value head:
+ *     codes  [pages, kv_heads, page_size, head_dim/2]      u8, two codes a byte, the
+ *            even element in the low half (the dense stream of eqat_pack)
+ *     params [pages, kv_heads, page_size, head_dim/group, 2] bf16, s then m
+ * for the keys and for the values.  Sequence b owns the pages in row b of
+ * page_table [sequences, max_pages]: its token at position p is token p %
+ * page_size of page page_table[b][p / page_size].
+ *
+ * A call works on `rows` rows, the new tokens of all sequences one after the
+ * other: rows row_offsets[b] up to row_offsets[b+1] belong to sequence b
+ * (row_offsets [sequences+1] starts at 0 and does not fall; a sequence may have
+ * none), which holds lengths[b] tokens WITH them, so that its n rows stand at
+ * positions lengths[b]-n .. lengths[b]-1.  The three arrays are int32 in device
+ * memory; the host knows upper bounds only, so a captured call serves every
+ * batch within them.  Rows from row_offsets[sequences] on belong to nobody:
+ * nothing is read or written for them.
+ * Contents of the arrays are not checked on the host: offsets are limited to
+ * rows and lengths to max_pages * page_size; a position below 0 or a page number
+ * outside the pool is not written, reads as zero, and as a key the latter gives
+ * undefined values; no access leaves the tensors.  Table entries behind a
+ * sequence's length may hold anything.
+ *
+ * X, Q, O, K, V are [rows, heads, head_dim] with heads and elements dense; the
+ * pitch of a row, in elements, is a multiple of 8 (a slice of a fused projection
+ * can be passed as it is).
+ *
+ * Geometry: bits 4; head_dim 64, 128 or 256; group 32, 64 or 128, at most
+ * head_dim; page_size a multiple of 16; page_size * max_pages at most 2^30; at most
+ * 2^37 bytes of codes for the keys (and as many for the values). */
+typedef struct {
+  int32_t bits;               /* 4                                                    */
+  int32_t group;              /* elements per group along head_dim                    */
+  int32_t head_dim;
+  int32_t kv_heads;
+  int32_t page_size;          /* tokens in a page                                     */
+  int32_t pages;              /* pages in the pool                                    */
+  int32_t sequences;
+  int32_t max_pages;          /* columns of page_table                                */
+  int64_t rows;               /* rows of the row tensors                              */
+} eqat_cache_desc;
+
+typedef struct {              /* the pool: device pointers, each 16-byte aligned */
+  uint8_t* k_codes;
+  eqat_bf16* k_params;
+  uint8_t* v_codes;
+  eqat_bf16* v_params;
+} eqat_cache;
+
+/* Quantises K and V of the rows and writes them to their places.  K_hat, V_hat
+ * [rows, kv_heads, head_dim] dense (both or neither may be NULL) receive, in
+ * bf16, what the cache now holds for them, as W_hat of qlinear_fakequant_fwd: a
+ * prompt's own attention can use the values that later tokens will see.  Two rows
+ * that name the same place leave it with bytes of either. */
+int eqat_cache_append(const eqat_cache_desc* desc, const eqat_bf16* K, int64_t k_pitch, const eqat_bf16* V,
+                      int64_t v_pitch, const int32_t* row_offsets, const int32_t* lengths,
+                      const int32_t* page_table, const eqat_cache* cache, eqat_bf16* K_hat, eqat_bf16* V_hat,
+                      void* stream);
+
+/* The values that the cache holds for the rows' positions, in bf16: the last
+ * row_offsets[b+1] - row_offsets[b] tokens of each sequence.
+ *   K_hat, V_hat [rows, kv_heads, head_dim] dense (out) */
+int eqat_cache_read(const eqat_cache_desc* desc, const int32_t* row_offsets, const int32_t* lengths,
+                    const int32_t* page_table, const eqat_cache* cache, eqat_bf16* K_hat, eqat_bf16* V_hat,
+                    void* stream);
+
+typedef struct {
+  int32_t q_heads;            /* a multiple of kv_heads; query head h reads kv head h / (q_heads/kv_heads) */
+  int32_t max_new;            /* no sequence has more rows in this call (rows beyond are left out)         */
+  float scale;                /* of the scores, e.g. head_dim^-1/2                                         */
+  int32_t window;             /* a row at position p sees keys p-window+1 .. p; 0: 0 .. p                  */
+} eqat_attention_desc;
+
+/* Bytes of scratch eqat_cache_attention needs on the current device, 256-byte
+ * aligned ((size_t)-1 if a descriptor is invalid).  Its contents do not matter and
+ * are overwritten: calls that may overlap (streams, graphs replayed side by
+ * side) need a workspace each. */
+size_t eqat_cache_workspace_bytes(const eqat_cache_desc* desc, const eqat_attention_desc* attn);
+
+/* Causal attention of the rows' queries over the cache, which already holds the
+ * rows' own keys and values (eqat_cache_append):
+ *     z_j = scale * sum_d Q_d K_jd,   O = sum_j softmax(z)_j V_j,
+ * over the keys j that a row sees.  A row that sees none gets zeros, and lse
+ * -infinity.  lse [rows, q_heads] fp32 dense (may be NULL): log of sum_j exp(z_j).
+ * Codes enter the products as exact integers; steps and minima multiply fp32
+ * sums, softmax statistics and outputs are fp32 until the final rounding, and the
+ * weights of the values (softmax times step) are rounded to bf16.
+ * Repeated calls give the same bits on one device; the order in which a long
+ * sequence is added up depends on the lengths of the whole batch.
+ *   Q [rows, q_heads, head_dim] bf16 (in)   O [rows, q_heads, head_dim] bf16 (out) */
+int eqat_cache_attention(const eqat_cache_desc* desc, const eqat_attention_desc* attn, const eqat_bf16* Q,
+                         int64_t q_pitch, const int32_t* row_offsets, const int32_t* lengths,
+                         const int32_t* page_table, const eqat_cache* cache, eqat_bf16* O, int64_t o_pitch,
+                         float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------ whole blocks */
 

@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, c_char_p, c_int, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, Structure, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 
 import torch
 
@@ -49,12 +49,26 @@ class eqat_e2e_qp_linear(Structure):
                 ("workspace", c_void_p), ("workspace_bytes", c_size_t)]
 
 
+class eqat_cache_desc(Structure):
+    _fields_ = [("bits", c_int32), ("group", c_int32), ("head_dim", c_int32), ("kv_heads", c_int32), ("page_size", c_int32),
+                ("pages", c_int32), ("sequences", c_int32), ("max_pages", c_int32), ("rows", c_int64)]
+
+
+class eqat_cache(Structure):
+    _fields_ = [("k_codes", c_void_p), ("k_params", c_void_p), ("v_codes", c_void_p), ("v_params", c_void_p)]
+
+
+class eqat_attention_desc(Structure):
+    _fields_ = [("q_heads", c_int32), ("max_new", c_int32), ("scale", c_float), ("window", c_int32)]
+
+
 def _load():
     if not os.path.exists(_LIB_PATH):
         raise ImportError(f"{_LIB_PATH} is missing: build it with `python -m paper_2407_11062_b200.build` "
                           "(there is no fallback path)")
     lib = ctypes.CDLL(_LIB_PATH)
     D, P = POINTER(eqat_desc), c_void_p
+    C, K, A = POINTER(eqat_cache_desc), POINTER(eqat_cache), POINTER(eqat_attention_desc)
     sigs = {
         "eqat_status_string": (c_char_p, [c_int]),
         "eqat_version": (c_int, []),
@@ -78,6 +92,10 @@ def _load():
         "eqat_gemm_tile": (c_int, [D, c_int, c_int, POINTER(c_int)]),
         "qlinear_packed_bwd_dx": (c_int, [D, P, P, P, P, P, P]),
         "qlinear_packed_bwd_ds": (c_int, [D, P, P, P, P, P, P, P, P, c_size_t, P]),
+        "eqat_cache_append": (c_int, [C, P, c_int64, P, c_int64, P, P, P, K, P, P, P]),
+        "eqat_cache_read": (c_int, [C, P, P, P, K, P, P, P]),
+        "eqat_cache_workspace_bytes": (c_size_t, [C, A]),
+        "eqat_cache_attention": (c_int, [C, A, P, c_int64, P, P, P, K, P, c_int64, P, P, c_size_t, P]),
         "eqat_block_ap_step": (c_int, [POINTER(eqat_block_ap_linear), c_int, POINTER(c_int), P]),
         "eqat_e2e_qp_step": (c_int, [POINTER(eqat_e2e_qp_linear), c_int, POINTER(c_int), P]),
     }
@@ -240,6 +258,57 @@ def qlinear_packed_bwd_ds(desc, X, dY, Wq_packed, z8, s16, ds, dz=None, workspac
     _check(lib.qlinear_packed_bwd_ds(ctypes.byref(desc), _ptr(X), _ptr(dY), _ptr(Wq_packed), _ptr(z8), _ptr(s16),
                                      _ptr(ds), _ptr(dz), _ptr(workspace), nbytes, _stream()),
            "qlinear_packed_bwd_ds")
+
+
+def make_cache_desc(group, head_dim, kv_heads, page_size, pages, sequences, max_pages, rows, bits=4) -> eqat_cache_desc:
+    return eqat_cache_desc(int(bits), int(group), int(head_dim), int(kv_heads), int(page_size), int(pages), int(sequences),
+                           int(max_pages), int(rows))
+
+
+def make_attention_desc(q_heads, max_new, scale, window=0) -> eqat_attention_desc:
+    return eqat_attention_desc(int(q_heads), int(max_new), float(scale), int(window))
+
+
+def _row_ptr(t):
+    """Address and row pitch of a [rows, heads, head_dim] tensor whose heads and elements are dense."""
+    if not t.is_cuda or t.dim() != 3 or t.stride(2) != 1 or t.stride(1) != t.size(2):
+        raise ValueError("expected a CUDA tensor [rows, heads, head_dim] with dense heads")
+    return t.data_ptr(), t.stride(0) if t.size(0) > 1 else max(t.stride(0), t.size(1) * t.size(2))
+
+
+def _pool(cache):
+    """`cache`: k_codes, k_params, v_codes, v_params."""
+    return ctypes.byref(eqat_cache(*[_ptr(t) for t in cache]))
+
+
+def cache_workspace_bytes(desc, attn) -> int:
+    n = lib.eqat_cache_workspace_bytes(ctypes.byref(desc), ctypes.byref(attn))
+    if n == ctypes.c_size_t(-1).value:
+        raise EqatError(EQAT_ERR_SHAPE, "eqat_cache_workspace_bytes")
+    return int(n)
+
+
+def eqat_cache_append(desc, K, V, row_offsets, lengths, page_table, cache, K_hat=None, V_hat=None):
+    """K, V: [rows, kv_heads, head_dim], rows of any pitch.  K_hat, V_hat (or None): what the cache now holds for them."""
+    k, k_pitch = _row_ptr(K)
+    v, v_pitch = _row_ptr(V)
+    _check(lib.eqat_cache_append(ctypes.byref(desc), k, k_pitch, v, v_pitch, _ptr(row_offsets), _ptr(lengths),
+                                 _ptr(page_table), _pool(cache), _ptr(K_hat), _ptr(V_hat), _stream()),
+           "eqat_cache_append")
+
+
+def eqat_cache_read(desc, row_offsets, lengths, page_table, cache, K_hat, V_hat):
+    _check(lib.eqat_cache_read(ctypes.byref(desc), _ptr(row_offsets), _ptr(lengths), _ptr(page_table), _pool(cache),
+                               _ptr(K_hat), _ptr(V_hat), _stream()), "eqat_cache_read")
+
+
+def eqat_cache_attention(desc, attn, Q, row_offsets, lengths, page_table, cache, O, lse=None, workspace=None):
+    """Q, O: [rows, q_heads, head_dim], rows of any pitch.  lse (or None): [rows, q_heads] fp32."""
+    q, q_pitch = _row_ptr(Q)
+    o, o_pitch = _row_ptr(O)
+    _check(lib.eqat_cache_attention(ctypes.byref(desc), ctypes.byref(attn), q, q_pitch, _ptr(row_offsets), _ptr(lengths),
+                                    _ptr(page_table), _pool(cache), o, o_pitch, _ptr(lse), _ptr(workspace),
+                                    _nbytes(workspace), _stream()), "eqat_cache_attention")
 
 
 def _nbytes(t):

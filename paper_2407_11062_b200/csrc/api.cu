@@ -1,6 +1,7 @@
 // C ABI (include/eqat.h): argument validation on the host, then launches.
 #include <stdint.h>
 
+#include "cache.cuh"
 #include "common.cuh"
 #include "elementwise.cuh"
 #include "gemm.cuh"
@@ -111,6 +112,40 @@ int v_packed_bwd_ds(const eqat_desc* d, const eqat_bf16* X, const eqat_bf16* dY,
   return EQAT_OK;
 }
 
+int check_cache_desc(const eqat_cache_desc* d) {
+  if (d == nullptr) return EQAT_ERR_NULL;
+  if (d->bits != 4) return EQAT_ERR_UNSUPPORTED;
+  if (d->head_dim != 64 && d->head_dim != 128 && d->head_dim != 256) return EQAT_ERR_UNSUPPORTED;
+  if (d->group != 32 && d->group != 64 && d->group != 128) return EQAT_ERR_UNSUPPORTED;
+  if (d->group > d->head_dim || d->kv_heads <= 0 || d->kv_heads > 65536) return EQAT_ERR_SHAPE;
+  if (d->page_size <= 0 || d->page_size % 16 != 0 || d->pages <= 0 || d->sequences <= 0 || d->max_pages <= 0) return EQAT_ERR_SHAPE;
+  if (d->sequences > 1 << 20 || d->rows <= 0 || d->rows > (int64_t)1 << 30) return EQAT_ERR_SHAPE;
+  if ((int64_t)d->page_size * d->max_pages > (int64_t)1 << 30) return EQAT_ERR_SHAPE;
+  // lines of 128 bytes of codes are counted in 30 bits; in steps, since the whole product may pass 64
+  const int64_t page = (int64_t)d->kv_heads * d->page_size * (d->head_dim / 2);
+  if (page > (int64_t)1 << 37 || page * d->pages > (int64_t)1 << 37) return EQAT_ERR_SHAPE;
+  return EQAT_OK;
+}
+
+int check_cache_ptrs(const int32_t* row_offsets, const int32_t* lengths, const int32_t* page_table, const eqat_cache* c) {
+  if (c == nullptr) return EQAT_ERR_NULL;
+  return check_ptrs(row_offsets, lengths, page_table, c->k_codes, c->k_params, c->v_codes, c->v_params);
+}
+
+inline bool pitch_ok(int64_t pitch, int64_t heads, int64_t head_dim) {
+  return pitch >= heads * head_dim && pitch % 8 == 0 && pitch < (int64_t)1 << 40;
+}
+
+int check_attention_desc(const eqat_cache_desc* d, const eqat_attention_desc* a) {
+  const int rc = check_cache_desc(d);
+  if (rc != EQAT_OK) return rc;
+  if (a == nullptr) return EQAT_ERR_NULL;
+  if (a->q_heads <= 0 || a->q_heads > 65536 || a->q_heads % d->kv_heads != 0) return EQAT_ERR_SHAPE;
+  if (a->max_new <= 0 || a->window < 0) return EQAT_ERR_SHAPE;
+  if (!(a->scale > -1e30f && a->scale < 1e30f)) return EQAT_ERR_UNSUPPORTED;
+  return EQAT_OK;
+}
+
 // The kernel that takes a packed forward.
 struct PackedRoute {
   int kernel;                            // EQAT_ROUTE_*
@@ -171,14 +206,15 @@ size_t eqat_workspace_bytes(const eqat_desc* d, int op) {
 
 int eqat_device_status(int* h_status, int* h_detail) {
   if (h_status == nullptr) return EQAT_ERR_NULL;
-  int st[5] = {0, 0, 0, 0, 0}, det[5] = {0, 0, 0, 0, 0};
+  int st[6] = {0, 0, 0, 0, 0, 0}, det[6] = {0, 0, 0, 0, 0, 0};
   EQAT_TRY(read_device_status(&st[0], &det[0]));      // GEMM kernels
   EQAT_TRY(read_stream_status(&st[1], &det[1]));      // staged streaming kernels
   EQAT_TRY(read_gemv_status(&st[2], &det[2]));        // matrix-vector kernels
   EQAT_TRY(read_slim_status(&st[3], &det[3]));        // weight-row kernels: few tokens,
   EQAT_TRY(read_wide_status(&st[4], &det[4]));        // prompts
+  EQAT_TRY(read_attention_status(&st[5], &det[5]));   // attention over the cache
   int k = 0;
-  while (k < 4 && st[k] == EQAT_OK) ++k;
+  while (k < 5 && st[k] == EQAT_OK) ++k;
   *h_status = st[k];
   if (h_detail != nullptr) *h_detail = det[k];
   return EQAT_OK;
@@ -190,6 +226,7 @@ int eqat_selftest_wait_expiry(int which, void* stream) {
   if (which == 2) return launch_wait_expiry_gemv(as_stream(stream));
   if (which == 3) return launch_wait_expiry_slim(as_stream(stream));
   if (which == 4) return launch_wait_expiry_wide(as_stream(stream));
+  if (which == 5) return launch_wait_expiry_attention(as_stream(stream));
   return EQAT_ERR_UNSUPPORTED;
 }
 
@@ -334,6 +371,47 @@ int qlinear_packed_bwd_ds(const eqat_desc* d, const eqat_bf16* X, const eqat_bf1
                           size_t workspace_bytes, void* stream) {
   EQAT_TRY(v_packed_bwd_ds(d, X, dY, Wq_packed, z, s16, ds, dz, workspace, workspace_bytes));
   return launch_packed_ds(*d, X, dY, Wq_packed, z, s16, ds, dz, workspace, as_stream(stream));
+}
+
+int eqat_cache_append(const eqat_cache_desc* d, const eqat_bf16* K, int64_t k_pitch, const eqat_bf16* V, int64_t v_pitch,
+                      const int32_t* row_offsets, const int32_t* lengths, const int32_t* page_table, const eqat_cache* cache,
+                      eqat_bf16* K_hat, eqat_bf16* V_hat, void* stream) {
+  EQAT_TRY(check_cache_desc(d));
+  if (!pitch_ok(k_pitch, d->kv_heads, d->head_dim) || !pitch_ok(v_pitch, d->kv_heads, d->head_dim)) return EQAT_ERR_SHAPE;
+  EQAT_TRY(check_ptrs(K, V));
+  EQAT_TRY(check_cache_ptrs(row_offsets, lengths, page_table, cache));
+  if ((K_hat == nullptr) != (V_hat == nullptr)) return EQAT_ERR_NULL;
+  if (!aligned16(K_hat) || !aligned16(V_hat)) return EQAT_ERR_ALIGN;
+  return launch_cache_append(*d, K, k_pitch, V, v_pitch, cache_view(*d, row_offsets, lengths, page_table, *cache), K_hat, V_hat,
+                             as_stream(stream));
+}
+
+int eqat_cache_read(const eqat_cache_desc* d, const int32_t* row_offsets, const int32_t* lengths, const int32_t* page_table,
+                    const eqat_cache* cache, eqat_bf16* K_hat, eqat_bf16* V_hat, void* stream) {
+  EQAT_TRY(check_cache_desc(d));
+  EQAT_TRY(check_cache_ptrs(row_offsets, lengths, page_table, cache));
+  EQAT_TRY(check_ptrs(K_hat, V_hat));
+  return launch_cache_read(*d, cache_view(*d, row_offsets, lengths, page_table, *cache), K_hat, V_hat, as_stream(stream));
+}
+
+size_t eqat_cache_workspace_bytes(const eqat_cache_desc* d, const eqat_attention_desc* a) {
+  return check_attention_desc(d, a) == EQAT_OK ? cache_attention_workspace(*d, *a) : (size_t)-1;
+}
+
+int eqat_cache_attention(const eqat_cache_desc* d, const eqat_attention_desc* a, const eqat_bf16* Q, int64_t q_pitch,
+                         const int32_t* row_offsets, const int32_t* lengths, const int32_t* page_table,
+                         const eqat_cache* cache, eqat_bf16* O, int64_t o_pitch, float* lse, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  EQAT_TRY(check_attention_desc(d, a));
+  if (!pitch_ok(q_pitch, a->q_heads, d->head_dim) || !pitch_ok(o_pitch, a->q_heads, d->head_dim)) return EQAT_ERR_SHAPE;
+  EQAT_TRY(check_ptrs(Q, O));
+  EQAT_TRY(check_cache_ptrs(row_offsets, lengths, page_table, cache));
+  if (!aligned16(lse)) return EQAT_ERR_ALIGN;
+  const size_t need = cache_attention_workspace(*d, *a);
+  if (need != 0 && (workspace == nullptr || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0))
+    return EQAT_ERR_WORKSPACE;
+  return launch_cache_attention(*d, *a, Q, q_pitch, cache_view(*d, row_offsets, lengths, page_table, *cache), O, o_pitch, lse,
+                                workspace, as_stream(stream));
 }
 
 int eqat_block_ap_step(const eqat_block_ap_linear* L, int count, int* h_failed, void* stream) {
