@@ -206,14 +206,15 @@ size_t eqat_workspace_bytes(const eqat_desc* d, int op) {
 
 int eqat_device_status(int* h_status, int* h_detail) {
   if (h_status == nullptr) return EQAT_ERR_NULL;
-  int st[5] = {0, 0, 0, 0, 0}, det[5] = {0, 0, 0, 0, 0};
+  int st[6] = {0, 0, 0, 0, 0, 0}, det[6] = {0, 0, 0, 0, 0, 0};
   EQAT_TRY(read_device_status(&st[0], &det[0]));      // GEMM kernels
   EQAT_TRY(read_stream_status(&st[1], &det[1]));      // staged streaming kernels
   EQAT_TRY(read_gemv_status(&st[2], &det[2]));        // matrix-vector kernels
   EQAT_TRY(read_slim_status(&st[3], &det[3]));        // weight-row kernels: few tokens,
   EQAT_TRY(read_wide_status(&st[4], &det[4]));        // prompts
+  EQAT_TRY(read_attention_status(&st[5], &det[5]));   // attention over the cache
   int k = 0;
-  while (k < 4 && st[k] == EQAT_OK) ++k;
+  while (k < 5 && st[k] == EQAT_OK) ++k;
   *h_status = st[k];
   if (h_detail != nullptr) *h_detail = det[k];
   return EQAT_OK;
@@ -225,6 +226,7 @@ int eqat_selftest_wait_expiry(int which, void* stream) {
   if (which == 2) return launch_wait_expiry_gemv(as_stream(stream));
   if (which == 3) return launch_wait_expiry_slim(as_stream(stream));
   if (which == 4) return launch_wait_expiry_wide(as_stream(stream));
+  if (which == 5) return launch_wait_expiry_attention(as_stream(stream));
   return EQAT_ERR_UNSUPPORTED;
 }
 

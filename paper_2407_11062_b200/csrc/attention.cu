@@ -1,30 +1,33 @@
-// Attention of a few new tokens over the 4-bit cache: decoding, drafted tokens.
+// Attention of new tokens over the 4-bit cache, on the tensor cores without expanding a code to more than a byte.
 //
-// A key/value head's codes are read once for up to 8 * NT query rows (new tokens x the query heads that share the head).
-// With step s and minimum m of a group and q a code, K = q s + m and V likewise, so
-//     Q . K_t  = sum over groups of  s_t (sum_d Q_d q_td) + m_t (sum_d Q_d)
-//     sum_t p_t V_t = sum_t (p_t s_t) (q_t - 8) + sum_t p_t (m_t + 8 s_t):
-// both products run on matrix instructions with codes as exact bf16 integers (128 + q for the keys, whose constant goes into
-// the second term; q - 8 for the values, where a long even softmax adds up to far less than 128 times its terms), steps and
-// minima multiply fp32 sums.  p_t s_t is rounded to bf16, as the softmax weights of any attention on these instructions are.
+// A CTA takes a tile of 128 tokens of one key/value head at a time, for 8 to 32 query rows (new tokens x the query heads
+// that share the head).  With step s and minimum m of a group and q a code, K = q s + m and V likewise, so
+//     Q . K_t       = sum over groups of  s_t (sum_d Q_d q_td) + m_t (sum_d Q_d)
+//     sum_t p_t V_t = sum_t (p_t s_t) q_t + sum_t p_t m_t:
+// the codes enter both products as they are, as bytes, and steps and minima multiply sums.  Tokens are the 128 rows of the
+// first product and elements of the head those of the second, so eight query rows are eight columns and not an eighth of a
+// 128-row tile; each code costs three operations per eight and one byte of shared memory.
+//   scores   kind::f8f6f4: the byte q is the e4m3 number q 2^-9 (0..7 below the normal range, 8..15 in the first binade).
+//            A query row is scaled by a power of two and split into two e4m3 numbers, the second one 2^-4 finer: exact for
+//            bf16 down to 2^-13 of the row's largest element, to 2^-22 of it below.
+//   values   kind::i8: p s as an integer of 23 bits, its three bytes as columns of their own, unsigned codes, sums exact in
+//            32 bits.  (In fp32 the sums of the uncentred codes would be rounded at some thousand times the size of a long
+//            even softmax's output.)
+// Groups of the keys are ranges of K with accumulators of their own, groups of the values have columns of their own.
 //
-// Scores are computed transposed (16 tokens x 8 rows), so the codes are always the 16-row operand and one user's single
-// query wastes nothing but columns.  The layout of the two operands:
-//   keys    ldmatrix gives a thread the words of tokens g, g + 8 (g = lane / 4): eight codes of one token; the nibbles 4
-//           apart are a register pair, so a word is two k-steps of one group.  The queries are put in that order once.
-//   values  ldmatrix.trans gives a thread halfword g of a 16-byte chunk for two neighbouring tokens: again pairs.
-//   p s     is transposed by movmatrix from the score layout to that of the second operand.
+// Every thread is one token of the tile in the softmax: scores arrive as columns of its lane of tensor memory, so no value
+// is exchanged between threads but a vote: a row's exponent is raised only when a score or a step leaves the range of the
+// 23 bits, then the integer sums are emptied into fp32 registers (a thread is one element of the head there).
 //
-// Work is dealt out in units of one 4-warp CTA's stage (4096 / head_dim tokens per warp); the units of all (sequence, row
-// tile, head) segments are laid end to end and every CTA takes an equal stretch, so batches of any lengths fill the device.
-// A segment that several CTAs share is joined by a second small kernel in a fixed order.  Inside a CTA every warp has its
-// own ring of stages, fed by its own lanes with tensor copies (codes, 128-byte swizzle: ldmatrix without conflicts) and bulk
-// copies (steps and minima), its own maximum, sum and accumulators; warps meet at the end of a segment.
+// Work is dealt out in tiles: those of all (sequence, row tile, head) segments are laid end to end and every CTA takes an
+// equal stretch, so batches of any lengths fill the device.  A segment that several CTAs share is joined by a second small
+// kernel in a fixed order.
 #include <type_traits>
 
 #include "cache.cuh"
 #include "common.cuh"
 #include "ptx.cuh"
+#include "wait.cuh"
 
 namespace eqat {
 namespace {
@@ -32,28 +35,42 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLazy = 8.0f;                        // a maximum may be exceeded by 2^8 before the sums are rescaled
+// Weights are p = 2^(z - shift), z the score in log2; the shift is the row's largest score (as of its last raise) plus
+// log2(unit) - kOne, unit a power of two above all steps that the row has counted, so p s < 2^23 as long as no score exceeds
+// that maximum by more than kLazy.
+constexpr float kLazy = 2.0f, kOne = 21.0f;
 
-template <int D, int G, int NT>
+// D: elements of a head, G: groups in it, NB: blocks of eight query rows.
+template <int D, int G, int NB>
 struct Shape {
-  static constexpr int kStageTokens = 4096 / D;                 // per warp
-  static constexpr int kCodeBytes = kStageTokens * D / 2;              // codes of the keys or of the values
-  static constexpr int kSteps = kStageTokens / 16;
-  static constexpr int kPieces = kSteps;                               // of 16 tokens, each in one page
-  static constexpr int kUnit = kWarps * kStageTokens;
-  static constexpr int kRows = 8 * NT;
-  static constexpr int kParamBytes = kStageTokens * G * 4;
-  static constexpr int kMergeFloats = kRows * D;                       // of a warp, in its ring
-  static constexpr int kStages = kMergeFloats * 4 > 6 * kCodeBytes ? 4 : 3;
-  static constexpr int kRingBytes = kStages * 2 * kCodeBytes;                    // codes of a warp (1024-byte aligned)
-  static constexpr int kParamCopies = kPieces * 8 * G > 32 ? kPieces * 8 * G / 32 : 1;    // 16-byte copies of a lane
-  static constexpr int kParamRing = kStages * 2 * kParamBytes;
-  static constexpr int kWarpBytes = kRingBytes + kParamRing;
-  static constexpr int kSmemBytes = 1024 + kWarps * kWarpBytes;
-  static constexpr int kRegCtas = NT * D <= 128 ? 4 : NT * D <= 256 ? 3 : 2;
-  static constexpr int kSmemCtas = 227 * 1024 / (kSmemBytes + 1024 + 512);
-  static constexpr int kCtas = kRegCtas < kSmemCtas ? kRegCtas : kSmemCtas;
-  static_assert(kMergeFloats * 4 <= kRingBytes, "the accumulators of a warp are exchanged through its ring");
+  static constexpr int kStageTokens = 16;                              // segments start at a multiple of this
+  static constexpr int kUnit = 128;                                    // tokens of a tile
+  static constexpr int kRows = 8 * NB;
+  static constexpr int kBlocks = D > 128 ? D / 128 : 1;                // blocks of 128 elements
+  static constexpr int kBlockGroups = G / kBlocks;
+  static constexpr int kParts = NB * kBlockGroups;                     // (row block, group) pairs of a block: three byte columns x 8
+  static constexpr int kWeightUnits = kParts == 1 ? 2 : kParts + kParts / 2;      // 16-byte units of a token's weights, per block
+  static constexpr int kWeightCols = 16 * kWeightUnits;
+  static constexpr int kScoreCols = 16 * NB * G;
+  static constexpr int kSumCols = kBlocks * kWeightCols;
+  // tensor memory: sums, then scores; 160 columns are taken as 128 + 32, with the last two score blocks in the 32
+  static constexpr int kCols = kScoreCols + kSumCols;
+  static constexpr bool kTwoParts = kCols > 128 && kCols <= 160 && G >= 2 && NB == 1;
+  static constexpr int kAlloc = kCols <= 64 ? 64 : kCols <= 128 || kTwoParts ? 128 : kCols <= 256 ? 256 : 512;
+  static constexpr int kOperandBytes = kBlocks * 128 * 128;            // of keys or values: 128 tokens x 128 bytes a block
+  static constexpr int kWeightBytes = kBlocks * kWeightUnits * 2048;
+  static constexpr int kQueryBytes = kBlocks * NB * 2048;
+  static constexpr int kNeedBytes = 1024 + 2 * kOperandBytes + kWeightBytes + kQueryBytes;
+  // Two CTAs that each hold one part and wait for the other must not fill the tensor memory: no more than three of them fit
+  // on an SM (4 * 57 KB are more than it has).
+  static constexpr int kSmemBytes = kTwoParts && kNeedBytes < 57 * 1024 ? 57 * 1024 : kNeedBytes;
+  static constexpr int kTmemCtas = 512 / (kAlloc + (kTwoParts ? 32 : 0));
+  static constexpr int kSmemCtas = 227 * 1024 / (kSmemBytes + 4096);
+  static constexpr int kRegCtas = kRows * (1 + G) + kRows * kBlocks <= 40 ? 4 : 3;
+  static constexpr int kCtas = kTmemCtas < kSmemCtas ? (kTmemCtas < kRegCtas ? kTmemCtas : kRegCtas) : (kSmemCtas < kRegCtas ? kSmemCtas : kRegCtas);
+  static constexpr int kLoads = D / 32;                                // 16-byte loads of a lane per tile, keys or values
+  static_assert((1 + G) * kRows * 512 <= 2 * kOperandBytes && kRows * D * 4 <= 2 * kOperandBytes, "sums meet in the operands' memory");
+  static_assert(kCols <= 512, "tensor memory");
 };
 
 struct AttentionArgs {
@@ -166,83 +183,112 @@ __device__ __forceinline__ Segment segment_of(const AttentionArgs& a, const Sequ
 }
 
 // ------------------------------------------------------------------ instructions
-__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
-  uint32_t r;
-  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
-  return r;
-}
-// D (16 x 8, fp32) += A (16 x 16, fp16) * B (16 x 8, fp16)
-__device__ __forceinline__ void mma_fp16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ float exp2_approx(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-// 16 bytes from global to shared memory, asynchronously; groups of copies are waited for by the thread that made them.
-__device__ __forceinline__ void copy_16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+// D[tmem] (+)= A[smem] * B[smem], bytes: e4m3 numbers with fp32 sums, unsigned integers with 32-bit sums.
+__device__ __forceinline__ void mma_e4m3(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int PENDING>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
-// q - 8 of the low nibbles of two bytes, times 2^-24, and of the high ones, times 2^-20: exact in fp16.
-__device__ __forceinline__ uint32_t add_fp16x2(uint32_t x, uint32_t y) {
-  const __half2 r = __hadd2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&y));
-  return *reinterpret_cast<const uint32_t*>(&r);
+__device__ __forceinline__ void mma_u8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ uint32_t centred_low(uint32_t w) { return add_fp16x2(w & 0x000F000Fu, 0x80088008u); }
-__device__ __forceinline__ uint32_t centred_high(uint32_t w) { return add_fp16x2(w & 0x00F000F0u, 0x80808080u); }
+// Instruction descriptors: fp32 sums of e4m3, both operands K-major; 32-bit sums of u8, both MN-major.
+constexpr uint32_t kScoreDesc = (1u << 4) | (8u << 24);
+constexpr uint32_t kSumDesc = (2u << 4) | (1u << 15) | (1u << 16) | (8u << 24);
+// Matrix descriptor of the weights: MN-major without swizzle, 16-byte units of columns 2048 bytes apart, 8 tokens 128.
+__device__ __forceinline__ uint64_t weight_desc(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(128u >> 4) << 16) | ((uint64_t)(2048u >> 4) << 32) | (1ull << 46);
+}
+// Two numbers as e4m3, low byte first, and back.
+__device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float2 from_e4m3x2(uint32_t v) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)v));
+  return __half22float2(*reinterpret_cast<const __half2*>(&r));
+}
 template <int G>
-__device__ __forceinline__ void load_params(uint32_t (&r)[G], uint32_t addr) {
+__device__ __forceinline__ void load_params(uint32_t (&r)[G], const uint32_t* p) {
   if constexpr (G == 1) {
-    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r[0]) : "r"(addr) : "memory");
+    r[0] = ptx::ld_global(p);
   } else if constexpr (G == 2) {
-    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr) : "memory");
+    const uint2 v = ptx::ld_global(reinterpret_cast<const uint2*>(p));
+    r[0] = v.x; r[1] = v.y;
   } else {
 #pragma unroll
     for (int i = 0; i < G; i += 4) {
-      const uint4 v = ptx::lds_128(addr + 4 * i);
+      const uint4 v = ptx::ld_global(reinterpret_cast<const uint4*>(p) + i / 4);
       r[i] = v.x; r[i + 1] = v.y; r[i + 2] = v.z; r[i + 3] = v.w;
     }
   }
 }
-
-__device__ __forceinline__ uint32_t pack_fp16x2(float lo, float hi) {
-  const __half2 v = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
+// A CTA's tensor memory (whole warp).
+__device__ __forceinline__ void take_columns(uint32_t smem_dst, uint32_t cols) { ptx::tmem_alloc(smem_dst, cols); }
 
 // ------------------------------------------------------------------ the kernel
+template <int ROWS, int G>
 struct AttentionCtl {
-  float top[kWarps][16], sum[kWarps][16], most[16];
+  uint64_t scores_done, sums_done;
+  uint32_t tmem[2];
+  int abort;
+  float least_unit;
+  // of the query rows
+  float back[ROWS], minus[ROWS], limit[ROWS];          // score in log2 = z * back; minus = -shift; arg above limit: raise
+  float top[ROWS], shift[ROWS], unit[ROWS], factor[ROWS], delta[ROWS];
+  float q_sum[G][ROWS];
+  int low[ROWS], high[ROWS];                           // keys that the row sees
+  float warp_top[kWarps][ROWS], warp_step[kWarps][ROWS];
+  float sums[1 + G][ROWS];
   int64_t scratch[kWarps + 2];
 };
 
-template <int D, int G, int NT>
-__global__ void __launch_bounds__(kThreads, (Shape<D, G, NT>::kCtas))
+template <int D, int G, int NB>
+__global__ void __launch_bounds__(kThreads, (Shape<D, G, NB>::kCtas))
 attention_kernel(const AttentionArgs a) {
-  using S = Shape<D, G, NT>;
-  constexpr int kChunks = D / 32;                                      // 16-byte chunks of a row of codes
-  constexpr int kGroupChunks = kChunks / G;
+  using S = Shape<D, G, NB>;
+  constexpr int kRows = S::kRows, kGroup = D / G;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ AttentionCtl ctl_block;
-  AttentionCtl* ctl = &ctl_block;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+  __shared__ __align__(16) AttentionCtl<kRows, G> ctl_block;
+  AttentionCtl<kRows, G>* ctl = &ctl_block;
+  volatile int* abort_flag = &ctl->abort;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t raw = ptx::smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
-  const uint32_t ring = base + warp * S::kRingBytes;
-  const uint32_t param_ring = base + kWarps * S::kRingBytes + warp * S::kParamRing;
-  float* merge = reinterpret_cast<float*>(smem_raw + (base - raw));
+  const uint32_t keys = base, values = keys + S::kOperandBytes, weights = values + S::kOperandBytes, queries = weights + S::kWeightBytes;
+  float* meet = reinterpret_cast<float*>(smem_raw + (base - raw));       // the operands' memory, between segments
+
+  if (tid == 0) {
+    ptx::mbar_init(ptx::smem_addr(&ctl->scores_done), 1);
+    ptx::mbar_init(ptx::smem_addr(&ctl->sums_done), 1);
+    ctl->abort = 0;
+    ptx::fence_mbar_init();
+  }
+  if (warp == 0) {
+    take_columns(ptx::smem_addr(&ctl->tmem[0]), S::kAlloc);
+    if (S::kTwoParts) take_columns(ptx::smem_addr(&ctl->tmem[1]), 32);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t sum_tmem = ctl->tmem[0], own_lanes = (uint32_t)(warp * 32) << 16;
+  auto score_tmem = [&](int group) -> uint32_t {                         // of the 16 NB columns of a group
+    if (S::kTwoParts && group >= G - 2) return ctl->tmem[1] + 16 * (group - (G - 2));
+    return sum_tmem + S::kSumCols + group * 16 * NB;
+  };
   ptx::grid_dependency_wait();
 
   const CacheView& v = a.cache;
@@ -251,17 +297,12 @@ attention_kernel(const AttentionArgs a) {
   const int64_t x_end = min(x + wp.per, wp.total);
   int b = wp.sequence;
   int64_t seq_before = wp.before;
-
-  // per-lane ldmatrix offset inside 16 tokens of codes: matrices (tokens 0-7, chunk j), (8-15, j), (0-7, j+1), (8-15, j+1)
-  const uint32_t mat_token = ((lane >> 3) & 1) * 8 + (lane & 7);
-  const uint32_t mat_linear = mat_token * (D / 2) + (lane >> 4) * 16;
-  const uint32_t mat_offset = mat_linear ^ (((mat_linear >> 7) & 7u) << 4);
-  const uint32_t copy_offset = (lane * 16) ^ (((lane * 16) >> 3) & 0x70u);
+  uint32_t scores_phase = 0, sums_phase = 0;
 
   while (x < x_end) {
     SequenceWork w = sequence_work<S>(a, b);
     int64_t have = work_units(v, w);
-    while (x >= seq_before + have) {                                   // sequences without rows have no units
+    while (x >= seq_before + have) {                                     // sequences without rows have no units
       seq_before += have;
       w = sequence_work<S>(a, ++b);
       have = work_units(v, w);
@@ -272,396 +313,445 @@ attention_kernel(const AttentionArgs a) {
     const int head = seg % v.kv_heads;
     const Segment sg = segment_of<S>(a, w, seg / v.kv_heads);
     const bool whole = u0 == 0 && u1 == w.units;
+    const int first_token = sg.from + u0 * S::kUnit;
+    const int tiles = first_token < sg.high ? min(u1 - u0, (sg.high - first_token + S::kUnit - 1) / S::kUnit) : 0;
 
-    // ---- the stages of this warp: tokens from + (4 (u0 + i) + warp) * kStageTokens
-    const int first_token = sg.from + (u0 * kWarps + warp) * S::kStageTokens;
-    const int stages = first_token < sg.high ? min(u1 - u0, (sg.high - first_token + S::kUnit - 1) / S::kUnit) : 0;
-    // Lane p < kPieces holds the page of piece p of the stage that is fetched next, as it was read: what is done with it
-    // waits until then.
+    // ---- fetching: a warp has 32 tokens of the tile, two pieces of 16 that lie in one page each; lanes 0 and 1 hold the
+    // pages of the next tile's pieces, as they were read
+    const int warp_token = first_token + 32 * warp;
     auto page_of = [&](int token) {
-      return lane < S::kPieces && token < sg.high ? ld_index(v.page_table + (int64_t)b * v.max_pages + page_index(a, token)) : 0;
+      return lane < 2 && token < sg.high ? ld_index(v.page_table + (int64_t)b * v.max_pages + page_index(a, token)) : 0;
     };
-    int page = page_of(first_token + 16 * lane);
-    auto fetch = [&](int i, int slot) {
-      if (i < stages) {
-        const int t = first_token + i * S::kUnit;
-        const int pieces = min(S::kPieces, (sg.high - t + 15) >> 4);
-        // token slots of the pool, which are less than 2^32; a page number outside counts as the nearest inside
-        const int token = t + 16 * lane;
-        const uint32_t place = ((uint32_t)min(max(page, 0), v.pages - 1) * v.kv_heads + head) * v.page_size +
-                               (token - page_index(a, token) * v.page_size);
-        uint32_t from[S::kPieces];
+    int page = page_of(warp_token + 16 * lane);
+    uint32_t place[2] = {0, 0};                                          // token slots of the pool, less than 2^32
+    auto find = [&](int i) {                                             // the places of tile i
+      const int token = warp_token + i * S::kUnit + 16 * lane;
+      // a page number outside the pool counts as the nearest inside
+      const uint32_t at = ((uint32_t)min(max(page, 0), v.pages - 1) * v.kv_heads + head) * v.page_size + (token - page_index(a, token) * v.page_size);
+      place[0] = __shfl_sync(0xFFFFFFFFu, at, 0);
+      place[1] = __shfl_sync(0xFFFFFFFFu, at, 1);
+      page = page_of(token + S::kUnit);
+    };
+    // 16-byte chunk i * 32 + lane of the warp's 32 tokens
+    auto fetch = [&](uint4 (&to)[S::kLoads], const uint8_t* codes, int i) {
+      const int token = warp_token + i * S::kUnit;
 #pragma unroll
-        for (int p = 0; p < S::kPieces; ++p) from[p] = __shfl_sync(0xFFFFFFFFu, place, p);
+      for (int p = 0; p < 2; ++p) {
+        const uint4* from = reinterpret_cast<const uint4*>(codes + (uint64_t)place[p] * (D / 2)) + lane;
 #pragma unroll
-        for (int p = 0; p < S::kPieces; ++p)
-          if (p < pieces) {
-            const uint8_t *ks = v.kq + (uint64_t)from[p] * (D / 2) + lane * 16, *vs = v.vq + (uint64_t)from[p] * (D / 2) + lane * 16;
-#pragma unroll
-            for (int j = 0; j < D / 64; ++j) {                         // 512 bytes a time; copy_offset: 16-byte chunks swizzled
-              const uint32_t dst = ring + slot * 2 * S::kCodeBytes + p * (8 * D) + j * 512 + (copy_offset ^ (((p * 8 * D + j * 512) >> 3) & 0x70u));
-              copy_16(dst, ks + j * 512);
-              copy_16(dst + S::kCodeBytes, vs + j * 512);
-            }
-          }
-        // 4 G chunks of parameters for each piece, of the keys and of the values
-#pragma unroll
-        for (int e = 0; e < S::kParamCopies; ++e) {
-          const int chunk = e * 32 + lane, p = chunk / (8 * G), part = chunk % (4 * G);
-          const bool keys = chunk % (8 * G) < 4 * G;
-          const uint32_t at = __shfl_sync(0xFFFFFFFFu, place, p);
-          if (p < pieces)
-            copy_16(param_ring + slot * 2 * S::kParamBytes + (keys ? 0 : S::kParamBytes) + p * 64 * G + part * 16,
-                    (keys ? v.kp : v.vp) + (uint64_t)at * G + part * 4);
-        }
-        page = page_of(t + S::kUnit + 16 * lane);
+        for (int j = 0; j < S::kLoads / 2; ++j)
+          to[p * (S::kLoads / 2) + j] = token + 16 * p < sg.high ? ptx::ld_global(from + 32 * j) : make_uint4(0u, 0u, 0u, 0u);
       }
-      copies_commit();
     };
-    __syncwarp();
+    auto fetch_params = [&](uint32_t (&to)[G], const uint32_t* params, int i) {      // of this thread's token
+      const int token = warp_token + i * S::kUnit + (lane & 16);
+      if (token < sg.high) {
+        load_params<G>(to, params + ((uint64_t)(lane < 16 ? place[0] : place[1]) + (lane & 15)) * G);
+      } else {
 #pragma unroll
-    for (int i = 0; i < S::kStages; ++i) fetch(i, i);
+        for (int e = 0; e < G; ++e) to[e] = 0u;
+      }
+    };
+    // Codes of a chunk (32 j .. 32 j + 31 of a token) as bytes: the even ones are 16 bytes 2 j of the token's row, the odd
+    // ones 16 bytes 2 j + 1; 16-byte pieces swizzled by the row.
+    auto spread = [&](const uint4 (&from)[S::kLoads], uint32_t operand) {
+#pragma unroll
+      for (int i = 0; i < S::kLoads; ++i) {
+        const int chunk = i * 32 + lane, token = 32 * warp + chunk / (D / 32), j = chunk % (D / 32);
+        const uint32_t row = operand + (j / 4) * 16384 + token * 128;
+        const uint4 c = from[i];
+        ptx::sts_128(row + ((((j % 4) * 2) ^ (token & 7)) << 4), c.x & 0x0F0F0F0Fu, c.y & 0x0F0F0F0Fu, c.z & 0x0F0F0F0Fu, c.w & 0x0F0F0F0Fu);
+        ptx::sts_128(row + ((((j % 4) * 2 + 1) ^ (token & 7)) << 4), (c.x >> 4) & 0x0F0F0F0Fu, (c.y >> 4) & 0x0F0F0F0Fu,
+                     (c.z >> 4) & 0x0F0F0F0Fu, (c.w >> 4) & 0x0F0F0F0Fu);
+      }
+    };
+    uint4 key_codes[S::kLoads], value_codes[S::kLoads];
+    uint32_t key_params[G], value_params[G], next_key_params[G], next_value_params[G];
+    if (tiles > 0) {
+      find(0);
+      fetch(key_codes, v.kq, 0);
+      fetch_params(next_key_params, v.kp, 0);
+      fetch(value_codes, v.vq, 0);
+      fetch_params(next_value_params, v.vp, 0);
+    }
 
-    // ---- the queries, in the order of the codes, and their sums per group.  A row is scaled by 2^k, so that its largest
-    // element lies in [2^14, 2^15), and rounded to fp16, which holds a bf16 number exactly down to 2^-28 of the largest; `back`
-    // undoes that and the 2^-24 of the codes.  (Rows beyond 2^115 become infinite.)
-    uint32_t q[NT][kChunks][4];
-    float q_sum[NT][G][2], back[NT][2];
-    int row_low[NT][2], row_high[NT][2];                               // keys that the rows of this lane's columns see
+    // ---- the queries: 16 threads a row, scaled so that the largest element lies in [128, 256), in the order of the codes
     const int base_pos = w.rows.length - w.rows.count;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int r = n * 8 + g, row = sg.first_row + r;
-      const eqat_bf16* src = a.Q + (int64_t)(w.rows.first + row / a.ratio) * a.q_pitch + (int64_t)(head * a.ratio + row % a.ratio) * D;
-      uint4 e[kChunks];
-      uint32_t most = 0;
+    for (int rb = 0; rb < NB; ++rb) {
+      constexpr int kEach = D / 16;                                      // elements of a thread
+      const int r = rb * 8 + tid / 16, part = tid % 16, row = sg.first_row + r;
+      uint32_t e[kEach / 2] = {};
+      if (r < sg.rows) {
+        const eqat_bf16* src = a.Q + (int64_t)(w.rows.first + row / a.ratio) * a.q_pitch + (int64_t)(head * a.ratio + row % a.ratio) * D + part * kEach;
 #pragma unroll
-      for (int j = 0; j < kChunks; ++j) {
-        e[j] = make_uint4(0u, 0u, 0u, 0u);
-        if (r < sg.rows) e[j] = ptx::ld_global(reinterpret_cast<const uint4*>(src + j * 32 + c * 8));
-        // bf16 bit patterns without the sign compare like the numbers
-        most = __vmaxu2(most, __vmaxu2(__vmaxu2(e[j].x & 0x7FFF7FFFu, e[j].y & 0x7FFF7FFFu), __vmaxu2(e[j].z & 0x7FFF7FFFu, e[j].w & 0x7FFF7FFFu)));
+        for (int j = 0; j < kEach / 2; j += 2) {
+          const uint2 y = ptx::ld_global(reinterpret_cast<const uint2*>(src + 2 * j));
+          e[j] = y.x; e[j + 1] = y.y;
+        }
+      }
+      uint32_t most = 0;                                                 // bf16 patterns without the sign compare like the numbers
+      float sum = 0.0f;
+#pragma unroll
+      for (int j = 0; j < kEach / 2; ++j) {
+        most = __vmaxu2(most, e[j] & 0x7FFF7FFFu);
+        sum += param_step(e[j]) + param_low(e[j]);
       }
       most = max(most & 0xFFFFu, most >> 16);
-      most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
-      most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-      const int k2 = most == 0 ? 0 : min(max(14 - ((int)(most >> 7) - 127), -100), 100);
-      const float up = __int_as_float((127 + k2) << 23), up16 = up * 0.0625f;
-      float sums[G];
 #pragma unroll
-      for (int k = 0; k < G; ++k) sums[k] = 0.0f;
+      for (int d = 1; d < 16; d <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
 #pragma unroll
-      for (int j = 0; j < kChunks; ++j) {
-        const float x0 = param_step(e[j].x), x1 = param_low(e[j].x), x2 = param_step(e[j].y), x3 = param_low(e[j].y);
-        const float x4 = param_step(e[j].z), x5 = param_low(e[j].z), x6 = param_step(e[j].w), x7 = param_low(e[j].w);
-        q[n][j][0] = pack_fp16x2(x0 * up, x4 * up);                    // the codes of nibbles 1 and 3 count 16-fold
-        q[n][j][1] = pack_fp16x2(x1 * up16, x5 * up16);
-        q[n][j][2] = pack_fp16x2(x2 * up, x6 * up);
-        q[n][j][3] = pack_fp16x2(x3 * up16, x7 * up16);
-        sums[j / kGroupChunks] += ((x0 + x1) + (x2 + x3)) + ((x4 + x5) + (x6 + x7));
+      for (int d = 1; d < kGroup / kEach; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+      const int up = most == 0 ? 0 : min(max(7 - ((int)(most >> 7) - 127), -100), 100);
+      const float scale = __int_as_float((127 + up) << 23);
+      if (part % (kGroup / kEach) == 0) ctl->q_sum[part * kEach / kGroup][r] = sum * __int_as_float((127 + up - 9) << 23);
+      if (part == 0) {
+        ctl->back[r] = __int_as_float((127 + 9 - up) << 23);             // undoes the scale and the 2^-9 of the codes
+        ctl->minus[r] = 0.0f;
+        ctl->top[r] = ctl->shift[r] = -INFINITY;
+        ctl->limit[r] = r < sg.rows ? -INFINITY : INFINITY;
+        ctl->unit[r] = r < sg.rows ? 0.0f : INFINITY;
+        const int pos = base_pos + row / a.ratio;
+        ctl->high[r] = r < sg.rows ? pos + 1 : 0;
+        ctl->low[r] = a.window > 0 ? pos + 1 - a.window : 0;
       }
-      const float down = __int_as_float((127 + 24 - k2) << 23);
+      // two rows of the operand: the leading e4m3 numbers, and 16 times what they leave
+      const int lead = rb * 16 + tid / 16, rest = lead + 8;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) back[n][i] = __shfl_sync(0xFFFFFFFFu, down, 8 * c + 4 * i);
-#pragma unroll
-      for (int k = 0; k < G; ++k) {
-        sums[k] += __shfl_xor_sync(0xFFFFFFFFu, sums[k], 1);
-        sums[k] += __shfl_xor_sync(0xFFFFFFFFu, sums[k], 2);
-        sums[k] *= __int_as_float((127 - 24 + k2) << 23);              // in the units of the products
-        q_sum[n][k][0] = __shfl_sync(0xFFFFFFFFu, sums[k], 8 * c);     // of rows 2 c, 2 c + 1
-        q_sum[n][k][1] = __shfl_sync(0xFFFFFFFFu, sums[k], 8 * c + 4);
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int rr = n * 8 + 2 * c + i;
-        const int pos = base_pos + (sg.first_row + rr) / a.ratio;
-        row_high[n][i] = rr < sg.rows ? pos + 1 : 0;
-        row_low[n][i] = a.window > 0 ? pos + 1 - a.window : 0;
+      for (int j = 0; j < kEach / 2; j += 2) {                           // four elements: two even, two odd
+        const float x0 = param_step(e[j]) * scale, x1 = param_low(e[j]) * scale, x2 = param_step(e[j + 1]) * scale, x3 = param_low(e[j + 1]) * scale;
+        const uint32_t even = to_e4m3x2(x0, x2), odd = to_e4m3x2(x1, x3);
+        const float2 fe = from_e4m3x2(even), fo = from_e4m3x2(odd);
+        const uint32_t even2 = to_e4m3x2((x0 - fe.x) * 16.0f, (x2 - fe.y) * 16.0f), odd2 = to_e4m3x2((x1 - fo.x) * 16.0f, (x3 - fo.y) * 16.0f);
+        const int d = part * kEach + 2 * j, in = d % 32;                 // of the head, of its chunk
+        const uint32_t at = queries + (d / 128) * (NB * 2048);
+        const int piece = (d % 128) / 32 * 2;
+        auto put = [&](int n, int half, uint32_t two) {
+          const uint32_t to = at + n * 128 + (((piece + half) ^ (n & 7)) << 4) + in / 2;
+          asm volatile("st.shared.u16 [%0], %1;" ::"r"(to), "h"((uint16_t)two) : "memory");
+        };
+        put(lead, 0, even);
+        put(lead, 1, odd);
+        put(rest, 0, even2);
+        put(rest, 1, odd2);
       }
     }
+    if (tid == 0) ctl->least_unit = 0.0f;
     // every row of the tile sees the keys [all_low, all_high)
     const int all_high = base_pos + sg.first_row / a.ratio + 1;
     const int all_low = a.window > 0 ? base_pos + (sg.first_row + sg.rows - 1) / a.ratio + 1 - a.window : 0;
 
-    float o[NT][kChunks * 2][4] = {};
-    float low_sum[NT][G][2] = {};                                      // sum of p (m + 8 s)
-    // Weights are p = 2^(z - shift), z the score in log2: with the shift at the largest score (as of its last raise) plus
-    // log2(unit) - 6, unit a power of two above all steps that the column has counted, p s lies below 2^14, in fp16's
-    // range, and is exact to 2^-12 of itself from the largest (about 2^6) down to 2^-20 of it, to 2^-31 of it below.
-    float total[NT][2] = {}, shift[NT][2], minus[NT][2] = {}, limit[NT][2], unit[NT][2] = {}, most[NT][2];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) shift[n][0] = shift[n][1] = limit[n][0] = limit[n][1] = -INFINITY;
+    float total[kRows] = {}, low_sum[G][kRows] = {};                     // of this thread's tokens
+    float out[S::kBlocks][kRows] = {};                                   // of this thread's element of the head, in units of codes
+    int since = 0;                                                       // tiles in the integer sums
 
-    int slot = 0;
-    for (int i = 0; i < stages; ++i) {
-      copies_wait<S::kStages - 1>();
-      __syncwarp();
-      const int t0 = first_token + i * S::kUnit;
-      const bool edge = t0 < all_low || t0 + S::kStageTokens > all_high;
-      const uint32_t kc = ring + slot * 2 * S::kCodeBytes, vc = kc + S::kCodeBytes;
-      const uint32_t kp = param_ring + slot * 2 * S::kParamBytes, vp = kp + S::kParamBytes;
-
-      // ---- scores, in units of log2 divided by `back`
-      float z[S::kSteps][NT][4], acc[S::kSteps][NT][4];
-      constexpr int kPairChunks = kChunks < 2 ? 1 : 2;                 // one ldmatrix
+    // Adds the integer sums to the registers.  A warp's 32 lanes are the elements 32 warp .. of a block: one group.
+    auto empty_sums = [&] {
 #pragma unroll
-      for (int j0 = 0; j0 < kChunks; j0 += kPairChunks) {
-        uint32_t words[S::kSteps][4];
+      for (int k = 0; k < S::kBlocks; ++k)
 #pragma unroll
-        for (int st = 0; st < S::kSteps; ++st)
-          ldmatrix_x4(words[st], kc + ((st * 8 * D + (mat_offset ^ (j0 * 16))) ^ (D == 64 && (st & 1) ? 64u : 0u)));
+        for (int rb = 0; rb < NB; ++rb) {
+          const int part = (warp * 32 * S::kBlockGroups / (D < 128 ? 64 : 128)) % S::kBlockGroups * NB + rb;
+          const uint32_t at = sum_tmem + own_lanes + k * S::kWeightCols;
+          uint32_t low16[16], high8[8];
+          ptx::tmem_ld_32x16(at + part * 16, low16);
+          ptx::tmem_ld_32x8(at + 16 * S::kParts + part * 8, high8);
+          ptx::tmem_ld_wait();
 #pragma unroll
-        for (int h = 0; h < kPairChunks; ++h) {
-          // codes as fp16 numbers below the normal range: q 2^-24 in the low nibble of a byte, q 2^-20 in the high one
-          const int j = j0 + h, k = j / kGroupChunks;
-#pragma unroll
-          for (int st = 0; st < S::kSteps; ++st) {
-            if (j % kGroupChunks == 0)
-#pragma unroll
-              for (int n = 0; n < NT; ++n) acc[st][n][0] = acc[st][n][1] = acc[st][n][2] = acc[st][n][3] = 0.0f;
-            const uint32_t wa = words[st][2 * h], wb = words[st][2 * h + 1];
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-              mma_fp16(acc[st][n], wa & 0x000F000Fu, wb & 0x000F000Fu, wa & 0x00F000F0u, wb & 0x00F000F0u, q[n][j][0], q[n][j][1]);
-          }
-#pragma unroll
-          for (int st = 0; st < S::kSteps; ++st) {
-            const uint32_t xa = words[st][2 * h] >> 8, xb = words[st][2 * h + 1] >> 8;
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-              mma_fp16(acc[st][n], xa & 0x000F000Fu, xb & 0x000F000Fu, xa & 0x00F000F0u, xb & 0x00F000F0u, q[n][j][2], q[n][j][3]);
-          }
-          if (j % kGroupChunks == kGroupChunks - 1) {
-#pragma unroll
-            for (int st = 0; st < S::kSteps; ++st) {
-              const uint32_t pa = ptx::lds_32(kp + ((st * 16 + g) * G + k) * 4), pb = ptx::lds_32(kp + ((st * 16 + 8 + g) * G + k) * 4);
-              const float sa = param_step(pa) * a.scale_log2, sb = param_step(pb) * a.scale_log2;
-              const float ma = param_low(pa) * a.scale_log2, mb = param_low(pb) * a.scale_log2;
-#pragma unroll
-              for (int n = 0; n < NT; ++n) {
-                float* zz = z[st][n];
-                zz[0] = fmaf(acc[st][n][0], sa, k == 0 ? q_sum[n][k][0] * ma : fmaf(q_sum[n][k][0], ma, zz[0]));
-                zz[1] = fmaf(acc[st][n][1], sa, k == 0 ? q_sum[n][k][1] * ma : fmaf(q_sum[n][k][1], ma, zz[1]));
-                zz[2] = fmaf(acc[st][n][2], sb, k == 0 ? q_sum[n][k][0] * mb : fmaf(q_sum[n][k][0], mb, zz[2]));
-                zz[3] = fmaf(acc[st][n][3], sb, k == 0 ? q_sum[n][k][1] * mb : fmaf(q_sum[n][k][1], mb, zz[3]));
-              }
-            }
-          }
+          for (int r = 0; r < 8; ++r)
+            out[k][rb * 8 + r] += fmaf((float)(int)high8[r], 65536.0f, fmaf((float)(int)low16[8 + r], 256.0f, (float)(int)low16[r]));
         }
-      }
-      if (edge) {
-#pragma unroll
-        for (int st = 0; st < S::kSteps; ++st) {
-          const int ta = t0 + st * 16 + g, tb = ta + 8;
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              if (ta < row_low[n][k] || ta >= row_high[n][k]) z[st][n][k] = -INFINITY;
-              if (tb < row_low[n][k] || tb >= row_high[n][k]) z[st][n][2 + k] = -INFINITY;
-            }
-        }
-      }
+      since = 0;
+    };
 
-      // ---- steps and minima of the values, and the largest step that each column counts
-      uint32_t vpar[S::kSteps][2][G];
-      float widest[NT][2];
-      {
-        float all = 0.0f;
+    for (int i = 0; i < tiles; ++i) {
+      const int t0 = first_token + i * S::kUnit, token = t0 + tid;
+      const bool edge = t0 < all_low || t0 + S::kUnit > all_high;
 #pragma unroll
-        for (int st = 0; st < S::kSteps; ++st)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            load_params<G>(vpar[st][h], vp + (st * 16 + 8 * h + g) * G * 4);
-#pragma unroll
-            for (int e = 0; e < G; ++e) all = fmaxf(all, param_step(vpar[st][h][e]));
-          }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) widest[n][0] = widest[n][1] = all;
+      for (int e = 0; e < G; ++e) {
+        key_params[e] = next_key_params[e];
+        value_params[e] = next_value_params[e];
       }
-      if (edge) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            float all = 0.0f;
-#pragma unroll
-            for (int st = 0; st < S::kSteps; ++st)
-#pragma unroll
-              for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < G; ++e)
-                  all = fmaxf(all, z[st][n][2 * h + k] == -INFINITY ? 0.0f : param_step(vpar[st][h][e]));
-            widest[n][k] = all;
-          }
+      spread(key_codes, keys);
+      if (i + 1 < tiles) {
+        find(i + 1);
+        fetch(key_codes, v.kq, i + 1);
+        fetch_params(next_key_params, v.kp, i + 1);
+        fetch_params(next_value_params, v.vp, i + 1);
       }
-
-      // ---- the columns' exponents are raised only when a score is 2^kLazy above the last maximum or a step above the last
-      // unit (or nothing has been seen)
-      bool raise = false;
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          float m = z[0][n][k];
-#pragma unroll
-          for (int st = 0; st < S::kSteps; ++st) m = fmaxf(m, fmaxf(z[st][n][k], z[st][n][2 + k]));
-          most[n][k] = m;
-          raise |= m * back[n][k] > limit[n][k] || widest[n][k] > unit[n][k];
-        }
-      if (__any_sync(0xFFFFFFFFu, raise)) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            float m = most[n][k], u = widest[n][k];
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1) {
-              m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-              u = fmaxf(u, __shfl_xor_sync(0xFFFFFFFFu, u, d));
-            }
-            m = fmaxf(m * back[n][k], limit[n][k] - kLazy);
-            if (u > unit[n][k])                                        // the next power of two
-              unit[n][k] = __uint_as_float((uint32_t)min(max((int)(__float_as_uint(u) >> 23) + 1, 127 - 60), 254) << 23);
-            const float to = m == -INFINITY ? -INFINITY : m + (float)((int)(__float_as_uint(unit[n][k]) >> 23) - 127 - 6);
-            const float f = to == -INFINITY ? 1.0f : exp2_approx(shift[n][k] - to);
-            limit[n][k] = m + kLazy;
-            shift[n][k] = to;
-            minus[n][k] = to == -INFINITY ? 0.0f : -to;
-            total[n][k] *= f;
-#pragma unroll
-            for (int e = 0; e < G; ++e) low_sum[n][e][k] *= f;
-#pragma unroll
-            for (int u2 = 0; u2 < kChunks * 2; ++u2) {
-              o[n][u2][k] *= f;
-              o[n][u2][2 + k] *= f;
-            }
-          }
-      }
-
-      // ---- softmax weights and the values
-#pragma unroll
-      for (int st = 0; st < S::kSteps; ++st) {
-        uint32_t ps[NT][G][2];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          float p[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) p[k] = exp2_approx(fmaf(z[st][n][k], back[n][k & 1], minus[n][k & 1]));
-          total[n][0] += p[0] + p[2];
-          total[n][1] += p[1] + p[3];
+      ptx::fence_proxy_async_smem();
+      ptx::tc_fence_before();
+      __syncthreads();
+      if (warp == 0) {
+        ptx::tc_fence_after();
+        if (ptx::elect_one()) {
 #pragma unroll
           for (int e = 0; e < G; ++e) {
-            const float sa = param_step(vpar[st][0][e]), sb = param_step(vpar[st][1][e]);
-            const float ma = fmaf(8.0f, sa, param_low(vpar[st][0][e])), mb = fmaf(8.0f, sb, param_low(vpar[st][1][e]));
-            float wa0 = p[0] * sa, wa1 = p[1] * sa, wb0 = p[2] * sb, wb1 = p[3] * sb;
-            if (!edge) {
-              low_sum[n][e][0] = fmaf(p[0], ma, fmaf(p[2], mb, low_sum[n][e][0]));
-              low_sum[n][e][1] = fmaf(p[1], ma, fmaf(p[3], mb, low_sum[n][e][1]));
-            } else {                                                   // what a row does not see counts nothing, NaN or not
-              const bool ha0 = z[st][n][0] == -INFINITY, ha1 = z[st][n][1] == -INFINITY;
-              const bool hb0 = z[st][n][2] == -INFINITY, hb1 = z[st][n][3] == -INFINITY;
-              wa0 = ha0 ? 0.0f : wa0; wa1 = ha1 ? 0.0f : wa1;
-              wb0 = hb0 ? 0.0f : wb0; wb1 = hb1 ? 0.0f : wb1;
-              low_sum[n][e][0] += (ha0 ? 0.0f : p[0] * ma) + (hb0 ? 0.0f : p[2] * mb);
-              low_sum[n][e][1] += (ha1 ? 0.0f : p[1] * ma) + (hb1 ? 0.0f : p[3] * mb);
-            }
-            ps[n][e][0] = transpose_8x8(pack_fp16x2(wa0, wa1));
-            ps[n][e][1] = transpose_8x8(pack_fp16x2(wb0, wb1));
+            const int at = e % S::kBlockGroups * kGroup, block = e / S::kBlockGroups;
+#pragma unroll
+            for (int k = 0; k < kGroup; k += 32)
+              mma_e4m3(score_tmem(e), ptx::smem_desc(keys + block * 16384 + at + k), ptx::smem_desc(queries + block * (NB * 2048) + at + k),
+                       kScoreDesc | ((uint32_t)(2 * NB) << 17), k != 0);
           }
+          ptx::mma_commit(ptx::smem_addr(&ctl->scores_done));
         }
+        __syncwarp();
+      }
+      if (i > 0) {                                                       // the last tile's values have been read
+        bounded_wait_warp(ptx::smem_addr(&ctl->sums_done), sums_phase, abort_flag, WAIT_EPI_ACC_FULL);
+        sums_phase ^= 1u;
+        if (since == 4096) {                                             // 15 * 255 * 128 * 4096 < 2^31
+          ptx::tc_fence_after();
+          empty_sums();
+        }
+      }
+      spread(value_codes, values);
+      if (i + 1 < tiles) fetch(value_codes, v.vq, i + 1);
+
+      bounded_wait_warp(ptx::smem_addr(&ctl->scores_done), scores_phase, abort_flag, WAIT_EPI_ACC_FULL);
+      scores_phase ^= 1u;
+      ptx::tc_fence_after();
+
+      // ---- this token's weights: exponents of all rows first
+      float arg[kRows];
+      float step = 0.0f;
+      bool raise = false;
 #pragma unroll
-        for (int j = 0; j < kChunks; j += 2) {
-          uint32_t r[4];
-          const uint32_t off = (st * 8 * D + (mat_offset ^ (j * 16))) ^ (D == 64 && (st & 1) ? 64u : 0u);
-          ldmatrix_x4_trans(r, vc + off);
+      for (int e = 0; e < G; ++e) {
+        const float ks = param_step(key_params[e]) * a.scale_log2, km = param_low(key_params[e]) * a.scale_log2;
+        step = fmaxf(step, param_step(value_params[e]));
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t ra = r[2 * h], rb = r[2 * h + 1], xa = ra >> 8, xb = rb >> 8;
-            const uint32_t a0 = centred_low(ra), a1 = centred_high(ra), a2 = centred_low(rb), a3 = centred_high(rb);
-            const uint32_t b0 = centred_low(xa), b1 = centred_high(xa), b2 = centred_low(xb), b3 = centred_high(xb);
+        for (int rb = 0; rb < NB; ++rb) {
+          uint32_t acc[16];
+          ptx::tmem_ld_32x16(score_tmem(e) + own_lanes + rb * 16, acc);
+          ptx::tmem_ld_wait();
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              const uint32_t* p = ps[n][(j + h) / kGroupChunks];
-              mma_fp16(o[n][2 * (j + h)], a0, a1, a2, a3, p[0], p[1]);
-              mma_fp16(o[n][2 * (j + h) + 1], b0, b1, b2, b3, p[0], p[1]);
+          for (int q4 = 0; q4 < 8; q4 += 4) {
+            const float4 qs = *reinterpret_cast<const float4*>(&ctl->q_sum[e][rb * 8 + q4]);
+            const float qv[4] = {qs.x, qs.y, qs.z, qs.w};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float z = fmaf(__uint_as_float(acc[8 + q4 + r]), 0.0625f, __uint_as_float(acc[q4 + r]));
+              float& to = arg[rb * 8 + q4 + r];
+              to = fmaf(z, ks, e == 0 ? qv[r] * km : fmaf(qv[r], km, to));
             }
           }
         }
       }
-      __syncwarp();                                                    // the stage has been read
-      fetch(i + S::kStages, slot);
-      slot = slot + 1 == S::kStages ? 0 : slot + 1;
+#pragma unroll
+      for (int r0 = 0; r0 < kRows; r0 += 4) {
+        const float4 bk = *reinterpret_cast<const float4*>(&ctl->back[r0]), mn = *reinterpret_cast<const float4*>(&ctl->minus[r0]);
+        const float bv[4] = {bk.x, bk.y, bk.z, bk.w}, mv[4] = {mn.x, mn.y, mn.z, mn.w};
+#pragma unroll
+        for (int r = 0; r < 4; ++r) arg[r0 + r] = fmaf(arg[r0 + r], bv[r], mv[r]);
+        if (edge) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const bool seen = token >= ctl->low[r0 + r] && token < ctl->high[r0 + r];
+            arg[r0 + r] = seen ? arg[r0 + r] : -INFINITY;
+            raise |= seen && step > ctl->unit[r0 + r];
+          }
+        }
+        const float4 lm = *reinterpret_cast<const float4*>(&ctl->limit[r0]);
+        raise |= arg[r0] > lm.x || arg[r0 + 1] > lm.y || arg[r0 + 2] > lm.z || arg[r0 + 3] > lm.w;
+      }
+      if (!edge) raise |= step > ctl->least_unit;
+
+      // Weights into the second product's operand, as three bytes each.
+      float p[kRows];
+      auto put_weights = [&] {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) p[r] = exp2_approx(arg[r]);
+#pragma unroll
+        for (int e = 0; e < G; ++e) {
+          const float s = param_step(value_params[e]);
+          const int block = e / S::kBlockGroups;
+#pragma unroll
+          for (int rb = 0; rb < NB; ++rb) {
+            uint32_t y[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+              y[r] = __float_as_uint(fmaf(p[rb * 8 + r], s, 8388608.0f));            // 2^23: the low 23 bits are round(p s)
+              if (edge) y[r] = arg[rb * 8 + r] == -INFINITY ? 0u : y[r];             // unseen: zero, whatever the step
+            }
+            uint32_t low[2], mid[2], high[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t t01 = __byte_perm(y[4 * h], y[4 * h + 1], 0x5140), t23 = __byte_perm(y[4 * h + 2], y[4 * h + 3], 0x5140);
+              low[h] = __byte_perm(t01, t23, 0x5410);
+              mid[h] = __byte_perm(t01, t23, 0x7632);
+              high[h] = __byte_perm(__byte_perm(y[4 * h], y[4 * h + 1], 0x0062), __byte_perm(y[4 * h + 2], y[4 * h + 3], 0x0062), 0x5410);
+            }
+            const int part = e % S::kBlockGroups * NB + rb;
+            const uint32_t at = weights + block * (S::kWeightUnits * 2048) + tid * 16;
+            ptx::sts_128(at + part * 2048, low[0], low[1], mid[0], mid[1]);
+            if (S::kParts == 1) ptx::sts_128(at + 2048, high[0], high[1], 0u, 0u);
+            else asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at + (S::kParts + part / 2) * 2048 + (part & 1) * 8), "r"(high[0]), "r"(high[1]) : "memory");
+          }
+        }
+      };
+      // The weights are written before it is known whether some thread wants its row's exponent raised, which is rare.
+      put_weights();
+      ptx::fence_proxy_async_smem();
+      ptx::tc_fence_before();
+      if (__syncthreads_or(raise)) {
+        // largest exponent and step that each row sees in the tile
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+          float m = arg[r], u = arg[r] == -INFINITY ? 0.0f : step;
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) {
+            m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+            u = fmaxf(u, __shfl_xor_sync(0xFFFFFFFFu, u, d));
+          }
+          if (lane == 0) {
+            ctl->warp_top[warp][r] = m;
+            ctl->warp_step[warp][r] = u;
+          }
+        }
+        __syncthreads();
+        if (warp == 0) {
+          float unit = INFINITY;
+          if (lane < sg.rows) {
+            const int r = lane;
+            const float m = fmaxf(fmaxf(ctl->warp_top[0][r], ctl->warp_top[1][r]), fmaxf(ctl->warp_top[2][r], ctl->warp_top[3][r]));
+            const float u = fmaxf(fmaxf(ctl->warp_step[0][r], ctl->warp_step[1][r]), fmaxf(ctl->warp_step[2][r], ctl->warp_step[3][r]));
+            unit = ctl->unit[r];
+            float factor = 1.0f, delta = 0.0f;
+            if (m > -INFINITY) {
+              if (u > unit || unit == 0.0f) unit = __uint_as_float((uint32_t)min(max((int)(__float_as_uint(u) >> 23) + 1, 127 - 60), 254) << 23);
+              const float one = kOne - (float)((int)(__float_as_uint(unit) >> 23) - 127);       // log2 of the weight of the maximum
+              const float top = fmaxf(ctl->top[r], m - ctl->minus[r]), shift = top - one;
+              factor = ctl->top[r] == -INFINITY ? 0.0f : exp2_approx(ctl->shift[r] - shift);
+              delta = -shift - ctl->minus[r];
+              ctl->top[r] = top;
+              ctl->shift[r] = shift;
+              ctl->minus[r] = -shift;
+              ctl->limit[r] = one + kLazy;
+              ctl->unit[r] = unit;
+            }
+            ctl->factor[r] = factor;
+            ctl->delta[r] = delta;
+          }
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) unit = fminf(unit, __shfl_xor_sync(0xFFFFFFFFu, unit, d));
+          if (lane == 0) ctl->least_unit = unit;
+        }
+        __syncthreads();
+        if (since > 0) {
+          ptx::tc_fence_after();
+          empty_sums();
+        }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+          const bool own = r < sg.rows;
+          const float f = own ? ctl->factor[r] : 1.0f;
+          arg[r] += own ? ctl->delta[r] : 0.0f;
+          total[r] *= f;
+#pragma unroll
+          for (int e = 0; e < G; ++e) low_sum[e][r] *= f;
+#pragma unroll
+          for (int k = 0; k < S::kBlocks; ++k) out[k][r] *= f;
+        }
+        put_weights();
+        ptx::fence_proxy_async_smem();
+        ptx::tc_fence_before();
+        __syncthreads();
+      }
+      if (warp == 0) {
+        ptx::tc_fence_after();
+        if (ptx::elect_one()) {
+#pragma unroll
+          for (int k = 0; k < S::kBlocks; ++k)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)                                  // 32 tokens each
+              mma_u8(sum_tmem + k * S::kWeightCols, ptx::smem_desc(values + k * 16384 + t * 4096),
+                     weight_desc(weights + k * (S::kWeightUnits * 2048) + t * 512), kSumDesc | ((uint32_t)(S::kWeightCols / 8) << 17),
+                     since > 0 || t > 0);
+          ptx::mma_commit(ptx::smem_addr(&ctl->sums_done));
+        }
+        __syncwarp();
+      }
+      ++since;
+      // what a row does not see counts nothing, NaN or not; a step that is not finite makes its group NaN
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) total[r] += p[r];
+#pragma unroll
+      for (int e = 0; e < G; ++e) {
+        const float m = fmaf(0.0f, param_step(value_params[e]), param_low(value_params[e]));
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+          if (edge) low_sum[e][r] += arg[r] == -INFINITY ? 0.0f : p[r] * m;
+          else low_sum[e][r] = fmaf(p[r], m, low_sum[e][r]);
+        }
+      }
+    }
+    if (tiles > 0) {
+      bounded_wait_warp(ptx::smem_addr(&ctl->sums_done), sums_phase, abort_flag, WAIT_EPI_ACC_FULL);
+      sums_phase ^= 1u;
+      ptx::tc_fence_after();
+      empty_sums();
     }
 
-    // ---- the four warps of the segment meet
+    // ---- sums over the tokens: every thread's values side by side, then a warp per row of them
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int r = 0; r < kRows; ++r) {
+      meet[r * 128 + tid] = total[r];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) {
-          total[n][k] += __shfl_xor_sync(0xFFFFFFFFu, total[n][k], d);
-#pragma unroll
-          for (int e = 0; e < G; ++e) low_sum[n][e][k] += __shfl_xor_sync(0xFFFFFFFFu, low_sum[n][e][k], d);
-        }
-        if (g == 0) ctl->top[warp][n * 8 + 2 * c + k] = shift[n][k];
-      }
+      for (int e = 0; e < G; ++e) meet[((1 + e) * kRows + r) * 128 + tid] = low_sum[e][r];
+    }
     __syncthreads();
-    {
-      float* mine = merge + warp * (S::kRingBytes / 4);
+    for (int n = warp; n < (1 + G) * kRows; n += kWarps) {
+      const float4 y = *reinterpret_cast<const float4*>(meet + n * 128 + lane * 4);
+      float sum = (y.x + y.y) + (y.z + y.w);
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+      if (lane == 0) ctl->sums[n / kRows][n % kRows] = sum;
+    }
+    __syncthreads();
+    // elements to their places: byte tid of a row is element 32 (tid / 32) + 2 (tid % 16) + (tid / 16 % 2)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int r = n * 8 + 2 * c + k;
-          const float m = fmaxf(fmaxf(ctl->top[0][r], ctl->top[1][r]), fmaxf(ctl->top[2][r], ctl->top[3][r]));
-          const float f = m == -INFINITY ? 0.0f : exp2_approx(shift[n][k] - m);
-          const float even = f * 0x1p24f, odd = f * 0x1p20f;           // the units of the codes
-          if (g == 0) ctl->sum[warp][r] = total[n][k] * f;
+    for (int k = 0; k < S::kBlocks; ++k) {
+      const int d = k * 128 + (tid & ~31) + 2 * (tid & 15) + ((tid >> 4) & 1);
+      if (d < D) {
 #pragma unroll
-          for (int j = 0; j < kChunks; ++j) {
-            const float low = low_sum[n][j / kGroupChunks][k] * f;
-            // elements 32 j + 4 g .. + 3 of row r; the 16-byte piece is turned by the row against bank conflicts
-            const float4 e = make_float4(fmaf(o[n][2 * j][k], even, low), fmaf(o[n][2 * j][2 + k], odd, low),
-                                         fmaf(o[n][2 * j + 1][k], even, low), fmaf(o[n][2 * j + 1][2 + k], odd, low));
-            *reinterpret_cast<float4*>(mine + r * D + (((j * 8 + g) ^ (r & 7)) << 2)) = e;
-          }
-          if (g == 0 && warp == 0) ctl->most[r] = m;
-        }
+        for (int r = 0; r < kRows; ++r) meet[r * D + d] = out[k][r] + ctl->sums[1 + d / kGroup][r];
+      }
     }
     __syncthreads();
     // a piece that starts inside the segment goes to the worker's first slot, one that ends inside it to the second
     const int64_t part_slot = 2 * (int64_t)blockIdx.x + (u0 == 0 ? 1 : 0);
     for (int r = warp; r < sg.rows; r += kWarps) {
-      const float m = ctl->most[r], l = (ctl->sum[0][r] + ctl->sum[1][r]) + (ctl->sum[2][r] + ctl->sum[3][r]);
+      const float m = ctl->shift[r], l = ctl->sums[0][r];
       const int row = sg.first_row + r;
-      const int64_t token = w.rows.first + row / a.ratio;
+      const int64_t out_row = w.rows.first + row / a.ratio;
       const int q_head = head * a.ratio + row % a.ratio;
       const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
-      eqat_bf16* out = a.O + token * a.o_pitch + (int64_t)q_head * D;
-      float* part = whole ? nullptr : a.partial + (part_slot * S::kRows + r) * (D + 4);
+      eqat_bf16* to = a.O + out_row * a.o_pitch + (int64_t)q_head * D;
+      float* part = whole ? nullptr : a.partial + (part_slot * kRows + r) * (D + 4);
 #pragma unroll
       for (int p = lane; p < D / 4; p += 32) {
-        float4 e = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-        for (int k = 0; k < kWarps; ++k) {
-          const float4 y = *reinterpret_cast<const float4*>(merge + k * (S::kRingBytes / 4) + r * D + ((p ^ (r & 7)) << 2));
-          e.x += y.x; e.y += y.y; e.z += y.z; e.w += y.w;
-        }
-        if (whole) *reinterpret_cast<uint2*>(out + p * 4) = make_uint2(pack_bf16x2(e.x * inv, e.y * inv), pack_bf16x2(e.z * inv, e.w * inv));
+        const float4 e = *reinterpret_cast<const float4*>(meet + r * D + p * 4);
+        if (whole) *reinterpret_cast<uint2*>(to + p * 4) = make_uint2(pack_bf16x2(e.x * inv, e.y * inv), pack_bf16x2(e.z * inv, e.w * inv));
         else *reinterpret_cast<float4*>(part + p * 4) = e;
       }
       if (lane == 0) {
         if (!whole) *reinterpret_cast<float2*>(part + D) = make_float2(m, l);
         else if (a.lse != nullptr)
-          a.lse[token * a.q_heads + q_head] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+          a.lse[out_row * a.q_heads + q_head] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
       }
     }
-    __syncthreads();                                                   // the rings may be filled again
+    __syncthreads();                                                     // the operands may be written again
     x += u1 - u0;
   }
   ptx::grid_dependents_launch();
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(ctl->tmem[0], S::kAlloc);
+    if (S::kTwoParts) ptx::tmem_dealloc(ctl->tmem[1], 32);
+  }
 }
 
 // Joins the segments that workers share: the CTA of the first worker boundary inside a segment adds up the pieces, in the
@@ -713,25 +803,36 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(const Attentio
 }
 
 // ------------------------------------------------------------------ host side
-int row_tiles(const eqat_cache_desc& d, const eqat_attention_desc& a) {
-  return (int64_t)a.max_new * (a.q_heads / d.kv_heads) <= 8 ? 1 : 2;
+// Blocks of eight query rows that a tile of the cache is read for: as many as the longest sequence's rows fill, as far as
+// accumulators and a thread's sums have room (32 rows x groups).
+int row_blocks(const eqat_cache_desc& d, const eqat_attention_desc& a) {
+  const int64_t rows = (int64_t)a.max_new * (a.q_heads / d.kv_heads);
+  const int groups = d.head_dim / d.group, most = d.head_dim == 256 && groups == 2 ? 1 : groups >= 4 ? 1 : groups == 2 ? 2 : 4;
+  int nb = 1;
+  while (nb < most && 8 * nb < rows) nb *= 2;
+  return nb;
 }
 
 template <typename F>
-int with_shape(const eqat_cache_desc& d, int nt, F&& f) {
+int with_shape(const eqat_cache_desc& d, int nb, F&& f) {
   const int g = d.head_dim / d.group;
-#define EQAT_SHAPE(DD, GG)                                                        \
-  if (d.head_dim == DD && g == GG)                                                \
-    return nt == 1 ? f(std::integral_constant<int, DD>(), std::integral_constant<int, GG>(), std::integral_constant<int, 1>()) \
-                   : f(std::integral_constant<int, DD>(), std::integral_constant<int, GG>(), std::integral_constant<int, 2>());
-  EQAT_SHAPE(64, 1)
-  EQAT_SHAPE(64, 2)
-  EQAT_SHAPE(128, 1)
-  EQAT_SHAPE(128, 2)
-  EQAT_SHAPE(128, 4)
-  EQAT_SHAPE(256, 2)
-  EQAT_SHAPE(256, 4)
-  EQAT_SHAPE(256, 8)
+#define EQAT_SHAPE(DD, GG, NN)                          \
+  if (d.head_dim == DD && g == GG && nb == NN)          \
+    return f(std::integral_constant<int, DD>(), std::integral_constant<int, GG>(), std::integral_constant<int, NN>());
+  EQAT_SHAPE(64, 1, 1)
+  EQAT_SHAPE(64, 1, 2)
+  EQAT_SHAPE(64, 1, 4)
+  EQAT_SHAPE(64, 2, 1)
+  EQAT_SHAPE(64, 2, 2)
+  EQAT_SHAPE(128, 1, 1)
+  EQAT_SHAPE(128, 1, 2)
+  EQAT_SHAPE(128, 1, 4)
+  EQAT_SHAPE(128, 2, 1)
+  EQAT_SHAPE(128, 2, 2)
+  EQAT_SHAPE(128, 4, 1)
+  EQAT_SHAPE(256, 2, 1)
+  EQAT_SHAPE(256, 4, 1)
+  EQAT_SHAPE(256, 8, 1)
 #undef EQAT_SHAPE
   return EQAT_ERR_UNSUPPORTED;
 }
@@ -767,7 +868,7 @@ int workers_of(const eqat_cache_desc& d, const eqat_attention_desc& a, int sms) 
 size_t cache_attention_workspace(const eqat_cache_desc& d, const eqat_attention_desc& a) {
   const int sms = sm_count();
   size_t bytes = (size_t)-1;
-  with_shape(d, row_tiles(d, a), [&](auto D, auto G, auto NT) {
+  with_shape(d, row_blocks(d, a), [&](auto D, auto G, auto NT) {
     using S = Shape<decltype(D)::value, decltype(G)::value, decltype(NT)::value>;
     const int w = workers_of<S>(d, a, sms > 0 ? sms : 148);
     bytes = w > 1 ? (size_t)2 * w * S::kRows * (decltype(D)::value + 4) * sizeof(float) : 0;
@@ -780,7 +881,7 @@ int launch_cache_attention(const eqat_cache_desc& d, const eqat_attention_desc& 
                            const CacheView& view, eqat_bf16* O, int64_t o_pitch, float* lse, void* workspace, cudaStream_t st) {
   const int sms = sm_count();
   if (sms <= 0) return EQAT_ERR_CUDA;
-  return with_shape(d, row_tiles(d, at), [&](auto DD, auto GG, auto NN) {
+  return with_shape(d, row_blocks(d, at), [&](auto DD, auto GG, auto NN) {
     constexpr int D = decltype(DD)::value, G = decltype(GG)::value, NT = decltype(NN)::value;
     using S = Shape<D, G, NT>;
     AttentionArgs a{};
@@ -807,5 +908,8 @@ int launch_cache_attention(const eqat_cache_desc& d, const eqat_attention_desc& 
     return launch_overlapped(attention_join_kernel<D, G, NT>, dim3(workers - 1, S::kRows), dim3(kThreads), 0, st, a, workers);
   });
 }
+
+int launch_wait_expiry_attention(cudaStream_t st) { return launch_wait_expiry(st); }
+int read_attention_status(int* status, int* detail) { return read_wait_status(status, detail); }
 
 }  // namespace eqat

@@ -71,4 +71,7 @@ size_t cache_attention_workspace(const eqat_cache_desc& d, const eqat_attention_
 int launch_cache_attention(const eqat_cache_desc& d, const eqat_attention_desc& a, const eqat_bf16* Q, int64_t q_pitch,
                            const CacheView& view, eqat_bf16* O, int64_t o_pitch, float* lse, void* workspace, cudaStream_t st);
 
+int launch_wait_expiry_attention(cudaStream_t st);
+int read_attention_status(int* status, int* detail);
+
 }  // namespace eqat

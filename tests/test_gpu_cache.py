@@ -402,6 +402,12 @@ def test_streams_and_graphs(eqat):
     assert eqat.device_status() == (0, 0)
 
 
+def test_the_wait_that_runs_out_is_reported(eqat):
+    assert eqat.device_status() == (0, 0)
+    eqat.eqat_selftest_wait_expiry(5)
+    assert eqat.device_status()[0] == eqat.EQAT_ERR_TIMEOUT and eqat.device_status() == (0, 0)
+
+
 def test_a_decoding_block(eqat):
     """Prompt and decoding steps of a small attention block on packed weights: projection, cache, attention, projection, each
     on what the call before has left on the device, against the same steps in 64 bits."""
