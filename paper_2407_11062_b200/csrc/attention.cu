@@ -33,7 +33,7 @@ namespace eqat {
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32;
+constexpr int kThreads = kWarps * 32, kJoinThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 // Weights are p = 2^(z - shift), z the score in log2; the shift is the row's largest score (as of its last raise) plus
 // log2(unit) - kOne, unit a power of two above all steps that the row has counted, so p s < 2^23 as long as no score exceeds
@@ -73,13 +73,20 @@ struct Shape {
   static_assert(kCols <= 512, "tensor memory");
 };
 
+// What a worker leaves behind for the join: its last segment, if it starts there and other workers go on with it.
+struct __align__(16) JoinRecord {
+  int first, first_row, rows, head;    // first row of the sequence, and the tile's rows as in Segment
+  int workers, unused[3];              // pieces; at most one: nothing to join
+};
+
 struct AttentionArgs {
   CacheView cache;
   const eqat_bf16* Q;
   int64_t q_pitch, o_pitch;
   eqat_bf16* O;
   float* lse;
-  float* partial;              // [2 * workers][rows of a tile][D + 2]
+  JoinRecord* records;         // [workers]
+  float* partial;              // [2 * workers][rows of a tile][D + 4]: sums, then the exponent and the sum of weights
   int q_heads, ratio, max_new, window;
   float scale_log2;            // scale * log2(e)
   uint32_t page_mul;           // n / (page_size / 16) = n * page_mul >> page_shift for n < 2^26
@@ -221,6 +228,11 @@ __device__ __forceinline__ float2 from_e4m3x2(uint32_t v) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)v));
   return __half22float2(*reinterpret_cast<const __half2*>(&r));
 }
+__device__ __forceinline__ float warp_max(float x) {
+  float r;
+  asm("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(r) : "f"(x));
+  return r;
+}
 template <int G>
 __device__ __forceinline__ void load_params(uint32_t (&r)[G], const uint32_t* p) {
   if constexpr (G == 1) {
@@ -298,6 +310,7 @@ attention_kernel(const AttentionArgs a) {
   int b = wp.sequence;
   int64_t seq_before = wp.before;
   uint32_t scores_phase = 0, sums_phase = 0;
+  if (tid == 0 && a.records != nullptr) a.records[blockIdx.x].workers = 0;
 
   while (x < x_end) {
     SequenceWork w = sequence_work<S>(a, b);
@@ -313,6 +326,8 @@ attention_kernel(const AttentionArgs a) {
     const int head = seg % v.kv_heads;
     const Segment sg = segment_of<S>(a, w, seg / v.kv_heads);
     const bool whole = u0 == 0 && u1 == w.units;
+    if (tid == 0 && u0 == 0 && !whole)                                   // the worker's last segment
+      a.records[blockIdx.x] = JoinRecord{w.rows.first, sg.first_row, sg.rows, head, (int)((x + w.units - 1) / wp.per) - (int)blockIdx.x + 1, {0, 0, 0}};
     const int first_token = sg.from + u0 * S::kUnit;
     const int tiles = first_token < sg.high ? min(u1 - u0, (sg.high - first_token + S::kUnit - 1) / S::kUnit) : 0;
 
@@ -339,8 +354,8 @@ attention_kernel(const AttentionArgs a) {
       for (int p = 0; p < 2; ++p) {
         const uint4* from = reinterpret_cast<const uint4*>(codes + (uint64_t)place[p] * (D / 2)) + lane;
 #pragma unroll
-        for (int j = 0; j < S::kLoads / 2; ++j)
-          to[p * (S::kLoads / 2) + j] = token + 16 * p < sg.high ? ptx::ld_global(from + 32 * j) : make_uint4(0u, 0u, 0u, 0u);
+        for (int j = 0; j < S::kLoads / 2; ++j)                          // what is not fetched keeps the codes of before
+          if (token + 16 * p < sg.high) to[p * (S::kLoads / 2) + j] = ptx::ld_global(from + 32 * j);
       }
     };
     auto fetch_params = [&](uint32_t (&to)[G], const uint32_t* params, int i) {      // of this thread's token
@@ -365,7 +380,7 @@ attention_kernel(const AttentionArgs a) {
                      (c.z >> 4) & 0x0F0F0F0Fu, (c.w >> 4) & 0x0F0F0F0Fu);
       }
     };
-    uint4 key_codes[S::kLoads], value_codes[S::kLoads];
+    uint4 key_codes[S::kLoads] = {}, value_codes[S::kLoads] = {};
     uint32_t key_params[G], value_params[G], next_key_params[G], next_value_params[G];
     if (tiles > 0) {
       find(0);
@@ -538,153 +553,145 @@ attention_kernel(const AttentionArgs a) {
           }
         }
       }
+      // Some rows of an edge tile do not see some of its tokens.
+      auto weigh = [&](auto is_edge) {
+        constexpr bool kEdge = decltype(is_edge)::value;
 #pragma unroll
-      for (int r0 = 0; r0 < kRows; r0 += 4) {
-        const float4 bk = *reinterpret_cast<const float4*>(&ctl->back[r0]), mn = *reinterpret_cast<const float4*>(&ctl->minus[r0]);
-        const float bv[4] = {bk.x, bk.y, bk.z, bk.w}, mv[4] = {mn.x, mn.y, mn.z, mn.w};
-#pragma unroll
-        for (int r = 0; r < 4; ++r) arg[r0 + r] = fmaf(arg[r0 + r], bv[r], mv[r]);
-        if (edge) {
+        for (int r0 = 0; r0 < kRows; r0 += 4) {
+          const float4 bk = *reinterpret_cast<const float4*>(&ctl->back[r0]), mn = *reinterpret_cast<const float4*>(&ctl->minus[r0]);
+          const float4 lm = *reinterpret_cast<const float4*>(&ctl->limit[r0]);
+          const float bv[4] = {bk.x, bk.y, bk.z, bk.w}, mv[4] = {mn.x, mn.y, mn.z, mn.w}, lv[4] = {lm.x, lm.y, lm.z, lm.w};
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const bool seen = token >= ctl->low[r0 + r] && token < ctl->high[r0 + r];
-            arg[r0 + r] = seen ? arg[r0 + r] : -INFINITY;
-            raise |= seen && step > ctl->unit[r0 + r];
+            arg[r0 + r] = fmaf(arg[r0 + r], bv[r], mv[r]);
+            if (kEdge) {
+              const bool seen = token >= ctl->low[r0 + r] && token < ctl->high[r0 + r];
+              arg[r0 + r] = seen ? arg[r0 + r] : -INFINITY;
+              raise |= seen && step > ctl->unit[r0 + r];
+            }
+            raise |= arg[r0 + r] > lv[r];
           }
         }
-        const float4 lm = *reinterpret_cast<const float4*>(&ctl->limit[r0]);
-        raise |= arg[r0] > lm.x || arg[r0 + 1] > lm.y || arg[r0 + 2] > lm.z || arg[r0 + 3] > lm.w;
-      }
-      if (!edge) raise |= step > ctl->least_unit;
-
-      // Weights into the second product's operand, as three bytes each.
-      float p[kRows];
-      auto put_weights = [&] {
+        if (!kEdge) raise |= step > ctl->least_unit;
+        // The weights are written before it is known whether some thread wants its row's exponent raised, which is rare.
+        float p[kRows];
+        for (;;) {
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) p[r] = exp2_approx(arg[r]);
+          for (int r = 0; r < kRows; ++r) p[r] = exp2_approx(arg[r]);
+#pragma unroll
+          for (int e = 0; e < G; ++e) {
+            const float s = param_step(value_params[e]);
+            const int block = e / S::kBlockGroups;
+#pragma unroll
+            for (int rb = 0; rb < NB; ++rb) {
+              uint32_t y[8];
+#pragma unroll
+              for (int r = 0; r < 8; ++r) {
+                y[r] = __float_as_uint(fmaf(p[rb * 8 + r], s, 8388608.0f));          // 2^23: the low 23 bits are round(p s)
+                if (kEdge) y[r] = arg[rb * 8 + r] == -INFINITY ? 0u : y[r];          // unseen: zero, whatever the step
+              }
+              uint32_t low[2], mid[2], high[2];
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const uint32_t t01 = __byte_perm(y[4 * h], y[4 * h + 1], 0x5140), t23 = __byte_perm(y[4 * h + 2], y[4 * h + 3], 0x5140);
+                low[h] = __byte_perm(t01, t23, 0x5410);
+                mid[h] = __byte_perm(t01, t23, 0x7632);
+                high[h] = __byte_perm(__byte_perm(y[4 * h], y[4 * h + 1], 0x0062), __byte_perm(y[4 * h + 2], y[4 * h + 3], 0x0062), 0x5410);
+              }
+              const int part = e % S::kBlockGroups * NB + rb;
+              const uint32_t at = weights + block * (S::kWeightUnits * 2048) + tid * 16;
+              ptx::sts_128(at + part * 2048, low[0], low[1], mid[0], mid[1]);
+              if (S::kParts == 1) ptx::sts_128(at + 2048, high[0], high[1], 0u, 0u);
+              else asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at + (S::kParts + part / 2) * 2048 + (part & 1) * 8), "r"(high[0]), "r"(high[1]) : "memory");
+            }
+          }
+          ptx::fence_proxy_async_smem();
+          ptx::tc_fence_before();
+          if (!__syncthreads_or(raise)) break;
+          raise = false;
+          // largest exponent and step that each row sees in the tile
+#pragma unroll
+          for (int r = 0; r < kRows; ++r) {
+            const float m = warp_max(arg[r]), u = warp_max(arg[r] == -INFINITY ? 0.0f : step);
+            if (lane == 0) {
+              ctl->warp_top[warp][r] = m;
+              ctl->warp_step[warp][r] = u;
+            }
+          }
+          __syncthreads();
+          if (warp == 0) {
+            float unit = INFINITY;
+            if (lane < sg.rows) {
+              const int r = lane;
+              const float m = fmaxf(fmaxf(ctl->warp_top[0][r], ctl->warp_top[1][r]), fmaxf(ctl->warp_top[2][r], ctl->warp_top[3][r]));
+              const float u = fmaxf(fmaxf(ctl->warp_step[0][r], ctl->warp_step[1][r]), fmaxf(ctl->warp_step[2][r], ctl->warp_step[3][r]));
+              unit = ctl->unit[r];
+              float factor = 1.0f, delta = 0.0f;
+              if (m > -INFINITY) {
+                if (u > unit || unit == 0.0f) unit = __uint_as_float((uint32_t)min(max((int)(__float_as_uint(u) >> 23) + 1, 127 - 60), 254) << 23);
+                const float one = kOne - (float)((int)(__float_as_uint(unit) >> 23) - 127);       // log2 of the weight of the maximum
+                const float top = fmaxf(ctl->top[r], m - ctl->minus[r]), shift = top - one;
+                factor = ctl->top[r] == -INFINITY ? 0.0f : exp2_approx(ctl->shift[r] - shift);
+                delta = -shift - ctl->minus[r];
+                ctl->top[r] = top;
+                ctl->shift[r] = shift;
+                ctl->minus[r] = -shift;
+                ctl->limit[r] = one + kLazy;
+                ctl->unit[r] = unit;
+              }
+              ctl->factor[r] = factor;
+              ctl->delta[r] = delta;
+            }
+            unit = -warp_max(-unit);
+            if (lane == 0) ctl->least_unit = unit;
+          }
+          __syncthreads();
+          if (since > 0) {
+            ptx::tc_fence_after();
+            empty_sums();
+          }
+#pragma unroll
+          for (int r = 0; r < kRows; ++r) {
+            const bool own = r < sg.rows;
+            const float f = own ? ctl->factor[r] : 1.0f;
+            arg[r] += own ? ctl->delta[r] : 0.0f;
+            total[r] *= f;
+#pragma unroll
+            for (int e = 0; e < G; ++e) low_sum[e][r] *= f;
+#pragma unroll
+            for (int k = 0; k < S::kBlocks; ++k) out[k][r] *= f;
+          }
+        }
+        if (warp == 0) {
+          ptx::tc_fence_after();
+          if (ptx::elect_one()) {
+#pragma unroll
+            for (int k = 0; k < S::kBlocks; ++k)
+#pragma unroll
+              for (int t = 0; t < 4; ++t)                                  // 32 tokens each
+                mma_u8(sum_tmem + k * S::kWeightCols, ptx::smem_desc(values + k * 16384 + t * 4096),
+                       weight_desc(weights + k * (S::kWeightUnits * 2048) + t * 512), kSumDesc | ((uint32_t)(S::kWeightCols / 8) << 17),
+                       since > 0 || t > 0);
+            ptx::mma_commit(ptx::smem_addr(&ctl->sums_done));
+          }
+          __syncwarp();
+        }
+        ++since;
+        // a step that is not finite makes its group NaN
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) total[r] += p[r];
 #pragma unroll
         for (int e = 0; e < G; ++e) {
-          const float s = param_step(value_params[e]);
-          const int block = e / S::kBlockGroups;
+          const float m = fmaf(0.0f, param_step(value_params[e]), param_low(value_params[e]));
 #pragma unroll
-          for (int rb = 0; rb < NB; ++rb) {
-            uint32_t y[8];
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-              y[r] = __float_as_uint(fmaf(p[rb * 8 + r], s, 8388608.0f));            // 2^23: the low 23 bits are round(p s)
-              if (edge) y[r] = arg[rb * 8 + r] == -INFINITY ? 0u : y[r];             // unseen: zero, whatever the step
-            }
-            uint32_t low[2], mid[2], high[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const uint32_t t01 = __byte_perm(y[4 * h], y[4 * h + 1], 0x5140), t23 = __byte_perm(y[4 * h + 2], y[4 * h + 3], 0x5140);
-              low[h] = __byte_perm(t01, t23, 0x5410);
-              mid[h] = __byte_perm(t01, t23, 0x7632);
-              high[h] = __byte_perm(__byte_perm(y[4 * h], y[4 * h + 1], 0x0062), __byte_perm(y[4 * h + 2], y[4 * h + 3], 0x0062), 0x5410);
-            }
-            const int part = e % S::kBlockGroups * NB + rb;
-            const uint32_t at = weights + block * (S::kWeightUnits * 2048) + tid * 16;
-            ptx::sts_128(at + part * 2048, low[0], low[1], mid[0], mid[1]);
-            if (S::kParts == 1) ptx::sts_128(at + 2048, high[0], high[1], 0u, 0u);
-            else asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at + (S::kParts + part / 2) * 2048 + (part & 1) * 8), "r"(high[0]), "r"(high[1]) : "memory");
+          for (int r = 0; r < kRows; ++r) {
+            if (kEdge) low_sum[e][r] += arg[r] == -INFINITY ? 0.0f : p[r] * m;
+            else low_sum[e][r] = fmaf(p[r], m, low_sum[e][r]);
           }
         }
       };
-      // The weights are written before it is known whether some thread wants its row's exponent raised, which is rare.
-      put_weights();
-      ptx::fence_proxy_async_smem();
-      ptx::tc_fence_before();
-      if (__syncthreads_or(raise)) {
-        // largest exponent and step that each row sees in the tile
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-          float m = arg[r], u = arg[r] == -INFINITY ? 0.0f : step;
-#pragma unroll
-          for (int d = 1; d < 32; d <<= 1) {
-            m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-            u = fmaxf(u, __shfl_xor_sync(0xFFFFFFFFu, u, d));
-          }
-          if (lane == 0) {
-            ctl->warp_top[warp][r] = m;
-            ctl->warp_step[warp][r] = u;
-          }
-        }
-        __syncthreads();
-        if (warp == 0) {
-          float unit = INFINITY;
-          if (lane < sg.rows) {
-            const int r = lane;
-            const float m = fmaxf(fmaxf(ctl->warp_top[0][r], ctl->warp_top[1][r]), fmaxf(ctl->warp_top[2][r], ctl->warp_top[3][r]));
-            const float u = fmaxf(fmaxf(ctl->warp_step[0][r], ctl->warp_step[1][r]), fmaxf(ctl->warp_step[2][r], ctl->warp_step[3][r]));
-            unit = ctl->unit[r];
-            float factor = 1.0f, delta = 0.0f;
-            if (m > -INFINITY) {
-              if (u > unit || unit == 0.0f) unit = __uint_as_float((uint32_t)min(max((int)(__float_as_uint(u) >> 23) + 1, 127 - 60), 254) << 23);
-              const float one = kOne - (float)((int)(__float_as_uint(unit) >> 23) - 127);       // log2 of the weight of the maximum
-              const float top = fmaxf(ctl->top[r], m - ctl->minus[r]), shift = top - one;
-              factor = ctl->top[r] == -INFINITY ? 0.0f : exp2_approx(ctl->shift[r] - shift);
-              delta = -shift - ctl->minus[r];
-              ctl->top[r] = top;
-              ctl->shift[r] = shift;
-              ctl->minus[r] = -shift;
-              ctl->limit[r] = one + kLazy;
-              ctl->unit[r] = unit;
-            }
-            ctl->factor[r] = factor;
-            ctl->delta[r] = delta;
-          }
-#pragma unroll
-          for (int d = 1; d < 32; d <<= 1) unit = fminf(unit, __shfl_xor_sync(0xFFFFFFFFu, unit, d));
-          if (lane == 0) ctl->least_unit = unit;
-        }
-        __syncthreads();
-        if (since > 0) {
-          ptx::tc_fence_after();
-          empty_sums();
-        }
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-          const bool own = r < sg.rows;
-          const float f = own ? ctl->factor[r] : 1.0f;
-          arg[r] += own ? ctl->delta[r] : 0.0f;
-          total[r] *= f;
-#pragma unroll
-          for (int e = 0; e < G; ++e) low_sum[e][r] *= f;
-#pragma unroll
-          for (int k = 0; k < S::kBlocks; ++k) out[k][r] *= f;
-        }
-        put_weights();
-        ptx::fence_proxy_async_smem();
-        ptx::tc_fence_before();
-        __syncthreads();
-      }
-      if (warp == 0) {
-        ptx::tc_fence_after();
-        if (ptx::elect_one()) {
-#pragma unroll
-          for (int k = 0; k < S::kBlocks; ++k)
-#pragma unroll
-            for (int t = 0; t < 4; ++t)                                  // 32 tokens each
-              mma_u8(sum_tmem + k * S::kWeightCols, ptx::smem_desc(values + k * 16384 + t * 4096),
-                     weight_desc(weights + k * (S::kWeightUnits * 2048) + t * 512), kSumDesc | ((uint32_t)(S::kWeightCols / 8) << 17),
-                     since > 0 || t > 0);
-          ptx::mma_commit(ptx::smem_addr(&ctl->sums_done));
-        }
-        __syncwarp();
-      }
-      ++since;
-      // what a row does not see counts nothing, NaN or not; a step that is not finite makes its group NaN
-#pragma unroll
-      for (int r = 0; r < kRows; ++r) total[r] += p[r];
-#pragma unroll
-      for (int e = 0; e < G; ++e) {
-        const float m = fmaf(0.0f, param_step(value_params[e]), param_low(value_params[e]));
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-          if (edge) low_sum[e][r] += arg[r] == -INFINITY ? 0.0f : p[r] * m;
-          else low_sum[e][r] = fmaf(p[r], m, low_sum[e][r]);
-        }
-      }
+      if (edge) weigh(std::true_type());
+      else weigh(std::false_type());
     }
     if (tiles > 0) {
       bounded_wait_warp(ptx::smem_addr(&ctl->sums_done), sums_phase, abort_flag, WAIT_EPI_ACC_FULL);
@@ -754,52 +761,68 @@ attention_kernel(const AttentionArgs a) {
   }
 }
 
-// Joins the segments that workers share: the CTA of the first worker boundary inside a segment adds up the pieces, in the
-// order of the workers.
-template <int D, int G, int NT>
-__global__ void __launch_bounds__(kThreads) attention_join_kernel(const AttentionArgs a, int workers) {
-  using S = Shape<D, G, NT>;
-  __shared__ int64_t scratch[kWarps + 2];
+// Joins the segments that workers share, in the order of the workers: a CTA per worker that starts a segment and does not
+// finish it, a warp per row.
+template <int D, int G, int NB>
+__global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const AttentionArgs a) {
+  using S = Shape<D, G, NB>;
+  constexpr int kFours = D / 128 > 0 ? D / 128 : 1;                      // float4 of a lane
   ptx::grid_dependency_wait();
   ptx::grid_dependents_launch();
-  const int w = blockIdx.x + 1, r = blockIdx.y;
-  const WorkPlace wp = find_work<S>(a, workers, [&](int64_t per) { return (int64_t)w * per; }, scratch);
-  const int64_t x = (int64_t)w * wp.per;
-  if (x >= wp.total) return;
-  const SequenceWork sw = sequence_work<S>(a, wp.sequence);
-  const int64_t in_seq = x - wp.before;
-  const int seg = (int)(in_seq / sw.units);
-  const int64_t start = wp.before + (int64_t)seg * sw.units, end = start + sw.units;
-  if (start == x || start / wp.per != w - 1) return;
-  const int head = seg % a.cache.kv_heads;
-  const Segment sg = segment_of<S>(a, sw, seg / a.cache.kv_heads);
-  if (r >= sg.rows) return;
-  const int first = w - 1, last = (int)((end - 1) / wp.per);
-  auto part = [&](int worker) {                                        // only the first worker's piece starts the segment
-    return a.partial + ((2 * (int64_t)worker + (worker == first ? 1 : 0)) * S::kRows + r) * (D + 4);
-  };
-  float m = -INFINITY;
-  for (int k = first; k <= last; ++k) m = fmaxf(m, ptx::ld_global(static_cast<const float*>(part(k) + D)));
-  float l = 0.0f;
-  float e[(D + kThreads - 1) / kThreads] = {};
-  for (int k = first; k <= last; ++k) {
-    const float* p = part(k);
-    const float f = m == -INFINITY ? 0.0f : exp2_approx(ptx::ld_global(p + D) - m);
-    l += f * ptx::ld_global(p + D + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = blockIdx.x;
+  const JoinRecord rec = a.records[first];
+  if (rec.workers <= 1) return;
+  for (int r = warp; r < rec.rows; r += kJoinThreads / 32) {
+    auto part = [&](int k) {                                             // only the first worker's piece starts the segment
+      return a.partial + ((2 * (int64_t)(first + k) + (k == 0 ? 1 : 0)) * S::kRows + r) * (D + 4);
+    };
+    float m = -INFINITY;
+    for (int k = lane; k < rec.workers; k += 32) m = fmaxf(m, ptx::ld_global(static_cast<const float*>(part(k) + D)));
+    m = warp_max(m);
+    float l = 0.0f;
+    float4 e[kFours] = {};
+    for (int k0 = 0; k0 < rec.workers; k0 += 32) {
+      float f = 0.0f;
+      if (k0 + lane < rec.workers && m > -INFINITY) {
+        const uint2 y = ptx::ld_global(reinterpret_cast<const uint2*>(part(k0 + lane) + D));
+        f = exp2_approx(__uint_as_float(y.x) - m);
+        l = fmaf(f, __uint_as_float(y.y), l);
+      }
+      const int n = min(32, rec.workers - k0);
+      for (int k = 0; k < n; k += 8) {
+        uint4 y[8][kFours];
 #pragma unroll
-    for (int i = 0; i < (D + kThreads - 1) / kThreads; ++i)
-      if (threadIdx.x + i * kThreads < D) e[i] += f * ptx::ld_global(p + threadIdx.x + i * kThreads);
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int i = 0; i < kFours; ++i)
+            y[j][i] = k + j < n && lane + 32 * i < D / 4 ? ptx::ld_global(reinterpret_cast<const uint4*>(part(k0 + k + j)) + lane + 32 * i) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float fj = __shfl_sync(0xFFFFFFFFu, f, k + j);
+#pragma unroll
+          for (int i = 0; i < kFours; ++i) {
+            e[i].x = fmaf(fj, __uint_as_float(y[j][i].x), e[i].x);
+            e[i].y = fmaf(fj, __uint_as_float(y[j][i].y), e[i].y);
+            e[i].z = fmaf(fj, __uint_as_float(y[j][i].z), e[i].z);
+            e[i].w = fmaf(fj, __uint_as_float(y[j][i].w), e[i].w);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, d);
+    const int row = rec.first_row + r;
+    const int64_t out_row = rec.first + row / a.ratio;
+    const int q_head = rec.head * a.ratio + row % a.ratio;
+    const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int i = 0; i < kFours; ++i)
+      if (lane + 32 * i < D / 4)
+        *reinterpret_cast<uint2*>(a.O + out_row * a.o_pitch + (int64_t)q_head * D + (lane + 32 * i) * 4) =
+            make_uint2(pack_bf16x2(e[i].x * inv, e[i].y * inv), pack_bf16x2(e[i].z * inv, e[i].w * inv));
+    if (lane == 0 && a.lse != nullptr)
+      a.lse[out_row * a.q_heads + q_head] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
   }
-  const int row = sg.first_row + r;
-  const int64_t token = sw.rows.first + row / a.ratio;
-  const int q_head = head * a.ratio + row % a.ratio;
-  const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
-#pragma unroll
-  for (int i = 0; i < (D + kThreads - 1) / kThreads; ++i)
-    if (threadIdx.x + i * kThreads < D)
-      a.O[token * a.o_pitch + (int64_t)q_head * D + threadIdx.x + i * kThreads] = __bfloat16_as_ushort(__float2bfloat16_rn(e[i] * inv));
-  if (threadIdx.x == 0 && a.lse != nullptr)
-    a.lse[token * a.q_heads + q_head] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
 // ------------------------------------------------------------------ host side
@@ -871,7 +894,7 @@ size_t cache_attention_workspace(const eqat_cache_desc& d, const eqat_attention_
   with_shape(d, row_blocks(d, a), [&](auto D, auto G, auto NT) {
     using S = Shape<decltype(D)::value, decltype(G)::value, decltype(NT)::value>;
     const int w = workers_of<S>(d, a, sms > 0 ? sms : 148);
-    bytes = w > 1 ? (size_t)2 * w * S::kRows * (decltype(D)::value + 4) * sizeof(float) : 0;
+    bytes = w > 1 ? (size_t)w * (sizeof(JoinRecord) + (size_t)2 * S::kRows * (decltype(D)::value + 4) * sizeof(float)) : 0;
     return EQAT_OK;
   });
   return bytes;
@@ -891,7 +914,6 @@ int launch_cache_attention(const eqat_cache_desc& d, const eqat_attention_desc& 
     a.O = O;
     a.o_pitch = o_pitch;
     a.lse = lse;
-    a.partial = static_cast<float*>(workspace);
     a.q_heads = at.q_heads;
     a.ratio = at.q_heads / d.kv_heads;
     a.max_new = at.max_new;
@@ -903,9 +925,13 @@ int launch_cache_attention(const eqat_cache_desc& d, const eqat_attention_desc& 
     static SmemOptIn opt;
     if (!opt.ensure(attention_kernel<D, G, NT>, S::kSmemBytes)) return (int)EQAT_ERR_CUDA;
     const int workers = workers_of<S>(d, at, sms);
+    if (workers > 1) {
+      a.records = static_cast<JoinRecord*>(workspace);
+      a.partial = reinterpret_cast<float*>(a.records + workers);
+    }
     const int rc = launch_overlapped(attention_kernel<D, G, NT>, dim3(workers), dim3(kThreads), S::kSmemBytes, st, a);
     if (rc != EQAT_OK || workers == 1) return rc;
-    return launch_overlapped(attention_join_kernel<D, G, NT>, dim3(workers - 1, S::kRows), dim3(kThreads), 0, st, a, workers);
+    return launch_overlapped(attention_join_kernel<D, G, NT>, dim3(workers - 1), dim3(kJoinThreads), 0, st, a);
   });
 }
 
