@@ -88,6 +88,7 @@ struct AttentionArgs {
   JoinRecord* records;         // [workers]
   float* partial;              // [2 * workers][rows of a tile][D + 4]: sums, then the exponent and the sum of weights
   int q_heads, ratio, max_new, window;
+  int ratio_shift;             // log2(ratio), or -1
   float scale_log2;            // scale * log2(e)
   uint32_t page_mul;           // n / (page_size / 16) = n * page_mul >> page_shift for n < 2^26
   int page_shift;
@@ -122,6 +123,11 @@ __device__ __forceinline__ int page_index(const AttentionArgs& a, int token) {
   return (int)(((uint64_t)(uint32_t)(token >> 4) * a.page_mul) >> a.page_shift);
 }
 
+// a / b for a >= 0: the 64-bit division, a subroutine of a hundred instructions, only where it is needed.
+__device__ __forceinline__ int64_t quotient(int64_t a, int b) { return (a >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b; }
+// New token of a row of a tile (rows run over the query heads of a token first).
+__device__ __forceinline__ int token_of_row(const AttentionArgs& a, int row) { return a.ratio_shift >= 0 ? row >> a.ratio_shift : row / a.ratio; }
+
 struct WorkPlace {
   int64_t total, per;          // units of the call, of a worker
   int64_t before;              // units of the sequences before `sequence`
@@ -152,7 +158,7 @@ __device__ __forceinline__ WorkPlace find_work(const AttentionArgs& a, int worke
   }
   WorkPlace p;
   p.total = total;
-  p.per = max((total + workers - 1) / workers, (int64_t)a.min_units);
+  p.per = max(quotient(total + workers - 1, workers), (int64_t)a.min_units);
   const int64_t x = f(p.per);
   if (x >= before && x < before + own) {
     int b = b0;
@@ -183,8 +189,8 @@ __device__ __forceinline__ Segment segment_of(const AttentionArgs& a, const Sequ
   s.first_row = tile * S::kRows;
   s.rows = min(S::kRows, n * a.ratio - s.first_row);
   const int base = w.rows.length - w.rows.count;
-  s.high = max(base + (s.first_row + s.rows - 1) / a.ratio + 1, 0);
-  s.low = a.window > 0 ? max(base + s.first_row / a.ratio + 1 - a.window, 0) : 0;
+  s.high = max(base + token_of_row(a, s.first_row + s.rows - 1) + 1, 0);
+  s.low = a.window > 0 ? max(base + token_of_row(a, s.first_row) + 1 - a.window, 0) : 0;
   s.from = s.low & ~(S::kStageTokens - 1);
   return s;
 }
@@ -321,7 +327,7 @@ attention_kernel(const AttentionArgs a) {
       have = work_units(v, w);
     }
     const int64_t in_seq = x - seq_before;
-    const int seg = (int)(in_seq / w.units), u0 = (int)(in_seq % w.units);
+    const int seg = (int)quotient(in_seq, w.units), u0 = (int)(in_seq - (int64_t)seg * w.units);
     const int u1 = (int)min((int64_t)w.units, u0 + (x_end - x));
     const int head = seg % v.kv_heads;
     const Segment sg = segment_of<S>(a, w, seg / v.kv_heads);
@@ -338,30 +344,29 @@ attention_kernel(const AttentionArgs a) {
       return lane < 2 && token < sg.high ? ld_index(v.page_table + (int64_t)b * v.max_pages + page_index(a, token)) : 0;
     };
     int page = page_of(warp_token + 16 * lane);
-    uint32_t place[2] = {0, 0};                                          // token slots of the pool, less than 2^32
-    auto find = [&](int i) {                                             // the places of tile i
+    struct Places { uint32_t at[2]; };                                   // token slots of the pool, less than 2^32
+    auto find = [&](int i) {                                             // the places of tile i (called for 0, 1, 2 ...)
       const int token = warp_token + i * S::kUnit + 16 * lane;
       // a page number outside the pool counts as the nearest inside
       const uint32_t at = ((uint32_t)min(max(page, 0), v.pages - 1) * v.kv_heads + head) * v.page_size + (token - page_index(a, token) * v.page_size);
-      place[0] = __shfl_sync(0xFFFFFFFFu, at, 0);
-      place[1] = __shfl_sync(0xFFFFFFFFu, at, 1);
       page = page_of(token + S::kUnit);
+      return Places{{__shfl_sync(0xFFFFFFFFu, at, 0), __shfl_sync(0xFFFFFFFFu, at, 1)}};
     };
     // 16-byte chunk i * 32 + lane of the warp's 32 tokens
-    auto fetch = [&](uint4 (&to)[S::kLoads], const uint8_t* codes, int i) {
+    auto fetch = [&](uint4 (&to)[S::kLoads], const uint8_t* codes, const Places& place, int i) {
       const int token = warp_token + i * S::kUnit;
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
-        const uint4* from = reinterpret_cast<const uint4*>(codes + (uint64_t)place[p] * (D / 2)) + lane;
+        const uint4* from = reinterpret_cast<const uint4*>(codes + (uint64_t)place.at[p] * (D / 2)) + lane;
 #pragma unroll
         for (int j = 0; j < S::kLoads / 2; ++j)                          // what is not fetched keeps the codes of before
           if (token + 16 * p < sg.high) to[p * (S::kLoads / 2) + j] = ptx::ld_global(from + 32 * j);
       }
     };
-    auto fetch_params = [&](uint32_t (&to)[G], const uint32_t* params, int i) {      // of this thread's token
+    auto fetch_params = [&](uint32_t (&to)[G], const uint32_t* params, const Places& place, int i) {      // of this thread's token
       const int token = warp_token + i * S::kUnit + (lane & 16);
       if (token < sg.high) {
-        load_params<G>(to, params + ((uint64_t)(lane < 16 ? place[0] : place[1]) + (lane & 15)) * G);
+        load_params<G>(to, params + ((uint64_t)(lane < 16 ? place.at[0] : place.at[1]) + (lane & 15)) * G);
       } else {
 #pragma unroll
         for (int e = 0; e < G; ++e) to[e] = 0u;
@@ -382,12 +387,13 @@ attention_kernel(const AttentionArgs a) {
     };
     uint4 key_codes[S::kLoads] = {}, value_codes[S::kLoads] = {};
     uint32_t key_params[G], value_params[G], next_key_params[G], next_value_params[G];
+    Places place{};
     if (tiles > 0) {
-      find(0);
-      fetch(key_codes, v.kq, 0);
-      fetch_params(next_key_params, v.kp, 0);
-      fetch(value_codes, v.vq, 0);
-      fetch_params(next_value_params, v.vp, 0);
+      place = find(0);
+      fetch(key_codes, v.kq, place, 0);
+      fetch_params(next_key_params, v.kp, place, 0);
+      fetch(value_codes, v.vq, place, 0);
+      fetch_params(next_value_params, v.vp, place, 0);
     }
 
     // ---- the queries: 16 threads a row, scaled so that the largest element lies in [128, 256), in the order of the codes
@@ -395,10 +401,10 @@ attention_kernel(const AttentionArgs a) {
 #pragma unroll
     for (int rb = 0; rb < NB; ++rb) {
       constexpr int kEach = D / 16;                                      // elements of a thread
-      const int r = rb * 8 + tid / 16, part = tid % 16, row = sg.first_row + r;
+      const int r = rb * 8 + tid / 16, part = tid % 16, row = sg.first_row + r, new_token = token_of_row(a, row);
       uint32_t e[kEach / 2] = {};
       if (r < sg.rows) {
-        const eqat_bf16* src = a.Q + (int64_t)(w.rows.first + row / a.ratio) * a.q_pitch + (int64_t)(head * a.ratio + row % a.ratio) * D + part * kEach;
+        const eqat_bf16* src = a.Q + (int64_t)(w.rows.first + new_token) * a.q_pitch + (int64_t)(head * a.ratio + row - new_token * a.ratio) * D + part * kEach;
 #pragma unroll
         for (int j = 0; j < kEach / 2; j += 2) {
           const uint2 y = ptx::ld_global(reinterpret_cast<const uint2*>(src + 2 * j));
@@ -426,7 +432,7 @@ attention_kernel(const AttentionArgs a) {
         ctl->top[r] = ctl->shift[r] = -INFINITY;
         ctl->limit[r] = r < sg.rows ? -INFINITY : INFINITY;
         ctl->unit[r] = r < sg.rows ? 0.0f : INFINITY;
-        const int pos = base_pos + row / a.ratio;
+        const int pos = base_pos + new_token;
         ctl->high[r] = r < sg.rows ? pos + 1 : 0;
         ctl->low[r] = a.window > 0 ? pos + 1 - a.window : 0;
       }
@@ -453,8 +459,8 @@ attention_kernel(const AttentionArgs a) {
     }
     if (tid == 0) ctl->least_unit = 0.0f;
     // every row of the tile sees the keys [all_low, all_high)
-    const int all_high = base_pos + sg.first_row / a.ratio + 1;
-    const int all_low = a.window > 0 ? base_pos + (sg.first_row + sg.rows - 1) / a.ratio + 1 - a.window : 0;
+    const int all_high = base_pos + token_of_row(a, sg.first_row) + 1;
+    const int all_low = a.window > 0 ? base_pos + token_of_row(a, sg.first_row + sg.rows - 1) + 1 - a.window : 0;
 
     float total[kRows] = {}, low_sum[G][kRows] = {};                     // of this thread's tokens
     float out[S::kBlocks][kRows] = {};                                   // of this thread's element of the head, in units of codes
@@ -489,10 +495,10 @@ attention_kernel(const AttentionArgs a) {
       }
       spread(key_codes, keys);
       if (i + 1 < tiles) {
-        find(i + 1);
-        fetch(key_codes, v.kq, i + 1);
-        fetch_params(next_key_params, v.kp, i + 1);
-        fetch_params(next_value_params, v.vp, i + 1);
+        place = find(i + 1);
+        fetch(key_codes, v.kq, place, i + 1);
+        fetch_params(next_key_params, v.kp, place, i + 1);
+        fetch_params(next_value_params, v.vp, place, i + 1);
       }
       ptx::fence_proxy_async_smem();
       ptx::tc_fence_before();
@@ -512,7 +518,8 @@ attention_kernel(const AttentionArgs a) {
         }
         __syncwarp();
       }
-      if (i > 0) {                                                       // the last tile's values have been read
+      // Under the product: the values of this tile.
+      if (i > 0) {                                                       // the last tile's values and weights have been read
         bounded_wait_warp(ptx::smem_addr(&ctl->sums_done), sums_phase, abort_flag, WAIT_EPI_ACC_FULL);
         sums_phase ^= 1u;
         if (since == 4096) {                                             // 15 * 255 * 128 * 4096 < 2^31
@@ -521,16 +528,15 @@ attention_kernel(const AttentionArgs a) {
         }
       }
       spread(value_codes, values);
-      if (i + 1 < tiles) fetch(value_codes, v.vq, i + 1);
-
+      if (i + 1 < tiles) fetch(value_codes, v.vq, place, i + 1);
       bounded_wait_warp(ptx::smem_addr(&ctl->scores_done), scores_phase, abort_flag, WAIT_EPI_ACC_FULL);
       scores_phase ^= 1u;
       ptx::tc_fence_after();
 
-      // ---- this token's weights: exponents of all rows first
+      // ---- this token's scores
       float arg[kRows];
       float step = 0.0f;
-      bool raise = false;
+      bool raise = i == 0;
 #pragma unroll
       for (int e = 0; e < G; ++e) {
         const float ks = param_step(key_params[e]) * a.scale_log2, km = param_low(key_params[e]) * a.scale_log2;
@@ -553,6 +559,7 @@ attention_kernel(const AttentionArgs a) {
           }
         }
       }
+
       // Some rows of an edge tile do not see some of its tokens.
       auto weigh = [&](auto is_edge) {
         constexpr bool kEdge = decltype(is_edge)::value;
@@ -573,11 +580,13 @@ attention_kernel(const AttentionArgs a) {
           }
         }
         if (!kEdge) raise |= step > ctl->least_unit;
-        // The weights are written before it is known whether some thread wants its row's exponent raised, which is rare.
+        // The weights are written before it is known whether some thread wants its row's exponent raised, which is rare
+        // behind a segment's first tile.
         float p[kRows];
-        for (;;) {
+        for (bool unset = i == 0;; unset = false) {
 #pragma unroll
           for (int r = 0; r < kRows; ++r) p[r] = exp2_approx(arg[r]);
+          if (!unset)
 #pragma unroll
           for (int e = 0; e < G; ++e) {
             const float s = param_step(value_params[e]);
@@ -730,9 +739,9 @@ attention_kernel(const AttentionArgs a) {
     const int64_t part_slot = 2 * (int64_t)blockIdx.x + (u0 == 0 ? 1 : 0);
     for (int r = warp; r < sg.rows; r += kWarps) {
       const float m = ctl->shift[r], l = ctl->sums[0][r];
-      const int row = sg.first_row + r;
-      const int64_t out_row = w.rows.first + row / a.ratio;
-      const int q_head = head * a.ratio + row % a.ratio;
+      const int row = sg.first_row + r, new_token = token_of_row(a, row);
+      const int64_t out_row = w.rows.first + new_token;
+      const int q_head = head * a.ratio + row - new_token * a.ratio;
       const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
       eqat_bf16* to = a.O + out_row * a.o_pitch + (int64_t)q_head * D;
       float* part = whole ? nullptr : a.partial + (part_slot * kRows + r) * (D + 4);
@@ -811,9 +820,9 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Atte
     }
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, d);
-    const int row = rec.first_row + r;
-    const int64_t out_row = rec.first + row / a.ratio;
-    const int q_head = rec.head * a.ratio + row % a.ratio;
+    const int row = rec.first_row + r, new_token = token_of_row(a, row);
+    const int64_t out_row = rec.first + new_token;
+    const int q_head = rec.head * a.ratio + row - new_token * a.ratio;
     const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
 #pragma unroll
     for (int i = 0; i < kFours; ++i)
@@ -916,6 +925,7 @@ int launch_cache_attention(const eqat_cache_desc& d, const eqat_attention_desc& 
     a.lse = lse;
     a.q_heads = at.q_heads;
     a.ratio = at.q_heads / d.kv_heads;
+    a.ratio_shift = (a.ratio & (a.ratio - 1)) == 0 ? log2_up(a.ratio) : -1;
     a.max_new = at.max_new;
     a.window = at.window < view.max_length ? at.window : 0;              // a window of the longest sequence hides nothing
     a.scale_log2 = at.scale * kLog2e;
