@@ -40,12 +40,13 @@ constexpr float kLog2e = 1.4426950408889634f;
 // that maximum by more than kLazy.
 constexpr float kLazy = 2.0f, kOne = 21.0f;
 
-// D: elements of a head, G: groups in it, NB: blocks of eight query rows.
-template <int D, int G, int NB>
+// D: elements of a head, G: groups in it, ROWS: query rows of a tile (1, 4, or a multiple of eight).
+template <int D, int G, int ROWS>
 struct Shape {
+  static constexpr int NB = (ROWS + 7) / 8;                            // blocks of eight rows: columns come in sixteens
   static constexpr int kStageTokens = 16;                              // segments start at a multiple of this
   static constexpr int kUnit = 128;                                    // tokens of a tile
-  static constexpr int kRows = 8 * NB;
+  static constexpr int kRows = ROWS;
   static constexpr int kBlocks = D > 128 ? D / 128 : 1;                // blocks of 128 elements
   static constexpr int kBlockGroups = G / kBlocks;
   static constexpr int kParts = NB * kBlockGroups;                     // (row block, group) pairs of a block: three byte columns x 8
@@ -66,7 +67,7 @@ struct Shape {
   static constexpr int kSmemBytes = kTwoParts && kNeedBytes < 57 * 1024 ? 57 * 1024 : kNeedBytes;
   static constexpr int kTmemCtas = 512 / (kAlloc + (kTwoParts ? 32 : 0));
   static constexpr int kSmemCtas = 227 * 1024 / (kSmemBytes + 4096);
-  static constexpr int kRegCtas = kRows * (1 + G) + kRows * kBlocks <= 40 ? 4 : 3;
+  static constexpr int kRegCtas = kRows * (1 + G + kBlocks) <= 40 && D <= 128 ? 4 : 3;
   static constexpr int kCtas = kTmemCtas < kSmemCtas ? (kTmemCtas < kRegCtas ? kTmemCtas : kRegCtas) : (kSmemCtas < kRegCtas ? kSmemCtas : kRegCtas);
   static constexpr int kLoads = D / 32;                                // 16-byte loads of a lane per tile, keys or values
   static_assert((1 + G) * kRows * 512 <= 2 * kOperandBytes && kRows * D * 4 <= 2 * kOperandBytes, "sums meet in the operands' memory");
@@ -234,6 +235,11 @@ __device__ __forceinline__ float2 from_e4m3x2(uint32_t v) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)v));
   return __half22float2(*reinterpret_cast<const __half2*>(&r));
 }
+__device__ __forceinline__ void sts_8(uint32_t addr, uint32_t v) { asm volatile("st.shared.u8 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+__device__ __forceinline__ void sts_32(uint32_t addr, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+__device__ __forceinline__ void sts_64(uint32_t addr, uint32_t a, uint32_t b) {
+  asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+}
 __device__ __forceinline__ float warp_max(float x) {
   float r;
   asm("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(r) : "f"(x));
@@ -274,19 +280,24 @@ struct AttentionCtl {
   int64_t scratch[kWarps + 2];
 };
 
-template <int D, int G, int NB>
-__global__ void __launch_bounds__(kThreads, (Shape<D, G, NB>::kCtas))
+template <int D, int G, int ROWS>
+__global__ void __launch_bounds__(kThreads, (Shape<D, G, ROWS>::kCtas))
 attention_kernel(const AttentionArgs a) {
-  using S = Shape<D, G, NB>;
-  constexpr int kRows = S::kRows, kGroup = D / G;
+  using S = Shape<D, G, ROWS>;
+  constexpr int kRows = ROWS, NB = S::NB, kGroup = D / G, kChunks = D / 32;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(16) AttentionCtl<kRows, G> ctl_block;
-  AttentionCtl<kRows, G>* ctl = &ctl_block;
+  __shared__ __align__(16) AttentionCtl<8 * NB, G> ctl_block;
+  AttentionCtl<8 * NB, G>* ctl = &ctl_block;
   volatile int* abort_flag = &ctl->abort;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t raw = ptx::smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
   const uint32_t keys = base, values = keys + S::kOperandBytes, weights = values + S::kOperandBytes, queries = weights + S::kWeightBytes;
   float* meet = reinterpret_cast<float*>(smem_raw + (base - raw));       // the operands' memory, between segments
+  // where this lane's first chunk goes in `keys`, as even codes (the odd ones: the other of two 16-byte pieces), and its
+  // token's weights
+  const uint32_t chunk_at = keys + (lane % kChunks / 4) * 16384 + (32 * warp + lane / kChunks) * 128 +
+                            (((lane % kChunks % 4 * 2) ^ (lane / kChunks & 7)) << 4);
+  const uint32_t weight_at = weights + tid * 16;
 
   if (tid == 0) {
     ptx::mbar_init(ptx::smem_addr(&ctl->scores_done), 1);
@@ -302,23 +313,34 @@ attention_kernel(const AttentionArgs a) {
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
+  for (int i = tid; i < S::kWeightBytes / 16; i += kThreads) ptx::sts_128(weights + i * 16, 0u, 0u, 0u, 0u);   // rows beyond ROWS stay so
   const uint32_t sum_tmem = ctl->tmem[0], own_lanes = (uint32_t)(warp * 32) << 16;
   auto score_tmem = [&](int group) -> uint32_t {                         // of the 16 NB columns of a group
     if (S::kTwoParts && group >= G - 2) return ctl->tmem[1] + 16 * (group - (G - 2));
     return sum_tmem + S::kSumCols + group * 16 * NB;
   };
+  const uint64_t keys_desc = ptx::smem_desc(keys), queries_desc = ptx::smem_desc(queries), values_desc = ptx::smem_desc(values),
+                 weights_desc = weight_desc(weights);
   ptx::grid_dependency_wait();
 
   const CacheView& v = a.cache;
   const WorkPlace wp = find_work<S>(a, gridDim.x, [&](int64_t per) { return (int64_t)blockIdx.x * per; }, ctl->scratch);
   int64_t x = (int64_t)blockIdx.x * wp.per;
+  const int64_t x_begin = x;
   const int64_t x_end = min(x + wp.per, wp.total);
   int b = wp.sequence;
   int64_t seq_before = wp.before;
   uint32_t scores_phase = 0, sums_phase = 0;
   if (tid == 0 && a.records != nullptr) a.records[blockIdx.x].workers = 0;
 
-  while (x < x_end) {
+  // The segment, or the part of one, that starts with unit x.
+  struct Job {
+    SequenceRows rows;
+    Segment sg;
+    int sequence, head, u0, u1, first_token, tiles;
+    bool whole;
+  };
+  auto next_job = [&] {
     SequenceWork w = sequence_work<S>(a, b);
     int64_t have = work_units(v, w);
     while (x >= seq_before + have) {                                     // sequences without rows have no units
@@ -327,84 +349,97 @@ attention_kernel(const AttentionArgs a) {
       have = work_units(v, w);
     }
     const int64_t in_seq = x - seq_before;
-    const int seg = (int)quotient(in_seq, w.units), u0 = (int)(in_seq - (int64_t)seg * w.units);
-    const int u1 = (int)min((int64_t)w.units, u0 + (x_end - x));
-    const int head = seg % v.kv_heads;
-    const Segment sg = segment_of<S>(a, w, seg / v.kv_heads);
-    const bool whole = u0 == 0 && u1 == w.units;
-    if (tid == 0 && u0 == 0 && !whole)                                   // the worker's last segment
-      a.records[blockIdx.x] = JoinRecord{w.rows.first, sg.first_row, sg.rows, head, (int)((x + w.units - 1) / wp.per) - (int)blockIdx.x + 1, {0, 0, 0}};
-    const int first_token = sg.from + u0 * S::kUnit;
-    const int tiles = first_token < sg.high ? min(u1 - u0, (sg.high - first_token + S::kUnit - 1) / S::kUnit) : 0;
+    const int seg = (int)quotient(in_seq, w.units), tile = seg / v.kv_heads;
+    Job j;
+    j.rows = w.rows;
+    j.sequence = b;
+    j.head = seg - tile * v.kv_heads;
+    j.sg = segment_of<S>(a, w, tile);
+    j.u0 = (int)(in_seq - (int64_t)seg * w.units);
+    j.u1 = (int)min((int64_t)w.units, j.u0 + (x_end - x));
+    j.whole = j.u0 == 0 && j.u1 == w.units;
+    j.first_token = j.sg.from + j.u0 * S::kUnit;
+    j.tiles = j.first_token < j.sg.high ? min(j.u1 - j.u0, (j.sg.high - j.first_token + S::kUnit - 1) / S::kUnit) : 0;
+    if (tid == 0 && j.u0 == 0 && !j.whole)                               // the worker's last segment
+      a.records[blockIdx.x] = JoinRecord{j.rows.first, j.sg.first_row, j.sg.rows, j.head, (int)quotient(x + w.units - 1, wp.per) - (int)blockIdx.x + 1, {0, 0, 0}};
+    x += j.u1 - j.u0;
+    return j;
+  };
 
-    // ---- fetching: a warp has 32 tokens of the tile, two pieces of 16 that lie in one page each; lanes 0 and 1 hold the
-    // pages of the next tile's pieces, as they were read
-    const int warp_token = first_token + 32 * warp;
-    auto page_of = [&](int token) {
-      return lane < 2 && token < sg.high ? ld_index(v.page_table + (int64_t)b * v.max_pages + page_index(a, token)) : 0;
-    };
-    int page = page_of(warp_token + 16 * lane);
-    struct Places { uint32_t at[2]; };                                   // token slots of the pool, less than 2^32
-    auto find = [&](int i) {                                             // the places of tile i (called for 0, 1, 2 ...)
-      const int token = warp_token + i * S::kUnit + 16 * lane;
-      // a page number outside the pool counts as the nearest inside
-      const uint32_t at = ((uint32_t)min(max(page, 0), v.pages - 1) * v.kv_heads + head) * v.page_size + (token - page_index(a, token) * v.page_size);
-      page = page_of(token + S::kUnit);
-      return Places{{__shfl_sync(0xFFFFFFFFu, at, 0), __shfl_sync(0xFFFFFFFFu, at, 1)}};
-    };
-    // 16-byte chunk i * 32 + lane of the warp's 32 tokens
-    auto fetch = [&](uint4 (&to)[S::kLoads], const uint8_t* codes, const Places& place, int i) {
-      const int token = warp_token + i * S::kUnit;
+  // ---- fetching: a warp has 32 tokens of the tile, two pieces of 16 that lie in one page each; lanes 0 and 1 hold the
+  // pages of the next tile's pieces, as they were read
+  const uint8_t *key_lane = v.kq + lane * 16, *value_lane = v.vq + lane * 16;
+  const uint32_t *key_param_lane = v.kp + (lane & 15) * G, *value_param_lane = v.vp + (lane & 15) * G;
+  int page = 0;
+  struct Places { uint32_t at[2]; };                                     // token slots of the pool, less than 2^32
+  auto page_of = [&](const Job& j, int i) {
+    const int token = j.first_token + i * S::kUnit + 32 * warp + 16 * lane;
+    return lane < 2 && token < j.sg.high ? ld_index(v.page_table + (int64_t)j.sequence * v.max_pages + page_index(a, token)) : 0;
+  };
+  auto find = [&](const Job& j, int i) {                                 // the places of tile i (called for 0, 1, 2 ...)
+    const int token = j.first_token + i * S::kUnit + 32 * warp + 16 * lane;
+    // a page number outside the pool counts as the nearest inside
+    const uint32_t at = ((uint32_t)min(max(page, 0), v.pages - 1) * v.kv_heads + j.head) * v.page_size + (token - page_index(a, token) * v.page_size);
+    page = page_of(j, i + 1);
+    return Places{{__shfl_sync(0xFFFFFFFFu, at, 0), __shfl_sync(0xFFFFFFFFu, at, 1)}};
+  };
+  // 16-byte chunks i * 32 + lane of the warp's 32 tokens; what is not fetched keeps the codes of before
+  auto fetch = [&](uint4 (&to)[S::kLoads], const uint8_t* from, const Places& place, int left) {
 #pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const uint4* from = reinterpret_cast<const uint4*>(codes + (uint64_t)place.at[p] * (D / 2)) + lane;
+    for (int p = 0; p < 2; ++p)
+      if (16 * p < left) {
+        const uint4* at = reinterpret_cast<const uint4*>(from + (uint64_t)place.at[p] * (D / 2));
 #pragma unroll
-        for (int j = 0; j < S::kLoads / 2; ++j)                          // what is not fetched keeps the codes of before
-          if (token + 16 * p < sg.high) to[p * (S::kLoads / 2) + j] = ptx::ld_global(from + 32 * j);
+        for (int j = 0; j < S::kLoads / 2; ++j) to[p * (S::kLoads / 2) + j] = ptx::ld_global(at + 32 * j);
       }
-    };
-    auto fetch_params = [&](uint32_t (&to)[G], const uint32_t* params, const Places& place, int i) {      // of this thread's token
-      const int token = warp_token + i * S::kUnit + (lane & 16);
-      if (token < sg.high) {
-        load_params<G>(to, params + ((uint64_t)(lane < 16 ? place.at[0] : place.at[1]) + (lane & 15)) * G);
-      } else {
+  };
+  auto fetch_params = [&](uint32_t (&to)[G], const uint32_t* from, const Places& place, int left) {      // of this thread's token
+    if ((lane & 16) < left) load_params<G>(to, from + (uint64_t)(lane < 16 ? place.at[0] : place.at[1]) * G);
+  };
+  auto left_of = [&](const Job& j, int i) { return j.sg.high - (j.first_token + i * S::kUnit + 32 * warp); };      // tokens from the warp's first on
+  // Codes of a chunk (32 j .. 32 j + 31 of a token) as bytes: the even ones are 16 bytes 2 j of the token's row, the odd
+  // ones 16 bytes 2 j + 1; 16-byte pieces swizzled by the row.
+  auto spread = [&](const uint4 (&from)[S::kLoads], int operand) {
 #pragma unroll
-        for (int e = 0; e < G; ++e) to[e] = 0u;
-      }
-    };
-    // Codes of a chunk (32 j .. 32 j + 31 of a token) as bytes: the even ones are 16 bytes 2 j of the token's row, the odd
-    // ones 16 bytes 2 j + 1; 16-byte pieces swizzled by the row.
-    auto spread = [&](const uint4 (&from)[S::kLoads], uint32_t operand) {
-#pragma unroll
-      for (int i = 0; i < S::kLoads; ++i) {
-        const int chunk = i * 32 + lane, token = 32 * warp + chunk / (D / 32), j = chunk % (D / 32);
-        const uint32_t row = operand + (j / 4) * 16384 + token * 128;
-        const uint4 c = from[i];
-        ptx::sts_128(row + ((((j % 4) * 2) ^ (token & 7)) << 4), c.x & 0x0F0F0F0Fu, c.y & 0x0F0F0F0Fu, c.z & 0x0F0F0F0Fu, c.w & 0x0F0F0F0Fu);
-        ptx::sts_128(row + ((((j % 4) * 2 + 1) ^ (token & 7)) << 4), (c.x >> 4) & 0x0F0F0F0Fu, (c.y >> 4) & 0x0F0F0F0Fu,
-                     (c.z >> 4) & 0x0F0F0F0Fu, (c.w >> 4) & 0x0F0F0F0Fu);
-      }
-    };
-    uint4 key_codes[S::kLoads] = {}, value_codes[S::kLoads] = {};
-    uint32_t key_params[G], value_params[G], next_key_params[G], next_value_params[G];
-    Places place{};
-    if (tiles > 0) {
-      place = find(0);
-      fetch(key_codes, v.kq, place, 0);
-      fetch_params(next_key_params, v.kp, place, 0);
-      fetch(value_codes, v.vq, place, 0);
-      fetch_params(next_value_params, v.vp, place, 0);
+    for (int i = 0; i < S::kLoads; ++i) {
+      const uint32_t at = (kChunks == 8 && (i & 1) ? chunk_at ^ 64u : chunk_at) + operand + i * (32 / kChunks * 128), odd = at ^ 16u;
+      const uint4 c = from[i];
+      ptx::sts_128(at, c.x & 0x0F0F0F0Fu, c.y & 0x0F0F0F0Fu, c.z & 0x0F0F0F0Fu, c.w & 0x0F0F0F0Fu);
+      ptx::sts_128(odd, (c.x >> 4) & 0x0F0F0F0Fu, (c.y >> 4) & 0x0F0F0F0Fu, (c.z >> 4) & 0x0F0F0F0Fu, (c.w >> 4) & 0x0F0F0F0Fu);
     }
+  };
+  uint4 key_codes[S::kLoads] = {}, value_codes[S::kLoads] = {};
+  uint32_t next_key_params[G] = {}, next_value_params[G] = {};
+  auto fetch_first = [&](const Job& j) {
+    if (j.tiles > 0) {
+      const Places place = find(j, 0);
+      const int left = left_of(j, 0);
+      fetch(key_codes, key_lane, place, left);
+      fetch_params(next_key_params, key_param_lane, place, left);
+      fetch(value_codes, value_lane, place, left);
+      fetch_params(next_value_params, value_param_lane, place, left);
+    }
+  };
+
+  Job job;
+  if (x < x_end) {
+    job = next_job();
+    page = page_of(job, 0);
+    fetch_first(job);
+  }
+  for (bool more = x_begin < x_end; more;) {
+    const Segment& sg = job.sg;
+    const int tiles = job.tiles;
 
     // ---- the queries: 16 threads a row, scaled so that the largest element lies in [128, 256), in the order of the codes
-    const int base_pos = w.rows.length - w.rows.count;
+    const int base_pos = job.rows.length - job.rows.count;
 #pragma unroll
     for (int rb = 0; rb < NB; ++rb) {
       constexpr int kEach = D / 16;                                      // elements of a thread
       const int r = rb * 8 + tid / 16, part = tid % 16, row = sg.first_row + r, new_token = token_of_row(a, row);
       uint32_t e[kEach / 2] = {};
       if (r < sg.rows) {
-        const eqat_bf16* src = a.Q + (int64_t)(w.rows.first + new_token) * a.q_pitch + (int64_t)(head * a.ratio + row - new_token * a.ratio) * D + part * kEach;
+        const eqat_bf16* src = a.Q + (int64_t)(job.rows.first + new_token) * a.q_pitch + (int64_t)(job.head * a.ratio + row - new_token * a.ratio) * D + part * kEach;
 #pragma unroll
         for (int j = 0; j < kEach / 2; j += 2) {
           const uint2 y = ptx::ld_global(reinterpret_cast<const uint2*>(src + 2 * j));
@@ -479,26 +514,28 @@ attention_kernel(const AttentionArgs a) {
           ptx::tmem_ld_32x8(at + 16 * S::kParts + part * 8, high8);
           ptx::tmem_ld_wait();
 #pragma unroll
-          for (int r = 0; r < 8; ++r)
+          for (int r = 0; r < 8 && r < kRows; ++r)
             out[k][rb * 8 + r] += fmaf((float)(int)high8[r], 65536.0f, fmaf((float)(int)low16[8 + r], 256.0f, (float)(int)low16[r]));
         }
       since = 0;
     };
 
+    Places place{};
     for (int i = 0; i < tiles; ++i) {
-      const int t0 = first_token + i * S::kUnit, token = t0 + tid;
+      const int t0 = job.first_token + i * S::kUnit, token = t0 + tid, left = left_of(job, i + 1);
       const bool edge = t0 < all_low || t0 + S::kUnit > all_high;
+      uint32_t key_params[G], value_params[G];
 #pragma unroll
       for (int e = 0; e < G; ++e) {
         key_params[e] = next_key_params[e];
         value_params[e] = next_value_params[e];
       }
-      spread(key_codes, keys);
+      spread(key_codes, 0);
       if (i + 1 < tiles) {
-        place = find(i + 1);
-        fetch(key_codes, v.kq, place, i + 1);
-        fetch_params(next_key_params, v.kp, place, i + 1);
-        fetch_params(next_value_params, v.vp, place, i + 1);
+        place = find(job, i + 1);
+        fetch(key_codes, key_lane, place, left);
+        fetch_params(next_key_params, key_param_lane, place, left);
+        fetch_params(next_value_params, value_param_lane, place, left);
       }
       ptx::fence_proxy_async_smem();
       ptx::tc_fence_before();
@@ -511,7 +548,7 @@ attention_kernel(const AttentionArgs a) {
             const int at = e % S::kBlockGroups * kGroup, block = e / S::kBlockGroups;
 #pragma unroll
             for (int k = 0; k < kGroup; k += 32)
-              mma_e4m3(score_tmem(e), ptx::smem_desc(keys + block * 16384 + at + k), ptx::smem_desc(queries + block * (NB * 2048) + at + k),
+              mma_e4m3(score_tmem(e), keys_desc + ((block * 16384 + at + k) >> 4), queries_desc + ((block * (NB * 2048) + at + k) >> 4),
                        kScoreDesc | ((uint32_t)(2 * NB) << 17), k != 0);
           }
           ptx::mma_commit(ptx::smem_addr(&ctl->scores_done));
@@ -527,8 +564,8 @@ attention_kernel(const AttentionArgs a) {
           empty_sums();
         }
       }
-      spread(value_codes, values);
-      if (i + 1 < tiles) fetch(value_codes, v.vq, place, i + 1);
+      spread(value_codes, S::kOperandBytes);
+      if (i + 1 < tiles) fetch(value_codes, value_lane, place, left);
       bounded_wait_warp(ptx::smem_addr(&ctl->scores_done), scores_phase, abort_flag, WAIT_EPI_ACC_FULL);
       scores_phase ^= 1u;
       ptx::tc_fence_after();
@@ -547,11 +584,11 @@ attention_kernel(const AttentionArgs a) {
           ptx::tmem_ld_32x16(score_tmem(e) + own_lanes + rb * 16, acc);
           ptx::tmem_ld_wait();
 #pragma unroll
-          for (int q4 = 0; q4 < 8; q4 += 4) {
+          for (int q4 = 0; q4 < 8 && q4 < kRows; q4 += 4) {
             const float4 qs = *reinterpret_cast<const float4*>(&ctl->q_sum[e][rb * 8 + q4]);
             const float qv[4] = {qs.x, qs.y, qs.z, qs.w};
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
+            for (int r = 0; r < 4 && r < kRows; ++r) {
               const float z = fmaf(__uint_as_float(acc[8 + q4 + r]), 0.0625f, __uint_as_float(acc[q4 + r]));
               float& to = arg[rb * 8 + q4 + r];
               to = fmaf(z, ks, e == 0 ? qv[r] * km : fmaf(qv[r], km, to));
@@ -569,7 +606,7 @@ attention_kernel(const AttentionArgs a) {
           const float4 lm = *reinterpret_cast<const float4*>(&ctl->limit[r0]);
           const float bv[4] = {bk.x, bk.y, bk.z, bk.w}, mv[4] = {mn.x, mn.y, mn.z, mn.w}, lv[4] = {lm.x, lm.y, lm.z, lm.w};
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
+          for (int r = 0; r < 4 && r < kRows; ++r) {
             arg[r0 + r] = fmaf(arg[r0 + r], bv[r], mv[r]);
             if (kEdge) {
               const bool seen = token >= ctl->low[r0 + r] && token < ctl->high[r0 + r];
@@ -595,23 +632,35 @@ attention_kernel(const AttentionArgs a) {
             for (int rb = 0; rb < NB; ++rb) {
               uint32_t y[8];
 #pragma unroll
-              for (int r = 0; r < 8; ++r) {
+              for (int r = 0; r < 8 && r < kRows; ++r) {
                 y[r] = __float_as_uint(fmaf(p[rb * 8 + r], s, 8388608.0f));          // 2^23: the low 23 bits are round(p s)
                 if (kEdge) y[r] = arg[rb * 8 + r] == -INFINITY ? 0u : y[r];          // unseen: zero, whatever the step
               }
-              uint32_t low[2], mid[2], high[2];
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const uint32_t t01 = __byte_perm(y[4 * h], y[4 * h + 1], 0x5140), t23 = __byte_perm(y[4 * h + 2], y[4 * h + 3], 0x5140);
-                low[h] = __byte_perm(t01, t23, 0x5410);
-                mid[h] = __byte_perm(t01, t23, 0x7632);
-                high[h] = __byte_perm(__byte_perm(y[4 * h], y[4 * h + 1], 0x0062), __byte_perm(y[4 * h + 2], y[4 * h + 3], 0x0062), 0x5410);
-              }
               const int part = e % S::kBlockGroups * NB + rb;
-              const uint32_t at = weights + block * (S::kWeightUnits * 2048) + tid * 16;
-              ptx::sts_128(at + part * 2048, low[0], low[1], mid[0], mid[1]);
-              if (S::kParts == 1) ptx::sts_128(at + 2048, high[0], high[1], 0u, 0u);
-              else asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at + (S::kParts + part / 2) * 2048 + (part & 1) * 8), "r"(high[0]), "r"(high[1]) : "memory");
+              const uint32_t at = weight_at + block * (S::kWeightUnits * 2048) + part * 2048;
+              const uint32_t high_at = weight_at + block * (S::kWeightUnits * 2048) + (S::kParts == 1 ? 2048 : (S::kParts + part / 2) * 2048 + (part & 1) * 8);
+              if constexpr (kRows == 1) {
+                sts_8(at, y[0]);
+                sts_8(at + 8, y[0] >> 8);
+                sts_8(high_at, y[0] >> 16);
+              } else {
+                uint32_t low[2], mid[2], high[2];
+#pragma unroll
+                for (int h = 0; h < 2 && 4 * h < kRows; ++h) {
+                  const uint32_t t01 = __byte_perm(y[4 * h], y[4 * h + 1], 0x5140), t23 = __byte_perm(y[4 * h + 2], y[4 * h + 3], 0x5140);
+                  low[h] = __byte_perm(t01, t23, 0x5410);
+                  mid[h] = __byte_perm(t01, t23, 0x7632);
+                  high[h] = __byte_perm(__byte_perm(y[4 * h], y[4 * h + 1], 0x0062), __byte_perm(y[4 * h + 2], y[4 * h + 3], 0x0062), 0x5410);
+                }
+                if constexpr (kRows == 4) {
+                  sts_32(at, low[0]);
+                  sts_32(at + 8, mid[0]);
+                  sts_32(high_at, high[0]);
+                } else {
+                  ptx::sts_128(at, low[0], low[1], mid[0], mid[1]);
+                  sts_64(high_at, high[0], high[1]);
+                }
+              }
             }
           }
           ptx::fence_proxy_async_smem();
@@ -678,8 +727,8 @@ attention_kernel(const AttentionArgs a) {
             for (int k = 0; k < S::kBlocks; ++k)
 #pragma unroll
               for (int t = 0; t < 4; ++t)                                  // 32 tokens each
-                mma_u8(sum_tmem + k * S::kWeightCols, ptx::smem_desc(values + k * 16384 + t * 4096),
-                       weight_desc(weights + k * (S::kWeightUnits * 2048) + t * 512), kSumDesc | ((uint32_t)(S::kWeightCols / 8) << 17),
+                mma_u8(sum_tmem + k * S::kWeightCols, values_desc + ((k * 16384 + t * 4096) >> 4),
+                       weights_desc + ((k * (S::kWeightUnits * 2048) + t * 512) >> 4), kSumDesc | ((uint32_t)(S::kWeightCols / 8) << 17),
                        since > 0 || t > 0);
             ptx::mma_commit(ptx::smem_addr(&ctl->sums_done));
           }
@@ -709,6 +758,14 @@ attention_kernel(const AttentionArgs a) {
       empty_sums();
     }
 
+    // the next segment is on its way while this one is finished
+    const Job done = job;
+    more = x < x_end;
+    if (more) {
+      job = next_job();
+      page = page_of(job, 0);
+    }
+
     // ---- sums over the tokens: every thread's values side by side, then a warp per row of them
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
@@ -724,6 +781,7 @@ attention_kernel(const AttentionArgs a) {
       for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
       if (lane == 0) ctl->sums[n / kRows][n % kRows] = sum;
     }
+    if (more) fetch_first(job);
     __syncthreads();
     // elements to their places: byte tid of a row is element 32 (tid / 32) + 2 (tid % 16) + (tid / 16 % 2)
 #pragma unroll
@@ -736,29 +794,28 @@ attention_kernel(const AttentionArgs a) {
     }
     __syncthreads();
     // a piece that starts inside the segment goes to the worker's first slot, one that ends inside it to the second
-    const int64_t part_slot = 2 * (int64_t)blockIdx.x + (u0 == 0 ? 1 : 0);
-    for (int r = warp; r < sg.rows; r += kWarps) {
+    const int64_t part_slot = 2 * (int64_t)blockIdx.x + (done.u0 == 0 ? 1 : 0);
+    for (int r = warp; r < done.sg.rows; r += kWarps) {
       const float m = ctl->shift[r], l = ctl->sums[0][r];
-      const int row = sg.first_row + r, new_token = token_of_row(a, row);
-      const int64_t out_row = w.rows.first + new_token;
-      const int q_head = head * a.ratio + row - new_token * a.ratio;
+      const int row = done.sg.first_row + r, new_token = token_of_row(a, row);
+      const int64_t out_row = done.rows.first + new_token;
+      const int q_head = done.head * a.ratio + row - new_token * a.ratio;
       const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
       eqat_bf16* to = a.O + out_row * a.o_pitch + (int64_t)q_head * D;
-      float* part = whole ? nullptr : a.partial + (part_slot * kRows + r) * (D + 4);
+      float* part = done.whole ? nullptr : a.partial + (part_slot * kRows + r) * (D + 4);
 #pragma unroll
       for (int p = lane; p < D / 4; p += 32) {
         const float4 e = *reinterpret_cast<const float4*>(meet + r * D + p * 4);
-        if (whole) *reinterpret_cast<uint2*>(to + p * 4) = make_uint2(pack_bf16x2(e.x * inv, e.y * inv), pack_bf16x2(e.z * inv, e.w * inv));
+        if (done.whole) *reinterpret_cast<uint2*>(to + p * 4) = make_uint2(pack_bf16x2(e.x * inv, e.y * inv), pack_bf16x2(e.z * inv, e.w * inv));
         else *reinterpret_cast<float4*>(part + p * 4) = e;
       }
       if (lane == 0) {
-        if (!whole) *reinterpret_cast<float2*>(part + D) = make_float2(m, l);
+        if (!done.whole) *reinterpret_cast<float2*>(part + D) = make_float2(m, l);
         else if (a.lse != nullptr)
           a.lse[out_row * a.q_heads + q_head] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
       }
     }
     __syncthreads();                                                     // the operands may be written again
-    x += u1 - u0;
   }
   ptx::grid_dependents_launch();
   ptx::tc_fence_before();
@@ -772,9 +829,9 @@ attention_kernel(const AttentionArgs a) {
 
 // Joins the segments that workers share, in the order of the workers: a CTA per worker that starts a segment and does not
 // finish it, a warp per row.
-template <int D, int G, int NB>
+template <int D, int G, int ROWS>
 __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const AttentionArgs a) {
-  using S = Shape<D, G, NB>;
+  using S = Shape<D, G, ROWS>;
   constexpr int kFours = D / 128 > 0 ? D / 128 : 1;                      // float4 of a lane
   ptx::grid_dependency_wait();
   ptx::grid_dependents_launch();
@@ -835,36 +892,39 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Atte
 }
 
 // ------------------------------------------------------------------ host side
-// Blocks of eight query rows that a tile of the cache is read for: as many as the longest sequence's rows fill, as far as
-// accumulators and a thread's sums have room (32 rows x groups).
-int row_blocks(const eqat_cache_desc& d, const eqat_attention_desc& a) {
+// Query rows that a tile of the cache is read for: as many as the longest sequence has, as far as accumulators and a thread's
+// sums have room (32 rows x groups).
+int tile_rows(const eqat_cache_desc& d, const eqat_attention_desc& a) {
   const int64_t rows = (int64_t)a.max_new * (a.q_heads / d.kv_heads);
-  const int groups = d.head_dim / d.group, most = d.head_dim == 256 && groups == 2 ? 1 : groups >= 4 ? 1 : groups == 2 ? 2 : 4;
-  int nb = 1;
-  while (nb < most && 8 * nb < rows) nb *= 2;
-  return nb;
+  const int groups = d.head_dim / d.group, most = groups >= 4 || d.head_dim == 256 ? 8 : groups == 2 ? 16 : 32;
+  if (rows == 1) return 1;
+  int n = 4;
+  while (n < most && n < rows) n *= 2;
+  return n;
 }
 
 template <typename F>
-int with_shape(const eqat_cache_desc& d, int nb, F&& f) {
+int with_shape(const eqat_cache_desc& d, int rows, F&& f) {
   const int g = d.head_dim / d.group;
-#define EQAT_SHAPE(DD, GG, NN)                          \
-  if (d.head_dim == DD && g == GG && nb == NN)          \
-    return f(std::integral_constant<int, DD>(), std::integral_constant<int, GG>(), std::integral_constant<int, NN>());
-  EQAT_SHAPE(64, 1, 1)
-  EQAT_SHAPE(64, 1, 2)
-  EQAT_SHAPE(64, 1, 4)
-  EQAT_SHAPE(64, 2, 1)
-  EQAT_SHAPE(64, 2, 2)
-  EQAT_SHAPE(128, 1, 1)
-  EQAT_SHAPE(128, 1, 2)
-  EQAT_SHAPE(128, 1, 4)
-  EQAT_SHAPE(128, 2, 1)
-  EQAT_SHAPE(128, 2, 2)
-  EQAT_SHAPE(128, 4, 1)
-  EQAT_SHAPE(256, 2, 1)
-  EQAT_SHAPE(256, 4, 1)
-  EQAT_SHAPE(256, 8, 1)
+#define EQAT_SHAPE(DD, GG, RR)                            \
+  if (d.head_dim == DD && g == GG && rows == RR)          \
+    return f(std::integral_constant<int, DD>(), std::integral_constant<int, GG>(), std::integral_constant<int, RR>());
+#define EQAT_SHAPES(DD, GG) EQAT_SHAPE(DD, GG, 1) EQAT_SHAPE(DD, GG, 4) EQAT_SHAPE(DD, GG, 8)
+  EQAT_SHAPES(64, 1)
+  EQAT_SHAPE(64, 1, 16)
+  EQAT_SHAPE(64, 1, 32)
+  EQAT_SHAPES(64, 2)
+  EQAT_SHAPE(64, 2, 16)
+  EQAT_SHAPES(128, 1)
+  EQAT_SHAPE(128, 1, 16)
+  EQAT_SHAPE(128, 1, 32)
+  EQAT_SHAPES(128, 2)
+  EQAT_SHAPE(128, 2, 16)
+  EQAT_SHAPES(128, 4)
+  EQAT_SHAPES(256, 2)
+  EQAT_SHAPES(256, 4)
+  EQAT_SHAPES(256, 8)
+#undef EQAT_SHAPES
 #undef EQAT_SHAPE
   return EQAT_ERR_UNSUPPORTED;
 }
@@ -900,7 +960,7 @@ int workers_of(const eqat_cache_desc& d, const eqat_attention_desc& a, int sms) 
 size_t cache_attention_workspace(const eqat_cache_desc& d, const eqat_attention_desc& a) {
   const int sms = sm_count();
   size_t bytes = (size_t)-1;
-  with_shape(d, row_blocks(d, a), [&](auto D, auto G, auto NT) {
+  with_shape(d, tile_rows(d, a), [&](auto D, auto G, auto NT) {
     using S = Shape<decltype(D)::value, decltype(G)::value, decltype(NT)::value>;
     const int w = workers_of<S>(d, a, sms > 0 ? sms : 148);
     bytes = w > 1 ? (size_t)w * (sizeof(JoinRecord) + (size_t)2 * S::kRows * (decltype(D)::value + 4) * sizeof(float)) : 0;
@@ -913,7 +973,7 @@ int launch_cache_attention(const eqat_cache_desc& d, const eqat_attention_desc& 
                            const CacheView& view, eqat_bf16* O, int64_t o_pitch, float* lse, void* workspace, cudaStream_t st) {
   const int sms = sm_count();
   if (sms <= 0) return EQAT_ERR_CUDA;
-  return with_shape(d, row_blocks(d, at), [&](auto DD, auto GG, auto NN) {
+  return with_shape(d, tile_rows(d, at), [&](auto DD, auto GG, auto NN) {
     constexpr int D = decltype(DD)::value, G = decltype(GG)::value, NT = decltype(NN)::value;
     using S = Shape<D, G, NT>;
     AttentionArgs a{};
