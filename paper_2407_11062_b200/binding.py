@@ -9,6 +9,7 @@ this module raises.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 from ctypes import POINTER, Structure, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 
@@ -107,6 +108,22 @@ def _load():
 
 lib = _load()
 LIB_PATH = _LIB_PATH
+
+
+def _load_marshal():
+    path = os.path.join(os.path.dirname(_LIB_PATH), "_marshal.so")
+    if not os.path.exists(path):
+        raise ImportError(f"{path} is missing: build it with `python -m paper_2407_11062_b200.build`")
+    spec = importlib.util.spec_from_file_location("paper_2407_11062_b200._marshal", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    module.bind(*[ctypes.cast(f, c_void_p).value for f in (lib.eqat_cache_append, lib.eqat_cache_read, lib.eqat_cache_attention)])
+    return module
+
+
+# The cache's calls, made for every block and token, are marshalled by compiled code (csrc/marshal.cpp): nine to eleven
+# tensors a call took the interpreter 6 us.
+_marshal = _load_marshal()
 
 
 def status_string(status: int) -> str:
@@ -269,18 +286,6 @@ def make_attention_desc(q_heads, max_new, scale, window=0) -> eqat_attention_des
     return eqat_attention_desc(int(q_heads), int(max_new), float(scale), int(window))
 
 
-def _row_ptr(t):
-    """Address and row pitch of a [rows, heads, head_dim] tensor whose heads and elements are dense."""
-    if not t.is_cuda or t.dim() != 3 or t.stride(2) != 1 or t.stride(1) != t.size(2):
-        raise ValueError("expected a CUDA tensor [rows, heads, head_dim] with dense heads")
-    return t.data_ptr(), t.stride(0) if t.size(0) > 1 else max(t.stride(0), t.size(1) * t.size(2))
-
-
-def _pool(cache):
-    """`cache`: k_codes, k_params, v_codes, v_params."""
-    return ctypes.byref(eqat_cache(*[_ptr(t) for t in cache]))
-
-
 def cache_workspace_bytes(desc, attn) -> int:
     n = lib.eqat_cache_workspace_bytes(ctypes.byref(desc), ctypes.byref(attn))
     if n == ctypes.c_size_t(-1).value:
@@ -288,27 +293,20 @@ def cache_workspace_bytes(desc, attn) -> int:
     return int(n)
 
 
+# `cache`: (k_codes, k_params, v_codes, v_params).  Row tensors are [rows, heads, head_dim] with dense heads, rows of any pitch.
 def eqat_cache_append(desc, K, V, row_offsets, lengths, page_table, cache, K_hat=None, V_hat=None):
-    """K, V: [rows, kv_heads, head_dim], rows of any pitch.  K_hat, V_hat (or None): what the cache now holds for them."""
-    k, k_pitch = _row_ptr(K)
-    v, v_pitch = _row_ptr(V)
-    _check(lib.eqat_cache_append(ctypes.byref(desc), k, k_pitch, v, v_pitch, _ptr(row_offsets), _ptr(lengths),
-                                 _ptr(page_table), _pool(cache), _ptr(K_hat), _ptr(V_hat), _stream()),
-           "eqat_cache_append")
+    """K_hat, V_hat (or None): what the cache now holds for K and V."""
+    _check(_marshal.cache_append(desc, K, V, row_offsets, lengths, page_table, cache, K_hat, V_hat), "eqat_cache_append")
 
 
 def eqat_cache_read(desc, row_offsets, lengths, page_table, cache, K_hat, V_hat):
-    _check(lib.eqat_cache_read(ctypes.byref(desc), _ptr(row_offsets), _ptr(lengths), _ptr(page_table), _pool(cache),
-                               _ptr(K_hat), _ptr(V_hat), _stream()), "eqat_cache_read")
+    _check(_marshal.cache_read(desc, row_offsets, lengths, page_table, cache, K_hat, V_hat), "eqat_cache_read")
 
 
 def eqat_cache_attention(desc, attn, Q, row_offsets, lengths, page_table, cache, O, lse=None, workspace=None):
-    """Q, O: [rows, q_heads, head_dim], rows of any pitch.  lse (or None): [rows, q_heads] fp32."""
-    q, q_pitch = _row_ptr(Q)
-    o, o_pitch = _row_ptr(O)
-    _check(lib.eqat_cache_attention(ctypes.byref(desc), ctypes.byref(attn), q, q_pitch, _ptr(row_offsets), _ptr(lengths),
-                                    _ptr(page_table), _pool(cache), o, o_pitch, _ptr(lse), _ptr(workspace),
-                                    _nbytes(workspace), _stream()), "eqat_cache_attention")
+    """lse (or None): [rows, q_heads] fp32."""
+    _check(_marshal.cache_attention(desc, attn, Q, row_offsets, lengths, page_table, cache, O, lse, workspace),
+           "eqat_cache_attention")
 
 
 def _nbytes(t):

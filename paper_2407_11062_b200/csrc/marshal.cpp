@@ -1,0 +1,180 @@
+// Argument marshalling of the calls that a decoding step makes for every block and token: tensors to the device pointers of
+// the C ABI, in one call into compiled code.  The interpreter took 6 of the 9 to 13 us of host time of such a call to ask
+// nine to eleven tensors for their addresses, more than the kernels run for one user's step.
+//
+// Nothing is computed here.  The addresses of the library's entry points are handed over by the binding (bind), so this
+// module links against neither library; statuses go back as they are.
+#define PY_SSIZE_T_CLEAN
+#include <Python.h>
+
+#include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include "eqat.h"
+
+namespace {
+
+decltype(&eqat_cache_append) g_append = nullptr;
+decltype(&eqat_cache_read) g_read = nullptr;
+decltype(&eqat_cache_attention) g_attention = nullptr;
+
+struct Refused {};                                   // the Python error is set
+
+const at::Tensor& tensor(PyObject* o) {
+  if (!THPVariable_Check(o)) {
+    PyErr_SetString(PyExc_TypeError, "expected a tensor");
+    throw Refused();
+  }
+  return THPVariable_Unpack(o);
+}
+
+// Address of a contiguous CUDA tensor; None: NULL.
+void* pointer(PyObject* o, size_t* bytes = nullptr) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o);
+  if (!t.is_cuda() || !t.is_contiguous()) {
+    PyErr_SetString(PyExc_ValueError, "expected a contiguous CUDA tensor");
+    throw Refused();
+  }
+  if (bytes != nullptr) *bytes = t.nbytes();
+  return t.data_ptr();
+}
+
+// Address and row pitch of a [rows, heads, head_dim] tensor whose heads and elements are dense.
+template <typename T>
+T* rows(PyObject* o, int64_t* pitch) {
+  const at::Tensor& t = tensor(o);
+  if (!t.is_cuda() || t.dim() != 3 || t.stride(2) != 1 || t.stride(1) != t.size(2)) {
+    PyErr_SetString(PyExc_ValueError, "expected a CUDA tensor [rows, heads, head_dim] with dense heads");
+    throw Refused();
+  }
+  const int64_t least = t.size(1) * t.size(2);
+  *pitch = t.size(0) > 1 || t.stride(0) > least ? t.stride(0) : least;
+  return static_cast<T*>(t.data_ptr());
+}
+
+// A descriptor of the binding (a ctypes structure).
+template <typename T>
+T structure(PyObject* o) {
+  Py_buffer view;
+  if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) throw Refused();
+  T value;
+  const bool fits = view.len == (Py_ssize_t)sizeof(T);
+  if (fits) memcpy(&value, view.buf, sizeof(T));
+  PyBuffer_Release(&view);
+  if (!fits) {
+    PyErr_SetString(PyExc_TypeError, "expected another descriptor");
+    throw Refused();
+  }
+  return value;
+}
+
+eqat_cache pool(PyObject* o) {
+  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) {
+    PyErr_SetString(PyExc_TypeError, "expected a cache: (k_codes, k_params, v_codes, v_params)");
+    throw Refused();
+  }
+  return eqat_cache{static_cast<uint8_t*>(pointer(PyTuple_GET_ITEM(o, 0))), static_cast<eqat_bf16*>(pointer(PyTuple_GET_ITEM(o, 1))),
+                    static_cast<uint8_t*>(pointer(PyTuple_GET_ITEM(o, 2))), static_cast<eqat_bf16*>(pointer(PyTuple_GET_ITEM(o, 3)))};
+}
+
+template <typename F>
+PyObject* call(Py_ssize_t given, Py_ssize_t wanted, F&& f) {
+  if (given != wanted || g_append == nullptr) {
+    PyErr_SetString(PyExc_TypeError, "wrong number of arguments, or called before bind()");
+    return nullptr;
+  }
+  try {
+    return PyLong_FromLong(f());
+  } catch (const Refused&) {
+    return nullptr;
+  } catch (const std::exception& e) {                // a tensor without storage, no CUDA device
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
+template <typename F>
+int launch(F&& f) {
+  void* stream = c10::cuda::getCurrentCUDAStream().stream();
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = f(stream);
+  Py_END_ALLOW_THREADS
+  return rc;
+}
+
+const int32_t* index_of(PyObject* o) { return static_cast<const int32_t*>(pointer(o)); }
+eqat_bf16* bf16_of(PyObject* o) { return static_cast<eqat_bf16*>(pointer(o)); }
+
+PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 3) {
+    PyErr_SetString(PyExc_TypeError, "bind(append, read, attention)");
+    return nullptr;
+  }
+  void* p[3];
+  for (int i = 0; i < 3; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (p[i] == nullptr) {
+      if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "an address is 0");
+      return nullptr;
+    }
+  }
+  g_read = reinterpret_cast<decltype(g_read)>(p[1]);
+  g_attention = reinterpret_cast<decltype(g_attention)>(p[2]);
+  g_append = reinterpret_cast<decltype(g_append)>(p[0]);
+  Py_RETURN_NONE;
+}
+
+// desc, K, V, row_offsets, lengths, page_table, cache, K_hat, V_hat
+PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 9, [&] {
+    const auto d = structure<eqat_cache_desc>(a[0]);
+    int64_t kp, vp;
+    const auto *K = rows<eqat_bf16>(a[1], &kp), *V = rows<eqat_bf16>(a[2], &vp);
+    const int32_t *off = index_of(a[3]), *len = index_of(a[4]), *table = index_of(a[5]);
+    const eqat_cache c = pool(a[6]);
+    eqat_bf16 *kh = bf16_of(a[7]), *vh = bf16_of(a[8]);
+    return launch([&](void* s) { return g_append(&d, K, kp, V, vp, off, len, table, &c, kh, vh, s); });
+  });
+}
+
+// desc, row_offsets, lengths, page_table, cache, K_hat, V_hat
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 7, [&] {
+    const auto d = structure<eqat_cache_desc>(a[0]);
+    const int32_t *off = index_of(a[1]), *len = index_of(a[2]), *table = index_of(a[3]);
+    const eqat_cache c = pool(a[4]);
+    eqat_bf16 *kh = bf16_of(a[5]), *vh = bf16_of(a[6]);
+    return launch([&](void* s) { return g_read(&d, off, len, table, &c, kh, vh, s); });
+  });
+}
+
+// desc, attn, Q, row_offsets, lengths, page_table, cache, O, lse, workspace
+PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 10, [&] {
+    const auto d = structure<eqat_cache_desc>(a[0]);
+    const auto t = structure<eqat_attention_desc>(a[1]);
+    int64_t qp, op;
+    const auto* Q = rows<eqat_bf16>(a[2], &qp);
+    const int32_t *off = index_of(a[3]), *len = index_of(a[4]), *table = index_of(a[5]);
+    const eqat_cache c = pool(a[6]);
+    auto* O = rows<eqat_bf16>(a[7], &op);
+    float* lse = static_cast<float*>(pointer(a[8]));
+    size_t bytes = 0;
+    void* ws = pointer(a[9], &bytes);
+    return launch([&](void* s) { return g_attention(&d, &t, Q, qp, off, len, table, &c, O, op, lse, ws, bytes, s); });
+  });
+}
+
+PyMethodDef g_methods[] = {
+    {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind)), METH_FASTCALL, "addresses of the library's entry points"},
+    {"cache_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_append)), METH_FASTCALL, "eqat_cache_append"},
+    {"cache_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_read)), METH_FASTCALL, "eqat_cache_read"},
+    {"cache_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_attention)), METH_FASTCALL, "eqat_cache_attention"},
+    {nullptr, nullptr, 0, nullptr}};
+PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling of the cache's calls", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__marshal(void) { return PyModule_Create(&g_module); }

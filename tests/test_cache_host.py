@@ -170,7 +170,20 @@ def test_workspace_is_asked_for(eqat):
         assert attention(eqat, d, a, **kw) == eqat.EQAT_ERR_WORKSPACE
 
 
-def test_the_binding_takes_rows_of_any_pitch_and_nothing_else(eqat):
+def test_the_binding_refuses_what_is_no_row_tensor(eqat):
+    """Decided before the library is called: tensors that are not on a GPU, no tensors, another descriptor, no cache."""
     import torch
+    d, a = desc(eqat), eqat.make_attention_desc(64, 1, 0.1)
+    x, i = torch.zeros(4, 8, 128, dtype=torch.bfloat16), torch.zeros(5, dtype=torch.int32)
     with pytest.raises(ValueError):
-        eqat._row_ptr(torch.zeros(2, 3, 64))                 # not on a GPU
+        eqat.eqat_cache_append(d, x, x, i, i, i, (i, i, i, i))
+    with pytest.raises(ValueError):
+        eqat.eqat_cache_read(d, i, i, i, (i, i, i, i), x, x)
+    with pytest.raises(ValueError):
+        eqat.eqat_cache_attention(d, a, x, i, i, i, (i, i, i, i), x)
+    for bad in ((a, x, x, i, i, i, (i, i, i, i)), (d, 1, x, i, i, i, (i, i, i, i)), (d, x, None, i, i, i, (i, i, i, i))):
+        with pytest.raises((TypeError, ValueError)):
+            eqat.eqat_cache_append(*bad)
+    for cache in (None, [i, i, i, i], (i, i, i)):
+        with pytest.raises((TypeError, ValueError)):
+            eqat.eqat_cache_read(d, None, None, None, cache, None, None)
