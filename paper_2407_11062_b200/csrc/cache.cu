@@ -58,117 +58,143 @@ struct Rows {
   eqat_bf16 *K_hat, *V_hat;                          // append: may be NULL
 };
 
-// GL: lanes of a group (group / 8).
-template <int GL, bool APPEND>
-__global__ void __launch_bounds__(kWarps * 32) cache_rows_kernel(const CacheView v, const Rows rows, int head_shift, int pieces) {
+// bf16 128 + q with a code in the last mantissa bits of each half, to q s + m, rounded once.
+__device__ __forceinline__ uint32_t value_pair(uint32_t codes, __nv_bfloat162 s, __nv_bfloat162 m) {
+  return as_word(__hfma2(__hsub2(as_pair(codes | 0x43004300u), as_pair(0x43004300u)), s, m));
+}
+
+// Keys (even blockIdx.y) or values of the rows, blockIdx.y / 2 says which `per` pieces of a row.
+template <int D, int GROUP, bool APPEND>
+__global__ void __launch_bounds__(kWarps * 32) cache_rows_kernel(const CacheView v, const Rows rows, int per) {
+  constexpr int kHead = D / 8, kLanes = GROUP / 8, kGroups = D / GROUP;    // vectors of a head, of a group
   ptx::grid_dependency_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t items = (int64_t)v.rows * 2 * pieces, step = (int64_t)gridDim.x * kWarps;
-  const int vectors = v.kv_heads << (head_shift - 3);                      // of a row
-  const int head_groups = 1 << (head_shift - 3 - (GL == 4 ? 2 : GL == 8 ? 3 : 4));
-  for (int64_t item = (int64_t)blockIdx.x * kWarps + warp; item < items; item += step) {
-    if (item + step >= items) ptx::grid_dependents_launch();
-    const int piece = (int)(item % pieces);
-    const int which = (int)(item / pieces % 2);                            // keys or values
-    const int row = (int)(item / pieces / 2);
-    const int first = piece * (32 * kVectors) + lane;
+  const int vectors = v.kv_heads * kHead;                                  // of a row
+  const bool keys = (blockIdx.y & 1) == 0;
+  const int from = (int)(blockIdx.y >> 1) * per * (32 * kVectors), upto = min(from + per * (32 * kVectors), vectors);
+  uint32_t* const codes = reinterpret_cast<uint32_t*>(keys ? v.kq : v.vq);
+  uint32_t* const params = keys ? v.kp : v.vp;
+  const eqat_bf16* const in = keys ? rows.K : rows.V;
+  const int64_t pitch = keys ? rows.k_pitch : rows.v_pitch;
+  uint4* const hat = reinterpret_cast<uint4*>(keys ? rows.K_hat : rows.V_hat);
+  const int step = (int)gridDim.x * kWarps;
+  for (int row = (int)blockIdx.x * kWarps + warp; row < v.rows; row += step) {
+    if (row >= v.rows - step) ptx::grid_dependents_launch();
+    const uint4* x_at = reinterpret_cast<const uint4*>(in + row * pitch) + lane;
     uint4 x[kVectors] = {};
-    if (APPEND) {
-      const uint4* from = reinterpret_cast<const uint4*>(which == 0 ? rows.K + row * rows.k_pitch : rows.V + row * rows.v_pitch);
+    auto load = [&](int at) {
 #pragma unroll
       for (int u = 0; u < kVectors; ++u)
-        if (first + 32 * u < vectors) x[u] = ptx::ld_global(from + first + 32 * u);
-    }
-    const RowPlace place = place_of(v, row, lane);
-    uint8_t* codes = which == 0 ? v.kq : v.vq;
-    uint32_t* params = which == 0 ? v.kp : v.vp;
-    uint4* out = reinterpret_cast<uint4*>(which == 0 ? rows.K_hat : rows.V_hat);
-    if (out != nullptr) out += (int64_t)row * vectors;
-    auto slot = [&](int vec) { return place.token + (int64_t)(vec >> (head_shift - 3)) * v.page_size; };
-    auto code_at = [&](int vec) {
-      return reinterpret_cast<uint32_t*>(codes) + (slot(vec) << (head_shift - 3)) + (vec & ((1 << (head_shift - 3)) - 1));
+        if (at + 32 * u + lane < upto) x[u] = ptx::ld_global(x_at + at + 32 * u);
     };
-    auto param_at = [&](int vec) { return params + slot(vec) * head_groups + (vec & ((1 << (head_shift - 3)) - 1)) / GL; };
-
-    if (APPEND) {
+    if (APPEND) load(from);
+    const RowPlace place = place_of(v, row, lane);
+    if (!place.owned) continue;
+    uint4* const out = hat == nullptr ? nullptr : hat + (int64_t)row * vectors + lane;
+    for (int at = from; at < upto; at += 32 * kVectors) {
+      // vector at + 32 u + lane: a head further in the pool every kHead vectors
+      const int64_t slot = place.token + (int64_t)((at + lane) / kHead) * v.page_size;
+      const int64_t next = (int64_t)(32 / kHead) * v.page_size;
+      uint32_t* const code_at = codes + slot * kHead + lane % kHead;
+      uint32_t* const param_at = params + slot * kGroups + lane % kHead / kLanes;
+      if (APPEND) {
 #pragma unroll
-      for (int u = 0; u < kVectors; ++u) {
-        const int vec = first + 32 * u;
-        if (piece * (32 * kVectors) + 32 * u >= vectors) break;            // the whole warp
-        const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-        // the NaN forms hand a NaN on
-        const __nv_bfloat162 lo = __hmin2_nan(__hmin2_nan(as_pair(w[0]), as_pair(w[1])), __hmin2_nan(as_pair(w[2]), as_pair(w[3])));
-        const __nv_bfloat162 hi = __hmax2_nan(__hmax2_nan(as_pair(w[0]), as_pair(w[1])), __hmax2_nan(as_pair(w[2]), as_pair(w[3])));
-        __nv_bfloat162 range = __halves2bfloat162(__hmax_nan(__low2bfloat16(hi), __high2bfloat16(hi)),
-                                                  __hneg(__hmin_nan(__low2bfloat16(lo), __high2bfloat16(lo))));
+        for (int u = 0; u < kVectors; ++u) {
+          const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+          // the NaN forms hand a NaN on
+          const __nv_bfloat162 lo = __hmin2_nan(__hmin2_nan(as_pair(w[0]), as_pair(w[1])), __hmin2_nan(as_pair(w[2]), as_pair(w[3])));
+          const __nv_bfloat162 hi = __hmax2_nan(__hmax2_nan(as_pair(w[0]), as_pair(w[1])), __hmax2_nan(as_pair(w[2]), as_pair(w[3])));
+          // (maximum, -minimum)
+          __nv_bfloat162 range = __hmax2_nan(as_pair(__byte_perm(as_word(hi), as_word(lo) ^ 0x80008000u, 0x5410)),
+                                             as_pair(__byte_perm(as_word(hi), as_word(lo) ^ 0x80008000u, 0x7632)));
 #pragma unroll
-        for (int d = 1; d < GL; d <<= 1) range = __hmax2_nan(range, as_pair(__shfl_xor_sync(0xFFFFFFFFu, as_word(range), d)));
-        const float most = __low2float(range), least = -__high2float(range);
-        float s = __bfloat162float(__float2bfloat16_rn(__fmul_rn(__fsub_rn(most, least), 1.0f / 15.0f)));
-        if (s < kStepMin) s = 0.0f;
-        if (!(s < __int_as_float(0x7F800000))) s = __int_as_float(0x7FC00000);
-        const float inverse = s > 0.0f ? __frcp_rn(s) : 0.0f;
-        // With s rounded by at most 2^-8 of itself a quotient stays below 15.06: no code leaves 0 .. 15.
-        uint32_t word = 0;
-        uint32_t value[4];
+          for (int d = 1; d < kLanes; d <<= 1) range = __hmax2_nan(range, as_pair(__shfl_xor_sync(0xFFFFFFFFu, as_word(range), d)));
+          const float most = __low2float(range), least = -__high2float(range);
+          float s = __bfloat162float(__float2bfloat16_rn(__fmul_rn(__fsub_rn(most, least), 1.0f / 15.0f)));
+          if (s < kStepMin) s = 0.0f;
+          if (!(s < __int_as_float(0x7F800000))) s = __int_as_float(0x7FC00000);
+          const float inverse = s > 0.0f ? __frcp_rn(s) : 0.0f;
+          // A code is the low bits of (x - m) / s + 1.5 * 2^23.  With s rounded by at most 2^-8 of itself a quotient stays below
+          // 15.06, so no code leaves 0 .. 15 (unless something is NaN).  The word is the sum of the shifted bit patterns,
+          // less those of the constant.
+          float t[8];
+          uint32_t word = 0;
 #pragma unroll
-        for (int i = 3; i >= 0; --i) {
-          const float even = __fadd_rn(__fmul_rn(__fsub_rn(__uint_as_float(w[i] << 16), least), inverse), kMagic);
-          const float odd = __fadd_rn(__fmul_rn(__fsub_rn(__uint_as_float(w[i] & 0xFFFF0000u), least), inverse), kMagic);
-          word = (word << 8) | ((__float_as_uint(odd) & 15u) << 4) | (__float_as_uint(even) & 15u);
-          value[i] = pack_bf16x2(fmaf(even - kMagic, s, least), fmaf(odd - kMagic, s, least));
-        }
-        if (vec < vectors && place.stands) {
-          *code_at(vec) = word;
-          if ((vec & (GL - 1)) == 0) *param_at(vec) = (__float_as_uint(s) >> 16) | (__float_as_uint(least) & 0xFFFF0000u);
-          if (out != nullptr) out[vec] = make_uint4(value[0], value[1], value[2], value[3]);
-        } else if (vec < vectors && place.owned && out != nullptr) {
-          out[vec] = make_uint4(0u, 0u, 0u, 0u);
-        }
-      }
-    } else if (place.owned) {
-      uint32_t word[kVectors] = {}, param[kVectors] = {};
-      if (place.stands) {
-#pragma unroll
-        for (int u = 0; u < kVectors; ++u)
-          if (first + 32 * u < vectors) {
-            word[u] = ptx::ld_global(static_cast<const uint32_t*>(code_at(first + 32 * u)));
-            param[u] = ptx::ld_global(static_cast<const uint32_t*>(param_at(first + 32 * u)));
+          for (int i = 0; i < 4; ++i) {
+            t[2 * i] = __fadd_rn(__fmul_rn(__fsub_rn(__uint_as_float(w[i] << 16), least), inverse), kMagic);
+            t[2 * i + 1] = __fadd_rn(__fmul_rn(__fsub_rn(__uint_as_float(w[i] & 0xFFFF0000u), least), inverse), kMagic);
           }
-      }
 #pragma unroll
-      for (int u = 0; u < kVectors; ++u) {
-        const float s = param_step(param[u]), least = param_low(param[u]);
-        uint32_t value[4];
+          for (int i = 7; i >= 0; --i) word = word * 16 + __float_as_uint(t[i]);
+          word -= 0x3F400000u;                                             // 0x4B400000 (1 + 16 + ... + 16^7) mod 2^32
+          if (at + 32 * u + lane < upto) {
+            if (place.stands) {
+              code_at[u * next * kHead] = word;
+              if (lane % kLanes == 0) param_at[u * next * kGroups] = (__float_as_uint(s) >> 16) | (__float_as_uint(least) & 0xFFFF0000u);
+            }
+            if (out != nullptr) {
+              const __nv_bfloat162 s2 = __float2bfloat162_rn(s), m2 = __float2bfloat162_rn(least);
+              uint32_t y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          value[i] = pack_bf16x2(fmaf((float)((word[u] >> (8 * i)) & 15u), s, least), fmaf((float)((word[u] >> (8 * i + 4)) & 15u), s, least));
-        if (first + 32 * u < vectors) out[first + 32 * u] = make_uint4(value[0], value[1], value[2], value[3]);
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t pair = __byte_perm(__float_as_uint(t[2 * i]), __float_as_uint(t[2 * i + 1]), 0x5410);
+                y[i] = place.stands ? value_pair(pair, s2, m2) : 0u;
+              }
+              out[at + 32 * u] = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+          }
+        }
+        if (at + 32 * kVectors < upto) load(at + 32 * kVectors);
+      } else {
+        uint32_t word[kVectors] = {}, param[kVectors] = {};
+        if (place.stands) {
+#pragma unroll
+          for (int u = 0; u < kVectors; ++u)
+            if (at + 32 * u + lane < upto) {
+              word[u] = ptx::ld_global(static_cast<const uint32_t*>(code_at + u * next * kHead));
+              param[u] = ptx::ld_global(static_cast<const uint32_t*>(param_at + u * next * kGroups));
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kVectors; ++u) {
+          const __nv_bfloat162 s2 = as_pair(__byte_perm(param[u], 0, 0x1010)), m2 = as_pair(__byte_perm(param[u], 0, 0x3232));
+          uint32_t y[4];                                                   // codes i and i + 4
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = value_pair((word[u] >> (4 * i)) & 0x000F000Fu, s2, m2);
+          if (at + 32 * u + lane < upto)
+            out[at + 32 * u] = make_uint4(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410), __byte_perm(y[0], y[1], 0x7632),
+                                          __byte_perm(y[2], y[3], 0x7632));
+        }
       }
     }
   }
-}
-
-inline int log2_of(int v) {
-  int s = 0;
-  while ((1 << s) < v) ++s;
-  return s;
 }
 
 template <bool APPEND>
 int launch_rows(const eqat_cache_desc& d, const CacheView& view, const Rows& rows, cudaStream_t st) {
-  const int vectors = d.kv_heads * d.head_dim / 8, pieces = (vectors + 32 * kVectors - 1) / (32 * kVectors);
-  const int64_t blocks = (d.rows * 2 * pieces + kWarps - 1) / kWarps;
   const int sms = sm_count();
   if (sms <= 0) return EQAT_ERR_CUDA;
-  const int64_t most = (int64_t)sms * 8;                                   // 64 warps an SM
-  const dim3 grid((unsigned)(blocks < most ? blocks : most));
-  const int shift = log2_of(d.head_dim);
-  switch (d.group) {
-    case 32: return launch_overlapped(cache_rows_kernel<4, APPEND>, grid, dim3(kWarps * 32), 0, st, view, rows, shift, pieces);
-    case 64: return launch_overlapped(cache_rows_kernel<8, APPEND>, grid, dim3(kWarps * 32), 0, st, view, rows, shift, pieces);
-    default: return launch_overlapped(cache_rows_kernel<16, APPEND>, grid, dim3(kWarps * 32), 0, st, view, rows, shift, pieces);
-  }
+  // A warp takes a whole row where there are enough of them, a piece of one otherwise.
+  const int pieces = (d.kv_heads * d.head_dim / 8 + 32 * kVectors - 1) / (32 * kVectors);
+  const int64_t warps = (int64_t)sms * 64;
+  int per = (int)(d.rows * 2 * pieces / warps);
+  per = per < 1 ? 1 : per > pieces ? pieces : per;
+  const int groups = (pieces + per - 1) / per;
+  if (groups > 32767) return EQAT_ERR_SHAPE;
+  const int64_t blocks = (d.rows + kWarps - 1) / kWarps, most = (warps / kWarps + 2 * groups - 1) / (2 * groups);
+  const dim3 grid((unsigned)(blocks < most ? blocks : most), (unsigned)(2 * groups));
+#define EQAT_ROWS(DD, GG) \
+  if (d.head_dim == DD && d.group == GG) return launch_overlapped(cache_rows_kernel<DD, GG, APPEND>, grid, dim3(kWarps * 32), 0, st, view, rows, per);
+  EQAT_ROWS(64, 32)
+  EQAT_ROWS(64, 64)
+  EQAT_ROWS(128, 32)
+  EQAT_ROWS(128, 64)
+  EQAT_ROWS(128, 128)
+  EQAT_ROWS(256, 32)
+  EQAT_ROWS(256, 64)
+  EQAT_ROWS(256, 128)
+#undef EQAT_ROWS
+  return EQAT_ERR_UNSUPPORTED;
 }
 
 }  // namespace
