@@ -109,7 +109,7 @@ int eqat_device_status(int* h_status, int* h_detail);
  * barrier that nothing ever signals, through the very wait routine of the GEMM
  * kernels (which = 0), of the streaming kernels (1), of the matrix-vector forward
  * (2), of the forward on weight-row tiles (3) or on pairs of them (4), or of the
- * attention over the cache (5); afterwards
+ * attention over the cache for few rows (5) or prompts (6); afterwards
  * eqat_device_status() must report EQAT_ERR_TIMEOUT once and EQAT_OK from then
  * on.  It touches no tensor. */
 int eqat_selftest_wait_expiry(int which, void* stream);
@@ -402,14 +402,26 @@ typedef struct {
  * side) need a workspace each. */
 size_t eqat_cache_workspace_bytes(const eqat_cache_desc* desc, const eqat_attention_desc* attn);
 
+/* How eqat_cache_attention divides a call, decided on the host from the descriptors
+ * alone (a diagnostic).  `sms` as in eqat_packed_fwd_route; h_plan receives two
+ * numbers: the query rows (new tokens x query heads of a key/value head) for which
+ * the kernel for few rows reads a tile of the cache, and the number of rows from
+ * which on a sequence goes to the kernel for prompts (0: none does). */
+int eqat_cache_attention_plan(const eqat_cache_desc* desc, const eqat_attention_desc* attn, int sms, int* h_plan);
+
 /* Causal attention of the rows' queries over the cache, which already holds the
  * rows' own keys and values (eqat_cache_append):
  *     z_j = scale * sum_d Q_d K_jd,   O = sum_j softmax(z)_j V_j,
  * over the keys j that a row sees.  A row that sees none gets zeros, and lse
  * -infinity.  lse [rows, q_heads] fp32 dense (may be NULL): log of sum_j exp(z_j).
- * Codes enter the products as exact integers; steps and minima multiply fp32
- * sums, softmax statistics and outputs are fp32 until the final rounding, and the
- * weights of the values (softmax times step) are rounded to bf16.
+ * Few rows (decoding, drafted tokens): codes enter the products as exact integers,
+ * steps and minima multiply the sums, and the weights of the values (softmax times
+ * step) are integers of 23 bits, the largest weight of a row between 2^20 and 2^23.
+ * Many rows (eqat_cache_attention_plan): keys, values and softmax weights are
+ * rounded to bf16, keys and values as eqat_cache_read gives them; a row that sees a
+ * group of values that is NaN becomes NaN as a whole.  Softmax statistics and
+ * outputs are held in 32 bits until the final rounding.  What a row does not see
+ * does not reach it, NaN or not.
  * Repeated calls give the same bits on one device; the order in which a long
  * sequence is added up depends on the lengths of the whole batch.
  *   Q [rows, q_heads, head_dim] bf16 (in)   O [rows, q_heads, head_dim] bf16 (out) */

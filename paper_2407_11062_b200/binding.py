@@ -96,6 +96,7 @@ def _load():
         "eqat_cache_append": (c_int, [C, P, c_int64, P, c_int64, P, P, P, K, P, P, P]),
         "eqat_cache_read": (c_int, [C, P, P, P, K, P, P, P]),
         "eqat_cache_workspace_bytes": (c_size_t, [C, A]),
+        "eqat_cache_attention_plan": (c_int, [C, A, c_int, POINTER(c_int)]),
         "eqat_cache_attention": (c_int, [C, A, P, c_int64, P, P, P, K, P, c_int64, P, P, c_size_t, P]),
         "eqat_block_ap_step": (c_int, [POINTER(eqat_block_ap_linear), c_int, POINTER(c_int), P]),
         "eqat_e2e_qp_step": (c_int, [POINTER(eqat_e2e_qp_linear), c_int, POINTER(c_int), P]),
@@ -291,6 +292,13 @@ def cache_workspace_bytes(desc, attn) -> int:
     if n == ctypes.c_size_t(-1).value:
         raise EqatError(EQAT_ERR_SHAPE, "eqat_cache_workspace_bytes")
     return int(n)
+
+
+def eqat_cache_attention_plan(desc, attn, sms=0):
+    """Query rows of a tile in the kernel for few rows, and the rows from which on a sequence goes to the one for prompts (0: none)."""
+    plan = (c_int * 2)()
+    _check(lib.eqat_cache_attention_plan(ctypes.byref(desc), ctypes.byref(attn), int(sms), plan), "eqat_cache_attention_plan")
+    return tuple(plan)
 
 
 # `cache`: (k_codes, k_params, v_codes, v_params).  Row tensors are [rows, heads, head_dim] with dense heads, rows of any pitch.

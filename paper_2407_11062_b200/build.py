@@ -16,7 +16,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libeqat_b200.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
 SOURCES = ("api.cu", "attention.cu", "cache.cu", "elementwise.cu", "gemm.cu", "gemv.cu", "noalloc.cu", "slim.cu", 
-           "stream.cu", "wide.cu")
+           "prompt.cu", "stream.cu", "wide.cu")
 
 
 def _nvcc() -> str:

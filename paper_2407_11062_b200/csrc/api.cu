@@ -1,6 +1,7 @@
 // C ABI (include/eqat.h): argument validation on the host, then launches.
 #include <stdint.h>
 
+#include "attention.cuh"
 #include "cache.cuh"
 #include "common.cuh"
 #include "elementwise.cuh"
@@ -142,6 +143,7 @@ int check_attention_desc(const eqat_cache_desc* d, const eqat_attention_desc* a)
   if (a == nullptr) return EQAT_ERR_NULL;
   if (a->q_heads <= 0 || a->q_heads > 65536 || a->q_heads % d->kv_heads != 0) return EQAT_ERR_SHAPE;
   if (a->max_new <= 0 || a->window < 0) return EQAT_ERR_SHAPE;
+  if (d->rows * (a->q_heads / d->kv_heads) > (int64_t)1 << 30) return EQAT_ERR_SHAPE;      // rows x heads are counted in 32 bits
   if (!(a->scale > -1e30f && a->scale < 1e30f)) return EQAT_ERR_UNSUPPORTED;
   return EQAT_OK;
 }
@@ -206,15 +208,16 @@ size_t eqat_workspace_bytes(const eqat_desc* d, int op) {
 
 int eqat_device_status(int* h_status, int* h_detail) {
   if (h_status == nullptr) return EQAT_ERR_NULL;
-  int st[6] = {0, 0, 0, 0, 0, 0}, det[6] = {0, 0, 0, 0, 0, 0};
+  int st[7] = {0, 0, 0, 0, 0, 0, 0}, det[7] = {0, 0, 0, 0, 0, 0, 0};
   EQAT_TRY(read_device_status(&st[0], &det[0]));      // GEMM kernels
   EQAT_TRY(read_stream_status(&st[1], &det[1]));      // staged streaming kernels
   EQAT_TRY(read_gemv_status(&st[2], &det[2]));        // matrix-vector kernels
   EQAT_TRY(read_slim_status(&st[3], &det[3]));        // weight-row kernels: few tokens,
   EQAT_TRY(read_wide_status(&st[4], &det[4]));        // prompts
-  EQAT_TRY(read_attention_status(&st[5], &det[5]));   // attention over the cache
+  EQAT_TRY(read_attention_status(&st[5], &det[5]));   // attention over the cache: few rows,
+  EQAT_TRY(read_prompt_status(&st[6], &det[6]));      // prompts
   int k = 0;
-  while (k < 5 && st[k] == EQAT_OK) ++k;
+  while (k < 6 && st[k] == EQAT_OK) ++k;
   *h_status = st[k];
   if (h_detail != nullptr) *h_detail = det[k];
   return EQAT_OK;
@@ -227,6 +230,7 @@ int eqat_selftest_wait_expiry(int which, void* stream) {
   if (which == 3) return launch_wait_expiry_slim(as_stream(stream));
   if (which == 4) return launch_wait_expiry_wide(as_stream(stream));
   if (which == 5) return launch_wait_expiry_attention(as_stream(stream));
+  if (which == 6) return launch_wait_expiry_prompt(as_stream(stream));
   return EQAT_ERR_UNSUPPORTED;
 }
 
@@ -396,6 +400,14 @@ int eqat_cache_read(const eqat_cache_desc* d, const int32_t* row_offsets, const 
 
 size_t eqat_cache_workspace_bytes(const eqat_cache_desc* d, const eqat_attention_desc* a) {
   return check_attention_desc(d, a) == EQAT_OK ? cache_attention_workspace(*d, *a) : (size_t)-1;
+}
+
+int eqat_cache_attention_plan(const eqat_cache_desc* d, const eqat_attention_desc* a, int sms, int* h_plan) {
+  EQAT_TRY(check_attention_desc(d, a));
+  if (h_plan == nullptr) return EQAT_ERR_NULL;
+  if (sms < 0) return EQAT_ERR_SHAPE;
+  cache_attention_plan(*d, *a, sms > 0 ? sms : sm_count(), h_plan);
+  return EQAT_OK;
 }
 
 int eqat_cache_attention(const eqat_cache_desc* d, const eqat_attention_desc* a, const eqat_bf16* Q, int64_t q_pitch,

@@ -24,7 +24,7 @@
 // kernel in a fixed order.
 #include <type_traits>
 
-#include "cache.cuh"
+#include "attention.cuh"
 #include "common.cuh"
 #include "ptx.cuh"
 #include "wait.cuh"
@@ -34,7 +34,6 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32, kJoinThreads = 256;
-constexpr float kLog2e = 1.4426950408889634f;
 // Weights are p = 2^(z - shift), z the score in log2; the shift is the row's largest score (as of its last raise) plus
 // log2(unit) - kOne, unit a power of two above all steps that the row has counted, so p s < 2^23 as long as no score exceeds
 // that maximum by more than kLazy.
@@ -73,61 +72,6 @@ struct Shape {
   static_assert((1 + G) * kRows * 512 <= 2 * kOperandBytes && kRows * D * 4 <= 2 * kOperandBytes, "sums meet in the operands' memory");
   static_assert(kCols <= 512, "tensor memory");
 };
-
-// What a worker leaves behind for the join: its last segment, if it starts there and other workers go on with it.
-struct __align__(16) JoinRecord {
-  int first, first_row, rows, head;    // first row of the sequence, and the tile's rows as in Segment
-  int workers, unused[3];              // pieces; at most one: nothing to join
-};
-
-struct AttentionArgs {
-  CacheView cache;
-  const eqat_bf16* Q;
-  int64_t q_pitch, o_pitch;
-  eqat_bf16* O;
-  float* lse;
-  JoinRecord* records;         // [workers]
-  float* partial;              // [2 * workers][rows of a tile][D + 4]: sums, then the exponent and the sum of weights
-  int q_heads, ratio, max_new, window;
-  int ratio_shift;             // log2(ratio), or -1
-  float scale_log2;            // scale * log2(e)
-  uint32_t page_mul;           // n / (page_size / 16) = n * page_mul >> page_shift for n < 2^26
-  int page_shift;
-  int min_units;               // least number of units of a worker
-};
-
-// ------------------------------------------------------------------ the work and its division
-// All segments of a sequence have the same number of units, so that a unit is found by division; early row tiles of a long
-// prompt and rows at the edge of a window leave some empty.
-struct SequenceWork {
-  SequenceRows rows;
-  int tiles, units;            // row tiles; units of a segment
-};
-template <typename S>
-__device__ __forceinline__ SequenceWork sequence_work(const AttentionArgs& a, int b) {
-  SequenceWork w;
-  w.rows = sequence_rows(a.cache, b);
-  const int64_t rows = (int64_t)min(w.rows.count, a.max_new) * a.ratio;
-  w.tiles = (int)((rows + S::kRows - 1) / S::kRows);
-  int span = w.rows.length;
-  if (a.window > 0) span = (int)min((int64_t)span, (int64_t)a.window + S::kRows / a.ratio + 1 + S::kStageTokens);
-  w.units = max(1, (span + S::kUnit - 1) / S::kUnit);
-  return w;
-}
-__device__ __forceinline__ int64_t work_units(const CacheView& v, const SequenceWork& w) {
-  return (int64_t)w.tiles * v.kv_heads * w.units;
-}
-
-// Page of a token, counted in the sequence: page_size / 16 = n < 2^26 pieces, m = ceil(2^s / n) with s = 26 + ceil(log2 n):
-// m n exceeds 2^s by less than n <= 2^(s - 26), so t m >> s is exact for t < 2^26.
-__device__ __forceinline__ int page_index(const AttentionArgs& a, int token) {
-  return (int)(((uint64_t)(uint32_t)(token >> 4) * a.page_mul) >> a.page_shift);
-}
-
-// a / b for a >= 0: the 64-bit division, a subroutine of a hundred instructions, only where it is needed.
-__device__ __forceinline__ int64_t quotient(int64_t a, int b) { return (a >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b; }
-// New token of a row of a tile (rows run over the query heads of a token first).
-__device__ __forceinline__ int token_of_row(const AttentionArgs& a, int row) { return a.ratio_shift >= 0 ? row >> a.ratio_shift : row / a.ratio; }
 
 struct WorkPlace {
   int64_t total, per;          // units of the call, of a worker
@@ -177,31 +121,7 @@ __device__ __forceinline__ WorkPlace find_work(const AttentionArgs& a, int worke
   return p;
 }
 
-// A segment: one row tile of one sequence over one key/value head.
-struct Segment {
-  int first_row, rows;         // of the tile, counted in (new token, query head of this key/value head)
-  int low, high;               // keys that any row of the tile sees: [low, high)
-  int from;                    // low, rounded down to a stage
-};
-template <typename S>
-__device__ __forceinline__ Segment segment_of(const AttentionArgs& a, const SequenceWork& w, int tile) {
-  Segment s;
-  const int n = min(w.rows.count, a.max_new);
-  s.first_row = tile * S::kRows;
-  s.rows = min(S::kRows, n * a.ratio - s.first_row);
-  const int base = w.rows.length - w.rows.count;
-  s.high = max(base + token_of_row(a, s.first_row + s.rows - 1) + 1, 0);
-  s.low = a.window > 0 ? max(base + token_of_row(a, s.first_row) + 1 - a.window, 0) : 0;
-  s.from = s.low & ~(S::kStageTokens - 1);
-  return s;
-}
-
 // ------------------------------------------------------------------ instructions
-__device__ __forceinline__ float exp2_approx(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
 // D[tmem] (+)= A[smem] * B[smem], bytes: e4m3 numbers with fp32 sums, unsigned integers with 32-bit sums.
 __device__ __forceinline__ void mma_e4m3(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -240,11 +160,6 @@ __device__ __forceinline__ void sts_32(uint32_t addr, uint32_t v) { asm volatile
 __device__ __forceinline__ void sts_64(uint32_t addr, uint32_t a, uint32_t b) {
   asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
 }
-__device__ __forceinline__ float warp_max(float x) {
-  float r;
-  asm("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(r) : "f"(x));
-  return r;
-}
 template <int G>
 __device__ __forceinline__ void load_params(uint32_t (&r)[G], const uint32_t* p) {
   if constexpr (G == 1) {
@@ -260,9 +175,6 @@ __device__ __forceinline__ void load_params(uint32_t (&r)[G], const uint32_t* p)
     }
   }
 }
-// A CTA's tensor memory (whole warp).
-__device__ __forceinline__ void take_columns(uint32_t smem_dst, uint32_t cols) { ptx::tmem_alloc(smem_dst, cols); }
-
 // ------------------------------------------------------------------ the kernel
 template <int ROWS, int G>
 struct AttentionCtl {
@@ -460,6 +372,7 @@ attention_kernel(const AttentionArgs a) {
       for (int d = 1; d < kGroup / kEach; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
       const int up = most == 0 ? 0 : min(max(7 - ((int)(most >> 7) - 127), -100), 100);
       const float scale = __int_as_float((127 + up) << 23);
+      if (most >= 0x7F80u) sum = __int_as_float(0x7FC00000);             // a NaN or an infinity: so are all scores
       if (part % (kGroup / kEach) == 0) ctl->q_sum[part * kEach / kGroup][r] = sum * __int_as_float((127 + up - 9) << 23);
       if (part == 0) {
         ctl->back[r] = __int_as_float((127 + 9 - up) << 23);             // undoes the scale and the 2^-9 of the codes
@@ -800,7 +713,8 @@ attention_kernel(const AttentionArgs a) {
       const int row = done.sg.first_row + r, new_token = token_of_row(a, row);
       const int64_t out_row = done.rows.first + new_token;
       const int q_head = done.head * a.ratio + row - new_token * a.ratio;
-      const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
+      const bool empty = m == -INFINITY && l == 0.0f;                    // (a row whose scores are all NaN is not)
+      const float inv = empty ? 0.0f : 1.0f / l;
       eqat_bf16* to = a.O + out_row * a.o_pitch + (int64_t)q_head * D;
       float* part = done.whole ? nullptr : a.partial + (part_slot * kRows + r) * (D + 4);
 #pragma unroll
@@ -812,7 +726,7 @@ attention_kernel(const AttentionArgs a) {
       if (lane == 0) {
         if (!done.whole) *reinterpret_cast<float2*>(part + D) = make_float2(m, l);
         else if (a.lse != nullptr)
-          a.lse[out_row * a.q_heads + q_head] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+          a.lse[out_row * a.q_heads + q_head] = empty ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
       }
     }
     __syncthreads();                                                     // the operands may be written again
@@ -849,9 +763,9 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Atte
     float4 e[kFours] = {};
     for (int k0 = 0; k0 < rec.workers; k0 += 32) {
       float f = 0.0f;
-      if (k0 + lane < rec.workers && m > -INFINITY) {
+      if (k0 + lane < rec.workers) {
         const uint2 y = ptx::ld_global(reinterpret_cast<const uint2*>(part(k0 + lane) + D));
-        f = exp2_approx(__uint_as_float(y.x) - m);
+        f = m == -INFINITY ? 1.0f : exp2_approx(__uint_as_float(y.x) - m);
         l = fmaf(f, __uint_as_float(y.y), l);
       }
       const int n = min(32, rec.workers - k0);
@@ -880,22 +794,23 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Atte
     const int row = rec.first_row + r, new_token = token_of_row(a, row);
     const int64_t out_row = rec.first + new_token;
     const int q_head = rec.head * a.ratio + row - new_token * a.ratio;
-    const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
+    const bool empty = m == -INFINITY && l == 0.0f;
+    const float inv = empty ? 0.0f : 1.0f / l;
 #pragma unroll
     for (int i = 0; i < kFours; ++i)
       if (lane + 32 * i < D / 4)
         *reinterpret_cast<uint2*>(a.O + out_row * a.o_pitch + (int64_t)q_head * D + (lane + 32 * i) * 4) =
             make_uint2(pack_bf16x2(e[i].x * inv, e[i].y * inv), pack_bf16x2(e[i].z * inv, e[i].w * inv));
     if (lane == 0 && a.lse != nullptr)
-      a.lse[out_row * a.q_heads + q_head] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+      a.lse[out_row * a.q_heads + q_head] = empty ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
   }
 }
 
 // ------------------------------------------------------------------ host side
 // Query rows that a tile of the cache is read for: as many as the longest sequence has, as far as accumulators and a thread's
 // sums have room (32 rows x groups).
-int tile_rows(const eqat_cache_desc& d, const eqat_attention_desc& a) {
-  const int64_t rows = (int64_t)a.max_new * (a.q_heads / d.kv_heads);
+int tile_rows(const eqat_cache_desc& d, const eqat_attention_desc& a, int most_rows) {
+  const int64_t longest = (int64_t)a.max_new * (a.q_heads / d.kv_heads), rows = longest < most_rows ? longest : most_rows;
   const int groups = d.head_dim / d.group, most = groups >= 4 || d.head_dim == 256 ? 8 : groups == 2 ? 16 : 32;
   if (rows == 1) return 1;
   int n = 4;
@@ -931,12 +846,6 @@ int with_shape(const eqat_cache_desc& d, int rows, F&& f) {
 
 constexpr int kMinUnits = 2;
 
-int log2_up(int v) {
-  int s = 0;
-  while ((1 << s) < v) ++s;
-  return s;
-}
-
 // Units that a call can have at most, as far as the host knows.
 template <typename S>
 int64_t most_units(const eqat_cache_desc& d, const eqat_attention_desc& a) {
@@ -957,10 +866,41 @@ int workers_of(const eqat_cache_desc& d, const eqat_attention_desc& a, int sms) 
 
 }  // namespace
 
+AttentionArgs attention_args(const eqat_cache_desc& d, const eqat_attention_desc& at, const eqat_bf16* Q, int64_t q_pitch,
+                             const CacheView& view, eqat_bf16* O, int64_t o_pitch, float* lse) {
+  auto log2_up = [](int v) {
+    int s = 0;
+    while ((1 << s) < v) ++s;
+    return s;
+  };
+  AttentionArgs a{};
+  a.cache = view;
+  a.Q = Q;
+  a.q_pitch = q_pitch;
+  a.O = O;
+  a.o_pitch = o_pitch;
+  a.lse = lse;
+  a.q_heads = at.q_heads;
+  a.ratio = at.q_heads / d.kv_heads;
+  a.ratio_shift = (a.ratio & (a.ratio - 1)) == 0 ? log2_up(a.ratio) : -1;
+  a.max_new = at.max_new;
+  a.window = at.window < view.max_length ? at.window : 0;                // a window of the longest sequence hides nothing
+  a.scale_log2 = at.scale * kLog2e;
+  a.page_shift = 26 + log2_up(d.page_size / 16);
+  a.page_mul = (uint32_t)((((uint64_t)1 << a.page_shift) + d.page_size / 16 - 1) / (d.page_size / 16));
+  return a;
+}
+
+void cache_attention_plan(const eqat_cache_desc& d, const eqat_attention_desc& a, int sms, int* plan) {
+  const bool prompts = prompt_attention_applies(d, a, sms);
+  plan[0] = tile_rows(d, a, prompts ? kPromptRows - 1 : INT32_MAX);
+  plan[1] = prompts ? kPromptRows : 0;
+}
+
 size_t cache_attention_workspace(const eqat_cache_desc& d, const eqat_attention_desc& a) {
   const int sms = sm_count();
   size_t bytes = (size_t)-1;
-  with_shape(d, tile_rows(d, a), [&](auto D, auto G, auto NT) {
+  with_shape(d, tile_rows(d, a, prompt_attention_applies(d, a, sms > 0 ? sms : 148) ? kPromptRows - 1 : INT32_MAX), [&](auto D, auto G, auto NT) {
     using S = Shape<decltype(D)::value, decltype(G)::value, decltype(NT)::value>;
     const int w = workers_of<S>(d, a, sms > 0 ? sms : 148);
     bytes = w > 1 ? (size_t)w * (sizeof(JoinRecord) + (size_t)2 * S::kRows * (decltype(D)::value + 4) * sizeof(float)) : 0;
@@ -973,24 +913,17 @@ int launch_cache_attention(const eqat_cache_desc& d, const eqat_attention_desc& 
                            const CacheView& view, eqat_bf16* O, int64_t o_pitch, float* lse, void* workspace, cudaStream_t st) {
   const int sms = sm_count();
   if (sms <= 0) return EQAT_ERR_CUDA;
-  return with_shape(d, tile_rows(d, at), [&](auto DD, auto GG, auto NN) {
+  AttentionArgs args = attention_args(d, at, Q, q_pitch, view, O, o_pitch, lse);
+  args.most_rows = INT32_MAX;
+  if (prompt_attention_applies(d, at, sms)) {                            // long sequences there, short ones here
+    const int rc = launch_prompt_attention(d, args, st);
+    if (rc != EQAT_OK) return rc;
+    args.most_rows = kPromptRows - 1;
+  }
+  return with_shape(d, tile_rows(d, at, args.most_rows), [&](auto DD, auto GG, auto NN) {
     constexpr int D = decltype(DD)::value, G = decltype(GG)::value, NT = decltype(NN)::value;
     using S = Shape<D, G, NT>;
-    AttentionArgs a{};
-    a.cache = view;
-    a.Q = Q;
-    a.q_pitch = q_pitch;
-    a.O = O;
-    a.o_pitch = o_pitch;
-    a.lse = lse;
-    a.q_heads = at.q_heads;
-    a.ratio = at.q_heads / d.kv_heads;
-    a.ratio_shift = (a.ratio & (a.ratio - 1)) == 0 ? log2_up(a.ratio) : -1;
-    a.max_new = at.max_new;
-    a.window = at.window < view.max_length ? at.window : 0;              // a window of the longest sequence hides nothing
-    a.scale_log2 = at.scale * kLog2e;
-    a.page_shift = 26 + log2_up(d.page_size / 16);
-    a.page_mul = (uint32_t)((((uint64_t)1 << a.page_shift) + d.page_size / 16 - 1) / (d.page_size / 16));
+    AttentionArgs a = args;
     a.min_units = kMinUnits;
     static SmemOptIn opt;
     if (!opt.ensure(attention_kernel<D, G, NT>, S::kSmemBytes)) return (int)EQAT_ERR_CUDA;

@@ -67,6 +67,7 @@ int launch_cache_append(const eqat_cache_desc& d, const eqat_bf16* K, int64_t k_
                         const CacheView& view, eqat_bf16* K_hat, eqat_bf16* V_hat, cudaStream_t st);
 int launch_cache_read(const eqat_cache_desc& d, const CacheView& view, eqat_bf16* K_hat, eqat_bf16* V_hat, cudaStream_t st);
 
+void cache_attention_plan(const eqat_cache_desc& d, const eqat_attention_desc& a, int sms, int* plan);
 size_t cache_attention_workspace(const eqat_cache_desc& d, const eqat_attention_desc& a);
 int launch_cache_attention(const eqat_cache_desc& d, const eqat_attention_desc& a, const eqat_bf16* Q, int64_t q_pitch,
                            const CacheView& view, eqat_bf16* O, int64_t o_pitch, float* lse, void* workspace, cudaStream_t st);

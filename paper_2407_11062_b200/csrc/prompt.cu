@@ -1,0 +1,486 @@
+// Attention of many new tokens over the 4-bit cache: prompts and pieces of them.
+//
+// With 64 rows (new tokens x query heads of a key/value head) and more the products bound, not the cache: a CTA takes 256
+// rows of one sequence and key/value head, as two halves of 128, against tiles of 128 keys.  The tile's keys and values are
+// expanded once, to bf16 (what eqat_cache_read gives), by four warps; rows are the 128 lanes of both products:
+//     S = Q K^T     128 x 128, operands in shared memory
+//     O += P V      P in tensor memory, in the place of S
+// Eight warps, one thread a row, do the softmax: maximum, then weights, which go to tensor memory as bf16; a row's sums are
+// rescaled only when its maximum rises by more than 2^8.  One warp issues all products; while one half is in its softmax
+// the other half's products run.
+//
+// Work of one tile and both halves: 8.4 MFLOP a product and half, 2100 cycles at the rate of a library product; about 2300
+// instructions of a warp for each half's softmax and 2000 for the expansion, so the issue of instructions and the tensor
+// core are near one another.
+#include "attention.cuh"
+#include "common.cuh"
+#include "ptx.cuh"
+#include "wait.cuh"
+
+namespace eqat {
+namespace {
+
+constexpr int kHalfWarps = 4, kSpreadWarps = 4;
+constexpr int kThreads = (2 * kHalfWarps + kSpreadWarps + 4) * 32;      // the products' warp is one of four
+// Registers of a thread: 128 at launch, divided anew over the four groups of warps (184 + 184 + 88 + 56 = 4 * 128).
+constexpr int kSoftmaxRegs = 184, kSpreadRegs = 88, kProductRegs = 56;
+constexpr float kLazy = 8.0f;                        // a maximum may be exceeded by 2^8 before the sums are rescaled
+constexpr int kTile = 128;                           // keys of a tile
+
+template <int D, int G>
+struct Shape {
+  static constexpr int kRows = 256, kUnit = kTile, kStageTokens = 16;
+  static constexpr int kBoxes = D / 64;                                // blocks of 64 elements: 128 rows x 128 bytes
+  static constexpr int kOperandBytes = kBoxes * 16384;                 // 128 rows of queries, keys or values
+  static constexpr int kStages = 2;
+  static constexpr int kSmemBytes = 1024 + (2 + 2 * kStages) * kOperandBytes;
+  static constexpr int kLoads = D / 32;                                // 16-byte loads of a lane per tile, keys or values
+  // tensor memory: scores (and weights) of the halves, then their outputs
+  static constexpr int kAlloc = 512;
+};
+
+struct PromptCtl {
+  uint64_t queries_full;
+  uint64_t keys_full[2], keys_free[2], values_full[2], values_free[2];
+  uint64_t scores_done[2], weights_full[2], sums_done[2];
+  uint32_t tmem;
+  int abort;
+  alignas(16) uint32_t strange[8][4];                // tokens of the last tiles with a step or minimum that is not finite
+  int64_t before[kThreads];                          // units of the sequences before a thread's
+  int64_t total;
+};
+
+__device__ __forceinline__ uint32_t as_word(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t*>(&x); }
+__device__ __forceinline__ __nv_bfloat162 as_pair(uint32_t x) { return *reinterpret_cast<__nv_bfloat162*>(&x); }
+
+// q s + m of the codes in nibbles I and I + 4, as a bf16 pair, rounded once.
+template <int I>
+__device__ __forceinline__ uint32_t value_pair(uint32_t w, __nv_bfloat162 s, __nv_bfloat162 m) {
+  const uint32_t codes = ((w >> (4 * I)) & 0x000F000Fu) | 0x43004300u;
+  return as_word(__hfma2(__hsub2(as_pair(codes), as_pair(0x43004300u)), s, m));
+}
+
+template <int D, int G>
+__global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs a) {
+  using S = Shape<D, G>;
+  constexpr int kChunks = D / 32, kGroupChunks = kChunks / G;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(16) PromptCtl ctl_block;
+  PromptCtl* ctl = &ctl_block;
+  volatile int* abort_flag = &ctl->abort;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t raw = ptx::smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
+  const uint32_t queries = base, keys = queries + 2 * S::kOperandBytes, values = keys + S::kStages * S::kOperandBytes;
+
+  if (threadIdx.x == 0) {
+    ptx::mbar_init(ptx::smem_addr(&ctl->queries_full), 2 * kHalfWarps);
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(ptx::smem_addr(&ctl->keys_full[i]), kSpreadWarps);
+      ptx::mbar_init(ptx::smem_addr(&ctl->values_full[i]), kSpreadWarps);
+      ptx::mbar_init(ptx::smem_addr(&ctl->keys_free[i]), 1);
+      ptx::mbar_init(ptx::smem_addr(&ctl->values_free[i]), 1);
+      ptx::mbar_init(ptx::smem_addr(&ctl->scores_done[i]), 1);
+      ptx::mbar_init(ptx::smem_addr(&ctl->weights_full[i]), kHalfWarps);
+      ptx::mbar_init(ptx::smem_addr(&ctl->sums_done[i]), 1);
+    }
+    ctl->abort = 0;
+    ptx::fence_mbar_init();
+  }
+  if (warp == 0) {
+    take_columns(ptx::smem_addr(&ctl->tmem), S::kAlloc);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = ctl->tmem;
+  ptx::grid_dependency_wait();
+
+  // ---- the items (sequence, row tile, head), and how many come before each thread's sequences
+  const CacheView& v = a.cache;
+  const int each = (v.sequences + kThreads - 1) / kThreads;
+  auto items_of = [&](int b, SequenceWork& w) {
+    w = sequence_work<S>(a, b);
+    return (int64_t)w.tiles * v.kv_heads;
+  };
+  {
+    int64_t own = 0;
+    SequenceWork w;
+    for (int b = (int)threadIdx.x * each; b < min(((int)threadIdx.x + 1) * each, v.sequences); ++b) own += items_of(b, w);
+    ctl->before[threadIdx.x] = own;
+    __syncthreads();
+    if (warp == 0) {                                                     // exclusive sums, 32 threads at a time
+      int64_t sum = 0;
+      for (int k = 0; k < kThreads; k += 32) {
+        const int64_t n = ctl->before[k + lane];
+        int64_t upto = n;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int64_t o = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+          if (lane >= d) upto += o;
+        }
+        ctl->before[k + lane] = sum + upto - n;
+        sum += __shfl_sync(0xFFFFFFFFu, upto, 31);
+      }
+      if (lane == 0) ctl->total = sum;
+    }
+    __syncthreads();
+  }
+  const int64_t total = ctl->total;
+  struct Job {
+    SequenceRows rows;
+    Segment sg;
+    int sequence, head, tiles, halves;
+  };
+  auto job_of = [&](int64_t x) {                                         // whole warp
+    int k = 0;
+    for (int i = 0; i < kThreads; i += 32) k += __popc(__ballot_sync(0xFFFFFFFFu, ctl->before[i + lane] <= x));
+    int b = (k - 1) * each;                                              // the last thread with no more than x before it
+    int64_t before = ctl->before[k - 1];
+    SequenceWork w;
+    for (int64_t n; x >= before + (n = items_of(b, w)); ++b) before += n;
+    const int in = (int)(x - before), tile = w.tiles - 1 - in / v.kv_heads;            // the longest rows first
+    Job j;
+    j.rows = w.rows;
+    j.sequence = b;
+    j.head = in % v.kv_heads;
+    j.sg = segment_of<S>(a, w, tile);
+    j.tiles = j.sg.from < j.sg.high ? (j.sg.high - j.sg.from + kTile - 1) / kTile : 0;
+    j.halves = j.sg.rows > 128 ? 2 : 1;
+    return j;
+  };
+  auto wait = [&](uint64_t& barrier, uint32_t phase) {
+    bounded_wait_warp(ptx::smem_addr(&barrier), phase & 1u, abort_flag, WAIT_EPI_ACC_FULL);
+  };
+  auto arrive = [&](uint64_t& barrier) {                                 // a warp's
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&barrier));
+  };
+
+  if (warp < 2 * kHalfWarps) {
+    // ================================================================== softmax: thread `row` of half h
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+    const int h = warp / kHalfWarps, row_in_half = threadIdx.x & 127;
+    const uint32_t own = (uint32_t)((warp % kHalfWarps) * 32) << 16;
+    const uint32_t scores = tmem + h * 128 + own, outputs = tmem + 256 + h * D + own;
+    const uint32_t query_row = queries + h * S::kOperandBytes + row_in_half * 128;
+    const float c = fmaxf(fabsf(a.scale_log2), 1e-35f);                  // (not 0: -infinity times 0 is NaN)
+    const uint32_t sign = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
+    uint32_t n = 0, count = 0;                                           // tiles of this half, of all items so far
+    for (int64_t x = blockIdx.x; x < total; x += gridDim.x) {
+      const Job job = job_of(x);
+      const int r = h * 128 + row_in_half, row = job.sg.first_row + r, new_token = token_of_row(a, row);
+      const bool real = r < job.sg.rows;
+      const int base_pos = job.rows.length - job.rows.count;
+      const int64_t out_row = job.rows.first + new_token;
+      const int q_head = job.head * a.ratio + row - new_token * a.ratio;
+      // ---- the row's query, in the order of the codes (0 4 1 5 2 6 3 7 of each eight)
+      if (job.tiles > 0) {
+        if (h < job.halves) {
+          const uint4* src = reinterpret_cast<const uint4*>(a.Q + out_row * a.q_pitch + (int64_t)q_head * D);
+#pragma unroll
+          for (int p = 0; p < D / 8; ++p) {
+            uint4 e = make_uint4(0u, 0u, 0u, 0u);
+            if (real) e = ptx::ld_global(src + p);
+            // an infinity becomes NaN: no score of the row means anything
+            e.x |= __vcmpeq2(e.x & 0x7F807F80u, 0x7F807F80u) & 0x00400040u;
+            e.y |= __vcmpeq2(e.y & 0x7F807F80u, 0x7F807F80u) & 0x00400040u;
+            e.z |= __vcmpeq2(e.z & 0x7F807F80u, 0x7F807F80u) & 0x00400040u;
+            e.w |= __vcmpeq2(e.w & 0x7F807F80u, 0x7F807F80u) & 0x00400040u;
+            ptx::sts_128(query_row + p / 8 * 16384 + (((p % 8) ^ (row_in_half & 7)) << 4), __byte_perm(e.x, e.z, 0x5410) ^ sign,
+                         __byte_perm(e.x, e.z, 0x7632) ^ sign, __byte_perm(e.y, e.w, 0x5410) ^ sign, __byte_perm(e.y, e.w, 0x7632) ^ sign);
+          }
+          ptx::fence_proxy_async_smem();
+        }
+        ptx::tc_fence_before();                                          // the last item's outputs have been read
+        arrive(ctl->queries_full);
+      }
+      const uint32_t first_count = count;
+      count += job.tiles;
+      if (h >= job.halves) continue;
+      // keys that this row, and that every row of the half, sees
+      const int high = real ? base_pos + new_token + 1 : 0, low = a.window > 0 ? base_pos + new_token + 1 - a.window : 0;
+      const int last_row = min(job.sg.rows, (h + 1) * 128) - 1;
+      const int all_high = base_pos + token_of_row(a, job.sg.first_row + h * 128) + 1;
+      const int all_low = a.window > 0 ? base_pos + token_of_row(a, job.sg.first_row + last_row) + 1 - a.window : 0;
+      float top = -INFINITY, sum = 0.0f;                                 // of the scores, before the scale; of the weights
+      // Values that are not finite have been spread as zeros, since zero times NaN is not zero: a row that sees one is NaN.
+      bool strange = false;
+      auto look = [&](int i) {                                           // at a tile whose values have been multiplied
+        const uint4 y = *reinterpret_cast<const uint4*>(ctl->strange[(first_count + i) & 7u]);
+        if ((y.x | y.y | y.z | y.w) == 0u) return;
+        const uint32_t words[4] = {y.x, y.y, y.z, y.w};
+        for (int t = 0; t < kTile; ++t) {
+          const int token = job.sg.from + i * kTile + t;
+          strange |= (words[t / 32] >> (t % 32) & 1u) != 0u && token < high && token >= low;
+        }
+      };
+      for (int i = 0; i < job.tiles; ++i, ++n) {
+        const int t0 = job.sg.from + i * kTile;
+        const bool edge = t0 < all_low || t0 + kTile > all_high;
+        wait(ctl->scores_done[h], n);
+        ptx::tc_fence_after();
+        if (i > 0) look(i - 1);
+        float s[kTile];                                                  // the row's scores
+#pragma unroll
+        for (int k = 0; k < kTile; k += 32) ptx::tmem_ld_32x32(scores + k, *reinterpret_cast<uint32_t(*)[32]>(s + k));
+        ptx::tmem_ld_wait();
+        if (edge) {
+          const int before = high - t0, from = low - t0;
+#pragma unroll
+          for (int j = 0; j < kTile; ++j) s[j] = j < before && j >= from ? s[j] : -INFINITY;
+        }
+        float m4[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+        for (int j = 4; j < kTile; ++j) m4[j & 3] = fmaxf(m4[j & 3], s[j]);
+        const float most = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+        const bool first = top == -INFINITY;
+        const bool raise = first ? most > -INFINITY : (most - top) * c > kLazy;
+        if (__any_sync(0xFFFFFFFFu, raise)) {
+          const float to = raise ? most : top;
+          const float f = first || !raise ? 1.0f : exp2_approx((top - to) * c);
+          top = to;
+          sum *= f;
+          // The sums of the tiles before are complete: this tile's scores were issued behind them.
+          if (i > 0) {
+#pragma unroll 1
+            for (int k = 0; k < D; k += 16) {
+              uint32_t o[16];
+              ptx::tmem_ld_32x16(outputs + k, o);
+              ptx::tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              ptx::tmem_st_32x16(outputs + k, o);
+            }
+          }
+        }
+        // ---- weights, over the scores, two a column
+        const float shift = top == -INFINITY ? 0.0f : top * c;
+        float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < kTile; k += 32) {
+          uint32_t p[16];
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) {
+            const float e0 = exp2_approx(fmaf(s[k + j], c, -shift)), e1 = exp2_approx(fmaf(s[k + j + 1], c, -shift));
+            s4[j & 2] += e0;
+            s4[(j & 2) + 1] += e1;
+            p[j / 2] = pack_bf16x2(e0, e1);
+          }
+          ptx::tmem_st_32x16(scores + k / 2, p);
+        }
+        sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+        ptx::tmem_st_wait();
+        ptx::tc_fence_before();
+        arrive(ctl->weights_full[h]);
+      }
+      // ---- outputs
+      if (job.tiles > 0) {
+        wait(ctl->sums_done[h], n - 1);
+        ptx::tc_fence_after();
+        look(job.tiles - 1);
+      }
+      const bool empty = top == -INFINITY && sum == 0.0f;                // (a row whose scores are all NaN is not)
+      const float inv = strange ? __int_as_float(0x7FC00000) : 1.0f / sum;
+      eqat_bf16* to = a.O + out_row * a.o_pitch + (int64_t)q_head * D;
+#pragma unroll 1
+      for (int k = 0; k < D / 32; ++k) {
+        uint32_t o[32];
+        if (job.tiles > 0) {
+          ptx::tmem_ld_32x32(outputs + 32 * k, o);
+          ptx::tmem_ld_wait();
+        }
+        if (real) {
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            float e[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = empty ? 0.0f : __uint_as_float(o[8 * p + j]) * inv;
+            *reinterpret_cast<uint4*>(to + 32 * k + 8 * p) = make_uint4(pack_bf16x2(e[0], e[2]), pack_bf16x2(e[4], e[6]), pack_bf16x2(e[1], e[3]), pack_bf16x2(e[5], e[7]));
+          }
+        }
+      }
+      if (real && a.lse != nullptr)
+        a.lse[out_row * a.q_heads + q_head] = empty ? -INFINITY : ((top == -INFINITY ? 0.0f : top * c) + log2f(sum)) * 0.69314718055994531f;
+    }
+  } else if (warp < 2 * kHalfWarps + kSpreadWarps) {
+    // ================================================================== keys and values as bf16
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kSpreadRegs));
+    const int w4 = warp - 2 * kHalfWarps;                                // 32 tokens of a tile
+    const int token_in = lane / kChunks, chunk = lane % kChunks;         // of this lane's first chunk; tokens 32 / kChunks apart
+    constexpr int kStep = 32 / kChunks;
+    const uint32_t row_at = (32 * w4 + token_in) * 128 + chunk / 2 * 16384;
+    uint32_t count = 0;                                                  // tiles so far
+    for (int64_t x = blockIdx.x; x < total; x += gridDim.x) {
+      const Job job = job_of(x);
+      int page = 0;
+      auto page_of = [&](int i) {
+        const int token = job.sg.from + i * kTile + 32 * w4 + 16 * lane;
+        return lane < 2 && token < job.sg.high ? ld_index(v.page_table + (int64_t)job.sequence * v.max_pages + page_index(a, token)) : 0;
+      };
+      struct Fetched { uint4 codes[S::kLoads]; uint32_t params[S::kLoads]; };
+      uint32_t at[2] = {0, 0};
+      auto find = [&](int i) {
+        const int token = job.sg.from + i * kTile + 32 * w4 + 16 * lane;
+        // a page number outside the pool counts as the nearest inside
+        const uint32_t place = ((uint32_t)min(max(page, 0), v.pages - 1) * v.kv_heads + job.head) * v.page_size + (token - page_index(a, token) * v.page_size);
+        at[0] = __shfl_sync(0xFFFFFFFFu, place, 0);
+        at[1] = __shfl_sync(0xFFFFFFFFu, place, 1);
+        page = page_of(i + 1);
+      };
+      auto fetch = [&](Fetched& f, const uint8_t* codes, const uint32_t* params, int i) {
+        const int left = job.sg.high - (job.sg.from + i * kTile + 32 * w4);              // tokens from the warp's first on
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const uint4* from = reinterpret_cast<const uint4*>(codes + (uint64_t)at[p] * (D / 2)) + lane;
+          const uint32_t* with = params + (uint64_t)at[p] * G + token_in * G + chunk / kGroupChunks;
+#pragma unroll
+          for (int j = 0; j < S::kLoads / 2; ++j) {
+            const int k = p * (S::kLoads / 2) + j;
+            f.codes[k] = make_uint4(0u, 0u, 0u, 0u);
+            f.params[k] = 0u;                                            // behind the last key: zeros
+            if (16 * p < left) f.codes[k] = ptx::ld_global(from + 32 * j);
+            if (16 * p + j * kStep + token_in < left) f.params[k] = ptx::ld_global(with + j * kStep * G);
+          }
+        }
+      };
+      auto spread = [&](const Fetched& f, uint32_t operand, uint32_t* strange) {
+        uint32_t marks = 0;
+#pragma unroll
+        for (int k = 0; k < S::kLoads; ++k) {
+          const int token = 32 * w4 + token_in + k * kStep;
+          uint32_t param = f.params[k];
+          if (strange != nullptr && ((param & 0x7F80u) == 0x7F80u || (param & 0x7F800000u) == 0x7F800000u)) {
+            param = 0u;
+            marks |= 1u << (token & 31);
+          }
+          const __nv_bfloat162 s2 = as_pair(__byte_perm(param, 0, 0x1010)), m2 = as_pair(__byte_perm(param, 0, 0x3232));
+          const uint32_t w[4] = {f.codes[k].x, f.codes[k].y, f.codes[k].z, f.codes[k].w};
+#pragma unroll
+          for (int p = 0; p < 4; ++p)
+            ptx::sts_128(operand + row_at + k * kStep * 128 + (((chunk % 2 * 4 + p) ^ (token & 7)) << 4), value_pair<0>(w[p], s2, m2),
+                         value_pair<1>(w[p], s2, m2), value_pair<2>(w[p], s2, m2), value_pair<3>(w[p], s2, m2));
+        }
+        if (strange != nullptr) {
+          marks = __reduce_or_sync(0xFFFFFFFFu, marks);
+          if (lane == 0) strange[w4] = marks;
+        }
+      };
+      Fetched key, value;
+      if (job.tiles > 0) {
+        page = page_of(0);
+        find(0);
+        fetch(key, v.kq, v.kp, 0);
+        fetch(value, v.vq, v.vp, 0);
+      }
+      for (int i = 0; i < job.tiles; ++i, ++count) {
+        const uint32_t stage = count & 1u, use = count >> 1;
+        if (use > 0) wait(ctl->keys_free[stage], use - 1);
+        spread(key, keys + stage * S::kOperandBytes, nullptr);
+        ptx::fence_proxy_async_smem();
+        arrive(ctl->keys_full[stage]);
+        if (i + 1 < job.tiles) {
+          find(i + 1);
+          fetch(key, v.kq, v.kp, i + 1);
+        }
+        if (use > 0) wait(ctl->values_free[stage], use - 1);
+        spread(value, values + stage * S::kOperandBytes, ctl->strange[count & 7u]);
+        ptx::fence_proxy_async_smem();
+        arrive(ctl->values_full[stage]);
+        if (i + 1 < job.tiles) fetch(value, v.vq, v.vp, i + 1);
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProductRegs));
+    if (warp == 2 * kHalfWarps + kSpreadWarps) {
+    // ================================================================== the products
+    constexpr uint32_t kScoreDesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile / 8) << 17) | (8u << 24);
+    constexpr uint32_t kSumDesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D / 8) << 17) | (8u << 24);
+    uint32_t count = 0, items = 0, n[2] = {0, 0};                        // tiles, items with any, tiles of the halves
+    for (int64_t x = blockIdx.x; x < total; x += gridDim.x) {
+      const Job job = job_of(x);
+      if (job.tiles == 0) continue;
+      auto multiply_keys = [&](int h, uint32_t stage, bool last) {
+        if (ptx::elect_one()) {
+          const uint64_t q = ptx::smem_desc(queries + h * S::kOperandBytes), k = ptx::smem_desc(keys + stage * S::kOperandBytes);
+#pragma unroll
+          for (int e = 0; e < D / 16; ++e)
+            ptx::mma_bf16_ss(tmem + h * 128, q + ((e / 4 * 16384 + e % 4 * 32) >> 4), k + ((e / 4 * 16384 + e % 4 * 32) >> 4), kScoreDesc, e != 0);
+          ptx::mma_commit(ptx::smem_addr(&ctl->scores_done[h]));
+          if (last) ptx::mma_commit(ptx::smem_addr(&ctl->keys_free[stage]));
+        }
+        __syncwarp();
+      };
+      wait(ctl->queries_full, items++);
+      wait(ctl->keys_full[count & 1u], count >> 1);
+      ptx::tc_fence_after();
+      for (int h = 0; h < job.halves; ++h) multiply_keys(h, count & 1u, h + 1 == job.halves);
+      for (int i = 0; i < job.tiles; ++i, ++count) {
+        const uint32_t stage = count & 1u, next = (count + 1) & 1u;
+        for (int h = 0; h < job.halves; ++h) {
+          wait(ctl->weights_full[h], n[h]++);
+          if (h == 0) wait(ctl->values_full[stage], count >> 1);
+          ptx::tc_fence_after();
+          if (ptx::elect_one()) {
+            const uint64_t b = ptx::smem_desc(values + stage * S::kOperandBytes, 16384);
+#pragma unroll
+            for (int e = 0; e < kTile / 16; ++e)
+              ptx::mma_bf16_ts(tmem + 256 + h * D, tmem + h * 128 + e * 8, b + ((e * 2048) >> 4), kSumDesc, i != 0 || e != 0);
+            ptx::mma_commit(ptx::smem_addr(&ctl->sums_done[h]));
+            if (h + 1 == job.halves) ptx::mma_commit(ptx::smem_addr(&ctl->values_free[stage]));
+          }
+          __syncwarp();
+          if (i + 1 < job.tiles) {
+            if (h == 0) {
+              wait(ctl->keys_full[next], (count + 1) >> 1);
+              ptx::tc_fence_after();
+            }
+            multiply_keys(h, next, h + 1 == job.halves);
+          }
+        }
+      }
+    }
+    }
+  }
+  ptx::grid_dependents_launch();
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(ctl->tmem, S::kAlloc);
+  }
+}
+
+template <int D, int G>
+int launch_shape(const AttentionArgs& a, int sms, cudaStream_t st) {
+  using S = Shape<D, G>;
+  static SmemOptIn opt;
+  if (!opt.ensure(prompt_kernel<D, G>, S::kSmemBytes)) return EQAT_ERR_CUDA;
+  return launch_overlapped(prompt_kernel<D, G>, dim3(sms), dim3(kThreads), S::kSmemBytes, st, a);
+}
+
+}  // namespace
+
+bool prompt_attention_applies(const eqat_cache_desc& d, const eqat_attention_desc& a, int sms) {
+  const int64_t ratio = a.q_heads / d.kv_heads;
+  if (d.head_dim > 128 || a.max_new * ratio < kPromptRows) return false;
+  // A tile of 256 rows and 128 keys takes one SM about 2700 cycles here and as eight tiles of 32 rows about 17000 in the
+  // kernel for few rows, which deals its tiles out over all SMs and splits a long sequence: few row tiles are better there.
+  const int64_t rows = d.rows < (int64_t)a.max_new * d.sequences ? d.rows : (int64_t)a.max_new * d.sequences;
+  const int64_t tiles = (rows * ratio + 255) / 256 * d.kv_heads;
+  return tiles * 6 >= sms;
+}
+
+int launch_prompt_attention(const eqat_cache_desc& d, AttentionArgs a, cudaStream_t st) {
+  const int sms = sm_count(), g = d.head_dim / d.group;
+  if (sms <= 0) return EQAT_ERR_CUDA;
+  a.least_rows = kPromptRows;
+  a.most_rows = INT32_MAX;
+  if (d.head_dim == 64) return g == 1 ? launch_shape<64, 1>(a, sms, st) : launch_shape<64, 2>(a, sms, st);
+  return g == 1 ? launch_shape<128, 1>(a, sms, st) : g == 2 ? launch_shape<128, 2>(a, sms, st) : launch_shape<128, 4>(a, sms, st);
+}
+
+int launch_wait_expiry_prompt(cudaStream_t st) { return launch_wait_expiry(st); }
+int read_prompt_status(int* status, int* detail) { return read_wait_status(status, detail); }
+
+}  // namespace eqat

@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 import torch
 
-from helpers import Guarded
+from helpers import TOL, Guarded
 from oracle import cache_oracle as C
 
 pytestmark = pytest.mark.gpu
@@ -244,6 +244,96 @@ def test_drafts_and_chunks(eqat, D, group, H, page, window):
     check_attention(c, O, lse, Q, held, window)
 
 
+def check_prompt(c, O, lse, Q, held, window=0, rows=None):
+    """Keys and values rounded to bf16 (each term of a score off by at most U of itself, each value by U), weights too."""
+    want, want_lse, mass, size = C.attention(Q.astype(np.float64), held[0], held[1], c.lengths, c.offsets, c.D ** -0.5, window)
+    delta = size * (U + 2 * c.D / 16 * 2.0 ** -23 + 2.0 ** -20)
+    bound = 1.02 * (U * np.abs(want) + (2 * U + 2 * delta[..., None] + 2.0 ** -14) * mass) + 1e-30
+    used = slice(0, int(c.offsets[-1])) if rows is None else rows
+    got = host(O)[used].astype(np.float64)
+    err = np.abs(got - want[used])
+    bad = ~(err <= bound[used])
+    assert not bad.any(), (np.argwhere(bad)[:5].tolist(), err[bad][:5], bound[used][bad][:5])
+    assert np.linalg.norm(got - want[used]) <= TOL * np.linalg.norm(want[used])
+    if lse is not None:
+        got = lse.cpu().numpy().astype(np.float64)[used]
+        seen = ~np.isneginf(want_lse[used])
+        assert np.array_equal(~seen, np.isneginf(got))
+        assert (np.abs(got[seen] - want_lse[used][seen]) <= delta[used][seen] + 2.0 ** -18 * (1 + np.abs(want_lse[used][seen]))).all()
+
+
+@pytest.mark.parametrize("D,group,page", [(128, 128, 16), (128, 64, 48), (128, 32, 64), (64, 64, 16), (64, 32, 32)])
+@pytest.mark.parametrize("window", [0, 1, 77])
+def test_prompts(eqat, D, group, page, window):
+    """Whole prompts, pieces behind a long text, sequences with few rows and none, in one call: both kernels take part."""
+    lengths, news = [260, 300, 61, 5, 700, 1, 1, 33], [260, 1, 60, 0, 150, 1, 3, 33]
+    c = Cache(eqat, D, group, 4, page, lengths, news, seed=D + group + window, pad_rows=2)
+    held = c.fill()
+    a = eqat.make_attention_desc(32, max(news), D ** -0.5, window)
+    assert eqat.eqat_cache_attention_plan(c.desc(), a)[1] == 64
+    Q, O, lse = run_attention(eqat, c, 32, window=window)
+    check_prompt(c, O, lse, Q, held, window)
+    for _ in range(3):
+        _, O2, lse2 = run_attention(eqat, c, 32, window=window, Q=Q)
+        assert torch.equal(O.view(torch.int16), O2.view(torch.int16)) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("ratio,H", [(1, 32), (5, 8), (7, 6)])
+def test_prompts_of_other_head_counts(eqat, ratio, H):
+    c = Cache(eqat, 128, 128, H, 16, [190, 401], [190, 130], seed=ratio)
+    held = c.fill()
+    assert eqat.eqat_cache_attention_plan(c.desc(), eqat.make_attention_desc(H * ratio, 190, 0.1))[1] == 64
+    Q, O, lse = run_attention(eqat, c, H * ratio)
+    check_prompt(c, O, lse, Q, held)
+
+
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 0.6])
+def test_prompts_with_other_scales(eqat, scale):
+    """Maxima that rise along the sequence, by more than 2^8 at once; a negative scale; none."""
+    c = Cache(eqat, 128, 128, 8, 16, [300, 520], [300, 90], seed=4)
+    held = c.fill()
+    Q = C.bf16((c.rng.standard_normal((c.rows, 32, 128)) * 2).astype(np.float32))
+    _, O, lse = run_attention(eqat, c, 32, scale=scale, Q=Q)
+    want, want_lse, mass, size = C.attention(Q.astype(np.float64), held[0], held[1], c.lengths, c.offsets, scale)
+    # scores of some tens are off by up to U of their terms' sum: the error of a weight is bounded by its exponential
+    delta = np.expm1(2 * size * (U + 2.0 ** -16))
+    assert (np.abs(host(O) - want) <= 1.02 * (U * np.abs(want) + (2 * U + delta[..., None] + 2.0 ** -14) * (mass + np.abs(want)))).all()
+    if scale <= 0.0:
+        assert np.linalg.norm(host(O) - want) <= 4 * TOL * np.linalg.norm(want)
+
+
+def test_prompts_do_not_see_what_is_masked(eqat):
+    """NaN keys and values at two positions: rows before them are untouched, rows behind are NaN; with a window, rows beyond
+    it are untouched again.  NaN queries spoil their own rows only."""
+    c = Cache(eqat, 128, 64, 8, 16, [300], [300], seed=6)
+    held = c.fill()
+    for i, pos in ((0, 100), (1, 140)):
+        page = c.table[0][pos // 16]
+        c.params[i][page, :, pos % 16] = np.nan
+        held[i][0][pos] = 0.0
+    c.upload()
+    Q = C.bf16(c.rng.standard_normal((300, 32, 128)).astype(np.float32))
+    Q[50, 3] = np.nan
+    Q, O, lse = run_attention(eqat, c, 32, window=64, Q=Q)
+    keep = [r for r in range(300) if r != 50 and not (100 <= r < 164 or 140 <= r < 204)]
+    check_prompt(c, O, lse, np.where(np.isnan(Q), 0, Q), held, 64, rows=keep)
+    got = host(O)
+    assert np.isnan(got[100:204]).all() and np.isnan(got[50, 3]).all()
+    assert np.isfinite(got[50, :3]).all() and np.isfinite(got[50, 4:]).all()
+
+
+def test_nan_queries_spoil_their_own_rows(eqat):
+    c = Cache(eqat, 128, 128, 2, 16, [700, 40], [1, 3], seed=8)
+    held = c.fill()
+    Q = C.bf16(c.rng.standard_normal((c.rows, 16, 128)).astype(np.float32))
+    Q[0, 5], Q[2, 1, 7] = np.nan, np.inf
+    Q, O, lse = run_attention(eqat, c, 16, Q=Q)
+    got, want = host(O), C.attention(np.where(np.isfinite(Q), Q, 0).astype(np.float64), held[0], held[1], c.lengths, c.offsets, 128 ** -0.5)[0]
+    assert not np.isfinite(got[0, 5]).any() and not np.isfinite(got[2, 1]).any()
+    got[0, 5], got[2, 1] = want[0, 5], want[2, 1]
+    assert np.isfinite(got).all() and np.linalg.norm(got - want) <= TOL * np.linalg.norm(want)
+
+
 def test_rows_that_see_nothing_are_zero(eqat):
     c = Cache(eqat, 128, 128, 2, 16, [0, 0, 2], [1, 3, 6], seed=1)
     held = c.fill()
@@ -404,8 +494,9 @@ def test_streams_and_graphs(eqat):
 
 def test_the_wait_that_runs_out_is_reported(eqat):
     assert eqat.device_status() == (0, 0)
-    eqat.eqat_selftest_wait_expiry(5)
-    assert eqat.device_status()[0] == eqat.EQAT_ERR_TIMEOUT and eqat.device_status() == (0, 0)
+    for which in (5, 6):
+        eqat.eqat_selftest_wait_expiry(which)
+        assert eqat.device_status()[0] == eqat.EQAT_ERR_TIMEOUT and eqat.device_status() == (0, 0)
 
 
 def test_a_decoding_block(eqat):
