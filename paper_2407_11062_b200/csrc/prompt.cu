@@ -6,8 +6,8 @@
 //     S = Q K^T     128 x 128, operands in shared memory
 //     O += P V      P in tensor memory, in the place of S
 // Eight warps, one thread a row, do the softmax: maximum, then weights, which go to tensor memory as bf16; a row's sums are
-// rescaled only when its maximum rises by more than 2^8.  One warp issues all products; while one half is in its softmax
-// the other half's products run.
+// rescaled only when its maximum rises by more than 2^8.  A warp for each half issues its products; while one half is in its
+// softmax the other half's products run.
 //
 // Work of one tile and both halves: 8.4 MFLOP a product and half, 2100 cycles at the rate of a library product; about 2300
 // instructions of a warp for each half's softmax and 2000 for the expansion, so the issue of instructions and the tensor
@@ -21,11 +21,11 @@ namespace eqat {
 namespace {
 
 constexpr int kHalfWarps = 4, kSpreadWarps = 4;
-constexpr int kThreads = (2 * kHalfWarps + kSpreadWarps + 4) * 32;      // the products' warp is one of four
+constexpr int kThreads = (2 * kHalfWarps + kSpreadWarps + 4) * 32;      // two of the last four issue the products
 // Registers of a thread: 128 at launch, divided anew over the four groups of warps (184 + 184 + 88 + 56 = 4 * 128).
 constexpr int kSoftmaxRegs = 184, kSpreadRegs = 88, kProductRegs = 56;
 constexpr float kLazy = 8.0f;                        // a maximum may be exceeded by 2^8 before the sums are rescaled
-constexpr int kTile = 128;                           // keys of a tile
+constexpr int kTile = 128, kStep = 64;               // keys that are expanded, that are multiplied at once
 
 template <int D, int G>
 struct Shape {
@@ -35,14 +35,15 @@ struct Shape {
   static constexpr int kStages = 2;
   static constexpr int kSmemBytes = 1024 + (2 + 2 * kStages) * kOperandBytes;
   static constexpr int kLoads = D / 32;                                // 16-byte loads of a lane per tile, keys or values
-  // tensor memory: scores (and weights) of the halves, then their outputs
-  static constexpr int kAlloc = 512;
+  // tensor memory of a half: scores of a step, weights of two steps, outputs
+  static constexpr int kAlloc = 512, kHalfCols = 256, kWeightCol = 64, kOutputCol = 128;
 };
 
 struct PromptCtl {
   uint64_t queries_full;
   uint64_t keys_full[2], keys_free[2], values_full[2], values_free[2];
-  uint64_t scores_done[2], weights_full[2], sums_done[2];
+  uint64_t scores_done[2], scores_read[2];
+  uint64_t weights_full[2][2], sums_done[2][2];      // of a half's even and odd steps: either side may be two steps ahead
   uint32_t tmem;
   int abort;
   alignas(16) uint32_t strange[8][4];                // tokens of the last tiles with a step or minimum that is not finite
@@ -60,6 +61,21 @@ __device__ __forceinline__ uint32_t value_pair(uint32_t w, __nv_bfloat162 s, __n
   return as_word(__hfma2(__hsub2(as_pair(codes), as_pair(0x43004300u)), s, m));
 }
 
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 w, x, y;\n\tmov.b64 {%0, %1}, w;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+
 template <int D, int G>
 __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs a) {
   using S = Shape<D, G>;
@@ -73,15 +89,18 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
   const uint32_t queries = base, keys = queries + 2 * S::kOperandBytes, values = keys + S::kStages * S::kOperandBytes;
 
   if (threadIdx.x == 0) {
-    ptx::mbar_init(ptx::smem_addr(&ctl->queries_full), 2 * kHalfWarps);
+    ptx::mbar_init(ptx::smem_addr(&ctl->queries_full), 2 * kHalfWarps + 2);      // also the products' warps: done with the item before
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(ptx::smem_addr(&ctl->keys_full[i]), kSpreadWarps);
       ptx::mbar_init(ptx::smem_addr(&ctl->values_full[i]), kSpreadWarps);
-      ptx::mbar_init(ptx::smem_addr(&ctl->keys_free[i]), 1);
-      ptx::mbar_init(ptx::smem_addr(&ctl->values_free[i]), 1);
+      ptx::mbar_init(ptx::smem_addr(&ctl->keys_free[i]), 2);
+      ptx::mbar_init(ptx::smem_addr(&ctl->values_free[i]), 2);
       ptx::mbar_init(ptx::smem_addr(&ctl->scores_done[i]), 1);
-      ptx::mbar_init(ptx::smem_addr(&ctl->weights_full[i]), kHalfWarps);
-      ptx::mbar_init(ptx::smem_addr(&ctl->sums_done[i]), 1);
+      ptx::mbar_init(ptx::smem_addr(&ctl->scores_read[i]), kHalfWarps);
+      ptx::mbar_init(ptx::smem_addr(&ctl->weights_full[i][0]), kHalfWarps);
+      ptx::mbar_init(ptx::smem_addr(&ctl->weights_full[i][1]), kHalfWarps);
+      ptx::mbar_init(ptx::smem_addr(&ctl->sums_done[i][0]), 1);
+      ptx::mbar_init(ptx::smem_addr(&ctl->sums_done[i][1]), 1);
     }
     ctl->abort = 0;
     ptx::fence_mbar_init();
@@ -130,7 +149,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
   struct Job {
     SequenceRows rows;
     Segment sg;
-    int sequence, head, tiles, halves;
+    int sequence, head, tiles, steps, halves;
   };
   auto job_of = [&](int64_t x) {                                         // whole warp
     int k = 0;
@@ -145,7 +164,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
     j.sequence = b;
     j.head = in % v.kv_heads;
     j.sg = segment_of<S>(a, w, tile);
-    j.tiles = j.sg.from < j.sg.high ? (j.sg.high - j.sg.from + kTile - 1) / kTile : 0;
+    j.steps = j.sg.from < j.sg.high ? (j.sg.high - j.sg.from + kStep - 1) / kStep : 0;
+    j.tiles = (j.steps + 1) / 2;
     j.halves = j.sg.rows > 128 ? 2 : 1;
     return j;
   };
@@ -162,11 +182,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     const int h = warp / kHalfWarps, row_in_half = threadIdx.x & 127;
     const uint32_t own = (uint32_t)((warp % kHalfWarps) * 32) << 16;
-    const uint32_t scores = tmem + h * 128 + own, outputs = tmem + 256 + h * D + own;
+    const uint32_t scores = tmem + h * S::kHalfCols + own, outputs = scores + S::kOutputCol;
     const uint32_t query_row = queries + h * S::kOperandBytes + row_in_half * 128;
     const float c = fmaxf(fabsf(a.scale_log2), 1e-35f);                  // (not 0: -infinity times 0 is NaN)
+    auto wait_sums = [&](uint32_t step) { wait(ctl->sums_done[h][step & 1u], step >> 1); };
     const uint32_t sign = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
-    uint32_t n = 0, count = 0;                                           // tiles of this half, of all items so far
+    uint32_t n = 0, count = 0, items = 0;                                // steps of this half, tiles of all items, items so far
     for (int64_t x = blockIdx.x; x < total; x += gridDim.x) {
       const Job job = job_of(x);
       const int r = h * 128 + row_in_half, row = job.sg.first_row + r, new_token = token_of_row(a, row);
@@ -197,7 +218,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
       }
       const uint32_t first_count = count;
       count += job.tiles;
-      if (h >= job.halves) continue;
+      if (h >= job.halves) {                                             // not ahead of the half that has rows
+        if (job.tiles > 0) wait(ctl->queries_full, items++);
+        continue;
+      }
+      if (job.tiles > 0) ++items;
       // keys that this row, and that every row of the half, sees
       const int high = real ? base_pos + new_token + 1 : 0, low = a.window > 0 ? base_pos + new_token + 1 - a.window : 0;
       const int last_row = min(job.sg.rows, (h + 1) * 128) - 1;
@@ -215,24 +240,25 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
           strange |= (words[t / 32] >> (t % 32) & 1u) != 0u && token < high && token >= low;
         }
       };
-      for (int i = 0; i < job.tiles; ++i, ++n) {
-        const int t0 = job.sg.from + i * kTile;
-        const bool edge = t0 < all_low || t0 + kTile > all_high;
+      for (int i = 0; i < job.steps; ++i, ++n) {
+        const int t0 = job.sg.from + i * kStep;
+        const bool edge = t0 < all_low || t0 + kStep > all_high;
         wait(ctl->scores_done[h], n);
         ptx::tc_fence_after();
-        if (i > 0) look(i - 1);
-        float s[kTile];                                                  // the row's scores
+        float s[kStep];                                                  // the row's scores
 #pragma unroll
-        for (int k = 0; k < kTile; k += 32) ptx::tmem_ld_32x32(scores + k, *reinterpret_cast<uint32_t(*)[32]>(s + k));
+        for (int k = 0; k < kStep; k += 32) ptx::tmem_ld_32x32(scores + k, *reinterpret_cast<uint32_t(*)[32]>(s + k));
         ptx::tmem_ld_wait();
+        ptx::tc_fence_before();
+        arrive(ctl->scores_read[h]);                                     // the next step's may come
         if (edge) {
           const int before = high - t0, from = low - t0;
 #pragma unroll
-          for (int j = 0; j < kTile; ++j) s[j] = j < before && j >= from ? s[j] : -INFINITY;
+          for (int j = 0; j < kStep; ++j) s[j] = j < before && j >= from ? s[j] : -INFINITY;
         }
         float m4[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-        for (int j = 4; j < kTile; ++j) m4[j & 3] = fmaxf(m4[j & 3], s[j]);
+        for (int j = 4; j < kStep; ++j) m4[j & 3] = fmaxf(m4[j & 3], s[j]);
         const float most = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
         const bool first = top == -INFINITY;
         const bool raise = first ? most > -INFINITY : (most - top) * c > kLazy;
@@ -241,8 +267,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
           const float f = first || !raise ? 1.0f : exp2_approx((top - to) * c);
           top = to;
           sum *= f;
-          // The sums of the tiles before are complete: this tile's scores were issued behind them.
           if (i > 0) {
+            wait_sums(n - 1);
+            ptx::tc_fence_after();
 #pragma unroll 1
             for (int k = 0; k < D; k += 16) {
               uint32_t o[16];
@@ -254,30 +281,40 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
             }
           }
         }
-        // ---- weights, over the scores, two a column
+        // ---- weights, two a column, in the place of those of two steps ago
+        if (i > 1) {
+          wait_sums(n - 2);
+          ptx::tc_fence_after();
+          if ((i & 1) == 0) look(i / 2 - 1);
+        }
         const float shift = top == -INFINITY ? 0.0f : top * c;
-        float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const float2 c2 = make_float2(c, c), shift2 = make_float2(-shift, -shift);
+        float2 parts[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
-        for (int k = 0; k < kTile; k += 32) {
+        for (int k = 0; k < kStep; k += 32) {
           uint32_t p[16];
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
-            const float e0 = exp2_approx(fmaf(s[k + j], c, -shift)), e1 = exp2_approx(fmaf(s[k + j + 1], c, -shift));
-            s4[j & 2] += e0;
-            s4[(j & 2) + 1] += e1;
-            p[j / 2] = pack_bf16x2(e0, e1);
+            float2 e = fma2(make_float2(s[k + j], s[k + j + 1]), c2, shift2);
+            e.x = exp2_approx(e.x);
+            e.y = exp2_approx(e.y);
+            parts[j / 2 & 1] = add2(parts[j / 2 & 1], e);
+            p[j / 2] = pack_bf16x2(e.x, e.y);
           }
-          ptx::tmem_st_32x16(scores + k / 2, p);
+          ptx::tmem_st_32x16(scores + S::kWeightCol + (n & 1u) * 32 + k / 2, p);
         }
-        sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
         ptx::tmem_st_wait();
         ptx::tc_fence_before();
-        arrive(ctl->weights_full[h]);
+        arrive(ctl->weights_full[h][n & 1u]);
+        parts[0] = add2(parts[0], parts[1]);
+        sum += parts[0].x + parts[0].y;
       }
       // ---- outputs
       if (job.tiles > 0) {
-        wait(ctl->sums_done[h], n - 1);
+        if (job.steps > 1) wait_sums(n - 2);                             // every phase is waited for
+        wait_sums(n - 1);
         ptx::tc_fence_after();
+        if (job.tiles > 1) look(job.tiles - 2);
         look(job.tiles - 1);
       }
       const bool empty = top == -INFINITY && sum == 0.0f;                // (a row whose scores are all NaN is not)
@@ -392,54 +429,64 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProductRegs));
-    if (warp == 2 * kHalfWarps + kSpreadWarps) {
-    // ================================================================== the products
-    constexpr uint32_t kScoreDesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile / 8) << 17) | (8u << 24);
-    constexpr uint32_t kSumDesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D / 8) << 17) | (8u << 24);
-    uint32_t count = 0, items = 0, n[2] = {0, 0};                        // tiles, items with any, tiles of the halves
-    for (int64_t x = blockIdx.x; x < total; x += gridDim.x) {
-      const Job job = job_of(x);
-      if (job.tiles == 0) continue;
-      auto multiply_keys = [&](int h, uint32_t stage, bool last) {
-        if (ptx::elect_one()) {
-          const uint64_t q = ptx::smem_desc(queries + h * S::kOperandBytes), k = ptx::smem_desc(keys + stage * S::kOperandBytes);
-#pragma unroll
-          for (int e = 0; e < D / 16; ++e)
-            ptx::mma_bf16_ss(tmem + h * 128, q + ((e / 4 * 16384 + e % 4 * 32) >> 4), k + ((e / 4 * 16384 + e % 4 * 32) >> 4), kScoreDesc, e != 0);
-          ptx::mma_commit(ptx::smem_addr(&ctl->scores_done[h]));
-          if (last) ptx::mma_commit(ptx::smem_addr(&ctl->keys_free[stage]));
+    const int h = warp - (2 * kHalfWarps + kSpreadWarps);                // a warp for each half
+    if (h < 2) {
+      // ================================================================ the products
+      constexpr uint32_t kScoreDesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kStep / 8) << 17) | (8u << 24);
+      constexpr uint32_t kSumDesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D / 8) << 17) | (8u << 24);
+      const uint64_t query_desc = ptx::smem_desc(queries + h * S::kOperandBytes);
+      const uint64_t key_desc = ptx::smem_desc(keys), value_desc = ptx::smem_desc(values, 16384);
+      const uint32_t scores = tmem + h * S::kHalfCols, outputs = scores + S::kOutputCol;
+      uint32_t count = 0, items = 0, n = 0;                              // tiles, items with any, steps of this half
+      for (int64_t x = blockIdx.x; x < total; x += gridDim.x) {
+        const Job job = job_of(x);
+        if (job.tiles == 0) continue;
+        if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&ctl->queries_full));
+        wait(ctl->queries_full, items++);
+        const bool own = h < job.halves;
+        if (!own) {                                                      // a half without rows hands back what it does not read
+          for (int i = 0; i < job.tiles; ++i, ++count) {
+            wait(ctl->keys_full[count & 1u], count >> 1);
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&ctl->keys_free[count & 1u]));
+            wait(ctl->values_full[count & 1u], count >> 1);
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&ctl->values_free[count & 1u]));
+          }
+          continue;
         }
-        __syncwarp();
-      };
-      wait(ctl->queries_full, items++);
-      wait(ctl->keys_full[count & 1u], count >> 1);
-      ptx::tc_fence_after();
-      for (int h = 0; h < job.halves; ++h) multiply_keys(h, count & 1u, h + 1 == job.halves);
-      for (int i = 0; i < job.tiles; ++i, ++count) {
-        const uint32_t stage = count & 1u, next = (count + 1) & 1u;
-        for (int h = 0; h < job.halves; ++h) {
-          wait(ctl->weights_full[h], n[h]++);
-          if (h == 0) wait(ctl->values_full[stage], count >> 1);
+        auto multiply_keys = [&](int i) {                                // scores of step i of the item
+          const uint32_t tile = count + i / 2, stage = tile & 1u;
+          if ((i & 1) == 0) wait(ctl->keys_full[stage], tile >> 1);
           ptx::tc_fence_after();
           if (ptx::elect_one()) {
-            const uint64_t b = ptx::smem_desc(values + stage * S::kOperandBytes, 16384);
+            const uint64_t k = key_desc + (uint64_t)(stage * (S::kOperandBytes >> 4) + (i & 1) * (kStep * 128 >> 4));
 #pragma unroll
-            for (int e = 0; e < kTile / 16; ++e)
-              ptx::mma_bf16_ts(tmem + 256 + h * D, tmem + h * 128 + e * 8, b + ((e * 2048) >> 4), kSumDesc, i != 0 || e != 0);
-            ptx::mma_commit(ptx::smem_addr(&ctl->sums_done[h]));
-            if (h + 1 == job.halves) ptx::mma_commit(ptx::smem_addr(&ctl->values_free[stage]));
+            for (int e = 0; e < D / 16; ++e)
+              ptx::mma_bf16_ss(scores, query_desc + ((e / 4 * 16384 + e % 4 * 32) >> 4), k + ((e / 4 * 16384 + e % 4 * 32) >> 4), kScoreDesc, e != 0);
+            ptx::mma_commit(ptx::smem_addr(&ctl->scores_done[h]));
+            if ((i & 1) != 0 || i + 1 == job.steps) ptx::mma_commit(ptx::smem_addr(&ctl->keys_free[stage]));
           }
           __syncwarp();
-          if (i + 1 < job.tiles) {
-            if (h == 0) {
-              wait(ctl->keys_full[next], (count + 1) >> 1);
-              ptx::tc_fence_after();
-            }
-            multiply_keys(h, next, h + 1 == job.halves);
+        };
+        multiply_keys(0);
+        for (int i = 0; i < job.steps; ++i, ++n) {
+          wait(ctl->scores_read[h], n);
+          if (i + 1 < job.steps) multiply_keys(i + 1);
+          const uint32_t tile = count + i / 2, stage = tile & 1u;
+          wait(ctl->weights_full[h][n & 1u], n >> 1);
+          if ((i & 1) == 0) wait(ctl->values_full[stage], tile >> 1);
+          ptx::tc_fence_after();
+          if (ptx::elect_one()) {
+            const uint64_t b = value_desc + (uint64_t)(stage * (S::kOperandBytes >> 4) + (i & 1) * (kStep * 128 >> 4));
+#pragma unroll
+            for (int e = 0; e < kStep / 16; ++e)
+              ptx::mma_bf16_ts(outputs, scores + S::kWeightCol + (n & 1u) * 32 + e * 8, b + ((e * 2048) >> 4), kSumDesc, i != 0 || e != 0);
+            ptx::mma_commit(ptx::smem_addr(&ctl->sums_done[h][n & 1u]));
+            if ((i & 1) != 0 || i + 1 == job.steps) ptx::mma_commit(ptx::smem_addr(&ctl->values_free[stage]));
           }
+          __syncwarp();
         }
+        count += job.tiles;
       }
-    }
     }
   }
   ptx::grid_dependents_launch();
