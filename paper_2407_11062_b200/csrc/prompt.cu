@@ -12,6 +12,8 @@
 // Work of one tile and both halves: 8.4 MFLOP a product and half, 2100 cycles at the rate of a library product; about 2300
 // instructions of a warp for each half's softmax and 2000 for the expansion, so the issue of instructions and the tensor
 // core are near one another.
+#include <type_traits>
+
 #include "attention.cuh"
 #include "common.cuh"
 #include "ptx.cuh"
@@ -74,6 +76,24 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   asm("{\n\t.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 w, x, y;\n\tmov.b64 {%0, %1}, w;\n\t}"
       : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return r;
+}
+
+// 2^x by the multiply-add pipes, for x <= 16: 2^n p(f) with n the nearest integer and f in [-1/2, 1/2], p of degree 3 with the
+// smallest relative error there (7.5e-5, from the exchange algorithm; a weight is rounded to bf16, 2^-8, right after).  Below
+// -126 it stays at 2^-126.  The special function unit takes 8 cycles for the 32 exponentials of a warp, 1000 cycles for the two
+// halves' steps; three of eight pairs go this way (1000 new tokens behind 7192, 64/8 heads: none 332 us, two 325, three 323,
+// four 340).
+constexpr int kPolyPairs = 3;
+__device__ __forceinline__ float2 exp2_poly(float2 x) {
+  x.x = fmaxf(x.x, -126.0f);
+  x.y = fmaxf(x.y, -126.0f);
+  const float2 t = add2(x, make_float2(12582912.0f, 12582912.0f));      // 1.5 * 2^23: the integer in the low bits
+  const float2 f = add2(x, fma2(t, make_float2(-1.0f, -1.0f), make_float2(12582912.0f, 12582912.0f)));
+  float2 p = fma2(f, make_float2(0.05517167f, 0.05517167f), make_float2(0.24261113f, 0.24261113f));
+  p = fma2(f, p, make_float2(0.69326097f, 0.69326097f));
+  p = fma2(f, p, make_float2(0.99992806f, 0.99992806f));
+  return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)),
+                     __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
 }
 
 template <int D, int G>
@@ -281,28 +301,33 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
             }
           }
         }
-        // ---- weights, two a column, in the place of those of two steps ago
-        if (i > 1) {
-          wait_sums(n - 2);
-          ptx::tc_fence_after();
-          if ((i & 1) == 0) look(i / 2 - 1);
-        }
+        // ---- weights, two a column, in the place of those of two steps ago: this step's scores were issued behind the
+        // product with those
+        if (i > 1 && (i & 1) == 0) look(i / 2 - 1);
         const float shift = top == -INFINITY ? 0.0f : top * c;
         const float2 c2 = make_float2(c, c), shift2 = make_float2(-shift, -shift);
         float2 parts[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+        auto weigh = [&](auto is_edge) {
 #pragma unroll
-        for (int k = 0; k < kStep; k += 32) {
-          uint32_t p[16];
+          for (int k = 0; k < kStep; k += 32) {
+            uint32_t p[16];
 #pragma unroll
-          for (int j = 0; j < 32; j += 2) {
-            float2 e = fma2(make_float2(s[k + j], s[k + j + 1]), c2, shift2);
-            e.x = exp2_approx(e.x);
-            e.y = exp2_approx(e.y);
-            parts[j / 2 & 1] = add2(parts[j / 2 & 1], e);
-            p[j / 2] = pack_bf16x2(e.x, e.y);
+            for (int j = 0; j < 32; j += 2) {
+              float2 e = fma2(make_float2(s[k + j], s[k + j + 1]), c2, shift2);
+              if (!decltype(is_edge)::value && j / 2 % 8 >= 8 - kPolyPairs) {
+                e = exp2_poly(e);
+              } else {
+                e.x = exp2_approx(e.x);
+                e.y = exp2_approx(e.y);
+              }
+              parts[j / 2 & 1] = add2(parts[j / 2 & 1], e);
+              p[j / 2] = pack_bf16x2(e.x, e.y);
+            }
+            ptx::tmem_st_32x16(scores + S::kWeightCol + (n & 1u) * 32 + k / 2, p);
           }
-          ptx::tmem_st_32x16(scores + S::kWeightCol + (n & 1u) * 32 + k / 2, p);
-        }
+        };
+        if (edge) weigh(std::true_type());                               // what is masked weighs 0, not 2^-126
+        else weigh(std::false_type());
         ptx::tmem_st_wait();
         ptx::tc_fence_before();
         arrive(ctl->weights_full[h][n & 1u]);
@@ -311,7 +336,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
       }
       // ---- outputs
       if (job.tiles > 0) {
-        if (job.steps > 1) wait_sums(n - 2);                             // every phase is waited for
         wait_sums(n - 1);
         ptx::tc_fence_after();
         if (job.tiles > 1) look(job.tiles - 2);

@@ -21,7 +21,7 @@ class Barrier:
             self.phase, self.pending = self.phase + 1, self.count
 
 
-def run(items, seed, one_sum_barrier=False, no_handshake=False, idle_ahead=False, one_weight_barrier=False):
+def run(items, seed, no_handshake=False, idle_ahead=False, one_weight_barrier=False):
     """items: (steps, halves).  Returns None, or what went wrong."""
     rnd = random.Random(seed)
     B = {"queries": Barrier(2 + (0 if no_handshake else 2))}          # one arrival stands for the four warps of a half
@@ -29,7 +29,7 @@ def run(items, seed, one_sum_barrier=False, no_handshake=False, idle_ahead=False
         for name, n in (("keys_full", 1), ("keys_free", 2), ("values_full", 1), ("values_free", 2), ("scores_done", 1),
                         ("scores_read", 1), ("weights0", 1), ("weights1", 1), ("sums0", 1), ("sums1", 1)):
             B[name, i] = Barrier(n)
-    wrong, ready = [], {0: -1, 1: -1}
+    wrong, ready, done = [], {0: -1, 1: -1}, {0: 0, 1: 0}   # item whose queries are written; steps whose sums are complete
     queue = {0: [], 1: []}                                  # what a half's products do when they finish
 
     def wait(key, phase):
@@ -39,7 +39,7 @@ def run(items, seed, one_sum_barrier=False, no_handshake=False, idle_ahead=False
             wrong.append(f"{key} passed in phase {B[key].phase}, waited for {phase}")
 
     def sums(h, step):
-        return (("sums0", h), step) if one_sum_barrier else ((f"sums{step % 2}", h), step >> 1)
+        return (f"sums{step % 2}", h), step >> 1
 
     def weights(h, step):
         return (("weights0", h), step) if one_weight_barrier else ((f"weights{step % 2}", h), step >> 1)
@@ -63,13 +63,11 @@ def run(items, seed, one_sum_barrier=False, no_handshake=False, idle_ahead=False
                 B["scores_read", h].arrive()
                 if i > 0 and rnd.random() < 0.3:            # the maximum has risen
                     yield from wait(*sums(h, n - 1))
-                if i > 1:
-                    yield from wait(*sums(h, n - 2))
                 yield
+                if i > 1 and done[h] < n - 1:
+                    wrong.append("weights written over those of a product that has not finished")
                 B[weights(h, n)[0]].arrive()
                 n += 1
-            if steps > 1:
-                yield from wait(*sums(h, n - 2))
             yield from wait(*sums(h, n - 1))
 
     def spread():
@@ -139,6 +137,7 @@ def run(items, seed, one_sum_barrier=False, no_handshake=False, idle_ahead=False
             for h in (0, 1):
                 if queue[h] and rnd.random() < 0.7:
                     for key in queue[h].pop(0):
+                        done[h] += key[0].startswith("sums")
                         B[key].arrive()
         elif agents[k] is not None:
             try:
@@ -159,10 +158,9 @@ def test_no_wait_lasts_and_none_passes_early(items):
 
 
 def test_the_model_sees_the_mistakes():
-    """One barrier for even and odd steps' sums, or weights: a wait two steps late meets the next phase of the same parity.  Without the
+    """One barrier for even and odd steps' weights: a wait that is two steps late meets the next phase of the same parity.  Without the
     products' part in the queries' barrier, the warp of a half without rows can be left behind by two items; a half without
     rows that does not wait for that barrier arrives for later items on it."""
-    assert any(run([(12, 2)], s, one_sum_barrier=True) for s in range(60))
     assert any(run([(12, 2)], s, one_weight_barrier=True) for s in range(60))
     assert any(run([(1, 1)] * 12, s, no_handshake=True) for s in range(400))
     assert any(run([(1, 1), (2, 1), (2, 1)], s, idle_ahead=True) for s in range(60))
@@ -176,7 +174,7 @@ def test_the_model_is_of_the_kernel():
     assert "wait(ctl->sums_done[h][step & 1u], step >> 1)" in text and "kTile = 128, kStep = 64" in text
     assert "if (h >= job.halves) {\n        if (job.tiles > 0) wait(ctl->queries_full, items++);" in re.sub(r" +\n", "\n", text)
     steps = text[text.index("for (int i = 0; i < job.steps; ++i, ++n) {\n        const int t0"):]
-    order = ["wait(ctl->scores_done[h], n)", "arrive(ctl->scores_read[h])", "wait_sums(n - 1)", "wait_sums(n - 2)", "arrive(ctl->weights_full[h][n & 1u])"]
+    order = ["wait(ctl->scores_done[h], n)", "arrive(ctl->scores_read[h])", "wait_sums(n - 1)", "arrive(ctl->weights_full[h][n & 1u])"]
     assert [steps.index(x) for x in order] == sorted(steps.index(x) for x in order)
     products = text[text.index("multiply_keys(0);"):]
     order = ["wait(ctl->scores_read[h], n)", "multiply_keys(i + 1)", "wait(ctl->weights_full[h][n & 1u], n >> 1)", "ctl->values_full[stage], tile >> 1",
