@@ -33,7 +33,7 @@ namespace eqat {
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32, kJoinThreads = 256;
+constexpr int kThreads = kWarps * 32, kJoinThreads = 512;
 // Weights are p = 2^(z - shift), z the score in log2; the shift is the row's largest score (as of its last raise) plus
 // log2(unit) - kOne, unit a power of two above all steps that the row has counted, so p s < 2^23 as long as no score exceeds
 // that maximum by more than kLazy.
@@ -48,14 +48,17 @@ struct Shape {
   static constexpr int kRows = ROWS;
   static constexpr int kBlocks = D > 128 ? D / 128 : 1;                // blocks of 128 elements
   static constexpr int kBlockGroups = G / kBlocks;
-  static constexpr int kParts = NB * kBlockGroups;                     // (row block, group) pairs of a block: three byte columns x 8
+  // Columns come in eights.  Few rows share one eight over the groups of a block: slot = group * ROWS + row.
+  static constexpr bool kShared = ROWS * G <= 8;
+  static constexpr int kSlots = ROWS * kBlockGroups;                   // of a block, where they are shared
+  static constexpr int kParts = kShared ? 1 : NB * kBlockGroups;       // eights of a block
   static constexpr int kWeightUnits = kParts == 1 ? 2 : kParts + kParts / 2;      // 16-byte units of a token's weights, per block
   static constexpr int kWeightCols = 16 * kWeightUnits;
-  static constexpr int kScoreCols = 16 * NB * G;
+  static constexpr int kScoreCols = kShared ? 16 : 16 * NB * G;
   static constexpr int kSumCols = kBlocks * kWeightCols;
   // tensor memory: sums, then scores; 160 columns are taken as 128 + 32, with the last two score blocks in the 32
   static constexpr int kCols = kScoreCols + kSumCols;
-  static constexpr bool kTwoParts = kCols > 128 && kCols <= 160 && G >= 2 && NB == 1;
+  static constexpr bool kTwoParts = kCols > 128 && kCols <= 160 && G >= 2 && NB == 1 && !kShared;
   static constexpr int kAlloc = kCols <= 64 ? 64 : kCols <= 128 || kTwoParts ? 128 : kCols <= 256 ? 256 : 512;
   static constexpr int kOperandBytes = kBlocks * 128 * 128;            // of keys or values: 128 tokens x 128 bytes a block
   static constexpr int kWeightBytes = kBlocks * kWeightUnits * 2048;
@@ -82,6 +85,22 @@ struct WorkPlace {
 template <typename S, typename F>
 __device__ __forceinline__ WorkPlace find_work(const AttentionArgs& a, int workers, F&& f, int64_t* scratch) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (a.cache.sequences <= 32) {                                         // every warp by itself
+    const int64_t own = lane < a.cache.sequences ? work_units(a.cache, sequence_work<S>(a, lane)) : 0;
+    int64_t upto = own;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t o = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+      if (lane >= d) upto += o;
+    }
+    WorkPlace p;
+    p.total = __shfl_sync(0xFFFFFFFFu, upto, 31);
+    p.per = max(quotient(p.total + workers - 1, workers), (int64_t)a.min_units);
+    const uint32_t behind = __ballot_sync(0xFFFFFFFFu, upto > f(p.per));     // sequences that end behind unit x
+    p.sequence = behind == 0u ? a.cache.sequences : __ffs(behind) - 1;
+    p.before = __shfl_sync(0xFFFFFFFFu, upto - own, behind == 0u ? 0 : __ffs(behind) - 1);
+    return p;
+  }
   const int each = (a.cache.sequences + kThreads - 1) / kThreads;
   const int b0 = min(tid * each, a.cache.sequences), b1 = min(b0 + each, a.cache.sequences);
   int64_t own = 0;
@@ -348,9 +367,12 @@ attention_kernel(const AttentionArgs a) {
 #pragma unroll
     for (int rb = 0; rb < NB; ++rb) {
       constexpr int kEach = D / 16;                                      // elements of a thread
-      const int r = rb * 8 + tid / 16, part = tid % 16, row = sg.first_row + r, new_token = token_of_row(a, row);
+      // shared eights: the row once for each group, with zeros for the other groups
+      const int slot = rb * 8 + tid / 16, part = tid % 16, r = S::kShared ? slot % kRows : slot, row = sg.first_row + r;
+      const int new_token = token_of_row(a, row), group = slot / kRows;
+      const bool real = r < sg.rows && (!S::kShared || group < G);
       uint32_t e[kEach / 2] = {};
-      if (r < sg.rows) {
+      if (real) {
         const eqat_bf16* src = a.Q + (int64_t)(job.rows.first + new_token) * a.q_pitch + (int64_t)(job.head * a.ratio + row - new_token * a.ratio) * D + part * kEach;
 #pragma unroll
         for (int j = 0; j < kEach / 2; j += 2) {
@@ -363,18 +385,20 @@ attention_kernel(const AttentionArgs a) {
 #pragma unroll
       for (int j = 0; j < kEach / 2; ++j) {
         most = __vmaxu2(most, e[j] & 0x7FFF7FFFu);
+        if (S::kShared && part * kEach / kGroup != group) e[j] = 0u;
         sum += param_step(e[j]) + param_low(e[j]);
       }
       most = max(most & 0xFFFFu, most >> 16);
 #pragma unroll
       for (int d = 1; d < 16; d <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
 #pragma unroll
-      for (int d = 1; d < kGroup / kEach; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+      for (int d = 1; d < (S::kShared ? 16 : kGroup / kEach); d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
       const int up = most == 0 ? 0 : min(max(7 - ((int)(most >> 7) - 127), -100), 100);
       const float scale = __int_as_float((127 + up) << 23);
       if (most >= 0x7F80u) sum = __int_as_float(0x7FC00000);             // a NaN or an infinity: so are all scores
-      if (part % (kGroup / kEach) == 0) ctl->q_sum[part * kEach / kGroup][r] = sum * __int_as_float((127 + up - 9) << 23);
-      if (part == 0) {
+      if (S::kShared ? part == 0 : part % (kGroup / kEach) == 0)
+        ctl->q_sum[S::kShared ? 0 : part * kEach / kGroup][slot] = sum * __int_as_float((127 + up - 9) << 23);
+      if (part == 0 && (!S::kShared || group == 0)) {
         ctl->back[r] = __int_as_float((127 + 9 - up) << 23);             // undoes the scale and the 2^-9 of the codes
         ctl->minus[r] = 0.0f;
         ctl->top[r] = ctl->shift[r] = -INFINITY;
@@ -420,15 +444,22 @@ attention_kernel(const AttentionArgs a) {
       for (int k = 0; k < S::kBlocks; ++k)
 #pragma unroll
         for (int rb = 0; rb < NB; ++rb) {
-          const int part = (warp * 32 * S::kBlockGroups / (D < 128 ? 64 : 128)) % S::kBlockGroups * NB + rb;
+          const int group = (warp * 32 * S::kBlockGroups / (D < 128 ? 64 : 128)) % S::kBlockGroups;
+          const int part = S::kShared ? 0 : group * NB + rb;
           const uint32_t at = sum_tmem + own_lanes + k * S::kWeightCols;
           uint32_t low16[16], high8[8];
           ptx::tmem_ld_32x16(at + part * 16, low16);
           ptx::tmem_ld_32x8(at + 16 * S::kParts + part * 8, high8);
           ptx::tmem_ld_wait();
 #pragma unroll
-          for (int r = 0; r < 8 && r < kRows; ++r)
-            out[k][rb * 8 + r] += fmaf((float)(int)high8[r], 65536.0f, fmaf((float)(int)low16[8 + r], 256.0f, (float)(int)low16[r]));
+          for (int slot = 0; slot < 8; ++slot) {
+            const float sum = fmaf((float)(int)high8[slot], 65536.0f, fmaf((float)(int)low16[8 + slot], 256.0f, (float)(int)low16[slot]));
+            if (S::kShared) {
+              if (slot < S::kSlots && slot / kRows == group) out[k][slot % kRows] += sum;
+            } else if (rb * 8 + slot < kRows) {
+              out[k][rb * 8 + slot] += sum;
+            }
+          }
         }
       since = 0;
     };
@@ -457,12 +488,10 @@ attention_kernel(const AttentionArgs a) {
         ptx::tc_fence_after();
         if (ptx::elect_one()) {
 #pragma unroll
-          for (int e = 0; e < G; ++e) {
-            const int at = e % S::kBlockGroups * kGroup, block = e / S::kBlockGroups;
-#pragma unroll
-            for (int k = 0; k < kGroup; k += 32)
-              mma_e4m3(score_tmem(e), keys_desc + ((block * 16384 + at + k) >> 4), queries_desc + ((block * (NB * 2048) + at + k) >> 4),
-                       kScoreDesc | ((uint32_t)(2 * NB) << 17), k != 0);
+          for (int d = 0; d < D; d += 32) {                              // a group's scores have columns of their own
+            const int block = d / 128, at = d % 128;
+            mma_e4m3(score_tmem(S::kShared ? 0 : d / kGroup), keys_desc + ((block * 16384 + at) >> 4),
+                     queries_desc + ((block * (NB * 2048) + at) >> 4), kScoreDesc | ((uint32_t)(2 * NB) << 17), (S::kShared ? d : d % kGroup) != 0);
           }
           ptx::mma_commit(ptx::smem_addr(&ctl->scores_done));
         }
@@ -487,29 +516,47 @@ attention_kernel(const AttentionArgs a) {
       float arg[kRows];
       float step = 0.0f;
       bool raise = i == 0;
+      if constexpr (S::kShared) {
+        uint32_t acc[16];
+        ptx::tmem_ld_32x16(score_tmem(0) + own_lanes, acc);
+        ptx::tmem_ld_wait();
+        const float4 q0 = *reinterpret_cast<const float4*>(&ctl->q_sum[0][0]), q1 = *reinterpret_cast<const float4*>(&ctl->q_sum[0][4]);
+        const float qv[8] = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
 #pragma unroll
-      for (int e = 0; e < G; ++e) {
-        const float ks = param_step(key_params[e]) * a.scale_log2, km = param_low(key_params[e]) * a.scale_log2;
-        step = fmaxf(step, param_step(value_params[e]));
+        for (int e = 0; e < G; ++e) {
+          const float ks = param_step(key_params[e]) * a.scale_log2, km = param_low(key_params[e]) * a.scale_log2;
+          step = fmaxf(step, param_step(value_params[e]));
 #pragma unroll
-        for (int rb = 0; rb < NB; ++rb) {
-          uint32_t acc[16];
-          ptx::tmem_ld_32x16(score_tmem(e) + own_lanes + rb * 16, acc);
-          ptx::tmem_ld_wait();
+          for (int r = 0; r < kRows; ++r) {
+            const int slot = e * kRows + r;
+            const float z = fmaf(__uint_as_float(acc[8 + slot]), 0.0625f, __uint_as_float(acc[slot]));
+            arg[r] = fmaf(z, ks, e == 0 ? qv[slot] * km : fmaf(qv[slot], km, arg[r]));
+          }
+        }
+      } else {
 #pragma unroll
-          for (int q4 = 0; q4 < 8 && q4 < kRows; q4 += 4) {
-            const float4 qs = *reinterpret_cast<const float4*>(&ctl->q_sum[e][rb * 8 + q4]);
-            const float qv[4] = {qs.x, qs.y, qs.z, qs.w};
+        for (int e = 0; e < G; ++e) {
+          const float ks = param_step(key_params[e]) * a.scale_log2, km = param_low(key_params[e]) * a.scale_log2;
+          step = fmaxf(step, param_step(value_params[e]));
 #pragma unroll
-            for (int r = 0; r < 4 && r < kRows; ++r) {
-              const float z = fmaf(__uint_as_float(acc[8 + q4 + r]), 0.0625f, __uint_as_float(acc[q4 + r]));
-              float& to = arg[rb * 8 + q4 + r];
-              to = fmaf(z, ks, e == 0 ? qv[r] * km : fmaf(qv[r], km, to));
+          for (int rb = 0; rb < NB; ++rb) {
+            uint32_t acc[16];
+            ptx::tmem_ld_32x16(score_tmem(e) + own_lanes + rb * 16, acc);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int q4 = 0; q4 < 8 && q4 < kRows; q4 += 4) {
+              const float4 qs = *reinterpret_cast<const float4*>(&ctl->q_sum[e][rb * 8 + q4]);
+              const float qv[4] = {qs.x, qs.y, qs.z, qs.w};
+#pragma unroll
+              for (int r = 0; r < 4 && r < kRows; ++r) {
+                const float z = fmaf(__uint_as_float(acc[8 + q4 + r]), 0.0625f, __uint_as_float(acc[q4 + r]));
+                float& to = arg[rb * 8 + q4 + r];
+                to = fmaf(z, ks, e == 0 ? qv[r] * km : fmaf(qv[r], km, to));
+              }
             }
           }
         }
       }
-
       // Some rows of an edge tile do not see some of its tokens.
       auto weigh = [&](auto is_edge) {
         constexpr bool kEdge = decltype(is_edge)::value;
@@ -537,43 +584,57 @@ attention_kernel(const AttentionArgs a) {
 #pragma unroll
           for (int r = 0; r < kRows; ++r) p[r] = exp2_approx(arg[r]);
           if (!unset)
-#pragma unroll
-          for (int e = 0; e < G; ++e) {
-            const float s = param_step(value_params[e]);
-            const int block = e / S::kBlockGroups;
-#pragma unroll
-            for (int rb = 0; rb < NB; ++rb) {
-              uint32_t y[8];
-#pragma unroll
-              for (int r = 0; r < 8 && r < kRows; ++r) {
-                y[r] = __float_as_uint(fmaf(p[rb * 8 + r], s, 8388608.0f));          // 2^23: the low 23 bits are round(p s)
-                if (kEdge) y[r] = arg[rb * 8 + r] == -INFINITY ? 0u : y[r];          // unseen: zero, whatever the step
-              }
-              const int part = e % S::kBlockGroups * NB + rb;
+{
+            // a weight as an integer: the low 23 bits of p s + 2^23; unseen, zero, whatever the step
+            auto bits_of = [&](int e, int r) {
+              const uint32_t y = __float_as_uint(fmaf(p[r], param_step(value_params[e]), 8388608.0f));
+              return kEdge && arg[r] == -INFINITY ? 0u : y;
+            };
+            // eight slots, their low and middle bytes in one 16-byte unit of the token, the high ones in half of another
+            auto put = [&](const uint32_t (&y)[8], int slots, int block, int part) {
               const uint32_t at = weight_at + block * (S::kWeightUnits * 2048) + part * 2048;
               const uint32_t high_at = weight_at + block * (S::kWeightUnits * 2048) + (S::kParts == 1 ? 2048 : (S::kParts + part / 2) * 2048 + (part & 1) * 8);
-              if constexpr (kRows == 1) {
+              if (slots == 1) {
                 sts_8(at, y[0]);
                 sts_8(at + 8, y[0] >> 8);
                 sts_8(high_at, y[0] >> 16);
-              } else {
-                uint32_t low[2], mid[2], high[2];
-#pragma unroll
-                for (int h = 0; h < 2 && 4 * h < kRows; ++h) {
-                  const uint32_t t01 = __byte_perm(y[4 * h], y[4 * h + 1], 0x5140), t23 = __byte_perm(y[4 * h + 2], y[4 * h + 3], 0x5140);
-                  low[h] = __byte_perm(t01, t23, 0x5410);
-                  mid[h] = __byte_perm(t01, t23, 0x7632);
-                  high[h] = __byte_perm(__byte_perm(y[4 * h], y[4 * h + 1], 0x0062), __byte_perm(y[4 * h + 2], y[4 * h + 3], 0x0062), 0x5410);
-                }
-                if constexpr (kRows == 4) {
-                  sts_32(at, low[0]);
-                  sts_32(at + 8, mid[0]);
-                  sts_32(high_at, high[0]);
-                } else {
-                  ptx::sts_128(at, low[0], low[1], mid[0], mid[1]);
-                  sts_64(high_at, high[0], high[1]);
-                }
+                return;
               }
+              uint32_t low[2], mid[2], high[2];
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const uint32_t t01 = __byte_perm(y[4 * h], y[4 * h + 1], 0x5140), t23 = __byte_perm(y[4 * h + 2], y[4 * h + 3], 0x5140);
+                low[h] = __byte_perm(t01, t23, 0x5410);
+                mid[h] = __byte_perm(t01, t23, 0x7632);
+                high[h] = __byte_perm(__byte_perm(y[4 * h], y[4 * h + 1], 0x0062), __byte_perm(y[4 * h + 2], y[4 * h + 3], 0x0062), 0x5410);
+              }
+              if (slots <= 4) {
+                sts_32(at, low[0]);
+                sts_32(at + 8, mid[0]);
+                sts_32(high_at, high[0]);
+              } else {
+                ptx::sts_128(at, low[0], low[1], mid[0], mid[1]);
+                sts_64(high_at, high[0], high[1]);
+              }
+            };
+            if constexpr (S::kShared) {
+#pragma unroll
+              for (int block = 0; block < S::kBlocks; ++block) {
+                uint32_t y[8] = {};
+#pragma unroll
+                for (int slot = 0; slot < S::kSlots; ++slot) y[slot] = bits_of(block * S::kBlockGroups + slot / kRows, slot % kRows);
+                put(y, S::kSlots, block, 0);
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < G; ++e)
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb) {
+                  uint32_t y[8] = {};
+#pragma unroll
+                  for (int r = 0; r < 8 && r < kRows; ++r) y[r] = bits_of(e, rb * 8 + r);
+                  put(y, kRows < 8 ? kRows : 8, e / S::kBlockGroups, e % S::kBlockGroups * NB + rb);
+                }
             }
           }
           ptx::fence_proxy_async_smem();
@@ -741,56 +802,81 @@ attention_kernel(const AttentionArgs a) {
   }
 }
 
-// Joins the segments that workers share, in the order of the workers: a CTA per worker that starts a segment and does not
-// finish it, a warp per row.
+// Joins the segments that workers share: a CTA per worker that starts a segment and does not finish it.  A row's pieces are
+// dealt out to 1 to 16 warps, each adds up its own in the order of the workers, and then theirs are added up.
 template <int D, int G, int ROWS>
 __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const AttentionArgs a) {
   using S = Shape<D, G, ROWS>;
   constexpr int kFours = D / 128 > 0 ? D / 128 : 1;                      // float4 of a lane
+  constexpr int kJoinWarps = kJoinThreads / 32, kSplit = kJoinWarps / (ROWS < kJoinWarps ? ROWS : kJoinWarps);       // warps of a row
+  __shared__ __align__(16) float sums[kJoinWarps][D], weights[kJoinWarps];
   ptx::grid_dependency_wait();
   ptx::grid_dependents_launch();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = blockIdx.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = blockIdx.x, split = warp % kSplit;
   const JoinRecord rec = a.records[first];
   if (rec.workers <= 1) return;
-  for (int r = warp; r < rec.rows; r += kJoinThreads / 32) {
+  for (int r0 = 0; r0 < rec.rows; r0 += kJoinWarps / kSplit) {
+    const int r = r0 + warp / kSplit;
     auto part = [&](int k) {                                             // only the first worker's piece starts the segment
       return a.partial + ((2 * (int64_t)(first + k) + (k == 0 ? 1 : 0)) * S::kRows + r) * (D + 4);
     };
-    float m = -INFINITY;
-    for (int k = lane; k < rec.workers; k += 32) m = fmaxf(m, ptx::ld_global(static_cast<const float*>(part(k) + D)));
-    m = warp_max(m);
-    float l = 0.0f;
+    float m = -INFINITY, l = 0.0f;
     float4 e[kFours] = {};
-    for (int k0 = 0; k0 < rec.workers; k0 += 32) {
-      float f = 0.0f;
-      if (k0 + lane < rec.workers) {
-        const uint2 y = ptx::ld_global(reinterpret_cast<const uint2*>(part(k0 + lane) + D));
-        f = m == -INFINITY ? 1.0f : exp2_approx(__uint_as_float(y.x) - m);
-        l = fmaf(f, __uint_as_float(y.y), l);
-      }
-      const int n = min(32, rec.workers - k0);
-      for (int k = 0; k < n; k += 8) {
-        uint4 y[8][kFours];
+    if (r < rec.rows) {
+      for (int k = lane; k < rec.workers; k += 32) m = fmaxf(m, ptx::ld_global(static_cast<const float*>(part(k) + D)));
+      m = warp_max(m);
+      const int each = (rec.workers + kSplit - 1) / kSplit, from = split * each, upto = min(from + each, rec.workers);
+      for (int k0 = from; k0 < upto; k0 += 32) {
+        float f = 0.0f;
+        if (k0 + lane < upto) {
+          const uint2 y = ptx::ld_global(reinterpret_cast<const uint2*>(part(k0 + lane) + D));
+          f = m == -INFINITY ? 1.0f : exp2_approx(__uint_as_float(y.x) - m);
+          l = fmaf(f, __uint_as_float(y.y), l);
+        }
+        const int n = min(32, upto - k0);
+        for (int k = 0; k < n; k += 8) {
+          uint4 y[8][kFours];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+          for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int i = 0; i < kFours; ++i)
-            y[j][i] = k + j < n && lane + 32 * i < D / 4 ? ptx::ld_global(reinterpret_cast<const uint4*>(part(k0 + k + j)) + lane + 32 * i) : make_uint4(0u, 0u, 0u, 0u);
+            for (int i = 0; i < kFours; ++i)
+              y[j][i] = k + j < n && lane + 32 * i < D / 4 ? ptx::ld_global(reinterpret_cast<const uint4*>(part(k0 + k + j)) + lane + 32 * i) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float fj = __shfl_sync(0xFFFFFFFFu, f, k + j);
+          for (int j = 0; j < 8; ++j) {
+            const float fj = __shfl_sync(0xFFFFFFFFu, f, k + j);
 #pragma unroll
-          for (int i = 0; i < kFours; ++i) {
-            e[i].x = fmaf(fj, __uint_as_float(y[j][i].x), e[i].x);
-            e[i].y = fmaf(fj, __uint_as_float(y[j][i].y), e[i].y);
-            e[i].z = fmaf(fj, __uint_as_float(y[j][i].z), e[i].z);
-            e[i].w = fmaf(fj, __uint_as_float(y[j][i].w), e[i].w);
+            for (int i = 0; i < kFours; ++i) {
+              e[i].x = fmaf(fj, __uint_as_float(y[j][i].x), e[i].x);
+              e[i].y = fmaf(fj, __uint_as_float(y[j][i].y), e[i].y);
+              e[i].z = fmaf(fj, __uint_as_float(y[j][i].z), e[i].z);
+              e[i].w = fmaf(fj, __uint_as_float(y[j][i].w), e[i].w);
+            }
           }
         }
       }
-    }
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, d);
+      for (int d = 1; d < 32; d <<= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, d);
+    }
+    if (kSplit > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kFours; ++i)
+        if (lane + 32 * i < D / 4) *reinterpret_cast<float4*>(&sums[warp][(lane + 32 * i) * 4]) = e[i];
+      if (lane == 0) weights[warp] = l;
+      __syncthreads();
+      if (split == 0) {
+        for (int k = 1; k < kSplit; ++k) {
+          l += weights[warp + k];
+#pragma unroll
+          for (int i = 0; i < kFours; ++i)
+            if (lane + 32 * i < D / 4) {
+              const float4 y = *reinterpret_cast<const float4*>(&sums[warp + k][(lane + 32 * i) * 4]);
+              e[i].x += y.x; e[i].y += y.y; e[i].z += y.z; e[i].w += y.w;
+            }
+        }
+      }
+    }
+    if (split != 0 || r >= rec.rows) continue;
     const int row = rec.first_row + r, new_token = token_of_row(a, row);
     const int64_t out_row = rec.first + new_token;
     const int q_head = rec.head * a.ratio + row - new_token * a.ratio;
@@ -894,7 +980,7 @@ AttentionArgs attention_args(const eqat_cache_desc& d, const eqat_attention_desc
 void cache_attention_plan(const eqat_cache_desc& d, const eqat_attention_desc& a, int sms, int* plan) {
   const bool prompts = prompt_attention_applies(d, a, sms);
   plan[0] = tile_rows(d, a, prompts ? kPromptRows - 1 : INT32_MAX);
-  plan[1] = prompts ? kPromptRows : 0;
+  plan[1] = prompts ? prompt_least_rows(d, a) : 0;
 }
 
 size_t cache_attention_workspace(const eqat_cache_desc& d, const eqat_attention_desc& a) {
@@ -916,9 +1002,11 @@ int launch_cache_attention(const eqat_cache_desc& d, const eqat_attention_desc& 
   AttentionArgs args = attention_args(d, at, Q, q_pitch, view, O, o_pitch, lse);
   args.most_rows = INT32_MAX;
   if (prompt_attention_applies(d, at, sms)) {                            // long sequences there, short ones here
+    args.least_rows = prompt_least_rows(d, at);
     const int rc = launch_prompt_attention(d, args, st);
-    if (rc != EQAT_OK) return rc;
-    args.most_rows = kPromptRows - 1;
+    if (rc != EQAT_OK || args.least_rows == 1) return rc;
+    args.most_rows = args.least_rows - 1;
+    args.least_rows = 0;
   }
   return with_shape(d, tile_rows(d, at, args.most_rows), [&](auto DD, auto GG, auto NN) {
     constexpr int D = decltype(DD)::value, G = decltype(GG)::value, NT = decltype(NN)::value;

@@ -542,10 +542,13 @@ bool prompt_attention_applies(const eqat_cache_desc& d, const eqat_attention_des
   return tiles * 6 >= sms;
 }
 
+int prompt_least_rows(const eqat_cache_desc& d, const eqat_attention_desc& a) {
+  return d.rows * (a.q_heads / d.kv_heads) >= (int64_t)d.sequences * kPromptRows ? 1 : kPromptRows;
+}
+
 int launch_prompt_attention(const eqat_cache_desc& d, AttentionArgs a, cudaStream_t st) {
   const int sms = sm_count(), g = d.head_dim / d.group;
   if (sms <= 0) return EQAT_ERR_CUDA;
-  a.least_rows = kPromptRows;
   a.most_rows = INT32_MAX;
   if (d.head_dim == 64) return g == 1 ? launch_shape<64, 1>(a, sms, st) : launch_shape<64, 2>(a, sms, st);
   return g == 1 ? launch_shape<128, 1>(a, sms, st) : g == 2 ? launch_shape<128, 2>(a, sms, st) : launch_shape<128, 4>(a, sms, st);

@@ -264,13 +264,16 @@ def check_prompt(c, O, lse, Q, held, window=0, rows=None):
 
 @pytest.mark.parametrize("D,group,page", [(128, 128, 16), (128, 64, 48), (128, 32, 64), (64, 64, 16), (64, 32, 32)])
 @pytest.mark.parametrize("window", [0, 1, 77])
-def test_prompts(eqat, D, group, page, window):
-    """Whole prompts, pieces behind a long text, sequences with few rows and none, in one call: both kernels take part."""
-    lengths, news = [260, 300, 61, 5, 700, 1, 1, 33], [260, 1, 60, 0, 150, 1, 3, 33]
+@pytest.mark.parametrize("short", [0, 80])
+def test_prompts(eqat, D, group, page, window, short):
+    """Whole prompts, pieces behind a long text, sequences with few rows and none, in one call; with many short sequences both
+    kernels take part, else the one for prompts has all."""
+    lengths = [260, 300, 61, 5, 700, 1, 1, 33] + [17 + i for i in range(short)]
+    news = [260, 1, 60, 0, 150, 1, 3, 33] + [1] * short
     c = Cache(eqat, D, group, 4, page, lengths, news, seed=D + group + window, pad_rows=2)
     held = c.fill()
     a = eqat.make_attention_desc(32, max(news), D ** -0.5, window)
-    assert eqat.eqat_cache_attention_plan(c.desc(), a)[1] == 64
+    assert eqat.eqat_cache_attention_plan(c.desc(), a)[1] == (64 if short else 1)
     Q, O, lse = run_attention(eqat, c, 32, window=window)
     check_prompt(c, O, lse, Q, held, window)
     for _ in range(3):
@@ -282,7 +285,7 @@ def test_prompts(eqat, D, group, page, window):
 def test_prompts_of_other_head_counts(eqat, ratio, H):
     c = Cache(eqat, 128, 128, H, 16, [190, 401], [190, 130], seed=ratio)
     held = c.fill()
-    assert eqat.eqat_cache_attention_plan(c.desc(), eqat.make_attention_desc(H * ratio, 190, 0.1))[1] == 64
+    assert eqat.eqat_cache_attention_plan(c.desc(), eqat.make_attention_desc(H * ratio, 190, 0.1))[1] == 1
     Q, O, lse = run_attention(eqat, c, H * ratio)
     check_prompt(c, O, lse, Q, held)
 
