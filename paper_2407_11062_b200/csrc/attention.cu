@@ -33,7 +33,7 @@ namespace eqat {
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32, kJoinThreads = 512;
+constexpr int kThreads = kWarps * 32, kJoinThreads = 256;
 // Weights are p = 2^(z - shift), z the score in log2; the shift is the row's largest score (as of its last raise) plus
 // log2(unit) - kOne, unit a power of two above all steps that the row has counted, so p s < 2^23 as long as no score exceeds
 // that maximum by more than kLazy.
@@ -86,7 +86,9 @@ template <typename S, typename F>
 __device__ __forceinline__ WorkPlace find_work(const AttentionArgs& a, int workers, F&& f, int64_t* scratch) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (a.cache.sequences <= 32) {                                         // every warp by itself
-    const int64_t own = lane < a.cache.sequences ? work_units(a.cache, sequence_work<S>(a, lane)) : 0;
+    SequenceWork w{};
+    if (lane < a.cache.sequences) w = sequence_work<S>(a, lane);
+    const int64_t own = work_units(a.cache, w);
     int64_t upto = own;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -95,7 +97,10 @@ __device__ __forceinline__ WorkPlace find_work(const AttentionArgs& a, int worke
     }
     WorkPlace p;
     p.total = __shfl_sync(0xFFFFFFFFu, upto, 31);
-    p.per = max(quotient(p.total + workers - 1, workers), (int64_t)a.min_units);
+    // A tile takes a worker about a microsecond, a piece of a segment the join 0.06: few tiles for a worker where a segment
+    // is short, sqrt(tiles / 16) where it is cut into many pieces (one head, 30000 tokens: 27.8 us with one, 17.8 with four).
+    const unsigned longest = __reduce_max_sync(0xFFFFFFFFu, w.tiles > 0 ? (unsigned)w.units : 0u);
+    p.per = max(quotient(p.total + workers - 1, workers), (int64_t)max(1, (int)sqrtf((float)longest * 0.0625f)));
     const uint32_t behind = __ballot_sync(0xFFFFFFFFu, upto > f(p.per));     // sequences that end behind unit x
     p.sequence = behind == 0u ? a.cache.sequences : __ffs(behind) - 1;
     p.before = __shfl_sync(0xFFFFFFFFu, upto - own, behind == 0u ? 0 : __ffs(behind) - 1);
@@ -122,7 +127,7 @@ __device__ __forceinline__ WorkPlace find_work(const AttentionArgs& a, int worke
   }
   WorkPlace p;
   p.total = total;
-  p.per = max(quotient(total + workers - 1, workers), (int64_t)a.min_units);
+  p.per = max(quotient(total + workers - 1, workers), (int64_t)1);
   const int64_t x = f(p.per);
   if (x >= before && x < before + own) {
     int b = b0;
@@ -930,8 +935,6 @@ int with_shape(const eqat_cache_desc& d, int rows, F&& f) {
   return EQAT_ERR_UNSUPPORTED;
 }
 
-constexpr int kMinUnits = 2;
-
 // Units that a call can have at most, as far as the host knows.
 template <typename S>
 int64_t most_units(const eqat_cache_desc& d, const eqat_attention_desc& a) {
@@ -945,7 +948,7 @@ int64_t most_units(const eqat_cache_desc& d, const eqat_attention_desc& a) {
 
 template <typename S>
 int workers_of(const eqat_cache_desc& d, const eqat_attention_desc& a, int sms) {
-  const int64_t want = (most_units<S>(d, a) + kMinUnits - 1) / kMinUnits;
+  const int64_t want = most_units<S>(d, a);
   const int64_t most = (int64_t)sms * S::kCtas;
   return (int)(want < 1 ? 1 : want < most ? want : most);
 }
@@ -1012,7 +1015,6 @@ int launch_cache_attention(const eqat_cache_desc& d, const eqat_attention_desc& 
     constexpr int D = decltype(DD)::value, G = decltype(GG)::value, NT = decltype(NN)::value;
     using S = Shape<D, G, NT>;
     AttentionArgs a = args;
-    a.min_units = kMinUnits;
     static SmemOptIn opt;
     if (!opt.ensure(attention_kernel<D, G, NT>, S::kSmemBytes)) return (int)EQAT_ERR_CUDA;
     const int workers = workers_of<S>(d, at, sms);

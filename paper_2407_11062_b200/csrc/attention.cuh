@@ -27,7 +27,6 @@ struct AttentionArgs {
   float scale_log2;            // scale * log2(e)
   uint32_t page_mul;           // n / (page_size / 16) = n * page_mul >> page_shift for n < 2^26
   int page_shift;
-  int min_units;               // least number of units of a worker
   int least_rows, most_rows;   // sequences with fewer or more rows (new tokens x ratio) are another kernel's
 };
 
