@@ -104,7 +104,7 @@ AttentionArgs attention_args(const eqat_cache_desc& d, const eqat_attention_desc
 
 // Sequences with at least this many rows (new tokens x query heads of a key/value head) are the prompt kernel's, in calls
 // that it takes part in; all of them are where the average has as many, which saves the launches for few rows.
-constexpr int kPromptRows = 64;
+constexpr int kPromptRows = 33;
 int prompt_least_rows(const eqat_cache_desc& d, const eqat_attention_desc& a);
 bool prompt_attention_applies(const eqat_cache_desc& d, const eqat_attention_desc& a, int sms);
 int launch_prompt_attention(const eqat_cache_desc& d, AttentionArgs a, cudaStream_t st);

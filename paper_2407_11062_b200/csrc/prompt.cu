@@ -1,6 +1,6 @@
 // Attention of many new tokens over the 4-bit cache: prompts and pieces of them.
 //
-// With 64 rows (new tokens x query heads of a key/value head) and more the products bound, not the cache: a CTA takes 256
+// With many rows (new tokens x query heads of a key/value head) the products bound, not the cache: a CTA takes 256
 // rows of one sequence and key/value head, as two halves of 128, against tiles of 128 keys.  The tile's keys and values are
 // expanded once, to bf16 (what eqat_cache_read gives), by four warps; rows are the 128 lanes of both products:
 //     S = Q K^T     128 x 128, operands in shared memory
@@ -535,11 +535,20 @@ int launch_shape(const AttentionArgs& a, int sms, cudaStream_t st) {
 bool prompt_attention_applies(const eqat_cache_desc& d, const eqat_attention_desc& a, int sms) {
   const int64_t ratio = a.q_heads / d.kv_heads;
   if (d.head_dim > 128 || a.max_new * ratio < kPromptRows) return false;
-  // A tile of 256 rows and 128 keys takes one SM about 2700 cycles here and as eight tiles of 32 rows about 17000 in the
-  // kernel for few rows, which deals its tiles out over all SMs and splits a long sequence: few row tiles are better there.
-  const int64_t rows = d.rows < (int64_t)a.max_new * d.sequences ? d.rows : (int64_t)a.max_new * d.sequences;
-  const int64_t tiles = (rows * ratio + 255) / 256 * d.kv_heads;
-  return tiles * 6 >= sms;
+  // Estimated cycles for 128 keys, if all sequences have the same number of rows or, where that is few, as many as possible have
+  // the most and the others one.  Here an SM takes about 4500 for an item, of up to 256 rows, and the items are dealt out whole.  The kernel for few rows takes 3700 for tiles of 32 rows, 2100 for 16 and
+  // 1000 + 100 a group for 8, and spreads any number of tiles over all SMs.  (2000 tokens, 64/8 heads, 40 rows, groups of 128:
+  // 32 sequences 78 us here, 110 there; 4 sequences of 8000 tokens 123 and 62.)
+  const int64_t most = (int64_t)a.max_new * d.sequences, rows = d.rows < most ? d.rows : most;
+  int64_t with = d.sequences < rows ? d.sequences : rows, each = (rows * ratio + with - 1) / with;
+  if (each < kPromptRows) {
+    each = a.max_new * ratio;
+    with = (rows - with) / a.max_new > 1 ? (rows - with) / a.max_new : 1;
+  }
+  const int groups = d.head_dim / d.group, tile = groups >= 4 ? 8 : groups == 2 ? 16 : 32;
+  const double here = (double)((with * d.kv_heads * ((each + 255) / 256) + sms - 1) / sms) * 4500.0;
+  const double there = (double)(with * d.kv_heads * ((each + tile - 1) / tile)) / sms * (tile == 8 ? 1000 + 100 * groups : tile == 16 ? 2100 : 3700);
+  return here < there;
 }
 
 int prompt_least_rows(const eqat_cache_desc& d, const eqat_attention_desc& a) {
