@@ -416,7 +416,8 @@ int eqat_cache_attention_plan(const eqat_cache_desc* desc, const eqat_attention_
  * -infinity.  lse [rows, q_heads] fp32 dense (may be NULL): log of sum_j exp(z_j).
  * Few rows (decoding, drafted tokens): codes enter the products as exact integers,
  * steps and minima multiply the sums, and the weights of the values (softmax times
- * step) are integers of 23 bits, the largest weight of a row between 2^20 and 2^23.
+ * step) are integers of 23 bits, the largest of a row between 2^20 and 2^23: keys
+ * with less than 2^-22 of the largest weight count nothing.
  * Many rows (eqat_cache_attention_plan): keys, values and softmax weights are
  * rounded to bf16, keys and values as eqat_cache_read gives them; a row that sees a
  * group of values that is NaN becomes NaN as a whole.  Softmax statistics and

@@ -143,7 +143,7 @@ int check_attention_desc(const eqat_cache_desc* d, const eqat_attention_desc* a)
   if (a == nullptr) return EQAT_ERR_NULL;
   if (a->q_heads <= 0 || a->q_heads > 65536 || a->q_heads % d->kv_heads != 0) return EQAT_ERR_SHAPE;
   if (a->max_new <= 0 || a->window < 0) return EQAT_ERR_SHAPE;
-  if (d->rows * (a->q_heads / d->kv_heads) > (int64_t)1 << 30) return EQAT_ERR_SHAPE;      // rows x heads are counted in 32 bits
+  if (d->rows * a->q_heads > (int64_t)1 << 30) return EQAT_ERR_SHAPE;      // rows x heads are counted in 32 bits
   if (!(a->scale > -1e30f && a->scale < 1e30f)) return EQAT_ERR_UNSUPPORTED;
   return EQAT_OK;
 }

@@ -1,6 +1,6 @@
 // Attention of new tokens over the 4-bit cache, on the tensor cores without expanding a code to more than a byte.
 //
-// A CTA takes a tile of 128 tokens of one key/value head at a time, for 8 to 32 query rows (new tokens x the query heads
+// A CTA takes a tile of 128 tokens of one key/value head at a time, for 1 to 32 query rows (new tokens x the query heads
 // that share the head).  With step s and minimum m of a group and q a code, K = q s + m and V likewise, so
 //     Q . K_t       = sum over groups of  s_t (sum_d Q_d q_td) + m_t (sum_d Q_d)
 //     sum_t p_t V_t = sum_t (p_t s_t) q_t + sum_t p_t m_t:
@@ -19,6 +19,18 @@
 // is exchanged between threads but a vote: a row's exponent is raised only when a score or a step leaves the range of the
 // 23 bits, then the integer sums are emptied into fp32 registers (a thread is one element of the head there).
 //
+// What bounds it: a tile costs the SM's shared-memory and L1 data path 256 cycles for writing the bytes, 256 for the tensor
+// core's reads of them, about 150 for fetching the codes and some 100 for weights and constants, of 1000 that it takes (HBM
+// would deliver one in 750); 270 instructions of a warp per 16 tokens at 1.9 a cycle.  8 x 65536 tokens, 64/8 heads, groups of
+// 128: 140 us, 4.1 TB/s; with one query head per key/value head 111 us, 5.1 TB/s.  64 x 4096 tokens of uneven lengths, pages of
+// 16: 61 us, 3.0 TB/s; there the ends of segments (queries, first raise, sums over the threads) take a fifth.
+// Measured and not kept:
+//   codes as fp16 operands of mma.sync m16n8k16, fed by ldmatrix (the first form)   64 x 4096: 63 us, 8 x 65536 slower by 12 %
+//   four warps that fetch and spread beside four that weigh                         69 us: the same data path
+//   scores of the next tile under this one's weights, one barrier a tile            73 us
+//   five CTAs an SM in 96 registers                                                 99 us
+// and kept: codes fetched past the L1 (64.8 -> 60.9 us).
+//
 // Work is dealt out in tiles: those of all (sequence, row tile, head) segments are laid end to end and every CTA takes an
 // equal stretch, so batches of any lengths fill the device.  A segment that several CTAs share is joined by a second small
 // kernel in a fixed order.
@@ -36,7 +48,8 @@ constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32, kJoinThreads = 256;
 // Weights are p = 2^(z - shift), z the score in log2; the shift is the row's largest score (as of its last raise) plus
 // log2(unit) - kOne, unit a power of two above all steps that the row has counted, so p s < 2^23 as long as no score exceeds
-// that maximum by more than kLazy.
+// that maximum by more than kLazy.  A weight below 2^-22 of the row's largest rounds to nothing; kLazy = 1 would make that 2^-23
+// and cost the raises that it does not save (64 x 4096 tokens 60.9 -> 63.6 us).
 constexpr float kLazy = 2.0f, kOne = 21.0f;
 
 // D: elements of a head, G: groups in it, ROWS: query rows of a tile (1, 4, or a multiple of eight).
@@ -56,7 +69,7 @@ struct Shape {
   static constexpr int kWeightCols = 16 * kWeightUnits;
   static constexpr int kScoreCols = kShared ? 16 : 16 * NB * G;
   static constexpr int kSumCols = kBlocks * kWeightCols;
-  // tensor memory: sums, then scores; 160 columns are taken as 128 + 32, with the last two score blocks in the 32
+  // tensor memory: sums, then scores; 160 columns are taken as 128 + 32, with the last two groups' scores in the 32
   static constexpr int kCols = kScoreCols + kSumCols;
   static constexpr bool kTwoParts = kCols > 128 && kCols <= 160 && G >= 2 && NB == 1 && !kShared;
   static constexpr int kAlloc = kCols <= 64 ? 64 : kCols <= 128 || kTwoParts ? 128 : kCols <= 256 ? 256 : 512;
@@ -326,7 +339,7 @@ attention_kernel(const AttentionArgs a) {
       if (16 * p < left) {
         const uint4* at = reinterpret_cast<const uint4*>(from + (uint64_t)place.at[p] * (D / 2));
 #pragma unroll
-        for (int j = 0; j < S::kLoads / 2; ++j) to[p * (S::kLoads / 2) + j] = ptx::ld_global(at + 32 * j);
+        for (int j = 0; j < S::kLoads / 2; ++j) to[p * (S::kLoads / 2) + j] = ptx::ld_global_once(at + 32 * j);
       }
   };
   auto fetch_params = [&](uint32_t (&to)[G], const uint32_t* from, const Places& place, int left) {      // of this thread's token

@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
   };
   auto job_of = [&](int64_t x) {                                         // whole warp
     int k = 0;
-    for (int i = 0; i < kThreads; i += 32) k += __popc(__ballot_sync(0xFFFFFFFFu, ctl->before[i + lane] <= x));
+    for (int i = 0; i * each < v.sequences; i += 32) k += __popc(__ballot_sync(0xFFFFFFFFu, (i + lane) * each < v.sequences && ctl->before[i + lane] <= x));
     int b = (k - 1) * each;                                              // the last thread with no more than x before it
     int64_t before = ctl->before[k - 1];
     SequenceWork w;

@@ -325,6 +325,12 @@ __device__ __forceinline__ uint4 ld_global(const uint4* p) {
   asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
   return v;
 }
+// 16 bytes that are read once: they take no line of the SM's cache.
+__device__ __forceinline__ uint4 ld_global_once(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
 // 32 bytes (address a multiple of 32 bytes).
 __device__ __forceinline__ void ld_global_256(const void* p, uint32_t (&r)[8]) {
   asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"

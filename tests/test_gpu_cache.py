@@ -62,7 +62,7 @@ class Cache:
 
     def fill(self):
         """Every token of every sequence, quantised by the oracle; returns the values that the cache stands for."""
-        held, self.sizes = [[], []], [[], []]
+        held, self.sizes, self.steps = [[], []], [[], []], []
         for i in (0, 1):
             for b, n in enumerate(self.lengths):
                 q, s, m = C.quantise(self.tokens(n), self.group)
@@ -71,9 +71,11 @@ class Cache:
                 self.codes[i][page, :, pos % self.page] = C.pack(q)
                 self.params[i][page, :, pos % self.page] = np.stack([s, m], -1)
                 held[i].append(C.values(q, s, m))
-                # what the kernels add up: s q and m for the keys, s (q - 8) and m + 8 s for the values
+                # what the kernels add up: s q and m
                 s, m = (np.repeat(x.astype(np.float64), self.group, -1) for x in (s, m))
-                self.sizes[i].append(s * 15 + np.abs(m) if i == 0 else s * 8 + np.abs(m + 8 * s))
+                self.sizes[i].append(s * 15 + np.abs(m))
+                if i == 1:
+                    self.steps.append(s)
         self.upload()
         return held
 
@@ -191,9 +193,13 @@ def check_attention(c, O, lse, Q, held, window=0, scale=None, rows=None):
     scale = c.D ** -0.5 if scale is None else scale
     want, want_lse, mass, size = C.attention(Q.astype(np.float64), held[0], held[1], c.lengths, c.offsets, scale, window, *c.sizes)
     delta = score_error(size, c.D, c.group)
-    # the output's rounding; that of softmax weights times steps to bf16; scores, in numerator and denominator; exp2, sums
-    # over at most 2^14 tokens a warp and the division in fp32
-    bound = 1.02 * (U * np.abs(want) + U * mass + (2 * delta[..., None] + 2.0 ** -16) * mass) + 1e-30
+    # the output's rounding; scores, in numerator and denominator; exp2, sums and the division in fp32; and each weight times
+    # step off by half a unit, of which the largest (a weight of 1 and at least half the largest step of the row) has 2^20 or
+    # more: 15 codes' worth a key, over a sum of weights of at least 1
+    longest = np.concatenate([np.full(n, k) for n, k in zip(c.news, c.lengths)] + [np.zeros(c.rows - int(c.offsets[-1]))])
+    unit = 15 * np.array([0.0 if not len(z) else float(z.max()) for z in c.steps])
+    each = np.concatenate([np.full(n, u) for n, u in zip(c.news, unit)] + [np.zeros(c.rows - int(c.offsets[-1]))])
+    bound = 1.02 * (U * np.abs(want) + (2 * delta[..., None] + 2.0 ** -16) * mass + (longest * each)[:, None, None] * 2.0 ** -21) + 1e-30
     used = slice(0, int(c.offsets[-1])) if rows is None else rows
     err = np.abs(host(O)[used].astype(np.float64) - want[used])
     bad = ~(err <= bound[used])
@@ -381,6 +387,25 @@ def test_what_a_row_does_not_see_may_be_nan(eqat):
     assert not np.isfinite(host(O)[2:]).any()
 
 
+def test_one_key_above_many(eqat):
+    """A key whose weight is 2^13 to 2^20 times that of each of 20000 others: theirs are few units, and their sum counts."""
+    c = Cache(eqat, 128, 128, 1, 64, [20001], [1], seed=12)
+    held = c.fill()
+    direction = np.sign(c.rng.standard_normal(128)).astype(np.float32)
+    Q = np.broadcast_to(direction, (1, 8, 128)) * np.float32([0.5, 0.75, 1, 1.25, 1.5, 1.75, 2, 2.25])[None, :, None]
+    q, s, m = C.quantise(direction[None, None] * np.float32(2.0), 128)
+    for pos in (0, 1, 9000, 20000):
+        c.codes[0][c.table[0][pos // 64], 0, pos % 64] = C.pack(q)[0, 0]
+        c.params[0][c.table[0][pos // 64], 0, pos % 64] = np.stack([s, m], -1)[0, 0]
+        held[0][0][pos] = C.values(q, s, m)[0]
+    c.upload()
+    Q = C.bf16(Q * np.float32(0.5))
+    _, O, lse = run_attention(eqat, c, 8, Q=Q)
+    check_attention(c, O, lse, Q, held)
+    want = C.attention(Q.astype(np.float64), held[0], held[1], c.lengths, c.offsets, 128 ** -0.5)[0]
+    assert np.linalg.norm(host(O) - want) <= TOL * np.linalg.norm(want)
+
+
 def test_more_rows_than_announced_are_left_out(eqat):
     c = Cache(eqat, 128, 128, 2, 16, [50, 60], [9, 3], seed=7)
     held = c.fill()
@@ -389,6 +414,12 @@ def test_more_rows_than_announced_are_left_out(eqat):
     check_attention(c, O, lse, Q, held, rows=rows)
     left = O[4:9].contiguous().view(torch.uint8)
     assert bool((left == 0xA5).all())
+    c = Cache(eqat, 128, 128, 8, 16, [300, 90], [300, 70], seed=7)            # the same in the kernel for prompts
+    held = c.fill()
+    assert eqat.eqat_cache_attention_plan(c.desc(), eqat.make_attention_desc(32, 120, 0.1))[1] == 1
+    Q, O, lse = run_attention(eqat, c, 32, max_new=120)
+    check_prompt(c, O, lse, Q, held, rows=list(range(120)) + list(range(300, 370)))
+    assert bool((O[120:300].contiguous().view(torch.uint8) == 0xA5).all())
 
 
 def test_arrays_that_say_too_much_stay_inside(eqat):
@@ -490,7 +521,7 @@ def test_streams_and_graphs(eqat):
             for b in range(3):
                 held[i][b][-1] = vals[b]
                 s, m = s8[b].astype(np.float64), m8[b].astype(np.float64)
-                c2.sizes[i][b][-1] = s * 15 + np.abs(m) if i == 0 else s * 8 + np.abs(m + 8 * s)
+                c2.sizes[i][b][-1] = s * 15 + np.abs(m)
         check_attention(c2, o, None, Q, held)
     assert eqat.device_status() == (0, 0)
 
