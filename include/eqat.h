@@ -418,8 +418,10 @@ int eqat_cache_attention_plan(const eqat_cache_desc* desc, const eqat_attention_
  * steps and minima multiply the sums, and the weights of the values (softmax times
  * step) are integers of 23 bits, the largest of a row between 2^20 and 2^23: keys
  * with less than 2^-22 of the largest weight count nothing.
- * Many rows (eqat_cache_attention_plan): keys, values and softmax weights are
- * rounded to bf16, keys and values as eqat_cache_read gives them; a row that sees a
+ * Many rows (eqat_cache_attention_plan): values and softmax weights are rounded to
+ * bf16, values as eqat_cache_read gives them, keys to fp16 in steps of 2^-11 of
+ * themselves or 2^-19 of the key's largest element; an infinite query element makes
+ * its row NaN, and so do products beyond fp32's range; a row that sees a
  * group of values that is NaN becomes NaN as a whole.  Softmax statistics and
  * outputs are held in 32 bits until the final rounding.  What a row does not see
  * does not reach it, NaN or not.

@@ -5,6 +5,10 @@
 // codes, so a group is 4, 8 or 16 neighbouring lanes: minimum and maximum travel as one bf16 pair (maximum, -minimum)
 // through two to four shuffles.  A warp takes one row's keys or values in pieces of 1024 elements and looks its sequence up
 // by a search of 32 offsets at a time while its vectors are on their way.
+//
+// HBM bounds long calls: reading 16 x 4096 tokens of 32 heads, groups of 64, takes 159 us, 0.82 of a copy's bandwidth; appending
+// prompts of 32 heads in groups of 32 with the values handed back 61.5 us, 0.83.  (One piece of a row at a time took 195 and 69.5 us.)
+// A call of one token takes 3 us, a launch.
 #include "cache.cuh"
 
 #include <cuda_bf16.h>

@@ -1,17 +1,23 @@
 // Attention of many new tokens over the 4-bit cache: prompts and pieces of them.
 //
-// With many rows (new tokens x query heads of a key/value head) the products bound, not the cache: a CTA takes 256
-// rows of one sequence and key/value head, as two halves of 128, against tiles of 128 keys.  The tile's keys and values are
-// expanded once, to bf16 (what eqat_cache_read gives), by four warps; rows are the 128 lanes of both products:
-//     S = Q K^T     128 x 128, operands in shared memory
-//     O += P V      P in tensor memory, in the place of S
+// With many rows (new tokens x query heads of a key/value head) the products bound, not the cache: a CTA takes 256 rows of
+// one sequence and key/value head, as two halves of 128, against tiles of 128 keys.  Four warps expand the tile once, its keys
+// to fp16 and its values to bf16 (what eqat_cache_read gives); rows are the 128 lanes of both products, in steps of 64 keys:
+//     S = Q K^T     128 x 64, operands in shared memory, fp16
+//     O += P V      P in tensor memory beside S, bf16
 // Eight warps, one thread a row, do the softmax: maximum, then weights, which go to tensor memory as bf16; a row's sums are
 // rescaled only when its maximum rises by more than 2^8.  A warp for each half issues its products; while one half is in its
 // softmax the other half's products run.
 //
-// Work of one tile and both halves: 8.4 MFLOP a product and half, 2100 cycles at the rate of a library product; about 2300
-// instructions of a warp for each half's softmax and 2000 for the expansion, so the issue of instructions and the tensor
-// core are near one another.
+// Keys as fp16 are off by 2^-11 of themselves at most, as bf16 by 2^-8.  Queries and keys that fp16 holds badly are scaled by
+// powers of two.  Error of the outputs against 64 bits (relative norm), and time, with keys as bf16 and as fp16:
+//     4 prompts of up to 1500, 32 heads of 64               0.0033, 92 us     0.0023, 101 us
+//     1000 new behind 7192, 64/8 heads of 128               0.0020, 326 us    0.0018, 339 us
+//     16 x 5 new, window 4000 (one tile of 40 rows)         0.0022, 72 us     0.0019, 76 us
+//
+// What bounds it: the latency of a step's softmax, about 2500 cycles of which the exponentials and their chain are most (three
+// of eight pairs are polynomials for that reason), and the last wave of CTAs: the second of these has 256 items for 148 SMs.
+// It runs at 760 TFLOP/s of masked-in products there.  Steps of 128 keys took 396 us for it where steps of 64 took 320.
 #include <type_traits>
 
 #include "attention.cuh"
@@ -49,6 +55,8 @@ struct PromptCtl {
   uint32_t tmem;
   int abort;
   alignas(16) uint32_t strange[8][4];                // tokens of the last tiles with a step or minimum that is not finite
+  alignas(16) uint32_t large[8][4];                  // tokens of the last tiles whose keys were scaled, and by
+  uint8_t scaled_by[8][kTile];                       // what power of two: its exponent's bits
   int64_t before[kThreads];                          // units of the sequences before a thread's
   int64_t total;
 };
@@ -56,7 +64,15 @@ struct PromptCtl {
 __device__ __forceinline__ uint32_t as_word(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t*>(&x); }
 __device__ __forceinline__ __nv_bfloat162 as_pair(uint32_t x) { return *reinterpret_cast<__nv_bfloat162*>(&x); }
 
-// q s + m of the codes in nibbles I and I + 4, as a bf16 pair, rounded once.
+__device__ __forceinline__ __half2 as_half_pair(uint32_t x) { return *reinterpret_cast<__half2*>(&x); }
+
+// q s + m of the codes in nibbles I and I + 4, rounded once: as an fp16 pair, as a bf16 pair.
+template <int I>
+__device__ __forceinline__ uint32_t key_pair(uint32_t w, __half2 s, __half2 m) {
+  const uint32_t codes = ((w >> (4 * I)) & 0x000F000Fu) | 0x64006400u;                     // 1024 + q
+  const __half2 r = __hfma2(__hsub2(as_half_pair(codes), as_half_pair(0x64006400u)), s, m);
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
 template <int I>
 __device__ __forceinline__ uint32_t value_pair(uint32_t w, __nv_bfloat162 s, __nv_bfloat162 m) {
   const uint32_t codes = ((w >> (4 * I)) & 0x000F000Fu) | 0x43004300u;
@@ -204,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
     const uint32_t own = (uint32_t)((warp % kHalfWarps) * 32) << 16;
     const uint32_t scores = tmem + h * S::kHalfCols + own, outputs = scores + S::kOutputCol;
     const uint32_t query_row = queries + h * S::kOperandBytes + row_in_half * 128;
-    const float c = fmaxf(fabsf(a.scale_log2), 1e-35f);                  // (not 0: -infinity times 0 is NaN)
+    float c = 1.0f;                                                      // the row's factor: its query is scaled too
     auto wait_sums = [&](uint32_t step) { wait(ctl->sums_done[h][step & 1u], step >> 1); };
     const uint32_t sign = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
     uint32_t n = 0, count = 0, items = 0;                                // steps of this half, tiles of all items, items so far
@@ -219,18 +235,28 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
       if (job.tiles > 0) {
         if (h < job.halves) {
           const uint4* src = reinterpret_cast<const uint4*>(a.Q + out_row * a.q_pitch + (int64_t)q_head * D);
+          // scaled by a power of two, so that the largest element lies in [1, 2), to fp16: exact down to 2^-17, off by at
+          // most 2^-25 below; an infinity becomes NaN: no score of the row means anything
+          uint4 e[D / 8];
+          uint32_t most = 0;
 #pragma unroll
           for (int p = 0; p < D / 8; ++p) {
-            uint4 e = make_uint4(0u, 0u, 0u, 0u);
-            if (real) e = ptx::ld_global(src + p);
-            // an infinity becomes NaN: no score of the row means anything
-            e.x |= __vcmpeq2(e.x & 0x7F807F80u, 0x7F807F80u) & 0x00400040u;
-            e.y |= __vcmpeq2(e.y & 0x7F807F80u, 0x7F807F80u) & 0x00400040u;
-            e.z |= __vcmpeq2(e.z & 0x7F807F80u, 0x7F807F80u) & 0x00400040u;
-            e.w |= __vcmpeq2(e.w & 0x7F807F80u, 0x7F807F80u) & 0x00400040u;
-            ptx::sts_128(query_row + p / 8 * 16384 + (((p % 8) ^ (row_in_half & 7)) << 4), __byte_perm(e.x, e.z, 0x5410) ^ sign,
-                         __byte_perm(e.x, e.z, 0x7632) ^ sign, __byte_perm(e.y, e.w, 0x5410) ^ sign, __byte_perm(e.y, e.w, 0x7632) ^ sign);
+            e[p] = make_uint4(0u, 0u, 0u, 0u);
+            if (real) e[p] = ptx::ld_global(src + p);
+            most = __vmaxu2(most, __vmaxu2(__vmaxu2(e[p].x & 0x7FFF7FFFu, e[p].y & 0x7FFF7FFFu), __vmaxu2(e[p].z & 0x7FFF7FFFu, e[p].w & 0x7FFF7FFFu)));
           }
+          most = max(most & 0xFFFFu, most >> 16);
+          const int up = most == 0 ? 0 : min(max(127 - (int)(most >> 7), -100), 100);
+          const float scale = most >= 0x7F80u ? __int_as_float(0x7FC00000) : __int_as_float((127 + up) << 23);
+          c = fmaxf(fabsf(a.scale_log2) * __int_as_float((127 - up) << 23), 1e-37f);      // (not 0: -infinity times 0 is NaN)
+          auto two = [&](uint32_t lo, uint32_t hi) {                     // bf16 numbers in the high halves
+            const __half2 r = __floats2half2_rn(__uint_as_float(lo) * scale, __uint_as_float(hi) * scale);
+            return *reinterpret_cast<const uint32_t*>(&r) ^ sign;
+          };
+#pragma unroll
+          for (int p = 0; p < D / 8; ++p)
+            ptx::sts_128(query_row + p / 8 * 16384 + (((p % 8) ^ (row_in_half & 7)) << 4), two(e[p].x << 16, e[p].z << 16),
+                         two(e[p].x & 0xFFFF0000u, e[p].z & 0xFFFF0000u), two(e[p].y << 16, e[p].w << 16), two(e[p].y & 0xFFFF0000u, e[p].w & 0xFFFF0000u));
           ptx::fence_proxy_async_smem();
         }
         ptx::tc_fence_before();                                          // the last item's outputs have been read
@@ -265,12 +291,18 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
         const bool edge = t0 < all_low || t0 + kStep > all_high;
         wait(ctl->scores_done[h], n);
         ptx::tc_fence_after();
+        const uint2 large = *reinterpret_cast<const uint2*>(&ctl->large[(first_count + i / 2) & 7u][i & 1 ? 2 : 0]);
         float s[kStep];                                                  // the row's scores
 #pragma unroll
         for (int k = 0; k < kStep; k += 32) ptx::tmem_ld_32x32(scores + k, *reinterpret_cast<uint32_t(*)[32]>(s + k));
         ptx::tmem_ld_wait();
         ptx::tc_fence_before();
         arrive(ctl->scores_read[h]);                                     // the next step's may come
+        if ((large.x | large.y) != 0u) {                                 // keys that fp16 holds badly, each with its own scale
+          const uint8_t* by = ctl->scaled_by[(first_count + i / 2) & 7u] + (i & 1) * kStep;
+#pragma unroll
+          for (int j = 0; j < kStep; ++j) s[j] *= __int_as_float((int)by[j] << 23);
+        }
         if (edge) {
           const int before = high - t0, from = low - t0;
 #pragma unroll
@@ -365,11 +397,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
         a.lse[out_row * a.q_heads + q_head] = empty ? -INFINITY : ((top == -INFINITY ? 0.0f : top * c) + log2f(sum)) * 0.69314718055994531f;
     }
   } else if (warp < 2 * kHalfWarps + kSpreadWarps) {
-    // ================================================================== keys and values as bf16
+    // ================================================================== keys as fp16, values as bf16
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kSpreadRegs));
     const int w4 = warp - 2 * kHalfWarps;                                // 32 tokens of a tile
     const int token_in = lane / kChunks, chunk = lane % kChunks;         // of this lane's first chunk; tokens 32 / kChunks apart
-    constexpr int kStep = 32 / kChunks;
+    constexpr int kApart = 32 / kChunks;
     const uint32_t row_at = (32 * w4 + token_in) * 128 + chunk / 2 * 16384;
     uint32_t count = 0;                                                  // tiles so far
     for (int64_t x = blockIdx.x; x < total; x += gridDim.x) {
@@ -401,17 +433,66 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
             f.codes[k] = make_uint4(0u, 0u, 0u, 0u);
             f.params[k] = 0u;                                            // behind the last key: zeros
             if (16 * p < left) f.codes[k] = ptx::ld_global(from + 32 * j);
-            if (16 * p + j * kStep + token_in < left) f.params[k] = ptx::ld_global(with + j * kStep * G);
+            if (16 * p + j * kApart + token_in < left) f.params[k] = ptx::ld_global(with + j * kApart * G);
           }
         }
       };
-      auto spread = [&](const Fetched& f, uint32_t operand, uint32_t* strange) {
+      // Keys as fp16.  A token whose largest element may be 2^14 or more, or is below 2^-6, where the steps would lose bits to
+      // fp16's least exponent, is scaled by a power of two of its own.
+      // Whether there may be one is found for the warp's tokens at once: none where every step lies in [2^-12, 2^9) and every
+      // minimum below 2^13.
+      auto spread_keys = [&](const Fetched& f, uint32_t operand, uint32_t slot) {
+        uint32_t most = 0, least = 0xFFFFFFFFu;
+#pragma unroll
+        for (int k = 0; k < S::kLoads; ++k) {
+          const uint32_t size = f.params[k] & 0x7FFF7FFFu;
+          most = __vmaxu2(most, size);
+          least = __vminu2(least, size);
+        }
+        const bool ordinary = (least & 0xFFFFu) >= (127 - 12) << 7 && (most & 0xFFFFu) < (127 + 9) << 7 && most >> 16 < (127 + 13) << 7;
+        auto spread = [&](auto scaled) {
+          uint32_t marks = 0;
+#pragma unroll
+          for (int k = 0; k < S::kLoads; ++k) {
+            const int token = 32 * w4 + token_in + k * kApart;
+            const uint32_t param = f.params[k];
+            float down = 1.0f;
+            if (decltype(scaled)::value) {
+              const float bound = fmaf(15.0f, fabsf(param_step(param)), fabsf(param_low(param)));
+              // not finite: the others count; a finite step and minimum may give an infinite bound
+              uint32_t exponent = (param & 0x7F80u) == 0x7F80u || (param & 0x7F800000u) == 0x7F800000u ? 0u : min(__float_as_uint(bound) >> 23, 254u);
+#pragma unroll
+              for (int d = 1; d < kChunks; d <<= 1) exponent = max(exponent, __shfl_xor_sync(0xFFFFFFFFu, exponent, d));
+              const int by = exponent > 127 + 13 ? (int)exponent - (127 + 13) : exponent > 0 && exponent < 127 - 6 ? max((int)exponent - 127, -100) : 0;
+              if (by != 0) marks |= 1u << (token & 31);
+              if (chunk == 0) ctl->scaled_by[slot][token] = (uint8_t)(127 + by);
+              down = __int_as_float((127 - by) << 23);
+            }
+            const __half2 s2 = __float2half2_rn(param_step(param) * down), m2 = __float2half2_rn(param_low(param) * down);
+            const uint32_t w[4] = {f.codes[k].x, f.codes[k].y, f.codes[k].z, f.codes[k].w};
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+              ptx::sts_128(operand + row_at + k * kApart * 128 + (((chunk % 2 * 4 + p) ^ (token & 7)) << 4), key_pair<0>(w[p], s2, m2),
+                           key_pair<1>(w[p], s2, m2), key_pair<2>(w[p], s2, m2), key_pair<3>(w[p], s2, m2));
+          }
+          if (decltype(scaled)::value) marks = __reduce_or_sync(0xFFFFFFFFu, marks);
+          if (lane == 0) ctl->large[slot][w4] = marks;
+        };
+        if (__all_sync(0xFFFFFFFFu, ordinary)) {
+          ctl->scaled_by[slot][32 * w4 + lane] = 127;                    // (the step's other warp may have some)
+          spread(std::false_type());
+        } else {
+          spread(std::true_type());
+        }
+      };
+      // Values as bf16.
+      auto spread_values = [&](const Fetched& f, uint32_t operand, uint32_t* strange) {
         uint32_t marks = 0;
 #pragma unroll
         for (int k = 0; k < S::kLoads; ++k) {
-          const int token = 32 * w4 + token_in + k * kStep;
+          const int token = 32 * w4 + token_in + k * kApart;
           uint32_t param = f.params[k];
-          if (strange != nullptr && ((param & 0x7F80u) == 0x7F80u || (param & 0x7F800000u) == 0x7F800000u)) {
+          if ((param & 0x7F80u) == 0x7F80u || (param & 0x7F800000u) == 0x7F800000u) {
             param = 0u;
             marks |= 1u << (token & 31);
           }
@@ -419,13 +500,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
           const uint32_t w[4] = {f.codes[k].x, f.codes[k].y, f.codes[k].z, f.codes[k].w};
 #pragma unroll
           for (int p = 0; p < 4; ++p)
-            ptx::sts_128(operand + row_at + k * kStep * 128 + (((chunk % 2 * 4 + p) ^ (token & 7)) << 4), value_pair<0>(w[p], s2, m2),
+            ptx::sts_128(operand + row_at + k * kApart * 128 + (((chunk % 2 * 4 + p) ^ (token & 7)) << 4), value_pair<0>(w[p], s2, m2),
                          value_pair<1>(w[p], s2, m2), value_pair<2>(w[p], s2, m2), value_pair<3>(w[p], s2, m2));
         }
-        if (strange != nullptr) {
-          marks = __reduce_or_sync(0xFFFFFFFFu, marks);
-          if (lane == 0) strange[w4] = marks;
-        }
+        marks = __reduce_or_sync(0xFFFFFFFFu, marks);
+        if (lane == 0) strange[w4] = marks;
       };
       Fetched key, value;
       if (job.tiles > 0) {
@@ -437,7 +516,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
       for (int i = 0; i < job.tiles; ++i, ++count) {
         const uint32_t stage = count & 1u, use = count >> 1;
         if (use > 0) wait(ctl->keys_free[stage], use - 1);
-        spread(key, keys + stage * S::kOperandBytes, nullptr);
+        spread_keys(key, keys + stage * S::kOperandBytes, count & 7u);
         ptx::fence_proxy_async_smem();
         arrive(ctl->keys_full[stage]);
         if (i + 1 < job.tiles) {
@@ -445,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
           fetch(key, v.kq, v.kp, i + 1);
         }
         if (use > 0) wait(ctl->values_free[stage], use - 1);
-        spread(value, values + stage * S::kOperandBytes, ctl->strange[count & 7u]);
+        spread_values(value, values + stage * S::kOperandBytes, ctl->strange[count & 7u]);
         ptx::fence_proxy_async_smem();
         arrive(ctl->values_full[stage]);
         if (i + 1 < job.tiles) fetch(value, v.vq, v.vp, i + 1);
@@ -456,7 +535,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
     const int h = warp - (2 * kHalfWarps + kSpreadWarps);                // a warp for each half
     if (h < 2) {
       // ================================================================ the products
-      constexpr uint32_t kScoreDesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kStep / 8) << 17) | (8u << 24);
+      constexpr uint32_t kScoreDesc = (1u << 4) | ((uint32_t)(kStep / 8) << 17) | (8u << 24);      // fp16 operands
       constexpr uint32_t kSumDesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D / 8) << 17) | (8u << 24);
       const uint64_t query_desc = ptx::smem_desc(queries + h * S::kOperandBytes);
       const uint64_t key_desc = ptx::smem_desc(keys), value_desc = ptx::smem_desc(values, 16384);

@@ -251,7 +251,7 @@ def test_drafts_and_chunks(eqat, D, group, H, page, window):
 
 
 def check_prompt(c, O, lse, Q, held, window=0, rows=None):
-    """Keys and values rounded to bf16 (each term of a score off by at most U of itself, each value by U), weights too."""
+    """Values and weights rounded to bf16 (each off by at most U of itself); U bounds the terms of a score too."""
     want, want_lse, mass, size = C.attention(Q.astype(np.float64), held[0], held[1], c.lengths, c.offsets, c.D ** -0.5, window)
     delta = size * (U + 2 * c.D / 16 * 2.0 ** -23 + 2.0 ** -20)
     bound = 1.02 * (U * np.abs(want) + (2 * U + 2 * delta[..., None] + 2.0 ** -14) * mass) + 1e-30
@@ -309,6 +309,34 @@ def test_prompts_with_other_scales(eqat, scale):
     assert (np.abs(host(O) - want) <= 1.02 * (U * np.abs(want) + (2 * U + delta[..., None] + 2.0 ** -14) * (mass + np.abs(want)))).all()
     if scale <= 0.0:
         assert np.linalg.norm(host(O) - want) <= 4 * TOL * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("D,group", [(128, 128), (128, 32), (64, 64)])
+def test_prompts_of_keys_of_every_size(eqat, D, group):
+    """Keys far above and below fp16's range, in sequences of their own and among others, with queries of the inverse size."""
+    c = Cache(eqat, D, group, 4, 16, [300, 290, 400, 333], [300, 290, 200, 333], seed=D + group)
+    held = c.fill()
+    sizes = [2.0 ** 40, 2.0 ** -40, None, 1.0]
+    for b, n in enumerate(c.lengths):
+        by = np.array([1.0, 2.0 ** -16, 2.0 ** -3, 2.0 ** -9])[np.arange(n) // 3 % 4] if sizes[b] is None else np.full(n, sizes[b])
+        pos = np.arange(n)
+        c.params[0][c.table[b][pos // 16], :, pos % 16] *= by[:, None, None, None].astype(np.float32)
+        held[0][b] = held[0][b] * by[:, None, None]
+        c.sizes[0][b] = c.sizes[0][b] * by[:, None, None]
+    c.upload()
+    Q = c.rng.standard_normal((c.rows, 32, D)).astype(np.float32)
+    for b, by in enumerate(sizes):
+        Q[c.offsets[b]:c.offsets[b + 1]] *= 1.0 if by is None else np.float32(1.0 / by)
+    Q = C.bf16(Q)
+    assert eqat.eqat_cache_attention_plan(c.desc(), eqat.make_attention_desc(32, 333, D ** -0.5))[1] == 1
+    _, O, lse = run_attention(eqat, c, 32, Q=Q)
+    check_prompt(c, O, lse, Q, held)
+    # a key is rounded to fp16 (2^-11), with 2^-25 of the power of two at most that its largest element is brought to (from
+    # 2^-6 on): 2^-19 of the largest; a query is exact to 2^-25 of its own
+    _, want_lse, _, size = C.attention(Q.astype(np.float64), held[0], held[1], c.lengths, c.offsets, D ** -0.5)
+    most = np.concatenate([np.abs(Q[c.offsets[b]:c.offsets[b + 1]]).sum(-1) * np.abs(np.asarray(held[0][b])).max() for b in range(4)]) * D ** -0.5
+    delta = size * (2.0 ** -11 + 2.0 ** -16) + most * 2.0 ** -18
+    assert (np.abs(lse.cpu().numpy() - want_lse) <= delta + 2.0 ** -18 * (1 + np.abs(want_lse))).all()
 
 
 def test_prompts_do_not_see_what_is_masked(eqat):
