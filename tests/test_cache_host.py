@@ -187,3 +187,33 @@ def test_the_binding_refuses_what_is_no_row_tensor(eqat):
     for cache in (None, [i, i, i, i], (i, i, i)):
         with pytest.raises((TypeError, ValueError)):
             eqat.eqat_cache_read(d, None, None, None, cache, None, None)
+
+
+@pytest.mark.parametrize("rows,q_heads,kv_heads,D,group,plan", [
+    (1, 64, 8, 128, 128, (8, 0)), (5, 64, 8, 128, 128, (32, 0)), (1000, 64, 8, 128, 128, (32, 1)), (1, 4, 4, 256, 64, (1, 0)),
+    (1000, 4, 4, 256, 64, (8, 0))])
+def test_how_a_call_is_divided(eqat, rows, q_heads, kv_heads, D, group, plan):
+    """One sequence on 148 SMs: few rows, a prompt, heads that the kernel for prompts does not take (tiles of 8 rows at most)."""
+    d = eqat.make_cache_desc(group, D, kv_heads, 16, 4096, 1, 2048, rows)
+    assert eqat.eqat_cache_attention_plan(d, eqat.make_attention_desc(q_heads, rows, 0.1), 148) == plan
+
+
+def test_bad_questions_about_a_call(eqat):
+    d = eqat.make_cache_desc(64, 128, 4, 16, 64, 1, 8, 1)
+    for a, sms in ((eqat.make_attention_desc(3, 1, 0.1), 148), (eqat.make_attention_desc(4, 1, 0.1), -1)):
+        with pytest.raises(eqat.EqatError):
+            eqat.eqat_cache_attention_plan(d, a, sms)
+    many = eqat.make_cache_desc(64, 128, 4, 16, 64, 1, 8, 1 << 28)
+    assert eqat.cache_workspace_bytes(many, eqat.make_attention_desc(4, 1, 0.1)) >= 0
+    with pytest.raises(eqat.EqatError):
+        eqat.cache_workspace_bytes(many, eqat.make_attention_desc(8, 1, 0.1))
+
+
+def test_tensor_memory_is_taken_before_the_next_launch_may_start():
+    """A CTA of the next launch must find what this one holds counted: columns are taken before dependents are let in."""
+    import pathlib
+    csrc = pathlib.Path(__file__).resolve().parents[1] / "paper_2407_11062_b200" / "csrc"
+    for name, kernel in (("attention.cu", "attention_kernel("), ("prompt.cu", "prompt_kernel(")):
+        text = (csrc / name).read_text()
+        body = text[text.index(kernel, text.index("__global__")):]
+        assert 0 < body.index("take_columns(") < body.index("grid_dependents_launch(")
