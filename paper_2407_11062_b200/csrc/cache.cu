@@ -7,7 +7,7 @@
 // by a search of 32 offsets at a time while its vectors are on their way.
 //
 // HBM bounds long calls: reading 16 x 4096 tokens of 32 heads, groups of 64, takes 159 us, 0.82 of a copy's bandwidth; appending
-// prompts of 32 heads in groups of 32 with the values handed back 61.5 us, 0.83.  (One piece of a row at a time took 195 and 69.5 us.)
+// prompts of 32 heads in groups of 32 with the values handed back 60 to 61.5 us, 0.83 to 0.85.  (One piece of a row at a time took 195 and 69.5 us.)
 // A call of one token takes 3 us, a launch.
 #include "cache.cuh"
 

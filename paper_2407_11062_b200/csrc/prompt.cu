@@ -17,7 +17,7 @@
 //
 // What bounds it: the latency of a step's softmax, about 2500 cycles of which the exponentials and their chain are most (three
 // of eight pairs are polynomials for that reason), and the last wave of CTAs: the second of these has 256 items for 148 SMs.
-// It runs at 760 TFLOP/s of masked-in products there.  Steps of 128 keys took 396 us for it where steps of 64 took 320.
+// It runs at 740 TFLOP/s there, masked products not counted.  Steps of 128 keys took 396 us for it where steps of 64 took 320.
 #include <type_traits>
 
 #include "attention.cuh"
