@@ -28,29 +28,53 @@ const at::Tensor& tensor(PyObject* o) {
   return THPVariable_Unpack(o);
 }
 
+// Of a type, and with as many elements as the descriptors say (counted in double: they have not been checked yet).
+void has(const at::Tensor& t, at::ScalarType type, double least) {
+  if (t.scalar_type() != type) {
+    PyErr_Format(PyExc_TypeError, "expected a tensor of type %s", c10::toString(type));
+    throw Refused();
+  }
+  if ((double)t.numel() < least) {
+    PyErr_SetString(PyExc_ValueError, "a tensor has fewer elements than the descriptors say");
+    throw Refused();
+  }
+}
+
 // Address of a contiguous CUDA tensor; None: NULL.
-void* pointer(PyObject* o, size_t* bytes = nullptr) {
+void* pointer(PyObject* o, at::ScalarType type, double least) {
   if (o == Py_None) return nullptr;
   const at::Tensor& t = tensor(o);
+  has(t, type, least);
   if (!t.is_cuda() || !t.is_contiguous()) {
     PyErr_SetString(PyExc_ValueError, "expected a contiguous CUDA tensor");
     throw Refused();
   }
-  if (bytes != nullptr) *bytes = t.nbytes();
   return t.data_ptr();
 }
 
-// Address and row pitch of a [rows, heads, head_dim] tensor whose heads and elements are dense.
-template <typename T>
-T* rows(PyObject* o, int64_t* pitch) {
+// Any type, e.g. a workspace.
+void* bytes_of(PyObject* o, size_t* bytes) {
+  if (o == Py_None) return nullptr;
   const at::Tensor& t = tensor(o);
-  if (!t.is_cuda() || t.dim() != 3 || t.stride(2) != 1 || t.stride(1) != t.size(2)) {
+  *bytes = t.nbytes();
+  return pointer(o, t.scalar_type(), 0.0);
+}
+
+// Address and row pitch of a [rows, heads, head_dim] tensor whose heads and elements are dense.
+eqat_bf16* rows_of(PyObject* o, const eqat_cache_desc& d, int64_t heads, int64_t* pitch) {
+  const at::Tensor& t = tensor(o);
+  has(t, at::kBFloat16, 0.0);
+  if (t.dim() != 3 || t.size(0) < d.rows || t.size(1) != heads || t.size(2) != d.head_dim) {
+    PyErr_SetString(PyExc_ValueError, "a row tensor's shape is not the descriptors' [rows, heads, head_dim]");
+    throw Refused();
+  }
+  if (!t.is_cuda() || t.stride(2) != 1 || t.stride(1) != t.size(2)) {
     PyErr_SetString(PyExc_ValueError, "expected a CUDA tensor [rows, heads, head_dim] with dense heads");
     throw Refused();
   }
   const int64_t least = t.size(1) * t.size(2);
   *pitch = t.size(0) > 1 || t.stride(0) > least ? t.stride(0) : least;
-  return static_cast<T*>(t.data_ptr());
+  return static_cast<eqat_bf16*>(t.data_ptr());
 }
 
 // A descriptor of the binding (a ctypes structure).
@@ -69,13 +93,17 @@ T structure(PyObject* o) {
   return value;
 }
 
-eqat_cache pool(PyObject* o) {
+eqat_cache pool(PyObject* o, const eqat_cache_desc& d) {
   if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) {
     PyErr_SetString(PyExc_TypeError, "expected a cache: (k_codes, k_params, v_codes, v_params)");
     throw Refused();
   }
-  return eqat_cache{static_cast<uint8_t*>(pointer(PyTuple_GET_ITEM(o, 0))), static_cast<eqat_bf16*>(pointer(PyTuple_GET_ITEM(o, 1))),
-                    static_cast<uint8_t*>(pointer(PyTuple_GET_ITEM(o, 2))), static_cast<eqat_bf16*>(pointer(PyTuple_GET_ITEM(o, 3)))};
+  const double tokens = (double)d.pages * d.kv_heads * d.page_size, codes = tokens * d.head_dim / 2;
+  const double params = d.group > 0 ? tokens * (d.head_dim / d.group) * 2 : 0.0;
+  void* p[4];
+  for (int i = 0; i < 4; ++i)
+    p[i] = pointer(PyTuple_GET_ITEM(o, i), i & 1 ? at::kBFloat16 : at::kByte, i & 1 ? params : codes);
+  return eqat_cache{static_cast<uint8_t*>(p[0]), static_cast<eqat_bf16*>(p[1]), static_cast<uint8_t*>(p[2]), static_cast<eqat_bf16*>(p[3])};
 }
 
 template <typename F>
@@ -104,8 +132,16 @@ int launch(F&& f) {
   return rc;
 }
 
-const int32_t* index_of(PyObject* o) { return static_cast<const int32_t*>(pointer(o)); }
-eqat_bf16* bf16_of(PyObject* o) { return static_cast<eqat_bf16*>(pointer(o)); }
+const int32_t* index_of(PyObject* o, double least) { return static_cast<const int32_t*>(pointer(o, at::kInt, least)); }
+eqat_bf16* values_of(PyObject* o, const eqat_cache_desc& d) {
+  return static_cast<eqat_bf16*>(pointer(o, at::kBFloat16, (double)d.rows * d.kv_heads * d.head_dim));
+}
+
+struct Places {
+  const int32_t *offsets, *lengths, *table;
+  Places(PyObject* const* a, const eqat_cache_desc& d)
+      : offsets(index_of(a[0], d.sequences + 1.0)), lengths(index_of(a[1], d.sequences)), table(index_of(a[2], (double)d.sequences * d.max_pages)) {}
+};
 
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 3) {
@@ -131,11 +167,11 @@ PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(n, 9, [&] {
     const auto d = structure<eqat_cache_desc>(a[0]);
     int64_t kp, vp;
-    const auto *K = rows<eqat_bf16>(a[1], &kp), *V = rows<eqat_bf16>(a[2], &vp);
-    const int32_t *off = index_of(a[3]), *len = index_of(a[4]), *table = index_of(a[5]);
-    const eqat_cache c = pool(a[6]);
-    eqat_bf16 *kh = bf16_of(a[7]), *vh = bf16_of(a[8]);
-    return launch([&](void* s) { return g_append(&d, K, kp, V, vp, off, len, table, &c, kh, vh, s); });
+    const auto *K = rows_of(a[1], d, d.kv_heads, &kp), *V = rows_of(a[2], d, d.kv_heads, &vp);
+    const Places place(a + 3, d);
+    const eqat_cache c = pool(a[6], d);
+    eqat_bf16 *kh = values_of(a[7], d), *vh = values_of(a[8], d);
+    return launch([&](void* s) { return g_append(&d, K, kp, V, vp, place.offsets, place.lengths, place.table, &c, kh, vh, s); });
   });
 }
 
@@ -143,10 +179,10 @@ PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return call(n, 7, [&] {
     const auto d = structure<eqat_cache_desc>(a[0]);
-    const int32_t *off = index_of(a[1]), *len = index_of(a[2]), *table = index_of(a[3]);
-    const eqat_cache c = pool(a[4]);
-    eqat_bf16 *kh = bf16_of(a[5]), *vh = bf16_of(a[6]);
-    return launch([&](void* s) { return g_read(&d, off, len, table, &c, kh, vh, s); });
+    const Places place(a + 1, d);
+    const eqat_cache c = pool(a[4], d);
+    eqat_bf16 *kh = values_of(a[5], d), *vh = values_of(a[6], d);
+    return launch([&](void* s) { return g_read(&d, place.offsets, place.lengths, place.table, &c, kh, vh, s); });
   });
 }
 
@@ -156,14 +192,14 @@ PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const auto d = structure<eqat_cache_desc>(a[0]);
     const auto t = structure<eqat_attention_desc>(a[1]);
     int64_t qp, op;
-    const auto* Q = rows<eqat_bf16>(a[2], &qp);
-    const int32_t *off = index_of(a[3]), *len = index_of(a[4]), *table = index_of(a[5]);
-    const eqat_cache c = pool(a[6]);
-    auto* O = rows<eqat_bf16>(a[7], &op);
-    float* lse = static_cast<float*>(pointer(a[8]));
+    const auto* Q = rows_of(a[2], d, t.q_heads, &qp);
+    const Places place(a + 3, d);
+    const eqat_cache c = pool(a[6], d);
+    auto* O = rows_of(a[7], d, t.q_heads, &op);
+    float* lse = static_cast<float*>(pointer(a[8], at::kFloat, (double)d.rows * t.q_heads));
     size_t bytes = 0;
-    void* ws = pointer(a[9], &bytes);
-    return launch([&](void* s) { return g_attention(&d, &t, Q, qp, off, len, table, &c, O, op, lse, ws, bytes, s); });
+    void* ws = bytes_of(a[9], &bytes);
+    return launch([&](void* s) { return g_attention(&d, &t, Q, qp, place.offsets, place.lengths, place.table, &c, O, op, lse, ws, bytes, s); });
   });
 }
 

@@ -217,3 +217,32 @@ def test_tensor_memory_is_taken_before_the_next_launch_may_start():
         text = (csrc / name).read_text()
         body = text[text.index(kernel, text.index("__global__")):]
         assert 0 < body.index("take_columns(") < body.index("grid_dependents_launch(")
+
+
+def test_the_binding_refuses_other_types_and_short_tensors(eqat):
+    """Each tensor in turn with another type or one element or row less; decided before anything else about it."""
+    import torch
+    d, a = eqat.make_cache_desc(64, 128, 2, 16, 3, 4, 5, 6), eqat.make_attention_desc(8, 1, 0.1)
+    x, q = torch.zeros(6, 2, 128, dtype=torch.bfloat16), torch.zeros(6, 8, 128, dtype=torch.bfloat16)
+    for wrong, match, kind in ((x.half(), "BFloat16", TypeError), (x[:5], "shape", ValueError), (x[:, :1], "shape", ValueError), (x, "CUDA", ValueError)):
+        with pytest.raises(kind, match=match):
+            eqat.eqat_cache_append(d, wrong, x, None, None, None, None)
+    for wrong, match, kind in ((q.float(), "BFloat16", TypeError), (q[:5], "shape", ValueError), (x, "shape", ValueError), (q, "CUDA", ValueError)):
+        with pytest.raises(kind, match=match):
+            eqat.eqat_cache_attention(d, a, wrong, None, None, None, None, q)
+    for at, need in ((0, 5), (1, 4), (2, 20)):
+        for t, match, kind in ((torch.zeros(need, dtype=torch.int64), "Int", TypeError),
+                               (torch.zeros(need - 1, dtype=torch.int32), "fewer", ValueError),
+                               (torch.zeros(need, dtype=torch.int32), "CUDA", ValueError)):
+            with pytest.raises(kind, match=match):
+                eqat.eqat_cache_read(d, *[t if i == at else None for i in range(3)], (None,) * 4, None, None)
+    tokens = 3 * 2 * 16
+    for at in range(4):
+        good = torch.zeros(tokens * 4, dtype=torch.bfloat16) if at & 1 else torch.zeros(tokens * 64, dtype=torch.uint8)
+        for t, match, kind in ((good.float(), "expected a tensor of type", TypeError), (good[:-1], "fewer", ValueError), (good, "CUDA", ValueError)):
+            with pytest.raises(kind, match=match):
+                eqat.eqat_cache_read(d, None, None, None, tuple(t if i == at else None for i in range(4)), None, None)
+    for at in range(2):
+        for t, match, kind in ((x.half(), "BFloat16", TypeError), (x[:5], "fewer", ValueError), (x, "CUDA", ValueError)):
+            with pytest.raises(kind, match=match):
+                eqat.eqat_cache_read(d, None, None, None, (None,) * 4, *[t if i == at else None for i in range(2)])

@@ -359,6 +359,23 @@ def test_prompts_do_not_see_what_is_masked(eqat):
     assert np.isfinite(got[50, :3]).all() and np.isfinite(got[50, 4:]).all()
 
 
+def test_outputs_of_another_type_or_size_are_refused(eqat):
+    """On the host: nothing is launched, the outputs stay."""
+    c = Cache(eqat, 128, 128, 2, 16, [40], [1], seed=9)
+    c.fill()
+    a = eqat.make_attention_desc(4, 1, 0.1)
+    Q = torch.zeros(1, 4, 128, dtype=torch.bfloat16, device="cuda")
+    O = torch.full_like(Q, 7.0)
+    ws = torch.empty(max(256, eqat.cache_workspace_bytes(c.desc(), a)), dtype=torch.uint8, device="cuda")
+    for lse, kind in ((torch.zeros(1, 4, dtype=torch.float16, device="cuda"), TypeError), (torch.zeros(3, device="cuda"), ValueError)):
+        with pytest.raises(kind):
+            eqat.eqat_cache_attention(c.desc(), a, Q, *c.where, O, lse, ws)
+    with pytest.raises(TypeError):
+        eqat.eqat_cache_attention(c.desc(), a, Q, *c.where, O.float(), None, ws)
+    torch.cuda.synchronize()
+    assert (O == 7.0).all()
+
+
 def test_nan_queries_spoil_their_own_rows(eqat):
     c = Cache(eqat, 128, 128, 2, 16, [700, 40], [1, 3], seed=8)
     held = c.fill()
