@@ -403,7 +403,8 @@ typedef struct {
 size_t eqat_cache_workspace_bytes(const eqat_cache_desc* desc, const eqat_attention_desc* attn);
 
 /* How eqat_cache_attention divides a call, decided on the host from the descriptors
- * alone (a diagnostic).  `sms` as in eqat_packed_fwd_route; h_plan receives two
+ * alone (a diagnostic).  `sms` as in eqat_packed_fwd_route (0 where there is no
+ * device: 148, as eqat_cache_workspace_bytes assumes there); h_plan receives two
  * numbers: the query rows (new tokens x query heads of a key/value head) for which
  * the kernel for few rows reads a tile of the cache, and the number of rows from
  * which on a sequence goes to the kernel for prompts (0: none does). */

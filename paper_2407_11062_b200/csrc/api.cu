@@ -406,7 +406,9 @@ int eqat_cache_attention_plan(const eqat_cache_desc* d, const eqat_attention_des
   EQAT_TRY(check_attention_desc(d, a));
   if (h_plan == nullptr) return EQAT_ERR_NULL;
   if (sms < 0) return EQAT_ERR_SHAPE;
-  cache_attention_plan(*d, *a, sms > 0 ? sms : sm_count(), h_plan);
+  if (sms == 0) sms = sm_count();
+  if (sms <= 0) sms = 148;                                               // no device: as for the workspace
+  cache_attention_plan(*d, *a, sms, h_plan);
   return EQAT_OK;
 }
 
