@@ -417,8 +417,10 @@ int eqat_cache_attention_plan(const eqat_cache_desc* desc, const eqat_attention_
  * -infinity.  lse [rows, q_heads] fp32 dense (may be NULL): log of sum_j exp(z_j).
  * Few rows (decoding, drafted tokens): codes enter the products as exact integers,
  * steps and minima multiply the sums, and the weights of the values (softmax times
- * step) are integers of 23 bits, the largest of a row between 2^20 and 2^23: keys
- * with less than 2^-22 of the largest weight count nothing.
+ * step) are integers of up to 23 bits, the largest of a row at least 2^20, rounded up
+ * or down by a fixed sequence over the positions so that they are right in the mean:
+ * an output's error is about sqrt(tokens) * 2^-20 of the row's largest product of
+ * softmax, step and 15, besides the output's own rounding to bf16.
  * Many rows (eqat_cache_attention_plan): values and softmax weights are rounded to
  * bf16, values as eqat_cache_read gives them, keys to fp16 in steps of 2^-11 of
  * themselves or 2^-19 of the key's largest element; an infinite query element makes

@@ -10,14 +10,14 @@
 //   scores   kind::f8f6f4: the byte q is the e4m3 number q 2^-9 (0..7 below the normal range, 8..15 in the first binade).
 //            A query row is scaled by a power of two and split into two e4m3 numbers, the second one 2^-4 finer: exact for
 //            bf16 down to 2^-13 of the row's largest element, to 2^-22 of it below.
-//   values   kind::i8: p s as an integer of 23 bits, its three bytes as columns of their own, unsigned codes, sums exact in
-//            32 bits.  (In fp32 the sums of the uncentred codes would be rounded at some thousand times the size of a long
+//   values   kind::i8: p s as an integer of up to 23 bits, its three bytes as columns of their own, unsigned codes, sums exact
+//            in 32 bits.  (In fp32 the sums of the uncentred codes would be rounded at some thousand times the size of a long
 //            even softmax's output.)
 // Groups of the keys are ranges of K with accumulators of their own, groups of the values have columns of their own.
 //
 // Every thread is one token of the tile in the softmax: scores arrive as columns of its lane of tensor memory, so no value
-// is exchanged between threads but a vote: a row's exponent is raised only when a score or a step leaves the range of the
-// 23 bits, then the integer sums are emptied into fp32 registers (a thread is one element of the head there).
+// is exchanged between threads but a vote: a row's exponent is changed only when a weight leaves the range of the 23 bits,
+// then the integer sums are emptied into fp32 registers (a thread is one element of the head there).
 //
 // What bounds it: a tile costs the SM's shared-memory and L1 data path 256 cycles for writing the bytes, 256 for the tensor
 // core's reads of them, about 150 for fetching the codes and some 100 for weights and constants, of 1000 that it takes (HBM
@@ -46,11 +46,18 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32, kJoinThreads = 256;
-// Weights are p = 2^(z - shift), z the score in log2; the shift is the row's largest score (as of its last raise) plus
-// log2(unit) - kOne, unit a power of two above all steps that the row has counted, so p s < 2^23 as long as no score exceeds
-// that maximum by more than kLazy.  A weight below 2^-22 of the row's largest rounds to nothing; kLazy = 1 would make that 2^-23
-// and cost the raises that it does not save (64 x 4096 tokens 60.9 -> 63.6 us).
-constexpr float kLazy = 2.0f, kOne = 21.0f;
+// Weights are p = 2^(z - top), z the score in log2 and top the row's largest as of its last raise.  The integers are
+// w = p s 2^E, rounded, with E of the row such that its largest p s so far, whichever token has it, lies in [2^20, 2^21): a
+// token with large steps that the row hardly sees leaves the others their bits, and so does one that takes nearly all of the
+// softmax and has small steps.  A raise makes both anew; it comes when some w would pass 2^23, or p 2^kLazy.
+// w is rounded down after a number in [0, 1) has been added that depends on the token's position alone (the fractions of
+// multiples of the golden ratio): a long tail of weights below half a unit then counts what it should in the mean.  Rounded to
+// the nearest they would be lost from sum w q and not from sum p and sum p m, which pulled the outputs of rows with one
+// dominant token to the minima of all others' groups.  What is a whole number already stays one.  The error of an output is about that of sqrt(tokens) / 3 units in its
+// sum: 2^-12 of the largest p s q for a million tokens.
+constexpr float kLazy = 8.0f, kTop = 20.0f;
+constexpr int kLeastExponent = -115, kMostExponent = 100;              // of 2^E
+constexpr float kWeightLimit = 8388608.0f * (1.0f - 0x1p-10f);
 
 // D: elements of a head, G: groups in it, ROWS: query rows of a tile (1, 4, or a multiple of eight).
 template <int D, int G, int ROWS>
@@ -218,13 +225,13 @@ struct AttentionCtl {
   uint64_t scores_done, sums_done;
   uint32_t tmem[2];
   int abort;
-  float least_unit;
   // of the query rows
-  float back[ROWS], minus[ROWS], limit[ROWS];          // score in log2 = z * back; minus = -shift; arg above limit: raise
-  float top[ROWS], shift[ROWS], unit[ROWS], factor[ROWS], delta[ROWS];
-  float q_sum[G][ROWS];
+  alignas(16) float back[ROWS], minus[ROWS], limit[ROWS];          // score in log2 = z * back; minus = -top; arg above limit: raise
+  alignas(16) float weight[ROWS], grain[ROWS];         // 2^E, 2^-E
+  float top[ROWS], peak[ROWS], factor[ROWS], delta[ROWS];      // peak: log2 of the largest 2^z s
+  alignas(16) float q_sum[G][ROWS];
   int low[ROWS], high[ROWS];                           // keys that the row sees
-  float warp_top[kWarps][ROWS], warp_step[kWarps][ROWS];
+  float warp_top[kWarps][ROWS], warp_peak[kWarps][ROWS];
   float sums[1 + G][ROWS];
   int64_t scratch[kWarps + 2];
 };
@@ -419,9 +426,9 @@ attention_kernel(const AttentionArgs a) {
       if (part == 0 && (!S::kShared || group == 0)) {
         ctl->back[r] = __int_as_float((127 + 9 - up) << 23);             // undoes the scale and the 2^-9 of the codes
         ctl->minus[r] = 0.0f;
-        ctl->top[r] = ctl->shift[r] = -INFINITY;
+        ctl->top[r] = ctl->peak[r] = -INFINITY;
         ctl->limit[r] = r < sg.rows ? -INFINITY : INFINITY;
-        ctl->unit[r] = r < sg.rows ? 0.0f : INFINITY;
+        ctl->weight[r] = ctl->grain[r] = 0.0f;
         const int pos = base_pos + new_token;
         ctl->high[r] = r < sg.rows ? pos + 1 : 0;
         ctl->low[r] = a.window > 0 ? pos + 1 - a.window : 0;
@@ -447,16 +454,15 @@ attention_kernel(const AttentionArgs a) {
         put(rest, 1, odd2);
       }
     }
-    if (tid == 0) ctl->least_unit = 0.0f;
     // every row of the tile sees the keys [all_low, all_high)
     const int all_high = base_pos + token_of_row(a, sg.first_row) + 1;
     const int all_low = a.window > 0 ? base_pos + token_of_row(a, sg.first_row + sg.rows - 1) + 1 - a.window : 0;
 
     float total[kRows] = {}, low_sum[G][kRows] = {};                     // of this thread's tokens
-    float out[S::kBlocks][kRows] = {};                                   // of this thread's element of the head, in units of codes
+    float out[S::kBlocks][kRows] = {};                                   // of this thread's element of the head: sums of p s q
     int since = 0;                                                       // tiles in the integer sums
 
-    // Adds the integer sums to the registers.  A warp's 32 lanes are the elements 32 warp .. of a block: one group.
+    // Adds the integer sums to the registers, in the rows' present units.  A warp's 32 lanes are the elements 32 warp .. of a block: one group.
     auto empty_sums = [&] {
 #pragma unroll
       for (int k = 0; k < S::kBlocks; ++k)
@@ -473,9 +479,9 @@ attention_kernel(const AttentionArgs a) {
           for (int slot = 0; slot < 8; ++slot) {
             const float sum = fmaf((float)(int)high8[slot], 65536.0f, fmaf((float)(int)low16[8 + slot], 256.0f, (float)(int)low16[slot]));
             if (S::kShared) {
-              if (slot < S::kSlots && slot / kRows == group) out[k][slot % kRows] += sum;
+              if (slot < S::kSlots && slot / kRows == group) out[k][slot % kRows] = fmaf(sum, ctl->grain[slot % kRows], out[k][slot % kRows]);
             } else if (rb * 8 + slot < kRows) {
-              out[k][rb * 8 + slot] += sum;
+              out[k][rb * 8 + slot] = fmaf(sum, ctl->grain[rb * 8 + slot], out[k][rb * 8 + slot]);
             }
           }
         }
@@ -589,23 +595,32 @@ attention_kernel(const AttentionArgs a) {
             if (kEdge) {
               const bool seen = token >= ctl->low[r0 + r] && token < ctl->high[r0 + r];
               arg[r0 + r] = seen ? arg[r0 + r] : -INFINITY;
-              raise |= seen && step > ctl->unit[r0 + r];
             }
             raise |= arg[r0 + r] > lv[r];
           }
         }
-        if (!kEdge) raise |= step > ctl->least_unit;
         // The weights are written before it is known whether some thread wants its row's exponent raised, which is rare
         // behind a segment's first tile.
-        float p[kRows];
+        float p[kRows], w[kRows];
+        float most = __fdividef(kWeightLimit, step);                     // of p 2^E: no w passes 2^23
+        const float add = __uint_as_float(0x3F800000u | ((uint32_t)token * 0x9E3779B1u >> 9)) - 1.0f;
         for (bool unset = i == 0;; unset = false) {
 #pragma unroll
           for (int r = 0; r < kRows; ++r) p[r] = exp2_approx(arg[r]);
-          if (!unset)
-{
-            // a weight as an integer: the low 23 bits of p s + 2^23; unseen, zero, whatever the step
+          if (!unset) {
+#pragma unroll
+            for (int r0 = 0; r0 < kRows; r0 += 4) {
+              const float4 we = *reinterpret_cast<const float4*>(&ctl->weight[r0]);
+              const float wv[4] = {we.x, we.y, we.z, we.w};
+#pragma unroll
+              for (int r = 0; r < 4 && r < kRows; ++r) {
+                w[r0 + r] = p[r0 + r] * wv[r];
+                raise |= w[r0 + r] > most;
+              }
+            }
+            // a weight as an integer: the low 23 bits of w + 2^23; unseen, zero, whatever the step
             auto bits_of = [&](int e, int r) {
-              const uint32_t y = __float_as_uint(fmaf(p[r], param_step(value_params[e]), 8388608.0f));
+              const uint32_t y = __float_as_uint(__fadd_rz(__fmaf_rz(w[r], param_step(value_params[e]), add), 8388608.0f));
               return kEdge && arg[r] == -INFINITY ? 0u : y;
             };
             // eight slots, their low and middle bytes in one 16-byte unit of the token, the high ones in half of another
@@ -659,47 +674,45 @@ attention_kernel(const AttentionArgs a) {
           ptx::tc_fence_before();
           if (!__syncthreads_or(raise)) break;
           raise = false;
-          // largest exponent and step that each row sees in the tile
+          most = INFINITY;                                               // once a tile
+          // the largest score and the largest p s that each row sees in the tile
+          const float step_log2 = log2f(step);
 #pragma unroll
           for (int r = 0; r < kRows; ++r) {
-            const float m = warp_max(arg[r]), u = warp_max(arg[r] == -INFINITY ? 0.0f : step);
+            const float m = warp_max(arg[r]), u = warp_max(arg[r] + step_log2);
             if (lane == 0) {
               ctl->warp_top[warp][r] = m;
-              ctl->warp_step[warp][r] = u;
+              ctl->warp_peak[warp][r] = u;
             }
           }
-          __syncthreads();
-          if (warp == 0) {
-            float unit = INFINITY;
-            if (lane < sg.rows) {
-              const int r = lane;
-              const float m = fmaxf(fmaxf(ctl->warp_top[0][r], ctl->warp_top[1][r]), fmaxf(ctl->warp_top[2][r], ctl->warp_top[3][r]));
-              const float u = fmaxf(fmaxf(ctl->warp_step[0][r], ctl->warp_step[1][r]), fmaxf(ctl->warp_step[2][r], ctl->warp_step[3][r]));
-              unit = ctl->unit[r];
-              float factor = 1.0f, delta = 0.0f;
-              if (m > -INFINITY) {
-                if (u > unit || unit == 0.0f) unit = __uint_as_float((uint32_t)min(max((int)(__float_as_uint(u) >> 23) + 1, 127 - 60), 254) << 23);
-                const float one = kOne - (float)((int)(__float_as_uint(unit) >> 23) - 127);       // log2 of the weight of the maximum
-                const float top = fmaxf(ctl->top[r], m - ctl->minus[r]), shift = top - one;
-                factor = ctl->top[r] == -INFINITY ? 0.0f : exp2_approx(ctl->shift[r] - shift);
-                delta = -shift - ctl->minus[r];
-                ctl->top[r] = top;
-                ctl->shift[r] = shift;
-                ctl->minus[r] = -shift;
-                ctl->limit[r] = one + kLazy;
-                ctl->unit[r] = unit;
-              }
-              ctl->factor[r] = factor;
-              ctl->delta[r] = delta;
-            }
-            unit = -warp_max(-unit);
-            if (lane == 0) ctl->least_unit = unit;
-          }
-          __syncthreads();
           if (since > 0) {
             ptx::tc_fence_after();
             empty_sums();
           }
+          __syncthreads();
+          if (warp == 0 && lane < sg.rows) {
+            const int r = lane;
+            const float m = fmaxf(fmaxf(ctl->warp_top[0][r], ctl->warp_top[1][r]), fmaxf(ctl->warp_top[2][r], ctl->warp_top[3][r]));
+            const float u = fmaxf(fmaxf(ctl->warp_peak[0][r], ctl->warp_peak[1][r]), fmaxf(ctl->warp_peak[2][r], ctl->warp_peak[3][r]));
+            float factor = 1.0f, delta = 0.0f;
+            if (m > -INFINITY) {
+              const float was = ctl->top[r], minus = ctl->minus[r];
+              const float top = fmaxf(was, m - minus), peak = fmaxf(ctl->peak[r], u - minus);
+              // (no steps so far: whatever comes makes a raise)
+              const int e = peak > -INFINITY ? min(max((int)(kTop - floorf(peak - top)), kLeastExponent), kMostExponent) : kMostExponent;
+              factor = was == -INFINITY ? 0.0f : exp2_approx(was - top);
+              delta = -top - minus;
+              ctl->top[r] = top;
+              ctl->peak[r] = peak;
+              ctl->minus[r] = -top;
+              ctl->limit[r] = kLazy;
+              ctl->weight[r] = __int_as_float((127 + e) << 23);
+              ctl->grain[r] = __int_as_float((127 - e) << 23);
+            }
+            ctl->factor[r] = factor;
+            ctl->delta[r] = delta;
+          }
+          __syncthreads();
 #pragma unroll
           for (int r = 0; r < kRows; ++r) {
             const bool own = r < sg.rows;
@@ -788,7 +801,7 @@ attention_kernel(const AttentionArgs a) {
     // a piece that starts inside the segment goes to the worker's first slot, one that ends inside it to the second
     const int64_t part_slot = 2 * (int64_t)blockIdx.x + (done.u0 == 0 ? 1 : 0);
     for (int r = warp; r < done.sg.rows; r += kWarps) {
-      const float m = ctl->shift[r], l = ctl->sums[0][r];
+      const float m = ctl->top[r], l = ctl->sums[0][r];
       const int row = done.sg.first_row + r, new_token = token_of_row(a, row);
       const int64_t out_row = done.rows.first + new_token;
       const int q_head = done.head * a.ratio + row - new_token * a.ratio;
