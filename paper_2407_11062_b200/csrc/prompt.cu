@@ -94,7 +94,14 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return r;
 }
 
-// 2^x by the multiply-add pipes, for x <= 16: 2^n p(f) with n the nearest integer and f in [-1/2, 1/2], p of degree 3 with the
+// The largest of three; NaN if one is.
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// 2^x by the multiply-add pipes, for x <= 16 (a NaN becomes some number: the row's sum is made NaN by its maximum): 2^n p(f) with n the nearest integer and f in [-1/2, 1/2], p of degree 3 with the
 // smallest relative error there (7.5e-5, from the exchange algorithm; a weight is rounded to bf16, 2^-8, right after).  Below
 // -126 it stays at 2^-126.  The special function unit takes 8 cycles for the 32 exponentials of a warp, 1000 cycles for the two
 // halves' steps; three of eight pairs go this way (1000 new tokens behind 7192, 64/8 heads: none 332 us, two 325, three 323,
@@ -301,7 +308,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
         if ((large.x | large.y) != 0u) {                                 // keys that fp16 holds badly, each with its own scale
           const uint8_t* by = ctl->scaled_by[(first_count + i / 2) & 7u] + (i & 1) * kStep;
 #pragma unroll
-          for (int j = 0; j < kStep; ++j) s[j] *= __int_as_float((int)by[j] << 23);
+          for (int j = 0; j < kStep; ++j) {
+            s[j] *= __int_as_float((int)by[j] << 23);
+            if (!(fabsf(s[j]) < INFINITY)) s[j] = __int_as_float(0x7FC00000);          // (-infinity is what is masked)
+          }
         }
         if (edge) {
           const int before = high - t0, from = low - t0;
@@ -310,8 +320,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
         }
         float m4[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-        for (int j = 4; j < kStep; ++j) m4[j & 3] = fmaxf(m4[j & 3], s[j]);
-        const float most = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+        for (int j = 4; j < kStep; j += 8)
+#pragma unroll
+          for (int k = 0; k < 4 && j + 2 * k < kStep; ++k) m4[k] = max_nan(m4[k], s[j + 2 * k], s[j + 2 * k + 1]);
+        const float most = max_nan(max_nan(m4[0], m4[1], m4[2]), m4[3], m4[3]);
         const bool first = top == -INFINITY;
         const bool raise = first ? most > -INFINITY : (most - top) * c > kLazy;
         if (__any_sync(0xFFFFFFFFu, raise)) {
@@ -333,6 +345,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
             }
           }
         }
+        // a score that is NaN or, scaled, beyond fp32: so is everything of the row
+        if (most != -INFINITY) sum = fmaf(0.0f, most * c, sum);
         // ---- weights, two a column, in the place of those of two steps ago: this step's scores were issued behind the
         // product with those
         if (i > 1 && (i & 1) == 0) look(i / 2 - 1);
@@ -460,13 +474,14 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
             if (decltype(scaled)::value) {
               const float bound = fmaf(15.0f, fabsf(param_step(param)), fabsf(param_low(param)));
               // not finite: the others count; a finite step and minimum may give an infinite bound
-              uint32_t exponent = (param & 0x7F80u) == 0x7F80u || (param & 0x7F800000u) == 0x7F800000u ? 0u : min(__float_as_uint(bound) >> 23, 254u);
+              const bool bad = (param & 0x7F80u) == 0x7F80u || (param & 0x7F800000u) == 0x7F800000u;
+              uint32_t exponent = bad ? 0u : min(__float_as_uint(bound) >> 23, 254u);
 #pragma unroll
               for (int d = 1; d < kChunks; d <<= 1) exponent = max(exponent, __shfl_xor_sync(0xFFFFFFFFu, exponent, d));
               const int by = exponent > 127 + 13 ? (int)exponent - (127 + 13) : exponent > 0 && exponent < 127 - 6 ? max((int)exponent - 127, -100) : 0;
               if (by != 0) marks |= 1u << (token & 31);
               if (chunk == 0) ctl->scaled_by[slot][token] = (uint8_t)(127 + by);
-              down = __int_as_float((127 - by) << 23);
+              down = bad ? __int_as_float(0x7FC00000) : __int_as_float((127 - by) << 23);      // NaN, not an infinity, in every score
             }
             const __half2 s2 = __float2half2_rn(param_step(param) * down), m2 = __float2half2_rn(param_low(param) * down);
             const uint32_t w[4] = {f.codes[k].x, f.codes[k].y, f.codes[k].z, f.codes[k].w};

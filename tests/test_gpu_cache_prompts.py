@@ -1,0 +1,63 @@
+"""Attention over the cache for prompts: keys, values and queries at the ends of the numbers' range."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as C
+from test_gpu_cache import Cache, host, run_attention
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def eqat():
+    from paper_2407_11062_b200.build import build_library
+    build_library()
+    from paper_2407_11062_b200 import binding
+    return binding
+
+
+def sixteen(eqat, D, group, seed):
+    """Sixteen sequences of 400 tokens, the last 250 of them new; sequence b is to have something at position 160 + b, which
+    is in the middle of a step for nearly all rows behind it."""
+    c = Cache(eqat, D, group, 2, 16, [400] * 16, [250] * 16, seed=seed)
+    held = c.fill()
+    assert eqat.eqat_cache_attention_plan(c.desc(), eqat.make_attention_desc(8, 250, 0.1))[1] == 1
+    return c, held
+
+
+def check_nan_behind(c, O, lse, heads=slice(None)):
+    """Rows from the position on are NaN, those before it are not."""
+    got, lse = host(O), lse.cpu().numpy()
+    for b in range(16):
+        mine, sums = got[c.offsets[b]:c.offsets[b + 1]], lse[c.offsets[b]:c.offsets[b + 1]]
+        first = 160 + b - 150
+        assert np.isnan(mine[first:, heads]).all() and np.isnan(sums[first:, heads]).all(), b
+        assert np.isfinite(mine[:first]).all() and np.isfinite(sums[:first]).all(), b
+
+
+@pytest.mark.parametrize("D,group", [(128, 128), (128, 32), (64, 64)])
+@pytest.mark.parametrize("bad", ["nan", "infinite minimum", "minus infinite minimum"])
+def test_a_key_that_is_not_finite_reaches_every_row_behind_it(eqat, D, group, bad):
+    c, _ = sixteen(eqat, D, group, D + group)
+    step, low = {"nan": (np.nan, np.nan), "infinite minimum": (0.5, np.inf), "minus infinite minimum": (0.5, -np.inf)}[bad]
+    for b in range(16):
+        page, at = c.table[b][(160 + b) // 16], (160 + b) % 16
+        c.params[0][page, :, at, -1, 0], c.params[0][page, :, at, -1, 1] = step, low
+    c.upload()
+    _, O, lse = run_attention(eqat, c, 8)
+    check_nan_behind(c, O, lse)
+
+
+@pytest.mark.parametrize("D,group", [(128, 128), (64, 32)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_a_score_beyond_fp32_makes_its_row_nan(eqat, D, group, sign):
+    """Keys of 2^126 in one position, all queries positive and of some units: sums of 2^131 and more."""
+    c, _ = sixteen(eqat, D, group, D + group)
+    for b in range(16):
+        page, at = c.table[b][(160 + b) // 16], (160 + b) % 16
+        c.params[0][page, :, at, :, 0], c.params[0][page, :, at, :, 1] = 0.0, sign * 2.0 ** 126
+    c.upload()
+    Q = C.bf16((c.rng.random((c.rows, 8, D)) * 2 + 4).astype(np.float32))
+    _, O, lse = run_attention(eqat, c, 8, Q=Q)
+    check_nan_behind(c, O, lse)
