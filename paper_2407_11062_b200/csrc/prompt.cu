@@ -453,8 +453,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
       };
       // Keys as fp16.  A token whose largest element may be 2^14 or more, or is below 2^-6, where the steps would lose bits to
       // fp16's least exponent, is scaled by a power of two of its own.
-      // Whether there may be one is found for the warp's tokens at once: none where every step lies in [2^-12, 2^9) and every
-      // minimum below 2^13.
+      // Whether there may be one is found for the warp's tokens at once: none where every step lies in [2^-8, 2^9), since 15
+      // steps then reach 2^-6 on one side of zero or the other, and every minimum below 2^13.
       auto spread_keys = [&](const Fetched& f, uint32_t operand, uint32_t slot) {
         uint32_t most = 0, least = 0xFFFFFFFFu;
 #pragma unroll
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
           most = __vmaxu2(most, size);
           least = __vminu2(least, size);
         }
-        const bool ordinary = (least & 0xFFFFu) >= (127 - 12) << 7 && (most & 0xFFFFu) < (127 + 9) << 7 && most >> 16 < (127 + 13) << 7;
+        const bool ordinary = (least & 0xFFFFu) >= (127 - 8) << 7 && (most & 0xFFFFu) < (127 + 9) << 7 && most >> 16 < (127 + 13) << 7;
         auto spread = [&](auto scaled) {
           uint32_t marks = 0;
 #pragma unroll

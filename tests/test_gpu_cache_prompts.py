@@ -61,3 +61,28 @@ def test_a_score_beyond_fp32_makes_its_row_nan(eqat, D, group, sign):
     Q = C.bf16((c.rng.random((c.rows, 8, D)) * 2 + 4).astype(np.float32))
     _, O, lse = run_attention(eqat, c, 8, Q=Q)
     check_nan_behind(c, O, lse)
+
+
+@pytest.mark.parametrize("D,group", [(128, 128), (128, 32), (64, 64)])
+@pytest.mark.parametrize("power", [-12, -10, -9, -8])
+def test_small_steps_keep_what_is_promised_of_a_key(eqat, D, group, power):
+    """Steps of 2^-12 to 2^-8 and minima of 33 * 2^-25, which lie between two fp16 numbers, everywhere but in one element that
+    the queries leave out: a key is off by 2^-11 of itself or 2^-19 of its largest element at most."""
+    c = Cache(eqat, D, group, 4, 16, [300], [300], seed=D + group)
+    held = c.fill()
+    for t in range(300):
+        page, at = c.table[0][t // 16], t % 16
+        c.codes[0][page, :, at] = 0
+        c.codes[0][page, :, at, 0] = 15
+        c.params[0][page, :, at, :, 0], c.params[0][page, :, at, :, 1] = 2.0 ** power, 33 * 2.0 ** -25
+    held[0][0][:] = 33 * 2.0 ** -25
+    held[0][0][:, :, 0] += 15 * 2.0 ** power
+    c.upload()
+    Q = C.bf16(((1 + c.rng.random((300, 32, D))) * 2.0 ** 12).astype(np.float32))
+    Q[..., 0] = 0
+    _, O, lse = run_attention(eqat, c, 32, Q=Q)
+    _, want, _, size = C.attention(Q.astype(np.float64), held[0], held[1], c.lengths, c.offsets, D ** -0.5)
+    most = np.abs(Q).sum(-1) * held[0][0].max() * D ** -0.5
+    # as for keys of every size; the queries are exact
+    delta = size * (2.0 ** -11 + 2.0 ** -16) + most * 2.0 ** -18
+    assert (np.abs(lse.cpu().numpy() - want) <= delta + 2.0 ** -18 * (1 + np.abs(want))).all()
