@@ -425,7 +425,7 @@ int eqat_cache_attention_plan(const eqat_cache_desc* desc, const eqat_attention_
  * bf16, values as eqat_cache_read gives them, keys to fp16 in steps of 2^-11 of
  * themselves or 2^-19 of the key's largest element; an infinite query element makes
  * its row NaN, and so do products beyond fp32's range; a row that sees a
- * group of values that is NaN becomes NaN as a whole.  Softmax statistics and
+ * group of values that is NaN, or that bf16 cannot hold, becomes NaN as a whole.  Softmax statistics and
  * outputs are held in 32 bits until the final rounding.  What a row does not see
  * does not reach it, NaN or not.
  * Repeated calls give the same bits on one device; the order in which a long

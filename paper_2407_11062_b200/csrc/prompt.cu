@@ -33,6 +33,7 @@ constexpr int kThreads = (2 * kHalfWarps + kSpreadWarps + 4) * 32;      // two o
 // Registers of a thread: 128 at launch, divided anew over the four groups of warps (184 + 184 + 88 + 56 = 4 * 128).
 constexpr int kSoftmaxRegs = 184, kSpreadRegs = 88, kProductRegs = 56;
 constexpr float kLazy = 8.0f;                        // a maximum may be exceeded by 2^8 before the sums are rescaled
+constexpr float kInfiniteValue = 0x1.FFp127f;        // rounds to an infinity of bf16, and all above
 constexpr int kTile = 128, kStep = 64;               // keys that are expanded, that are multiplied at once
 
 template <int D, int G>
@@ -54,7 +55,7 @@ struct PromptCtl {
   uint64_t weights_full[2][2], sums_done[2][2];      // of a half's even and odd steps: either side may be two steps ahead
   uint32_t tmem;
   int abort;
-  alignas(16) uint32_t strange[8][4];                // tokens of the last tiles with a step or minimum that is not finite
+  alignas(16) uint32_t strange[8][4];                // tokens of the last tiles with a group that bf16 cannot hold
   alignas(16) uint32_t large[8][4];                  // tokens of the last tiles whose keys were scaled, and by
   uint8_t scaled_by[8][kTile];                       // what power of two: its exponent's bits
   int64_t before[kThreads];                          // units of the sequences before a thread's
@@ -282,7 +283,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
       const int all_high = base_pos + token_of_row(a, job.sg.first_row + h * 128) + 1;
       const int all_low = a.window > 0 ? base_pos + token_of_row(a, job.sg.first_row + last_row) + 1 - a.window : 0;
       float top = -INFINITY, sum = 0.0f;                                 // of the scores, before the scale; of the weights
-      // Values that are not finite have been spread as zeros, since zero times NaN is not zero: a row that sees one is NaN.
+      // Groups of values that bf16 cannot hold have been spread as zeros, since zero times NaN is not zero: a row that sees
+      // one is NaN.
       bool strange = false;
       auto look = [&](int i) {                                           // at a tile whose values have been multiplied
         const uint4 y = *reinterpret_cast<const uint4*>(ctl->strange[(first_count + i) & 7u]);
@@ -500,14 +502,14 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
           spread(std::true_type());
         }
       };
-      // Values as bf16.
+      // Values as bf16.  A group that is not finite, or whose largest value would round to an infinity, is marked.
       auto spread_values = [&](const Fetched& f, uint32_t operand, uint32_t* strange) {
         uint32_t marks = 0;
 #pragma unroll
         for (int k = 0; k < S::kLoads; ++k) {
           const int token = 32 * w4 + token_in + k * kApart;
           uint32_t param = f.params[k];
-          if ((param & 0x7F80u) == 0x7F80u || (param & 0x7F800000u) == 0x7F800000u) {
+          if (!(fabsf(fmaf(15.0f, param_step(param), param_low(param))) < kInfiniteValue)) {
             param = 0u;
             marks |= 1u << (token & 31);
           }

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import cache_oracle as C
-from test_gpu_cache import Cache, host, run_attention
+from test_gpu_cache import Cache, check_prompt, host, run_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -86,3 +86,27 @@ def test_small_steps_keep_what_is_promised_of_a_key(eqat, D, group, power):
     # as for keys of every size; the queries are exact
     delta = size * (2.0 ** -11 + 2.0 ** -16) + most * 2.0 ** -18
     assert (np.abs(lse.cpu().numpy() - want) <= delta + 2.0 ** -18 * (1 + np.abs(want))).all()
+
+
+@pytest.mark.parametrize("D,group", [(128, 128), (128, 32), (64, 64)])
+def test_values_that_round_to_an_infinity_reach_those_who_see_them_only(eqat, D, group):
+    """A group of finite numbers from 2^119 to bf16's largest: step 17 * 2^120, the largest code stands for 255.5 * 2^120."""
+    c, held = sixteen(eqat, D, group, D + group)
+    x = np.full(D, 2.0 ** 119, np.float32)
+    x[-1] = 255 * 2.0 ** 120
+    q, s, m = C.quantise(x, group)
+    assert np.isfinite(C.bf16(x)).all() and np.isinf(C.bf16(C.values(q, s, m).astype(np.float32))[-1])
+    for b in range(16):
+        page, at = c.table[b][(160 + b) // 16], (160 + b) % 16
+        c.codes[1][page, :, at], c.params[1][page, :, at] = C.pack(q), np.stack([s, m], -1)
+    c.upload()
+    Q, O, lse = run_attention(eqat, c, 8)
+    got, before = host(O), []
+    for b in range(16):
+        first = c.offsets[b] + 10 + b
+        assert np.isnan(got[first:c.offsets[b + 1]]).all()
+        before += range(c.offsets[b], first)
+    assert np.isfinite(lse.cpu().numpy()).all()
+    for b in range(16):
+        held[1][b][160 + b] = 0.0
+    check_prompt(c, O, None, Q, held, rows=before)
