@@ -414,7 +414,8 @@ int eqat_cache_attention_plan(const eqat_cache_desc* desc, const eqat_attention_
  * rows' own keys and values (eqat_cache_append):
  *     z_j = scale * sum_d Q_d K_jd,   O = sum_j softmax(z)_j V_j,
  * over the keys j that a row sees.  A row that sees none gets zeros, and lse
- * -infinity.  lse [rows, q_heads] fp32 dense (may be NULL): log of sum_j exp(z_j).
+ * -infinity.  A query row whose largest element is below 2^-100 loses bits.
+ * lse [rows, q_heads] fp32 dense (may be NULL): log of sum_j exp(z_j).
  * Few rows (decoding, drafted tokens): codes enter the products as exact integers,
  * steps and minima multiply the sums, and the weights of the values (softmax times
  * step) are integers of up to 23 bits, the largest of a row at least 2^20, rounded up
@@ -424,10 +425,10 @@ int eqat_cache_attention_plan(const eqat_cache_desc* desc, const eqat_attention_
  * Many rows (eqat_cache_attention_plan): values and softmax weights are rounded to
  * bf16, values as eqat_cache_read gives them, keys to fp16 in steps of 2^-11 of
  * themselves or 2^-19 of the key's largest element; an infinite query element makes
- * its row NaN, and so do products beyond fp32's range; a row that sees a
- * group of values that is NaN, or that bf16 cannot hold, becomes NaN as a whole.  Softmax statistics and
- * outputs are held in 32 bits until the final rounding.  What a row does not see
- * does not reach it, NaN or not.
+ * its row NaN, and so do products of keys and the row brought to [1, 2) that pass
+ * fp32's range; a row that sees a group of values that is NaN, or that bf16 cannot
+ * hold, becomes NaN as a whole.  Softmax statistics and outputs are held in 32 bits
+ * until the final rounding.  What a row does not see does not reach it, NaN or not.
  * Repeated calls give the same bits on one device; the order in which a long
  * sequence is added up depends on the lengths of the whole batch.
  *   Q [rows, q_heads, head_dim] bf16 (in)   O [rows, q_heads, head_dim] bf16 (out) */

@@ -411,20 +411,20 @@ attention_kernel(const AttentionArgs a) {
       for (int j = 0; j < kEach / 2; ++j) {
         most = __vmaxu2(most, e[j] & 0x7FFF7FFFu);
         if (S::kShared && part * kEach / kGroup != group) e[j] = 0u;
-        sum += param_step(e[j]) + param_low(e[j]);
+        sum += (param_step(e[j]) + param_low(e[j])) * 0x1p-9f;           // (128 of the largest numbers stay finite)
       }
       most = max(most & 0xFFFFu, most >> 16);
 #pragma unroll
       for (int d = 1; d < 16; d <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
 #pragma unroll
       for (int d = 1; d < (S::kShared ? 16 : kGroup / kEach); d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-      const int up = most == 0 ? 0 : min(max(7 - ((int)(most >> 7) - 127), -100), 100);
+      const int up = most == 0 ? 0 : min(7 - ((int)(most >> 7) - 127), 100);       // -120 at least
       const float scale = __int_as_float((127 + up) << 23);
       if (most >= 0x7F80u) sum = __int_as_float(0x7FC00000);             // a NaN or an infinity: so are all scores
       if (S::kShared ? part == 0 : part % (kGroup / kEach) == 0)
-        ctl->q_sum[S::kShared ? 0 : part * kEach / kGroup][slot] = sum * __int_as_float((127 + up - 9) << 23);
+        ctl->q_sum[S::kShared ? 0 : part * kEach / kGroup][slot] = sum * __int_as_float((127 + up + 9) << 23);
       if (part == 0 && (!S::kShared || group == 0)) {
-        ctl->back[r] = __int_as_float((127 + 9 - up) << 23);             // undoes the scale and the 2^-9 of the codes
+        ctl->back[r] = __int_as_float((127 - up) << 23);                 // undoes the scale
         ctl->minus[r] = 0.0f;
         ctl->top[r] = ctl->peak[r] = -INFINITY;
         ctl->limit[r] = r < sg.rows ? -INFINITY : INFINITY;
@@ -548,7 +548,7 @@ attention_kernel(const AttentionArgs a) {
         const float qv[8] = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
 #pragma unroll
         for (int e = 0; e < G; ++e) {
-          const float ks = param_step(key_params[e]) * a.scale_log2, km = param_low(key_params[e]) * a.scale_log2;
+          const float ks = param_step(key_params[e]) * (a.scale_log2 * 512.0f), km = param_low(key_params[e]) * a.scale_log2;
           step = fmaxf(step, param_step(value_params[e]));
 #pragma unroll
           for (int r = 0; r < kRows; ++r) {
@@ -560,7 +560,7 @@ attention_kernel(const AttentionArgs a) {
       } else {
 #pragma unroll
         for (int e = 0; e < G; ++e) {
-          const float ks = param_step(key_params[e]) * a.scale_log2, km = param_low(key_params[e]) * a.scale_log2;
+          const float ks = param_step(key_params[e]) * (a.scale_log2 * 512.0f), km = param_low(key_params[e]) * a.scale_log2;
           step = fmaxf(step, param_step(value_params[e]));
 #pragma unroll
           for (int rb = 0; rb < NB; ++rb) {

@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
       if (job.tiles > 0) {
         if (h < job.halves) {
           const uint4* src = reinterpret_cast<const uint4*>(a.Q + out_row * a.q_pitch + (int64_t)q_head * D);
-          // scaled by a power of two, so that the largest element lies in [1, 2), to fp16: exact down to 2^-17, off by at
+          // scaled by a power of two, so that the largest element lies in [1, 2), [2, 4) from 2^127 on, to fp16: exact down to 2^-17, off by at
           // most 2^-25 below; an infinity becomes NaN: no score of the row means anything
           uint4 e[D / 8];
           uint32_t most = 0;
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
             most = __vmaxu2(most, __vmaxu2(__vmaxu2(e[p].x & 0x7FFF7FFFu, e[p].y & 0x7FFF7FFFu), __vmaxu2(e[p].z & 0x7FFF7FFFu, e[p].w & 0x7FFF7FFFu)));
           }
           most = max(most & 0xFFFFu, most >> 16);
-          const int up = most == 0 ? 0 : min(max(127 - (int)(most >> 7), -100), 100);
+          const int up = most == 0 ? 0 : min(max(127 - (int)(most >> 7), -126), 100);
           const float scale = most >= 0x7F80u ? __int_as_float(0x7FC00000) : __int_as_float((127 + up) << 23);
           c = fmaxf(fabsf(a.scale_log2) * __int_as_float((127 - up) << 23), 1e-37f);      // (not 0: -infinity times 0 is NaN)
           auto two = [&](uint32_t lo, uint32_t hi) {                     // bf16 numbers in the high halves
@@ -480,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
               uint32_t exponent = bad ? 0u : min(__float_as_uint(bound) >> 23, 254u);
 #pragma unroll
               for (int d = 1; d < kChunks; d <<= 1) exponent = max(exponent, __shfl_xor_sync(0xFFFFFFFFu, exponent, d));
-              const int by = exponent > 127 + 13 ? (int)exponent - (127 + 13) : exponent > 0 && exponent < 127 - 6 ? max((int)exponent - 127, -100) : 0;
+              const int by = exponent > 127 + 13 ? (int)exponent - (127 + 13) : exponent > 0 && exponent < 127 - 6 ? (int)exponent - 127 : 0;
               if (by != 0) marks |= 1u << (token & 31);
               if (chunk == 0) ctl->scaled_by[slot][token] = (uint8_t)(127 + by);
               down = bad ? __int_as_float(0x7FC00000) : __int_as_float((127 - by) << 23);      // NaN, not an infinity, in every score

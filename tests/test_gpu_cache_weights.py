@@ -152,3 +152,33 @@ def test_flat_groups_of_values(eqat, ratio, size):
     check_norms(got[:1], want[:1])
     check_norms(got[1:, :, :64], want[1:, :, :64])
     check_norms(got[1:, :, 64:], want[1:, :, 64:])
+
+
+@pytest.mark.parametrize("n", [1, 200])
+@pytest.mark.parametrize("power,keys,scale", [(-98, 98, 1.0), (100, -100, 1.0), (110, -110, 1.0), (118, -118, 1.0), (124, -118, 2.0 ** -6)])
+def test_queries_of_any_size(eqat, n, power, keys, scale):
+    """With keys of the inverse size, in the kernel for few rows and in the one for prompts; one such row among ordinary ones."""
+    c = Cache(eqat, 128, 64, 4, 16, [300, 290], [n, n], seed=7)
+    held, scale = c.fill(), scale * 128 ** -0.5
+    assert eqat.eqat_cache_attention_plan(c.desc(), eqat.make_attention_desc(32, n, 0.1))[1] == (n > 1)
+    ordinary = [p.copy() for p in c.params], [h.copy() for h in held[0]]
+    for b, tokens in enumerate(c.lengths):
+        pos = np.arange(tokens)
+        c.params[0][c.table[b][pos // 16], :, pos % 16] *= np.float32(2.0 ** keys)
+        held[0][b] = held[0][b] * 2.0 ** keys
+    c.upload()
+    Q = c.rng.standard_normal((c.rows, 32, 128)).astype(np.float32)
+    Q[..., 3] = 2.0 + np.abs(Q[..., 3])                         # every row's largest element lies in [2, 8)
+    large = C.bf16(Q * np.float32(2.0 ** power))
+    assert (np.abs(large).max(-1) >= 2.0 ** (power + 1)).all() and (np.abs(large).max(-1) < 2.0 ** (power + 3)).all()
+    _, O, _ = run_attention(eqat, c, 32, Q=large, scale=scale)
+    check_norms(host(O).astype(np.float64), C.attention(large.astype(np.float64), held[0], held[1], c.lengths, c.offsets, scale)[0])
+    c.params, held[0] = ordinary
+    c.upload()
+    Q = C.bf16(Q)
+    want = C.attention(Q.astype(np.float64), held[0], held[1], c.lengths, c.offsets, 128 ** -0.5)[0]
+    Q[0, 1] = large[0, 1]
+    _, O, _ = run_attention(eqat, c, 32, Q=Q)
+    got = host(O).astype(np.float64)
+    got[0, 1] = want[0, 1]
+    check_norms(got, want)
