@@ -103,9 +103,24 @@ AttentionArgs attention_args(const eqat_cache_desc& d, const eqat_attention_desc
                              const CacheView& view, eqat_bf16* O, int64_t o_pitch, float* lse);
 
 // Sequences with at least this many rows (new tokens x query heads of a key/value head) are the prompt kernel's, in calls
-// that it takes part in; all of them are where the average has as many, which saves the launches for few rows.
+// that it takes part in; all of them are where that is estimated to be no worse, which saves the launches for few rows.
 constexpr int kPromptRows = 33;
-int prompt_least_rows(const eqat_cache_desc& d, const eqat_attention_desc& a);
+
+// A call as unequal as its descriptors allow: as many sequences as possible with max_new new tokens, the others with what is
+// left of the rows.
+struct UnequalBatch {
+  int64_t with, rest, each;    // sequences with the most new tokens, others, and the tokens of one of these, rounded up
+};
+inline UnequalBatch unequal_batch(const eqat_cache_desc& d, const eqat_attention_desc& a) {
+  const int64_t have = d.sequences < d.rows ? d.sequences : d.rows;      // with any
+  const int64_t most = have * a.max_new, rows = d.rows < most ? d.rows : most;
+  UnequalBatch u{};
+  u.with = a.max_new > 1 ? (rows - have) / (a.max_new - 1) : have;
+  u.rest = have - u.with;
+  u.each = u.rest > 0 ? (rows - u.with * a.max_new + u.rest - 1) / u.rest : 0;
+  return u;
+}
+int prompt_least_rows(const eqat_cache_desc& d, const eqat_attention_desc& a, int sms);
 bool prompt_attention_applies(const eqat_cache_desc& d, const eqat_attention_desc& a, int sms);
 int launch_prompt_attention(const eqat_cache_desc& d, AttentionArgs a, cudaStream_t st);
 

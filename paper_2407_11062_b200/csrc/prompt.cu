@@ -647,8 +647,21 @@ bool prompt_attention_applies(const eqat_cache_desc& d, const eqat_attention_des
   return here < there;
 }
 
-int prompt_least_rows(const eqat_cache_desc& d, const eqat_attention_desc& a) {
-  return d.rows * (a.q_heads / d.kv_heads) >= (int64_t)d.sequences * kPromptRows ? 1 : kPromptRows;
+int prompt_least_rows(const eqat_cache_desc& d, const eqat_attention_desc& a, int sms) {
+  const int64_t ratio = a.q_heads / d.kv_heads;
+  if (d.rows * ratio < (int64_t)d.sequences * kPromptRows) return kPromptRows;
+  if ((d.rows - (int64_t)(d.sequences - 1) * a.max_new) * ratio >= kPromptRows) return 1;        // none can have fewer
+  // Cycles where short sequences, as long as the table has room for and with one row, become items here, and where they go to
+  // the kernel for few rows: an item takes 4500 for 128 keys, a tile there 1000, the two launches 17000 (9 us).  The long ones
+  // are taken as whole prompts.  (64/8 heads, all here against divided: a prompt of 2000 and one token behind 32768 604 and 173 us,
+  // and 31 such tokens 1182 and 408; four prompts of 640 to 1336 178 and 187.)
+  const UnequalBatch u = unequal_batch(d, a);
+  const double length = (double)d.max_pages * d.page_size, key = 4500.0 / 128;
+  const double prompts = (double)(u.with * d.kv_heads * ((a.max_new * ratio + 255) / 256)) * a.max_new / 2 / sms;
+  const double shorts = (double)(u.rest * d.kv_heads) * length / sms;
+  const double together = (prompts + shorts > length ? prompts + shorts : length) * key;
+  const double apart = (prompts > a.max_new ? prompts : a.max_new) * key + shorts / 128 * 1000 + 17000;
+  return together <= apart ? 1 : kPromptRows;
 }
 
 int launch_prompt_attention(const eqat_cache_desc& d, AttentionArgs a, cudaStream_t st) {

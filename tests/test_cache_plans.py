@@ -25,3 +25,19 @@ def test_a_plan_without_a_device_is_that_of_148_sms(eqat):
             "    print(e.eqat_cache_attention_plan(d, a) == e.eqat_cache_attention_plan(d, a, 148))\n")
     done = subprocess.run([sys.executable, "-c", code], cwd=ROOT, env={**os.environ, "CUDA_VISIBLE_DEVICES": ""}, capture_output=True, text=True)
     assert done.returncode == 0 and done.stdout.split() == ["True", "True"], (done.returncode, done.stdout, done.stderr[-500:])
+
+
+@pytest.mark.parametrize("sequences,new,most,length,heads,plan", [
+    # one prompt beside decoding over long texts: the texts are the kernel's for few rows, in tiles of one token's rows
+    (32, 2031, 2000, 32768, (64, 8), (8, 33)), (2, 2001, 2000, 32768, (64, 8), (8, 33)), (32, 2031, 2000, 4096, (64, 8), (8, 33)),
+    (256, 767, 512, 2048, (64, 8), (8, 33)), (256, 767, 512, 1024, (32, 32), (1, 33)),
+    # prompts only, of different lengths: one launch
+    (4, 3952, 1336, 1344, (64, 8), (32, 1)), (4, 3952, 1336, 1344, (32, 32), (32, 1)), (8, 2350, 700, 704, (64, 8), (32, 1)),
+    # none can be short, whatever the lengths
+    (1, 1000, 1000, 1 << 20, (64, 8), (32, 1)), (2, 1020, 1000, 1 << 20, (64, 8), (32, 1)),
+    # few rows only: tiles for an ordinary sequence
+    (100, 103, 4, 4096, (64, 8), (16, 0)), (100, 100, 4, 4096, (64, 8), (8, 0)), (16, 64, 4, 6016, (64, 8), (32, 0)),
+    (100, 100, 16, 4096, (8, 8), (1, 0))])
+def test_unequal_batches(eqat, sequences, new, most, length, heads, plan):
+    d = eqat.make_cache_desc(128, 128, heads[1], 16, 1 << 18, sequences, length // 16, new)
+    assert eqat.eqat_cache_attention_plan(d, eqat.make_attention_desc(heads[0], most, 0.1), 148) == plan

@@ -110,3 +110,16 @@ def test_values_that_round_to_an_infinity_reach_those_who_see_them_only(eqat, D,
     for b in range(16):
         held[1][b][160 + b] = 0.0
     check_prompt(c, O, None, Q, held, rows=before)
+
+
+@pytest.mark.parametrize("D,group,ratio", [(128, 128, 8), (128, 32, 8), (64, 64, 3), (128, 64, 4)])
+def test_decoding_beside_a_prompt(eqat, D, group, ratio):
+    """Both kernels, the one for few rows in tiles of one token's rows; some sequences have more than a tile."""
+    lengths, news = [3000, 260, 17, 900, 1, 2100, 0, 64], [1, 200, 2, 1, 1, 1, 0, 4]
+    c = Cache(eqat, D, group, 8, 16, lengths, news, seed=D + group, pad_rows=1)
+    held = c.fill()
+    # by the number of sequences and rows an ordinary one has one or two tokens
+    plan = eqat.eqat_cache_attention_plan(c.desc(), eqat.make_attention_desc(8 * ratio, 200, 0.1))
+    assert plan[1] == 33 and plan[0] < 32
+    Q, O, lse = run_attention(eqat, c, 8 * ratio)
+    check_prompt(c, O, lse, Q, held)
