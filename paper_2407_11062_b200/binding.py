@@ -111,7 +111,14 @@ lib = _load()
 LIB_PATH = _LIB_PATH
 
 
+# The cache's calls, made for every block and token, are marshalled by compiled code (csrc/marshal.cpp): nine to eleven
+# tensors a call took the interpreter 6 us.  It is built against the installed torch, so nothing else here needs it: it is
+# loaded by the first of these calls.
+_marshal = None
+
+
 def _load_marshal():
+    global _marshal
     path = os.path.join(os.path.dirname(_LIB_PATH), "_marshal.so")
     if not os.path.exists(path):
         raise ImportError(f"{path} is missing: build it with `python -m paper_2407_11062_b200.build`")
@@ -119,12 +126,8 @@ def _load_marshal():
     module = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(module)
     module.bind(*[ctypes.cast(f, c_void_p).value for f in (lib.eqat_cache_append, lib.eqat_cache_read, lib.eqat_cache_attention)])
+    _marshal = module
     return module
-
-
-# The cache's calls, made for every block and token, are marshalled by compiled code (csrc/marshal.cpp): nine to eleven
-# tensors a call took the interpreter 6 us.
-_marshal = _load_marshal()
 
 
 def status_string(status: int) -> str:
@@ -304,16 +307,16 @@ def eqat_cache_attention_plan(desc, attn, sms=0):
 # `cache`: (k_codes, k_params, v_codes, v_params).  Row tensors are [rows, heads, head_dim] with dense heads, rows of any pitch.
 def eqat_cache_append(desc, K, V, row_offsets, lengths, page_table, cache, K_hat=None, V_hat=None):
     """K_hat, V_hat (or None): what the cache now holds for K and V."""
-    _check(_marshal.cache_append(desc, K, V, row_offsets, lengths, page_table, cache, K_hat, V_hat), "eqat_cache_append")
+    _check((_marshal or _load_marshal()).cache_append(desc, K, V, row_offsets, lengths, page_table, cache, K_hat, V_hat), "eqat_cache_append")
 
 
 def eqat_cache_read(desc, row_offsets, lengths, page_table, cache, K_hat, V_hat):
-    _check(_marshal.cache_read(desc, row_offsets, lengths, page_table, cache, K_hat, V_hat), "eqat_cache_read")
+    _check((_marshal or _load_marshal()).cache_read(desc, row_offsets, lengths, page_table, cache, K_hat, V_hat), "eqat_cache_read")
 
 
 def eqat_cache_attention(desc, attn, Q, row_offsets, lengths, page_table, cache, O, lse=None, workspace=None):
     """lse (or None): [rows, q_heads] fp32."""
-    _check(_marshal.cache_attention(desc, attn, Q, row_offsets, lengths, page_table, cache, O, lse, workspace),
+    _check((_marshal or _load_marshal()).cache_attention(desc, attn, Q, row_offsets, lengths, page_table, cache, O, lse, workspace),
            "eqat_cache_attention")
 
 
