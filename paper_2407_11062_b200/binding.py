@@ -118,10 +118,13 @@ _marshal = None
 
 
 def _load_marshal():
+    from .build import marshal_fits
     global _marshal
     path = os.path.join(os.path.dirname(_LIB_PATH), "_marshal.so")
     if not os.path.exists(path):
         raise ImportError(f"{path} is missing: build it with `python -m paper_2407_11062_b200.build`")
+    if not marshal_fits(path):
+        raise ImportError(f"{path} is for another Python or torch: build it again with `python -m paper_2407_11062_b200.build`")
     spec = importlib.util.spec_from_file_location("paper_2407_11062_b200._marshal", path)
     module = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(module)

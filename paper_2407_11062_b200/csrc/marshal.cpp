@@ -209,7 +209,8 @@ PyMethodDef g_methods[] = {
     {"cache_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_read)), METH_FASTCALL, "eqat_cache_read"},
     {"cache_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_attention)), METH_FASTCALL, "eqat_cache_attention"},
     {nullptr, nullptr, 0, nullptr}};
-PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling of the cache's calls", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
+// (EQAT_BUILT_FOR: Python and torch; the build looks for it)
+PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling of the cache's calls, " EQAT_BUILT_FOR, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
