@@ -40,6 +40,17 @@ void has(const at::Tensor& t, at::ScalarType type, double least) {
   }
 }
 
+// The launch goes to the current device and its current stream: so must every tensor of the call.  (Asked for once a call, and
+// only where there is a CUDA tensor.)
+thread_local int t_device = -1;
+void here(const at::Tensor& t) {
+  if (t_device < 0) t_device = c10::cuda::current_device();
+  if (t.get_device() != t_device) {
+    PyErr_Format(PyExc_ValueError, "a tensor is on cuda:%d, the current device is cuda:%d", (int)t.get_device(), t_device);
+    throw Refused();
+  }
+}
+
 // Address of a contiguous CUDA tensor; None: NULL.
 void* pointer(PyObject* o, at::ScalarType type, double least) {
   if (o == Py_None) return nullptr;
@@ -49,6 +60,7 @@ void* pointer(PyObject* o, at::ScalarType type, double least) {
     PyErr_SetString(PyExc_ValueError, "expected a contiguous CUDA tensor");
     throw Refused();
   }
+  here(t);
   return t.data_ptr();
 }
 
@@ -72,6 +84,7 @@ eqat_bf16* rows_of(PyObject* o, const eqat_cache_desc& d, int64_t heads, int64_t
     PyErr_SetString(PyExc_ValueError, "expected a CUDA tensor [rows, heads, head_dim] with dense heads");
     throw Refused();
   }
+  here(t);
   const int64_t least = t.size(1) * t.size(2);
   *pitch = t.size(0) > 1 || t.stride(0) > least ? t.stride(0) : least;
   return static_cast<eqat_bf16*>(t.data_ptr());
@@ -112,6 +125,7 @@ PyObject* call(Py_ssize_t given, Py_ssize_t wanted, F&& f) {
     PyErr_SetString(PyExc_TypeError, "wrong number of arguments, or called before bind()");
     return nullptr;
   }
+  t_device = -1;
   try {
     return PyLong_FromLong(f());
   } catch (const Refused&) {
