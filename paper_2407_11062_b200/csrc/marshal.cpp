@@ -86,7 +86,7 @@ eqat_bf16* rows_of(PyObject* o, const eqat_cache_desc& d, int64_t heads, int64_t
   }
   here(t);
   const int64_t least = t.size(1) * t.size(2);
-  *pitch = t.size(0) > 1 || t.stride(0) > least ? t.stride(0) : least;
+  *pitch = t.size(0) > 1 ? t.stride(0) : least;      // of a single row a stride says nothing
   return static_cast<eqat_bf16*>(t.data_ptr());
 }
 

@@ -59,3 +59,15 @@ def test_tensors_of_another_device_are_refused(eqat):
         away.append()
         away.attend()
     assert torch.equal(here.O.cpu(), away.O.cpu())
+
+
+@pytest.mark.parametrize("stride", [1, 129, 1003, 4096])
+def test_the_stride_of_a_single_row_does_not_matter(eqat, stride):
+    want, got = Step(eqat), Step(eqat)
+    for name in ("K", "V", "Q", "O"):
+        t = getattr(got, name)
+        setattr(got, name, t.as_strided(t.shape, (stride, *t.stride()[1:])))
+    for step in (want, got):
+        step.append()
+        step.attend()
+    assert all(torch.equal(x, y) for x, y in zip(want.pool, got.pool)) and torch.equal(want.O, got.O) and bool((got.O != 0).any())
