@@ -407,7 +407,8 @@ size_t eqat_cache_workspace_bytes(const eqat_cache_desc* desc, const eqat_attent
  * device: 148, as eqat_cache_workspace_bytes assumes there); h_plan receives two
  * numbers: the query rows (new tokens x query heads of a key/value head) for which
  * the kernel for few rows reads a tile of the cache, and the number of rows from
- * which on a sequence goes to the kernel for prompts (0: none does). */
+ * which on a sequence goes to the kernel for prompts (0: none does; so for heads of
+ * 256 and where the page table has room for more than 2^25 tokens of a sequence). */
 int eqat_cache_attention_plan(const eqat_cache_desc* desc, const eqat_attention_desc* attn, int sms, int* h_plan);
 
 /* Causal attention of the rows' queries over the cache, which already holds the

@@ -34,6 +34,7 @@ constexpr int kThreads = (2 * kHalfWarps + kSpreadWarps + 4) * 32;      // two o
 constexpr int kSoftmaxRegs = 184, kSpreadRegs = 88, kProductRegs = 56;
 constexpr float kLazy = 8.0f;                        // a maximum may be exceeded by 2^8 before the sums are rescaled
 constexpr float kInfiniteValue = 0x1.FFp127f;        // rounds to an infinity of bf16, and all above
+constexpr int64_t kPromptTokens = 1 << 25;           // of the longest sequence
 constexpr int kTile = 128, kStep = 64;               // keys that are expanded, that are multiplied at once
 
 template <int D, int G>
@@ -637,6 +638,9 @@ int launch_shape(const AttentionArgs& a, int sms, cudaStream_t st) {
 bool prompt_attention_applies(const eqat_cache_desc& d, const eqat_attention_desc& a, int sms) {
   const int64_t ratio = a.q_heads / d.kv_heads;
   if (d.head_dim > 128 || a.max_new * ratio < kPromptRows) return false;
+  // A CTA's idle half waits for as long as an item of the other half lasts, about 1.3 us for 64 keys: 0.7 s here, of the 2 s after
+  // which a wait gives up.
+  if ((int64_t)d.max_pages * d.page_size > kPromptTokens) return false;
   // Estimated cycles for 128 keys, if all sequences have the same number of rows or, where that is few, as many as possible have
   // the most and the others one.  Here an SM takes about 4500 for an item, of up to 256 rows, and the items are dealt out whole.  The kernel for few rows takes 3700 for tiles of 32 rows, 2100 for 16 and
   // 1000 + 100 a group for 8, and spreads any number of tiles over all SMs.  (2000 tokens, 64/8 heads, 40 rows, groups of 128:

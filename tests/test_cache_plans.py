@@ -41,3 +41,16 @@ def test_a_plan_without_a_device_is_that_of_148_sms(eqat):
 def test_unequal_batches(eqat, sequences, new, most, length, heads, plan):
     d = eqat.make_cache_desc(128, 128, heads[1], 16, 1 << 18, sequences, length // 16, new)
     assert eqat.eqat_cache_attention_plan(d, eqat.make_attention_desc(heads[0], most, 0.1), 148) == plan
+
+
+@pytest.mark.parametrize("tokens,plan", [(1 << 20, (32, 1)), (1 << 25, (32, 1)), ((1 << 25) + 1024, (32, 0)), (1 << 30, (32, 0))])
+def test_sequences_that_outlast_the_waits_are_not_for_the_kernel_for_prompts(eqat, tokens, plan):
+    """There a wait may last for a whole item: 2^30 tokens would take 20 s, a wait gives up after 2.  In the kernel for few rows every wait
+    is for a tile."""
+    d = eqat.make_cache_desc(128, 128, 8, 1024, 1024, 1, tokens // 1024, 1000)
+    assert eqat.eqat_cache_attention_plan(d, eqat.make_attention_desc(64, 1000, 0.1), 148) == plan
+
+
+def test_heads_of_256_are_not_for_the_kernel_for_prompts(eqat):
+    d = eqat.make_cache_desc(128, 256, 8, 16, 1024, 1, 1024, 1000)
+    assert eqat.eqat_cache_attention_plan(d, eqat.make_attention_desc(64, 1000, 0.1), 148) == (8, 0)
