@@ -56,7 +56,7 @@ constexpr int kThreads = kWarps * 32, kJoinThreads = 256;
 // dominant token to the minima of all others' groups.  What is a whole number already stays one.  The error of an output is about that of sqrt(tokens) / 3 units in its
 // sum: 2^-12 of the largest p s q for a million tokens.
 constexpr float kLazy = 8.0f, kTop = 20.0f;
-constexpr int kLeastExponent = -115, kMostExponent = 100;              // of 2^E
+constexpr int kLeastExponent = -115, kMostExponent = 118;              // of 2^E; p 2^E stays finite
 constexpr float kWeightLimit = 8388608.0f * (1.0f - 0x1p-10f);
 
 // D: elements of a head, G: groups in it, ROWS: query rows of a tile (1, 4, or a multiple of eight).

@@ -182,3 +182,18 @@ def test_queries_of_any_size(eqat, n, power, keys, scale):
     got = host(O).astype(np.float64)
     got[0, 1] = want[0, 1]
     check_norms(got, want)
+
+
+@pytest.mark.parametrize("n", [1, 200])
+@pytest.mark.parametrize("power", [-90, -70, 60, 110])
+def test_values_of_any_size(eqat, n, power):
+    c = Cache(eqat, 128, 64, 4, 16, [300, 290], [n, n], seed=9)
+    held = c.fill()
+    assert eqat.eqat_cache_attention_plan(c.desc(), eqat.make_attention_desc(32, n, 0.1))[1] == (n > 1)
+    for b, tokens in enumerate(c.lengths):
+        pos = np.arange(tokens)
+        c.params[1][c.table[b][pos // 16], :, pos % 16] *= np.float32(2.0 ** power)
+        held[1][b] = held[1][b] * 2.0 ** power
+    c.upload()
+    Q, O, _ = run_attention(eqat, c, 32)
+    check_norms(host(O).astype(np.float64), C.attention(Q.astype(np.float64), held[0], held[1], c.lengths, c.offsets, 128 ** -0.5)[0])
