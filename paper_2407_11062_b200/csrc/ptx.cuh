@@ -338,12 +338,7 @@ __device__ __forceinline__ void ld_global_256(const void* p, uint32_t (&r)[8]) {
                : "l"(p));
 }
 
-// 4-byte and 16-byte loads from a 32-bit shared-memory address.
-__device__ __forceinline__ uint32_t lds_32(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-  return v;
-}
+// 16-byte load from a 32-bit shared-memory address.
 __device__ __forceinline__ uint4 lds_128(uint32_t addr) {
   uint4 v;
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
