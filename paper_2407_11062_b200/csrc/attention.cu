@@ -53,8 +53,8 @@ constexpr int kThreads = kWarps * 32, kJoinThreads = 256;
 // w is rounded down after a number in [0, 1) has been added that depends on the token's position alone (the fractions of
 // multiples of the golden ratio): a long tail of weights below half a unit then counts what it should in the mean.  Rounded to
 // the nearest they would be lost from sum w q and not from sum p and sum p m, which pulled the outputs of rows with one
-// dominant token to the minima of all others' groups.  What is a whole number already stays one.  The error of an output is about that of sqrt(tokens) / 3 units in its
-// sum: 2^-12 of the largest p s q for a million tokens.
+// dominant token to the minima of all others' groups.  What is a whole number already stays one.  The error of an output is
+// about that of sqrt(tokens) / 3 units in its sum: 2^-12 of the largest p s q for a million tokens.
 constexpr float kLazy = 8.0f, kTop = 20.0f;
 constexpr int kLeastExponent = -115, kMostExponent = 118;              // of 2^E; p 2^E stays finite
 constexpr float kWeightLimit = 8388608.0f * (1.0f - 0x1p-10f);
@@ -226,7 +226,7 @@ struct AttentionCtl {
   uint32_t tmem[2];
   int abort;
   // of the query rows
-  alignas(16) float back[ROWS], minus[ROWS], limit[ROWS];          // score in log2 = z * back; minus = -top; arg above limit: raise
+  alignas(16) float back[ROWS], minus[ROWS], limit[ROWS];      // score in log2 = z * back; minus = -top; arg above limit: raise
   alignas(16) float weight[ROWS], grain[ROWS];         // 2^E, 2^-E
   float top[ROWS], peak[ROWS], factor[ROWS], delta[ROWS];      // peak: log2 of the largest 2^z s
   alignas(16) float q_sum[G][ROWS];
@@ -462,7 +462,8 @@ attention_kernel(const AttentionArgs a) {
     float out[S::kBlocks][kRows] = {};                                   // of this thread's element of the head: sums of p s q
     int since = 0;                                                       // tiles in the integer sums
 
-    // Adds the integer sums to the registers, in the rows' present units.  A warp's 32 lanes are the elements 32 warp .. of a block: one group.
+    // Adds the integer sums to the registers, in the rows' present units.  A warp's 32 lanes are the elements 32 warp .. of a
+    // block: one group.
     auto empty_sums = [&] {
 #pragma unroll
       for (int k = 0; k < S::kBlocks; ++k)

@@ -106,18 +106,20 @@ AttentionArgs attention_args(const eqat_cache_desc& d, const eqat_attention_desc
 // that it takes part in; all of them are where that is estimated to be no worse, which saves the launches for few rows.
 constexpr int kPromptRows = 33;
 
-// A call as unequal as its descriptors allow: as many sequences as possible with max_new new tokens, the others with what is
-// left of the rows.
+// A call as unequal as its descriptors allow if every sequence has a row: as many as possible with max_new new tokens, or with
+// all that the others leave, and these with what is left of the rows.
 struct UnequalBatch {
-  int64_t with, rest, each;    // sequences with the most new tokens, others, and the tokens of one of these, rounded up
+  int64_t longest, with;       // the most new tokens, sequences that have them
+  int64_t rest, each;          // other sequences, the tokens of one of these, rounded up
 };
 inline UnequalBatch unequal_batch(const eqat_cache_desc& d, const eqat_attention_desc& a) {
-  const int64_t have = d.sequences < d.rows ? d.sequences : d.rows;      // with any
+  const int64_t have = d.sequences < d.rows ? d.sequences : d.rows;
   const int64_t most = have * a.max_new, rows = d.rows < most ? d.rows : most;
   UnequalBatch u{};
-  u.with = a.max_new > 1 ? (rows - have) / (a.max_new - 1) : have;
+  u.longest = a.max_new < rows - have + 1 ? a.max_new : rows - have + 1;
+  u.with = u.longest > 1 ? (rows - have) / (u.longest - 1) : have;
   u.rest = have - u.with;
-  u.each = u.rest > 0 ? (rows - u.with * a.max_new + u.rest - 1) / u.rest : 0;
+  u.each = u.rest > 0 ? (rows - u.with * u.longest + u.rest - 1) / u.rest : 0;
   return u;
 }
 int prompt_least_rows(const eqat_cache_desc& d, const eqat_attention_desc& a, int sms);

@@ -109,8 +109,8 @@ __device__ __forceinline__ float max_nan(float a, float b, float c) {
   return r;
 }
 
-// 2^x by the multiply-add pipes, for x <= 16 (a NaN becomes some number: the row's sum is made NaN by its maximum): 2^n p(f) with n the nearest integer and f in [-1/2, 1/2], p of degree 3 with the
-// smallest relative error there (7.5e-5, from the exchange algorithm; a weight is rounded to bf16, 2^-8, right after).  Below
+// 2^x by the multiply-add pipes, for x <= 16 (a NaN becomes some number: the row's sum is made NaN by its maximum): 2^n p(f)
+// with n the nearest integer and f in [-1/2, 1/2], p of degree 3 with the smallest relative error there (7.5e-5, from the exchange algorithm; a weight is rounded to bf16, 2^-8, right after).  Below
 // -126 it stays at 2^-126.  The special function unit takes 8 cycles for the 32 exponentials of a warp, 1000 cycles for the two
 // halves' steps; three of eight pairs go this way (1000 new tokens behind 7192, 64/8 heads: none 332 us, two 325, three 323,
 // four 340).
@@ -250,8 +250,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttentionArgs
       if (job.tiles > 0) {
         if (h < job.halves) {
           const uint4* src = reinterpret_cast<const uint4*>(a.Q + out_row * a.q_pitch + (int64_t)q_head * D);
-          // scaled by a power of two, so that the largest element lies in [1, 2), [2, 4) from 2^127 on, to fp16: exact down to 2^-17, off by at
-          // most 2^-25 below; an infinity becomes NaN: no score of the row means anything
+          // scaled by a power of two, so that the largest element lies in [1, 2), [2, 4) from 2^127 on, to fp16: exact down to
+          // 2^-17, off by at most 2^-25 below; an infinity becomes NaN: no score of the row means anything
           uint4 e[D / 8];
           uint32_t most = 0;
 #pragma unroll
@@ -642,8 +642,9 @@ bool prompt_attention_applies(const eqat_cache_desc& d, const eqat_attention_des
   // which a wait gives up.
   if ((int64_t)d.max_pages * d.page_size > kPromptTokens) return false;
   // Estimated cycles for 128 keys, if all sequences have the same number of rows or, where that is few, as many as possible have
-  // the most and the others one.  Here an SM takes about 4500 for an item, of up to 256 rows, and the items are dealt out whole.  The kernel for few rows takes 3700 for tiles of 32 rows, 2100 for 16 and
-  // 1000 + 100 a group for 8, and spreads any number of tiles over all SMs.  (2000 tokens, 64/8 heads, 40 rows, groups of 128:
+  // the most and the others one.  Here an SM takes about 4500 for an item, of up to 256 rows, and the items are dealt out
+  // whole.  The kernel for few rows takes 3700 for tiles of 32 rows, 2100 for 16 and 1000 + 100 a group for 8, and spreads any
+  // number of tiles over all SMs.  (2000 tokens, 64/8 heads, 40 rows, groups of 128:
   // 32 sequences 78 us here, 110 there; 4 sequences of 8000 tokens 123 and 62.)
   const int64_t most = (int64_t)a.max_new * d.sequences, rows = d.rows < most ? d.rows : most;
   int64_t with = d.sequences < rows ? d.sequences : rows, each = (rows * ratio + with - 1) / with;
@@ -667,10 +668,10 @@ int prompt_least_rows(const eqat_cache_desc& d, const eqat_attention_desc& a, in
   // and 31 such tokens 1182 and 408; four prompts of 640 to 1336 178 and 187.)
   const UnequalBatch u = unequal_batch(d, a);
   const double length = (double)d.max_pages * d.page_size, key = 4500.0 / 128;
-  const double prompts = (double)(u.with * d.kv_heads * ((a.max_new * ratio + 255) / 256)) * a.max_new / 2 / sms;
+  const double prompts = (double)(u.with * d.kv_heads * ((u.longest * ratio + 255) / 256)) * u.longest / 2 / sms;
   const double shorts = (double)(u.rest * d.kv_heads) * length / sms;
   const double together = (prompts + shorts > length ? prompts + shorts : length) * key;
-  const double apart = (prompts > a.max_new ? prompts : a.max_new) * key + shorts / 128 * 1000 + 17000;
+  const double apart = (prompts > u.longest ? prompts : u.longest) * key + shorts / 128 * 1000 + 17000;
   return together <= apart ? 1 : kPromptRows;
 }
 

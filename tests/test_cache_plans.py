@@ -35,6 +35,8 @@ def test_a_plan_without_a_device_is_that_of_148_sms(eqat):
     (4, 3952, 1336, 1344, (64, 8), (32, 1)), (4, 3952, 1336, 1344, (32, 32), (32, 1)), (8, 2350, 700, 704, (64, 8), (32, 1)),
     # none can be short, whatever the lengths
     (1, 1000, 1000, 1 << 20, (64, 8), (32, 1)), (2, 1020, 1000, 1 << 20, (64, 8), (32, 1)),
+    # the same with max_new far above what the rows leave for one sequence
+    (32, 2031, 1 << 20, 32768, (64, 8), (8, 33)), (4, 3952, 1 << 20, 1344, (64, 8), (32, 1)),
     # few rows only: tiles for an ordinary sequence
     (100, 103, 4, 4096, (64, 8), (16, 0)), (100, 100, 4, 4096, (64, 8), (8, 0)), (16, 64, 4, 6016, (64, 8), (32, 0)),
     (100, 100, 16, 4096, (8, 8), (1, 0))])
