@@ -21,10 +21,10 @@
 //
 // What bounds it: a tile costs the SM's shared-memory and L1 data path 256 cycles for writing the bytes, 256 for the tensor
 // core's reads of them, about 150 for fetching the codes and some 100 for weights and constants, of 1000 that it takes (HBM
-// would deliver one in 750); 270 instructions of a warp per 16 tokens at 1.9 a cycle.  8 x 65536 tokens, 64/8 heads, groups of
-// 128: 140 us, 4.1 TB/s; with one query head per key/value head 111 us, 5.1 TB/s.  64 x 4096 tokens of uneven lengths, pages of
-// 16: 61 us, 3.0 TB/s; there the ends of segments (queries, first raise, sums over the threads) take a fifth.
-// Measured and not kept:
+// would deliver one in 750); of the issue slots 51 % are taken.  8 x 65536 tokens, 64/8 heads, groups of 128: 142 us, 4.0 TB/s;
+// with one query head per key/value head 122 us, 4.7 TB/s (single calls, nothing in the L2).  64 x 4096 tokens of uneven
+// lengths, pages of 16: 59 us, 3.1 TB/s; there the ends of segments (queries, first raise, sums over the threads) take a fifth.
+// Measured and not kept, beside 61 us for the last of these:
 //   codes as fp16 operands of mma.sync m16n8k16, fed by ldmatrix (the first form)   64 x 4096: 63 us, 8 x 65536 slower by 12 %
 //   four warps that fetch and spread beside four that weigh                         69 us: the same data path
 //   scores of the next tile under this one's weights, one barrier a tile            73 us
@@ -119,6 +119,7 @@ __device__ __forceinline__ WorkPlace find_work(const AttentionArgs& a, int worke
     p.total = __shfl_sync(0xFFFFFFFFu, upto, 31);
     // A tile takes a worker about a microsecond, a piece of a segment the join 0.06: few tiles for a worker where a segment
     // is short, sqrt(tiles / 16) where it is cut into many pieces (one head, 30000 tokens: 27.8 us with one, 17.8 with four).
+    // More than 32 sequences of such lengths have tiles enough for all workers.
     const unsigned longest = __reduce_max_sync(0xFFFFFFFFu, w.tiles > 0 ? (unsigned)w.units : 0u);
     p.per = max(quotient(p.total + workers - 1, workers), (int64_t)max(1, (int)sqrtf((float)longest * 0.0625f)));
     const uint32_t behind = __ballot_sync(0xFFFFFFFFu, upto > f(p.per));     // sequences that end behind unit x

@@ -14,10 +14,11 @@
 //     4 prompts of up to 1500, 32 heads of 64               0.0033, 92 us     0.0023 to 0.0024, 101 us
 //     1000 new behind 7192, 64/8 heads of 128               0.0020, 326 us    0.0018, 339 us
 //     16 x 5 new, window 4000 (one tile of 40 rows)         0.0022, 72 us     0.0019, 76 us
+// A maximum that passes NaN on made that 104, 335 and 77 us.
 //
 // What bounds it: the latency of a step's softmax, about 2500 cycles of which the exponentials and their chain are most (three
 // of eight pairs are polynomials for that reason), and the last wave of CTAs: the second of these has 256 items for 148 SMs.
-// It runs at 740 TFLOP/s there, masked products not counted.  Steps of 128 keys took 396 us for it where steps of 64 took 320.
+// It runs at 755 TFLOP/s there, masked products not counted.  Steps of 128 keys took 396 us for it where steps of 64 took 320.
 #include <type_traits>
 
 #include "attention.cuh"

@@ -123,6 +123,17 @@ def test_decoding_by_norm(eqat, D, group, H, page, ratio):
     check_norms(host(O).astype(np.float64), C.attention(Q.astype(np.float64), held[0], held[1], c.lengths, c.offsets, D ** -0.5)[0])
 
 
+@pytest.mark.parametrize("D,group,H,page", GEOMETRIES)
+@pytest.mark.parametrize("window,scale", [(0, 1.0), (50, 1.0), (0, 6.0), (0, -3.0)])
+def test_drafts_by_norm(eqat, D, group, H, page, window, scale):
+    """Also with sharp softmaxes, whose maxima rise along a sequence."""
+    c = Cache(eqat, D, group, H, page, [9, 40, 300, 3, 129, 75, 0, 1500], [5, 0, 7, 5, 1, 15, 2, 16], seed=D + group, pad_rows=2)
+    held, scale = c.fill(), scale * D ** -0.5
+    Q, O, _ = run_attention(eqat, c, H * 2, window=window, scale=scale)
+    rows = int(c.offsets[-1])
+    check_norms(host(O).astype(np.float64)[:rows], C.attention(Q.astype(np.float64), held[0], held[1], c.lengths, c.offsets, scale, window)[0][:rows])
+
+
 @pytest.mark.parametrize("ratio", [1, 4, 8])
 def test_a_sequence_in_many_pieces_by_norm(eqat, ratio):
     c = Cache(eqat, 128, 128, 1, 64, [20011], [1], seed=3)
