@@ -47,14 +47,14 @@ def repeated(eqat, c, copies, Q):
 
 
 def expected(c, held, Q):
-    """fp64 outputs of `repeated`, the log-sum-exp and the largest weight of each row."""
-    k, v = (np.repeat(h[0], Q.shape[1] // c.H, 1).transpose(1, 0, 2) for h in held)        # [q_heads, tokens, D]
-    z = np.einsum("bhd,htd->bht", Q.astype(np.float64), k, optimize=True) * c.D ** -0.5
-    top = z.max(-1, keepdims=True)
-    p = np.exp(z - top)
-    total = p.sum(-1, keepdims=True)
+    """Outputs of `repeated` in 64 bits, the log-sum-exp and the largest weight of each row."""
+    k, v = (torch.from_numpy(h[0]).cuda().repeat_interleave(Q.shape[1] // c.H, 1).transpose(0, 1) for h in held)      # [q_heads, tokens, D]
+    z = torch.from_numpy(Q).cuda().double().transpose(0, 1) @ k.transpose(1, 2) * c.D ** -0.5                        # [q_heads, copies, tokens]
+    top = z.amax(-1, keepdim=True)
+    p = torch.exp(z - top)
+    total = p.sum(-1, keepdim=True)
     p /= total
-    return np.einsum("bht,htd->bhd", p, v, optimize=True), (top + np.log(total))[..., 0], p.max(-1)
+    return [x.transpose(0, 1).cpu().numpy() for x in (p @ v, (top + torch.log(total))[..., 0], p.amax(-1))]
 
 
 def check_norms(got, want):
