@@ -7,7 +7,7 @@
 
 norm, for a row of n elements, in 32 bits or more between the roundings named:
     h = bf16(x + r),  c = (mean(h^2) + eps)^(-1/2),  y = bf16(h c w)
-or, in 8 bits, for each group with a = max |h w|  (binary32, half to even; 0 where a < 2^-120):
+or, in 8 bits, for each group with a = max |h w|  (binary32, half to even; 0 where a < 2^-110):
     q = rint(h w * (127/a))  or  e4m3(h w * (448/a)),   scale = a c / 127  or  a c / 448,   y = bf16(q scale)
     gradient, v = dy w:  dx = dr + c (v - h c^2 mean(v h)),   dw = sum over rows of dy h c
 
@@ -27,7 +27,7 @@ own = False
 
 DEV = "cuda"
 BF16 = torch.bfloat16
-SMALL = 2.0 ** -120
+SMALL = 2.0 ** -110
 
 
 # ---------------------------------------------------------------------------------------------- cases
