@@ -438,6 +438,201 @@ int eqat_cache_attention(const eqat_cache_desc* desc, const eqat_attention_desc*
                          const int32_t* page_table, const eqat_cache* cache, eqat_bf16* O, int64_t o_pitch,
                          float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------ between the linears of a block */
+
+/* What a decoder block computes between its linears (no counterpart in the paper,
+ * which trains whole blocks of such models): the norm of the residual stream, the
+ * positions of queries and keys, and the gated product of two projections, each
+ * with its backward pass.  Sizes are on the host; nothing is allocated, and calls
+ * can be captured.  Statistics, angles and sums are held in 32 bits or more and
+ * every output is rounded once, where nothing else is said.  In place means the
+ * very same array (and pitch); arrays that overlap in any other way give undefined
+ * values. */
+
+/* ---- root-mean-square norm of the residual stream
+ *
+ * A row of the stream, with what a linear adds to it:
+ *     h = bf16(x + r),   c = (mean(h^2) + eps)^(-1/2),   y = bf16((h * w) * c).
+ * The norm is that of h as it is stored.  Optionally the result is held in 8 bits,
+ * every `group` consecutive elements with a scale of their own: with
+ * t = fl(h * w) and a = max |t| over the group, both binary32,
+ *     EQAT_CODES_INT8:  q = rint(fl(t * fl(127 / a)))    scale = a * c / 127
+ *     EQAT_CODES_E4M3:  q = e4m3(fl(t * fl(448 / a)))    scale = a * c / 448
+ * (half to even; a < 2^-110: q = 0, scale = 0).  c is left out of the decision, so
+ * codes do not depend on the order in which squares are added up.  y is then
+ * bf16(q * scale), what the codes stand for, as K_hat of eqat_cache_append.  A row
+ * with a NaN gives NaN in y and the scales, one with an infinity NaN where it
+ * stands (its group) and zeros elsewhere; codes of such groups may be anything.
+ *
+ * features: a multiple of 8, at most 32768.  group (with codes): 32, 64, 128 or 256
+ * dividing features, or features itself; 0 without codes. */
+enum { EQAT_CODES_NONE = 0, EQAT_CODES_INT8 = 1, EQAT_CODES_E4M3 = 2 };
+
+typedef struct {
+  int64_t rows;
+  int32_t features;
+  int32_t codes;              /* EQAT_CODES_*                                         */
+  int32_t group;              /* elements per scale                                   */
+  float eps;                  /* finite, not negative                                 */
+} eqat_norm_desc;
+
+/*   X [rows, features], W [features] bf16 (in); R [rows, features] bf16 (in) or NULL: h = x
+ *   H [rows, features] bf16 (out), may be NULL; may be X or R
+ *   Y [rows, features] bf16 (out), may be NULL with codes
+ *   codes [rows, features] u8 or s8, scales [rows, features/group] fp32 (out): both, or both NULL
+ *   with EQAT_CODES_NONE */
+int eqat_rms_norm_fwd(const eqat_norm_desc* desc, const eqat_bf16* X, const eqat_bf16* R, const eqat_bf16* W,
+                      eqat_bf16* H, eqat_bf16* Y, void* codes, float* scales, void* stream);
+
+/* Bytes of scratch eqat_rms_norm_bwd needs for dW on the current device, 256-byte
+ * aligned ((size_t)-1 if the descriptor is invalid).  Calls that may overlap need a
+ * workspace each. */
+size_t eqat_rms_norm_workspace_bytes(const eqat_norm_desc* desc);
+
+/* With v = dy * w:
+ *     dx = dr + c * (v - h * c^2 * mean(v * h)),   dw = sum over the rows of dy * h * c.
+ * dx is the gradient of h, so of x and of r; dr what reaches h from the stream behind
+ * it.  (Codes pass it through: the descriptor's are not looked at.)  dw is added up
+ * in an order that depends on the device and the shape alone.
+ *   dY, H [rows, features], W [features] bf16 (in); dR [rows, features] bf16 (in) or NULL
+ *   dX [rows, features] bf16 (out), may be dR or dY
+ *   dW [features] fp32 (out), may be NULL: then no workspace is needed */
+int eqat_rms_norm_bwd(const eqat_norm_desc* desc, const eqat_bf16* dY, const eqat_bf16* H, const eqat_bf16* W,
+                      const eqat_bf16* dR, eqat_bf16* dX, float* dW, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
+/* ---- rotary positions
+ *
+ * The first rotary_dim elements of a head, as pairs (a, b): elements i and
+ * i + rotary_dim/2 (EQAT_ROTARY_HALVES) or 2i and 2i + 1 (EQAT_ROTARY_PAIRS).  At
+ * position p, with the frequency f_i of the pair,
+ *     (a cos pf - b sin pf, b cos pf + a sin pf) * amplitude.
+ * The other elements are handed on.  Frequencies are given as fractions of a turn
+ * per position, in units of 2^-64: turns[i] = round(2^64 f_i / 2 pi) mod 2^64, so
+ * that p * turns[i] mod 2^64 is the angle whatever the position; what remains is
+ * rounded to 2^-32 of a turn. */
+enum { EQAT_ROTARY_HALVES = 0, EQAT_ROTARY_PAIRS = 1 };
+
+typedef struct {
+  int64_t rows;
+  int32_t q_heads;            /* at least 1                                           */
+  int32_t kv_heads;           /* 0: no keys                                           */
+  int32_t head_dim;           /* a multiple of 8, at most 512                         */
+  int32_t rotary_dim;         /* even, 2 .. head_dim                                  */
+  int32_t layout;             /* EQAT_ROTARY_HALVES or _PAIRS                         */
+  int32_t sequences;          /* with row_offsets; 0 with positions                   */
+  float amplitude;            /* finite; 1 without scaling                            */
+} eqat_rotary_desc;
+
+/* Frequencies of a model made for texts of some length, and for longer ones
+ * (`factor` times as long).  With f_i = base^(-2i/rotary_dim):
+ *   EQAT_ROTARY_PLAIN   f_i
+ *   EQAT_ROTARY_LINEAR  f_i / factor: positions interpolated
+ *   EQAT_ROTARY_BASE    f_i of the base * factor^(rotary_dim/(rotary_dim - 2)): the fastest pair
+ *                       as it was, the slowest divided by factor
+ *   EQAT_ROTARY_RAMP    by the turns t_i = length * f_i / 2 pi that a pair makes in the length the
+ *                       model was made for: f_i where t_i >= high, f_i / factor where t_i <= low,
+ *                       in between k f_i + (1 - k) f_i / factor with k = (t_i - low)/(high - low)
+ * (arXiv 2306.15595 and 2309.00071 describe them.) */
+enum { EQAT_ROTARY_PLAIN = 0, EQAT_ROTARY_LINEAR = 1, EQAT_ROTARY_BASE = 2, EQAT_ROTARY_RAMP = 3 };
+
+typedef struct {
+  int32_t kind;               /* EQAT_ROTARY_PLAIN ...                                */
+  int32_t rotary_dim;
+  double base;                /* > 0                                                  */
+  double factor;              /* > 0; not looked at by PLAIN                          */
+  double low, high, length;   /* RAMP: 0 <= low < high, length > 0                    */
+} eqat_rotary_scaling;
+
+/* h_turns receives rotary_dim/2 numbers, on the host; eqat_rotary_turns_of takes
+ * frequencies of the caller's own, radians per position (finite). */
+int eqat_rotary_turns(const eqat_rotary_scaling* scaling, uint64_t* h_turns);
+int eqat_rotary_turns_of(const double* h_frequencies, int count, uint64_t* h_turns);
+
+/* Positions are given either way:
+ *   - positions [rows] int32, of any sign; row_offsets and lengths NULL;
+ *   - positions NULL, row_offsets [sequences+1] and lengths [sequences] int32 as in
+ *     the calls of the cache: the n rows of sequence b stand at lengths[b]-n ..
+ *     lengths[b]-1; rows of no sequence are left as they were.
+ * Q, K, Q_out, K_out [rows, heads, head_dim] bf16, heads and elements dense, the
+ * pitch of a row in elements a multiple of 8; K and K_out are not looked at without
+ * keys.  Q_out may be Q, K_out K, with the same pitch.  The backward pass, gradients
+ * in and out, is the transposed rotation, the same amplitude.
+ *   turns [rotary_dim/2] (in, device) */
+int eqat_rotary_fwd(const eqat_rotary_desc* desc, const eqat_bf16* Q, int64_t q_pitch, const eqat_bf16* K, int64_t k_pitch,
+                    const uint64_t* turns, const int32_t* positions, const int32_t* row_offsets,
+                    const int32_t* lengths, eqat_bf16* Q_out, int64_t q_out_pitch, eqat_bf16* K_out,
+                    int64_t k_out_pitch, void* stream);
+int eqat_rotary_bwd(const eqat_rotary_desc* desc, const eqat_bf16* dQ, int64_t q_pitch, const eqat_bf16* dK, int64_t k_pitch,
+                    const uint64_t* turns, const int32_t* positions, const int32_t* row_offsets,
+                    const int32_t* lengths, eqat_bf16* dQ_out, int64_t q_out_pitch, eqat_bf16* dK_out,
+                    int64_t k_out_pitch, void* stream);
+
+/* ---- gated product
+ *
+ *     H = act(G) * U,   dG = dH * U * act'(G),   dU = dH * act(G),
+ * with act(g) = g / (1 + e^-g) (EQAT_ACT_SILU), g Phi(g) with the normal
+ * distribution's Phi (EQAT_ACT_GELU), or g / (1 + e^(-2z)), z = (2/pi)^(1/2)
+ * (g + 0.044715 g^3) (EQAT_ACT_GELU_TANH).  Values of act below 2^-110 may be 0. */
+enum { EQAT_ACT_SILU = 0, EQAT_ACT_GELU = 1, EQAT_ACT_GELU_TANH = 2 };
+
+typedef struct {
+  int64_t rows;
+  int32_t features;           /* a multiple of 8                                      */
+  int32_t activation;         /* EQAT_ACT_*                                           */
+} eqat_gated_desc;
+
+/* For projections that stand already (qlinear_fakequant_fwd, or one linear for both).
+ * Rows of G, U, dG, dU have a pitch in elements, a multiple of 8 and at least
+ * features (the halves of one tensor can be passed as they are); H and dH are dense.
+ * H may be G or U where those are dense; dG and dU may be G, U (with their pitch) or dH. */
+int eqat_gated_fwd(const eqat_gated_desc* desc, const eqat_bf16* G, int64_t g_pitch, const eqat_bf16* U, int64_t u_pitch,
+                   eqat_bf16* H, void* stream);
+int eqat_gated_bwd(const eqat_gated_desc* desc, const eqat_bf16* dH, const eqat_bf16* G, int64_t g_pitch, const eqat_bf16* U,
+                   int64_t u_pitch, eqat_bf16* dG, int64_t dg_pitch, eqat_bf16* dU, int64_t du_pitch, void* stream);
+
+typedef struct {              /* a weight as qlinear_packed_fwd takes it: device pointers */
+  const uint8_t* Wq_packed;   /* [out, in*N/8]                                        */
+  const eqat_fp16* s16;       /* [out, in/g]                                          */
+  const void* z;              /* [out, in/g] uint8 or fp16 (desc.zero_point_format)   */
+} eqat_packed_weight;
+
+/* Both projections of a feed-forward block and their product, the weights packed:
+ *     G = X * W_gate^T,   U = X * W_up^T,   H = act(G) * U
+ * for two weights of one descriptor (out_features of each).  Large batches: one
+ * kernel in which a tile holds both projections of its features; G and U leave it
+ * only if they are wanted (for the backward pass), and H is that of the sums before
+ * they are rounded.  A few tokens: one pass over both weights, likewise.  Between
+ * them (eqat_packed_gated_route): two calls of qlinear_packed_fwd and one of
+ * eqat_gated_fwd, through G and U or, where these are NULL, the workspace; H is that
+ * of G and U as they are rounded.  Weights enter the products as in
+ * qlinear_packed_fwd.
+ *   X [T,in] bf16, gate, up (in)   H [T,out] bf16 (out)
+ *   G, U [T,out] bf16 (out): both, or both NULL */
+size_t eqat_packed_gated_workspace_bytes(const eqat_desc* desc);
+int qlinear_packed_gated_fwd(const eqat_desc* desc, int activation, const eqat_bf16* X, const eqat_packed_weight* gate,
+                             const eqat_packed_weight* up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* How qlinear_packed_gated_fwd takes a problem, decided on the host from the
+ * descriptor alone (a diagnostic); `sms` as in eqat_packed_fwd_route. */
+enum {
+  EQAT_GATED_COMPOSED = 0,    /* two projections and their product                    */
+  EQAT_GATED_TILED = 1,       /* one kernel, tiles of both projections                */
+  EQAT_GATED_MATRIX_VECTOR = 2
+};
+int eqat_packed_gated_route(const eqat_desc* desc, int sms);
+
+/* dG and dU as in eqat_gated_bwd, and
+ *     dX = dG * W_gate + dU * W_up
+ * of them as they are stored, one contraction over the features of both.  The step
+ * sizes' gradients are qlinear_packed_bwd_ds of X with dG, and with dU.
+ *   dH, G, U [T,out] bf16, gate, up (in)   dX [T,in], dG, dU [T,out] bf16 (out); dG and dU may
+ *   be G, U or dH */
+int qlinear_packed_gated_bwd(const eqat_desc* desc, int activation, const eqat_bf16* dH, const eqat_bf16* G,
+                             const eqat_bf16* U, const eqat_packed_weight* gate, const eqat_packed_weight* up,
+                             eqat_bf16* dX, eqat_bf16* dG, eqat_bf16* dU, void* stream);
+
 /* ------------------------------------------------------------------ whole blocks */
 
 /* Both phases of the paper work on one transformer block at a time (Block-AP,

@@ -11,7 +11,7 @@ from __future__ import annotations
 import ctypes
 import importlib.util
 import os
-from ctypes import POINTER, Structure, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, Structure, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 
 import torch
 
@@ -25,6 +25,11 @@ EQAT_ZP_U8, EQAT_ZP_FP16 = 0, 1
 EQAT_ROUTE_MATRIX_VECTOR, EQAT_ROUTE_WEIGHT_ROWS, EQAT_ROUTE_WEIGHT_ROW_PAIRS, EQAT_ROUTE_TILED = 1, 2, 3, 4
 EQAT_GEMM_Y, EQAT_GEMM_DX, EQAT_GEMM_DW, EQAT_GEMM_LATENT_Y, EQAT_GEMM_LATENT_DX = 0, 1, 2, 3, 4
 EQAT_GEMM_PACKED_Y, EQAT_GEMM_PACKED_DX, EQAT_GEMM_PACKED_DS = 5, 6, 7
+EQAT_CODES_NONE, EQAT_CODES_INT8, EQAT_CODES_E4M3 = 0, 1, 2
+EQAT_ROTARY_HALVES, EQAT_ROTARY_PAIRS = 0, 1
+EQAT_ROTARY_PLAIN, EQAT_ROTARY_LINEAR, EQAT_ROTARY_BASE, EQAT_ROTARY_RAMP = 0, 1, 2, 3
+EQAT_ACT_SILU, EQAT_ACT_GELU, EQAT_ACT_GELU_TANH = 0, 1, 2
+EQAT_GATED_COMPOSED, EQAT_GATED_TILED, EQAT_GATED_MATRIX_VECTOR = 0, 1, 2
 
 
 class EqatError(RuntimeError):
@@ -63,6 +68,28 @@ class eqat_attention_desc(Structure):
     _fields_ = [("q_heads", c_int32), ("max_new", c_int32), ("scale", c_float), ("window", c_int32)]
 
 
+class eqat_norm_desc(Structure):
+    _fields_ = [("rows", c_int64), ("features", c_int32), ("codes", c_int32), ("group", c_int32), ("eps", c_float)]
+
+
+class eqat_rotary_desc(Structure):
+    _fields_ = [("rows", c_int64), ("q_heads", c_int32), ("kv_heads", c_int32), ("head_dim", c_int32), ("rotary_dim", c_int32),
+                ("layout", c_int32), ("sequences", c_int32), ("amplitude", c_float)]
+
+
+class eqat_rotary_scaling(Structure):
+    _fields_ = [("kind", c_int32), ("rotary_dim", c_int32), ("base", c_double), ("factor", c_double), ("low", c_double),
+                ("high", c_double), ("length", c_double)]
+
+
+class eqat_gated_desc(Structure):
+    _fields_ = [("rows", c_int64), ("features", c_int32), ("activation", c_int32)]
+
+
+class eqat_packed_weight(Structure):
+    _fields_ = [("Wq_packed", c_void_p), ("s16", c_void_p), ("z", c_void_p)]
+
+
 def _load():
     if not os.path.exists(_LIB_PATH):
         raise ImportError(f"{_LIB_PATH} is missing: build it with `python -m paper_2407_11062_b200.build` "
@@ -70,6 +97,8 @@ def _load():
     lib = ctypes.CDLL(_LIB_PATH)
     D, P = POINTER(eqat_desc), c_void_p
     C, K, A = POINTER(eqat_cache_desc), POINTER(eqat_cache), POINTER(eqat_attention_desc)
+    N, R, G, W = POINTER(eqat_norm_desc), POINTER(eqat_rotary_desc), POINTER(eqat_gated_desc), POINTER(eqat_packed_weight)
+    rotary = [R, P, c_int64, P, c_int64, P, P, P, P, P, c_int64, P, c_int64, P]
     sigs = {
         "eqat_status_string": (c_char_p, [c_int]),
         "eqat_version": (c_int, []),
@@ -98,6 +127,19 @@ def _load():
         "eqat_cache_workspace_bytes": (c_size_t, [C, A]),
         "eqat_cache_attention_plan": (c_int, [C, A, c_int, POINTER(c_int)]),
         "eqat_cache_attention": (c_int, [C, A, P, c_int64, P, P, P, K, P, c_int64, P, P, c_size_t, P]),
+        "eqat_rms_norm_fwd": (c_int, [N, P, P, P, P, P, P, P, P]),
+        "eqat_rms_norm_workspace_bytes": (c_size_t, [N]),
+        "eqat_rms_norm_bwd": (c_int, [N, P, P, P, P, P, P, P, c_size_t, P]),
+        "eqat_rotary_turns": (c_int, [POINTER(eqat_rotary_scaling), POINTER(c_uint64)]),
+        "eqat_rotary_turns_of": (c_int, [POINTER(c_double), c_int, POINTER(c_uint64)]),
+        "eqat_rotary_fwd": (c_int, rotary),
+        "eqat_rotary_bwd": (c_int, rotary),
+        "eqat_gated_fwd": (c_int, [G, P, c_int64, P, c_int64, P, P]),
+        "eqat_gated_bwd": (c_int, [G, P, P, c_int64, P, c_int64, P, c_int64, P, c_int64, P]),
+        "eqat_packed_gated_workspace_bytes": (c_size_t, [D]),
+        "eqat_packed_gated_route": (c_int, [D, c_int]),
+        "qlinear_packed_gated_fwd": (c_int, [D, c_int, P, W, W, P, P, P, P, c_size_t, P]),
+        "qlinear_packed_gated_bwd": (c_int, [D, c_int, P, P, P, W, W, P, P, P, P]),
         "eqat_block_ap_step": (c_int, [POINTER(eqat_block_ap_linear), c_int, POINTER(c_int), P]),
         "eqat_e2e_qp_step": (c_int, [POINTER(eqat_e2e_qp_linear), c_int, POINTER(c_int), P]),
     }
@@ -111,8 +153,8 @@ lib = _load()
 LIB_PATH = _LIB_PATH
 
 
-# The cache's calls, made for every block and token, are marshalled by compiled code (csrc/marshal.cpp): nine to eleven
-# tensors a call took the interpreter 6 us.  It is built against the installed torch, so nothing else here needs it: it is
+# The calls of the cache and those between a block's linears, made for every block and token, are marshalled by compiled code
+# (csrc/marshal.cpp): nine to eleven tensors a call took the interpreter 6 us.  It is built against the installed torch, so nothing else here needs it: it is
 # loaded by the first of these calls.
 _marshal = None
 
@@ -128,7 +170,10 @@ def _load_marshal():
     spec = importlib.util.spec_from_file_location("paper_2407_11062_b200._marshal", path)
     module = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(module)
-    module.bind(*[ctypes.cast(f, c_void_p).value for f in (lib.eqat_cache_append, lib.eqat_cache_read, lib.eqat_cache_attention)])
+    module.bind(*[ctypes.cast(f, c_void_p).value for f in (
+        lib.eqat_cache_append, lib.eqat_cache_read, lib.eqat_cache_attention, lib.eqat_rms_norm_fwd, lib.eqat_rms_norm_bwd,
+        lib.eqat_rotary_fwd, lib.eqat_rotary_bwd, lib.eqat_gated_fwd, lib.eqat_gated_bwd, lib.qlinear_packed_gated_fwd,
+        lib.qlinear_packed_gated_bwd)])
     _marshal = module
     return module
 
@@ -321,6 +366,102 @@ def eqat_cache_attention(desc, attn, Q, row_offsets, lengths, page_table, cache,
     """lse (or None): [rows, q_heads] fp32."""
     _check((_marshal or _load_marshal()).cache_attention(desc, attn, Q, row_offsets, lengths, page_table, cache, O, lse, workspace),
            "eqat_cache_attention")
+
+
+def make_norm_desc(rows, features, eps, codes=EQAT_CODES_NONE, group=0) -> eqat_norm_desc:
+    return eqat_norm_desc(int(rows), int(features), int(codes), int(group), float(eps))
+
+
+def rms_norm_workspace_bytes(desc) -> int:
+    n = lib.eqat_rms_norm_workspace_bytes(ctypes.byref(desc))
+    if n == ctypes.c_size_t(-1).value:
+        raise EqatError(EQAT_ERR_SHAPE, "eqat_rms_norm_workspace_bytes")
+    return int(n)
+
+
+def eqat_rms_norm_fwd(desc, X, R, W, H, Y, codes=None, scales=None):
+    """R, H: the residual's other half and their sum (or None)."""
+    _check((_marshal or _load_marshal()).rms_norm_fwd(desc, X, R, W, H, Y, codes, scales), "eqat_rms_norm_fwd")
+
+
+def eqat_rms_norm_bwd(desc, dY, H, W, dR, dX, dW=None, workspace=None):
+    """dR: gradient that reaches H otherwise (or None); dW: fp32 (or None, then no workspace)."""
+    _check((_marshal or _load_marshal()).rms_norm_bwd(desc, dY, H, W, dR, dX, dW, workspace), "eqat_rms_norm_bwd")
+
+
+def make_rotary_desc(rows, q_heads, kv_heads, head_dim, rotary_dim=None, layout=EQAT_ROTARY_HALVES, amplitude=1.0,
+                     sequences=0) -> eqat_rotary_desc:
+    return eqat_rotary_desc(int(rows), int(q_heads), int(kv_heads), int(head_dim), int(head_dim if rotary_dim is None else rotary_dim),
+                            int(layout), int(sequences), float(amplitude))
+
+
+def _turns_tensor(buffer):
+    return torch.tensor(list(buffer), dtype=torch.uint64).view(torch.int64)
+
+
+def rotary_turns(rotary_dim, base=10000.0, kind=EQAT_ROTARY_PLAIN, factor=1.0, low=0.0, high=0.0, length=0.0) -> torch.Tensor:
+    """The pairs' turns a position in units of 2^-64, int64 on the host (eqat_rotary_turns): to be moved to the device once."""
+    if not 0 < int(rotary_dim) <= 512:
+        raise EqatError(EQAT_ERR_SHAPE, "eqat_rotary_turns")
+    turns = (c_uint64 * max(1, int(rotary_dim) // 2))()
+    scaling = eqat_rotary_scaling(int(kind), int(rotary_dim), float(base), float(factor), float(low), float(high), float(length))
+    _check(lib.eqat_rotary_turns(ctypes.byref(scaling), turns), "eqat_rotary_turns")
+    return _turns_tensor(turns)
+
+
+def rotary_turns_of(frequencies) -> torch.Tensor:
+    """The same of frequencies of the caller's own, radians a position."""
+    f = [float(x) for x in frequencies]
+    turns = (c_uint64 * max(1, len(f)))()
+    _check(lib.eqat_rotary_turns_of((c_double * max(1, len(f)))(*f), len(f), turns), "eqat_rotary_turns_of")
+    return _turns_tensor(turns)
+
+
+# Q, K: [rows, heads, head_dim] as for the cache; positions [rows] int32, or row_offsets and lengths as in the cache's calls.
+def eqat_rotary_fwd(desc, Q, K, turns, Q_out, K_out, positions=None, row_offsets=None, lengths=None):
+    _check((_marshal or _load_marshal()).rotary_fwd(desc, Q, K, turns, Q_out, K_out, positions, row_offsets, lengths), "eqat_rotary_fwd")
+
+
+def eqat_rotary_bwd(desc, dQ, dK, turns, dQ_out, dK_out, positions=None, row_offsets=None, lengths=None):
+    _check((_marshal or _load_marshal()).rotary_bwd(desc, dQ, dK, turns, dQ_out, dK_out, positions, row_offsets, lengths), "eqat_rotary_bwd")
+
+
+def make_gated_desc(rows, features, activation=EQAT_ACT_SILU) -> eqat_gated_desc:
+    return eqat_gated_desc(int(rows), int(features), int(activation))
+
+
+def eqat_gated_fwd(desc, G, U, H):
+    """G, U: [rows, features], rows of any pitch."""
+    _check((_marshal or _load_marshal()).gated_fwd(desc, G, U, H), "eqat_gated_fwd")
+
+
+def eqat_gated_bwd(desc, dH, G, U, dG, dU):
+    _check((_marshal or _load_marshal()).gated_bwd(desc, dH, G, U, dG, dU), "eqat_gated_bwd")
+
+
+def packed_gated_workspace_bytes(desc) -> int:
+    n = lib.eqat_packed_gated_workspace_bytes(ctypes.byref(desc))
+    if n == ctypes.c_size_t(-1).value:
+        raise EqatError(EQAT_ERR_SHAPE, "eqat_packed_gated_workspace_bytes")
+    return int(n)
+
+
+def eqat_packed_gated_route(desc, sms=0) -> int:
+    """How qlinear_packed_gated_fwd takes a problem (EQAT_GATED_*)."""
+    route = lib.eqat_packed_gated_route(ctypes.byref(desc), int(sms))
+    if route < 0:
+        raise EqatError(route, "eqat_packed_gated_route")
+    return route
+
+
+# A weight: (Wq_packed, s16, z).
+def qlinear_packed_gated_fwd(desc, activation, X, gate, up, H, G=None, U=None, workspace=None):
+    """G, U: the projections, for the backward pass (or None)."""
+    _check((_marshal or _load_marshal()).packed_gated_fwd(desc, activation, X, gate, up, H, G, U, workspace), "qlinear_packed_gated_fwd")
+
+
+def qlinear_packed_gated_bwd(desc, activation, dH, G, U, gate, up, dX, dG, dU):
+    _check((_marshal or _load_marshal()).packed_gated_bwd(desc, activation, dH, G, U, gate, up, dX, dG, dU), "qlinear_packed_gated_bwd")
 
 
 def _nbytes(t):

@@ -16,8 +16,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libeqat_b200.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
-SOURCES = ("api.cu", "attention.cu", "cache.cu", "elementwise.cu", "gemm.cu", "gemv.cu", "noalloc.cu", "prompt.cu", "slim.cu",
-           "stream.cu", "wide.cu")
+SOURCES = ("api.cu", "attention.cu", "cache.cu", "elementwise.cu", "gated.cu", "gemm.cu", "gemv.cu", "noalloc.cu", "norm.cu",
+           "prompt.cu", "rotary.cu", "slim.cu", "stream.cu", "wide.cu")
 
 
 def _nvcc() -> str:

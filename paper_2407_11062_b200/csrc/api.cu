@@ -1,7 +1,10 @@
 // C ABI (include/eqat.h): argument validation on the host, then launches.
 #include <stdint.h>
 
+#include <cmath>
+
 #include "attention.cuh"
+#include "between.cuh"
 #include "cache.cuh"
 #include "common.cuh"
 #include "elementwise.cuh"
@@ -148,6 +151,63 @@ int check_attention_desc(const eqat_cache_desc* d, const eqat_attention_desc* a)
   return EQAT_OK;
 }
 
+int check_norm_desc(const eqat_norm_desc* d) {
+  if (d == nullptr) return EQAT_ERR_NULL;
+  if (d->rows <= 0 || d->rows > (int64_t)1 << 30) return EQAT_ERR_SHAPE;
+  if (d->features <= 0 || d->features % 8 != 0 || d->features > 32768) return EQAT_ERR_SHAPE;
+  if (!(d->eps >= 0.0f && d->eps < 1e30f)) return EQAT_ERR_UNSUPPORTED;
+  if (d->codes != EQAT_CODES_NONE && d->codes != EQAT_CODES_INT8 && d->codes != EQAT_CODES_E4M3) return EQAT_ERR_UNSUPPORTED;
+  if (d->codes == EQAT_CODES_NONE) return d->group == 0 ? EQAT_OK : EQAT_ERR_SHAPE;
+  if (d->group == d->features) return EQAT_OK;
+  if (d->group != 32 && d->group != 64 && d->group != 128 && d->group != 256) return EQAT_ERR_UNSUPPORTED;
+  return d->features % d->group == 0 ? EQAT_OK : EQAT_ERR_SHAPE;
+}
+
+int check_rotary_desc(const eqat_rotary_desc* d) {
+  if (d == nullptr) return EQAT_ERR_NULL;
+  if (d->rows <= 0 || d->rows > (int64_t)1 << 30) return EQAT_ERR_SHAPE;
+  if (d->q_heads <= 0 || d->q_heads > 65536 || d->kv_heads < 0 || d->kv_heads > 65536) return EQAT_ERR_SHAPE;
+  if (d->head_dim <= 0 || d->head_dim % 8 != 0 || d->head_dim > 512) return EQAT_ERR_SHAPE;
+  if (d->rotary_dim <= 0 || d->rotary_dim % 2 != 0 || d->rotary_dim > d->head_dim) return EQAT_ERR_SHAPE;
+  if (d->layout != EQAT_ROTARY_HALVES && d->layout != EQAT_ROTARY_PAIRS) return EQAT_ERR_UNSUPPORTED;
+  if (d->sequences < 0 || d->sequences > 1 << 20) return EQAT_ERR_SHAPE;
+  return std::isfinite(d->amplitude) ? EQAT_OK : EQAT_ERR_UNSUPPORTED;
+}
+
+int check_gated_desc(const eqat_gated_desc* d) {
+  if (d == nullptr) return EQAT_ERR_NULL;
+  if (d->rows <= 0 || d->rows > (int64_t)1 << 30) return EQAT_ERR_SHAPE;
+  if (d->features <= 0 || d->features % 8 != 0) return EQAT_ERR_SHAPE;
+  return d->activation >= EQAT_ACT_SILU && d->activation <= EQAT_ACT_GELU_TANH ? EQAT_OK : EQAT_ERR_UNSUPPORTED;
+}
+
+int rotary(const eqat_rotary_desc* d, const RotaryRows& r, bool backward, void* stream) {
+  int rc = check_rotary_desc(d);
+  if (rc != EQAT_OK) return rc;
+  if (!pitch_ok(r.q_pitch, d->q_heads, d->head_dim) || !pitch_ok(r.q_out_pitch, d->q_heads, d->head_dim)) return EQAT_ERR_SHAPE;
+  if ((rc = check_ptrs(r.q, r.q_out, r.turns)) != EQAT_OK) return rc;
+  if (d->kv_heads > 0) {
+    if (!pitch_ok(r.k_pitch, d->kv_heads, d->head_dim) || !pitch_ok(r.k_out_pitch, d->kv_heads, d->head_dim)) return EQAT_ERR_SHAPE;
+    if ((rc = check_ptrs(r.k, r.k_out)) != EQAT_OK) return rc;
+  }
+  // one of the two ways to give positions
+  if (r.positions != nullptr) {
+    if (r.row_offsets != nullptr || r.lengths != nullptr) return EQAT_ERR_UNSUPPORTED;
+    if (!aligned16(r.positions)) return EQAT_ERR_ALIGN;
+  } else {
+    if (d->sequences <= 0) return EQAT_ERR_SHAPE;
+    if ((rc = check_ptrs(r.row_offsets, r.lengths)) != EQAT_OK) return rc;
+  }
+  return launch_rotary(*d, r, backward, static_cast<cudaStream_t>(stream));
+}
+
+// A fraction of a turn per position, in units of 2^-64 (the extended type has the 64 bits).
+uint64_t turns_of(long double radians) {
+  const long double turn = radians / 6.283185307179586476925286766559005768L;
+  const long double scaled = std::rint((turn - std::floor(turn)) * 18446744073709551616.0L);
+  return scaled >= 18446744073709551616.0L ? 0 : (uint64_t)scaled;
+}
+
 // The kernel that takes a packed forward.
 struct PackedRoute {
   int kernel;                            // EQAT_ROUTE_*
@@ -164,6 +224,23 @@ PackedRoute packed_route(const eqat_desc& d, int sms) {
   else if (wide_fwd_applies(d, sms, r.wide)) r.kernel = EQAT_ROUTE_WEIGHT_ROW_PAIRS;
   else r.kernel = EQAT_ROUTE_TILED;
   return r;
+}
+
+inline size_t up_to_256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// On the current device (sms = 0; without one, as on a device of 148), or as on a device of `sms` SMs.
+int gated_route(const eqat_desc& d, int sms) {
+  if (sms == 0 && sm_count() <= 0) sms = 148;
+  return packed_route(d, sms).kernel == EQAT_ROUTE_TILED ? EQAT_GATED_TILED : EQAT_GATED_COMPOSED;
+}
+
+int check_gated_weights(const eqat_desc* d, int activation, const eqat_packed_weight* gate, const eqat_packed_weight* up) {
+  const int rc = check_gemm_desc(d, true);
+  if (rc != EQAT_OK) return rc;
+  if (d->out_features > 1 << 29) return EQAT_ERR_SHAPE;                  // both are counted in 32 bits
+  if (activation < EQAT_ACT_SILU || activation > EQAT_ACT_GELU_TANH) return EQAT_ERR_UNSUPPORTED;
+  if (gate == nullptr || up == nullptr) return EQAT_ERR_NULL;
+  return check_ptrs(gate->Wq_packed, gate->s16, gate->z, up->Wq_packed, up->s16, up->z);
 }
 
 #define EQAT_TRY(expr)            \
@@ -426,6 +503,150 @@ int eqat_cache_attention(const eqat_cache_desc* d, const eqat_attention_desc* a,
     return EQAT_ERR_WORKSPACE;
   return launch_cache_attention(*d, *a, Q, q_pitch, cache_view(*d, row_offsets, lengths, page_table, *cache), O, o_pitch, lse,
                                 workspace, as_stream(stream));
+}
+
+int eqat_rms_norm_fwd(const eqat_norm_desc* d, const eqat_bf16* X, const eqat_bf16* R, const eqat_bf16* W, eqat_bf16* H,
+                      eqat_bf16* Y, void* codes, float* scales, void* stream) {
+  EQAT_TRY(check_norm_desc(d));
+  EQAT_TRY(check_ptrs(X, W));
+  if (d->codes == EQAT_CODES_NONE) {
+    if (codes != nullptr || scales != nullptr) return EQAT_ERR_UNSUPPORTED;
+    EQAT_TRY(check_ptrs(Y));
+  } else {
+    EQAT_TRY(check_ptrs(codes, scales));
+    if (!aligned16(Y)) return EQAT_ERR_ALIGN;
+  }
+  if (!aligned16(R) || !aligned16(H)) return EQAT_ERR_ALIGN;
+  return launch_norm_fwd(*d, X, R, W, H, Y, codes, scales, as_stream(stream));
+}
+
+size_t eqat_rms_norm_workspace_bytes(const eqat_norm_desc* d) {
+  if (check_norm_desc(d) != EQAT_OK) return (size_t)-1;
+  const int sms = sm_count();
+  return norm_workspace(*d, sms > 0 ? sms : 148);                        // no device: as for the cache
+}
+
+int eqat_rms_norm_bwd(const eqat_norm_desc* d, const eqat_bf16* dY, const eqat_bf16* H, const eqat_bf16* W, const eqat_bf16* dR,
+                      eqat_bf16* dX, float* dW, void* workspace, size_t workspace_bytes, void* stream) {
+  EQAT_TRY(check_norm_desc(d));
+  EQAT_TRY(check_ptrs(dY, H, W, dX));
+  if (!aligned16(dR) || !aligned16(dW)) return EQAT_ERR_ALIGN;
+  if (dW != nullptr && (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 ||
+                        workspace_bytes < eqat_rms_norm_workspace_bytes(d)))
+    return EQAT_ERR_WORKSPACE;
+  return launch_norm_bwd(*d, dY, H, W, dR, dX, dW, workspace, as_stream(stream));
+}
+
+int eqat_rotary_turns(const eqat_rotary_scaling* s, uint64_t* h_turns) {
+  if (s == nullptr || h_turns == nullptr) return EQAT_ERR_NULL;
+  if (s->rotary_dim <= 0 || s->rotary_dim % 2 != 0 || s->rotary_dim > 512) return EQAT_ERR_SHAPE;
+  if (s->kind < EQAT_ROTARY_PLAIN || s->kind > EQAT_ROTARY_RAMP) return EQAT_ERR_UNSUPPORTED;
+  if (!(std::isfinite(s->base) && s->base > 0.0)) return EQAT_ERR_UNSUPPORTED;
+  if (s->kind != EQAT_ROTARY_PLAIN && !(std::isfinite(s->factor) && s->factor > 0.0)) return EQAT_ERR_UNSUPPORTED;
+  if (s->kind == EQAT_ROTARY_RAMP &&
+      !(std::isfinite(s->high) && s->low >= 0.0 && s->low < s->high && std::isfinite(s->length) && s->length > 0.0))
+    return EQAT_ERR_UNSUPPORTED;
+  const int n = s->rotary_dim / 2;
+  long double base = s->base;
+  if (s->kind == EQAT_ROTARY_BASE && n > 1) base *= std::pow((long double)s->factor, (long double)n / (n - 1));
+  for (int i = 0; i < n; ++i) {
+    long double f = std::pow(base, -(long double)i / n);
+    if (!std::isfinite(f)) return EQAT_ERR_UNSUPPORTED;
+    if (s->kind == EQAT_ROTARY_LINEAR) f /= s->factor;
+    if (s->kind == EQAT_ROTARY_RAMP) {
+      const long double t = s->length * f / 6.283185307179586476925286766559005768L;
+      long double k = (t - s->low) / ((long double)s->high - s->low);
+      k = k < 0.0L ? 0.0L : k > 1.0L ? 1.0L : k;
+      f = k * f + (1.0L - k) * f / s->factor;
+    }
+    h_turns[i] = turns_of(f);
+  }
+  return EQAT_OK;
+}
+
+int eqat_rotary_turns_of(const double* h_frequencies, int count, uint64_t* h_turns) {
+  if (h_frequencies == nullptr || h_turns == nullptr) return EQAT_ERR_NULL;
+  if (count <= 0) return EQAT_ERR_SHAPE;
+  for (int i = 0; i < count; ++i)
+    if (!std::isfinite(h_frequencies[i])) return EQAT_ERR_UNSUPPORTED;
+  for (int i = 0; i < count; ++i) h_turns[i] = turns_of(h_frequencies[i]);
+  return EQAT_OK;
+}
+
+int eqat_rotary_fwd(const eqat_rotary_desc* d, const eqat_bf16* Q, int64_t q_pitch, const eqat_bf16* K, int64_t k_pitch,
+                    const uint64_t* turns, const int32_t* positions, const int32_t* row_offsets, const int32_t* lengths,
+                    eqat_bf16* Q_out, int64_t q_out_pitch, eqat_bf16* K_out, int64_t k_out_pitch, void* stream) {
+  return rotary(d, RotaryRows{Q, K, q_pitch, k_pitch, Q_out, K_out, q_out_pitch, k_out_pitch, turns, positions, row_offsets, lengths},
+                false, stream);
+}
+
+int eqat_rotary_bwd(const eqat_rotary_desc* d, const eqat_bf16* dQ, int64_t q_pitch, const eqat_bf16* dK, int64_t k_pitch,
+                    const uint64_t* turns, const int32_t* positions, const int32_t* row_offsets, const int32_t* lengths,
+                    eqat_bf16* dQ_out, int64_t q_out_pitch, eqat_bf16* dK_out, int64_t k_out_pitch, void* stream) {
+  return rotary(d, RotaryRows{dQ, dK, q_pitch, k_pitch, dQ_out, dK_out, q_out_pitch, k_out_pitch, turns, positions, row_offsets, lengths},
+                true, stream);
+}
+
+int eqat_gated_fwd(const eqat_gated_desc* d, const eqat_bf16* G, int64_t g_pitch, const eqat_bf16* U, int64_t u_pitch,
+                   eqat_bf16* H, void* stream) {
+  EQAT_TRY(check_gated_desc(d));
+  if (!pitch_ok(g_pitch, 1, d->features) || !pitch_ok(u_pitch, 1, d->features)) return EQAT_ERR_SHAPE;
+  EQAT_TRY(check_ptrs(G, U, H));
+  return launch_gated_fwd(*d, G, g_pitch, U, u_pitch, H, as_stream(stream));
+}
+
+int eqat_gated_bwd(const eqat_gated_desc* d, const eqat_bf16* dH, const eqat_bf16* G, int64_t g_pitch, const eqat_bf16* U,
+                   int64_t u_pitch, eqat_bf16* dG, int64_t dg_pitch, eqat_bf16* dU, int64_t du_pitch, void* stream) {
+  EQAT_TRY(check_gated_desc(d));
+  if (!pitch_ok(g_pitch, 1, d->features) || !pitch_ok(u_pitch, 1, d->features)) return EQAT_ERR_SHAPE;
+  if (!pitch_ok(dg_pitch, 1, d->features) || !pitch_ok(du_pitch, 1, d->features)) return EQAT_ERR_SHAPE;
+  EQAT_TRY(check_ptrs(dH, G, U, dG, dU));
+  return launch_gated_bwd(*d, dH, G, g_pitch, U, u_pitch, dG, dg_pitch, dU, du_pitch, as_stream(stream));
+}
+
+size_t eqat_packed_gated_workspace_bytes(const eqat_desc* d) {
+  if (check_gemm_desc(d, true) != EQAT_OK) return (size_t)-1;
+  if (gated_route(*d, 0) != EQAT_GATED_COMPOSED) return 0;
+  return 2 * up_to_256((size_t)d->tokens * d->out_features * sizeof(eqat_bf16));
+}
+
+int eqat_packed_gated_route(const eqat_desc* d, int sms) {
+  EQAT_TRY(check_gemm_desc(d, true));
+  if (sms < 0) return EQAT_ERR_SHAPE;
+  return gated_route(*d, sms);
+}
+
+int qlinear_packed_gated_fwd(const eqat_desc* d, int activation, const eqat_bf16* X, const eqat_packed_weight* gate,
+                             const eqat_packed_weight* up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  EQAT_TRY(check_gated_weights(d, activation, gate, up));
+  EQAT_TRY(check_ptrs(X, H));
+  if ((G == nullptr) != (U == nullptr)) return EQAT_ERR_NULL;
+  if (!aligned16(G) || !aligned16(U)) return EQAT_ERR_ALIGN;
+  const int route = gated_route(*d, 0);
+  if (route == EQAT_GATED_TILED) return launch_packed_gated(*d, activation, X, *gate, *up, H, G, U, as_stream(stream));
+  if (G == nullptr) {
+    const size_t one = up_to_256((size_t)d->tokens * d->out_features * sizeof(eqat_bf16));
+    if (workspace == nullptr || workspace_bytes < 2 * one || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+      return EQAT_ERR_WORKSPACE;
+    G = static_cast<eqat_bf16*>(workspace);
+    U = reinterpret_cast<eqat_bf16*>(static_cast<uint8_t*>(workspace) + one);
+  }
+  EQAT_TRY(qlinear_packed_fwd(d, X, gate->Wq_packed, gate->s16, gate->z, G, stream));
+  EQAT_TRY(qlinear_packed_fwd(d, X, up->Wq_packed, up->s16, up->z, U, stream));
+  const eqat_gated_desc g{d->tokens, d->out_features, activation};
+  return launch_gated_fwd(g, G, d->out_features, U, d->out_features, H, as_stream(stream));
+}
+
+int qlinear_packed_gated_bwd(const eqat_desc* d, int activation, const eqat_bf16* dH, const eqat_bf16* G, const eqat_bf16* U,
+                             const eqat_packed_weight* gate, const eqat_packed_weight* up, eqat_bf16* dX, eqat_bf16* dG,
+                             eqat_bf16* dU, void* stream) {
+  EQAT_TRY(check_gated_weights(d, activation, gate, up));
+  EQAT_TRY(check_ptrs(dH, G, U, dX, dG, dU));
+  const eqat_gated_desc g{d->tokens, d->out_features, activation};
+  const int64_t pitch = d->out_features;
+  EQAT_TRY(launch_gated_bwd(g, dH, G, pitch, U, pitch, dG, pitch, dU, pitch, as_stream(stream)));
+  return launch_packed_gated_dx(*d, dG, dU, *gate, *up, dX, as_stream(stream));
 }
 
 int eqat_block_ap_step(const eqat_block_ap_linear* L, int count, int* h_failed, void* stream) {

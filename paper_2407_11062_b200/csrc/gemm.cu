@@ -38,6 +38,13 @@
 // codes and reduces runs of `group` columns, so the [out,in] weight gradient
 // never leaves the chip; or, for the Block-AP weight gradient, applies Eqs. 3-5
 // to the accumulators next to the latent weights and writes dW, ds and dz.
+// Two packed weights of one shape, the projections of a gated feed-forward block:
+//   EPI_GATED  half of a tile's columns are rows of the gate's weight and half the
+//              same rows of the other's (in a pair, each CTA expands one of the two),
+//              so that a row's thread finds both projections of its features in
+//              tensor memory and stores their product;
+//   EPI_JOINT  dX of both in one contraction: the first half of K is dG and the
+//              gate's weight, the second half dU and the other's.
 // Packed kernels walk their tiles row by row (the few MB of codes stay in L2,
 // each activation panel is fetched once); dense kernels in bands of row-tiles.
 //
@@ -48,6 +55,7 @@
 // of a CTA that is gone.
 #include <cuda.h>
 
+#include "activation.cuh"
 #include "common.cuh"
 #include "codec.cuh"
 #include "expand.cuh"
@@ -67,7 +75,7 @@ constexpr int UMMA_K = 16;       // K per tcgen05.mma for 16-bit inputs
 constexpr int kDeqWarps = 16;      // packed kernels: warps 2-17 expand codes; the first of them also run the epilogue
 constexpr uint64_t kDrainLimitNs = 50000000ull;    // 50 ms per stage at teardown
 
-enum Epilogue : int { EPI_STORE = 0, EPI_DS = 1, EPI_STE = 2 };
+enum Epilogue : int { EPI_STORE = 0, EPI_DS = 1, EPI_STE = 2, EPI_GATED = 3, EPI_JOINT = 4 };
 
 // The packed weight is the B operand of the packed kernels and an epilogue operand of EPI_DS.
 struct GemmParams : PackedWeight {
@@ -82,6 +90,13 @@ struct GemmParams : PackedWeight {
   const float* z32;          // [out, in/group]
   float Q;                   // 2^N - 1
   int dz_literal;            // Eq. 4 clamped branch: -1 instead of -s
+  // EPI_GATED / EPI_JOINT: the other weight, of the same shape
+  const uint8_t* other_Wq;
+  const eqat_fp16* other_s16;
+  const void* other_zq;
+  int other_sectors;         // as wq_sectors
+  int activation;            // EPI_GATED: D = act(gate) * other
+  eqat_bf16 *gate_out, *other_out;   // EPI_GATED: the projections themselves, or null
 };
 
 template <int MT, bool PACKED, bool PAIR, int BN>
@@ -181,6 +196,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
             const GemmParams p) {
   using C = Cfg<MT, PACKED, PAIR, BN>;
   constexpr bool LATENT = PACKED && BITS == 16;
+  constexpr bool GATED = EPI == EPI_GATED, JOINT = EPI == EPI_JOINT;
+  constexpr int kColumns = GATED ? BN / 2 : BN;                    // of D in a tile
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = ptx::smem_addr(smem_raw);
   const uint32_t pad = (1024u - (raw_addr & 1023u)) & 1023u;
@@ -195,7 +212,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
   const int cluster_id = (int)blockIdx.x / C::kCtas;
   const int num_clusters = (int)gridDim.x / C::kCtas;
   const int num_m = (p.M + C::kClusterM - 1) / C::kClusterM;
-  const int num_n = (p.N + BN - 1) / BN;
+  const int num_n = (p.N + kColumns - 1) / kColumns;
   const int num_tiles = num_m * num_n;
   const int num_kb = (p.K + BK - 1) / BK;
   constexpr int kBand = 4096 / C::kClusterM;
@@ -223,7 +240,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
     ctl->abort = 0;
     ptx::fence_mbar_init();
     ptx::tma_prefetch_desc(&tmap_a);
-    if (!PACKED || LATENT) ptx::tma_prefetch_desc(&tmap_b);
+    if (!PACKED || LATENT || JOINT) ptx::tma_prefetch_desc(&tmap_b);
   }
   if (PAIR) {                                                      // the other CTA runs, and its barriers exist, from here on
     __syncthreads();
@@ -267,7 +284,24 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       ptx::tc_fence_after();
       return ok;
     };
-    if constexpr (EPI == EPI_STORE) {
+    // A lane owns a row, so a plain store instruction would hit 32 different lines, and it is the stores, not
+    // the TMEM loads, that set the pace of this epilogue.  The four lanes of a quad therefore trade 16-byte
+    // pieces so that each store instruction writes 64 contiguous bytes of one row per quad: 8 lines instead
+    // of 32.  (N is a multiple of 16 for every shape the library accepts, so a piece is never ragged.)
+    auto store32 = [&](eqat_bf16* D, int col0, uint32_t (&o)[16]) {  // 32 columns of this lane's row as bf16 pairs
+      quad_transpose(o, lane);
+      const int q = lane & 3;
+      if (col0 + q * 8 < p.N) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int mk = m - q + k;
+          if (mk < p.M)
+            *reinterpret_cast<uint4*>(D + (size_t)mk * p.N + col0 + q * 8) =
+                make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+        }
+      }
+    };
+    if constexpr (EPI == EPI_STORE || JOINT) {
       if (!accumulators()) return false;
 #pragma unroll 1
       for (int c = 0; c < BN / 32; ++c) {
@@ -275,24 +309,41 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
         ptx::tmem_ld_32x32(t_row + c * 32, r);
         ptx::tmem_ld_wait();
         const int col0 = n_blk * BN + c * 32;
-        // A lane owns a row, so a plain store instruction would hit 32 different lines, and it is the stores, not
-        // the TMEM loads, that set the pace of this epilogue.  The four lanes of a quad therefore trade 16-byte
-        // pieces so that each store instruction writes 64 contiguous bytes of one row per quad: 8 lines instead
-        // of 32.  (N is a multiple of 16 for every shape the library accepts, so a piece is never ragged.)
         uint32_t o[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[i] = pack_bf16x2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
-        quad_transpose(o, lane);
-        const int q = lane & 3;
-        if (col0 + q * 8 < p.N) {
+        store32(p.D, col0, o);
+      }
+    } else if constexpr (GATED) {
+      // Columns c and BN/2 + c of the accumulator are the two projections of one feature.  The projections go out first, where
+      // they are wanted: read from tensor memory once more, they need not be held beside the product.
+      if (!accumulators()) return false;
+#pragma unroll 1
+      for (int c = 0; c < kColumns / 32; ++c) {
+        const int col0 = n_blk * kColumns + c * 32;
+        uint32_t o[16];
+        if (p.gate_out != nullptr) {
+#pragma unroll 1
+          for (int s = 0; s < 2; ++s) {
+            uint32_t r[32];
+            ptx::tmem_ld_32x32(t_row + s * kColumns + c * 32, r);
+            ptx::tmem_ld_wait();
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int mk = m - q + k;
-            if (mk < p.M)
-              *reinterpret_cast<uint4*>(p.D + (size_t)mk * p.N + col0 + q * 8) =
-                  make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+            for (int i = 0; i < 16; ++i) o[i] = pack_bf16x2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
+            store32(s == 0 ? p.gate_out : p.other_out, col0, o);
           }
         }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          uint32_t g[16], u[16];
+          ptx::tmem_ld_32x16(t_row + c * 32 + s * 16, g);
+          ptx::tmem_ld_32x16(t_row + kColumns + c * 32 + s * 16, u);
+          ptx::tmem_ld_wait();
+          EQAT_WITH_ACTIVATION(p.activation, _Pragma("unroll") for (int i = 0; i < 8; ++i)
+                                                 o[8 * s + i] = pack_bf16x2(activate<kAct>(__uint_as_float(g[2 * i])) * __uint_as_float(u[2 * i]),
+                                                                            activate<kAct>(__uint_as_float(g[2 * i + 1])) * __uint_as_float(u[2 * i + 1])));
+        }
+        store32(p.D, col0, o);
       }
     } else if constexpr (EPI == EPI_STE) {
       // Block-AP: the accumulator row is the gradient of row m of W_hat.  Eqs. 3-5 are applied to it here,
@@ -544,7 +595,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
 #pragma unroll
             for (int b = 0; b < C::kTileM / 64; ++b) load(a_dst + b * (BK * 128), &tmap_a, m0 + b * 64, kb * BK);
           } else {
-            load(a_dst, &tmap_a, kb * BK, m0);
+            const bool second = JOINT && 2 * kb >= num_kb;
+            load(a_dst, second ? &tmap_b : &tmap_a, (second ? kb - num_kb / 2 : kb) * BK, m0);
           }
           if (!PACKED) {
             if (B_MN) {
@@ -700,6 +752,11 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       const bool split_units = p.group_shift == 5;                // groups of 32: the halves of a unit differ
       const size_t code_step = (size_t)kStep * (B_MN ? (size_t)BK * pitch : (size_t)(8 * BITS));   // bytes between runs
       const uint32_t full_b_lead = lead(ptx::smem_addr(&ctl->full_b[0]));
+      // EPI_GATED: this thread's rows are of one weight; EPI_JOINT: `w` has the weight that the last fetch took
+      PackedWeight w = p;
+      constexpr int kWeightRows = GATED ? BN / 2 : BN;             // rows of a weight in a tile's B operand
+      const int brow = (rank * U + t) & (kWeightRows - 1);         // K-major: this thread's among them
+      if (GATED && rank * U + t >= kWeightRows) { w.Wq = p.other_Wq; w.s16 = p.other_s16; w.zq = p.other_zq; w.wq_sectors = p.other_sectors; }
       long gk = 0;                                                // global index of the tile's K block 0
       int acc = 0;
       uint32_t acc_phase = 0;
@@ -708,10 +765,10 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
         tile_coords<PACKED, kBand>(tile, num_m, num_n, m_blk, n_blk);
         // this group's first K block of the tile (R = 2: K is a multiple of 128, so gk is even)
         const int kb_first = R * (int)(((long)grp - gk / R) & (NG - 1));
-        const int wrow0 = B_MN ? kb_first * BK + kr : n_blk * BN + rank * U + t;
+        const int wrow0 = B_MN ? (JOINT ? 0 : kb_first * BK) + kr : n_blk * kWeightRows + brow;
         const int unit0 = B_MN ? n_blk * (BN / 64) + rank * kBoxes + box : kb_first;
         const bool valid = B_MN ? (unit0 < chunks_in) : (wrow0 < p.out_features);
-        const uint8_t* code_ptr = LATENT ? nullptr : p.Wq + (valid ? (size_t)wrow0 * pitch + (size_t)unit0 * (8 * BITS) : 0);
+        const uint8_t* code_ptr = LATENT ? nullptr : w.Wq + (valid ? (size_t)wrow0 * pitch + (size_t)unit0 * (8 * BITS) : 0);
         // first group of the row that a run starting at K block kb needs
         const size_t g_row0 = B_MN ? (size_t)kr * p.groups_per_row + (size_t)((unit0 << 6) >> p.group_shift)
                                    : (size_t)(valid ? wrow0 : 0) * p.groups_per_row;
@@ -726,11 +783,21 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
                 ring_lz[j][1] = ptx::ld_global(p.z32 + gi + 1);
               }
             }
+          } else if (JOINT) {
+            if (valid) {
+              const bool second = 2 * kb >= num_kb;
+              const int k = second ? kb - num_kb / 2 : kb;
+              w.Wq = second ? p.other_Wq : p.Wq;
+              w.s16 = second ? p.other_s16 : p.s16;
+              w.zq = second ? p.other_zq : p.zq;
+              load_codes64<BITS>(w.Wq + (size_t)(k * BK + kr) * pitch + (size_t)unit0 * (8 * BITS), ring_w[j][0]);
+              load_group_params(w, g_row0 + (size_t)k * BK * p.groups_per_row, g_count, ring_g[j]);
+            }
           } else if (valid) {
             if constexpr (R == 2) {
               // the run's 32 bytes are one sector of the packed row when the matrix itself starts on a 32-byte
               // boundary (row pitch and unit offsets are multiples of 32); otherwise two 16-byte loads
-              if (p.wq_sectors) {
+              if (w.wq_sectors) {
                 ptx::ld_global_256(code_ptr, reinterpret_cast<uint32_t(&)[8]>(ring_w[j][0][0]));
               } else {
                 load_codes64<BITS>(code_ptr, ring_w[j][0]);
@@ -741,7 +808,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
             }
             code_ptr += code_step;
             const size_t gi = B_MN ? g_row0 + (size_t)kb * BK * p.groups_per_row : g_row0 + (size_t)((kb << 6) >> p.group_shift);
-            load_group_params(p, gi, g_count, ring_g[j]);
+            load_group_params(w, gi, g_count, ring_g[j]);
           }
         };
 #pragma unroll
@@ -969,11 +1036,14 @@ int launch(const Operand& a, const Operand& b, const GemmParams& p, cudaStream_t
   if (!opt_in.ensure(kern, C::kSmemBytes)) return EQAT_ERR_CUDA;
   CUtensorMap ta, tb;
   if (!operand_tmap(&ta, a, C::kTileM)) return EQAT_ERR_CUDA;
-  if (PACKED && BITS != 16) tb = ta;                            // packed codes are fetched with ordinary loads
+  if (EPI == EPI_JOINT) {                                       // the second half of K has an A of its own
+    if (!operand_tmap(&tb, b, C::kTileM)) return EQAT_ERR_CUDA;
+  } else if (PACKED && BITS != 16) tb = ta;                     // packed codes are fetched with ordinary loads
   else if (!operand_tmap(&tb, b, C::kBRows)) return EQAT_ERR_CUDA;
   const int sms = sm_count();
   if (sms < C::kCtas) return EQAT_ERR_CUDA;
-  const int tiles = ((p.M + C::kClusterM - 1) / C::kClusterM) * ((p.N + BN - 1) / BN);
+  constexpr int kColumns = EPI == EPI_GATED ? BN / 2 : BN;
+  const int tiles = ((p.M + C::kClusterM - 1) / C::kClusterM) * ((p.N + kColumns - 1) / kColumns);
   const int clusters = tiles < sms / C::kCtas ? tiles : sms / C::kCtas;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(clusters * C::kCtas), 1, 1);
@@ -1104,6 +1174,22 @@ int launch_packed(const Operand& a, GemmParams& p, cudaStream_t st) {
                 : launch<2, false, B_MN, true, EPI_STORE, BITS, false>(a, a, p, st);
 }
 
+// Two packed weights (EPI_GATED: side by side in a tile, EPI_JOINT: one after the other along K).
+template <int EPI, bool B_MN, int BITS>
+int launch_two(const Operand& a, const Operand& b, GemmParams& p, cudaStream_t st) {
+  const TileShape s = packed_shape(p.M, EPI == EPI_GATED ? 2 * p.N : p.N, sm_count());
+  if (s.bn == 128) return launch<1, false, B_MN, true, EPI, BITS, false, 128>(a, b, p, st);
+  return s.pair ? launch<2, false, B_MN, true, EPI, BITS, true>(a, b, p, st)
+                : launch<2, false, B_MN, true, EPI, BITS, false>(a, b, p, st);
+}
+
+void set_other(GemmParams& p, const eqat_packed_weight& w) {
+  p.other_Wq = w.Wq_packed;
+  p.other_s16 = w.s16;
+  p.other_zq = w.z;
+  p.other_sectors = (reinterpret_cast<uintptr_t>(w.Wq_packed) & 31u) == 0 ? 1 : 0;
+}
+
 template <int BITS>
 int launch_ds(const Operand& a, const Operand& b, GemmParams& p, cudaStream_t st) {
   const TileShape s = ds_shape(p.M, p.N, p.partial != nullptr ? kBN : 1 << p.group_shift, sm_count());
@@ -1197,6 +1283,37 @@ int launch_packed_dx(const eqat_desc& d, const eqat_bf16* dY, const uint8_t* Wq,
     case 2: return launch_packed<true, 2>(a, p, st);
     case 3: return launch_packed<true, 3>(a, p, st);
     default: return launch_packed<true, 4>(a, p, st);
+  }
+}
+
+int launch_packed_gated(const eqat_desc& d, int activation, const eqat_bf16* X, const eqat_packed_weight& gate,
+                        const eqat_packed_weight& up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, cudaStream_t st) {
+  GemmParams p = base_params((int)d.tokens, d.out_features, d.in_features);
+  p.D = H;
+  p.gate_out = G;
+  p.other_out = U;
+  p.activation = activation;
+  set_weight(p, d, gate.Wq_packed, gate.s16, gate.z);
+  set_other(p, up);
+  const Operand a{X, (uint64_t)d.tokens, (uint64_t)d.in_features, false};
+  switch (d.bits) {
+    case 2: return launch_two<EPI_GATED, false, 2>(a, a, p, st);
+    case 3: return launch_two<EPI_GATED, false, 3>(a, a, p, st);
+    default: return launch_two<EPI_GATED, false, 4>(a, a, p, st);
+  }
+}
+
+int launch_packed_gated_dx(const eqat_desc& d, const eqat_bf16* dG, const eqat_bf16* dU, const eqat_packed_weight& gate,
+                           const eqat_packed_weight& up, eqat_bf16* dX, cudaStream_t st) {
+  GemmParams p = base_params((int)d.tokens, d.in_features, 2 * d.out_features);
+  p.D = dX;
+  set_weight(p, d, gate.Wq_packed, gate.s16, gate.z);
+  set_other(p, up);
+  const Operand a{dG, (uint64_t)d.tokens, (uint64_t)d.out_features, false}, b{dU, (uint64_t)d.tokens, (uint64_t)d.out_features, false};
+  switch (d.bits) {
+    case 2: return launch_two<EPI_JOINT, true, 2>(a, b, p, st);
+    case 3: return launch_two<EPI_JOINT, true, 3>(a, b, p, st);
+    default: return launch_two<EPI_JOINT, true, 4>(a, b, p, st);
   }
 }
 

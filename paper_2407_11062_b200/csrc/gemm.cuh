@@ -54,6 +54,12 @@ int launch_packed_fwd(const eqat_desc& d, const eqat_bf16* X, const uint8_t* Wq,
                       const void* zq, eqat_bf16* Y, cudaStream_t st);
 int launch_packed_dx(const eqat_desc& d, const eqat_bf16* dY, const uint8_t* Wq, const eqat_fp16* s16,
                      const void* zq, eqat_bf16* dX, cudaStream_t st);
+// H = act(X * dequant(gate)^T) * (X * dequant(up)^T) in one kernel; G and U, the projections, or null.
+int launch_packed_gated(const eqat_desc& d, int activation, const eqat_bf16* X, const eqat_packed_weight& gate,
+                        const eqat_packed_weight& up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, cudaStream_t st);
+// dX = dG * dequant(gate) + dU * dequant(up) in one contraction.
+int launch_packed_gated_dx(const eqat_desc& d, const eqat_bf16* dG, const eqat_bf16* dU, const eqat_packed_weight& gate,
+                           const eqat_packed_weight& up, eqat_bf16* dX, cudaStream_t st);
 // ds (and optionally dz) reduced in the epilogue of dY^T * X.  One group per row needs
 // packed_ds_workspace_bytes(d) bytes of scratch for the per-tile partial sums (0 otherwise).
 size_t packed_ds_workspace_bytes(const eqat_desc& d);
