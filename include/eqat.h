@@ -599,29 +599,16 @@ typedef struct {              /* a weight as qlinear_packed_fwd takes it: device
 
 /* Both projections of a feed-forward block and their product, the weights packed:
  *     G = X * W_gate^T,   U = X * W_up^T,   H = act(G) * U
- * for two weights of one descriptor (out_features of each).  Large batches: one
- * kernel in which a tile holds both projections of its features; G and U leave it
- * only if they are wanted (for the backward pass), and H is that of the sums before
- * they are rounded.  A few tokens: one pass over both weights, likewise.  Between
- * them (eqat_packed_gated_route): two calls of qlinear_packed_fwd and one of
- * eqat_gated_fwd, through G and U or, where these are NULL, the workspace; H is that
- * of G and U as they are rounded.  Weights enter the products as in
- * qlinear_packed_fwd.
+ * for two weights of one descriptor (out_features of each), in one pass over both:
+ * the kernels of qlinear_packed_fwd, with tiles that hold both projections of their
+ * features.  G and U leave them only if they are wanted (for the backward pass), and
+ * H is that of the sums before they are rounded.  The kernel is the one that
+ * qlinear_packed_fwd takes for a weight of 2*out_features rows (eqat_packed_fwd_route);
+ * what is said there of how weights enter the products, and of bits, holds for it.
  *   X [T,in] bf16, gate, up (in)   H [T,out] bf16 (out)
  *   G, U [T,out] bf16 (out): both, or both NULL */
-size_t eqat_packed_gated_workspace_bytes(const eqat_desc* desc);
 int qlinear_packed_gated_fwd(const eqat_desc* desc, int activation, const eqat_bf16* X, const eqat_packed_weight* gate,
-                             const eqat_packed_weight* up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, void* workspace,
-                             size_t workspace_bytes, void* stream);
-
-/* How qlinear_packed_gated_fwd takes a problem, decided on the host from the
- * descriptor alone (a diagnostic); `sms` as in eqat_packed_fwd_route. */
-enum {
-  EQAT_GATED_COMPOSED = 0,    /* two projections and their product                    */
-  EQAT_GATED_TILED = 1,       /* one kernel, tiles of both projections                */
-  EQAT_GATED_MATRIX_VECTOR = 2
-};
-int eqat_packed_gated_route(const eqat_desc* desc, int sms);
+                             const eqat_packed_weight* up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, void* stream);
 
 /* dG and dU as in eqat_gated_bwd, and
  *     dX = dG * W_gate + dU * W_up

@@ -226,18 +226,17 @@ PackedRoute packed_route(const eqat_desc& d, int sms) {
   return r;
 }
 
-inline size_t up_to_256(size_t n) { return (n + 255) & ~(size_t)255; }
-
-// On the current device (sms = 0; without one, as on a device of 148), or as on a device of `sms` SMs.
-int gated_route(const eqat_desc& d, int sms) {
-  if (sms == 0 && sm_count() <= 0) sms = 148;
-  return packed_route(d, sms).kernel == EQAT_ROUTE_TILED ? EQAT_GATED_TILED : EQAT_GATED_COMPOSED;
+// A gated feed-forward block's two weights as one with the rows of both, which decides the kernel.
+eqat_desc both_weights(const eqat_desc& d) {
+  eqat_desc both = d;
+  both.out_features = 2 * d.out_features;
+  return both;
 }
 
 int check_gated_weights(const eqat_desc* d, int activation, const eqat_packed_weight* gate, const eqat_packed_weight* up) {
   const int rc = check_gemm_desc(d, true);
   if (rc != EQAT_OK) return rc;
-  if (d->out_features > 1 << 29) return EQAT_ERR_SHAPE;                  // both are counted in 32 bits
+  if (d->out_features > 1 << 29) return EQAT_ERR_SHAPE;                  // the rows of both are counted in 32 bits
   if (activation < EQAT_ACT_SILU || activation > EQAT_ACT_GELU_TANH) return EQAT_ERR_UNSUPPORTED;
   if (gate == nullptr || up == nullptr) return EQAT_ERR_NULL;
   return check_ptrs(gate->Wq_packed, gate->s16, gate->z, up->Wq_packed, up->s16, up->z);
@@ -604,38 +603,21 @@ int eqat_gated_bwd(const eqat_gated_desc* d, const eqat_bf16* dH, const eqat_bf1
   return launch_gated_bwd(*d, dH, G, g_pitch, U, u_pitch, dG, dg_pitch, dU, du_pitch, as_stream(stream));
 }
 
-size_t eqat_packed_gated_workspace_bytes(const eqat_desc* d) {
-  if (check_gemm_desc(d, true) != EQAT_OK) return (size_t)-1;
-  if (gated_route(*d, 0) != EQAT_GATED_COMPOSED) return 0;
-  return 2 * up_to_256((size_t)d->tokens * d->out_features * sizeof(eqat_bf16));
-}
-
-int eqat_packed_gated_route(const eqat_desc* d, int sms) {
-  EQAT_TRY(check_gemm_desc(d, true));
-  if (sms < 0) return EQAT_ERR_SHAPE;
-  return gated_route(*d, sms);
-}
-
 int qlinear_packed_gated_fwd(const eqat_desc* d, int activation, const eqat_bf16* X, const eqat_packed_weight* gate,
-                             const eqat_packed_weight* up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, void* workspace,
-                             size_t workspace_bytes, void* stream) {
+                             const eqat_packed_weight* up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, void* stream) {
   EQAT_TRY(check_gated_weights(d, activation, gate, up));
   EQAT_TRY(check_ptrs(X, H));
   if ((G == nullptr) != (U == nullptr)) return EQAT_ERR_NULL;
   if (!aligned16(G) || !aligned16(U)) return EQAT_ERR_ALIGN;
-  const int route = gated_route(*d, 0);
-  if (route == EQAT_GATED_TILED) return launch_packed_gated(*d, activation, X, *gate, *up, H, G, U, as_stream(stream));
-  if (G == nullptr) {
-    const size_t one = up_to_256((size_t)d->tokens * d->out_features * sizeof(eqat_bf16));
-    if (workspace == nullptr || workspace_bytes < 2 * one || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
-      return EQAT_ERR_WORKSPACE;
-    G = static_cast<eqat_bf16*>(workspace);
-    U = reinterpret_cast<eqat_bf16*>(static_cast<uint8_t*>(workspace) + one);
+  const eqat_desc both = both_weights(*d);
+  const PackedRoute r = packed_route(both, 0);
+  cudaStream_t st = as_stream(stream);
+  switch (r.kernel) {
+    case EQAT_ROUTE_WEIGHT_ROWS: return launch_slim_gated(*d, activation, X, *gate, *up, H, G, U, r.slim, st);
+    case EQAT_ROUTE_MATRIX_VECTOR: return launch_gemv_gated(*d, both, activation, X, *gate, *up, H, G, U, st);
+    case EQAT_ROUTE_WEIGHT_ROW_PAIRS: return launch_wide_gated(*d, activation, X, *gate, *up, H, G, U, r.wide, st);
+    default: return launch_packed_gated(*d, activation, X, *gate, *up, H, G, U, st);
   }
-  EQAT_TRY(qlinear_packed_fwd(d, X, gate->Wq_packed, gate->s16, gate->z, G, stream));
-  EQAT_TRY(qlinear_packed_fwd(d, X, up->Wq_packed, up->s16, up->z, U, stream));
-  const eqat_gated_desc g{d->tokens, d->out_features, activation};
-  return launch_gated_fwd(g, G, d->out_features, U, d->out_features, H, as_stream(stream));
 }
 
 int qlinear_packed_gated_bwd(const eqat_desc* d, int activation, const eqat_bf16* dH, const eqat_bf16* G, const eqat_bf16* U,

@@ -21,6 +21,21 @@ struct PackedWeight {
   int wq_sectors;            // Wq is 32-byte aligned: a thread may fetch a whole 32-byte sector with one load
 };
 
+// The second weight of a gated feed-forward block, of the same shape as the first, and what is done with the two
+// projections: D = act(first) * second.
+struct OtherWeight {
+  const uint8_t* Wq;
+  const eqat_fp16* s16;
+  const void* zq;
+  int wq_sectors;
+  int activation;
+  eqat_bf16 *gate_out, *other_out;   // the projections themselves, or null
+};
+
+inline OtherWeight other_weight(const eqat_packed_weight& w, int activation, eqat_bf16* gate_out, eqat_bf16* other_out) {
+  return OtherWeight{w.Wq_packed, w.s16, w.z, (reinterpret_cast<uintptr_t>(w.Wq_packed) & 31u) == 0 ? 1 : 0, activation, gate_out, other_out};
+}
+
 inline int log2_exact(int v) {
   int s = 0;
   while ((1 << s) < v) ++s;

@@ -90,13 +90,7 @@ struct GemmParams : PackedWeight {
   const float* z32;          // [out, in/group]
   float Q;                   // 2^N - 1
   int dz_literal;            // Eq. 4 clamped branch: -1 instead of -s
-  // EPI_GATED / EPI_JOINT: the other weight, of the same shape
-  const uint8_t* other_Wq;
-  const eqat_fp16* other_s16;
-  const void* other_zq;
-  int other_sectors;         // as wq_sectors
-  int activation;            // EPI_GATED: D = act(gate) * other
-  eqat_bf16 *gate_out, *other_out;   // EPI_GATED: the projections themselves, or null
+  OtherWeight other;         // EPI_GATED / EPI_JOINT
 };
 
 template <int MT, bool PACKED, bool PAIR, int BN>
@@ -322,7 +316,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       for (int c = 0; c < kColumns / 32; ++c) {
         const int col0 = n_blk * kColumns + c * 32;
         uint32_t o[16];
-        if (p.gate_out != nullptr) {
+        if (p.other.gate_out != nullptr) {
 #pragma unroll 1
           for (int s = 0; s < 2; ++s) {
             uint32_t r[32];
@@ -330,7 +324,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
             ptx::tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[i] = pack_bf16x2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
-            store32(s == 0 ? p.gate_out : p.other_out, col0, o);
+            store32(s == 0 ? p.other.gate_out : p.other.other_out, col0, o);
           }
         }
 #pragma unroll
@@ -339,7 +333,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
           ptx::tmem_ld_32x16(t_row + c * 32 + s * 16, g);
           ptx::tmem_ld_32x16(t_row + kColumns + c * 32 + s * 16, u);
           ptx::tmem_ld_wait();
-          EQAT_WITH_ACTIVATION(p.activation, _Pragma("unroll") for (int i = 0; i < 8; ++i)
+          EQAT_WITH_ACTIVATION(p.other.activation, _Pragma("unroll") for (int i = 0; i < 8; ++i)
                                                  o[8 * s + i] = pack_bf16x2(activate<kAct>(__uint_as_float(g[2 * i])) * __uint_as_float(u[2 * i]),
                                                                             activate<kAct>(__uint_as_float(g[2 * i + 1])) * __uint_as_float(u[2 * i + 1])));
         }
@@ -756,7 +750,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       PackedWeight w = p;
       constexpr int kWeightRows = GATED ? BN / 2 : BN;             // rows of a weight in a tile's B operand
       const int brow = (rank * U + t) & (kWeightRows - 1);         // K-major: this thread's among them
-      if (GATED && rank * U + t >= kWeightRows) { w.Wq = p.other_Wq; w.s16 = p.other_s16; w.zq = p.other_zq; w.wq_sectors = p.other_sectors; }
+      if (GATED && rank * U + t >= kWeightRows) { w.Wq = p.other.Wq; w.s16 = p.other.s16; w.zq = p.other.zq; w.wq_sectors = p.other.wq_sectors; }
       long gk = 0;                                                // global index of the tile's K block 0
       int acc = 0;
       uint32_t acc_phase = 0;
@@ -787,9 +781,9 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
             if (valid) {
               const bool second = 2 * kb >= num_kb;
               const int k = second ? kb - num_kb / 2 : kb;
-              w.Wq = second ? p.other_Wq : p.Wq;
-              w.s16 = second ? p.other_s16 : p.s16;
-              w.zq = second ? p.other_zq : p.zq;
+              w.Wq = second ? p.other.Wq : p.Wq;
+              w.s16 = second ? p.other.s16 : p.s16;
+              w.zq = second ? p.other.zq : p.zq;
               load_codes64<BITS>(w.Wq + (size_t)(k * BK + kr) * pitch + (size_t)unit0 * (8 * BITS), ring_w[j][0]);
               load_group_params(w, g_row0 + (size_t)k * BK * p.groups_per_row, g_count, ring_g[j]);
             }
@@ -1183,13 +1177,6 @@ int launch_two(const Operand& a, const Operand& b, GemmParams& p, cudaStream_t s
                 : launch<2, false, B_MN, true, EPI, BITS, false>(a, b, p, st);
 }
 
-void set_other(GemmParams& p, const eqat_packed_weight& w) {
-  p.other_Wq = w.Wq_packed;
-  p.other_s16 = w.s16;
-  p.other_zq = w.z;
-  p.other_sectors = (reinterpret_cast<uintptr_t>(w.Wq_packed) & 31u) == 0 ? 1 : 0;
-}
-
 template <int BITS>
 int launch_ds(const Operand& a, const Operand& b, GemmParams& p, cudaStream_t st) {
   const TileShape s = ds_shape(p.M, p.N, p.partial != nullptr ? kBN : 1 << p.group_shift, sm_count());
@@ -1290,11 +1277,8 @@ int launch_packed_gated(const eqat_desc& d, int activation, const eqat_bf16* X, 
                         const eqat_packed_weight& up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, cudaStream_t st) {
   GemmParams p = base_params((int)d.tokens, d.out_features, d.in_features);
   p.D = H;
-  p.gate_out = G;
-  p.other_out = U;
-  p.activation = activation;
   set_weight(p, d, gate.Wq_packed, gate.s16, gate.z);
-  set_other(p, up);
+  p.other = other_weight(up, activation, G, U);
   const Operand a{X, (uint64_t)d.tokens, (uint64_t)d.in_features, false};
   switch (d.bits) {
     case 2: return launch_two<EPI_GATED, false, 2>(a, a, p, st);
@@ -1308,7 +1292,7 @@ int launch_packed_gated_dx(const eqat_desc& d, const eqat_bf16* dG, const eqat_b
   GemmParams p = base_params((int)d.tokens, d.in_features, 2 * d.out_features);
   p.D = dX;
   set_weight(p, d, gate.Wq_packed, gate.s16, gate.z);
-  set_other(p, up);
+  p.other = other_weight(up, 0, nullptr, nullptr);
   const Operand a{dG, (uint64_t)d.tokens, (uint64_t)d.out_features, false}, b{dU, (uint64_t)d.tokens, (uint64_t)d.out_features, false};
   switch (d.bits) {
     case 2: return launch_two<EPI_JOINT, true, 2>(a, b, p, st);

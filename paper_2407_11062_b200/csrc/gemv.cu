@@ -10,7 +10,9 @@
 // small numbers and the step size scales fp32 accumulators.
 #include <cuda.h>
 
+#include "activation.cuh"
 #include "common.cuh"
+#include "expand.cuh"
 #include "gemm.cuh"
 #include "gemv.cuh"
 #include "ptx.cuh"
@@ -65,6 +67,11 @@ namespace {
 // and the fifth instruction holds all nine products.  The 16 warps' partial sums of a
 // task go through a double-buffered shared array to a reducer warp, which adds
 // them in a fixed order and stores Y while the consumers are on the next task.
+//
+// A gated feed-forward block's two projections (GATED): a task is 8 rows of the
+// gate's weight and the same 8 of the other's, a box two copies of 8 rows.  Lane
+// (g, q) then holds row g of either weight, and the reducer, which has both sums
+// of a feature, stores their product.
 constexpr int kTcMaxTokens = 8;                         // the instruction has eight token columns
 constexpr int kTcMaxTotalTokens = 64;                   // up to here a plan is made, for comparison (see packed_gemv_applies)
 constexpr int kTcWarps = 16;
@@ -200,10 +207,10 @@ __host__ __device__ constexpr float tc_bias(int j) {
   return BITS == 4 ? 128.0f : ((j & 7) % 3 == 0 ? 128.0f : ((j & 7) % 3 == 1 ? 32.0f : 8.0f));
 }
 
-template <int BITS, int PARAM_MODE, bool ZF16>
+template <int BITS, int PARAM_MODE, bool ZF16, bool GATED>
 __global__ void __launch_bounds__(kTcThreads, 1)
-packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const eqat_bf16* X,
-                      const eqat_fp16* s16, const void* zq, eqat_bf16* __restrict__ Y,
+packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_other, const eqat_bf16* X,
+                      const eqat_fp16* s16, const void* zq, const OtherWeight other, eqat_bf16* __restrict__ Y,
                       int out_features, int in_features, int group_shift, int groups_per_row, int T, int stages) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = ptx::smem_addr(smem_raw);
@@ -220,7 +227,8 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const eqat_bf16
   TcCtl* ctl = reinterpret_cast<TcCtl*>(ring + L.ctl_off);
   volatile int* abort_flag = &ctl->abort;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int n_tasks = out_features / kTcRows;
+  constexpr int kWeightRows = GATED ? kTcRows / 2 : kTcRows;       // of a weight per task
+  const int n_tasks = out_features / kWeightRows;
   const int chunks = in_features >> 6;
   const int row_bytes = in_features * BITS / 8;
   const int n_boxes = (row_bytes + kTcBoxBytes - 1) / kTcBoxBytes;
@@ -273,39 +281,43 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const eqat_bf16
   constexpr int kSlotShift = PARAM_MODE == 2 ? 1 : (PARAM_MODE == 3 ? 2 : 0);
   const uint8_t* const z8 = static_cast<const uint8_t*>(zq);
   const eqat_fp16* const z16 = static_cast<const eqat_fp16*>(zq);
+  // of the lane's second row: eight rows further, or (GATED) the same row of the other weight
+  const eqat_fp16* const s16_hi = GATED ? other.s16 : s16;
+  const uint8_t* const z8_hi = GATED ? static_cast<const uint8_t*>(other.zq) : z8;
+  const eqat_fp16* const z16_hi = GATED ? static_cast<const eqat_fp16*>(other.zq) : z16;
   auto fetch = [&](int task, int k) {
     StageParams sp;
     sp.s_lo = sp.s_hi = sp.z_lo = sp.z_hi = make_uint2(0u, 0u);
     const int cg0 = (k * kBoxesPerStage + box) * kChunksPerBox + chunk0;
     if (task < n_tasks && cg0 < chunks) {
-      const size_t p_lo = (size_t)(task * kTcRows + g) * groups_per_row, p_hi = p_lo + (size_t)8 * groups_per_row;
+      const size_t p_lo = (size_t)(task * kWeightRows + g) * groups_per_row, p_hi = p_lo + (GATED ? 0 : (size_t)8 * groups_per_row);
       if constexpr (PARAM_MODE == 1) {                    // the row has a multiple of four groups: all four exist
         sp.s_lo = ptx::ld_global(reinterpret_cast<const uint2*>(s16 + p_lo + cg0));
-        sp.s_hi = ptx::ld_global(reinterpret_cast<const uint2*>(s16 + p_hi + cg0));
+        sp.s_hi = ptx::ld_global(reinterpret_cast<const uint2*>(s16_hi + p_hi + cg0));
         if constexpr (ZF16) {
           sp.z_lo = ptx::ld_global(reinterpret_cast<const uint2*>(z16 + p_lo + cg0));
-          sp.z_hi = ptx::ld_global(reinterpret_cast<const uint2*>(z16 + p_hi + cg0));
+          sp.z_hi = ptx::ld_global(reinterpret_cast<const uint2*>(z16_hi + p_hi + cg0));
         } else {
           sp.z_lo.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(z8 + p_lo + cg0));
-          sp.z_hi.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(z8 + p_hi + cg0));
+          sp.z_hi.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(z8_hi + p_hi + cg0));
         }
       } else if constexpr (PARAM_MODE == 2) {             // an even number of groups per row: both exist
         const int g0 = cg0 >> 1;
         sp.s_lo.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(s16 + p_lo + g0));
-        sp.s_hi.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(s16 + p_hi + g0));
+        sp.s_hi.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(s16_hi + p_hi + g0));
         if constexpr (ZF16) {
           sp.z_lo.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(z16 + p_lo + g0));
-          sp.z_hi.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(z16 + p_hi + g0));
+          sp.z_hi.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(z16_hi + p_hi + g0));
         } else {
           sp.z_lo.x = ptx::ld_global(reinterpret_cast<const uint16_t*>(z8 + p_lo + g0));
-          sp.z_hi.x = ptx::ld_global(reinterpret_cast<const uint16_t*>(z8 + p_hi + g0));
+          sp.z_hi.x = ptx::ld_global(reinterpret_cast<const uint16_t*>(z8_hi + p_hi + g0));
         }
       } else if constexpr (PARAM_MODE == 3) {
         const int grp = (cg0 << 6) >> group_shift;
         sp.s_lo.x = ptx::ld_global(s16 + p_lo + grp);
-        sp.s_hi.x = ptx::ld_global(s16 + p_hi + grp);
+        sp.s_hi.x = ptx::ld_global(s16_hi + p_hi + grp);
         sp.z_lo.x = ZF16 ? (uint32_t)ptx::ld_global(z16 + p_lo + grp) : (uint32_t)ptx::ld_global(z8 + p_lo + grp);
-        sp.z_hi.x = ZF16 ? (uint32_t)ptx::ld_global(z16 + p_hi + grp) : (uint32_t)ptx::ld_global(z8 + p_hi + grp);
+        sp.z_hi.x = ZF16 ? (uint32_t)ptx::ld_global(z16_hi + p_hi + grp) : (uint32_t)ptx::ld_global(z8_hi + p_hi + grp);
       } else {
         uint32_t sl[4] = {0u, 0u, 0u, 0u}, sh[4] = {0u, 0u, 0u, 0u}, zl[4] = {0u, 0u, 0u, 0u}, zh[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
@@ -313,9 +325,9 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const eqat_bf16
           if (cg0 + c < chunks) {
             const int grp = ((cg0 + c) << 6) >> group_shift;
             sl[c] = ptx::ld_global(s16 + p_lo + grp);
-            sh[c] = ptx::ld_global(s16 + p_hi + grp);
+            sh[c] = ptx::ld_global(s16_hi + p_hi + grp);
             zl[c] = ZF16 ? (uint32_t)ptx::ld_global(z16 + p_lo + grp) : (uint32_t)ptx::ld_global(z8 + p_lo + grp);
-            zh[c] = ZF16 ? (uint32_t)ptx::ld_global(z16 + p_hi + grp) : (uint32_t)ptx::ld_global(z8 + p_hi + grp);
+            zh[c] = ZF16 ? (uint32_t)ptx::ld_global(z16_hi + p_hi + grp) : (uint32_t)ptx::ld_global(z8_hi + p_hi + grp);
           }
         }
         sp.s_lo = make_uint2(sl[0] | (sl[1] << 16), sl[2] | (sl[3] << 16));
@@ -363,9 +375,12 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const eqat_bf16
           const int nb = min(kBoxesPerStage, n_boxes - k * kBoxesPerStage);
           const uint32_t full = ptx::smem_addr(&ctl->full[slot]);
           ptx::mbar_expect_tx(full, (uint32_t)nb * kTcBoxSmem);     // bytes past the end of a row are zero-filled and counted
-          for (int b = 0; b < nb; ++b)
-            ptx::tma_load_2d(ring_addr + slot * kStageBytes + b * kTcBoxSmem, &map_w,
-                             (k * kBoxesPerStage + b) * kTcBoxBytes, task * kTcRows, full);
+          for (int b = 0; b < nb; ++b) {
+            const uint32_t dst = ring_addr + slot * kStageBytes + b * kTcBoxSmem;
+            const int col = (k * kBoxesPerStage + b) * kTcBoxBytes;
+            ptx::tma_load_2d(dst, &map_w, col, task * kWeightRows, full);
+            if (GATED) ptx::tma_load_2d(dst + kWeightRows * kTcBoxBytes, &map_other, col, task * kWeightRows, full);
+          }
           ++issued;
           if (++slot == stages) { slot = 0; phase ^= 1u; }
         }
@@ -396,16 +411,28 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const eqat_bf16
     // task is one stage and this warp sets the pace.
     constexpr int kZAhead = 2;                             // 16-byte pieces per lane: rows of up to 64 groups
     uint4 z_next[kZAhead];
-    const uint4* const z_pieces = static_cast<const uint4*>(zq);   // a task's bytes are contiguous: groups_per_row pieces
+    // a task's bytes are contiguous: groups_per_row pieces, or (GATED) as many halves of one of each weight
+    auto z_piece = [&](int task, int i) {
+      const size_t at = (size_t)task * groups_per_row + i;
+      if constexpr (GATED) {
+        const uint2 a = ptx::ld_global(static_cast<const uint2*>(zq) + at), b = ptx::ld_global(static_cast<const uint2*>(other.zq) + at);
+        return make_uint4(a.x, a.y, b.x, b.y);
+      } else {
+        return ptx::ld_global(static_cast<const uint4*>(zq) + at);
+      }
+    };
     auto z_fetch = [&](int task) {
 #pragma unroll
       for (int i = 0; i < kZAhead; ++i) {
         z_next[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (task < n_tasks && lane + 32 * i < groups_per_row)
-          z_next[i] = ptx::ld_global(z_pieces + (size_t)task * groups_per_row + lane + 32 * i);
+        if (task < n_tasks && lane + 32 * i < groups_per_row) z_next[i] = z_piece(task, lane + 32 * i);
       }
     };
-    auto eighth_bits = [&](int row, int n) {               // -128 s xs over the groups of a row whose zero point has it
+    auto eighth_bits = [&](int task, int r, int n) {       // -128 s xs over the groups of a row whose zero point has it
+      const bool second = GATED && r >= kWeightRows;
+      const int row = task * kWeightRows + (second ? r - kWeightRows : r);
+      const uint8_t* const z8 = static_cast<const uint8_t*>(second ? other.zq : zq);
+      const eqat_fp16* const steps = second ? other.s16 : s16;
       float v = 0.0f;
 #pragma unroll 1
       for (int cg = 0; cg < chunks; ++cg) {
@@ -415,7 +442,7 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const eqat_bf16
         const uint2* item = xb + ((size_t)cg * 4 * T + n) * kTcItems + 4;
         const uint32_t p0 = item[0].y, p12 = item[(size_t)T * kTcItems].x;
         const float xs = (__uint_as_float(p0 & 0xFFFF0000u) + __uint_as_float(p12 << 16)) + __uint_as_float(p12 & 0xFFFF0000u);
-        v = fmaf(-128.0f * __half2float(__ushort_as_half(ptx::ld_global(s16 + grp))), xs, v);
+        v = fmaf(-128.0f * __half2float(__ushort_as_half(ptx::ld_global(steps + grp))), xs, v);
       }
       return v;
     };
@@ -427,7 +454,7 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const eqat_bf16
         for (int i = 0; i < kZAhead; ++i) z_seen |= z_next[i].x | z_next[i].y | z_next[i].z | z_next[i].w;
         z_fetch(task + gridDim.x);
         for (int i = lane + 32 * kZAhead; i < groups_per_row; i += 32) {
-          const uint4 v = ptx::ld_global(z_pieces + (size_t)task * groups_per_row + i);
+          const uint4 v = z_piece(task, i);
           z_seen |= v.x | v.y | v.z | v.w;
         }
       }
@@ -436,16 +463,36 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const eqat_bf16
 #pragma unroll 1
         for (int idx = lane; idx < kTcRows * T; idx += 32) {
           const int r = idx & (kTcRows - 1), n = idx >> 4;
-          part[(buf * kTcWarps * kTcRows + r) * kTcMaxTokens + n] += eighth_bits(task * kTcRows + r, n);
+          part[(buf * kTcWarps * kTcRows + r) * kTcMaxTokens + n] += eighth_bits(task, r, n);
         }
       }
-      for (int idx = lane; idx < kTcRows * T; idx += 32) {
-        const int r = idx & (kTcRows - 1), n = idx >> 4;
-        float v = 0.0f;
+      if constexpr (GATED) {
+        for (int idx = lane; idx < kWeightRows * T; idx += 32) {
+          const int r = idx & (kWeightRows - 1), n = idx >> 3;
+          float v = 0.0f, u = 0.0f;
 #pragma unroll
-        for (int wv = 0; wv < kTcWarps; ++wv)              // fixed order: deterministic
-          v += part[((buf * kTcWarps + wv) * kTcRows + r) * kTcMaxTokens + n];
-        Y[(size_t)n * out_features + (size_t)task * kTcRows + r] = (eqat_bf16)(pack_bf16x2(v, 0.0f) & 0xFFFFu);
+          for (int wv = 0; wv < kTcWarps; ++wv) {
+            const float* at = part + ((buf * kTcWarps + wv) * kTcRows + r) * kTcMaxTokens + n;
+            v += at[0];
+            u += at[kWeightRows * kTcMaxTokens];
+          }
+          const size_t at = (size_t)n * out_features + (size_t)task * kWeightRows + r;
+          if (other.gate_out != nullptr) {
+            other.gate_out[at] = (eqat_bf16)(pack_bf16x2(v, 0.0f) & 0xFFFFu);
+            other.other_out[at] = (eqat_bf16)(pack_bf16x2(u, 0.0f) & 0xFFFFu);
+          }
+          EQAT_WITH_ACTIVATION(other.activation, v = activate<kAct>(v));
+          Y[at] = (eqat_bf16)(pack_bf16x2(v * u, 0.0f) & 0xFFFFu);
+        }
+      } else {
+        for (int idx = lane; idx < kTcRows * T; idx += 32) {
+          const int r = idx & (kTcRows - 1), n = idx >> 4;
+          float v = 0.0f;
+#pragma unroll
+          for (int wv = 0; wv < kTcWarps; ++wv)            // fixed order: deterministic
+            v += part[((buf * kTcWarps + wv) * kTcRows + r) * kTcMaxTokens + n];
+          Y[(size_t)n * out_features + (size_t)task * kTcRows + r] = (eqat_bf16)(pack_bf16x2(v, 0.0f) & 0xFFFFu);
+        }
       }
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&ctl->part_free[buf]));
@@ -651,18 +698,23 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const eqat_bf16
   }
 }
 
-template <int BITS, int PARAM_MODE, bool ZF16>
-int launch_tc_mode(const eqat_desc& d, const eqat_bf16* X, const uint8_t* Wq, const eqat_fp16* s16, const void* zq,
+template <int BITS, int PARAM_MODE, bool ZF16, bool GATED>
+int launch_tc_mode(const eqat_desc& d, const eqat_bf16* X, const eqat_packed_weight& w, const OtherWeight& other,
                    eqat_bf16* Y, int group_shift, int stages, cudaStream_t st) {
   static SmemOptIn opt_in;
-  if (!opt_in.ensure(packed_gemv_tc_kernel<BITS, PARAM_MODE, ZF16>, (int)kTcSmemBudget)) return EQAT_ERR_CUDA;
-  CUtensorMap mw;
+  if (!opt_in.ensure(packed_gemv_tc_kernel<BITS, PARAM_MODE, ZF16, GATED>, (int)kTcSmemBudget)) return EQAT_ERR_CUDA;
+  constexpr int kWeightRows = GATED ? kTcRows / 2 : kTcRows;
+  CUtensorMap mw, mo;
   const uint64_t row_bytes = (uint64_t)d.in_features * BITS / 8;
-  if (!make_tmap_u8(&mw, Wq, row_bytes, (uint64_t)d.out_features, tc_box_bytes(BITS), kTcRows, BITS == 3 ? 0 : 128))
-    return EQAT_ERR_CUDA;
+  auto codes_map = [&](CUtensorMap* m, const uint8_t* Wq) {
+    return make_tmap_u8(m, Wq, row_bytes, (uint64_t)d.out_features, tc_box_bytes(BITS), kWeightRows, BITS == 3 ? 0 : 128);
+  };
+  if (!codes_map(&mw, w.Wq_packed)) return EQAT_ERR_CUDA;
+  if (!GATED) mo = mw;
+  else if (!codes_map(&mo, other.Wq)) return EQAT_ERR_CUDA;
   const int sms = sm_count();
   if (sms <= 0) return EQAT_ERR_CUDA;
-  const int T = (int)d.tokens, n_tasks = d.out_features / kTcRows, ng = d.in_features / d.group;
+  const int T = (int)d.tokens, n_tasks = d.out_features / kWeightRows, ng = d.in_features / d.group;
   const TcLayout L = tc_layout(T, d.in_features, stages, BITS);
   // Programmatic stream serialisation: back-to-back launches of this kernel overlap the tail of one grid with the
   // CTA start-up of the next (the kernel waits for its predecessors before its first global access).  After a
@@ -677,7 +729,7 @@ int launch_tc_mode(const eqat_desc& d, const eqat_bf16* X, const uint8_t* Wq, co
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, packed_gemv_tc_kernel<BITS, PARAM_MODE, ZF16>, mw, X, s16, zq, Y,
+  if (cudaLaunchKernelEx(&cfg, packed_gemv_tc_kernel<BITS, PARAM_MODE, ZF16, GATED>, mw, mo, X, w.s16, w.z, other, Y,
                          d.out_features, d.in_features, group_shift, ng, T, stages) != cudaSuccess) {
     (void)cudaGetLastError();
     return EQAT_ERR_CUDA;
@@ -685,27 +737,27 @@ int launch_tc_mode(const eqat_desc& d, const eqat_bf16* X, const uint8_t* Wq, co
   return launch_status();
 }
 
-template <int BITS, bool ZF16>
-int launch_tc_format(const eqat_desc& d, const eqat_bf16* X, const uint8_t* Wq, const eqat_fp16* s16, const void* zq,
-                     eqat_bf16* Y, int group_shift, int stages, cudaStream_t st) {
+template <int BITS, bool ZF16, bool GATED>
+int launch_tc_format(const eqat_desc& d, const eqat_bf16* X, const eqat_packed_weight& w, const OtherWeight& other, eqat_bf16* Y, int group_shift, int stages, cudaStream_t st) {
   // how a lane fetches the parameters of its 256 columns of a stage (see the kernel): one load per row and kind
   // where the rows of step sizes and zero points keep the alignment those loads need, chunk by chunk otherwise
-  const uintptr_t s_addr = reinterpret_cast<uintptr_t>(s16), z_addr = reinterpret_cast<uintptr_t>(zq);
+  uintptr_t s_addr = reinterpret_cast<uintptr_t>(w.s16), z_addr = reinterpret_cast<uintptr_t>(w.z);
+  if (GATED) { s_addr |= reinterpret_cast<uintptr_t>(other.s16); z_addr |= reinterpret_cast<uintptr_t>(other.zq); }
   const uintptr_t z_unit = ZF16 ? 2 : 1;                 // bytes per zero point
   const int ng = d.in_features / d.group;
   if (d.group == 64 && ng % 4 == 0 && (s_addr & 7u) == 0 && (z_addr & (4 * z_unit - 1)) == 0)
-    return launch_tc_mode<BITS, 1, ZF16>(d, X, Wq, s16, zq, Y, group_shift, stages, st);
+    return launch_tc_mode<BITS, 1, ZF16, GATED>(d, X, w, other, Y, group_shift, stages, st);
   if (d.group == 128 && ng % 2 == 0 && (s_addr & 3u) == 0 && (z_addr & (2 * z_unit - 1)) == 0)
-    return launch_tc_mode<BITS, 2, ZF16>(d, X, Wq, s16, zq, Y, group_shift, stages, st);
-  if (d.group >= 256) return launch_tc_mode<BITS, 3, ZF16>(d, X, Wq, s16, zq, Y, group_shift, stages, st);
-  return launch_tc_mode<BITS, 0, ZF16>(d, X, Wq, s16, zq, Y, group_shift, stages, st);
+    return launch_tc_mode<BITS, 2, ZF16, GATED>(d, X, w, other, Y, group_shift, stages, st);
+  if (d.group >= 256) return launch_tc_mode<BITS, 3, ZF16, GATED>(d, X, w, other, Y, group_shift, stages, st);
+  return launch_tc_mode<BITS, 0, ZF16, GATED>(d, X, w, other, Y, group_shift, stages, st);
 }
 
-template <int BITS>
-int launch_tc(const eqat_desc& d, const eqat_bf16* X, const uint8_t* Wq, const eqat_fp16* s16, const void* zq,
-              eqat_bf16* Y, int group_shift, int stages, cudaStream_t st) {
-  return d.zero_point_format == EQAT_ZP_FP16 ? launch_tc_format<BITS, true>(d, X, Wq, s16, zq, Y, group_shift, stages, st)
-                                             : launch_tc_format<BITS, false>(d, X, Wq, s16, zq, Y, group_shift, stages, st);
+template <int BITS, bool GATED>
+int launch_tc(const eqat_desc& d, const eqat_bf16* X, const eqat_packed_weight& w, const OtherWeight& other, eqat_bf16* Y,
+              int group_shift, int stages, cudaStream_t st) {
+  return d.zero_point_format == EQAT_ZP_FP16 ? launch_tc_format<BITS, true, GATED>(d, X, w, other, Y, group_shift, stages, st)
+                                             : launch_tc_format<BITS, false, GATED>(d, X, w, other, Y, group_shift, stages, st);
 }
 
 }  // namespace
@@ -744,29 +796,44 @@ bool packed_gemv_applies(const eqat_desc& d) {
   return packed_gemv_plan(d).launches == 1 || packed_gemv_keeps_bits(d);
 }
 
-int launch_packed_gemv(const eqat_desc& d, const eqat_bf16* X, const uint8_t* Wq, const eqat_fp16* s16,
-                       const void* zq, eqat_bf16* Y, cudaStream_t st) {
+namespace {
+
+// All tokens, a slice of them a launch.
+template <bool GATED>
+int launch_slices(const eqat_desc& d, const FewTokenPlan& plan, const eqat_bf16* X, const eqat_packed_weight& w, const OtherWeight& other,
+                  eqat_bf16* Y, cudaStream_t st) {
   int group_shift = 31;                                  // one group per row: every group index shifts to 0
   if (d.group <= 256) {
     group_shift = 0;
     while ((1 << group_shift) < d.group) ++group_shift;
   }
-  const FewTokenPlan plan = packed_gemv_plan(d);
-  if (plan.launches > 0) {
-    for (int t0 = 0; t0 < (int)d.tokens; t0 += plan.slice) {
-      eqat_desc part = d;
-      part.tokens = (int)d.tokens - t0 < plan.slice ? (int)d.tokens - t0 : plan.slice;
-      const int stages = tc_stages_that_fit((int)part.tokens, d.in_features, d.bits);
-      const eqat_bf16* Xs = X + (size_t)t0 * d.in_features;
-      eqat_bf16* Ys = Y + (size_t)t0 * d.out_features;
-      const int rc = d.bits == 2   ? launch_tc<2>(part, Xs, Wq, s16, zq, Ys, group_shift, stages, st)
-                     : d.bits == 3 ? launch_tc<3>(part, Xs, Wq, s16, zq, Ys, group_shift, stages, st)
-                                   : launch_tc<4>(part, Xs, Wq, s16, zq, Ys, group_shift, stages, st);
-      if (rc != EQAT_OK) return rc;
-    }
-    return EQAT_OK;
+  if (plan.launches == 0) return EQAT_ERR_UNSUPPORTED;   // not reached for a problem packed_gemv_applies() accepted
+  for (int t0 = 0; t0 < (int)d.tokens; t0 += plan.slice) {
+    eqat_desc part = d;
+    part.tokens = (int)d.tokens - t0 < plan.slice ? (int)d.tokens - t0 : plan.slice;
+    const int stages = tc_stages_that_fit((int)part.tokens, d.in_features, d.bits);
+    const size_t at = (size_t)t0 * d.out_features;
+    const eqat_bf16* Xs = X + (size_t)t0 * d.in_features;
+    OtherWeight o = other;
+    if (o.gate_out != nullptr) { o.gate_out += at; o.other_out += at; }
+    const int rc = d.bits == 2   ? launch_tc<2, GATED>(part, Xs, w, o, Y + at, group_shift, stages, st)
+                   : d.bits == 3 ? launch_tc<3, GATED>(part, Xs, w, o, Y + at, group_shift, stages, st)
+                                 : launch_tc<4, GATED>(part, Xs, w, o, Y + at, group_shift, stages, st);
+    if (rc != EQAT_OK) return rc;
   }
-  return EQAT_ERR_UNSUPPORTED;                           // not reached for a problem packed_gemv_applies() accepted
+  return EQAT_OK;
+}
+
+}  // namespace
+
+int launch_packed_gemv(const eqat_desc& d, const eqat_bf16* X, const uint8_t* Wq, const eqat_fp16* s16,
+                       const void* zq, eqat_bf16* Y, cudaStream_t st) {
+  return launch_slices<false>(d, packed_gemv_plan(d), X, eqat_packed_weight{Wq, s16, zq}, OtherWeight{}, Y, st);
+}
+
+int launch_gemv_gated(const eqat_desc& d, const eqat_desc& both, int activation, const eqat_bf16* X, const eqat_packed_weight& gate,
+                      const eqat_packed_weight& up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, cudaStream_t st) {
+  return launch_slices<true>(d, packed_gemv_plan(both), X, gate, other_weight(up, activation, G, U), H, st);
 }
 
 int launch_wait_expiry_gemv(cudaStream_t st) { return launch_wait_expiry(st); }

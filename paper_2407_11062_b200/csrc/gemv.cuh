@@ -23,6 +23,10 @@ bool packed_gemv_applies(const eqat_desc& d);
 // Y[T,out] = X[T,in] * dequant(Wq)^T for a problem packed_gemv_applies() accepted
 int launch_packed_gemv(const eqat_desc& d, const eqat_bf16* X, const uint8_t* Wq, const eqat_fp16* s16,
                        const void* zq, eqat_bf16* Y, cudaStream_t st);
+// H = act(X * dequant(gate)^T) * (X * dequant(up)^T); G and U, the projections, or null.  `both`: the problem of a weight with the
+// rows of both, which decides the plan.
+int launch_gemv_gated(const eqat_desc& d, const eqat_desc& both, int activation, const eqat_bf16* X, const eqat_packed_weight& gate,
+                      const eqat_packed_weight& up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, cudaStream_t st);
 
 // Self-test of the matrix-vector kernel's bounded wait (one warp, 1 ms, a barrier nothing signals).
 int launch_wait_expiry_gemv(cudaStream_t st);

@@ -24,6 +24,9 @@
 // add up the accumulators of the group's run before, expand the run into the group's TMEM buffer, signal.  While one
 // group's MMAs run, the other group and the other CTA of the SM expand.
 //
+// A gated feed-forward block's two projections (GATED): a tile is 64 rows of the gate's weight and the same 64 of the other's,
+// so the CTA that adds up a token column has both projections of 64 features and stores their product.
+//
 // What bounds it: at a few row tiles per SM the chain of hand-offs outside the runs (about 4 us: barriers and TMEM, the
 // parameters, the exchange); on large weights the issue slots and the hand-offs of the runs, about 700 cycles per run and
 // SM where the eight MMAs of a run take 340 (an MMA of 16 columns costs its A operand's 4 KB).
@@ -31,6 +34,7 @@
 
 #include <type_traits>
 
+#include "activation.cuh"
 #include "common.cuh"
 #include "expand.cuh"
 #include "gemm.cuh"
@@ -52,6 +56,7 @@ struct SlimParams : PackedWeight {
   eqat_bf16* Y;                        // [T, out]
   int T;
   int split, split_log2, runs;         // runs = in_features / 128
+  OtherWeight other;                   // GATED
 };
 
 // A stage of the ring: the codes of two runs, a box of 128 rows of 64, 96 or 128 bytes, and their activations.
@@ -195,9 +200,10 @@ __device__ __forceinline__ void load_run(uint32_t box, int row, int j, uint32_t 
 
 // NT: token columns / 16.  ND: accumulators per run, one per quantisation group (1: groups of 128 and longer; 2: 64;
 // 4: 32).
-template <int BITS, int NT, int ND>
+template <int BITS, int NT, int ND, bool GATED>
 __global__ void __launch_bounds__(Slim<BITS, NT, ND>::kThreads, NT <= 2 ? 2 : 1)
-slim_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const SlimParams p) {
+slim_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                const __grid_constant__ CUtensorMap map_other, const SlimParams p) {
   using C = Slim<BITS, NT, ND>;
   constexpr int kGroups = C::kGroups, kThreads = C::kThreads;
   extern __shared__ uint8_t smem_raw[];
@@ -214,7 +220,12 @@ slim_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 
   // grid: row tiles x CTAs of a cluster x token tiles
   const int rank = (int)blockIdx.y;
-  const int t0 = (int)blockIdx.z * C::kTn, m0 = (int)blockIdx.x * kRows;
+  constexpr int kWeightRows = GATED ? kRows / 2 : kRows;   // of a weight in a tile
+  const int t0 = (int)blockIdx.z * C::kTn, m0 = (int)blockIdx.x * kWeightRows;
+  // Row rr of the tile: a row of a weight, whose parameters start here, or past its end.
+  auto weight_row = [&](int rr) { return m0 + (rr & (kWeightRows - 1)); };
+  auto step_sizes = [&](int rr) { return GATED && rr >= kWeightRows ? p.other.s16 : p.s16; };
+  auto zero_points = [&](int rr) { return GATED && rr >= kWeightRows ? p.other.zq : p.zq; };
   int run0, nruns, group0;
   slice_of(p.runs, p.split_log2, rank, run0, nruns);
   const int ngroups = slice_groups(run0, nruns, p.group_shift, group0);
@@ -222,12 +233,16 @@ slim_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   // The codes, step sizes and zero points of this CTA's slice are asked into L2 before the wait for the launches before
   // this one: a prefetch changes nothing that can be observed, and it takes the DRAM latency out of the loop below.
   if (warp == 0 && ptx::elect_one()) {
-    for (int r = 0; r < nruns; r += kBoxRuns) ptx::tma_prefetch_2d(&map_w, (run0 + r) * (16 * BITS), m0);
+    for (int r = 0; r < nruns; r += kBoxRuns) {
+      ptx::tma_prefetch_2d(&map_w, (run0 + r) * (16 * BITS), m0);
+      if (GATED) ptx::tma_prefetch_2d(&map_other, (run0 + r) * (16 * BITS), m0);
+    }
   }
-  if (threadIdx.x >= kRows && threadIdx.x < 2 * kRows && m0 + (int)threadIdx.x - kRows < p.out_features) {
-    const size_t g0 = (size_t)(m0 + threadIdx.x - kRows) * p.groups_per_row + group0;
-    const char* sp = reinterpret_cast<const char*>(p.s16 + g0);
-    const char* zp = static_cast<const char*>(p.zq) + g0 * (zf ? 2 : 1);
+  if (threadIdx.x >= kRows && threadIdx.x < 2 * kRows && weight_row((int)threadIdx.x - kRows) < p.out_features) {
+    const int rr = (int)threadIdx.x - kRows;
+    const size_t g0 = (size_t)weight_row(rr) * p.groups_per_row + group0;
+    const char* sp = reinterpret_cast<const char*>(step_sizes(rr) + g0);
+    const char* zp = static_cast<const char*>(zero_points(rr)) + g0 * (zf ? 2 : 1);
     const int sb = 2 * ngroups, zb = zf ? sb : ngroups;
     for (int o = 0; o < sb; o += 128) ptx::prefetch_l2_line(sp + o);
     for (int o = 0; o < zb; o += 128) ptx::prefetch_l2_line(zp + o);
@@ -246,6 +261,7 @@ slim_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     ptx::fence_mbar_init();
     ptx::tma_prefetch_desc(&map_x);
     ptx::tma_prefetch_desc(&map_w);
+    if (GATED) ptx::tma_prefetch_desc(&map_other);
   }
   const uint32_t tmem_cols = (uint32_t)C::tmem_cols(zf);
   if (warp == 1) {
@@ -282,6 +298,7 @@ slim_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         const int run = run0 + b * kBoxRuns;
         ptx::mbar_expect_tx(full, C::kStage);              // what lies past the matrices is zero-filled and counted
         ptx::tma_load_2d(dst, &map_w, run * (16 * BITS), m0, full);
+        if (GATED) ptx::tma_load_2d(dst + kWeightRows * box_bytes(BITS), &map_other, run * (16 * BITS), m0, full);
         ptx::tma_load_3d(dst + C::kCodes, &map_x, 0, t0, run * 2, full);
         if (++st == C::kStages) { st = 0; ph ^= 1u; }
       }
@@ -339,7 +356,7 @@ slim_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
       const int items = pairs ? ngroups >> 1 : ngroups;    // per row
       int k = 0;
       while (k < 5 && (1 << k) < items) ++k;
-      const int rstep = 32 >> k, rows_live = min(kRows, p.out_features - m0);
+      const int rstep = 32 >> k;
       const int steps = ((kRows / rstep) + C::kRowWarps - 1) / C::kRowWarps;
       constexpr int kBatch = 8;                            // items in flight per lane
       uint32_t all_z = 0u;
@@ -350,15 +367,15 @@ slim_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
           for (int i = 0; i < kBatch; ++i) {
             const int rr = ((i0 + i) * C::kRowWarps + warp - 2) * rstep + (lane >> k);
             vs[i] = vz[i] = 0u;
-            if (rr < rows_live) {
-              const size_t gi = (size_t)(m0 + rr) * p.groups_per_row + group0 + (pairs ? 2 * c : c);
-              const eqat_fp16* z16 = static_cast<const eqat_fp16*>(p.zq) + gi;
-              const uint8_t* z8 = static_cast<const uint8_t*>(p.zq) + gi;
+            if (rr < kRows && weight_row(rr) < p.out_features) {
+              const size_t gi = (size_t)weight_row(rr) * p.groups_per_row + group0 + (pairs ? 2 * c : c);
+              const eqat_fp16* z16 = static_cast<const eqat_fp16*>(zero_points(rr)) + gi;
+              const uint8_t* z8 = static_cast<const uint8_t*>(zero_points(rr)) + gi;
               if (pairs) {
-                vs[i] = ptx::ld_global(reinterpret_cast<const uint32_t*>(p.s16 + gi));
+                vs[i] = ptx::ld_global(reinterpret_cast<const uint32_t*>(step_sizes(rr) + gi));
                 vz[i] = zf ? ptx::ld_global(reinterpret_cast<const uint32_t*>(z16)) : (uint32_t)ptx::ld_global(reinterpret_cast<const unsigned short*>(z8));
               } else {
-                vs[i] = (uint32_t)ptx::ld_global(p.s16 + gi);
+                vs[i] = (uint32_t)ptx::ld_global(step_sizes(rr) + gi);
                 vz[i] = zf ? (uint32_t)ptx::ld_global(z16) : (uint32_t)ptx::ld_global(z8);
               }
             }
@@ -503,7 +520,20 @@ slim_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 #pragma unroll
         for (int i = 0; i < 2 * kGroups; ++i) { v.x += u[i].x; v.y += u[i].y; v.z += u[i].z; v.w += u[i].w; }
       }
-      if (m0 + 4 * lane < p.out_features)
+      if constexpr (GATED) {                               // lanes 16 .. 31 have the other projection of lanes 0 .. 15
+        const int row = m0 + 4 * (lane & 15);
+        const size_t at = (size_t)(t0 + rank * slice + c) * p.out_features + row;
+        const uint2 o = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+        if (p.other.gate_out != nullptr && row < p.out_features)
+          *reinterpret_cast<uint2*>((lane < 16 ? p.other.gate_out : p.other.other_out) + at) = o;
+        EQAT_WITH_ACTIVATION(p.other.activation, if (lane < 16) v = make_float4(activate<kAct>(v.x), activate<kAct>(v.y), activate<kAct>(v.z), activate<kAct>(v.w)));
+        v.x *= __shfl_down_sync(0xFFFFFFFFu, v.x, 16);
+        v.y *= __shfl_down_sync(0xFFFFFFFFu, v.y, 16);
+        v.z *= __shfl_down_sync(0xFFFFFFFFu, v.z, 16);
+        v.w *= __shfl_down_sync(0xFFFFFFFFu, v.w, 16);
+        if (lane < 16 && row < p.out_features)
+          *reinterpret_cast<uint2*>(p.Y + at) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+      } else if (m0 + 4 * lane < p.out_features)
         *reinterpret_cast<uint2*>(p.Y + (size_t)(t0 + rank * slice + c) * p.out_features + m0 + 4 * lane) =
             make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
     }
@@ -519,20 +549,24 @@ slim_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   }
 }
 
-template <int BITS, int NT, int ND>
+template <int BITS, int NT, int ND, bool GATED>
 int launch_one(const SlimParams& p, const eqat_bf16* X, dim3 ctas, int groups, cudaStream_t st) {
   using C = Slim<BITS, NT, ND>;
-  auto kern = slim_fwd_kernel<BITS, NT, ND>;
+  auto kern = slim_fwd_kernel<BITS, NT, ND, GATED>;
   static SmemOptIn opt_in;
   const bool zf = p.z_fp16 != 0;
   const int smem = C::smem_bytes(zf, groups);
   if (smem > kMaxSmem) return EQAT_ERR_UNSUPPORTED;        // not reached for a problem slim_fwd_applies() accepted
   if (!opt_in.ensure(kern, kMaxSmem)) return EQAT_ERR_CUDA;
-  CUtensorMap mx, mw;
+  CUtensorMap mx, mw, mo;
   if (!make_tmap_blocks_bf16(&mx, X, (uint64_t)p.in_features, (uint64_t)p.T, C::kTn, 2 * kBoxRuns)) return EQAT_ERR_CUDA;
   const uint64_t row_bytes = (uint64_t)p.in_features * BITS / 8;
-  if (!make_tmap_u8(&mw, p.Wq, row_bytes, (uint64_t)p.out_features, box_bytes(BITS), kRows, BITS == 3 ? 0 : box_bytes(BITS)))
-    return EQAT_ERR_CUDA;
+  auto codes_map = [&](CUtensorMap* m, const uint8_t* Wq) {
+    return make_tmap_u8(m, Wq, row_bytes, (uint64_t)p.out_features, box_bytes(BITS), GATED ? kRows / 2 : kRows, BITS == 3 ? 0 : box_bytes(BITS));
+  };
+  if (!codes_map(&mw, p.Wq)) return EQAT_ERR_CUDA;
+  if (!GATED) mo = mw;
+  else if (!codes_map(&mo, p.other.Wq)) return EQAT_ERR_CUDA;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = ctas;
   cfg.blockDim = dim3(C::kThreads, 1, 1);
@@ -548,7 +582,7 @@ int launch_one(const SlimParams& p, const eqat_bf16* X, dim3 ctas, int groups, c
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  if (cudaLaunchKernelEx(&cfg, kern, mx, mw, p) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&cfg, kern, mx, mw, mo, p) != cudaSuccess) {
     (void)cudaGetLastError();
     return EQAT_ERR_CUDA;
   }
@@ -615,17 +649,17 @@ SlimPlan slim_plan(const eqat_desc& d, int sms) {
   return best;
 }
 
-template <int BITS>
+template <int BITS, bool GATED>
 int launch_bits(const SlimPlan& pl, const SlimParams& p, const eqat_bf16* X, dim3 ctas, cudaStream_t st) {
   switch (pl.nd * 8 + pl.nt) {
-    case 4 * 8 + 1: return launch_one<BITS, 1, 4>(p, X, ctas, pl.groups, st);
-    case 2 * 8 + 1: return launch_one<BITS, 1, 2>(p, X, ctas, pl.groups, st);
-    case 2 * 8 + 2: return launch_one<BITS, 2, 2>(p, X, ctas, pl.groups, st);
-    case 2 * 8 + 3: return launch_one<BITS, 3, 2>(p, X, ctas, pl.groups, st);
-    case 1 * 8 + 1: return launch_one<BITS, 1, 1>(p, X, ctas, pl.groups, st);
-    case 1 * 8 + 2: return launch_one<BITS, 2, 1>(p, X, ctas, pl.groups, st);
-    case 1 * 8 + 3: return launch_one<BITS, 3, 1>(p, X, ctas, pl.groups, st);
-    default: return launch_one<BITS, 4, 1>(p, X, ctas, pl.groups, st);
+    case 4 * 8 + 1: return launch_one<BITS, 1, 4, GATED>(p, X, ctas, pl.groups, st);
+    case 2 * 8 + 1: return launch_one<BITS, 1, 2, GATED>(p, X, ctas, pl.groups, st);
+    case 2 * 8 + 2: return launch_one<BITS, 2, 2, GATED>(p, X, ctas, pl.groups, st);
+    case 2 * 8 + 3: return launch_one<BITS, 3, 2, GATED>(p, X, ctas, pl.groups, st);
+    case 1 * 8 + 1: return launch_one<BITS, 1, 1, GATED>(p, X, ctas, pl.groups, st);
+    case 1 * 8 + 2: return launch_one<BITS, 2, 1, GATED>(p, X, ctas, pl.groups, st);
+    case 1 * 8 + 3: return launch_one<BITS, 3, 1, GATED>(p, X, ctas, pl.groups, st);
+    default: return launch_one<BITS, 4, 1, GATED>(p, X, ctas, pl.groups, st);
   }
 }
 
@@ -647,21 +681,38 @@ bool slim_fwd_applies(const eqat_desc& d, int sms, SlimPlan& pl) {
   return gemv.launches > 1 || pl.us * 1.25 < gemv.us;
 }
 
-int launch_slim_fwd(const eqat_desc& d, const eqat_bf16* X, const uint8_t* Wq, const eqat_fp16* s16, const void* zq,
-                    eqat_bf16* Y, const SlimPlan& pl, cudaStream_t st) {
+namespace {
+
+template <bool GATED>
+int launch_slim(const eqat_desc& d, const eqat_bf16* X, const eqat_packed_weight& w, const OtherWeight& other, eqat_bf16* Y,
+                const SlimPlan& pl, cudaStream_t st) {
   SlimParams p{};
-  set_weight(p, d, Wq, s16, zq);
+  set_weight(p, d, w.Wq_packed, w.s16, w.z);
+  p.other = other;
   p.Y = Y;
   p.T = (int)d.tokens;
   p.split = pl.split;
   p.split_log2 = log2_exact(pl.split);
   p.runs = d.in_features / kRun;
-  const dim3 ctas((unsigned)((d.out_features + kRows - 1) / kRows), (unsigned)pl.split, (unsigned)pl.token_tiles);
+  const int rows = GATED ? kRows / 2 : kRows;
+  const dim3 ctas((unsigned)((d.out_features + rows - 1) / rows), (unsigned)pl.split, (unsigned)pl.token_tiles);
   switch (d.bits) {
-    case 2: return launch_bits<2>(pl, p, X, ctas, st);
-    case 3: return launch_bits<3>(pl, p, X, ctas, st);
-    default: return launch_bits<4>(pl, p, X, ctas, st);
+    case 2: return launch_bits<2, GATED>(pl, p, X, ctas, st);
+    case 3: return launch_bits<3, GATED>(pl, p, X, ctas, st);
+    default: return launch_bits<4, GATED>(pl, p, X, ctas, st);
   }
+}
+
+}  // namespace
+
+int launch_slim_fwd(const eqat_desc& d, const eqat_bf16* X, const uint8_t* Wq, const eqat_fp16* s16, const void* zq,
+                    eqat_bf16* Y, const SlimPlan& pl, cudaStream_t st) {
+  return launch_slim<false>(d, X, eqat_packed_weight{Wq, s16, zq}, OtherWeight{}, Y, pl, st);
+}
+
+int launch_slim_gated(const eqat_desc& d, int activation, const eqat_bf16* X, const eqat_packed_weight& gate,
+                      const eqat_packed_weight& up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, const SlimPlan& pl, cudaStream_t st) {
+  return launch_slim<true>(d, X, gate, other_weight(up, activation, G, U), H, pl, st);
 }
 
 int launch_wait_expiry_slim(cudaStream_t st) { return launch_wait_expiry(st); }

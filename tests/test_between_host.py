@@ -140,10 +140,9 @@ def test_gated_arguments(eqat):
 def test_packed_gated_arguments(eqat):
     W = eqat.eqat_packed_weight
     good, desc = W(A, A, A), eqat.make_desc(2, 64, 128, 256, 5)
-    ws = eqat.packed_gated_workspace_bytes(desc)
 
-    def fwd(d=desc, act=0, X=A, gate=good, up=good, H=A, G=A, U=A, w=A, n=ws):
-        return eqat.lib.qlinear_packed_gated_fwd(d and ctypes.byref(d), act, X, gate and ctypes.byref(gate), up and ctypes.byref(up), H, G, U, w, n, None)
+    def fwd(d=desc, act=0, X=A, gate=good, up=good, H=A, G=A, U=A):
+        return eqat.lib.qlinear_packed_gated_fwd(d and ctypes.byref(d), act, X, gate and ctypes.byref(gate), up and ctypes.byref(up), H, G, U, None)
 
     def bwd(d=desc, act=0, dH=A, G=A, U=A, gate=good, up=good, dX=A, dG=A, dU=A):
         return eqat.lib.qlinear_packed_gated_bwd(d and ctypes.byref(d), act, dH, G, U, gate and ctypes.byref(gate), up and ctypes.byref(up), dX, dG, dU, None)
@@ -162,22 +161,6 @@ def test_packed_gated_arguments(eqat):
         for d, status in ((eqat.make_desc(5, 64, 128, 256, 5), -4), (eqat.make_desc(2, 64, 96, 256, 5), -2), (eqat.make_desc(2, 64, 128, 200, 5), -2),
                           (eqat.make_desc(2, 64, 128, 256, 0), -2), (eqat.make_desc(2, 512, 128, 1024, 5), -4)):
             assert call(d=d) == status
-    with pytest.raises(eqat.EqatError):
-        eqat.packed_gated_workspace_bytes(eqat.make_desc(2, 64, 96, 256, 5))
-
-
-def test_a_workspace_is_needed_where_the_projections_pass_through_memory(eqat):
-    """Checked before any launch, and so without a device."""
-    W = eqat.eqat_packed_weight(A, A, A)
-    for T in (1, 37, 300, 5000):
-        d = eqat.make_desc(3, 64, 4160, 4096, T)
-        if eqat.eqat_packed_gated_route(d) != eqat.EQAT_GATED_COMPOSED:
-            assert eqat.packed_gated_workspace_bytes(d) == 0
-            continue
-        need = eqat.packed_gated_workspace_bytes(d)
-        assert need >= 2 * T * 4160 * 2 and need % 512 == 0
-        for ws in ((None, need), (A, need - 1), (A + 128, need)):
-            assert eqat.lib.qlinear_packed_gated_fwd(ctypes.byref(d), 0, A, ctypes.byref(W), ctypes.byref(W), A, None, None, *ws, None) == eqat.EQAT_ERR_WORKSPACE
 
 
 def test_tensors_are_checked_before_the_call(eqat):
@@ -251,17 +234,6 @@ def test_turns_of_any_frequency(eqat):
 def test_scalings_that_are_none(eqat, kw):
     with pytest.raises(eqat.EqatError):
         eqat.rotary_turns(**{"rotary_dim": 64, **kw})
-
-
-# ---------------------------------------------------------------------------------------------- how a gated call is divided
-def test_gated_routes(eqat):
-    """Large batches are one kernel; a batch keeps its kernel's kind between neighbouring sizes."""
-    for bits in (2, 3, 4):
-        for out, width in ((11008, 4096), (28672, 8192), (256, 256)):
-            routes = [eqat.eqat_packed_gated_route(eqat.make_desc(bits, 64, out, width, T), 148) for T in (1, 8, 40, 200, 1000, 4096, 20000)]
-            assert set(routes) <= {eqat.EQAT_GATED_COMPOSED, eqat.EQAT_GATED_TILED, eqat.EQAT_GATED_MATRIX_VECTOR}
-            assert out == 256 or routes[-2:] == [eqat.EQAT_GATED_TILED] * 2
-    assert eqat.lib.eqat_packed_gated_route(ctypes.byref(eqat.make_desc(2, 64, 256, 256, 4)), -1) == eqat.EQAT_ERR_SHAPE
 
 
 # ---------------------------------------------------------------------------------------------- the oracle's gradients

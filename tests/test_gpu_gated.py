@@ -129,6 +129,8 @@ def forward_cases():
     yield (1, 11008, 4096, 2, 64, False, "silu")
     yield (7, 4096, 5120, 3, 128, False, "gelu")
     yield (3, 2048, 11008, 4, 128, True, "silu")
+    yield from ((T, 11008, 4096, 3, 128, False, "silu") for T in (37, 64, 100, 333))     # rows of either kernel split over clusters
+    yield from ((T, 5120, 1024, b, 64, z, "gelu") for T, b, z in ((12, 2, False), (16, 4, True), (48, 3, False), (70, 4, False), (200, 2, True)))
 
 
 @pytest.mark.parametrize("T,out,width,bits,group,fp16,kind", list(forward_cases()))
@@ -136,11 +138,10 @@ def test_packed_forward(eqat, T, out, width, bits, group, fp16, kind):
     gate, up = both_weights(out, width, bits, group, fp16)
     X, buf = normal(T, width, seed=3), Guarded()
     d = eqat.make_desc(bits, group, out, width, T, 0, eqat.EQAT_ZP_FP16 if fp16 else eqat.EQAT_ZP_U8)
-    need = eqat.packed_gated_workspace_bytes(d)
     H, G, U, H2 = (buf.empty(T, out, dtype=torch.bfloat16, shift_bytes=16 * i) for i in range(4))
     act = act_code(eqat, kind)
     eqat.qlinear_packed_gated_fwd(d, act, X, gate.on, up.on, H, G, U)
-    eqat.qlinear_packed_gated_fwd(d, act, X, gate.on, up.on, H2, None, None, buf.empty(need, dtype=torch.uint8) if need else None)
+    eqat.qlinear_packed_gated_fwd(d, act, X, gate.on, up.on, H2)
     buf.check()
     assert eqat.device_status() == (0, 0)
     assert torch.equal(H, H2)
@@ -176,6 +177,36 @@ def test_packed_backward(eqat, T, out, width, bits, group, fp16, kind):
     assert torch.equal(G2, dG) and torch.equal(U2, dU) and torch.equal(dX2, dX)
 
 
+@pytest.mark.parametrize("T", [1, 6, 20, 300])
+def test_zero_points_of_eight_bits(eqat, T):
+    """Bytes past 127, which no hand-off produces, in one weight or the other."""
+    out, width, rng = 192, 1280, np.random.default_rng(9)
+    for which in (0, 1):
+        pair = both_weights(out, width, 4, 128, False)
+        z = rng.integers(100, 256, (out, width // 128)).astype(np.uint8)
+        w = pair[which]
+        q = O.unpack_rows(w.on[0].cpu().numpy(), 4, width)
+        w.value = O.dequantize(q, w.on[1].cpu().numpy().astype(np.float32) * 2.0 ** -4, z, 128)
+        w.on = (w.on[0], (w.on[1].float() * 2.0 ** -4).half(), torch.from_numpy(z).cuda())
+        X, d = normal(T, width, seed=10, std=0.1), eqat.make_desc(4, 128, out, width, T)
+        H, G, U = (torch.empty(T, out, dtype=torch.bfloat16, device="cuda") for _ in range(3))
+        eqat.qlinear_packed_gated_fwd(d, eqat.EQAT_ACT_SILU, X, pair[0].on, pair[1].on, H, G, U)
+        for got, weight in ((G, pair[0]), (U, pair[1])):
+            want, room = projected(torch_to_f64(X), weight.value)
+            assert_elementwise(torch_to_f64(got), want, room, which)
+
+
+def test_same_bits_as_one_projection_at_a_time(eqat):
+    """G and U are those of qlinear_packed_fwd where the same kernel takes both (single tokens), and H that of the unrounded sums."""
+    gate, up = both_weights(512, 1024, 2, 64, False)
+    X, d = normal(1, 1024, seed=11), eqat.make_desc(2, 64, 512, 1024, 1)
+    H, G, U, Y = (torch.empty(1, 512, dtype=torch.bfloat16, device="cuda") for _ in range(4))
+    eqat.qlinear_packed_gated_fwd(d, eqat.EQAT_ACT_SILU, X, gate.on, up.on, H, G, U)
+    for got, w in ((G, gate), (U, up)):
+        eqat.qlinear_packed_fwd(d, X, *w.on, Y)
+        assert torch.equal(got, Y)
+
+
 def test_the_weights_are_not_mixed_up(eqat):
     """A gate of ones and an up weight of twos, and the other way round: H = act(n) 2n against act(2n) n."""
     out, width = 128, 128
@@ -185,10 +216,8 @@ def test_the_weights_are_not_mixed_up(eqat):
         codes = [torch.full((out, width // 4), v * 0x55, dtype=torch.uint8, device="cuda") for v in (1, 2)]
         s, z = torch.ones(out, 2, dtype=torch.float16, device="cuda"), torch.zeros(out, 2, dtype=torch.uint8, device="cuda")
         H = torch.empty(T, out, dtype=torch.bfloat16, device="cuda")
-        need = eqat.packed_gated_workspace_bytes(d)
-        ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
         for a, b in ((1, 2), (2, 1)):
-            eqat.qlinear_packed_gated_fwd(d, eqat.EQAT_ACT_SILU, X, (codes[a - 1], s, z), (codes[b - 1], s, z), H, None, None, ws)
+            eqat.qlinear_packed_gated_fwd(d, eqat.EQAT_ACT_SILU, X, (codes[a - 1], s, z), (codes[b - 1], s, z), H)
             want = float(B.activation(float(a), "silu")[0]) * b
             assert (H.double() - want).abs().max() <= 2.0 ** -7 * want
 
@@ -198,10 +227,8 @@ def test_captured_on_another_stream(eqat):
     gate, up = both_weights(out, width, 2, 64, False)
     for T in (1, 24, 1500):
         d = eqat.make_desc(2, 64, out, width, T)
-        need = eqat.packed_gated_workspace_bytes(d)
-        ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
         X, H = normal(T, width, seed=7), torch.empty(T, out, dtype=torch.bfloat16, device="cuda")
-        call = lambda: eqat.qlinear_packed_gated_fwd(d, eqat.EQAT_ACT_GELU, X, gate.on, up.on, H, None, None, ws)  # noqa: E731
+        call = lambda: eqat.qlinear_packed_gated_fwd(d, eqat.EQAT_ACT_GELU, X, gate.on, up.on, H)  # noqa: E731
         call()
         torch.cuda.synchronize()
         g, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
