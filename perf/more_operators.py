@@ -380,13 +380,10 @@ def _plan(s):
     from paper_2407_11062_b200 import binding as eqat
     c = s["case"]
 
-    def scratch(need):
-        return torch.empty(need, dtype=torch.uint8, device=DEV) if need else None
-
     if c["op"] == "norm":
         kind = {"": eqat.EQAT_CODES_NONE, "int8": eqat.EQAT_CODES_INT8, "e4m3": eqat.EQAT_CODES_E4M3}[c["codes"]]
         desc = eqat.make_norm_desc(c["rows"], c["features"], 1e-5, kind, c["group"])
-        return eqat, desc, scratch(eqat.rms_norm_workspace_bytes(desc)) if c["backward"] else None
+        return eqat, desc, torch.empty(eqat.rms_norm_workspace_bytes(desc), dtype=torch.uint8, device=DEV) if c["backward"] else None
     if c["op"] == "rotary":
         p = _scaling(c)
         kind = {"plain": eqat.EQAT_ROTARY_PLAIN, "linear": eqat.EQAT_ROTARY_LINEAR, "base": eqat.EQAT_ROTARY_BASE,
@@ -401,7 +398,7 @@ def _plan(s):
         return eqat, eqat.make_gated_desc(c["rows"], c["features"], act), None
     zeros = eqat.EQAT_ZP_U8 if c["zeros"] == "u8" else eqat.EQAT_ZP_FP16
     desc = eqat.make_desc(c["bits"], c["group"], c["inner"], c["width"], c["tokens"], 0, zeros)
-    return eqat, desc, (act, scratch(eqat.packed_gated_workspace_bytes(desc)) if not c["backward"] and not c["keep"] else None)
+    return eqat, desc, act
 
 
 def _call(s):
@@ -424,11 +421,10 @@ def _call(s):
             return [s["dG"], s["dU"]]
         eqat.eqat_gated_fwd(desc, s["G"], s["U"], s["H"])
         return s["H"]
-    act, scratch = more
     if c["backward"]:
-        eqat.qlinear_packed_gated_bwd(desc, act, s["dH"], s["G"], s["U"], s["gate"], s["up"], s["dX"], s["dG"], s["dU"])
+        eqat.qlinear_packed_gated_bwd(desc, more, s["dH"], s["G"], s["U"], s["gate"], s["up"], s["dX"], s["dG"], s["dU"])
         return [s["dX"], s["dG"], s["dU"]]
-    eqat.qlinear_packed_gated_fwd(desc, act, s["X"], s["gate"], s["up"], s["H"], s["G"], s["U"], scratch)
+    eqat.qlinear_packed_gated_fwd(desc, more, s["X"], s["gate"], s["up"], s["H"], s["G"], s["U"])
     return [s["H"], s["G"], s["U"]] if c["keep"] else s["H"]
 
 
