@@ -599,16 +599,29 @@ typedef struct {              /* a weight as qlinear_packed_fwd takes it: device
 
 /* Both projections of a feed-forward block and their product, the weights packed:
  *     G = X * W_gate^T,   U = X * W_up^T,   H = act(G) * U
- * for two weights of one descriptor (out_features of each), in one pass over both:
- * the kernels of qlinear_packed_fwd, with tiles that hold both projections of their
- * features.  G and U leave them only if they are wanted (for the backward pass), and
- * H is that of the sums before they are rounded.  The kernel is the one that
- * qlinear_packed_fwd takes for a weight of 2*out_features rows (eqat_packed_fwd_route);
- * what is said there of how weights enter the products, and of bits, holds for it.
+ * for two weights of one descriptor (out_features of each).  The kernel is the one
+ * that qlinear_packed_fwd takes for a weight of 2*out_features rows, with tiles that
+ * hold both projections of their features: one pass over both weights, in which G
+ * and U leave the kernel only if they are wanted (for the backward pass), and H is
+ * that of the sums before they are rounded.  The exception are prompts for which that
+ * kernel is EQAT_ROUTE_WEIGHT_ROW_PAIRS (eqat_packed_gated_route): two calls of
+ * qlinear_packed_fwd and one of eqat_gated_fwd, through G and U or, where these are
+ * NULL, through the workspace; H is then that of G and U as they are rounded.  What
+ * is said of qlinear_packed_fwd, of how weights enter the products and of bits, holds.
  *   X [T,in] bf16, gate, up (in)   H [T,out] bf16 (out)
  *   G, U [T,out] bf16 (out): both, or both NULL */
 int qlinear_packed_gated_fwd(const eqat_desc* desc, int activation, const eqat_bf16* X, const eqat_packed_weight* gate,
-                             const eqat_packed_weight* up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, void* stream);
+                             const eqat_packed_weight* up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Bytes of scratch the call needs on the current device without G and U, 256-byte
+ * aligned (0 if none, (size_t)-1 if the descriptor is invalid).  Calls that may
+ * overlap need a workspace each. */
+size_t eqat_packed_gated_workspace_bytes(const eqat_desc* desc);
+
+/* The kernel that decides how the call goes out, EQAT_ROUTE_* (a diagnostic); `sms`
+ * as in eqat_packed_fwd_route. */
+int eqat_packed_gated_route(const eqat_desc* desc, int sms);
 
 /* dG and dU as in eqat_gated_bwd, and
  *     dX = dG * W_gate + dU * W_up

@@ -135,7 +135,9 @@ def _load():
         "eqat_rotary_bwd": (c_int, rotary),
         "eqat_gated_fwd": (c_int, [G, P, c_int64, P, c_int64, P, P]),
         "eqat_gated_bwd": (c_int, [G, P, P, c_int64, P, c_int64, P, c_int64, P, c_int64, P]),
-        "qlinear_packed_gated_fwd": (c_int, [D, c_int, P, W, W, P, P, P, P]),
+        "eqat_packed_gated_workspace_bytes": (c_size_t, [D]),
+        "eqat_packed_gated_route": (c_int, [D, c_int]),
+        "qlinear_packed_gated_fwd": (c_int, [D, c_int, P, W, W, P, P, P, P, c_size_t, P]),
         "qlinear_packed_gated_bwd": (c_int, [D, c_int, P, P, P, W, W, P, P, P, P]),
         "eqat_block_ap_step": (c_int, [POINTER(eqat_block_ap_linear), c_int, POINTER(c_int), P]),
         "eqat_e2e_qp_step": (c_int, [POINTER(eqat_e2e_qp_linear), c_int, POINTER(c_int), P]),
@@ -436,10 +438,25 @@ def eqat_gated_bwd(desc, dH, G, U, dG, dU):
     _check((_marshal or _load_marshal()).gated_bwd(desc, dH, G, U, dG, dU), "eqat_gated_bwd")
 
 
+def packed_gated_workspace_bytes(desc) -> int:
+    n = lib.eqat_packed_gated_workspace_bytes(ctypes.byref(desc))
+    if n == ctypes.c_size_t(-1).value:
+        raise EqatError(EQAT_ERR_SHAPE, "eqat_packed_gated_workspace_bytes")
+    return int(n)
+
+
+def eqat_packed_gated_route(desc, sms=0) -> int:
+    """The kernel that decides how qlinear_packed_gated_fwd goes out (EQAT_ROUTE_*)."""
+    route = lib.eqat_packed_gated_route(ctypes.byref(desc), int(sms))
+    if route < 0:
+        raise EqatError(route, "eqat_packed_gated_route")
+    return route
+
+
 # A weight: (Wq_packed, s16, z).
-def qlinear_packed_gated_fwd(desc, activation, X, gate, up, H, G=None, U=None):
-    """G, U: the projections, for the backward pass (or None)."""
-    _check((_marshal or _load_marshal()).packed_gated_fwd(desc, activation, X, gate, up, H, G, U), "qlinear_packed_gated_fwd")
+def qlinear_packed_gated_fwd(desc, activation, X, gate, up, H, G=None, U=None, workspace=None):
+    """G, U: the projections, for the backward pass (or None); workspace: packed_gated_workspace_bytes, without them."""
+    _check((_marshal or _load_marshal()).packed_gated_fwd(desc, activation, X, gate, up, H, G, U, workspace), "qlinear_packed_gated_fwd")
 
 
 def qlinear_packed_gated_bwd(desc, activation, dH, G, U, gate, up, dX, dG, dU):

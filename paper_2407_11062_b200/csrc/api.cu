@@ -226,11 +226,21 @@ PackedRoute packed_route(const eqat_desc& d, int sms) {
   return r;
 }
 
-// A gated feed-forward block's two weights as one with the rows of both, which decides the kernel.
-eqat_desc both_weights(const eqat_desc& d) {
-  eqat_desc both = d;
-  both.out_features = 2 * d.out_features;
-  return both;
+// How a gated feed-forward block's projections are taken: the kernel of a weight with the rows of both, except that prompts of
+// the kernel on pairs of weight-row tiles go through memory, one weight after the other.
+struct GatedRoute {
+  eqat_desc both;
+  PackedRoute packed;
+  bool composed() const { return packed.kernel == EQAT_ROUTE_WEIGHT_ROW_PAIRS; }
+  // one projection in the workspace
+  size_t bytes() const { return ((size_t)both.tokens * (both.out_features / 2) * sizeof(eqat_bf16) + 255) & ~(size_t)255; }
+};
+// (Without a device, as on one of 148 SMs.)
+GatedRoute gated_route(const eqat_desc& d, int sms) {
+  GatedRoute r{d, {}};
+  r.both.out_features = 2 * d.out_features;
+  r.packed = packed_route(r.both, sms == 0 && sm_count() <= 0 ? 148 : sms);
+  return r;
 }
 
 int check_gated_weights(const eqat_desc* d, int activation, const eqat_packed_weight* gate, const eqat_packed_weight* up) {
@@ -603,21 +613,44 @@ int eqat_gated_bwd(const eqat_gated_desc* d, const eqat_bf16* dH, const eqat_bf1
   return launch_gated_bwd(*d, dH, G, g_pitch, U, u_pitch, dG, dg_pitch, dU, du_pitch, as_stream(stream));
 }
 
+size_t eqat_packed_gated_workspace_bytes(const eqat_desc* d) {
+  if (check_gemm_desc(d, true) != EQAT_OK || d->out_features > 1 << 29) return (size_t)-1;
+  const GatedRoute r = gated_route(*d, 0);
+  return r.composed() ? 2 * r.bytes() : 0;
+}
+
+int eqat_packed_gated_route(const eqat_desc* d, int sms) {
+  EQAT_TRY(check_gemm_desc(d, true));
+  if (sms < 0 || d->out_features > 1 << 29) return EQAT_ERR_SHAPE;
+  return gated_route(*d, sms).packed.kernel;
+}
+
 int qlinear_packed_gated_fwd(const eqat_desc* d, int activation, const eqat_bf16* X, const eqat_packed_weight* gate,
-                             const eqat_packed_weight* up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, void* stream) {
+                             const eqat_packed_weight* up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, void* workspace,
+                             size_t workspace_bytes, void* stream) {
   EQAT_TRY(check_gated_weights(d, activation, gate, up));
   EQAT_TRY(check_ptrs(X, H));
   if ((G == nullptr) != (U == nullptr)) return EQAT_ERR_NULL;
   if (!aligned16(G) || !aligned16(U)) return EQAT_ERR_ALIGN;
-  const eqat_desc both = both_weights(*d);
-  const PackedRoute r = packed_route(both, 0);
+  const GatedRoute r = gated_route(*d, 0);
   cudaStream_t st = as_stream(stream);
-  switch (r.kernel) {
-    case EQAT_ROUTE_WEIGHT_ROWS: return launch_slim_gated(*d, activation, X, *gate, *up, H, G, U, r.slim, st);
-    case EQAT_ROUTE_MATRIX_VECTOR: return launch_gemv_gated(*d, both, activation, X, *gate, *up, H, G, U, st);
-    case EQAT_ROUTE_WEIGHT_ROW_PAIRS: return launch_wide_gated(*d, activation, X, *gate, *up, H, G, U, r.wide, st);
-    default: return launch_packed_gated(*d, activation, X, *gate, *up, H, G, U, st);
+  if (!r.composed()) {
+    switch (r.packed.kernel) {
+      case EQAT_ROUTE_WEIGHT_ROWS: return launch_slim_gated(*d, activation, X, *gate, *up, H, G, U, r.packed.slim, st);
+      case EQAT_ROUTE_MATRIX_VECTOR: return launch_gemv_gated(*d, r.both, activation, X, *gate, *up, H, G, U, st);
+      default: return launch_packed_gated(*d, activation, X, *gate, *up, H, G, U, st);
+    }
   }
+  if (G == nullptr) {
+    if (workspace == nullptr || workspace_bytes < 2 * r.bytes() || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+      return EQAT_ERR_WORKSPACE;
+    G = static_cast<eqat_bf16*>(workspace);
+    U = reinterpret_cast<eqat_bf16*>(static_cast<uint8_t*>(workspace) + r.bytes());
+  }
+  EQAT_TRY(qlinear_packed_fwd(d, X, gate->Wq_packed, gate->s16, gate->z, G, stream));
+  EQAT_TRY(qlinear_packed_fwd(d, X, up->Wq_packed, up->s16, up->z, U, stream));
+  const eqat_gated_desc g{d->tokens, d->out_features, activation};
+  return launch_gated_fwd(g, G, d->out_features, U, d->out_features, H, st);
 }
 
 int qlinear_packed_gated_bwd(const eqat_desc* d, int activation, const eqat_bf16* dH, const eqat_bf16* G, const eqat_bf16* U,

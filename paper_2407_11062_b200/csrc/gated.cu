@@ -18,6 +18,7 @@ struct GatedParams {
   int64_t g_pitch, u_pitch, dg_pitch, du_pitch;      // in vectors of 8
   int64_t total;                                     // vectors in all
   int vecs;                                          // of a row
+  int row_step, col_step;                            // what a step of the grid is
 };
 
 __device__ __forceinline__ void unpack(const uint4& v, float (&f)[8]) {
@@ -36,9 +37,14 @@ template <int ACT, bool BACKWARD>
 __global__ void __launch_bounds__(kThreads) gated_kernel(const GatedParams p) {
   ptx::grid_dependency_wait();
   const int64_t step = (int64_t)gridDim.x * kThreads;
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < p.total; i += step) {
-    const int64_t row = i / p.vecs;
-    const int col = (int)(i - row * p.vecs);
+  int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  int64_t row = i / p.vecs;
+  int col = (int)(i - row * p.vecs);
+  for (; i < p.total; i += step, row += p.row_step, col += p.col_step) {
+    if (col >= p.vecs) {
+      col -= p.vecs;
+      ++row;
+    }
     float g[8], u[8];
     unpack(ptx::ld_global_once(reinterpret_cast<const uint4*>(p.G) + row * p.g_pitch + col), g);
     unpack(ptx::ld_global_once(reinterpret_cast<const uint4*>(p.U) + row * p.u_pitch + col), u);
@@ -71,6 +77,9 @@ int launch_gated(const eqat_gated_desc& d, GatedParams p, cudaStream_t st) {
   p.total = d.rows * p.vecs;
   const int64_t need = (p.total + kThreads - 1) / kThreads, most = (int64_t)sms * 8;
   const dim3 grid((unsigned)(need < most ? need : most));
+  const int step = (int)grid.x * kThreads;
+  p.row_step = step / p.vecs;
+  p.col_step = step % p.vecs;
   EQAT_WITH_ACTIVATION(d.activation, return launch_overlapped(gated_kernel<kAct, BACKWARD>, grid, dim3(kThreads), 0, st, p));
   return EQAT_ERR_UNSUPPORTED;
 }

@@ -310,7 +310,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       }
     } else if constexpr (GATED) {
       // Columns c and BN/2 + c of the accumulator are the two projections of one feature.  The projections go out first, where
-      // they are wanted: read from tensor memory once more, they need not be held beside the product.
+      // they are wanted: read from tensor memory once more, they need not be held beside the product.  (All
+      // sixteen expansion warps on the epilogue, in two sets of columns, were 1 % slower: 4096 tokens, 7B, 2 bits, 630 and 638 us.)
       if (!accumulators()) return false;
 #pragma unroll 1
       for (int c = 0; c < kColumns / 32; ++c) {

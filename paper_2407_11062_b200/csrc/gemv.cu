@@ -68,10 +68,12 @@ namespace {
 // task go through a double-buffered shared array to a reducer warp, which adds
 // them in a fixed order and stores Y while the consumers are on the next task.
 //
-// A gated feed-forward block's two projections (GATED): a task is 8 rows of the
-// gate's weight and the same 8 of the other's, a box two copies of 8 rows.  Lane
-// (g, q) then holds row g of either weight, and the reducer, which has both sums
-// of a feature, stores their product.
+// A gated feed-forward block's two projections (GATED): a task is 16 rows of the
+// gate's weight and the same 16 of the other's.  The first half of a stage's boxes
+// and of the warps are the gate's, the second half the other's, over the same
+// columns; the reducer, which has both sums of a feature, stores their product.
+// (Boxes of 8 rows of either weight, twice as many copies of half the size, took
+// 17.9 us where this takes 15.3: one token of 11008 x 4096, 2 bits.)
 constexpr int kTcMaxTokens = 8;                         // the instruction has eight token columns
 constexpr int kTcMaxTotalTokens = 64;                   // up to here a plan is made, for comparison (see packed_gemv_applies)
 constexpr int kTcWarps = 16;
@@ -227,12 +229,13 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
   TcCtl* ctl = reinterpret_cast<TcCtl*>(ring + L.ctl_off);
   volatile int* abort_flag = &ctl->abort;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int kWeightRows = GATED ? kTcRows / 2 : kTcRows;       // of a weight per task
-  const int n_tasks = out_features / kWeightRows;
+  constexpr int kWeightBoxes = GATED ? kBoxesPerStage / 2 : kBoxesPerStage;     // of a weight per stage
+  constexpr int kWeightWarps = GATED ? kTcWarps / 2 : kTcWarps;
+  const int n_tasks = out_features / kTcRows;
   const int chunks = in_features >> 6;
   const int row_bytes = in_features * BITS / 8;
   const int n_boxes = (row_bytes + kTcBoxBytes - 1) / kTcBoxBytes;
-  const int task_stages = (n_boxes + kBoxesPerStage - 1) / kBoxesPerStage;
+  const int task_stages = (n_boxes + kWeightBoxes - 1) / kWeightBoxes;
   const int chunks_pad = n_boxes * kChunksPerBox;
 
   // Launched with programmatic stream serialisation: the next launch of the stream may start as soon as every
@@ -279,45 +282,42 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
   // Zero points: one byte per slot in z_lo.x / z_hi.x, or (ZF16) one fp16 value per slot like the step sizes.
   struct StageParams { uint2 s_lo, s_hi, z_lo, z_hi; };
   constexpr int kSlotShift = PARAM_MODE == 2 ? 1 : (PARAM_MODE == 3 ? 2 : 0);
+  if (GATED && warp >= kWeightWarps && warp < kTcWarps) { s16 = other.s16; zq = other.zq; }      // this warp's weight
   const uint8_t* const z8 = static_cast<const uint8_t*>(zq);
   const eqat_fp16* const z16 = static_cast<const eqat_fp16*>(zq);
-  // of the lane's second row: eight rows further, or (GATED) the same row of the other weight
-  const eqat_fp16* const s16_hi = GATED ? other.s16 : s16;
-  const uint8_t* const z8_hi = GATED ? static_cast<const uint8_t*>(other.zq) : z8;
-  const eqat_fp16* const z16_hi = GATED ? static_cast<const eqat_fp16*>(other.zq) : z16;
   auto fetch = [&](int task, int k) {
     StageParams sp;
     sp.s_lo = sp.s_hi = sp.z_lo = sp.z_hi = make_uint2(0u, 0u);
-    const int cg0 = (k * kBoxesPerStage + box) * kChunksPerBox + chunk0;
+    const int cg0 = (k * kWeightBoxes + box % kWeightBoxes) * kChunksPerBox + chunk0;
     if (task < n_tasks && cg0 < chunks) {
-      const size_t p_lo = (size_t)(task * kWeightRows + g) * groups_per_row, p_hi = p_lo + (GATED ? 0 : (size_t)8 * groups_per_row);
+      const size_t p_lo = (size_t)(task * kTcRows + g) * groups_per_row, p_hi = p_lo + (size_t)8 * groups_per_row;
       if constexpr (PARAM_MODE == 1) {                    // the row has a multiple of four groups: all four exist
         sp.s_lo = ptx::ld_global(reinterpret_cast<const uint2*>(s16 + p_lo + cg0));
-        sp.s_hi = ptx::ld_global(reinterpret_cast<const uint2*>(s16_hi + p_hi + cg0));
+        sp.s_hi = ptx::ld_global(reinterpret_cast<const uint2*>(s16 + p_hi + cg0));
         if constexpr (ZF16) {
           sp.z_lo = ptx::ld_global(reinterpret_cast<const uint2*>(z16 + p_lo + cg0));
-          sp.z_hi = ptx::ld_global(reinterpret_cast<const uint2*>(z16_hi + p_hi + cg0));
+          sp.z_hi = ptx::ld_global(reinterpret_cast<const uint2*>(z16 + p_hi + cg0));
         } else {
           sp.z_lo.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(z8 + p_lo + cg0));
-          sp.z_hi.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(z8_hi + p_hi + cg0));
+          sp.z_hi.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(z8 + p_hi + cg0));
         }
       } else if constexpr (PARAM_MODE == 2) {             // an even number of groups per row: both exist
         const int g0 = cg0 >> 1;
         sp.s_lo.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(s16 + p_lo + g0));
-        sp.s_hi.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(s16_hi + p_hi + g0));
+        sp.s_hi.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(s16 + p_hi + g0));
         if constexpr (ZF16) {
           sp.z_lo.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(z16 + p_lo + g0));
-          sp.z_hi.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(z16_hi + p_hi + g0));
+          sp.z_hi.x = ptx::ld_global(reinterpret_cast<const uint32_t*>(z16 + p_hi + g0));
         } else {
           sp.z_lo.x = ptx::ld_global(reinterpret_cast<const uint16_t*>(z8 + p_lo + g0));
-          sp.z_hi.x = ptx::ld_global(reinterpret_cast<const uint16_t*>(z8_hi + p_hi + g0));
+          sp.z_hi.x = ptx::ld_global(reinterpret_cast<const uint16_t*>(z8 + p_hi + g0));
         }
       } else if constexpr (PARAM_MODE == 3) {
         const int grp = (cg0 << 6) >> group_shift;
         sp.s_lo.x = ptx::ld_global(s16 + p_lo + grp);
-        sp.s_hi.x = ptx::ld_global(s16_hi + p_hi + grp);
+        sp.s_hi.x = ptx::ld_global(s16 + p_hi + grp);
         sp.z_lo.x = ZF16 ? (uint32_t)ptx::ld_global(z16 + p_lo + grp) : (uint32_t)ptx::ld_global(z8 + p_lo + grp);
-        sp.z_hi.x = ZF16 ? (uint32_t)ptx::ld_global(z16_hi + p_hi + grp) : (uint32_t)ptx::ld_global(z8_hi + p_hi + grp);
+        sp.z_hi.x = ZF16 ? (uint32_t)ptx::ld_global(z16 + p_hi + grp) : (uint32_t)ptx::ld_global(z8 + p_hi + grp);
       } else {
         uint32_t sl[4] = {0u, 0u, 0u, 0u}, sh[4] = {0u, 0u, 0u, 0u}, zl[4] = {0u, 0u, 0u, 0u}, zh[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
@@ -325,9 +325,9 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
           if (cg0 + c < chunks) {
             const int grp = ((cg0 + c) << 6) >> group_shift;
             sl[c] = ptx::ld_global(s16 + p_lo + grp);
-            sh[c] = ptx::ld_global(s16_hi + p_hi + grp);
+            sh[c] = ptx::ld_global(s16 + p_hi + grp);
             zl[c] = ZF16 ? (uint32_t)ptx::ld_global(z16 + p_lo + grp) : (uint32_t)ptx::ld_global(z8 + p_lo + grp);
-            zh[c] = ZF16 ? (uint32_t)ptx::ld_global(z16_hi + p_hi + grp) : (uint32_t)ptx::ld_global(z8_hi + p_hi + grp);
+            zh[c] = ZF16 ? (uint32_t)ptx::ld_global(z16 + p_hi + grp) : (uint32_t)ptx::ld_global(z8 + p_hi + grp);
           }
         }
         sp.s_lo = make_uint2(sl[0] | (sl[1] << 16), sl[2] | (sl[3] << 16));
@@ -372,14 +372,14 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             break;
           }
           ptx::fence_proxy_async_smem();                            // consumers' reads of this stage before the copies' writes
-          const int nb = min(kBoxesPerStage, n_boxes - k * kBoxesPerStage);
+          const int nb = min(kWeightBoxes, n_boxes - k * kWeightBoxes);
           const uint32_t full = ptx::smem_addr(&ctl->full[slot]);
-          ptx::mbar_expect_tx(full, (uint32_t)nb * kTcBoxSmem);     // bytes past the end of a row are zero-filled and counted
+          ptx::mbar_expect_tx(full, (uint32_t)((GATED ? 2 : 1) * nb) * kTcBoxSmem);     // bytes past the end of a row are zero-filled and counted
           for (int b = 0; b < nb; ++b) {
             const uint32_t dst = ring_addr + slot * kStageBytes + b * kTcBoxSmem;
-            const int col = (k * kBoxesPerStage + b) * kTcBoxBytes;
-            ptx::tma_load_2d(dst, &map_w, col, task * kWeightRows, full);
-            if (GATED) ptx::tma_load_2d(dst + kWeightRows * kTcBoxBytes, &map_other, col, task * kWeightRows, full);
+            const int col = (k * kWeightBoxes + b) * kTcBoxBytes;
+            ptx::tma_load_2d(dst, &map_w, col, task * kTcRows, full);
+            if (GATED) ptx::tma_load_2d(dst + kWeightBoxes * kTcBoxSmem, &map_other, col, task * kTcRows, full);
           }
           ++issued;
           if (++slot == stages) { slot = 0; phase ^= 1u; }
@@ -411,15 +411,15 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     // task is one stage and this warp sets the pace.
     constexpr int kZAhead = 2;                             // 16-byte pieces per lane: rows of up to 64 groups
     uint4 z_next[kZAhead];
-    // a task's bytes are contiguous: groups_per_row pieces, or (GATED) as many halves of one of each weight
+    // a task's bytes are contiguous: groups_per_row pieces (GATED: of both weights, as one)
     auto z_piece = [&](int task, int i) {
       const size_t at = (size_t)task * groups_per_row + i;
+      uint4 v = ptx::ld_global(static_cast<const uint4*>(zq) + at);
       if constexpr (GATED) {
-        const uint2 a = ptx::ld_global(static_cast<const uint2*>(zq) + at), b = ptx::ld_global(static_cast<const uint2*>(other.zq) + at);
-        return make_uint4(a.x, a.y, b.x, b.y);
-      } else {
-        return ptx::ld_global(static_cast<const uint4*>(zq) + at);
+        const uint4 u = ptx::ld_global(static_cast<const uint4*>(other.zq) + at);
+        v = make_uint4(v.x | u.x, v.y | u.y, v.z | u.z, v.w | u.w);
       }
+      return v;
     };
     auto z_fetch = [&](int task) {
 #pragma unroll
@@ -428,11 +428,8 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         if (task < n_tasks && lane + 32 * i < groups_per_row) z_next[i] = z_piece(task, lane + 32 * i);
       }
     };
-    auto eighth_bits = [&](int task, int r, int n) {       // -128 s xs over the groups of a row whose zero point has it
-      const bool second = GATED && r >= kWeightRows;
-      const int row = task * kWeightRows + (second ? r - kWeightRows : r);
-      const uint8_t* const z8 = static_cast<const uint8_t*>(second ? other.zq : zq);
-      const eqat_fp16* const steps = second ? other.s16 : s16;
+    // -128 s xs over the groups of a row whose zero point has it
+    auto eighth_bits = [&](const uint8_t* z8, const eqat_fp16* s16, int row, int n) {
       float v = 0.0f;
 #pragma unroll 1
       for (int cg = 0; cg < chunks; ++cg) {
@@ -442,7 +439,7 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         const uint2* item = xb + ((size_t)cg * 4 * T + n) * kTcItems + 4;
         const uint32_t p0 = item[0].y, p12 = item[(size_t)T * kTcItems].x;
         const float xs = (__uint_as_float(p0 & 0xFFFF0000u) + __uint_as_float(p12 << 16)) + __uint_as_float(p12 & 0xFFFF0000u);
-        v = fmaf(-128.0f * __half2float(__ushort_as_half(ptx::ld_global(steps + grp))), xs, v);
+        v = fmaf(-128.0f * __half2float(__ushort_as_half(ptx::ld_global(s16 + grp))), xs, v);
       }
       return v;
     };
@@ -463,36 +460,31 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
 #pragma unroll 1
         for (int idx = lane; idx < kTcRows * T; idx += 32) {
           const int r = idx & (kTcRows - 1), n = idx >> 4;
-          part[(buf * kTcWarps * kTcRows + r) * kTcMaxTokens + n] += eighth_bits(task, r, n);
+          float* const at = part + (buf * kTcWarps * kTcRows + r) * kTcMaxTokens + n;
+          at[0] += eighth_bits(z8, s16, task * kTcRows + r, n);
+          if constexpr (GATED)
+            at[kWeightWarps * kTcRows * kTcMaxTokens] += eighth_bits(static_cast<const uint8_t*>(other.zq), other.s16, task * kTcRows + r, n);
         }
       }
-      if constexpr (GATED) {
-        for (int idx = lane; idx < kWeightRows * T; idx += 32) {
-          const int r = idx & (kWeightRows - 1), n = idx >> 3;
-          float v = 0.0f, u = 0.0f;
+      for (int idx = lane; idx < kTcRows * T; idx += 32) {
+        const int r = idx & (kTcRows - 1), n = idx >> 4;
+        float v = 0.0f;
 #pragma unroll
-          for (int wv = 0; wv < kTcWarps; ++wv) {
-            const float* at = part + ((buf * kTcWarps + wv) * kTcRows + r) * kTcMaxTokens + n;
-            v += at[0];
-            u += at[kWeightRows * kTcMaxTokens];
-          }
-          const size_t at = (size_t)n * out_features + (size_t)task * kWeightRows + r;
+        for (int wv = 0; wv < kWeightWarps; ++wv)          // fixed order: deterministic
+          v += part[((buf * kTcWarps + wv) * kTcRows + r) * kTcMaxTokens + n];
+        const size_t at = (size_t)n * out_features + (size_t)task * kTcRows + r;
+        if constexpr (GATED) {
+          float u = 0.0f;
+#pragma unroll
+          for (int wv = kWeightWarps; wv < kTcWarps; ++wv) u += part[((buf * kTcWarps + wv) * kTcRows + r) * kTcMaxTokens + n];
           if (other.gate_out != nullptr) {
             other.gate_out[at] = (eqat_bf16)(pack_bf16x2(v, 0.0f) & 0xFFFFu);
             other.other_out[at] = (eqat_bf16)(pack_bf16x2(u, 0.0f) & 0xFFFFu);
           }
           EQAT_WITH_ACTIVATION(other.activation, v = activate<kAct>(v));
-          Y[at] = (eqat_bf16)(pack_bf16x2(v * u, 0.0f) & 0xFFFFu);
+          v *= u;
         }
-      } else {
-        for (int idx = lane; idx < kTcRows * T; idx += 32) {
-          const int r = idx & (kTcRows - 1), n = idx >> 4;
-          float v = 0.0f;
-#pragma unroll
-          for (int wv = 0; wv < kTcWarps; ++wv)            // fixed order: deterministic
-            v += part[((buf * kTcWarps + wv) * kTcRows + r) * kTcMaxTokens + n];
-          Y[(size_t)n * out_features + (size_t)task * kTcRows + r] = (eqat_bf16)(pack_bf16x2(v, 0.0f) & 0xFFFFu);
-        }
+        Y[at] = (eqat_bf16)(pack_bf16x2(v, 0.0f) & 0xFFFFu);
       }
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&ctl->part_free[buf]));
@@ -579,7 +571,7 @@ packed_gemv_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     for (int task = blockIdx.x; task < n_tasks && alive; task += gridDim.x) {
       float tot[4] = {0.0f, 0.0f, 0.0f, 0.0f};                         // rows g, g + 8 x tokens 2q, 2q + 1
       for (int k = 0; k < task_stages; ++k) {
-        const int gbox = k * kBoxesPerStage + box;
+        const int gbox = k * kWeightBoxes + box % kWeightBoxes;
         const bool have = gbox < n_boxes;
         const StageParams sp = nx[0];
 #pragma unroll
@@ -703,18 +695,17 @@ int launch_tc_mode(const eqat_desc& d, const eqat_bf16* X, const eqat_packed_wei
                    eqat_bf16* Y, int group_shift, int stages, cudaStream_t st) {
   static SmemOptIn opt_in;
   if (!opt_in.ensure(packed_gemv_tc_kernel<BITS, PARAM_MODE, ZF16, GATED>, (int)kTcSmemBudget)) return EQAT_ERR_CUDA;
-  constexpr int kWeightRows = GATED ? kTcRows / 2 : kTcRows;
   CUtensorMap mw, mo;
   const uint64_t row_bytes = (uint64_t)d.in_features * BITS / 8;
   auto codes_map = [&](CUtensorMap* m, const uint8_t* Wq) {
-    return make_tmap_u8(m, Wq, row_bytes, (uint64_t)d.out_features, tc_box_bytes(BITS), kWeightRows, BITS == 3 ? 0 : 128);
+    return make_tmap_u8(m, Wq, row_bytes, (uint64_t)d.out_features, tc_box_bytes(BITS), kTcRows, BITS == 3 ? 0 : 128);
   };
   if (!codes_map(&mw, w.Wq_packed)) return EQAT_ERR_CUDA;
   if (!GATED) mo = mw;
   else if (!codes_map(&mo, other.Wq)) return EQAT_ERR_CUDA;
   const int sms = sm_count();
   if (sms <= 0) return EQAT_ERR_CUDA;
-  const int T = (int)d.tokens, n_tasks = d.out_features / kWeightRows, ng = d.in_features / d.group;
+  const int T = (int)d.tokens, n_tasks = d.out_features / kTcRows, ng = d.in_features / d.group;
   const TcLayout L = tc_layout(T, d.in_features, stages, BITS);
   // Programmatic stream serialisation: back-to-back launches of this kernel overlap the tail of one grid with the
   // CTA start-up of the next (the kernel waits for its predecessors before its first global access).  After a

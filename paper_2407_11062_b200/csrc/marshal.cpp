@@ -349,16 +349,18 @@ int number(PyObject* o) {
   return v < 0 || v > 1000 ? -1 : (int)v;              // no activation either way
 }
 
-// desc, activation, X, gate, up, H, G, U
+// desc, activation, X, gate, up, H, G, U, workspace
 PyObject* packed_gated_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return call(n, 8, [&] {
+  return call(n, 9, [&] {
     const auto d = structure<eqat_desc>(a[0]);
     const int act = number(a[1]);
     const double inner = (double)d.tokens * d.out_features;
     const auto* X = dense(a[2], (double)d.tokens * d.in_features);
     const eqat_packed_weight gate = weight_of(a[3], d), up = weight_of(a[4], d);
     auto *H = dense(a[5], inner), *G = dense(a[6], inner), *U = dense(a[7], inner);
-    return launch([&](void* s) { return g_packed_gated_fwd(&d, act, X, &gate, &up, H, G, U, s); });
+    size_t bytes = 0;
+    void* ws = bytes_of(a[8], &bytes);
+    return launch([&](void* s) { return g_packed_gated_fwd(&d, act, X, &gate, &up, H, G, U, ws, bytes, s); });
   });
 }
 

@@ -3,9 +3,11 @@
 //     h = bf16(x + r),  c = (mean(h^2) + eps)^(-1/2),  y = h w c
 //     dx = dr + c (v - h c^2 mean(v h)),  v = dy w;     dw = sum over the rows of dy h c
 //
-// One pass: a row's threads keep it in registers between the sum over it and the output, so each tensor crosses HBM once: 8
-// bytes an element forward with a residual (7 + 4/group with codes in place of y), 8 backward.  A thread owns the same
-// columns of every row it meets, so w is read once a block and dw is added up in registers.
+// One pass: each tensor crosses HBM once, 8 bytes an element forward with a residual (7 + 4/group with codes in place of y), 8
+// backward.  A thread owns the same columns of every row it meets, so w is read once a block and dw is added up in registers.
+// What a thread will read of the next rows it copies into shared memory itself (cp.async, up to two rows ahead): nobody else
+// reads its places, so a row costs no barrier but that of the sum, and the copies run on through it.  A block with a single
+// row loads into registers.
 #include <cuda_fp8.h>
 
 #include "between.cuh"
@@ -17,6 +19,7 @@ namespace {
 
 constexpr int kBlock = 256;                          // threads of a block that gives each row to a warp
 constexpr int kMaxThreads = 512;                     // of a block that shares a row
+constexpr int kRingBytes = 200 * 1024;               // shared memory of an SM for the blocks' rings
 constexpr float kSmallGroup = 0x1p-110f;             // 127 / a and 448 / a are finite above
 
 __device__ __forceinline__ void unpack(const uint4& v, float (&f)[8]) {
@@ -26,6 +29,12 @@ __device__ __forceinline__ void unpack(const uint4& v, float (&f)[8]) {
     f[2 * i] = __uint_as_float(w[i] << 16);
     f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
   }
+}
+// The sum rounded to bf16 once; rounding to binary32 on the way would not change it (operands of 8 bits whose exponents differ by
+// more than 16 are nowhere near half a step).
+__device__ __forceinline__ uint32_t add_pair(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 s = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&s);
 }
 __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
   return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
@@ -58,6 +67,17 @@ __device__ __forceinline__ Reduced reduce_row(Reduced x, Reduced (*red)[32], int
   return x;
 }
 
+__device__ __forceinline__ void copy_16(uint32_t dst, const uint4* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// All copies but those of the last stages - 1 groups have arrived.
+__device__ __forceinline__ void copies_arrived(int stages) {
+  if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+  else if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+  else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+
 struct NormFwd {
   const eqat_bf16 *X, *R, *W;
   eqat_bf16 *H, *Y;
@@ -69,52 +89,92 @@ struct NormFwd {
 };
 
 // VPT vectors of a row per thread.  A row belongs to a warp (WARP) or to the block.
-template <int VPT, bool WARP, int CODES>
-__global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(const NormFwd p) {
+template <int VPT, bool WARP, int CODES, bool RING>
+__global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(const NormFwd p, int stages) {
   __shared__ Reduced red[2][32];
+  extern __shared__ __align__(16) uint8_t ring[];
   const int lane = threadIdx.x & 31;
   const int at = WARP ? lane : (int)threadIdx.x, span = WARP ? 32 : (int)blockDim.x;
   const int step = (int)gridDim.x * (WARP ? kBlock / 32 : 1);
+  const int first = WARP ? (int)blockIdx.x * (kBlock / 32) + (int)(threadIdx.x >> 5) : (int)blockIdx.x;
   constexpr float kTop = CODES == EQAT_CODES_INT8 ? 127.0f : 448.0f;
+  const bool residual = p.R != nullptr;
+  const uint32_t mine = ptx::smem_addr(ring) + threadIdx.x * 16, pitch = blockDim.x * 16;      // of this thread; to its next vector
+  const uint32_t stage_bytes = pitch * VPT * (residual ? 2 : 1);
   ptx::grid_dependency_wait();
+  auto ask = [&](int row, int stage) {
+    if (row < p.rows) {
+      const size_t base = (size_t)row * p.vecs + at;
+      uint32_t dst = mine + stage * stage_bytes;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i, dst += pitch)
+        if (at + i * span < p.vecs) copy_16(dst, reinterpret_cast<const uint4*>(p.X) + base + i * span);
+      if (residual) {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i, dst += pitch)
+          if (at + i * span < p.vecs) copy_16(dst, reinterpret_cast<const uint4*>(p.R) + base + i * span);
+      }
+    }
+    copies_issued();
+  };
+  int ahead = first, fill = 0;                       // the row asked for next, and its stage
+  if (RING) {
+    for (int k = 0; k + 1 < stages; ++k, ahead += step) ask(ahead, fill++);
+  }
   uint4 w[VPT];
 #pragma unroll
   for (int i = 0; i < VPT; ++i)
     w[i] = at + i * span < p.vecs ? ptx::ld_global(reinterpret_cast<const uint4*>(p.W) + at + i * span) : make_uint4(0u, 0u, 0u, 0u);
-  int turn = 0;
-  for (int row = WARP ? (int)blockIdx.x * (kBlock / 32) + (int)(threadIdx.x >> 5) : (int)blockIdx.x; row < p.rows; row += step, ++turn) {
+  int turn = 0, stage = 0;
+  for (int row = first; row < p.rows; row += step, ++turn) {
     if (row >= p.rows - step) ptx::grid_dependents_launch();
     const size_t base = (size_t)row * p.vecs + at;
     uint4 x[VPT], r[VPT];
+    if (RING) {
+      ask(ahead, fill);
+      ahead += step;
+      if (++fill == stages) fill = 0;
+      copies_arrived(stages);
+    }
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       x[i] = r[i] = make_uint4(0u, 0u, 0u, 0u);
       if (at + i * span < p.vecs) {
-        x[i] = ptx::ld_global_once(reinterpret_cast<const uint4*>(p.X) + base + i * span);
-        if (p.R != nullptr) r[i] = ptx::ld_global_once(reinterpret_cast<const uint4*>(p.R) + base + i * span);
+        if (RING) {
+          x[i] = ptx::lds_128(mine + stage * stage_bytes + i * pitch);
+          if (residual) r[i] = ptx::lds_128(mine + stage * stage_bytes + (VPT + i) * pitch);
+        } else {
+          x[i] = ptx::ld_global_once(reinterpret_cast<const uint4*>(p.X) + base + i * span);
+          if (residual) r[i] = ptx::ld_global_once(reinterpret_cast<const uint4*>(p.R) + base + i * span);
+        }
       }
     }
+    if (RING && ++stage == stages) stage = 0;
+    // With codes, the products of up to two vectors a thread are held through the sum, more are formed again.
+    constexpr int kHeld = VPT < 2 ? 1 : 2;
+    float t[kHeld][8], most[VPT];
     Reduced s{0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
+      if (residual) x[i] = make_uint4(add_pair(x[i].x, r[i].x), add_pair(x[i].y, r[i].y), add_pair(x[i].z, r[i].z), add_pair(x[i].w, r[i].w));
       float h[8], g[8];
       unpack(x[i], h);
-      if (p.R != nullptr) {
-        unpack(r[i], g);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] += g[e];
-        x[i] = pack(h);
-        if (p.H != nullptr && at + i * span < p.vecs) reinterpret_cast<uint4*>(p.H)[base + i * span] = x[i];
-        unpack(x[i], h);
-      } else if (p.H != nullptr && p.H != p.X && at + i * span < p.vecs) {
-        reinterpret_cast<uint4*>(p.H)[base + i * span] = x[i];
-      }
+      if (p.H != nullptr && (residual || p.H != p.X) && at + i * span < p.vecs) reinterpret_cast<uint4*>(p.H)[base + i * span] = x[i];
 #pragma unroll
       for (int e = 0; e < 8; ++e) s.a = fmaf(h[e], h[e], s.a);
-      if (CODES != EQAT_CODES_NONE && p.lanes == 0) {
+      if constexpr (CODES != EQAT_CODES_NONE) {
         unpack(w[i], g);
+        most[i] = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s.most = fmaxf(s.most, fabsf(h[e] * g[e]));
+        for (int e = 0; e < 8; ++e) {
+          t[i % kHeld][e] = h[e] * g[e];
+          most[i] = fmaxf(most[i], fabsf(t[i % kHeld][e]));
+        }
+        if (p.lanes == 0) {
+          s.most = fmaxf(s.most, most[i]);
+        } else {
+          for (int d = 1; d < p.lanes; d <<= 1) most[i] = fmaxf(most[i], __shfl_xor_sync(0xFFFFFFFFu, most[i], d));
+        }
       }
     }
     s = reduce_row<WARP>(s, red, turn);
@@ -122,42 +182,51 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(c
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const bool live = at + i * span < p.vecs;
-      float h[8], g[8];
-      unpack(x[i], h);
-      unpack(w[i], g);
+      float (&h)[8] = t[i % kHeld];
+      if (CODES == EQAT_CODES_NONE || VPT > kHeld) {
+        float g[8];
+        unpack(x[i], h);
+        unpack(w[i], g);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) h[e] *= g[e];
+        for (int e = 0; e < 8; ++e) h[e] *= g[e];
+      }
       if constexpr (CODES == EQAT_CODES_NONE) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) h[e] *= c;
         if (live) reinterpret_cast<uint4*>(p.Y)[base + i * span] = pack(h);
       } else {
-        float most = s.most;
-        if (p.lanes != 0) {
-          most = 0.0f;
+        float a = p.lanes == 0 ? s.most : most[i];
+        if (a < kSmallGroup) a = 0.0f;
+        const float up = a > 0.0f ? __fdiv_rn(kTop, a) : 0.0f;
+        const float scale = a * c * (1.0f / kTop);
+        uint32_t q[2];
+        if constexpr (CODES == EQAT_CODES_INT8) {
+          // |t| is at most 127 (1 + 2^-23), so the low byte of t + 1.5 2^23 is the code
+          uint32_t k[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(h[e]));
-          for (int d = 1; d < p.lanes; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
-        }
-        if (most < kSmallGroup) most = 0.0f;
-        const float up = most > 0.0f ? __fdiv_rn(kTop, most) : 0.0f;
-        const float scale = most * c * (1.0f / kTop);
-        uint32_t q[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float t = __fmul_rn(h[e], up);
-          if constexpr (CODES == EQAT_CODES_INT8) {
-            const int k = min(max(__float2int_rn(t), -127), 127);
-            q[e] = (uint32_t)k & 0xFFu;
-            h[e] = (float)k * scale;
-          } else {
-            q[e] = __nv_cvt_float_to_fp8(t, __NV_SATFINITE, __NV_E4M3);
-            h[e] = __half2float(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)q[e], __NV_E4M3)) * scale;
+          for (int e = 0; e < 8; ++e) {
+            const float v = __fadd_rn(__fmul_rn(h[e], up), 12582912.0f);
+            k[e] = __float_as_uint(v);
+            h[e] = (v - 12582912.0f) * scale;
           }
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            q[j] = __byte_perm(__byte_perm(k[4 * j], k[4 * j + 1], 0x0040), __byte_perm(k[4 * j + 2], k[4 * j + 3], 0x0040), 0x5410);
+        } else {
+          uint32_t k[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            k[e] = __nv_cvt_float2_to_fp8x2(make_float2(__fmul_rn(h[2 * e], up), __fmul_rn(h[2 * e + 1], up)), __NV_SATFINITE, __NV_E4M3);
+            const __half2_raw v = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)k[e], __NV_E4M3);
+            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&v));
+            h[2 * e] = y.x * scale;
+            h[2 * e + 1] = y.y * scale;
+          }
+          q[0] = k[0] | (k[1] << 16);
+          q[1] = k[2] | (k[3] << 16);
         }
         if (live) {
-          reinterpret_cast<uint2*>(p.codes)[base + i * span] = make_uint2(q[0] | (q[1] << 8) | (q[2] << 16) | (q[3] << 24),
-                                                                           q[4] | (q[5] << 8) | (q[6] << 16) | (q[7] << 24));
+          reinterpret_cast<uint2*>(p.codes)[base + i * span] = make_uint2(q[0], q[1]);
           if (p.Y != nullptr) reinterpret_cast<uint4*>(p.Y)[base + i * span] = pack(h);
           if (p.lanes == 0) {
             if (at == 0 && i == 0) p.scales[row] = scale;
@@ -178,14 +247,39 @@ struct NormBwd {
   float eps, inverse_n;
 };
 
+// `stages` of the ring, then (WARP) the warps' sums, [warps][features], in the same places.
 template <int VPT, bool WARP>
-__global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_bwd_kernel(const NormBwd p) {
+__global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_bwd_kernel(const NormBwd p, int stages) {
   __shared__ Reduced red[2][32];
-  extern __shared__ float share[];                   // WARP: [warps][features]
+  extern __shared__ __align__(16) uint8_t ring[];
+  float* const share = reinterpret_cast<float*>(ring);
+  constexpr int kHeld = VPT < 2 ? 1 : 2;
   const int lane = threadIdx.x & 31;
   const int at = WARP ? lane : (int)threadIdx.x, span = WARP ? 32 : (int)blockDim.x;
   const int step = (int)gridDim.x * (WARP ? kBlock / 32 : 1);
+  const int first = WARP ? (int)blockIdx.x * (kBlock / 32) + (int)(threadIdx.x >> 5) : (int)blockIdx.x;
+  const bool residual = p.dR != nullptr;
+  const uint32_t mine = ptx::smem_addr(ring) + threadIdx.x * 16, pitch = blockDim.x * 16;
+  const uint32_t stage_bytes = pitch * VPT * (residual ? 3 : 2);
   ptx::grid_dependency_wait();
+  auto ask = [&](int row, int stage) {
+    if (row < p.rows) {
+      const size_t base = (size_t)row * p.vecs + at;
+      uint32_t dst = mine + stage * stage_bytes;
+#pragma unroll
+      for (int t = 0; t < 3; ++t) {
+        const eqat_bf16* src = t == 0 ? p.H : t == 1 ? p.dY : p.dR;
+        if (t < 2 || residual) {
+#pragma unroll
+          for (int i = 0; i < VPT; ++i, dst += pitch)
+            if (at + i * span < p.vecs) copy_16(dst, reinterpret_cast<const uint4*>(src) + base + i * span);
+        }
+      }
+    }
+    copies_issued();
+  };
+  int ahead = first, fill = 0;
+  for (int k = 0; k + 1 < stages; ++k, ahead += step) ask(ahead, fill++);
   uint4 w[VPT];
   float dw[VPT][8];
 #pragma unroll
@@ -194,31 +288,32 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_bwd_kernel(c
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw[i][e] = 0.0f;
   }
-  int turn = 0;
-  for (int row = WARP ? (int)blockIdx.x * (kBlock / 32) + (int)(threadIdx.x >> 5) : (int)blockIdx.x; row < p.rows; row += step, ++turn) {
+  int turn = 0, stage = 0;
+  for (int row = first; row < p.rows; row += step, ++turn) {
     if (row >= p.rows - step) ptx::grid_dependents_launch();
-    const size_t base = (size_t)row * p.vecs + at;
-    uint4 h4[VPT], y4[VPT], r4[VPT];
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      h4[i] = y4[i] = r4[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (at + i * span < p.vecs) {
-        h4[i] = ptx::ld_global_once(reinterpret_cast<const uint4*>(p.H) + base + i * span);
-        y4[i] = ptx::ld_global_once(reinterpret_cast<const uint4*>(p.dY) + base + i * span);
-        if (p.dR != nullptr) r4[i] = ptx::ld_global_once(reinterpret_cast<const uint4*>(p.dR) + base + i * span);
-      }
-    }
+    ask(ahead, fill);
+    ahead += step;
+    if (++fill == stages) fill = 0;
+    copies_arrived(stages);
+    const uint32_t slot = mine + stage * stage_bytes;
+    if (++stage == stages) stage = 0;
+    auto vector_of = [&](int tensor, int i) {
+      return at + i * span < p.vecs ? ptx::lds_128(slot + (tensor * VPT + i) * pitch) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    // Up to two vectors a thread are held through the sum as they are used after it; of more, the row is read once more.
+    float h[kHeld][8], y[kHeld][8];
     Reduced s{0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      float h[8], y[8], g[8];
-      unpack(h4[i], h);
-      unpack(y4[i], y);
+      float (&hh)[8] = h[i % kHeld], (&yy)[8] = y[i % kHeld];
+      unpack(vector_of(0, i), hh);
+      unpack(vector_of(1, i), yy);
+      float g[8];
       unpack(w[i], g);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        s.a = fmaf(h[e], h[e], s.a);
-        s.b = fmaf(y[e] * g[e], h[e], s.b);
+        s.a = fmaf(hh[e], hh[e], s.a);
+        s.b = fmaf(yy[e] * g[e], hh[e], s.b);
       }
     }
     s = reduce_row<WARP>(s, red, turn);
@@ -226,22 +321,26 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_bwd_kernel(c
     const float k = c * c * (s.b * p.inverse_n);
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      float h[8], y[8], g[8], r[8];
-      unpack(h4[i], h);
-      unpack(y4[i], y);
+      float (&hh)[8] = h[i % kHeld], (&yy)[8] = y[i % kHeld];
+      if constexpr (VPT > kHeld) {
+        unpack(vector_of(0, i), hh);
+        unpack(vector_of(1, i), yy);
+      }
+      float g[8], r[8];
       unpack(w[i], g);
-      unpack(r4[i], r);
+      unpack(residual ? vector_of(2, i) : make_uint4(0u, 0u, 0u, 0u), r);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        dw[i][e] = fmaf(y[e], h[e] * c, dw[i][e]);
-        r[e] = fmaf(c, fmaf(-h[e], k, y[e] * g[e]), r[e]);
+        dw[i][e] = fmaf(yy[e], hh[e] * c, dw[i][e]);
+        r[e] = fmaf(c, fmaf(-hh[e], k, yy[e] * g[e]), r[e]);
       }
-      if (at + i * span < p.vecs) reinterpret_cast<uint4*>(p.dX)[base + i * span] = pack(r);
+      if (at + i * span < p.vecs) reinterpret_cast<uint4*>(p.dX)[(size_t)row * p.vecs + at + i * span] = pack(r);
     }
   }
   if (p.partial == nullptr) return;
   const int features = p.vecs * 8;
   float* out = p.partial + (size_t)blockIdx.x * features;
+  if (WARP) __syncthreads();                         // the ring is done with
   if (WARP) out = share + (size_t)(threadIdx.x >> 5) * features;
 #pragma unroll
   for (int i = 0; i < VPT; ++i)
@@ -261,23 +360,25 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_bwd_kernel(c
   }
 }
 
-// dW[f] = sum of the blocks' partial sums: eight threads take an eighth of the blocks each, 32 features to a block.
-__global__ void __launch_bounds__(256) norm_dw_kernel(const float* partial, int blocks, int features, float* dW) {
-  __shared__ float part[8][33];
+// dW[f] = sum of the blocks' partial sums: 32 warps take every 32nd block each, 32 features to a block, then the first warp adds
+// the warps' sums up.
+constexpr int kSumWarps = 32;
+__global__ void __launch_bounds__(kSumWarps * 32) norm_dw_kernel(const float* partial, int blocks, int features, float* dW) {
+  __shared__ float part[kSumWarps][33];
   ptx::grid_dependency_wait();
   ptx::grid_dependents_launch();
-  const int f = (int)blockIdx.x * 32 + (threadIdx.x & 31), j = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, f = (int)blockIdx.x * 32 + lane, j = threadIdx.x >> 5;
   float v = 0.0f;
-  if (f < features)
-    for (int b = j; b < blocks; b += 8) v += ptx::ld_global(partial + (size_t)b * features + f);
-  part[j][threadIdx.x & 31] = v;
-  __syncthreads();
-  if (j == 0 && f < features) {
-    v = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v += part[i][threadIdx.x];
-    dW[f] = v;
+  if (f < features) {
+#pragma unroll 8
+    for (int b = j; b < blocks; b += kSumWarps) v += ptx::ld_global(partial + (size_t)b * features + f);
   }
+  part[j][lane] = v;
+  __syncthreads();
+  v = part[lane][j];                                 // warp j: the sums of feature j of the block's
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+  if (lane == 0 && (int)blockIdx.x * 32 + j < features) dW[blockIdx.x * 32 + j] = v;
 }
 
 // Threads of a row and vectors of each.
@@ -289,28 +390,66 @@ RowShape row_shape(int vecs) {
   return {vpt, ((vecs + vpt - 1) / vpt + 31) / 32 * 32};
 }
 
-int blocks_of(int64_t rows, int threads, int sms) {
-  const int64_t need = threads == 32 ? (rows + kBlock / 32 - 1) / (kBlock / 32) : rows;
-  const int64_t most = (int64_t)sms * (threads == 32 ? 2048 / kBlock : 2048 / threads);
-  return (int)(need < most ? need : most);
+// How a call goes out: blocks, and stages of the ring.
+struct Launch {
+  int blocks, stages;
+  size_t smem;
+};
+// `tensors` in the ring; `busy`: threads of an SM that the kernel's registers leave room for.
+Launch launch_shape(int64_t rows, const RowShape& s, int tensors, int busy, int sms) {
+  const int threads = s.threads == 32 ? kBlock : s.threads, rows_of_block = s.threads == 32 ? kBlock / 32 : 1;
+  const int stage = threads * s.vpt * tensors * 16;
+  int per_sm = busy / threads < 1 ? 1 : busy / threads;
+  // two rows ahead, if need be with fewer blocks; one row ahead where three stages do not fit an SM
+  int stages = 3;
+  while (per_sm > 1 && per_sm * stages * stage > kRingBytes) --per_sm;
+  while (stages > 1 && stages * stage > kRingBytes) --stages;
+  const int64_t need = (rows + rows_of_block - 1) / rows_of_block, most = (int64_t)sms * per_sm;
+  return {(int)(need < most ? need : most), stages, (size_t)stages * stage};
 }
-
-// The backward pass holds w's sums and three tensors in registers.
-int backward_blocks(const eqat_norm_desc& d, int sms) {
+Launch backward_shape(const eqat_norm_desc& d, int sms) {
   const RowShape s = row_shape(d.features / 8);
-  const int64_t need = s.threads == 32 ? (d.rows + kBlock / 32 - 1) / (kBlock / 32) : d.rows;
-  const int64_t most = (int64_t)sms * (s.threads == 32 ? 4 : (s.threads <= 512 ? 1024 / s.threads : 1));
-  return (int)(need < most ? need : most);
+  Launch l = launch_shape(d.rows, s, 3, 512, sms);
+  const size_t share = (size_t)(kBlock / 32) * d.features * sizeof(float);
+  if (s.threads == 32 && l.smem < share) l.smem = share;
+  return l;
 }
 
-template <int VPT, bool WARP>
-int launch_fwd(const eqat_norm_desc& d, const NormFwd& p, int threads, int sms, cudaStream_t st) {
-  const dim3 grid(blocks_of(d.rows, threads, sms)), block(WARP ? kBlock : threads);
-  switch (d.codes) {
-    case EQAT_CODES_INT8: return launch_overlapped(norm_fwd_kernel<VPT, WARP, EQAT_CODES_INT8>, grid, block, 0, st, p);
-    case EQAT_CODES_E4M3: return launch_overlapped(norm_fwd_kernel<VPT, WARP, EQAT_CODES_E4M3>, grid, block, 0, st, p);
-    default: return launch_overlapped(norm_fwd_kernel<VPT, WARP, EQAT_CODES_NONE>, grid, block, 0, st, p);
+template <typename... P, typename... A>
+int launch_with(void (*kernel)(P...), SmemOptIn& opt_in, const Launch& l, int threads, cudaStream_t st, A... args) {
+  if (l.smem > 40000 && !opt_in.ensure(kernel, kRingBytes)) return EQAT_ERR_CUDA;
+  return launch_overlapped(kernel, dim3(l.blocks), dim3(threads), l.smem, st, args...);
+}
+
+template <int VPT, bool WARP, int CODES>
+int launch_codes(const eqat_norm_desc& d, const NormFwd& p, const RowShape& s, int sms, cudaStream_t st) {
+  static SmemOptIn opt_in[2];
+  const int threads = WARP ? kBlock : s.threads;
+  Launch l = launch_shape(d.rows, s, p.R != nullptr ? 2 : 1, 1024, sms);
+  // Without codes the blocks are many and HBM sets the pace: twice as many as an SM holds, loading into registers, took 55.3 us
+  // of 8191 x 5120 (a block for each row 55.4), the ring 60.5.  With codes it is the instructions, and the copies under them
+  // are worth it: 2001 x 8192 in e4m3 31.0 and 28.1 us.
+  const int64_t need = (d.rows + (WARP ? kBlock / 32 : 1) - 1) / (WARP ? kBlock / 32 : 1), twice = (int64_t)sms * (2048 / threads);
+  if constexpr (CODES != EQAT_CODES_NONE) {
+    if (need > l.blocks) return launch_with(norm_fwd_kernel<VPT, WARP, CODES, true>, opt_in[0], l, threads, st, p, l.stages);
+  } else {
+    l.blocks = (int)(need < twice ? need : twice);
   }
+  l.smem = 0;
+  return launch_with(norm_fwd_kernel<VPT, WARP, CODES, false>, opt_in[1], l, threads, st, p, l.stages);
+}
+template <int VPT, bool WARP>
+int launch_fwd(const eqat_norm_desc& d, const NormFwd& p, const RowShape& s, int sms, cudaStream_t st) {
+  switch (d.codes) {
+    case EQAT_CODES_INT8: return launch_codes<VPT, WARP, EQAT_CODES_INT8>(d, p, s, sms, st);
+    case EQAT_CODES_E4M3: return launch_codes<VPT, WARP, EQAT_CODES_E4M3>(d, p, s, sms, st);
+    default: return launch_codes<VPT, WARP, EQAT_CODES_NONE>(d, p, s, sms, st);
+  }
+}
+template <int VPT, bool WARP>
+int launch_bwd(const NormBwd& p, const RowShape& s, const Launch& l, cudaStream_t st) {
+  static SmemOptIn opt_in;
+  return launch_with(norm_bwd_kernel<VPT, WARP>, opt_in, l, WARP ? kBlock : s.threads, st, p, l.stages);
 }
 
 }  // namespace
@@ -323,32 +462,29 @@ int launch_norm_fwd(const eqat_norm_desc& d, const eqat_bf16* X, const eqat_bf16
   const NormFwd p{X, R, W, H, Y, static_cast<uint8_t*>(codes), scales, (int)d.rows, vecs, d.eps, 1.0f / (float)d.features,
                   d.group > 0 && d.group <= 256 && d.group != d.features ? d.group / 8 : 0};
   const RowShape s = row_shape(vecs);
-  if (s.threads == 32) return s.vpt == 1 ? launch_fwd<1, true>(d, p, 32, sms, st) : launch_fwd<2, true>(d, p, 32, sms, st);
-  return s.vpt == 2   ? launch_fwd<2, false>(d, p, s.threads, sms, st)
-         : s.vpt == 4 ? launch_fwd<4, false>(d, p, s.threads, sms, st)
-                      : launch_fwd<8, false>(d, p, s.threads, sms, st);
+  if (s.threads == 32) return s.vpt == 1 ? launch_fwd<1, true>(d, p, s, sms, st) : launch_fwd<2, true>(d, p, s, sms, st);
+  return s.vpt == 2   ? launch_fwd<2, false>(d, p, s, sms, st)
+         : s.vpt == 4 ? launch_fwd<4, false>(d, p, s, sms, st)
+                      : launch_fwd<8, false>(d, p, s, sms, st);
 }
 
-size_t norm_workspace(const eqat_norm_desc& d, int sms) { return (size_t)backward_blocks(d, sms) * d.features * sizeof(float); }
+size_t norm_workspace(const eqat_norm_desc& d, int sms) { return (size_t)backward_shape(d, sms).blocks * d.features * sizeof(float); }
 
 int launch_norm_bwd(const eqat_norm_desc& d, const eqat_bf16* dY, const eqat_bf16* H, const eqat_bf16* W, const eqat_bf16* dR,
                     eqat_bf16* dX, float* dW, void* workspace, cudaStream_t st) {
   const int sms = sm_count();
   if (sms <= 0) return EQAT_ERR_CUDA;
-  const int vecs = d.features / 8, blocks = backward_blocks(d, sms);
+  const int vecs = d.features / 8;
+  const Launch l = backward_shape(d, sms);
   const NormBwd p{dY, H, W, dR, dX, dW != nullptr ? static_cast<float*>(workspace) : nullptr, (int)d.rows, vecs, d.eps,
                   1.0f / (float)d.features};
   const RowShape s = row_shape(vecs);
-  const dim3 grid(blocks);
-  const size_t share = (size_t)(kBlock / 32) * d.features * sizeof(float);
-  int rc;
-  if (s.threads == 32) rc = s.vpt == 1 ? launch_overlapped(norm_bwd_kernel<1, true>, grid, dim3(kBlock), share, st, p)
-                                       : launch_overlapped(norm_bwd_kernel<2, true>, grid, dim3(kBlock), share, st, p);
-  else rc = s.vpt == 2   ? launch_overlapped(norm_bwd_kernel<2, false>, grid, dim3(s.threads), 0, st, p)
-            : s.vpt == 4 ? launch_overlapped(norm_bwd_kernel<4, false>, grid, dim3(s.threads), 0, st, p)
-                         : launch_overlapped(norm_bwd_kernel<8, false>, grid, dim3(s.threads), 0, st, p);
+  const int rc = s.threads == 32 ? (s.vpt == 1 ? launch_bwd<1, true>(p, s, l, st) : launch_bwd<2, true>(p, s, l, st))
+                 : s.vpt == 2    ? launch_bwd<2, false>(p, s, l, st)
+                 : s.vpt == 4    ? launch_bwd<4, false>(p, s, l, st)
+                                 : launch_bwd<8, false>(p, s, l, st);
   if (rc != EQAT_OK || dW == nullptr) return rc;
-  return launch_overlapped(norm_dw_kernel, dim3((d.features + 31) / 32), dim3(256), 0, st, p.partial, blocks, d.features, dW);
+  return launch_overlapped(norm_dw_kernel, dim3((d.features + 31) / 32), dim3(kSumWarps * 32), 0, st, p.partial, l.blocks, d.features, dW);
 }
 
 }  // namespace eqat

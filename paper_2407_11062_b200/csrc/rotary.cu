@@ -4,9 +4,12 @@
 // units of 2^-64 of a turn, so the product of integers, mod 2^64, is the angle of any position without an error that grows
 // with it (in binary32 a position of 100000 would leave 2^-8 of a radian).
 //
-// 4 bytes an element cross HBM, which bounds long calls.  A block takes up to eight rows: its warps look the rows' positions
-// up, its threads compute the rows' sines and cosines into shared memory, once for all heads, and then every thread turns
-// 2 x 8 elements at a time (HALVES: a vector of each half; PAIRS: one vector).
+// 4 bytes an element cross HBM, which bounds long calls.  A thread owns one item of a row, the same in each of the block's up to
+// four rows: 2 x 8 elements of a head (HALVES: a vector of each half; PAIRS: one vector), whose places it works out once.  It
+// asks for the vectors of all its rows first; while they are on their way the block's warps look the rows' positions up, and its
+// threads compute the rows' sines and cosines into shared memory.
+#include <type_traits>
+
 #include "between.cuh"
 #include "common.cuh"
 #include "ptx.cuh"
@@ -15,11 +18,11 @@ namespace eqat {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxRows = kThreads / 32;              // rows of a block: one a warp
+constexpr int kMaxRows = 4;                          // rows of a block, all of whose vectors a thread has on their way
 
 struct RotaryParams : RotaryRows {
   int rows, sequences, q_heads, heads, head_dim, rotary_dim;
-  int block_rows, block_heads;
+  int block_rows, turned, rest;                      // rows of a block; items of a head that turn, and that are handed on
   float amplitude, sine;                             // sine: amplitude, or its negative (backward)
 };
 
@@ -50,6 +53,12 @@ __device__ __forceinline__ void halves_of(uint32_t w, float& lo, float& hi) {
   hi = __uint_as_float(w & 0xFFFF0000u);
 }
 
+template <typename T>
+__device__ __forceinline__ T load_part(const eqat_bf16* p) {
+  if constexpr (sizeof(T) == 16) return ptx::ld_global_once(reinterpret_cast<const uint4*>(p));
+  else return ptx::ld_global(p);
+}
+
 // VECTORS: 16 bytes at a time (a half of the turned part, or all of it, is whole vectors), else element by element.
 template <int LAYOUT, bool VECTORS>
 __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryParams p) {
@@ -59,8 +68,32 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryParams p) 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int pairs = p.rotary_dim >> 1;
   const int row0 = (int)blockIdx.x * p.block_rows, nrows = min(p.block_rows, p.rows - row0);
-  const int head0 = (int)blockIdx.y * p.block_heads, nheads = min(p.block_heads, p.heads - head0);
+  constexpr int kWide = VECTORS ? 8 : 1;
+  // this thread's item: the c-th of a head, turned ones first, then those handed on
+  const int item = (int)blockIdx.y * kThreads + (int)threadIdx.x, items = p.turned + p.rest;
+  int head = item / items;
+  const int c = item - head * items;
+  if (head >= p.heads) head = -1;
+  const bool query = head < p.q_heads;
+  const int64_t at = (int64_t)(query ? max(head, 0) : head - p.q_heads) * p.head_dim;
+  const int64_t src_pitch = query ? p.q_pitch : p.k_pitch, dst_pitch = query ? p.q_out_pitch : p.k_out_pitch;
+  const eqat_bf16* const src = (query ? p.q : p.k) + row0 * src_pitch + at;
+  eqat_bf16* const dst = (query ? p.q_out : p.k_out) + row0 * dst_pitch + at;
+  const bool turns = head >= 0 && c < p.turned, rests = head >= 0 && c >= p.turned && src != dst;
+  // first and (HALVES, or single elements) second part of an item that turns; place of one that is handed on
+  const int ea = !turns ? p.rotary_dim + (c - p.turned) * kWide : LAYOUT == EQAT_ROTARY_HALVES ? c * kWide : VECTORS ? c * kWide : 2 * c;
+  const int eb = LAYOUT == EQAT_ROTARY_HALVES ? ea + pairs : ea + 1;
+  constexpr bool kTwo = LAYOUT == EQAT_ROTARY_HALVES || !VECTORS;          // an item that turns has two parts
+  using Part = std::conditional_t<VECTORS, uint4, eqat_bf16>;
   ptx::grid_dependency_wait();
+  Part va[kMaxRows], vb[kTwo ? kMaxRows : 1];
+#pragma unroll
+  for (int i = 0; i < kMaxRows; ++i) {
+    const eqat_bf16* const in = src + i * src_pitch;
+    if (i < nrows && (turns || rests)) va[i] = load_part<Part>(in + ea);
+    if constexpr (kTwo)
+      if (i < nrows && turns) vb[i] = load_part<Part>(in + eb);
+  }
   if (warp < nrows) {
     int pos = 0;
     const bool live = position_of(p, row0 + warp, lane, pos);
@@ -80,64 +113,45 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryParams p) 
   }
   __syncthreads();
   ptx::grid_dependents_launch();
-
-  // items of a head: turned first, then handed on
-  constexpr int kWide = VECTORS ? 8 : 1;
-  const int turned = LAYOUT == EQAT_ROTARY_HALVES ? pairs / kWide : p.rotary_dim / (VECTORS ? 8 : 2);
-  const int rest = (p.head_dim - p.rotary_dim) / kWide, items = turned + rest;
-  const int per_row = nheads * items;
-  for (int i = threadIdx.x; i < nrows * per_row; i += kThreads) {
-    const int r = i / per_row, j = i - r * per_row;
-    const int h = j / items, c = j - h * items, head = head0 + h, row = row0 + r;
-    if (!s_live[r]) continue;
-    const bool query = head < p.q_heads;
-    const int64_t at = (int64_t)(query ? head : head - p.q_heads) * p.head_dim;
-    const eqat_bf16* src = query ? p.q + row * p.q_pitch + at : p.k + row * p.k_pitch + at;
-    eqat_bf16* dst = query ? p.q_out + row * p.q_out_pitch + at : p.k_out + row * p.k_out_pitch + at;
-    if (c >= turned) {
-      if (src != dst) {
-        const int e = p.rotary_dim + (c - turned) * kWide;
-        if constexpr (VECTORS) *reinterpret_cast<uint4*>(dst + e) = ptx::ld_global_once(reinterpret_cast<const uint4*>(src + e));
-        else dst[e] = ptx::ld_global(src + e);
-      }
-      continue;
-    }
-    const float2* turn = s_turn + r * pairs;
+#pragma unroll
+  for (int i = 0; i < kMaxRows; ++i) {
+    if (i >= nrows || !s_live[i]) continue;
+    eqat_bf16* const out = dst + i * dst_pitch;
+    if (rests) *reinterpret_cast<Part*>(out + ea) = va[i];
+    if (!turns) continue;
     if constexpr (!VECTORS) {
-      const int ia = LAYOUT == EQAT_ROTARY_HALVES ? c : 2 * c, ib = LAYOUT == EQAT_ROTARY_HALVES ? c + pairs : 2 * c + 1;
-      const float a = __uint_as_float((uint32_t)ptx::ld_global(src + ia) << 16), b = __uint_as_float((uint32_t)ptx::ld_global(src + ib) << 16);
-      const float2 t = turn[c];
+      const float a = __uint_as_float((uint32_t)va[i] << 16), b = __uint_as_float((uint32_t)vb[i] << 16);
+      const float2 t = s_turn[i * pairs + c];
       const uint32_t o = pack_bf16x2(a * t.x - b * t.y, b * t.x + a * t.y);
-      dst[ia] = (eqat_bf16)(o & 0xFFFFu);
-      dst[ib] = (eqat_bf16)(o >> 16);
-    } else if constexpr (LAYOUT == EQAT_ROTARY_HALVES) {
-      const uint4 va = ptx::ld_global_once(reinterpret_cast<const uint4*>(src) + c);
-      const uint4 vb = ptx::ld_global_once(reinterpret_cast<const uint4*>(src + pairs) + c);
-      const uint32_t wa[4] = {va.x, va.y, va.z, va.w}, wb[4] = {vb.x, vb.y, vb.z, vb.w};
-      uint32_t oa[4], ob[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float4 t = reinterpret_cast<const float4*>(turn + 8 * c)[e];
-        float a0, a1, b0, b1;
-        halves_of(wa[e], a0, a1);
-        halves_of(wb[e], b0, b1);
-        oa[e] = pack_bf16x2(a0 * t.x - b0 * t.y, a1 * t.z - b1 * t.w);
-        ob[e] = pack_bf16x2(b0 * t.x + a0 * t.y, b1 * t.z + a1 * t.w);
-      }
-      reinterpret_cast<uint4*>(dst)[c] = make_uint4(oa[0], oa[1], oa[2], oa[3]);
-      reinterpret_cast<uint4*>(dst + pairs)[c] = make_uint4(ob[0], ob[1], ob[2], ob[3]);
+      out[ea] = (eqat_bf16)(o & 0xFFFFu);
+      out[eb] = (eqat_bf16)(o >> 16);
     } else {
-      const uint4 v = ptx::ld_global_once(reinterpret_cast<const uint4*>(src) + c);
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-      uint32_t o[4];
+      const float4* turn = reinterpret_cast<const float4*>(s_turn + i * pairs + (kTwo ? ea : ea / 2));
+      const uint32_t wa[4] = {va[i].x, va[i].y, va[i].z, va[i].w};
+      uint32_t oa[4];
+      if constexpr (kTwo) {
+        const uint32_t wb[4] = {vb[i].x, vb[i].y, vb[i].z, vb[i].w};
+        uint32_t ob[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 t = turn[4 * c + e];
-        float a, b;
-        halves_of(w[e], a, b);
-        o[e] = pack_bf16x2(a * t.x - b * t.y, b * t.x + a * t.y);
+        for (int e = 0; e < 4; ++e) {
+          const float4 t = turn[e];
+          float a0, a1, b0, b1;
+          halves_of(wa[e], a0, a1);
+          halves_of(wb[e], b0, b1);
+          oa[e] = pack_bf16x2(a0 * t.x - b0 * t.y, a1 * t.z - b1 * t.w);
+          ob[e] = pack_bf16x2(b0 * t.x + a0 * t.y, b1 * t.z + a1 * t.w);
+        }
+        *reinterpret_cast<uint4*>(out + eb) = make_uint4(ob[0], ob[1], ob[2], ob[3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 t = reinterpret_cast<const float2*>(turn)[e];
+          float a, b;
+          halves_of(wa[e], a, b);
+          oa[e] = pack_bf16x2(a * t.x - b * t.y, b * t.x + a * t.y);
+        }
       }
-      reinterpret_cast<uint4*>(dst)[c] = make_uint4(o[0], o[1], o[2], o[3]);
+      *reinterpret_cast<uint4*>(out + ea) = make_uint4(oa[0], oa[1], oa[2], oa[3]);
     }
   }
 }
@@ -157,22 +171,19 @@ int launch_rotary(const eqat_rotary_desc& d, const RotaryRows& rows, bool backwa
   p.rotary_dim = d.rotary_dim;
   p.amplitude = d.amplitude;
   p.sine = backward ? -d.amplitude : d.amplitude;
-  // Several rows a block where there are enough of them, several blocks a row where there are few.
-  const int64_t wave = (int64_t)sms * 4;
-  int64_t per = d.rows / wave;
-  p.block_rows = (int)(per < 1 ? 1 : per > kMaxRows ? kMaxRows : per);
-  const int64_t bx = (d.rows + p.block_rows - 1) / p.block_rows;
-  const int row_items = p.heads * (d.head_dim / 16);
-  int64_t by = (wave + bx - 1) / bx;
-  const int64_t most = (row_items + kThreads - 1) / kThreads;
-  by = by > most ? most : by;
-  by = by > p.heads ? p.heads : by;
-  by = by < 1 ? 1 : by;
-  p.block_heads = (int)((p.heads + by - 1) / by);
-  const dim3 grid((unsigned)bx, (unsigned)((p.heads + p.block_heads - 1) / p.block_heads));
-  const size_t smem = (size_t)p.block_rows * (d.rotary_dim / 2) * sizeof(float2);
   const bool halves = d.layout == EQAT_ROTARY_HALVES;
   const bool vectors = d.rotary_dim % (halves ? 16 : 8) == 0;
+  const int wide = vectors ? 8 : 1;
+  const bool in_place = rows.q == rows.q_out && (d.kv_heads == 0 || rows.k == rows.k_out);
+  p.turned = halves || !vectors ? d.rotary_dim / 2 / wide : d.rotary_dim / wide;
+  p.rest = in_place ? 0 : (d.head_dim - d.rotary_dim) / wide;
+  const int64_t chunks = ((int64_t)p.heads * (p.turned + p.rest) + kThreads - 1) / kThreads;
+  if (chunks > 65535) return EQAT_ERR_SHAPE;
+  // several rows a block where there are enough blocks all the same
+  int64_t per = d.rows * chunks / ((int64_t)sms * 8);
+  p.block_rows = (int)(per < 1 ? 1 : per > kMaxRows ? kMaxRows : per);
+  const dim3 grid((unsigned)((d.rows + p.block_rows - 1) / p.block_rows), (unsigned)chunks);
+  const size_t smem = (size_t)p.block_rows * (d.rotary_dim / 2) * sizeof(float2);
   if (halves)
     return vectors ? launch_overlapped(rotary_kernel<EQAT_ROTARY_HALVES, true>, grid, dim3(kThreads), smem, st, p)
                    : launch_overlapped(rotary_kernel<EQAT_ROTARY_HALVES, false>, grid, dim3(kThreads), smem, st, p);

@@ -11,14 +11,10 @@
 // K is split over the pairs of a cluster where the tiles alone do not fill the chip; the partial sums meet in the shared
 // memory of the CTA that owns a token column and are added in a fixed order (run-to-run identical, no scratch memory).
 //
-// A gated feed-forward block's two projections (GATED): a CTA's rows are 64 of the gate's weight and the same 64 of the other's,
-// so the CTA that adds up a token column has both projections of 64 features and stores their product.
-//
 // Roles (18 warps, one CTA per SM): warp 0 TMA producer, warp 1 MMA issuer (first CTA of the pair) and TMEM owner, four
 // groups of 128 row threads.  A run = 128 codes of a row; group g takes the runs g, g + 4, ... of the CTA's K slice.
 #include <cuda.h>
 
-#include "activation.cuh"
 #include "common.cuh"
 #include "expand.cuh"
 #include "gemm.cuh"
@@ -43,7 +39,6 @@ struct WideParams : PackedWeight {
   int split, split_log2, runs;         // runs = in_features / 128
   int stages;
   int tile0;                           // first row tile of the launch (an even number)
-  OtherWeight other;                   // GATED
 };
 
 struct WideCtl {
@@ -71,10 +66,9 @@ __device__ __forceinline__ void load_run(uint32_t box, int row, uint32_t (&w)[4 
   }
 }
 
-template <int BITS, bool GATED>
+template <int BITS>
 __global__ void __launch_bounds__(kThreads, 1)
-wide_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
-                const __grid_constant__ CUtensorMap map_other, const WideParams p) {
+wide_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const WideParams p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = ptx::smem_addr(smem_raw);
   const uint32_t ring_addr = (raw_addr + 1023u) & ~1023u;
@@ -87,17 +81,13 @@ wide_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 
   // grid: row tiles (an even number) x pairs of a cluster x token tiles; cluster = 2 row tiles x split
   const int half = (int)(blockIdx.x & 1u), ks = (int)blockIdx.y;
-  constexpr int kWeightRows = GATED ? kRows / 2 : kRows;   // of a weight in a CTA's tile
-  const int m0 = (p.tile0 + (int)blockIdx.x) * kWeightRows, t0 = (int)blockIdx.z * p.tn;
+  const int m0 = (p.tile0 + (int)blockIdx.x) * kRows, t0 = (int)blockIdx.z * p.tn;
   const int run0 = (p.runs * ks) >> p.split_log2, nruns = ((p.runs * (ks + 1)) >> p.split_log2) - run0;
   // barriers that both CTAs of a pair signal live in its first CTA
   auto lead = [&](const void* bar) { return ptx::map_to_cta(ptx::smem_addr(bar), (uint32_t)(2 * ks)); };
 
   if (warp == 0 && m0 < p.out_features && ptx::elect_one()) {   // into L2 before the wait for the launches before this one
-    for (int r = 0; r < nruns; ++r) {
-      ptx::tma_prefetch_2d(&map_w, (run0 + r) * code_bytes(BITS), m0);
-      if (GATED) ptx::tma_prefetch_2d(&map_other, (run0 + r) * code_bytes(BITS), m0);
-    }
+    for (int r = 0; r < nruns; ++r) ptx::tma_prefetch_2d(&map_w, (run0 + r) * code_bytes(BITS), m0);
   }
   if (threadIdx.x == 64) {
     for (int s = 0; s < stages; ++s) {
@@ -138,7 +128,6 @@ wide_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         const uint32_t full_x = lead(&ctl->full_x[st]);
         ptx::mbar_expect_tx(full_c, kCodes);               // what lies past the matrices is zero-filled and counted
         ptx::tma_load_2d(dst + p.tn * 128, &map_w, (run0 + r) * code_bytes(BITS), m0, full_c);
-        if (GATED) ptx::tma_load_2d(dst + p.tn * 128 + kWeightRows * code_bytes(BITS), &map_other, (run0 + r) * code_bytes(BITS), m0, full_c);
         ptx::mbar_expect_tx_cluster(full_x, (uint32_t)p.tn * 128);
         ptx::tma_load_3d_pair(dst, &map_x, 0, t0 + half * (p.tn >> 1), (run0 + r) * 2, full_x);
         if (++st == stages) { st = 0; ph ^= 1u; }
@@ -180,9 +169,7 @@ wide_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   } else {
     // ---------------------------------------------------------------- row threads
     const int g = (warp - 2) >> 2, quad = warp & 3;
-    const int box_row = quad * 32 + lane, row = m0 + (box_row & (kWeightRows - 1));
-    PackedWeight weight = p;                               // the one that this thread's row is of
-    if (GATED && box_row >= kWeightRows) { weight.s16 = p.other.s16; weight.zq = p.other.zq; }
+    const int box_row = quad * 32 + lane, row = m0 + box_row;
     const bool valid = row < p.out_features;               // uniform over a warp: out_features is a multiple of 64
     const uint32_t t_a = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(g * 64);
     const size_t g_row = (size_t)(valid ? row : 0) * p.groups_per_row;
@@ -190,7 +177,7 @@ wide_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     const uint32_t a_full = lead(&ctl->a_full[g]);
     GroupParamsRaw gp;
     gp.s = gp.z = make_uint2(0u, 0u);
-    auto fetch = [&](int r) { load_group_params(weight, g_row + (size_t)(((run0 + r) * kRun) >> p.group_shift), g_count, gp); };
+    auto fetch = [&](int r) { load_group_params(p, g_row + (size_t)(((run0 + r) * kRun) >> p.group_shift), g_count, gp); };
     if (g < nruns) fetch(g);
     for (int r = g; r < nruns; r += kGroups) {
       // First the group's run before has to have left its TMEM buffer, i.e. its stage is empty: its MMAs, and with them those
@@ -288,9 +275,10 @@ wide_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     // a lane sums four columns of two neighbouring rows; a warp stores 128 bytes of each column
     const int cols = min(slice, p.T - t0 - ks * slice);
     const float4* part = reinterpret_cast<const float4*>(ring);
-    auto sum_rows = [&](int cg, int row2, float4 (&v)[2]) {
-      v[0] = part[cg * kRows + row2];
-      v[1] = part[cg * kRows + row2 + 1];
+    for (int i = warp; i < (slice >> 2) * 2; i += kThreads / 32) {
+      const int cg = i >> 1, row2 = (i & 1) * 64 + 2 * lane;
+      if (4 * cg >= cols) break;
+      float4 v[2] = {part[cg * kRows + row2], part[cg * kRows + row2 + 1]};
       for (int s = 1; s < p.split; ++s) {                  // fixed order: deterministic
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -298,38 +286,13 @@ wide_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
           v[j].x += u.x; v[j].y += u.y; v[j].z += u.z; v[j].w += u.w;
         }
       }
-    };
-    auto store_rows = [&](eqat_bf16* Y, int cg, int row, const float4 (&v)[2]) {
-      const uint32_t o[4] = {pack_bf16x2(v[0].x, v[1].x), pack_bf16x2(v[0].y, v[1].y), pack_bf16x2(v[0].z, v[1].z),
-                             pack_bf16x2(v[0].w, v[1].w)};
-      eqat_bf16* y = Y + (size_t)(t0 + ks * slice + 4 * cg) * p.out_features + row;
+      if (m0 + row2 < p.out_features) {
+        const uint32_t o[4] = {pack_bf16x2(v[0].x, v[1].x), pack_bf16x2(v[0].y, v[1].y), pack_bf16x2(v[0].z, v[1].z),
+                               pack_bf16x2(v[0].w, v[1].w)};
+        eqat_bf16* y = p.Y + (size_t)(t0 + ks * slice + 4 * cg) * p.out_features + m0 + row2;
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if (4 * cg + c < cols) *reinterpret_cast<uint32_t*>(y + (size_t)c * p.out_features) = o[c];
-    };
-    if constexpr (GATED) {
-      for (int cg = warp; 4 * cg < cols; cg += kThreads / 32) {
-        const int row = m0 + 2 * lane;
-        float4 g[2], u[2];
-        sum_rows(cg, 2 * lane, g);
-        sum_rows(cg, kWeightRows + 2 * lane, u);
-        if (row >= p.out_features) continue;
-        if (p.other.gate_out != nullptr) {
-          store_rows(p.other.gate_out, cg, row, g);
-          store_rows(p.other.other_out, cg, row, u);
-        }
-        EQAT_WITH_ACTIVATION(p.other.activation, _Pragma("unroll") for (int j = 0; j < 2; ++j) g[j] =
-                                                     make_float4(activate<kAct>(g[j].x) * u[j].x, activate<kAct>(g[j].y) * u[j].y,
-                                                                 activate<kAct>(g[j].z) * u[j].z, activate<kAct>(g[j].w) * u[j].w));
-        store_rows(p.Y, cg, row, g);
-      }
-    } else {
-      for (int i = warp; i < (slice >> 2) * 2; i += kThreads / 32) {
-        const int cg = i >> 1, row2 = (i & 1) * 64 + 2 * lane;
-        if (4 * cg >= cols) break;
-        float4 v[2];
-        sum_rows(cg, row2, v);
-        if (m0 + row2 < p.out_features) store_rows(p.Y, cg, m0 + row2, v);
+        for (int c = 0; c < 4; ++c)
+          if (4 * cg + c < cols) *reinterpret_cast<uint32_t*>(y + (size_t)c * p.out_features) = o[c];
       }
     }
   }
@@ -346,10 +309,10 @@ constexpr int kMaxSplit = 4;           // pairs per cluster: eight CTAs, the por
 // Clusters of two, four and eight CTAs that a B200 of 148 SMs kept resident, for plans made without a device.
 constexpr int kResidentOf148[3] = {74, 32, 13};
 
-template <int BITS, bool GATED>
+template <int BITS>
 bool opted_in() {
   static SmemOptIn opt_in;
-  return opt_in.ensure(wide_fwd_kernel<BITS, GATED>, kMaxSmem);
+  return opt_in.ensure(wide_fwd_kernel<BITS>, kMaxSmem);
 }
 
 void set_launch(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[2], dim3 ctas, int split, cudaStream_t st) {
@@ -379,15 +342,15 @@ int max_clusters(int bits, int lg) {
     const int c = cache[dev][lg].load(std::memory_order_relaxed);
     if (c > 0) return c;
   }
-  if (!(bits == 2 ? opted_in<2, false>() : (bits == 3 ? opted_in<3, false>() : opted_in<4, false>()))) return 0;
+  if (!(bits == 2 ? opted_in<2>() : (bits == 3 ? opted_in<3>() : opted_in<4>()))) return 0;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[2];
   set_launch(cfg, attr, dim3(2u, 1u << lg, 1u), 1 << lg, nullptr);
   cfg.numAttrs = 1;
   int n = 0;
-  const cudaError_t e = bits == 2   ? cudaOccupancyMaxActiveClusters(&n, wide_fwd_kernel<2, false>, &cfg)
-                        : bits == 3 ? cudaOccupancyMaxActiveClusters(&n, wide_fwd_kernel<3, false>, &cfg)
-                                    : cudaOccupancyMaxActiveClusters(&n, wide_fwd_kernel<4, false>, &cfg);
+  const cudaError_t e = bits == 2   ? cudaOccupancyMaxActiveClusters(&n, wide_fwd_kernel<2>, &cfg)
+                        : bits == 3 ? cudaOccupancyMaxActiveClusters(&n, wide_fwd_kernel<3>, &cfg)
+                                    : cudaOccupancyMaxActiveClusters(&n, wide_fwd_kernel<4>, &cfg);
   if (e != cudaSuccess) {
     (void)cudaGetLastError();
     return 0;
@@ -396,38 +359,33 @@ int max_clusters(int bits, int lg) {
   return n;
 }
 
-template <int BITS, bool GATED>
+template <int BITS>
 int launch_bits(const WideParams& p, const eqat_bf16* X, dim3 ctas, cudaStream_t st) {
-  auto kern = wide_fwd_kernel<BITS, GATED>;
-  if (!opted_in<BITS, GATED>()) return EQAT_ERR_CUDA;
-  CUtensorMap mx, mw, mo;
+  auto kern = wide_fwd_kernel<BITS>;
+  if (!opted_in<BITS>()) return EQAT_ERR_CUDA;
+  CUtensorMap mx, mw;
   if (!make_tmap_blocks_bf16(&mx, X, (uint64_t)p.in_features, (uint64_t)p.T, (uint32_t)p.tn / 2, 2)) return EQAT_ERR_CUDA;
-  auto codes_map = [&](CUtensorMap* m, const uint8_t* Wq) {
-    return make_tmap_u8(m, Wq, (uint64_t)p.in_features * BITS / 8, (uint64_t)p.out_features, code_bytes(BITS), GATED ? kRows / 2 : kRows,
-                        BITS == 3 ? 0 : code_bytes(BITS));
-  };
-  if (!codes_map(&mw, p.Wq)) return EQAT_ERR_CUDA;
-  if (!GATED) mo = mw;
-  else if (!codes_map(&mo, p.other.Wq)) return EQAT_ERR_CUDA;
+  if (!make_tmap_u8(&mw, p.Wq, (uint64_t)p.in_features * BITS / 8, (uint64_t)p.out_features, code_bytes(BITS), kRows,
+                    BITS == 3 ? 0 : code_bytes(BITS)))
+    return EQAT_ERR_CUDA;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[2];
   set_launch(cfg, attr, ctas, p.split, st);
-  if (cudaLaunchKernelEx(&cfg, kern, mx, mw, mo, p) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&cfg, kern, mx, mw, p) != cudaSuccess) {
     (void)cudaGetLastError();
     return EQAT_ERR_CUDA;
   }
   return launch_status();
 }
 
-template <bool GATED>
 int launch_rows(WideParams& p, int bits, const eqat_bf16* X, int pairs, int split, int token_tiles, cudaStream_t st) {
   p.split = split;
   p.split_log2 = log2_exact(split);
   const dim3 ctas((unsigned)pairs * 2u, (unsigned)split, (unsigned)token_tiles);
   switch (bits) {
-    case 2: return launch_bits<2, GATED>(p, X, ctas, st);
-    case 3: return launch_bits<3, GATED>(p, X, ctas, st);
-    default: return launch_bits<4, GATED>(p, X, ctas, st);
+    case 2: return launch_bits<2>(p, X, ctas, st);
+    case 3: return launch_bits<3>(p, X, ctas, st);
+    default: return launch_bits<4>(p, X, ctas, st);
   }
 }
 
@@ -507,39 +465,22 @@ bool wide_fwd_applies(const eqat_desc& d, int given_sms, WidePlan& best) {
   return best.us * (d.bits == 4 ? 1.08 : 1.0) < 0.95 * tiled;
 }
 
-namespace {
-
-template <bool GATED>
-int launch_wide(const eqat_desc& d, const eqat_bf16* X, const eqat_packed_weight& w, const OtherWeight& other, eqat_bf16* Y,
-                const WidePlan& pl, cudaStream_t st) {
+int launch_wide_fwd(const eqat_desc& d, const eqat_bf16* X, const uint8_t* Wq, const eqat_fp16* s16, const void* zq,
+                    eqat_bf16* Y, const WidePlan& pl, cudaStream_t st) {
   WideParams p{};
-  set_weight(p, d, w.Wq_packed, w.s16, w.z);
-  p.other = other;
+  set_weight(p, d, Wq, s16, zq);
   p.Y = Y;
   p.T = (int)d.tokens;
   p.tn = pl.tn;
   p.runs = d.in_features / kRun;
   p.stages = stages_that_fit(d.bits, pl.tn);
-  const int rows = GATED ? kRows : 2 * kRows;                            // of a weight in a pair's tile
-  const int pairs = (d.out_features + rows - 1) / rows;
-  int rc = launch_rows<GATED>(p, d.bits, X, pl.first_pairs, pl.split, pl.token_tiles, st);
+  const int pairs = (d.out_features + 2 * kRows - 1) / (2 * kRows);
+  int rc = launch_rows(p, d.bits, X, pl.first_pairs, pl.split, pl.token_tiles, st);
   if (rc == EQAT_OK && pl.first_pairs < pairs) {
     p.tile0 = 2 * pl.first_pairs;
-    rc = launch_rows<GATED>(p, d.bits, X, pairs - pl.first_pairs, pl.rest_split, pl.token_tiles, st);
+    rc = launch_rows(p, d.bits, X, pairs - pl.first_pairs, pl.rest_split, pl.token_tiles, st);
   }
   return rc;
-}
-
-}  // namespace
-
-int launch_wide_fwd(const eqat_desc& d, const eqat_bf16* X, const uint8_t* Wq, const eqat_fp16* s16, const void* zq,
-                    eqat_bf16* Y, const WidePlan& pl, cudaStream_t st) {
-  return launch_wide<false>(d, X, eqat_packed_weight{Wq, s16, zq}, OtherWeight{}, Y, pl, st);
-}
-
-int launch_wide_gated(const eqat_desc& d, int activation, const eqat_bf16* X, const eqat_packed_weight& gate,
-                      const eqat_packed_weight& up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, const WidePlan& pl, cudaStream_t st) {
-  return launch_wide<true>(d, X, gate, other_weight(up, activation, G, U), H, pl, st);
 }
 
 int launch_wait_expiry_wide(cudaStream_t st) { return launch_wait_expiry(st); }

@@ -18,10 +18,6 @@ bool wide_fwd_applies(const eqat_desc& d, int sms, WidePlan& plan);
 // Y[T,out] = X[T,in] * dequant(Wq)^T
 int launch_wide_fwd(const eqat_desc& d, const eqat_bf16* X, const uint8_t* Wq, const eqat_fp16* s16, const void* zq,
                     eqat_bf16* Y, const WidePlan& plan, cudaStream_t st);
-// H = act(X * dequant(gate)^T) * (X * dequant(up)^T); G and U, the projections, or null.  The plan is that of a weight with the
-// rows of both.
-int launch_wide_gated(const eqat_desc& d, int activation, const eqat_bf16* X, const eqat_packed_weight& gate,
-                      const eqat_packed_weight& up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, const WidePlan& plan, cudaStream_t st);
 
 // Self-test of the kernel's bounded wait (one warp, 1 ms, a barrier nothing signals).
 int launch_wait_expiry_wide(cudaStream_t st);

@@ -142,7 +142,7 @@ def test_packed_gated_arguments(eqat):
     good, desc = W(A, A, A), eqat.make_desc(2, 64, 128, 256, 5)
 
     def fwd(d=desc, act=0, X=A, gate=good, up=good, H=A, G=A, U=A):
-        return eqat.lib.qlinear_packed_gated_fwd(d and ctypes.byref(d), act, X, gate and ctypes.byref(gate), up and ctypes.byref(up), H, G, U, None)
+        return eqat.lib.qlinear_packed_gated_fwd(d and ctypes.byref(d), act, X, gate and ctypes.byref(gate), up and ctypes.byref(up), H, G, U, None, 0, None)
 
     def bwd(d=desc, act=0, dH=A, G=A, U=A, gate=good, up=good, dX=A, dG=A, dU=A):
         return eqat.lib.qlinear_packed_gated_bwd(d and ctypes.byref(d), act, dH, G, U, gate and ctypes.byref(gate), up and ctypes.byref(up), dX, dG, dU, None)
@@ -161,6 +161,26 @@ def test_packed_gated_arguments(eqat):
         for d, status in ((eqat.make_desc(5, 64, 128, 256, 5), -4), (eqat.make_desc(2, 64, 96, 256, 5), -2), (eqat.make_desc(2, 64, 128, 200, 5), -2),
                           (eqat.make_desc(2, 64, 128, 256, 0), -2), (eqat.make_desc(2, 512, 128, 1024, 5), -4)):
             assert call(d=d) == status
+
+
+def test_a_workspace_is_needed_where_the_projections_pass_through_memory(eqat):
+    """Checked before any launch, and so without a device."""
+    W, seen = eqat.eqat_packed_weight(A, A, A), set()
+    for bits in (2, 3, 4):
+        for T in (1, 8, 37, 64, 100, 300, 600, 5000, 20000):
+            d = eqat.make_desc(bits, 64, 11008, 4096, T)
+            need, route = eqat.packed_gated_workspace_bytes(d), eqat.eqat_packed_gated_route(d, 148)
+            seen.add(route)
+            assert route == eqat.eqat_packed_fwd_route(eqat.make_desc(bits, 64, 22016, 4096, T), 148)[0]
+            assert (need > 0) == (route == eqat.EQAT_ROUTE_WEIGHT_ROW_PAIRS)
+            if need:
+                assert need >= 2 * T * 11008 * 2 and need % 512 == 0
+                for ws in ((None, need), (A, need - 1), (A + 128, need)):
+                    assert eqat.lib.qlinear_packed_gated_fwd(ctypes.byref(d), 0, A, ctypes.byref(W), ctypes.byref(W), A, None, None, *ws, None) == eqat.EQAT_ERR_WORKSPACE
+    assert seen == {eqat.EQAT_ROUTE_MATRIX_VECTOR, eqat.EQAT_ROUTE_WEIGHT_ROWS, eqat.EQAT_ROUTE_WEIGHT_ROW_PAIRS, eqat.EQAT_ROUTE_TILED}
+    assert eqat.lib.eqat_packed_gated_route(ctypes.byref(eqat.make_desc(2, 64, 256, 256, 4)), -1) == eqat.EQAT_ERR_SHAPE
+    with pytest.raises(eqat.EqatError):
+        eqat.packed_gated_workspace_bytes(eqat.make_desc(2, 64, 96, 256, 5))
 
 
 def test_tensors_are_checked_before_the_call(eqat):

@@ -75,8 +75,8 @@ class Block:
         b["cache"] = eqat.make_cache_desc(GROUP, D, KV, 16, 20, 2, 5, T)
         b["attn"] = eqat.make_attention_desc(HEADS, new, D ** -0.5)
         b["gated"] = self.gate.desc(T)
-        need = eqat.cache_workspace_bytes(b["cache"], b["attn"])
-        b["ws"] = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+        for name, need in (("ws1", eqat.cache_workspace_bytes(b["cache"], b["attn"])), ("ws2", eqat.packed_gated_workspace_bytes(b["gated"]))):
+            b[name] = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
         b["off"], b["len"] = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
         return b
 
@@ -87,10 +87,10 @@ class Block:
         heads = b["qkv"].view(-1, HEADS + 2 * KV, D)
         eqat.eqat_rotary_fwd(b["rotary"], heads[:, :HEADS], heads[:, HEADS:HEADS + KV], self.turns, b["q"], b["k"], None, b["off"], b["len"])
         eqat.eqat_cache_append(b["cache"], b["k"], heads[:, HEADS + KV:], *where)
-        eqat.eqat_cache_attention(b["cache"], b["attn"], b["q"], *where, b["att"], None, b["ws"])
+        eqat.eqat_cache_attention(b["cache"], b["attn"], b["q"], *where, b["att"], None, b["ws1"])
         self.o(b["att"].view(-1, HEADS * D), b["a"])
         eqat.eqat_rms_norm_fwd(b["norm"], b["a"], b["x"], self.w2, b["h2"], b["y2"])
-        eqat.qlinear_packed_gated_fwd(b["gated"], eqat.EQAT_ACT_SILU, b["y2"], self.gate.on, self.up.on, b["f"])
+        eqat.qlinear_packed_gated_fwd(b["gated"], eqat.EQAT_ACT_SILU, b["y2"], self.gate.on, self.up.on, b["f"], None, None, b["ws2"])
         self.down(b["f"], b["out"])
 
     def check(self, b, lens, news, keys, values):

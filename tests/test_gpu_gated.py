@@ -138,10 +138,11 @@ def test_packed_forward(eqat, T, out, width, bits, group, fp16, kind):
     gate, up = both_weights(out, width, bits, group, fp16)
     X, buf = normal(T, width, seed=3), Guarded()
     d = eqat.make_desc(bits, group, out, width, T, 0, eqat.EQAT_ZP_FP16 if fp16 else eqat.EQAT_ZP_U8)
+    need = eqat.packed_gated_workspace_bytes(d)
     H, G, U, H2 = (buf.empty(T, out, dtype=torch.bfloat16, shift_bytes=16 * i) for i in range(4))
     act = act_code(eqat, kind)
     eqat.qlinear_packed_gated_fwd(d, act, X, gate.on, up.on, H, G, U)
-    eqat.qlinear_packed_gated_fwd(d, act, X, gate.on, up.on, H2)
+    eqat.qlinear_packed_gated_fwd(d, act, X, gate.on, up.on, H2, None, None, buf.empty(need, dtype=torch.uint8) if need else None)
     buf.check()
     assert eqat.device_status() == (0, 0)
     assert torch.equal(H, H2)
@@ -196,17 +197,6 @@ def test_zero_points_of_eight_bits(eqat, T):
             assert_elementwise(torch_to_f64(got), want, room, which)
 
 
-def test_same_bits_as_one_projection_at_a_time(eqat):
-    """G and U are those of qlinear_packed_fwd where the same kernel takes both (single tokens), and H that of the unrounded sums."""
-    gate, up = both_weights(512, 1024, 2, 64, False)
-    X, d = normal(1, 1024, seed=11), eqat.make_desc(2, 64, 512, 1024, 1)
-    H, G, U, Y = (torch.empty(1, 512, dtype=torch.bfloat16, device="cuda") for _ in range(4))
-    eqat.qlinear_packed_gated_fwd(d, eqat.EQAT_ACT_SILU, X, gate.on, up.on, H, G, U)
-    for got, w in ((G, gate), (U, up)):
-        eqat.qlinear_packed_fwd(d, X, *w.on, Y)
-        assert torch.equal(got, Y)
-
-
 def test_the_weights_are_not_mixed_up(eqat):
     """A gate of ones and an up weight of twos, and the other way round: H = act(n) 2n against act(2n) n."""
     out, width = 128, 128
@@ -216,8 +206,10 @@ def test_the_weights_are_not_mixed_up(eqat):
         codes = [torch.full((out, width // 4), v * 0x55, dtype=torch.uint8, device="cuda") for v in (1, 2)]
         s, z = torch.ones(out, 2, dtype=torch.float16, device="cuda"), torch.zeros(out, 2, dtype=torch.uint8, device="cuda")
         H = torch.empty(T, out, dtype=torch.bfloat16, device="cuda")
+        need = eqat.packed_gated_workspace_bytes(d)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
         for a, b in ((1, 2), (2, 1)):
-            eqat.qlinear_packed_gated_fwd(d, eqat.EQAT_ACT_SILU, X, (codes[a - 1], s, z), (codes[b - 1], s, z), H)
+            eqat.qlinear_packed_gated_fwd(d, eqat.EQAT_ACT_SILU, X, (codes[a - 1], s, z), (codes[b - 1], s, z), H, None, None, ws)
             want = float(B.activation(float(a), "silu")[0]) * b
             assert (H.double() - want).abs().max() <= 2.0 ** -7 * want
 
@@ -225,10 +217,12 @@ def test_the_weights_are_not_mixed_up(eqat):
 def test_captured_on_another_stream(eqat):
     out, width = 256, 512
     gate, up = both_weights(out, width, 2, 64, False)
-    for T in (1, 24, 1500):
+    for T in (1, 24, 200, 1500):
         d = eqat.make_desc(2, 64, out, width, T)
+        need = eqat.packed_gated_workspace_bytes(d)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
         X, H = normal(T, width, seed=7), torch.empty(T, out, dtype=torch.bfloat16, device="cuda")
-        call = lambda: eqat.qlinear_packed_gated_fwd(d, eqat.EQAT_ACT_GELU, X, gate.on, up.on, H)  # noqa: E731
+        call = lambda: eqat.qlinear_packed_gated_fwd(d, eqat.EQAT_ACT_GELU, X, gate.on, up.on, H, None, None, ws)  # noqa: E731
         call()
         torch.cuda.synchronize()
         g, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
