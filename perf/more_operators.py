@@ -398,7 +398,8 @@ def _plan(s):
         return eqat, eqat.make_gated_desc(c["rows"], c["features"], act), None
     zeros = eqat.EQAT_ZP_U8 if c["zeros"] == "u8" else eqat.EQAT_ZP_FP16
     desc = eqat.make_desc(c["bits"], c["group"], c["inner"], c["width"], c["tokens"], 0, zeros)
-    return eqat, desc, act
+    need = 0 if c["backward"] or c["keep"] else eqat.packed_gated_workspace_bytes(desc)
+    return eqat, desc, (act, torch.empty(need, dtype=torch.uint8, device=DEV) if need else None)
 
 
 def _call(s):
@@ -421,10 +422,11 @@ def _call(s):
             return [s["dG"], s["dU"]]
         eqat.eqat_gated_fwd(desc, s["G"], s["U"], s["H"])
         return s["H"]
+    act, scratch = more
     if c["backward"]:
-        eqat.qlinear_packed_gated_bwd(desc, more, s["dH"], s["G"], s["U"], s["gate"], s["up"], s["dX"], s["dG"], s["dU"])
+        eqat.qlinear_packed_gated_bwd(desc, act, s["dH"], s["G"], s["U"], s["gate"], s["up"], s["dX"], s["dG"], s["dU"])
         return [s["dX"], s["dG"], s["dU"]]
-    eqat.qlinear_packed_gated_fwd(desc, more, s["X"], s["gate"], s["up"], s["H"], s["G"], s["U"])
+    eqat.qlinear_packed_gated_fwd(desc, act, s["X"], s["gate"], s["up"], s["H"], s["G"], s["U"], scratch)
     return [s["H"], s["G"], s["U"]] if c["keep"] else s["H"]
 
 
