@@ -88,7 +88,8 @@ typedef struct {
 enum { EQAT_ZP_U8 = 0, EQAT_ZP_FP16 = 1 };
 
 /* Operations that need caller-provided scratch memory (eqat_workspace_bytes). */
-enum { EQAT_OP_FAKEQUANT_BWD = 1, EQAT_OP_PACKED_BWD_DS = 2 };
+enum { EQAT_OP_FAKEQUANT_BWD = 1, EQAT_OP_PACKED_BWD_DS = 2,
+       EQAT_OP_PACKED_GATED_FWD = 3, EQAT_OP_PACKED_GATED_BWD = 4 };
 
 const char* eqat_status_string(int status);
 int eqat_version(void);
@@ -603,35 +604,37 @@ typedef struct {              /* a weight as qlinear_packed_fwd takes it: device
  * that qlinear_packed_fwd takes for a weight of 2*out_features rows, with tiles that
  * hold both projections of their features: one pass over both weights, in which G
  * and U leave the kernel only if they are wanted (for the backward pass), and H is
- * that of the sums before they are rounded.  The exception are prompts for which that
- * kernel is EQAT_ROUTE_WEIGHT_ROW_PAIRS (eqat_packed_gated_route): two calls of
+ * that of the sums before they are rounded.  The exception are prompts for which
+ * eqat_packed_gated_route says EQAT_ROUTE_WEIGHT_ROW_PAIRS: two calls of
  * qlinear_packed_fwd and one of eqat_gated_fwd, through G and U or, where these are
  * NULL, through the workspace; H is then that of G and U as they are rounded.  What
  * is said of qlinear_packed_fwd, of how weights enter the products and of bits, holds.
+ * Without G and U it needs eqat_workspace_bytes(desc, EQAT_OP_PACKED_GATED_FWD) bytes
+ * of scratch on the current device (0: workspace may be NULL; with G and U it always
+ * may).  Calls that may overlap need a workspace each, here and in the backward pass.
  *   X [T,in] bf16, gate, up (in)   H [T,out] bf16 (out)
  *   G, U [T,out] bf16 (out): both, or both NULL */
 int qlinear_packed_gated_fwd(const eqat_desc* desc, int activation, const eqat_bf16* X, const eqat_packed_weight* gate,
                              const eqat_packed_weight* up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, void* workspace,
                              size_t workspace_bytes, void* stream);
 
-/* Bytes of scratch the call needs on the current device without G and U, 256-byte
- * aligned (0 if none, (size_t)-1 if the descriptor is invalid).  Calls that may
- * overlap need a workspace each. */
-size_t eqat_packed_gated_workspace_bytes(const eqat_desc* desc);
-
-/* The kernel that decides how the call goes out, EQAT_ROUTE_* (a diagnostic); `sms`
- * as in eqat_packed_fwd_route. */
+/* The kernel that the call goes to, EQAT_ROUTE_* (a diagnostic): that of the 2*out_features
+ * rows, or EQAT_ROUTE_TILED in the place of EQAT_ROUTE_WEIGHT_ROW_PAIRS where it is
+ * expected to be faster than two projections.  `sms` as in eqat_packed_fwd_route. */
 int eqat_packed_gated_route(const eqat_desc* desc, int sms);
 
 /* dG and dU as in eqat_gated_bwd, and
  *     dX = dG * W_gate + dU * W_up
  * of them as they are stored, one contraction over the features of both.  The step
  * sizes' gradients are qlinear_packed_bwd_ds of X with dG, and with dU.
+ * Few tokens split the contraction over the chip and add its parts up in a fixed
+ * order, through eqat_workspace_bytes(desc, EQAT_OP_PACKED_GATED_BWD) bytes of scratch.
  *   dH, G, U [T,out] bf16, gate, up (in)   dX [T,in], dG, dU [T,out] bf16 (out); dG and dU may
  *   be G, U or dH */
 int qlinear_packed_gated_bwd(const eqat_desc* desc, int activation, const eqat_bf16* dH, const eqat_bf16* G,
                              const eqat_bf16* U, const eqat_packed_weight* gate, const eqat_packed_weight* up,
-                             eqat_bf16* dX, eqat_bf16* dG, eqat_bf16* dU, void* stream);
+                             eqat_bf16* dX, eqat_bf16* dG, eqat_bf16* dU, void* workspace, size_t workspace_bytes,
+                             void* stream);
 
 /* ------------------------------------------------------------------ whole blocks */
 

@@ -20,7 +20,7 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libeqat_b2
 EQAT_OK = 0
 EQAT_ERR_NULL, EQAT_ERR_SHAPE, EQAT_ERR_ALIGN, EQAT_ERR_UNSUPPORTED = -1, -2, -3, -4
 EQAT_ERR_WORKSPACE, EQAT_ERR_CUDA, EQAT_ERR_TIMEOUT = -5, -6, -7
-EQAT_OP_FAKEQUANT_BWD, EQAT_OP_PACKED_BWD_DS = 1, 2
+EQAT_OP_FAKEQUANT_BWD, EQAT_OP_PACKED_BWD_DS, EQAT_OP_PACKED_GATED_FWD, EQAT_OP_PACKED_GATED_BWD = 1, 2, 3, 4
 EQAT_ZP_U8, EQAT_ZP_FP16 = 0, 1
 EQAT_ROUTE_MATRIX_VECTOR, EQAT_ROUTE_WEIGHT_ROWS, EQAT_ROUTE_WEIGHT_ROW_PAIRS, EQAT_ROUTE_TILED = 1, 2, 3, 4
 EQAT_GEMM_Y, EQAT_GEMM_DX, EQAT_GEMM_DW, EQAT_GEMM_LATENT_Y, EQAT_GEMM_LATENT_DX = 0, 1, 2, 3, 4
@@ -135,10 +135,9 @@ def _load():
         "eqat_rotary_bwd": (c_int, rotary),
         "eqat_gated_fwd": (c_int, [G, P, c_int64, P, c_int64, P, P]),
         "eqat_gated_bwd": (c_int, [G, P, P, c_int64, P, c_int64, P, c_int64, P, c_int64, P]),
-        "eqat_packed_gated_workspace_bytes": (c_size_t, [D]),
         "eqat_packed_gated_route": (c_int, [D, c_int]),
         "qlinear_packed_gated_fwd": (c_int, [D, c_int, P, W, W, P, P, P, P, c_size_t, P]),
-        "qlinear_packed_gated_bwd": (c_int, [D, c_int, P, P, P, W, W, P, P, P, P]),
+        "qlinear_packed_gated_bwd": (c_int, [D, c_int, P, P, P, W, W, P, P, P, P, c_size_t, P]),
         "eqat_block_ap_step": (c_int, [POINTER(eqat_block_ap_linear), c_int, POINTER(c_int), P]),
         "eqat_e2e_qp_step": (c_int, [POINTER(eqat_e2e_qp_linear), c_int, POINTER(c_int), P]),
     }
@@ -438,13 +437,6 @@ def eqat_gated_bwd(desc, dH, G, U, dG, dU):
     _check((_marshal or _load_marshal()).gated_bwd(desc, dH, G, U, dG, dU), "eqat_gated_bwd")
 
 
-def packed_gated_workspace_bytes(desc) -> int:
-    n = lib.eqat_packed_gated_workspace_bytes(ctypes.byref(desc))
-    if n == ctypes.c_size_t(-1).value:
-        raise EqatError(EQAT_ERR_SHAPE, "eqat_packed_gated_workspace_bytes")
-    return int(n)
-
-
 def eqat_packed_gated_route(desc, sms=0) -> int:
     """The kernel that decides how qlinear_packed_gated_fwd goes out (EQAT_ROUTE_*)."""
     route = lib.eqat_packed_gated_route(ctypes.byref(desc), int(sms))
@@ -455,12 +447,13 @@ def eqat_packed_gated_route(desc, sms=0) -> int:
 
 # A weight: (Wq_packed, s16, z).
 def qlinear_packed_gated_fwd(desc, activation, X, gate, up, H, G=None, U=None, workspace=None):
-    """G, U: the projections, for the backward pass (or None); workspace: packed_gated_workspace_bytes, without them."""
+    """G, U: the projections, for the backward pass (or None); workspace: EQAT_OP_PACKED_GATED_FWD, without them."""
     _check((_marshal or _load_marshal()).packed_gated_fwd(desc, activation, X, gate, up, H, G, U, workspace), "qlinear_packed_gated_fwd")
 
 
-def qlinear_packed_gated_bwd(desc, activation, dH, G, U, gate, up, dX, dG, dU):
-    _check((_marshal or _load_marshal()).packed_gated_bwd(desc, activation, dH, G, U, gate, up, dX, dG, dU), "qlinear_packed_gated_bwd")
+def qlinear_packed_gated_bwd(desc, activation, dH, G, U, gate, up, dX, dG, dU, workspace=None):
+    """workspace: EQAT_OP_PACKED_GATED_BWD."""
+    _check((_marshal or _load_marshal()).packed_gated_bwd(desc, activation, dH, G, U, gate, up, dX, dG, dU, workspace), "qlinear_packed_gated_bwd")
 
 
 def _nbytes(t):

@@ -151,6 +151,10 @@ int check_attention_desc(const eqat_cache_desc* d, const eqat_attention_desc* a)
   return EQAT_OK;
 }
 
+inline bool workspace_ok(const void* workspace, size_t bytes, size_t need) {
+  return need == 0 || (workspace != nullptr && bytes >= need && (reinterpret_cast<uintptr_t>(workspace) & 255u) == 0);
+}
+
 int check_norm_desc(const eqat_norm_desc* d) {
   if (d == nullptr) return EQAT_ERR_NULL;
   if (d->rows <= 0 || d->rows > (int64_t)1 << 30) return EQAT_ERR_SHAPE;
@@ -226,27 +230,53 @@ PackedRoute packed_route(const eqat_desc& d, int sms) {
   return r;
 }
 
-// How a gated feed-forward block's projections are taken: the kernel of a weight with the rows of both, except that prompts of
-// the kernel on pairs of weight-row tiles go through memory, one weight after the other.
+// How a gated feed-forward block's projections are taken: by the kernel of a weight with the rows of both.  The kernel on pairs of
+// weight-row tiles has no tiles of two weights: there the projections go through memory, one weight after the other, or the
+// tiled kernel takes both, whichever is expected to be faster.  Over 28 calls of 65 to 700 tokens (2 x 1408 x 2048 to 2 x 28672 x
+// 8192) the choice is wrong in one, by 3 %.  11008 x 4096, 2 bits, 128 / 333 / 640 tokens: 49, 82, 115 us through memory, 71,
+// 95, 141 us in one kernel; 1408 x 2048, 512 tokens: 28 and 22 us.
 struct GatedRoute {
   eqat_desc both;
   PackedRoute packed;
-  bool composed() const { return packed.kernel == EQAT_ROUTE_WEIGHT_ROW_PAIRS; }
+  int kernel;                            // EQAT_ROUTE_*; EQAT_ROUTE_WEIGHT_ROW_PAIRS: through memory
   // one projection in the workspace
   size_t bytes() const { return ((size_t)both.tokens * (both.out_features / 2) * sizeof(eqat_bf16) + 255) & ~(size_t)255; }
 };
-// (Without a device, as on one of 148 SMs.)
+// SMs of the current device; without one, as of one of 148.
+int sms_or_148() {
+  const int n = sm_count();
+  return n > 0 ? n : 148;
+}
 GatedRoute gated_route(const eqat_desc& d, int sms) {
-  GatedRoute r{d, {}};
+  if (sms == 0 && sm_count() <= 0) sms = 148;
+  GatedRoute r{d, {}, 0};
   r.both.out_features = 2 * d.out_features;
-  r.packed = packed_route(r.both, sms == 0 && sm_count() <= 0 ? 148 : sms);
+  r.packed = packed_route(r.both, sms);
+  r.kernel = r.packed.kernel;
+  if (r.kernel == EQAT_ROUTE_WEIGHT_ROW_PAIRS) {
+    const int n = sms > 0 ? sms : sm_count();
+    const PackedRoute one = packed_route(d, sms);
+    const double us = one.kernel == EQAT_ROUTE_WEIGHT_ROW_PAIRS ? one.wide.us : packed_tiled_us(d, n);
+    const double product = 3.0 + (double)d.tokens * d.out_features * 6.0 / 5.5e6;          // of the element-wise kernel
+    if (2.0 * us + product >= packed_tiled_us(r.both, n)) r.kernel = EQAT_ROUTE_TILED;
+  }
   return r;
 }
 
-int check_gated_weights(const eqat_desc* d, int activation, const eqat_packed_weight* gate, const eqat_packed_weight* up) {
+size_t gated_fwd_workspace(const eqat_desc& d) {
+  const GatedRoute r = gated_route(d, 0);
+  return r.kernel == EQAT_ROUTE_WEIGHT_ROW_PAIRS ? 2 * r.bytes() : 0;
+}
+
+int check_gated_desc(const eqat_desc* d) {
   const int rc = check_gemm_desc(d, true);
   if (rc != EQAT_OK) return rc;
-  if (d->out_features > 1 << 29) return EQAT_ERR_SHAPE;                  // the rows of both are counted in 32 bits
+  return d->out_features <= 1 << 29 ? EQAT_OK : EQAT_ERR_SHAPE;          // the rows of both are counted in 32 bits
+}
+
+int check_gated_weights(const eqat_desc* d, int activation, const eqat_packed_weight* gate, const eqat_packed_weight* up) {
+  const int rc = check_gated_desc(d);
+  if (rc != EQAT_OK) return rc;
   if (activation < EQAT_ACT_SILU || activation > EQAT_ACT_GELU_TANH) return EQAT_ERR_UNSUPPORTED;
   if (gate == nullptr || up == nullptr) return EQAT_ERR_NULL;
   return check_ptrs(gate->Wq_packed, gate->s16, gate->z, up->Wq_packed, up->s16, up->z);
@@ -288,6 +318,10 @@ size_t eqat_workspace_bytes(const eqat_desc* d, int op) {
   if (op == EQAT_OP_PACKED_BWD_DS) {
     if (check_gemm_desc(d, true) != EQAT_OK) return (size_t)-1;
     return packed_ds_workspace_bytes(*d);
+  }
+  if (op == EQAT_OP_PACKED_GATED_FWD || op == EQAT_OP_PACKED_GATED_BWD) {
+    if (check_gated_desc(d) != EQAT_OK) return (size_t)-1;
+    return op == EQAT_OP_PACKED_GATED_FWD ? gated_fwd_workspace(*d) : packed_gated_dx_workspace(*d, sms_or_148());
   }
   return (size_t)-1;
 }
@@ -531,8 +565,7 @@ int eqat_rms_norm_fwd(const eqat_norm_desc* d, const eqat_bf16* X, const eqat_bf
 
 size_t eqat_rms_norm_workspace_bytes(const eqat_norm_desc* d) {
   if (check_norm_desc(d) != EQAT_OK) return (size_t)-1;
-  const int sms = sm_count();
-  return norm_workspace(*d, sms > 0 ? sms : 148);                        // no device: as for the cache
+  return norm_workspace(*d, sms_or_148());
 }
 
 int eqat_rms_norm_bwd(const eqat_norm_desc* d, const eqat_bf16* dY, const eqat_bf16* H, const eqat_bf16* W, const eqat_bf16* dR,
@@ -540,9 +573,7 @@ int eqat_rms_norm_bwd(const eqat_norm_desc* d, const eqat_bf16* dY, const eqat_b
   EQAT_TRY(check_norm_desc(d));
   EQAT_TRY(check_ptrs(dY, H, W, dX));
   if (!aligned16(dR) || !aligned16(dW)) return EQAT_ERR_ALIGN;
-  if (dW != nullptr && (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 ||
-                        workspace_bytes < eqat_rms_norm_workspace_bytes(d)))
-    return EQAT_ERR_WORKSPACE;
+  if (dW != nullptr && !workspace_ok(workspace, workspace_bytes, eqat_rms_norm_workspace_bytes(d))) return EQAT_ERR_WORKSPACE;
   return launch_norm_bwd(*d, dY, H, W, dR, dX, dW, workspace, as_stream(stream));
 }
 
@@ -613,16 +644,10 @@ int eqat_gated_bwd(const eqat_gated_desc* d, const eqat_bf16* dH, const eqat_bf1
   return launch_gated_bwd(*d, dH, G, g_pitch, U, u_pitch, dG, dg_pitch, dU, du_pitch, as_stream(stream));
 }
 
-size_t eqat_packed_gated_workspace_bytes(const eqat_desc* d) {
-  if (check_gemm_desc(d, true) != EQAT_OK || d->out_features > 1 << 29) return (size_t)-1;
-  const GatedRoute r = gated_route(*d, 0);
-  return r.composed() ? 2 * r.bytes() : 0;
-}
-
 int eqat_packed_gated_route(const eqat_desc* d, int sms) {
-  EQAT_TRY(check_gemm_desc(d, true));
-  if (sms < 0 || d->out_features > 1 << 29) return EQAT_ERR_SHAPE;
-  return gated_route(*d, sms).packed.kernel;
+  EQAT_TRY(check_gated_desc(d));
+  if (sms < 0) return EQAT_ERR_SHAPE;
+  return gated_route(*d, sms).kernel;
 }
 
 int qlinear_packed_gated_fwd(const eqat_desc* d, int activation, const eqat_bf16* X, const eqat_packed_weight* gate,
@@ -634,16 +659,14 @@ int qlinear_packed_gated_fwd(const eqat_desc* d, int activation, const eqat_bf16
   if (!aligned16(G) || !aligned16(U)) return EQAT_ERR_ALIGN;
   const GatedRoute r = gated_route(*d, 0);
   cudaStream_t st = as_stream(stream);
-  if (!r.composed()) {
-    switch (r.packed.kernel) {
-      case EQAT_ROUTE_WEIGHT_ROWS: return launch_slim_gated(*d, activation, X, *gate, *up, H, G, U, r.packed.slim, st);
-      case EQAT_ROUTE_MATRIX_VECTOR: return launch_gemv_gated(*d, r.both, activation, X, *gate, *up, H, G, U, st);
-      default: return launch_packed_gated(*d, activation, X, *gate, *up, H, G, U, st);
-    }
+  switch (r.kernel) {
+    case EQAT_ROUTE_WEIGHT_ROWS: return launch_slim_gated(*d, activation, X, *gate, *up, H, G, U, r.packed.slim, st);
+    case EQAT_ROUTE_MATRIX_VECTOR: return launch_gemv_gated(*d, r.both, activation, X, *gate, *up, H, G, U, st);
+    case EQAT_ROUTE_TILED: return launch_packed_gated(*d, activation, X, *gate, *up, H, G, U, st);
+    default: break;
   }
   if (G == nullptr) {
-    if (workspace == nullptr || workspace_bytes < 2 * r.bytes() || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
-      return EQAT_ERR_WORKSPACE;
+    if (!workspace_ok(workspace, workspace_bytes, 2 * r.bytes())) return EQAT_ERR_WORKSPACE;
     G = static_cast<eqat_bf16*>(workspace);
     U = reinterpret_cast<eqat_bf16*>(static_cast<uint8_t*>(workspace) + r.bytes());
   }
@@ -655,13 +678,14 @@ int qlinear_packed_gated_fwd(const eqat_desc* d, int activation, const eqat_bf16
 
 int qlinear_packed_gated_bwd(const eqat_desc* d, int activation, const eqat_bf16* dH, const eqat_bf16* G, const eqat_bf16* U,
                              const eqat_packed_weight* gate, const eqat_packed_weight* up, eqat_bf16* dX, eqat_bf16* dG,
-                             eqat_bf16* dU, void* stream) {
+                             eqat_bf16* dU, void* workspace, size_t workspace_bytes, void* stream) {
   EQAT_TRY(check_gated_weights(d, activation, gate, up));
   EQAT_TRY(check_ptrs(dH, G, U, dX, dG, dU));
+  if (!workspace_ok(workspace, workspace_bytes, packed_gated_dx_workspace(*d, sms_or_148()))) return EQAT_ERR_WORKSPACE;
   const eqat_gated_desc g{d->tokens, d->out_features, activation};
   const int64_t pitch = d->out_features;
   EQAT_TRY(launch_gated_bwd(g, dH, G, pitch, U, pitch, dG, pitch, dU, pitch, as_stream(stream)));
-  return launch_packed_gated_dx(*d, dG, dU, *gate, *up, dX, as_stream(stream));
+  return launch_packed_gated_dx(*d, dG, dU, *gate, *up, dX, workspace, as_stream(stream));
 }
 
 int eqat_block_ap_step(const eqat_block_ap_linear* L, int count, int* h_failed, void* stream) {

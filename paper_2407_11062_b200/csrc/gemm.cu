@@ -44,7 +44,10 @@
 //              so that a row's thread finds both projections of its features in
 //              tensor memory and stores their product;
 //   EPI_JOINT  dX of both in one contraction: the first half of K is dG and the
-//              gate's weight, the second half dU and the other's.
+//              gate's weight, the second half dU and the other's.  K is long (both
+//              weights' rows) and few tokens make few tiles: its parts are taken by
+//              clusters of their own, the sums go to memory in fp32 and are added up
+//              by a second kernel.
 // Packed kernels walk their tiles row by row (the few MB of codes stay in L2,
 // each activation panel is fetched once); dense kernels in bands of row-tiles.
 //
@@ -91,6 +94,7 @@ struct GemmParams : PackedWeight {
   float Q;                   // 2^N - 1
   int dz_literal;            // Eq. 4 clamped branch: -1 instead of -s
   OtherWeight other;         // EPI_GATED / EPI_JOINT
+  int split;                 // EPI_JOINT: parts of K; their sums go to partial [split][M][N] if more than one
 };
 
 template <int MT, bool PACKED, bool PAIR, int BN>
@@ -210,6 +214,21 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
   const int num_tiles = num_m * num_n;
   const int num_kb = (p.K + BK - 1) / BK;
   constexpr int kBand = 4096 / C::kClusterM;
+  // What a cluster takes in turn: whole tiles, or (JOINT) the parts of tiles' K, part of a tile after part.
+  const int num_items = JOINT ? num_tiles * p.split : num_tiles;
+  struct Item {
+    int m_blk, n_blk, part, first_kb, num_kb;
+  };
+  auto item_at = [&](int i) {
+    Item t{0, 0, 0, 0, num_kb};
+    tile_coords<PACKED, kBand>(JOINT ? i / p.split : i, num_m, num_n, t.m_blk, t.n_blk);
+    if constexpr (JOINT) {
+      t.part = i % p.split;
+      t.first_kb = (int)((long)num_kb * t.part / p.split);
+      t.num_kb = (int)((long)num_kb * (t.part + 1) / p.split) - t.first_kb;
+    }
+    return t;
+  };
 
   // A barrier that both CTAs of a pair signal lives in the first CTA: `lead(bar)` is its address there.
   auto lead = [&](uint32_t bar) -> uint32_t { return PAIR ? ptx::map_to_cta(bar, 0) : bar; };
@@ -268,7 +287,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
   // as two K blocks.  Block-AP backward of 2048 x 2048, 512 tokens: 27.5, 26.3, 27.6, 24.7 us.)
   const int quad = warp & 3;
   const int row_in_tile = quad * 32 + lane;
-  auto epilogue_tile = [&](int m0, int n_blk, int acc, uint32_t acc_phase) -> bool {
+  auto epilogue_tile = [&](int m0, int n_blk, int part, int acc, uint32_t acc_phase) -> bool {
     const int h = MT == 2 ? (warp - 2) >> 2 : 0;
     const uint32_t t_row = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)((acc * MT + h) * BN);
     const int m = m0 + h * BM + row_in_tile;
@@ -303,6 +322,14 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
         ptx::tmem_ld_32x32(t_row + c * 32, r);
         ptx::tmem_ld_wait();
         const int col0 = n_blk * BN + c * 32;
+        if (JOINT && p.split > 1) {
+          if (m < p.M && col0 < p.N) {
+            uint4* const out = reinterpret_cast<uint4*>(p.partial + ((size_t)part * p.M + m) * p.N + col0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) out[i] = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+          }
+          continue;
+        }
         uint32_t o[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[i] = pack_bf16x2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
@@ -567,12 +594,11 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       long issued = 0;
       bool ok = true;
       constexpr uint32_t kBytes = PACKED ? C::kABytes : C::kStageBytes;   // this CTA's bytes per stage
-      for (int tile = cluster_id; tile < num_tiles && ok; tile += num_clusters) {
-        int m_blk, n_blk;
-        tile_coords<PACKED, kBand>(tile, num_m, num_n, m_blk, n_blk);
-        const int m0 = m_blk * C::kClusterM + rank * C::kTileM;    // this CTA's rows of A
-        const int n0 = n_blk * BN + rank * C::kBRows;              // this CTA's rows of B
-        for (int kb = 0; kb < num_kb; ++kb) {
+      for (int i = cluster_id; i < num_items && ok; i += num_clusters) {
+        const Item t = item_at(i);
+        const int m0 = t.m_blk * C::kClusterM + rank * C::kTileM;  // this CTA's rows of A
+        const int n0 = t.n_blk * BN + rank * C::kBRows;            // this CTA's rows of B
+        for (int kb = 0; kb < t.num_kb; ++kb) {
           if (!bounded_wait<PAIR>(ptx::smem_addr(&ctl->empty[stage]), phase ^ 1u, abort_flag, WAIT_PRODUCER_EMPTY, 64)) {
             ok = false;
             break;
@@ -590,8 +616,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
 #pragma unroll
             for (int b = 0; b < C::kTileM / 64; ++b) load(a_dst + b * (BK * 128), &tmap_a, m0 + b * 64, kb * BK);
           } else {
-            const bool second = JOINT && 2 * kb >= num_kb;
-            load(a_dst, second ? &tmap_b : &tmap_a, (second ? kb - num_kb / 2 : kb) * BK, m0);
+            const bool second = JOINT && 2 * (t.first_kb + kb) >= num_kb;
+            load(a_dst, second ? &tmap_b : &tmap_a, (t.first_kb + kb - (second ? num_kb / 2 : 0)) * BK, m0);
           }
           if (!PACKED) {
             if (B_MN) {
@@ -646,11 +672,12 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       int acc = 0;
       uint32_t acc_phase = 0;
       bool ok = true;
-      for (int tile = cluster_id; tile < num_tiles && ok; tile += num_clusters) {
+      for (int i = cluster_id; i < num_items && ok; i += num_clusters) {
+        const int item_kb = item_at(i).num_kb;
         const bool room = bounded_wait<PAIR>(ptx::smem_addr(&ctl->acc_empty[acc]), acc_phase ^ 1u, abort_flag, WAIT_MMA_ACC_EMPTY, 64);
         ptx::tc_fence_after();
         const uint32_t d_tmem = tmem_base + (uint32_t)(acc * MT * BN);
-        for (int kb = 0; kb < num_kb; ++kb) {
+        for (int kb = 0; kb < item_kb; ++kb) {
           bool got = room && bounded_wait<PAIR>(ptx::smem_addr(&ctl->full[stage]), phase, abort_flag, WAIT_MMA_FULL, PACKED ? 32 : 0);
           if (PACKED && got)
             got = bounded_wait<PAIR>(ptx::smem_addr(&ctl->full_b[stage_b]), phase_b, abort_flag, WAIT_MMA_FULL, 32);
@@ -696,10 +723,9 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
     // ------------------------------------------------------------ epilogue warps (dense kernels)
     int acc = 0;
     uint32_t acc_phase = 0;
-    for (int tile = cluster_id; tile < num_tiles; tile += num_clusters) {
-      int m_blk, n_blk;
-      tile_coords<PACKED, kBand>(tile, num_m, num_n, m_blk, n_blk);
-      if (!epilogue_tile(m_blk * C::kClusterM + rank * C::kTileM, n_blk, acc, acc_phase)) break;
+    for (int i = cluster_id; i < num_items; i += num_clusters) {
+      const Item t = item_at(i);
+      if (!epilogue_tile(t.m_blk * C::kClusterM + rank * C::kTileM, t.n_blk, t.part, acc, acc_phase)) break;
       if (++acc == C::kAccSets) { acc = 0; acc_phase ^= 1u; }
     }
   } else {
@@ -755,9 +781,9 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       long gk = 0;                                                // global index of the tile's K block 0
       int acc = 0;
       uint32_t acc_phase = 0;
-      for (int tile = cluster_id; tile < num_tiles && ok; tile += num_clusters) {
-        int m_blk, n_blk;
-        tile_coords<PACKED, kBand>(tile, num_m, num_n, m_blk, n_blk);
+      for (int item = cluster_id; item < num_items && ok; item += num_clusters) {
+        const Item it = item_at(item);
+        const int n_blk = it.n_blk, item_kb = it.num_kb;
         // this group's first K block of the tile (R = 2: K is a multiple of 128, so gk is even)
         const int kb_first = R * (int)(((long)grp - gk / R) & (NG - 1));
         const int wrow0 = B_MN ? (JOINT ? 0 : kb_first * BK) + kr : n_blk * kWeightRows + brow;
@@ -780,8 +806,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
             }
           } else if (JOINT) {
             if (valid) {
-              const bool second = 2 * kb >= num_kb;
-              const int k = second ? kb - num_kb / 2 : kb;
+              const bool second = 2 * (it.first_kb + kb) >= num_kb;
+              const int k = it.first_kb + kb - (second ? num_kb / 2 : 0);
               w.Wq = second ? p.other.Wq : p.Wq;
               w.s16 = second ? p.other.s16 : p.s16;
               w.zq = second ? p.other.zq : p.zq;
@@ -808,12 +834,12 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
         };
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-          if (kb_first + kStep * j < num_kb) fetch(j, kb_first + kStep * j);
-        for (int kb0 = kb_first; kb0 < num_kb && ok; kb0 += 2 * kStep) {
+          if (kb_first + kStep * j < item_kb) fetch(j, kb_first + kStep * j);
+        for (int kb0 = kb_first; kb0 < item_kb && ok; kb0 += 2 * kStep) {
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const int kb = kb0 + kStep * j;                         // first K block of the run (R = 2: kb + 1 < num_kb too)
-            if (ok && kb < num_kb) {
+            const int kb = kb0 + kStep * j;                         // first K block of the run (R = 2: kb + 1 < item_kb too)
+            if (ok && kb < item_kb) {
               const int stage = (int)((gk + kb) & (C::kStagesB - 1));   // R = 2: even; the run's second block is stage + 1
               const uint32_t phase = (uint32_t)(((gk + kb) / C::kStagesB) & 1);
               // packed codes: the stage must have been released by the tensor core; latent weights: the raw tile
@@ -881,7 +907,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
                     for (int c = 0; c < 8; ++c)
                       ptx::sts_128((row_sx + (uint32_t)u * C::kBBytes) ^ ((uint32_t)c << 4), 0u, 0u, 0u, 0u);
                 }
-                if (kb + 2 * kStep < num_kb) fetch(j, kb + 2 * kStep);
+                if (kb + 2 * kStep < item_kb) fetch(j, kb + 2 * kStep);
                 ptx::fence_proxy_async_smem();
               }
               ok = warp_agrees(free_stage);
@@ -895,9 +921,9 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
             }
           }
         }
-        gk += num_kb;
+        gk += item_kb;
         if (warp < 2 + C::kEpiWarps && ok) {
-          ok = epilogue_tile(m_blk * C::kClusterM + rank * C::kTileM, n_blk, acc, acc_phase);
+          ok = epilogue_tile(it.m_blk * C::kClusterM + rank * C::kTileM, n_blk, it.part, acc, acc_phase);
           if (++acc == C::kAccSets) { acc = 0; acc_phase ^= 1u; }
         }
       }
@@ -940,6 +966,24 @@ __global__ void finish_row_sums_kernel(const float* partial, int num_n, int out_
   }
   ds[o] = a;
   if (dz != nullptr) dz[o] = -__half2float(__ushort_as_half(ptx::ld_global(s16 + o))) * b;
+}
+
+// Adds up the clusters' sums in their order and rounds once: eight columns a thread.
+__global__ void __launch_bounds__(256) finish_split_kernel(const float* partial, int split, size_t vecs, eqat_bf16* D) {
+  ptx::grid_dependents_launch();
+  ptx::grid_dependency_wait();
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= vecs) return;
+  float v[8] = {};
+#pragma unroll 4
+  for (int s = 0; s < split; ++s) {
+    const uint4* at = reinterpret_cast<const uint4*>(partial) + ((size_t)s * vecs + i) * 2;
+    const uint4 a = ptx::ld_global(at), b = ptx::ld_global(at + 1);
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += __uint_as_float(w[e]);
+  }
+  reinterpret_cast<uint4*>(D)[i] = pack8(v);
 }
 
 // ------------------------------------------------------------------ host side
@@ -1039,7 +1083,8 @@ int launch(const Operand& a, const Operand& b, const GemmParams& p, cudaStream_t
   if (sms < C::kCtas) return EQAT_ERR_CUDA;
   constexpr int kColumns = EPI == EPI_GATED ? BN / 2 : BN;
   const int tiles = ((p.M + C::kClusterM - 1) / C::kClusterM) * ((p.N + kColumns - 1) / kColumns);
-  const int clusters = tiles < sms / C::kCtas ? tiles : sms / C::kCtas;
+  const int items = EPI == EPI_JOINT ? tiles * p.split : tiles;
+  const int clusters = items < sms / C::kCtas ? items : sms / C::kCtas;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(clusters * C::kCtas), 1, 1);
   cfg.blockDim = dim3(C::kThreads, 1, 1);
@@ -1171,8 +1216,7 @@ int launch_packed(const Operand& a, GemmParams& p, cudaStream_t st) {
 
 // Two packed weights (EPI_GATED: side by side in a tile, EPI_JOINT: one after the other along K).
 template <int EPI, bool B_MN, int BITS>
-int launch_two(const Operand& a, const Operand& b, GemmParams& p, cudaStream_t st) {
-  const TileShape s = packed_shape(p.M, EPI == EPI_GATED ? 2 * p.N : p.N, sm_count());
+int launch_two(const Operand& a, const Operand& b, GemmParams& p, const TileShape& s, cudaStream_t st) {
   if (s.bn == 128) return launch<1, false, B_MN, true, EPI, BITS, false, 128>(a, b, p, st);
   return s.pair ? launch<2, false, B_MN, true, EPI, BITS, true>(a, b, p, st)
                 : launch<2, false, B_MN, true, EPI, BITS, false>(a, b, p, st);
@@ -1280,26 +1324,73 @@ int launch_packed_gated(const eqat_desc& d, int activation, const eqat_bf16* X, 
   p.D = H;
   set_weight(p, d, gate.Wq_packed, gate.s16, gate.z);
   p.other = other_weight(up, activation, G, U);
+  const TileShape s = packed_shape(p.M, 2 * p.N, sm_count());
   const Operand a{X, (uint64_t)d.tokens, (uint64_t)d.in_features, false};
   switch (d.bits) {
-    case 2: return launch_two<EPI_GATED, false, 2>(a, a, p, st);
-    case 3: return launch_two<EPI_GATED, false, 3>(a, a, p, st);
-    default: return launch_two<EPI_GATED, false, 4>(a, a, p, st);
+    case 2: return launch_two<EPI_GATED, false, 2>(a, a, p, s, st);
+    case 3: return launch_two<EPI_GATED, false, 3>(a, a, p, s, st);
+    default: return launch_two<EPI_GATED, false, 4>(a, a, p, s, st);
   }
 }
 
+namespace {
+
+// Tiles of dX of two weights, and the parts of their K.
+struct JointPlan {
+  TileShape shape;
+  int split;
+};
+// The least expected time over the three shapes of packed tiles and up to eight parts of at least 16 K blocks.  A K block of 64
+// takes a cluster 0.42 / 0.49 / 0.47 us (2 / 3 / 4-bit codes) on tiles of 128 x 128, 0.88 / 1.13 / 1.15 on 256 x 256, 0.65 / 0.72 / 0.67
+// on the 512 x 256 of a pair, as in the forward (wide.cu); a tile's epilogue about 3 us; the parts' sums, at most 64 MB so that they
+// stay in L2, are written and read at about 5 TB/s.  2 x 11008 x 4096, 2 bits, 1 / 256 / 512 / 1200 tokens: 137, 140, 144, 228 us with K whole, 45, 61, 84, 211 split.
+JointPlan joint_plan(const eqat_desc& d, int sms) {
+  const int T = (int)d.tokens, in = d.in_features, kb = 2 * (d.out_features / BK);
+  const TileShape shapes[3] = {{1, false, 128}, {2, false, kBN}, {2, true, kBN}};
+  const double cost[3][3] = {{0.42, 0.49, 0.47}, {0.88, 1.13, 1.15}, {0.65, 0.72, 0.67}};
+  JointPlan best{shapes[0], 1};
+  double least = 0.0;
+  for (int i = 0; i < 3; ++i) {
+    const TileShape& s = shapes[i];
+    const long clusters = sms / (s.pair ? 2 : 1);
+    const long tiles = (long)((T + s.rows() - 1) / s.rows()) * ((in + s.bn - 1) / s.bn);
+    for (int split = 1; split <= 8 && clusters > 0; ++split) {
+      if (split > 1 && (kb < 16 * split || (double)split * T * in * 4.0 > 64e6)) break;
+      const long rounds = (tiles * split + clusters - 1) / clusters;
+      const double us = rounds * (((kb + split - 1) / split) * cost[i][d.bits - 2] + 3.0) +
+                        (split > 1 ? 4.0 + (double)split * T * in * 8.0 / 5.0e6 : 0.0);
+      if (least == 0.0 || us < least) {
+        least = us;
+        best = JointPlan{s, split};
+      }
+    }
+  }
+  return best;
+}
+
+}  // namespace
+
+size_t packed_gated_dx_workspace(const eqat_desc& d, int sms) {
+  const int split = joint_plan(d, sms).split;
+  return split == 1 ? 0 : (size_t)split * d.tokens * d.in_features * sizeof(float);
+}
+
 int launch_packed_gated_dx(const eqat_desc& d, const eqat_bf16* dG, const eqat_bf16* dU, const eqat_packed_weight& gate,
-                           const eqat_packed_weight& up, eqat_bf16* dX, cudaStream_t st) {
+                           const eqat_packed_weight& up, eqat_bf16* dX, void* workspace, cudaStream_t st) {
   GemmParams p = base_params((int)d.tokens, d.in_features, 2 * d.out_features);
   p.D = dX;
+  const JointPlan plan = joint_plan(d, sm_count());
+  p.split = plan.split;
+  p.partial = static_cast<float*>(workspace);
   set_weight(p, d, gate.Wq_packed, gate.s16, gate.z);
   p.other = other_weight(up, 0, nullptr, nullptr);
   const Operand a{dG, (uint64_t)d.tokens, (uint64_t)d.out_features, false}, b{dU, (uint64_t)d.tokens, (uint64_t)d.out_features, false};
-  switch (d.bits) {
-    case 2: return launch_two<EPI_JOINT, true, 2>(a, b, p, st);
-    case 3: return launch_two<EPI_JOINT, true, 3>(a, b, p, st);
-    default: return launch_two<EPI_JOINT, true, 4>(a, b, p, st);
-  }
+  const int rc = d.bits == 2   ? launch_two<EPI_JOINT, true, 2>(a, b, p, plan.shape, st)
+                 : d.bits == 3 ? launch_two<EPI_JOINT, true, 3>(a, b, p, plan.shape, st)
+                               : launch_two<EPI_JOINT, true, 4>(a, b, p, plan.shape, st);
+  if (rc != EQAT_OK || p.split == 1) return rc;
+  const size_t vecs = (size_t)d.tokens * d.in_features / 8;
+  return launch_overlapped(finish_split_kernel, dim3((unsigned)((vecs + 255) / 256)), dim3(256), 0, st, p.partial, p.split, vecs, dX);
 }
 
 size_t packed_ds_workspace_bytes(const eqat_desc& d) {

@@ -57,9 +57,10 @@ int launch_packed_dx(const eqat_desc& d, const eqat_bf16* dY, const uint8_t* Wq,
 // H = act(X * dequant(gate)^T) * (X * dequant(up)^T) in one kernel; G and U, the projections, or null.
 int launch_packed_gated(const eqat_desc& d, int activation, const eqat_bf16* X, const eqat_packed_weight& gate,
                         const eqat_packed_weight& up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, cudaStream_t st);
-// dX = dG * dequant(gate) + dU * dequant(up) in one contraction.
+// dX = dG * dequant(gate) + dU * dequant(up) in one contraction.  Few tokens need scratch, for sums over parts of K.
+size_t packed_gated_dx_workspace(const eqat_desc& d, int sms);
 int launch_packed_gated_dx(const eqat_desc& d, const eqat_bf16* dG, const eqat_bf16* dU, const eqat_packed_weight& gate,
-                           const eqat_packed_weight& up, eqat_bf16* dX, cudaStream_t st);
+                           const eqat_packed_weight& up, eqat_bf16* dX, void* workspace, cudaStream_t st);
 // ds (and optionally dz) reduced in the epilogue of dY^T * X.  One group per row needs
 // packed_ds_workspace_bytes(d) bytes of scratch for the per-tile partial sums (0 otherwise).
 size_t packed_ds_workspace_bytes(const eqat_desc& d);

@@ -364,16 +364,18 @@ PyObject* packed_gated_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// desc, activation, dH, G, U, gate, up, dX, dG, dU
+// desc, activation, dH, G, U, gate, up, dX, dG, dU, workspace
 PyObject* packed_gated_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return call(n, 10, [&] {
+  return call(n, 11, [&] {
     const auto d = structure<eqat_desc>(a[0]);
     const int act = number(a[1]);
     const double inner = (double)d.tokens * d.out_features;
     const auto *dH = dense(a[2], inner), *G = dense(a[3], inner), *U = dense(a[4], inner);
     const eqat_packed_weight gate = weight_of(a[5], d), up = weight_of(a[6], d);
     auto *dX = dense(a[7], (double)d.tokens * d.in_features), *dG = dense(a[8], inner), *dU = dense(a[9], inner);
-    return launch([&](void* s) { return g_packed_gated_bwd(&d, act, dH, G, U, &gate, &up, dX, dG, dU, s); });
+    size_t bytes = 0;
+    void* ws = bytes_of(a[10], &bytes);
+    return launch([&](void* s) { return g_packed_gated_bwd(&d, act, dH, G, U, &gate, &up, dX, dG, dU, ws, bytes, s); });
   });
 }
 

@@ -391,6 +391,16 @@ int launch_rows(WideParams& p, int bits, const eqat_bf16* X, int pairs, int spli
 
 }  // namespace
 
+// Expected time of the tiled kernel (the terms: below).
+double packed_tiled_us(const eqat_desc& d, int sms) {
+  const int T = (int)d.tokens, cols = (d.out_features + 255) / 256, kb = d.in_features / 64;
+  if (packed_shape(T, d.out_features, sms).bn == 128) return 5.0 + kb * (d.bits == 2 ? 0.48 : (d.bits == 3 ? 0.58 : 0.52));
+  if (T <= 256) return 8.0 + ((cols + sms - 1) / sms) * kb * (d.bits == 2 ? 0.88 : (d.bits == 3 ? 1.13 : 1.15));
+  const int tiles = cols * ((T + 511) / 512), slots = sms / 2;
+  return 8.0 + ((tiles + slots - 1) / slots) * kb * (d.bits == 2 ? 0.65 : (d.bits == 3 ? 0.72 : 0.67)) *
+                   (tiles * 5 > slots * 4 ? 1.1 : 1.0);
+}
+
 // Whether this kernel is expected to beat the tiled kernel of gemm.cu (512 or 256 TOKENS x 256 weight rows per tile, or 128 x
 // 128 where all of those fit the chip at once), and with which token tiles and split of K.  The terms are fits to timings on
 // the 7B, 13B and 70B shapes from 65 to 2048 tokens (within 15 %).  Here: a CTA costs 5 us plus 0.018 us per token column
@@ -449,17 +459,8 @@ bool wide_fwd_applies(const eqat_desc& d, int given_sms, WidePlan& best) {
       }
     }
   }
-  const int cols = (d.out_features + 255) / 256, kb = d.in_features / 64;
-  double tiled;
-  if (packed_shape(T, d.out_features, sms).bn == 128)
-    return best.us < 5.0 + kb * (d.bits == 2 ? 0.48 : (d.bits == 3 ? 0.58 : 0.52));
-  if (T <= 256) {
-    tiled = 8.0 + ((cols + sms - 1) / sms) * kb * (d.bits == 2 ? 0.88 : (d.bits == 3 ? 1.13 : 1.15));
-  } else {
-    const int tiles = cols * ((T + 511) / 512), slots = sms / 2;
-    tiled = 8.0 + ((tiles + slots - 1) / slots) * kb * (d.bits == 2 ? 0.65 : (d.bits == 3 ? 0.72 : 0.67)) *
-                      (tiles * 5 > slots * 4 ? 1.1 : 1.0);
-  }
+  const double tiled = packed_tiled_us(d, sms);
+  if (packed_shape(T, d.out_features, sms).bn == 128) return best.us < tiled;
   // With 4-bit codes this kernel takes 15 % more than its estimate on average, the tiled one 2 %, over 300 calls of 300 to
   // 4096 tokens (8192 x 28672, 2048 tokens: estimated 616 against 668 us, measured 910 against 760 us).
   return best.us * (d.bits == 4 ? 1.08 : 1.0) < 0.95 * tiled;

@@ -15,6 +15,8 @@ struct WidePlan {
 // True when the kernel is the one to take for this packed forward, and how: on the current device (sms = 0), or on one of
 // `sms` SMs that are grouped like a B200's.
 bool wide_fwd_applies(const eqat_desc& d, int sms, WidePlan& plan);
+// Expected time of the tiled kernel of gemm.cu for more than 64 tokens on a device of `sms` SMs.
+double packed_tiled_us(const eqat_desc& d, int sms);
 // Y[T,out] = X[T,in] * dequant(Wq)^T
 int launch_wide_fwd(const eqat_desc& d, const eqat_bf16* X, const uint8_t* Wq, const eqat_fp16* s16, const void* zq,
                     eqat_bf16* Y, const WidePlan& plan, cudaStream_t st);

@@ -144,8 +144,8 @@ def test_packed_gated_arguments(eqat):
     def fwd(d=desc, act=0, X=A, gate=good, up=good, H=A, G=A, U=A):
         return eqat.lib.qlinear_packed_gated_fwd(d and ctypes.byref(d), act, X, gate and ctypes.byref(gate), up and ctypes.byref(up), H, G, U, None, 0, None)
 
-    def bwd(d=desc, act=0, dH=A, G=A, U=A, gate=good, up=good, dX=A, dG=A, dU=A):
-        return eqat.lib.qlinear_packed_gated_bwd(d and ctypes.byref(d), act, dH, G, U, gate and ctypes.byref(gate), up and ctypes.byref(up), dX, dG, dU, None)
+    def bwd(d=desc, act=0, dH=A, G=A, U=A, gate=good, up=good, dX=A, dG=A, dU=A, w=A, n=1 << 30):
+        return eqat.lib.qlinear_packed_gated_bwd(d and ctypes.byref(d), act, dH, G, U, gate and ctypes.byref(gate), up and ctypes.byref(up), dX, dG, dU, w, n, None)
 
     for call, names in ((fwd, ("d", "X", "gate", "up", "H", "G", "U")), (bwd, ("d", "dH", "G", "U", "gate", "up", "dX", "dG", "dU"))):
         for name in names:
@@ -169,9 +169,10 @@ def test_a_workspace_is_needed_where_the_projections_pass_through_memory(eqat):
     for bits in (2, 3, 4):
         for T in (1, 8, 37, 64, 100, 300, 600, 5000, 20000):
             d = eqat.make_desc(bits, 64, 11008, 4096, T)
-            need, route = eqat.packed_gated_workspace_bytes(d), eqat.eqat_packed_gated_route(d, 148)
+            need, route = eqat.workspace_bytes(d, eqat.EQAT_OP_PACKED_GATED_FWD), eqat.eqat_packed_gated_route(d, 148)
             seen.add(route)
-            assert route == eqat.eqat_packed_fwd_route(eqat.make_desc(bits, 64, 22016, 4096, T), 148)[0]
+            rows = eqat.eqat_packed_fwd_route(eqat.make_desc(bits, 64, 22016, 4096, T), 148)[0]
+            assert route == rows or (rows, route) == (eqat.EQAT_ROUTE_WEIGHT_ROW_PAIRS, eqat.EQAT_ROUTE_TILED)
             assert (need > 0) == (route == eqat.EQAT_ROUTE_WEIGHT_ROW_PAIRS)
             if need:
                 assert need >= 2 * T * 11008 * 2 and need % 512 == 0
@@ -179,8 +180,24 @@ def test_a_workspace_is_needed_where_the_projections_pass_through_memory(eqat):
                     assert eqat.lib.qlinear_packed_gated_fwd(ctypes.byref(d), 0, A, ctypes.byref(W), ctypes.byref(W), A, None, None, *ws, None) == eqat.EQAT_ERR_WORKSPACE
     assert seen == {eqat.EQAT_ROUTE_MATRIX_VECTOR, eqat.EQAT_ROUTE_WEIGHT_ROWS, eqat.EQAT_ROUTE_WEIGHT_ROW_PAIRS, eqat.EQAT_ROUTE_TILED}
     assert eqat.lib.eqat_packed_gated_route(ctypes.byref(eqat.make_desc(2, 64, 256, 256, 4)), -1) == eqat.EQAT_ERR_SHAPE
-    with pytest.raises(eqat.EqatError):
-        eqat.packed_gated_workspace_bytes(eqat.make_desc(2, 64, 96, 256, 5))
+    for op in (eqat.EQAT_OP_PACKED_GATED_FWD, eqat.EQAT_OP_PACKED_GATED_BWD):
+        with pytest.raises(eqat.EqatError):
+            eqat.workspace_bytes(eqat.make_desc(2, 64, 96, 256, 5), op)
+
+
+def test_few_tokens_split_the_contraction(eqat):
+    """The parts of the backward pass's sums: at most eight, each with work, none for batches that fill the chip."""
+    W = eqat.eqat_packed_weight(A, A, A)
+    for out, width in ((64, 128), (192, 384), (1408, 2048), (11008, 4096), (28672, 8192), (64, 9600)):
+        for T in (1, 128, 129, 256, 300, 600, 1000, 2000, 4096, 20000):
+            d = eqat.make_desc(2, 64, out, width, T)
+            need = eqat.workspace_bytes(d, eqat.EQAT_OP_PACKED_GATED_BWD)
+            parts, rest = divmod(need, 4 * T * width)
+            assert rest == 0 and parts != 1 and parts <= 8 and 2 * out // 64 >= 16 * parts and need <= 64e6
+            assert T > 128 or out < 1408 or parts >= 2
+            if need:
+                for ws in ((None, need), (A, need - 1), (A + 128, need)):
+                    assert eqat.lib.qlinear_packed_gated_bwd(ctypes.byref(d), 0, A, A, A, ctypes.byref(W), ctypes.byref(W), A, A, A, *ws, None) == eqat.EQAT_ERR_WORKSPACE
 
 
 def test_tensors_are_checked_before_the_call(eqat):

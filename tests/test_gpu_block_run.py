@@ -75,7 +75,7 @@ class Block:
         b["cache"] = eqat.make_cache_desc(GROUP, D, KV, 16, 20, 2, 5, T)
         b["attn"] = eqat.make_attention_desc(HEADS, new, D ** -0.5)
         b["gated"] = self.gate.desc(T)
-        for name, need in (("ws1", eqat.cache_workspace_bytes(b["cache"], b["attn"])), ("ws2", eqat.packed_gated_workspace_bytes(b["gated"]))):
+        for name, need in (("ws1", eqat.cache_workspace_bytes(b["cache"], b["attn"])), ("ws2", eqat.workspace_bytes(b["gated"], eqat.EQAT_OP_PACKED_GATED_FWD))):
             b[name] = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
         b["off"], b["len"] = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
         return b
@@ -164,13 +164,15 @@ def test_training_pass(eqat):
     norm = eqat.make_norm_desc(T, E, EPS)
     ws = torch.empty(eqat.rms_norm_workspace_bytes(norm), dtype=torch.uint8, device="cuda")
     desc = block.gate.desc(T)
+    need = eqat.workspace_bytes(desc, eqat.EQAT_OP_PACKED_GATED_BWD)
+    ws_dx = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
 
     def step():
         eqat.eqat_rms_norm_fwd(norm, x, dout, block.w1, h, y)
         eqat.qlinear_packed_gated_fwd(desc, eqat.EQAT_ACT_SILU, y, block.gate.on, block.up.on, f, G, U)
         block.down(f, out)
         eqat.qlinear_packed_bwd_dx(block.down.desc(T), dout, *block.down.on, df)
-        eqat.qlinear_packed_gated_bwd(desc, eqat.EQAT_ACT_SILU, df, G, U, block.gate.on, block.up.on, dy, dG, dU)
+        eqat.qlinear_packed_gated_bwd(desc, eqat.EQAT_ACT_SILU, df, G, U, block.gate.on, block.up.on, dy, dG, dU, ws_dx)
         for w, d, ds in ((block.gate, dG, ds_gate), (block.up, dU, ds_up)):
             eqat.qlinear_packed_bwd_ds(desc, y, d, w.on[0], w.on[2], None, ds)
         eqat.eqat_rms_norm_bwd(norm, dy, h, block.w1, dout, dh, dw, ws)

@@ -126,6 +126,8 @@ def forward_cases():
     yield from ((1029, 1088, 768, b, g, z, "silu") for b in (2, 3, 4) for g, z in ((64, True), (256, False)))
     yield (4099, 4160, 256, 2, 64, False, "silu")                   # pairs of CTAs, ragged in both directions
     yield (2500, 4224, 512, 3, 32, True, "gelu_tanh")
+    yield from ((200, 11008, 256, b, 64, z, k) for b, z, k in ((2, False, "silu"), (3, True, "gelu"), (4, False, "gelu_tanh")))   # single CTAs of 256 rows
+    yield from ((257, 11008, 128, b, 128, False, "silu") for b in (2, 3, 4))
     yield (1, 11008, 4096, 2, 64, False, "silu")
     yield (7, 4096, 5120, 3, 128, False, "gelu")
     yield (3, 2048, 11008, 4, 128, True, "silu")
@@ -138,7 +140,7 @@ def test_packed_forward(eqat, T, out, width, bits, group, fp16, kind):
     gate, up = both_weights(out, width, bits, group, fp16)
     X, buf = normal(T, width, seed=3), Guarded()
     d = eqat.make_desc(bits, group, out, width, T, 0, eqat.EQAT_ZP_FP16 if fp16 else eqat.EQAT_ZP_U8)
-    need = eqat.packed_gated_workspace_bytes(d)
+    need = eqat.workspace_bytes(d, eqat.EQAT_OP_PACKED_GATED_FWD)
     H, G, U, H2 = (buf.empty(T, out, dtype=torch.bfloat16, shift_bytes=16 * i) for i in range(4))
     act = act_code(eqat, kind)
     eqat.qlinear_packed_gated_fwd(d, act, X, gate.on, up.on, H, G, U)
@@ -158,14 +160,18 @@ def test_packed_forward(eqat, T, out, width, bits, group, fp16, kind):
 
 @pytest.mark.parametrize("T,out,width,bits,group,fp16,kind", [
     (1, 64, 128, 2, 64, False, "silu"), (5, 128, 256, 3, 32, True, "gelu"), (130, 192, 384, 4, 128, False, "gelu_tanh"), (300, 320, 640, 2, 640, False, "silu"),
-    (1029, 1088, 768, 3, 256, True, "silu"), (1029, 1088, 768, 2, 64, False, "gelu"), (3000, 448, 4224, 4, 32, False, "silu"), (2100, 11008, 512, 2, 64, True, "silu")])
+    (1029, 1088, 768, 3, 256, True, "silu"), (1029, 1088, 768, 2, 64, False, "gelu"), (3000, 448, 4224, 4, 32, False, "silu"), (2100, 11008, 512, 2, 64, True, "silu"),
+    (1, 11008, 4096, 2, 64, False, "silu"), (130, 4096, 2048, 4, 128, False, "silu"), (640, 1088, 4096, 3, 64, True, "gelu"), (70, 2112, 512, 2, 64, False, "silu"),
+    (150, 64, 9600, 2, 64, False, "silu"), (150, 128, 9600, 3, 128, True, "silu"), (256, 64, 9600, 4, 32, False, "gelu")])
 def test_packed_backward(eqat, T, out, width, bits, group, fp16, kind):
     gate, up = both_weights(out, width, bits, group, fp16)
     dH, G, U, buf = normal(T, out, seed=4, std=0.1), normal(T, out, seed=5, std=1.5), normal(T, out, seed=6), Guarded()
     d = eqat.make_desc(bits, group, out, width, T, 0, eqat.EQAT_ZP_FP16 if fp16 else eqat.EQAT_ZP_U8)
     dX, dG, dU = buf.empty(T, width, dtype=torch.bfloat16), *(buf.empty(T, out, dtype=torch.bfloat16, shift_bytes=16) for _ in range(2))
     act = act_code(eqat, kind)
-    eqat.qlinear_packed_gated_bwd(d, act, dH, G, U, gate.on, up.on, dX, dG, dU)
+    need = eqat.workspace_bytes(d, eqat.EQAT_OP_PACKED_GATED_BWD)
+    ws = buf.empty(need, dtype=torch.uint8) if need else None
+    eqat.qlinear_packed_gated_bwd(d, act, dH, G, U, gate.on, up.on, dX, dG, dU, ws)
     buf.check()
     assert eqat.device_status() == (0, 0)
     check_grads(torch_to_f64(dG), torch_to_f64(dU), torch_to_f64(dH), torch_to_f64(G), torch_to_f64(U), kind)
@@ -174,7 +180,9 @@ def test_packed_backward(eqat, T, out, width, bits, group, fp16, kind):
     assert_elementwise(torch_to_f64(dX), ref, contraction_bound(ref, size, square), "dX")
     # gradients in place of the projections; the same bits
     G2, U2, dX2 = G.clone(), U.clone(), torch.empty_like(dX)
-    eqat.qlinear_packed_gated_bwd(d, act, dH, G2, U2, gate.on, up.on, dX2, G2, U2)
+    if need:
+        ws.fill_(0xFF)
+    eqat.qlinear_packed_gated_bwd(d, act, dH, G2, U2, gate.on, up.on, dX2, G2, U2, ws)
     assert torch.equal(G2, dG) and torch.equal(U2, dU) and torch.equal(dX2, dX)
 
 
@@ -206,7 +214,7 @@ def test_the_weights_are_not_mixed_up(eqat):
         codes = [torch.full((out, width // 4), v * 0x55, dtype=torch.uint8, device="cuda") for v in (1, 2)]
         s, z = torch.ones(out, 2, dtype=torch.float16, device="cuda"), torch.zeros(out, 2, dtype=torch.uint8, device="cuda")
         H = torch.empty(T, out, dtype=torch.bfloat16, device="cuda")
-        need = eqat.packed_gated_workspace_bytes(d)
+        need = eqat.workspace_bytes(d, eqat.EQAT_OP_PACKED_GATED_FWD)
         ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
         for a, b in ((1, 2), (2, 1)):
             eqat.qlinear_packed_gated_fwd(d, eqat.EQAT_ACT_SILU, X, (codes[a - 1], s, z), (codes[b - 1], s, z), H, None, None, ws)
@@ -219,7 +227,7 @@ def test_captured_on_another_stream(eqat):
     gate, up = both_weights(out, width, 2, 64, False)
     for T in (1, 24, 200, 1500):
         d = eqat.make_desc(2, 64, out, width, T)
-        need = eqat.packed_gated_workspace_bytes(d)
+        need = eqat.workspace_bytes(d, eqat.EQAT_OP_PACKED_GATED_FWD)
         ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
         X, H = normal(T, width, seed=7), torch.empty(T, out, dtype=torch.bfloat16, device="cuda")
         call = lambda: eqat.qlinear_packed_gated_fwd(d, eqat.EQAT_ACT_GELU, X, gate.on, up.on, H, None, None, ws)  # noqa: E731
