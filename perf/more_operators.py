@@ -398,7 +398,7 @@ def _plan(s):
         return eqat, eqat.make_gated_desc(c["rows"], c["features"], act), None
     zeros = eqat.EQAT_ZP_U8 if c["zeros"] == "u8" else eqat.EQAT_ZP_FP16
     desc = eqat.make_desc(c["bits"], c["group"], c["inner"], c["width"], c["tokens"], 0, zeros)
-    need = 0 if c["backward"] or c["keep"] else eqat.packed_gated_workspace_bytes(desc)
+    need = 0 if c["keep"] else eqat.workspace_bytes(desc, eqat.EQAT_OP_PACKED_GATED_BWD if c["backward"] else eqat.EQAT_OP_PACKED_GATED_FWD)
     return eqat, desc, (act, torch.empty(need, dtype=torch.uint8, device=DEV) if need else None)
 
 
@@ -424,7 +424,7 @@ def _call(s):
         return s["H"]
     act, scratch = more
     if c["backward"]:
-        eqat.qlinear_packed_gated_bwd(desc, act, s["dH"], s["G"], s["U"], s["gate"], s["up"], s["dX"], s["dG"], s["dU"])
+        eqat.qlinear_packed_gated_bwd(desc, act, s["dH"], s["G"], s["U"], s["gate"], s["up"], s["dX"], s["dG"], s["dU"], scratch)
         return [s["dX"], s["dG"], s["dU"]]
     eqat.qlinear_packed_gated_fwd(desc, act, s["X"], s["gate"], s["up"], s["H"], s["G"], s["U"], scratch)
     return [s["H"], s["G"], s["U"]] if c["keep"] else s["H"]
