@@ -223,7 +223,7 @@ slim_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   constexpr int kWeightRows = GATED ? kRows / 2 : kRows;   // of a weight in a tile
   const int t0 = (int)blockIdx.z * C::kTn, m0 = (int)blockIdx.x * kWeightRows;
   // Row rr of the tile: a row of a weight, whose parameters start here, or past its end.
-  auto weight_row = [&](int rr) { return m0 + (rr & (kWeightRows - 1)); };
+  auto weight_row = [&](int rr) { return m0 + (GATED ? rr & (kWeightRows - 1) : rr); };
   auto step_sizes = [&](int rr) { return GATED && rr >= kWeightRows ? p.other.s16 : p.s16; };
   auto zero_points = [&](int rr) { return GATED && rr >= kWeightRows ? p.other.zq : p.zq; };
   int run0, nruns, group0;
@@ -355,7 +355,8 @@ slim_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
       const int items = pairs ? ngroups >> 1 : ngroups;    // per row
       int k = 0;
       while (k < 5 && (1 << k) < items) ++k;
-      const int rstep = 32 >> k;
+      const int rstep = 32 >> k, rows_live = min(kWeightRows, p.out_features - m0);      // of each weight
+      auto live = [&](int rr) { return GATED ? rr < kRows && (rr & (kWeightRows - 1)) < rows_live : rr < rows_live; };
       const int steps = ((kRows / rstep) + C::kRowWarps - 1) / C::kRowWarps;
       constexpr int kBatch = 8;                            // items in flight per lane
       uint32_t all_z = 0u;
@@ -366,7 +367,7 @@ slim_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
           for (int i = 0; i < kBatch; ++i) {
             const int rr = ((i0 + i) * C::kRowWarps + warp - 2) * rstep + (lane >> k);
             vs[i] = vz[i] = 0u;
-            if (rr < kRows && weight_row(rr) < p.out_features) {
+            if (live(rr)) {
               const size_t gi = (size_t)weight_row(rr) * p.groups_per_row + group0 + (pairs ? 2 * c : c);
               const eqat_fp16* z16 = static_cast<const eqat_fp16*>(zero_points(rr)) + gi;
               const uint8_t* z8 = static_cast<const uint8_t*>(zero_points(rr)) + gi;
