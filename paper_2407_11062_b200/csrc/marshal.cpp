@@ -297,7 +297,7 @@ PyObject* rotary(PyObject* const* a, Py_ssize_t n, decltype(&eqat_rotary_fwd) en
     auto* Q_out = rows_of(a[4], d.rows, d.q_heads, d.head_dim, &qop);
     const eqat_bf16* K = nullptr;
     eqat_bf16* K_out = nullptr;
-    if (a[2] != Py_None || a[5] != Py_None || d.kv_heads > 0) {
+    if (d.kv_heads > 0) {
       K = rows_of(a[2], d.rows, d.kv_heads, d.head_dim, &kp);
       K_out = rows_of(a[5], d.rows, d.kv_heads, d.head_dim, &kop);
     }

@@ -6,8 +6,13 @@
 // One pass: each tensor crosses HBM once, 8 bytes an element forward with a residual (7 + 4/group with codes in place of y), 8
 // backward.  A thread owns the same columns of every row it meets, so w is read once a block and dw is added up in registers.
 // What a thread will read of the next rows it copies into shared memory itself (cp.async, up to two rows ahead): nobody else
-// reads its places, so a row costs no barrier but that of the sum, and the copies run on through it.  A block with a single
-// row loads into registers.
+// reads its places, so a row costs no barrier but that of the sum, and the copies run on through it.  Blocks with a single row,
+// and the forward pass without codes, load into registers.
+//
+// Times on a B200, states larger than L2 (of a copy's bandwidth): forward of 8191 x 5120 with a residual 54.7 us (0.94), of 2001 x
+// 8192 in e4m3 26.4 us (0.86: conversions and the groups' maxima), backward of 4096 x 4096 26.2 us (0.78; 22.4 us without dw, whose
+// partial sums are a launch of 3 us), one row of 4096 2.6 us, a launch.  Before the ring and with the row unpacked twice the
+// backward pass took 38.2 us, 9 of them the sum of the partial sums by eight warps of a block.
 #include <cuda_fp8.h>
 
 #include "between.cuh"
@@ -395,13 +400,12 @@ struct Launch {
   int blocks, stages;
   size_t smem;
 };
-// `tensors` in the ring; `busy`: threads of an SM that the kernel's registers leave room for.
-Launch launch_shape(int64_t rows, const RowShape& s, int tensors, int busy, int sms) {
+// `tensors` in the ring; `busy`: threads of an SM that the kernel's registers leave room for; `stages`: at most.
+Launch launch_shape(int64_t rows, const RowShape& s, int tensors, int busy, int stages, int sms) {
   const int threads = s.threads == 32 ? kBlock : s.threads, rows_of_block = s.threads == 32 ? kBlock / 32 : 1;
   const int stage = threads * s.vpt * tensors * 16;
   int per_sm = busy / threads < 1 ? 1 : busy / threads;
-  // two rows ahead, if need be with fewer blocks; one row ahead where three stages do not fit an SM
-  int stages = 3;
+  // all stages, if need be with fewer blocks; fewer stages where they do not fit an SM
   while (per_sm > 1 && per_sm * stages * stage > kRingBytes) --per_sm;
   while (stages > 1 && stages * stage > kRingBytes) --stages;
   const int64_t need = (rows + rows_of_block - 1) / rows_of_block, most = (int64_t)sms * per_sm;
@@ -409,7 +413,7 @@ Launch launch_shape(int64_t rows, const RowShape& s, int tensors, int busy, int 
 }
 Launch backward_shape(const eqat_norm_desc& d, int sms) {
   const RowShape s = row_shape(d.features / 8);
-  Launch l = launch_shape(d.rows, s, 3, 512, sms);
+  Launch l = launch_shape(d.rows, s, 3, 512, 3, sms);
   const size_t share = (size_t)(kBlock / 32) * d.features * sizeof(float);
   if (s.threads == 32 && l.smem < share) l.smem = share;
   return l;
@@ -425,10 +429,10 @@ template <int VPT, bool WARP, int CODES>
 int launch_codes(const eqat_norm_desc& d, const NormFwd& p, const RowShape& s, int sms, cudaStream_t st) {
   static SmemOptIn opt_in[2];
   const int threads = WARP ? kBlock : s.threads;
-  Launch l = launch_shape(d.rows, s, p.R != nullptr ? 2 : 1, 1024, sms);
+  Launch l = launch_shape(d.rows, s, p.R != nullptr ? 2 : 1, 1024, 2, sms);
   // Without codes the blocks are many and HBM sets the pace: twice as many as an SM holds, loading into registers, took 55.3 us
   // of 8191 x 5120 (a block for each row 55.4), the ring 60.5.  With codes it is the instructions, and the copies under them
-  // are worth it: 2001 x 8192 in e4m3 31.0 and 28.1 us.
+  // are worth it: 2001 x 8192 in e4m3 29.5 us without the ring, 26.4, 27.5, 29.5 with one, two, three rows ahead.
   const int64_t need = (d.rows + (WARP ? kBlock / 32 : 1) - 1) / (WARP ? kBlock / 32 : 1), twice = (int64_t)sms * (2048 / threads);
   if constexpr (CODES != EQAT_CODES_NONE) {
     if (need > l.blocks) return launch_with(norm_fwd_kernel<VPT, WARP, CODES, true>, opt_in[0], l, threads, st, p, l.stages);

@@ -127,6 +127,15 @@ def test_values_that_are_no_numbers(eqat, n):
     assert scales[:, 0].isnan().tolist() == [False, True, False, True, True, False] and Y[1].isnan().all()
 
 
+def test_rows_beyond_the_range(eqat):
+    """Squares past binary32: zeros.  No eps and no size: NaN; no eps and a small row: as by the formula."""
+    X = torch.ones(4, 128, dtype=torch.bfloat16, device="cuda")
+    X[1], X[2], X[3] = 2.0 ** 100, 0, 2.0 ** -30
+    W, Y = weight_of(128, 30), torch.empty_like(X)
+    eqat.eqat_rms_norm_fwd(eqat.make_norm_desc(4, 128, 0.0), X, None, W, None, Y)
+    assert torch.equal(Y[0], W) and (Y[1] == 0).all() and Y[2].isnan().all() and torch.equal(Y[3], W)
+
+
 @pytest.mark.parametrize("rows,n", SHAPES)
 @pytest.mark.parametrize("residual", [True, False])
 def test_backward(eqat, rows, n, residual):

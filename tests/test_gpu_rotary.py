@@ -136,6 +136,15 @@ def test_gradient_is_the_transpose(eqat):
         assert abs(float(a.sum() - b.sum())) <= 8 * HALF_STEP * float((a.square().sum() + b.square().sum()).sqrt())
 
 
+def test_without_keys_nothing_is_asked_of_them(eqat):
+    Q, pos = heads(5, 2, 64, 12), torch.arange(5, dtype=torch.int32, device="cuda")
+    turns, d = eqat.rotary_turns(64).cuda(), eqat.make_rotary_desc(5, 2, 0, 64)
+    got = [torch.empty_like(Q) for _ in range(2)]
+    eqat.eqat_rotary_fwd(d, Q, None, turns, got[0], None, pos)
+    eqat.eqat_rotary_fwd(d, Q, torch.empty(0), turns, got[1], Q, pos)
+    assert torch.equal(*got)
+
+
 def test_captured(eqat):
     """A captured call serves other lengths and tables."""
     off, lens = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, 1, 2], [9, 100]))
