@@ -464,8 +464,8 @@ int eqat_cache_attention(const eqat_cache_desc* desc, const eqat_attention_desc*
  * bf16(q * scale), what the codes stand for, as K_hat of eqat_cache_append.  A row
  * with a NaN gives NaN in y and the scales, one with an infinity NaN where it
  * stands (its group) and zeros elsewhere; codes of such groups may be anything.  A
- * row whose sum of squares passes binary32 gives zeros, with eps = 0 a row of zeros
- * gives NaN.
+ * row whose sum of squares passes binary32 gives zeros (NaN where h * w passes it
+ * too), with eps = 0 a row of zeros gives NaN.
  *
  * features: a multiple of 8, at most 32768.  group (with codes): 32, 64, 128 or 256
  * dividing features, or features itself; 0 without codes. */
@@ -518,8 +518,8 @@ enum { EQAT_ROTARY_HALVES = 0, EQAT_ROTARY_PAIRS = 1 };
 
 typedef struct {
   int64_t rows;
-  int32_t q_heads;            /* at least 1                                           */
-  int32_t kv_heads;           /* 0: no keys                                           */
+  int32_t q_heads;            /* 1 .. 16384                                           */
+  int32_t kv_heads;           /* 0 .. 16384; 0: no keys                               */
   int32_t head_dim;           /* a multiple of 8, at most 512                         */
   int32_t rotary_dim;         /* even, 2 .. head_dim                                  */
   int32_t layout;             /* EQAT_ROTARY_HALVES or _PAIRS                         */

@@ -179,8 +179,7 @@ int launch_rotary(const eqat_rotary_desc& d, const RotaryRows& rows, bool backwa
   const bool in_place = rows.q == rows.q_out && (d.kv_heads == 0 || rows.k == rows.k_out);
   p.turned = halves || !vectors ? d.rotary_dim / 2 / wide : d.rotary_dim / wide;
   p.rest = in_place ? 0 : (d.head_dim - d.rotary_dim) / wide;
-  const int64_t chunks = ((int64_t)p.heads * (p.turned + p.rest) + kThreads - 1) / kThreads;
-  if (chunks > 65535) return EQAT_ERR_SHAPE;
+  const int64_t chunks = ((int64_t)p.heads * (p.turned + p.rest) + kThreads - 1) / kThreads;      // below 2^16: 2^15 heads of 511 items
   // several rows a block where there are enough blocks all the same
   int64_t per = d.rows * chunks / ((int64_t)sms * 8);
   p.block_rows = (int)(per < 1 ? 1 : per > kMaxRows ? kMaxRows : per);

@@ -319,3 +319,12 @@ def test_oracle_e4m3():
     rng = np.random.default_rng(3)
     x = np.concatenate([every, (every[1:] + every[:-1]) / 2, rng.uniform(-448, 448, 4000), rng.uniform(-0.02, 0.02, 4000)]).astype(np.float32)
     assert np.array_equal(B.e4m3(x), torch.from_numpy(x).to(torch.float8_e4m3fn).double().numpy())
+
+
+def test_rows_of_many_heads(eqat):
+    """What a row may hold at most fits the grid; more is refused."""
+    most = dict(head_dim=512, rotary_dim=2, layout=0)
+    for q, k in ((16385, 1), (1, 16385), (65536, 0)):
+        d = eqat.make_rotary_desc(**{**ROTARY, **most, "q_heads": q, "kv_heads": k})
+        assert _rotary(eqat, d, qp=512 << 17, kp=512 << 17, qop=512 << 17, kop=512 << 17) == eqat.EQAT_ERR_SHAPE
+    assert (2 * 16384 * (1 + 510) + 255) // 256 < 1 << 16
