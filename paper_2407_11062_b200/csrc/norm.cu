@@ -7,9 +7,9 @@
 // backward.  A thread owns the same columns of every row it meets, so w is read once a block and dw is added up in registers.
 // What a thread will read of the next rows it copies into shared memory itself (cp.async, up to two rows ahead): nobody else
 // reads its places, so a row costs no barrier but that of the sum, and the copies run on through it.  Blocks with a single row,
-// and the forward pass without codes, load into registers.
+// and the forward pass without codes, load into registers, 32 bytes at a time where everything is aligned to them.
 //
-// Times on a B200, states larger than L2 (of a copy's bandwidth): forward of 8191 x 5120 with a residual 54.7 us (0.94), of 2001 x
+// Times on a B200, states larger than L2 (of a copy's bandwidth): forward of 8191 x 5120 with a residual 52.4 us (0.98), of 2001 x
 // 8192 in e4m3 26.4 us (0.86: conversions and the groups' maxima), backward of 4096 x 4096 26.2 us (0.78; 22.4 us without dw, whose
 // partial sums are a launch of 3 us), one row of 4096 2.6 us, a launch.  Before the ring and with the row unpacked twice the
 // backward pass took 38.2 us, 9 of them the sum of the partial sums by eight warps of a block.
@@ -17,6 +17,7 @@
 
 #include "between.cuh"
 #include "common.cuh"
+#include "pieces.cuh"
 #include "ptx.cuh"
 
 namespace eqat {
@@ -44,6 +45,12 @@ __device__ __forceinline__ uint32_t add_pair(uint32_t a, uint32_t b) {
 __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
   return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
 }
+
+__device__ __forceinline__ void two_vectors(const Piece<16>& v, uint4& a, uint4& b) {
+  a = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+  b = make_uint4(v.w[4], v.w[5], v.w[6], v.w[7]);
+}
+__device__ __forceinline__ Piece<16> one_piece(const uint4& a, const uint4& b) { return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}}; }
 
 // The sum of a pair and the maximum of a third over the threads of a row: a warp, or the block.  `red` is used in turns: a
 // thread that writes the same half again has passed the barrier of the turn between, and so have all the readers.
@@ -93,15 +100,21 @@ struct NormFwd {
   int lanes;                                         // codes: vectors of a group (4 .. 32 neighbouring lanes), or 0: the row
 };
 
-// VPT vectors of a row per thread.  A row belongs to a warp (WARP) or to the block.
-template <int VPT, bool WARP, int CODES, bool RING>
+// VPT vectors of a row per thread.  A row belongs to a warp (WARP) or to the block.  How it comes in: by the ring, or by loads of a
+// vector or of two neighbours, which are the same places whether they come as one piece or, for want of alignment, as two: a sum's
+// order hangs on the shape alone.
+enum Loads : int { BY_RING, BY_VECTORS, BY_NEIGHBOURS, BY_PAIRS };
+template <int VPT, bool WARP, int CODES, int LOADS>
 __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(const NormFwd p, int stages) {
   __shared__ Reduced red[2][32];
   extern __shared__ __align__(16) uint8_t ring[];
+  constexpr bool RING = LOADS == BY_RING, PAIRS = LOADS == BY_PAIRS, NEXT = PAIRS || LOADS == BY_NEIGHBOURS;
+  static_assert(!NEXT || (CODES == EQAT_CODES_NONE && VPT % 2 == 0), "two neighbours");
   const int lane = threadIdx.x & 31;
   const int at = WARP ? lane : (int)threadIdx.x, span = WARP ? 32 : (int)blockDim.x;
   const int step = (int)gridDim.x * (WARP ? kBlock / 32 : 1);
   const int first = WARP ? (int)blockIdx.x * (kBlock / 32) + (int)(threadIdx.x >> 5) : (int)blockIdx.x;
+  auto place = [&](int i) { return NEXT ? ((i >> 1) * span + at) * 2 + (i & 1) : at + i * span; };      // of vector i of this thread
   constexpr float kTop = CODES == EQAT_CODES_INT8 ? 127.0f : 448.0f;
   const bool residual = p.R != nullptr;
   const uint32_t mine = ptx::smem_addr(ring) + threadIdx.x * 16, pitch = blockDim.x * 16;      // of this thread; to its next vector
@@ -109,15 +122,15 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(c
   ptx::grid_dependency_wait();
   auto ask = [&](int row, int stage) {
     if (row < p.rows) {
-      const size_t base = (size_t)row * p.vecs + at;
+      const size_t base = (size_t)row * p.vecs;
       uint32_t dst = mine + stage * stage_bytes;
 #pragma unroll
       for (int i = 0; i < VPT; ++i, dst += pitch)
-        if (at + i * span < p.vecs) copy_16(dst, reinterpret_cast<const uint4*>(p.X) + base + i * span);
+        if (place(i) < p.vecs) copy_16(dst, reinterpret_cast<const uint4*>(p.X) + base + place(i));
       if (residual) {
 #pragma unroll
         for (int i = 0; i < VPT; ++i, dst += pitch)
-          if (at + i * span < p.vecs) copy_16(dst, reinterpret_cast<const uint4*>(p.R) + base + i * span);
+          if (place(i) < p.vecs) copy_16(dst, reinterpret_cast<const uint4*>(p.R) + base + place(i));
       }
     }
     copies_issued();
@@ -129,11 +142,11 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(c
   uint4 w[VPT];
 #pragma unroll
   for (int i = 0; i < VPT; ++i)
-    w[i] = at + i * span < p.vecs ? ptx::ld_global(reinterpret_cast<const uint4*>(p.W) + at + i * span) : make_uint4(0u, 0u, 0u, 0u);
+    w[i] = place(i) < p.vecs ? ptx::ld_global(reinterpret_cast<const uint4*>(p.W) + place(i)) : make_uint4(0u, 0u, 0u, 0u);
   int turn = 0, stage = 0;
-  for (int row = first; row < p.rows; row += step, ++turn) {
+  for (int row = first; row < p.rows; row = PAIRS ? p.rows : row + step, ++turn) {          // (a block for each row: no loop, and its registers)
     if (row >= p.rows - step) ptx::grid_dependents_launch();
-    const size_t base = (size_t)row * p.vecs + at;
+    const size_t base = (size_t)row * p.vecs;
     uint4 x[VPT], r[VPT];
     if (RING) {
       ask(ahead, fill);
@@ -142,15 +155,21 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(c
       copies_arrived(stages);
     }
 #pragma unroll
+    for (int i = 0; i < VPT; ++i) x[i] = r[i] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      x[i] = r[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (at + i * span < p.vecs) {
-        if (RING) {
+      if (place(i) < p.vecs) {
+        if constexpr (PAIRS) {
+          if (i % 2 == 0) {
+            two_vectors(load_piece<16>(p.X + (base + place(i)) * 8), x[i], x[i + 1]);
+            if (residual) two_vectors(load_piece<16>(p.R + (base + place(i)) * 8), r[i], r[i + 1]);
+          }
+        } else if (RING) {
           x[i] = ptx::lds_128(mine + stage * stage_bytes + i * pitch);
           if (residual) r[i] = ptx::lds_128(mine + stage * stage_bytes + (VPT + i) * pitch);
         } else {
-          x[i] = ptx::ld_global_once(reinterpret_cast<const uint4*>(p.X) + base + i * span);
-          if (residual) r[i] = ptx::ld_global_once(reinterpret_cast<const uint4*>(p.R) + base + i * span);
+          x[i] = ptx::ld_global_once(reinterpret_cast<const uint4*>(p.X) + base + place(i));
+          if (residual) r[i] = ptx::ld_global_once(reinterpret_cast<const uint4*>(p.R) + base + place(i));
         }
       }
     }
@@ -164,7 +183,10 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(c
       if (residual) x[i] = make_uint4(add_pair(x[i].x, r[i].x), add_pair(x[i].y, r[i].y), add_pair(x[i].z, r[i].z), add_pair(x[i].w, r[i].w));
       float h[8], g[8];
       unpack(x[i], h);
-      if (p.H != nullptr && (residual || p.H != p.X) && at + i * span < p.vecs) reinterpret_cast<uint4*>(p.H)[base + i * span] = x[i];
+      if (p.H != nullptr && (residual || p.H != p.X) && place(i) < p.vecs) {
+        if constexpr (!PAIRS) reinterpret_cast<uint4*>(p.H)[base + place(i)] = x[i];
+        else if (i % 2 == 1) store_piece(p.H + (base + place(i - 1)) * 8, one_piece(x[i - 1], x[i]));
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) s.a = fmaf(h[e], h[e], s.a);
       if constexpr (CODES != EQAT_CODES_NONE) {
@@ -186,7 +208,7 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(c
     const float c = rsqrtf(fmaf(s.a, p.inverse_n, p.eps));
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const bool live = at + i * span < p.vecs;
+      const bool live = place(i) < p.vecs;
       float (&h)[8] = t[i % kHeld];
       if (CODES == EQAT_CODES_NONE || VPT > kHeld) {
         float g[8];
@@ -198,7 +220,12 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(c
       if constexpr (CODES == EQAT_CODES_NONE) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) h[e] *= c;
-        if (live) reinterpret_cast<uint4*>(p.Y)[base + i * span] = pack(h);
+        x[i] = pack(h);
+        if constexpr (!PAIRS) {
+          if (live) reinterpret_cast<uint4*>(p.Y)[base + place(i)] = x[i];
+        } else if (live && i % 2 == 1) {
+          store_piece(p.Y + (base + place(i - 1)) * 8, one_piece(x[i - 1], x[i]));
+        }
       } else {
         float a = p.lanes == 0 ? s.most : most[i];
         if (a < kSmallGroup) a = 0.0f;
@@ -231,12 +258,12 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(c
           q[1] = k[2] | (k[3] << 16);
         }
         if (live) {
-          reinterpret_cast<uint2*>(p.codes)[base + i * span] = make_uint2(q[0], q[1]);
-          if (p.Y != nullptr) reinterpret_cast<uint4*>(p.Y)[base + i * span] = pack(h);
+          reinterpret_cast<uint2*>(p.codes)[base + place(i)] = make_uint2(q[0], q[1]);
+          if (p.Y != nullptr) reinterpret_cast<uint4*>(p.Y)[base + place(i)] = pack(h);
           if (p.lanes == 0) {
             if (at == 0 && i == 0) p.scales[row] = scale;
           } else if ((lane & (p.lanes - 1)) == 0) {
-            p.scales[(size_t)row * (p.vecs / p.lanes) + (at + i * span) / p.lanes] = scale;
+            p.scales[(size_t)row * (p.vecs / p.lanes) + place(i) / p.lanes] = scale;
           }
         }
       }
@@ -427,20 +454,25 @@ int launch_with(void (*kernel)(P...), SmemOptIn& opt_in, const Launch& l, int th
 
 template <int VPT, bool WARP, int CODES>
 int launch_codes(const eqat_norm_desc& d, const NormFwd& p, const RowShape& s, int sms, cudaStream_t st) {
-  static SmemOptIn opt_in[2];
+  static SmemOptIn opt_in[3];
   const int threads = WARP ? kBlock : s.threads;
-  Launch l = launch_shape(d.rows, s, p.R != nullptr ? 2 : 1, 1024, 2, sms);
-  // Without codes the blocks are many and HBM sets the pace: twice as many as an SM holds, loading into registers, took 55.3 us
-  // of 8191 x 5120 (a block for each row 55.4), the ring 60.5.  With codes it is the instructions, and the copies under them
-  // are worth it: 2001 x 8192 in e4m3 29.5 us without the ring, 26.4, 27.5, 29.5 with one, two, three rows ahead.
   const int64_t need = (d.rows + (WARP ? kBlock / 32 : 1) - 1) / (WARP ? kBlock / 32 : 1), twice = (int64_t)sms * (2048 / threads);
+  // Without codes the blocks are many and HBM sets the pace, 8191 x 5120: 52.4 us on pairs with a block for each row, 53.0 with twice as
+  // many blocks as an SM holds; on vectors 55.4 and 54.8, which is also about what neighbours take; the ring 60.5.  With codes it is the instructions, and the copies under them
+  // are worth it, 2001 x 8192 in e4m3: 29.5 us without the ring, 26.4, 27.5, 29.5 with one, two, three rows ahead; 28.5 on pairs, a
+  // block for each row.
   if constexpr (CODES != EQAT_CODES_NONE) {
-    if (need > l.blocks) return launch_with(norm_fwd_kernel<VPT, WARP, CODES, true>, opt_in[0], l, threads, st, p, l.stages);
+    const Launch l = launch_shape(d.rows, s, p.R != nullptr ? 2 : 1, 1024, 2, sms);
+    if (need > l.blocks) return launch_with(norm_fwd_kernel<VPT, WARP, CODES, BY_RING>, opt_in[0], l, threads, st, p, l.stages);
+    return launch_with(norm_fwd_kernel<VPT, WARP, CODES, BY_VECTORS>, opt_in[1], Launch{l.blocks, 1, 0}, threads, st, p, 1);
   } else {
-    l.blocks = (int)(need < twice ? need : twice);
+    if constexpr (VPT % 2 == 0)
+      if (p.vecs % 2 == 0 && aligned32(p.X, p.R, p.H, p.Y))
+        return launch_with(norm_fwd_kernel<VPT, WARP, CODES, BY_PAIRS>, opt_in[2], Launch{(int)need, 1, 0}, threads, st, p, 1);
+      else if (p.vecs % 2 == 0)
+        return launch_with(norm_fwd_kernel<VPT, WARP, CODES, BY_NEIGHBOURS>, opt_in[0], Launch{(int)(need < twice ? need : twice), 1, 0}, threads, st, p, 1);
+    return launch_with(norm_fwd_kernel<VPT, WARP, CODES, BY_VECTORS>, opt_in[1], Launch{(int)(need < twice ? need : twice), 1, 0}, threads, st, p, 1);
   }
-  l.smem = 0;
-  return launch_with(norm_fwd_kernel<VPT, WARP, CODES, false>, opt_in[1], l, threads, st, p, l.stages);
 }
 template <int VPT, bool WARP>
 int launch_fwd(const eqat_norm_desc& d, const NormFwd& p, const RowShape& s, int sms, cudaStream_t st) {

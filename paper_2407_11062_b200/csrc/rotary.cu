@@ -4,23 +4,24 @@
 // units of 2^-64 of a turn, so the product of integers, mod 2^64, is the angle of any position without an error that grows
 // with it (in binary32 a position of 100000 would leave 2^-8 of a radian).
 //
-// 4 bytes an element cross HBM, which bounds long calls.  A thread owns one item of a row, the same in each of the block's up to
-// four rows: 2 x 8 elements of a head (HALVES: a vector of each half; PAIRS: one vector), whose places it works out once.  It
-// asks for the vectors of all its rows first; while they are on their way the block's warps look the rows' positions up, and its
-// threads compute the rows' sines and cosines into shared memory.  4094 rows of 80 heads of 128, a quarter of each turned: 29.3 us,
-// 0.87 of a copy's bandwidth (a thread on every 256th item of eight rows, one load at a time: 62.3; items kept, positions first:
-// 43.6); 64 rows of 72 heads 3.2 us, a launch and two waits for memory.
-#include <type_traits>
-
+// 4 bytes an element cross HBM, which bounds long calls.  A thread owns one item of a row, the same in each of the block's rows:
+// 2 x 16 elements of a head (HALVES: a piece of each half; PAIRS: one piece; 8 each where alignment says so), whose places it works out
+// once.  It asks for the pieces of all its rows first; while they are on their way the block's warps look the rows' positions up, and
+// its threads compute the rows' sines and cosines into shared memory.  4094 rows of 80 heads of 128, a quarter of each turned: 28.2 us,
+// 0.91 of a copy's bandwidth (a thread on every 256th item of eight rows, one load at a time: 62.3; items kept, positions first: 43.6;
+// 16 bytes at a time, four rows of 256 threads: 29.3; 32 bytes and up to 64, 192, 280 threads: 28.8, 28.7, 30.2; one row of 192:
+// 32.4); 64 rows of 72 heads 3.0 us, a launch and two waits for memory.
 #include "between.cuh"
 #include "common.cuh"
+#include "pieces.cuh"
 #include "ptx.cuh"
 
 namespace eqat {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kMaxRows = 4;                          // rows of a block, all of whose vectors a thread has on their way
+// Elements of a piece: 16, 8 or 1.  Rows of a block, all of whose pieces a thread has on their way, and its threads at most.
+__host__ __device__ constexpr int max_rows(int wide) { return wide == 16 ? 2 : 4; }
+__host__ __device__ constexpr int max_threads(int wide) { return wide == 16 ? 128 : 256; }
 
 struct RotaryParams : RotaryRows {
   int rows, sequences, q_heads, heads, head_dim, rotary_dim;
@@ -55,24 +56,18 @@ __device__ __forceinline__ void halves_of(uint32_t w, float& lo, float& hi) {
   hi = __uint_as_float(w & 0xFFFF0000u);
 }
 
-template <typename T>
-__device__ __forceinline__ T load_part(const eqat_bf16* p) {
-  if constexpr (sizeof(T) == 16) return ptx::ld_global_once(reinterpret_cast<const uint4*>(p));
-  else return ptx::ld_global(p);
-}
-
-// VECTORS: 16 bytes at a time (a half of the turned part, or all of it, is whole vectors), else element by element.
-template <int LAYOUT, bool VECTORS>
-__global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryParams p) {
-  __shared__ int s_pos[kMaxRows];
-  __shared__ bool s_live[kMaxRows];
+// WIDE elements at a time (a half of the turned part, or all of it, is whole pieces).
+template <int LAYOUT, int WIDE>
+__global__ void __launch_bounds__(max_threads(WIDE)) rotary_kernel(const RotaryParams p) {
+  constexpr int kRows = max_rows(WIDE);
+  __shared__ int s_pos[kRows];
+  __shared__ bool s_live[kRows];
   extern __shared__ __align__(16) float2 s_turn[];   // [block_rows][rotary_dim / 2]: cosine, sine, times the amplitude
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int pairs = p.rotary_dim >> 1;
   const int row0 = (int)blockIdx.x * p.block_rows, nrows = min(p.block_rows, p.rows - row0);
-  constexpr int kWide = VECTORS ? 8 : 1;
   // this thread's item: the c-th of a head, turned ones first, then those handed on
-  const int item = (int)blockIdx.y * kThreads + (int)threadIdx.x, items = p.turned + p.rest;
+  const int item = (int)(blockIdx.y * blockDim.x + threadIdx.x), items = p.turned + p.rest;
   int head = item / items;
   const int c = item - head * items;
   if (head >= p.heads) head = -1;
@@ -82,19 +77,18 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryParams p) 
   const eqat_bf16* const src = (query ? p.q : p.k) + row0 * src_pitch + at;
   eqat_bf16* const dst = (query ? p.q_out : p.k_out) + row0 * dst_pitch + at;
   const bool turns = head >= 0 && c < p.turned, rests = head >= 0 && c >= p.turned && src != dst;
-  // first and (HALVES, or single elements) second part of an item that turns; place of one that is handed on
-  const int ea = !turns ? p.rotary_dim + (c - p.turned) * kWide : LAYOUT == EQAT_ROTARY_HALVES ? c * kWide : VECTORS ? c * kWide : 2 * c;
+  constexpr bool kTwo = LAYOUT == EQAT_ROTARY_HALVES || WIDE == 1;         // an item that turns has two parts
+  // first and (kTwo) second part of an item that turns; place of one that is handed on
+  const int ea = !turns ? p.rotary_dim + (c - p.turned) * WIDE : LAYOUT == EQAT_ROTARY_PAIRS && WIDE == 1 ? 2 * c : c * WIDE;
   const int eb = LAYOUT == EQAT_ROTARY_HALVES ? ea + pairs : ea + 1;
-  constexpr bool kTwo = LAYOUT == EQAT_ROTARY_HALVES || !VECTORS;          // an item that turns has two parts
-  using Part = std::conditional_t<VECTORS, uint4, eqat_bf16>;
   ptx::grid_dependency_wait();
-  Part va[kMaxRows], vb[kTwo ? kMaxRows : 1];
+  Piece<WIDE> va[kRows], vb[kTwo ? kRows : 1];
 #pragma unroll
-  for (int i = 0; i < kMaxRows; ++i) {
+  for (int i = 0; i < kRows; ++i) {
     const eqat_bf16* const in = src + i * src_pitch;
-    if (i < nrows && (turns || rests)) va[i] = load_part<Part>(in + ea);
+    if (i < nrows && (turns || rests)) va[i] = load_piece<WIDE>(in + ea);
     if constexpr (kTwo)
-      if (i < nrows && turns) vb[i] = load_part<Part>(in + eb);
+      if (i < nrows && turns) vb[i] = load_piece<WIDE>(in + eb);
   }
   if (warp < nrows) {
     int pos = 0;
@@ -105,7 +99,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryParams p) 
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < nrows * pairs; i += kThreads) {
+  for (int i = threadIdx.x; i < nrows * pairs; i += (int)blockDim.x) {
     const int r = i / pairs, k = i - r * pairs;
     const uint2 f = ptx::ld_global(reinterpret_cast<const uint2*>(p.turns) + k);
     const uint64_t angle = (uint64_t)(int64_t)s_pos[r] * (((uint64_t)f.y << 32) | f.x) + 0x80000000ull;
@@ -116,46 +110,64 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryParams p) 
   __syncthreads();
   ptx::grid_dependents_launch();
 #pragma unroll
-  for (int i = 0; i < kMaxRows; ++i) {
+  for (int i = 0; i < kRows; ++i) {
     if (i >= nrows || !s_live[i]) continue;
     eqat_bf16* const out = dst + i * dst_pitch;
-    if (rests) *reinterpret_cast<Part*>(out + ea) = va[i];
+    if (rests) store_piece(out + ea, va[i]);
     if (!turns) continue;
-    if constexpr (!VECTORS) {
-      const float a = __uint_as_float((uint32_t)va[i] << 16), b = __uint_as_float((uint32_t)vb[i] << 16);
+    if constexpr (WIDE == 1) {
+      const float a = __uint_as_float((uint32_t)va[i].w << 16), b = __uint_as_float((uint32_t)vb[i].w << 16);
       const float2 t = s_turn[i * pairs + c];
       const uint32_t o = pack_bf16x2(a * t.x - b * t.y, b * t.x + a * t.y);
       out[ea] = (eqat_bf16)(o & 0xFFFFu);
       out[eb] = (eqat_bf16)(o >> 16);
     } else {
-      const float4* turn = reinterpret_cast<const float4*>(s_turn + i * pairs + (kTwo ? ea : ea / 2));
-      const uint32_t wa[4] = {va[i].x, va[i].y, va[i].z, va[i].w};
-      uint32_t oa[4];
+      const float2* const turn = s_turn + i * pairs + (kTwo ? ea : ea / 2);
+      Piece<WIDE> oa;
       if constexpr (kTwo) {
-        const uint32_t wb[4] = {vb[i].x, vb[i].y, vb[i].z, vb[i].w};
-        uint32_t ob[4];
+        Piece<WIDE> ob;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float4 t = turn[e];
+        for (int e = 0; e < WIDE / 2; ++e) {
+          const float4 t = reinterpret_cast<const float4*>(turn)[e];
           float a0, a1, b0, b1;
-          halves_of(wa[e], a0, a1);
-          halves_of(wb[e], b0, b1);
-          oa[e] = pack_bf16x2(a0 * t.x - b0 * t.y, a1 * t.z - b1 * t.w);
-          ob[e] = pack_bf16x2(b0 * t.x + a0 * t.y, b1 * t.z + a1 * t.w);
+          halves_of(va[i].w[e], a0, a1);
+          halves_of(vb[i].w[e], b0, b1);
+          oa.w[e] = pack_bf16x2(a0 * t.x - b0 * t.y, a1 * t.z - b1 * t.w);
+          ob.w[e] = pack_bf16x2(b0 * t.x + a0 * t.y, b1 * t.z + a1 * t.w);
         }
-        *reinterpret_cast<uint4*>(out + eb) = make_uint4(ob[0], ob[1], ob[2], ob[3]);
+        store_piece(out + eb, ob);
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 t = reinterpret_cast<const float2*>(turn)[e];
+        for (int e = 0; e < WIDE / 2; ++e) {
+          const float2 t = turn[e];
           float a, b;
-          halves_of(wa[e], a, b);
-          oa[e] = pack_bf16x2(a * t.x - b * t.y, b * t.x + a * t.y);
+          halves_of(va[i].w[e], a, b);
+          oa.w[e] = pack_bf16x2(a * t.x - b * t.y, b * t.x + a * t.y);
         }
       }
-      *reinterpret_cast<uint4*>(out + ea) = make_uint4(oa[0], oa[1], oa[2], oa[3]);
+      store_piece(out + ea, oa);
     }
   }
+}
+
+template <int WIDE>
+int launch_pieces(const eqat_rotary_desc& d, const RotaryRows& rows, RotaryParams& p, int sms, cudaStream_t st) {
+  const bool halves = d.layout == EQAT_ROTARY_HALVES;
+  const bool in_place = rows.q == rows.q_out && (d.kv_heads == 0 || rows.k == rows.k_out);
+  p.turned = halves || WIDE == 1 ? d.rotary_dim / 2 / WIDE : d.rotary_dim / WIDE;
+  p.rest = in_place ? 0 : (d.head_dim - d.rotary_dim) / WIDE;
+  constexpr int kMost = max_threads(WIDE);
+  const int64_t items = (int64_t)p.heads * (p.turned + p.rest), chunks = (items + kMost - 1) / kMost;   // below 2^16: 2^15 heads of 511 / 256 items
+  // threads enough for a row in as many blocks, and a warp for each row's position
+  const int even = (int)((items + chunks - 1) / chunks + 31) / 32 * 32, least = 32 * max_rows(WIDE);
+  const dim3 threads(WIDE != 16 ? kMost : even > least ? even : least);
+  // several rows a block where there are enough blocks all the same
+  const int64_t per = d.rows * chunks / ((int64_t)sms * 8);
+  p.block_rows = (int)(per < 1 ? 1 : per > max_rows(WIDE) ? max_rows(WIDE) : per);
+  const dim3 grid((unsigned)((d.rows + p.block_rows - 1) / p.block_rows), (unsigned)chunks);
+  const size_t smem = (size_t)p.block_rows * (d.rotary_dim / 2) * sizeof(float2);
+  return halves ? launch_overlapped(rotary_kernel<EQAT_ROTARY_HALVES, WIDE>, grid, threads, smem, st, p)
+                : launch_overlapped(rotary_kernel<EQAT_ROTARY_PAIRS, WIDE>, grid, threads, smem, st, p);
 }
 
 }  // namespace
@@ -173,23 +185,12 @@ int launch_rotary(const eqat_rotary_desc& d, const RotaryRows& rows, bool backwa
   p.rotary_dim = d.rotary_dim;
   p.amplitude = d.amplitude;
   p.sine = backward ? -d.amplitude : d.amplitude;
-  const bool halves = d.layout == EQAT_ROTARY_HALVES;
-  const bool vectors = d.rotary_dim % (halves ? 16 : 8) == 0;
-  const int wide = vectors ? 8 : 1;
-  const bool in_place = rows.q == rows.q_out && (d.kv_heads == 0 || rows.k == rows.k_out);
-  p.turned = halves || !vectors ? d.rotary_dim / 2 / wide : d.rotary_dim / wide;
-  p.rest = in_place ? 0 : (d.head_dim - d.rotary_dim) / wide;
-  const int64_t chunks = ((int64_t)p.heads * (p.turned + p.rest) + kThreads - 1) / kThreads;      // below 2^16: 2^15 heads of 511 items
-  // several rows a block where there are enough blocks all the same
-  int64_t per = d.rows * chunks / ((int64_t)sms * 8);
-  p.block_rows = (int)(per < 1 ? 1 : per > kMaxRows ? kMaxRows : per);
-  const dim3 grid((unsigned)((d.rows + p.block_rows - 1) / p.block_rows), (unsigned)chunks);
-  const size_t smem = (size_t)p.block_rows * (d.rotary_dim / 2) * sizeof(float2);
-  if (halves)
-    return vectors ? launch_overlapped(rotary_kernel<EQAT_ROTARY_HALVES, true>, grid, dim3(kThreads), smem, st, p)
-                   : launch_overlapped(rotary_kernel<EQAT_ROTARY_HALVES, false>, grid, dim3(kThreads), smem, st, p);
-  return vectors ? launch_overlapped(rotary_kernel<EQAT_ROTARY_PAIRS, true>, grid, dim3(kThreads), smem, st, p)
-                 : launch_overlapped(rotary_kernel<EQAT_ROTARY_PAIRS, false>, grid, dim3(kThreads), smem, st, p);
+  const int part = d.layout == EQAT_ROTARY_HALVES ? d.rotary_dim / 2 : d.rotary_dim;             // what has to be whole pieces
+  const bool keys = d.kv_heads > 0;
+  if (part % 16 == 0 && d.head_dim % 16 == 0 && (rows.q_pitch | rows.q_out_pitch) % 16 == 0 && aligned32(rows.q, rows.q_out) &&
+      (!keys || ((rows.k_pitch | rows.k_out_pitch) % 16 == 0 && aligned32(rows.k, rows.k_out))))
+    return launch_pieces<16>(d, rows, p, sms, st);
+  return part % 8 == 0 ? launch_pieces<8>(d, rows, p, sms, st) : launch_pieces<1>(d, rows, p, sms, st);
 }
 
 }  // namespace eqat
