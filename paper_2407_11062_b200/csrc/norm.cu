@@ -4,19 +4,24 @@
 //     dx = dr + c (v - h c^2 mean(v h)),  v = dy w;     dw = sum over the rows of dy h c
 //
 // One pass: each tensor crosses HBM once, 8 bytes an element forward with a residual (7 + 4/group with codes in place of y), 8
-// backward.  A thread owns the same columns of every row it meets, so w is read once a block and dw is added up in registers.
-// What a thread will read of the next rows it copies into shared memory itself (cp.async, up to two rows ahead): nobody else
-// reads its places, so a row costs no barrier but that of the sum, and the copies run on through it.  Blocks with a single row,
-// and the forward pass without codes, load into registers, 32 bytes at a time where everything is aligned to them.
+// backward.
 //
-// Times on a B200, states larger than L2 (of a copy's bandwidth): forward of 8191 x 5120 with a residual 52.4 us (0.98), of 2001 x
-// 8192 in e4m3 26.4 us (0.86: conversions and the groups' maxima), backward of 4096 x 4096 26.2 us (0.78; 22.4 us without dw, whose
-// partial sums are a launch of 3 us), one row of 4096 2.6 us, a launch.  Before the ring and with the row unpacked twice the
-// backward pass took 38.2 us, 9 of them the sum of the partial sums by eight warps of a block.
+// Forward: a row a block (a warp for short ones), 32 bytes of each tensor at a time where everything is aligned to them.  What hides
+// the way to HBM are many blocks an SM, so registers count: rows one after the other in blocks that stay, the next ones copied ahead
+// or not, took 54.8 and 60.5 us where this takes 50.1 (8191 x 5120 with a residual, 1.02 of a copy's bandwidth), 16 bytes at a time
+// 55.4.  With codes (2001 x 8192 in e4m3: 24.7 us, 0.92: conversions and the groups' maxima) blocks have 256 threads at most, so that
+// some load while others convert: 27.0 with 512, 26.5 with a row copied ahead.  One row of 4096: 2.6 us, a launch.
+//
+// Backward: a thread owns the same columns of every row that its block meets, so w is read once a block and dw is added up in registers.
+// What it will read of the next rows it copies into shared memory itself (cp.async, up to two rows ahead): nobody else reads its
+// places, so a row costs no barrier but that of the sum, and the copies run on through it.  4096 x 4096: 26.4 us (0.78; 22.4 us
+// without dw, whose partial sums are a launch of 3 us).  Before the ring and with the row unpacked twice it took 38.2 us, 9 of them the
+// sum of the partial sums by eight warps of a block.
 #include <cuda_fp8.h>
 
 #include "between.cuh"
 #include "common.cuh"
+#include "expand.cuh"
 #include "pieces.cuh"
 #include "ptx.cuh"
 
@@ -25,6 +30,7 @@ namespace {
 
 constexpr int kBlock = 256;                          // threads of a block that gives each row to a warp
 constexpr int kMaxThreads = 512;                     // of a block that shares a row
+constexpr int kLoopThreads = 128;                    // forward: of a block that takes one row after the other
 constexpr int kRingBytes = 200 * 1024;               // shared memory of an SM for the blocks' rings
 constexpr float kSmallGroup = 0x1p-110f;             // 127 / a and 448 / a are finite above
 
@@ -97,83 +103,56 @@ struct NormFwd {
   float* scales;
   int rows, vecs;                                    // vecs: 16-byte vectors of a row
   float eps, inverse_n;
-  int lanes;                                         // codes: vectors of a group (4 .. 32 neighbouring lanes), or 0: the row
+  int lanes, lanes_log2;                             // codes: vectors of a group (4 .. 32 neighbouring lanes), or 0: the row
+  int groups;                                        // of a row
 };
 
-// VPT vectors of a row per thread.  A row belongs to a warp (WARP) or to the block.  How it comes in: by the ring, or by loads of a
-// vector or of two neighbours, which are the same places whether they come as one piece or, for want of alignment, as two: a sum's
-// order hangs on the shape alone.
-enum Loads : int { BY_RING, BY_VECTORS, BY_NEIGHBOURS, BY_PAIRS };
-template <int VPT, bool WARP, int CODES, int LOADS>
-__global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(const NormFwd p, int stages) {
+// VPT vectors of a row per thread; a row belongs to a warp (WARP) or to the block.  Wide blocks have one row: a loop over rows costs
+// registers, and with them threads of an SM (LOOP: short rows, where starting a block costs more).  A thread's vectors are
+// neighbours by two where a row has an even number of them (NEXT); WIDE: and they are moved as one piece.  So the order of a sum
+// hangs on the shape alone, not on alignment.
+template <int VPT, bool WARP, bool LOOP, int CODES, bool NEXT, bool WIDE>
+__global__ void __launch_bounds__(WARP ? kBlock : LOOP ? kLoopThreads : kMaxThreads, WARP ? (LOOP ? 8 : 4) : LOOP ? 8 : VPT == 2 ? 3 : VPT == 4 ? 2 : 1)
+norm_fwd_kernel(const NormFwd p) {
+  static_assert(!NEXT || VPT % 2 == 0, "two neighbours");
   __shared__ Reduced red[2][32];
-  extern __shared__ __align__(16) uint8_t ring[];
-  constexpr bool RING = LOADS == BY_RING, PAIRS = LOADS == BY_PAIRS, NEXT = PAIRS || LOADS == BY_NEIGHBOURS;
-  static_assert(!NEXT || (CODES == EQAT_CODES_NONE && VPT % 2 == 0), "two neighbours");
   const int lane = threadIdx.x & 31;
   const int at = WARP ? lane : (int)threadIdx.x, span = WARP ? 32 : (int)blockDim.x;
+  auto place = [&](int i) { return NEXT ? ((i >> 1) * span + at) * 2 + (i & 1) : at + i * span; };      // of vector i of this thread
   const int step = (int)gridDim.x * (WARP ? kBlock / 32 : 1);
   const int first = WARP ? (int)blockIdx.x * (kBlock / 32) + (int)(threadIdx.x >> 5) : (int)blockIdx.x;
-  auto place = [&](int i) { return NEXT ? ((i >> 1) * span + at) * 2 + (i & 1) : at + i * span; };      // of vector i of this thread
   constexpr float kTop = CODES == EQAT_CODES_INT8 ? 127.0f : 448.0f;
   const bool residual = p.R != nullptr;
-  const uint32_t mine = ptx::smem_addr(ring) + threadIdx.x * 16, pitch = blockDim.x * 16;      // of this thread; to its next vector
-  const uint32_t stage_bytes = pitch * VPT * (residual ? 2 : 1);
   ptx::grid_dependency_wait();
-  auto ask = [&](int row, int stage) {
-    if (row < p.rows) {
-      const size_t base = (size_t)row * p.vecs;
-      uint32_t dst = mine + stage * stage_bytes;
-#pragma unroll
-      for (int i = 0; i < VPT; ++i, dst += pitch)
-        if (place(i) < p.vecs) copy_16(dst, reinterpret_cast<const uint4*>(p.X) + base + place(i));
-      if (residual) {
-#pragma unroll
-        for (int i = 0; i < VPT; ++i, dst += pitch)
-          if (place(i) < p.vecs) copy_16(dst, reinterpret_cast<const uint4*>(p.R) + base + place(i));
-      }
-    }
-    copies_issued();
-  };
-  int ahead = first, fill = 0;                       // the row asked for next, and its stage
-  if (RING) {
-    for (int k = 0; k + 1 < stages; ++k, ahead += step) ask(ahead, fill++);
-  }
   uint4 w[VPT];
 #pragma unroll
   for (int i = 0; i < VPT; ++i)
     w[i] = place(i) < p.vecs ? ptx::ld_global(reinterpret_cast<const uint4*>(p.W) + place(i)) : make_uint4(0u, 0u, 0u, 0u);
-  int turn = 0, stage = 0;
-  for (int row = first; row < p.rows; row = PAIRS ? p.rows : row + step, ++turn) {          // (a block for each row: no loop, and its registers)
-    if (row >= p.rows - step) ptx::grid_dependents_launch();
+  int turn = 0;
+  for (int row = first; row < p.rows; row = LOOP ? row + step : p.rows, ++turn) {
     const size_t base = (size_t)row * p.vecs;
-    uint4 x[VPT], r[VPT];
-    if (RING) {
-      ask(ahead, fill);
-      ahead += step;
-      if (++fill == stages) fill = 0;
-      copies_arrived(stages);
-    }
+    uint4 x[VPT] = {}, r[VPT] = {};
+    // vectors of this thread in a row, stored or loaded
+    auto load = [&](const eqat_bf16* from, uint4 (&v)[VPT]) {
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) x[i] = r[i] = make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      if (place(i) < p.vecs) {
-        if constexpr (PAIRS) {
-          if (i % 2 == 0) {
-            two_vectors(load_piece<16>(p.X + (base + place(i)) * 8), x[i], x[i + 1]);
-            if (residual) two_vectors(load_piece<16>(p.R + (base + place(i)) * 8), r[i], r[i + 1]);
-          }
-        } else if (RING) {
-          x[i] = ptx::lds_128(mine + stage * stage_bytes + i * pitch);
-          if (residual) r[i] = ptx::lds_128(mine + stage * stage_bytes + (VPT + i) * pitch);
+      for (int i = 0; i < VPT; ++i) {
+        if constexpr (WIDE) {
+          if (i % 2 == 0 && place(i) < p.vecs) two_vectors(load_piece<16>(from + (base + place(i)) * 8), v[i], v[i + 1]);
         } else {
-          x[i] = ptx::ld_global_once(reinterpret_cast<const uint4*>(p.X) + base + place(i));
-          if (residual) r[i] = ptx::ld_global_once(reinterpret_cast<const uint4*>(p.R) + base + place(i));
+          if (place(i) < p.vecs) v[i] = ptx::ld_global_once(reinterpret_cast<const uint4*>(from) + base + place(i));
         }
       }
-    }
-    if (RING && ++stage == stages) stage = 0;
+    };
+    auto store = [&](eqat_bf16* to, int i) {           // vector i of x, or with it the one before
+      if constexpr (WIDE) {
+        if (i % 2 == 1 && place(i) < p.vecs) store_piece(to + (base + place(i - 1)) * 8, one_piece(x[i - 1], x[i]));
+      } else {
+        if (place(i) < p.vecs) reinterpret_cast<uint4*>(to)[base + place(i)] = x[i];
+      }
+    };
+    load(p.X, x);
+    if (residual) load(p.R, r);
+    if (!LOOP || row >= p.rows - step) ptx::grid_dependents_launch();
     // With codes, the products of up to two vectors a thread are held through the sum, more are formed again.
     constexpr int kHeld = VPT < 2 ? 1 : 2;
     float t[kHeld][8], most[VPT];
@@ -183,10 +162,7 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(c
       if (residual) x[i] = make_uint4(add_pair(x[i].x, r[i].x), add_pair(x[i].y, r[i].y), add_pair(x[i].z, r[i].z), add_pair(x[i].w, r[i].w));
       float h[8], g[8];
       unpack(x[i], h);
-      if (p.H != nullptr && (residual || p.H != p.X) && place(i) < p.vecs) {
-        if constexpr (!PAIRS) reinterpret_cast<uint4*>(p.H)[base + place(i)] = x[i];
-        else if (i % 2 == 1) store_piece(p.H + (base + place(i - 1)) * 8, one_piece(x[i - 1], x[i]));
-      }
+      if (p.H != nullptr && (residual || p.H != p.X)) store(p.H, i);
 #pragma unroll
       for (int e = 0; e < 8; ++e) s.a = fmaf(h[e], h[e], s.a);
       if constexpr (CODES != EQAT_CODES_NONE) {
@@ -199,16 +175,20 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(c
         }
         if (p.lanes == 0) {
           s.most = fmaxf(s.most, most[i]);
-        } else {
+        } else if (!NEXT) {
           for (int d = 1; d < p.lanes; d <<= 1) most[i] = fmaxf(most[i], __shfl_xor_sync(0xFFFFFFFFu, most[i], d));
+        } else if (i % 2 == 1) {                       // both are of one group, which is half as many lanes
+          most[i] = fmaxf(most[i - 1], most[i]);
+          for (int d = 1; d < p.lanes / 2; d <<= 1) most[i] = fmaxf(most[i], __shfl_xor_sync(0xFFFFFFFFu, most[i], d));
+          most[i - 1] = most[i];
         }
       }
     }
     s = reduce_row<WARP>(s, red, turn);
     const float c = rsqrtf(fmaf(s.a, p.inverse_n, p.eps));
+    uint2 even, odd = make_uint2(0u, 0u);              // codes of two vectors
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const bool live = place(i) < p.vecs;
       float (&h)[8] = t[i % kHeld];
       if (CODES == EQAT_CODES_NONE || VPT > kHeld) {
         float g[8];
@@ -221,17 +201,13 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(c
 #pragma unroll
         for (int e = 0; e < 8; ++e) h[e] *= c;
         x[i] = pack(h);
-        if constexpr (!PAIRS) {
-          if (live) reinterpret_cast<uint4*>(p.Y)[base + place(i)] = x[i];
-        } else if (live && i % 2 == 1) {
-          store_piece(p.Y + (base + place(i - 1)) * 8, one_piece(x[i - 1], x[i]));
-        }
+        store(p.Y, i);
       } else {
         float a = p.lanes == 0 ? s.most : most[i];
         if (a < kSmallGroup) a = 0.0f;
         const float up = a > 0.0f ? __fdiv_rn(kTop, a) : 0.0f;
         const float scale = a * c * (1.0f / kTop);
-        uint32_t q[2];
+        even = odd;
         if constexpr (CODES == EQAT_CODES_INT8) {
           // |t| is at most 127 (1 + 2^-23), so the low byte of t + 1.5 2^23 is the code
           uint32_t k[8];
@@ -241,9 +217,8 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(c
             k[e] = __float_as_uint(v);
             h[e] = (v - 12582912.0f) * scale;
           }
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-            q[j] = __byte_perm(__byte_perm(k[4 * j], k[4 * j + 1], 0x0040), __byte_perm(k[4 * j + 2], k[4 * j + 3], 0x0040), 0x5410);
+          odd = make_uint2(__byte_perm(__byte_perm(k[0], k[1], 0x0040), __byte_perm(k[2], k[3], 0x0040), 0x5410),
+                           __byte_perm(__byte_perm(k[4], k[5], 0x0040), __byte_perm(k[6], k[7], 0x0040), 0x5410));
         } else {
           uint32_t k[4];
 #pragma unroll
@@ -254,16 +229,17 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_fwd_kernel(c
             h[2 * e] = y.x * scale;
             h[2 * e + 1] = y.y * scale;
           }
-          q[0] = k[0] | (k[1] << 16);
-          q[1] = k[2] | (k[3] << 16);
+          odd = make_uint2(k[0] | (k[1] << 16), k[2] | (k[3] << 16));
         }
-        if (live) {
-          reinterpret_cast<uint2*>(p.codes)[base + place(i)] = make_uint2(q[0], q[1]);
-          if (p.Y != nullptr) reinterpret_cast<uint4*>(p.Y)[base + place(i)] = pack(h);
+        x[i] = pack(h);
+        if (p.Y != nullptr) store(p.Y, i);
+        if (place(i) < p.vecs) {
+          if constexpr (!NEXT) reinterpret_cast<uint2*>(p.codes)[base + place(i)] = odd;
+          else if (i % 2 == 1) reinterpret_cast<uint4*>(p.codes)[(base + place(i - 1)) / 2] = make_uint4(even.x, even.y, odd.x, odd.y);
           if (p.lanes == 0) {
             if (at == 0 && i == 0) p.scales[row] = scale;
-          } else if ((lane & (p.lanes - 1)) == 0) {
-            p.scales[(size_t)row * (p.vecs / p.lanes) + place(i) / p.lanes] = scale;
+          } else if (NEXT ? i % 2 == 0 && (lane & (p.lanes / 2 - 1)) == 0 : (lane & (p.lanes - 1)) == 0) {
+            p.scales[(size_t)row * p.groups + (place(i) >> p.lanes_log2)] = scale;
           }
         }
       }
@@ -417,8 +393,9 @@ __global__ void __launch_bounds__(kSumWarps * 32) norm_dw_kernel(const float* pa
 struct RowShape {
   int vpt, threads;                                  // threads 32: a warp a row
 };
-RowShape row_shape(int vecs) {
-  const int vpt = vecs <= 32 ? 1 : vecs <= 2 * kMaxThreads ? 2 : vecs <= 4 * kMaxThreads ? 4 : 8;
+// `pairs`: threads that a row of two vectors a thread may have.
+RowShape row_shape(int vecs, int pairs) {
+  const int vpt = vecs <= 32 ? 1 : vecs <= 2 * pairs ? 2 : vecs <= 4 * kMaxThreads ? 4 : 8;
   return {vpt, ((vecs + vpt - 1) / vpt + 31) / 32 * 32};
 }
 
@@ -439,7 +416,7 @@ Launch launch_shape(int64_t rows, const RowShape& s, int tensors, int busy, int 
   return {(int)(need < most ? need : most), stages, (size_t)stages * stage};
 }
 Launch backward_shape(const eqat_norm_desc& d, int sms) {
-  const RowShape s = row_shape(d.features / 8);
+  const RowShape s = row_shape(d.features / 8, kMaxThreads);
   Launch l = launch_shape(d.rows, s, 3, 512, 3, sms);
   const size_t share = (size_t)(kBlock / 32) * d.features * sizeof(float);
   if (s.threads == 32 && l.smem < share) l.smem = share;
@@ -452,34 +429,24 @@ int launch_with(void (*kernel)(P...), SmemOptIn& opt_in, const Launch& l, int th
   return launch_overlapped(kernel, dim3(l.blocks), dim3(threads), l.smem, st, args...);
 }
 
-template <int VPT, bool WARP, int CODES>
+template <int VPT, bool WARP, bool LOOP, int CODES>
 int launch_codes(const eqat_norm_desc& d, const NormFwd& p, const RowShape& s, int sms, cudaStream_t st) {
-  static SmemOptIn opt_in[3];
+  constexpr int kRows = WARP ? kBlock / 32 : 1;
   const int threads = WARP ? kBlock : s.threads;
-  const int64_t need = (d.rows + (WARP ? kBlock / 32 : 1) - 1) / (WARP ? kBlock / 32 : 1), twice = (int64_t)sms * (2048 / threads);
-  // Without codes the blocks are many and HBM sets the pace, 8191 x 5120: 52.4 us on pairs with a block for each row, 53.0 with twice as
-  // many blocks as an SM holds; on vectors 55.4 and 54.8, which is also about what neighbours take; the ring 60.5.  With codes it is the instructions, and the copies under them
-  // are worth it, 2001 x 8192 in e4m3: 29.5 us without the ring, 26.4, 27.5, 29.5 with one, two, three rows ahead; 28.5 on pairs, a
-  // block for each row.
-  if constexpr (CODES != EQAT_CODES_NONE) {
-    const Launch l = launch_shape(d.rows, s, p.R != nullptr ? 2 : 1, 1024, 2, sms);
-    if (need > l.blocks) return launch_with(norm_fwd_kernel<VPT, WARP, CODES, BY_RING>, opt_in[0], l, threads, st, p, l.stages);
-    return launch_with(norm_fwd_kernel<VPT, WARP, CODES, BY_VECTORS>, opt_in[1], Launch{l.blocks, 1, 0}, threads, st, p, 1);
-  } else {
-    if constexpr (VPT % 2 == 0)
-      if (p.vecs % 2 == 0 && aligned32(p.X, p.R, p.H, p.Y))
-        return launch_with(norm_fwd_kernel<VPT, WARP, CODES, BY_PAIRS>, opt_in[2], Launch{(int)need, 1, 0}, threads, st, p, 1);
-      else if (p.vecs % 2 == 0)
-        return launch_with(norm_fwd_kernel<VPT, WARP, CODES, BY_NEIGHBOURS>, opt_in[0], Launch{(int)(need < twice ? need : twice), 1, 0}, threads, st, p, 1);
-    return launch_with(norm_fwd_kernel<VPT, WARP, CODES, BY_VECTORS>, opt_in[1], Launch{(int)(need < twice ? need : twice), 1, 0}, threads, st, p, 1);
-  }
+  const int64_t need = (d.rows + kRows - 1) / kRows, twice = (int64_t)sms * (2048 / threads);
+  const dim3 grid((unsigned)(LOOP && need > twice ? twice : need)), block(threads);
+  if constexpr (VPT % 2 == 0)
+    if (p.vecs % 2 == 0)
+      return aligned32(p.X, p.R, p.H, p.Y) ? launch_overlapped(norm_fwd_kernel<VPT, WARP, LOOP, CODES, true, true>, grid, block, 0, st, p)
+                                           : launch_overlapped(norm_fwd_kernel<VPT, WARP, LOOP, CODES, true, false>, grid, block, 0, st, p);
+  return launch_overlapped(norm_fwd_kernel<VPT, WARP, LOOP, CODES, false, false>, grid, block, 0, st, p);
 }
-template <int VPT, bool WARP>
+template <int VPT, bool WARP, bool LOOP>
 int launch_fwd(const eqat_norm_desc& d, const NormFwd& p, const RowShape& s, int sms, cudaStream_t st) {
   switch (d.codes) {
-    case EQAT_CODES_INT8: return launch_codes<VPT, WARP, EQAT_CODES_INT8>(d, p, s, sms, st);
-    case EQAT_CODES_E4M3: return launch_codes<VPT, WARP, EQAT_CODES_E4M3>(d, p, s, sms, st);
-    default: return launch_codes<VPT, WARP, EQAT_CODES_NONE>(d, p, s, sms, st);
+    case EQAT_CODES_INT8: return launch_codes<VPT, WARP, LOOP && !WARP, EQAT_CODES_INT8>(d, p, s, sms, st);
+    case EQAT_CODES_E4M3: return launch_codes<VPT, WARP, LOOP && !WARP, EQAT_CODES_E4M3>(d, p, s, sms, st);
+    default: return launch_codes<VPT, WARP, LOOP, EQAT_CODES_NONE>(d, p, s, sms, st);
   }
 }
 template <int VPT, bool WARP>
@@ -495,13 +462,16 @@ int launch_norm_fwd(const eqat_norm_desc& d, const eqat_bf16* X, const eqat_bf16
   const int sms = sm_count();
   if (sms <= 0) return EQAT_ERR_CUDA;
   const int vecs = d.features / 8;
+  const int lanes = d.group > 0 && d.group <= 256 && d.group != d.features ? d.group / 8 : 0;
   const NormFwd p{X, R, W, H, Y, static_cast<uint8_t*>(codes), scales, (int)d.rows, vecs, d.eps, 1.0f / (float)d.features,
-                  d.group > 0 && d.group <= 256 && d.group != d.features ? d.group / 8 : 0};
-  const RowShape s = row_shape(vecs);
-  if (s.threads == 32) return s.vpt == 1 ? launch_fwd<1, true>(d, p, s, sms, st) : launch_fwd<2, true>(d, p, s, sms, st);
-  return s.vpt == 2   ? launch_fwd<2, false>(d, p, s, sms, st)
-         : s.vpt == 4 ? launch_fwd<4, false>(d, p, s, sms, st)
-                      : launch_fwd<8, false>(d, p, s, sms, st);
+                  lanes, lanes > 0 ? log2_exact(lanes) : 0, lanes > 0 ? vecs / lanes : 1};
+  // With codes blocks of up to 256 threads, several an SM, so that some load while others convert.
+  const RowShape s = row_shape(vecs, d.codes == EQAT_CODES_NONE ? kMaxThreads : kMaxThreads / 2);
+  if (s.threads == 32) return s.vpt == 1 ? launch_fwd<1, true, true>(d, p, s, sms, st) : launch_fwd<2, true, false>(d, p, s, sms, st);
+  return s.threads <= kLoopThreads ? launch_fwd<2, false, true>(d, p, s, sms, st)          // (two vectors a thread)
+         : s.vpt == 2              ? launch_fwd<2, false, false>(d, p, s, sms, st)
+         : s.vpt == 4              ? launch_fwd<4, false, false>(d, p, s, sms, st)
+                                   : launch_fwd<8, false, false>(d, p, s, sms, st);
 }
 
 size_t norm_workspace(const eqat_norm_desc& d, int sms) { return (size_t)backward_shape(d, sms).blocks * d.features * sizeof(float); }
@@ -514,7 +484,7 @@ int launch_norm_bwd(const eqat_norm_desc& d, const eqat_bf16* dY, const eqat_bf1
   const Launch l = backward_shape(d, sms);
   const NormBwd p{dY, H, W, dR, dX, dW != nullptr ? static_cast<float*>(workspace) : nullptr, (int)d.rows, vecs, d.eps,
                   1.0f / (float)d.features};
-  const RowShape s = row_shape(vecs);
+  const RowShape s = row_shape(vecs, kMaxThreads);
   const int rc = s.threads == 32 ? (s.vpt == 1 ? launch_bwd<1, true>(p, s, l, st) : launch_bwd<2, true>(p, s, l, st))
                  : s.vpt == 2    ? launch_bwd<2, false>(p, s, l, st)
                  : s.vpt == 4    ? launch_bwd<4, false>(p, s, l, st)
