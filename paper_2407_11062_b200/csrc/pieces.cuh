@@ -1,4 +1,4 @@
-// 8 or 16 neighbouring bf16 numbers, moved at once: 16 bytes, or 32 where everything is aligned to them.  (Or one.)
+// 8 or 16 neighbouring bf16 numbers, moved at once: 16 bytes, or 32 where everything is aligned to them.  (Or 1, 2, 4.)
 //
 // With 32 bytes a warp's load is whole 1 KB runs and a thread needs half as many of them; with them goes a block for every
 // piece, not blocks that stay.  gated.cu, norm.cu and rotary.cu have what it brought.
@@ -25,6 +25,11 @@ __device__ __forceinline__ Piece<N> load_piece(const eqat_bf16* p) {
     ptx::ld_global_once_256(p, v.w);
   } else if constexpr (N == 1) {
     v.w = ptx::ld_global(p);
+  } else if constexpr (N == 2) {
+    v.w[0] = ptx::ld_global(reinterpret_cast<const uint32_t*>(p));
+  } else if constexpr (N == 4) {
+    const uint2 u = ptx::ld_global(reinterpret_cast<const uint2*>(p));
+    v.w[0] = u.x, v.w[1] = u.y;
   } else {
     const uint4 u = ptx::ld_global_once(reinterpret_cast<const uint4*>(p));
     v.w[0] = u.x, v.w[1] = u.y, v.w[2] = u.z, v.w[3] = u.w;
@@ -35,6 +40,8 @@ template <int N>
 __device__ __forceinline__ void store_piece(eqat_bf16* p, const Piece<N>& v) {
   if constexpr (N == 16) ptx::st_global_256(p, v.w);
   else if constexpr (N == 1) *p = v.w;
+  else if constexpr (N == 2) *reinterpret_cast<uint32_t*>(p) = v.w[0];
+  else if constexpr (N == 4) *reinterpret_cast<uint2*>(p) = make_uint2(v.w[0], v.w[1]);
   else *reinterpret_cast<uint4*>(p) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
 }
 

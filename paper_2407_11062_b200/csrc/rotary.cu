@@ -10,7 +10,8 @@
 // its threads compute the rows' sines and cosines into shared memory.  4094 rows of 80 heads of 128, a quarter of each turned: 28.2 us,
 // 0.91 of a copy's bandwidth (a thread on every 256th item of eight rows, one load at a time: 62.3; items kept, positions first: 43.6;
 // 16 bytes at a time, four rows of 256 threads: 29.3; 32 bytes and up to 64, 192, 280 threads: 28.8, 28.7, 30.2; one row of 192:
-// 32.4); 64 rows of 72 heads 3.0 us, a launch and two waits for memory.
+// 32.4); 64 rows of 72 heads 3.0 us, a launch and two waits for memory.  4096 rows of 40 heads of 128, 34 elements of each turned: 25.2 us as
+// halves, 14.4 as pairs (element by element 55.7 and 51.5).
 #include "between.cuh"
 #include "common.cuh"
 #include "pieces.cuh"
@@ -19,7 +20,7 @@
 namespace eqat {
 namespace {
 
-// Elements of a piece: 16, 8 or 1.  Rows of a block, all of whose pieces a thread has on their way, and its threads at most.
+// Elements of a piece: 16 or 8, and of halves that are not whole pieces of 8 also 4, 2 or 1.  Rows of a block, all of whose pieces a thread has on their way, and its threads at most.
 __host__ __device__ constexpr int max_rows(int wide) { return wide == 16 ? 2 : 4; }
 __host__ __device__ constexpr int max_threads(int wide) { return wide == 16 ? 128 : 256; }
 
@@ -56,8 +57,10 @@ __device__ __forceinline__ void halves_of(uint32_t w, float& lo, float& hi) {
   hi = __uint_as_float(w & 0xFFFF0000u);
 }
 
-// WIDE elements at a time (a half of the turned part, or all of it, is whole pieces).
-template <int LAYOUT, int WIDE>
+// WIDE elements at a time: a half of the turned part (HALVES) is whole pieces; of neighbouring pairs the last piece may be turned in
+// part (PART: asking costs 5 %).  Behind halves that are not whole pieces of 8 the rest is handed on two by two up to the next 16 bytes, from there 16 bytes
+// at a time.
+template <int LAYOUT, int WIDE, bool PART>
 __global__ void __launch_bounds__(max_threads(WIDE)) rotary_kernel(const RotaryParams p) {
   constexpr int kRows = max_rows(WIDE);
   __shared__ int s_pos[kRows];
@@ -77,18 +80,25 @@ __global__ void __launch_bounds__(max_threads(WIDE)) rotary_kernel(const RotaryP
   const eqat_bf16* const src = (query ? p.q : p.k) + row0 * src_pitch + at;
   eqat_bf16* const dst = (query ? p.q_out : p.k_out) + row0 * dst_pitch + at;
   const bool turns = head >= 0 && c < p.turned, rests = head >= 0 && c >= p.turned && src != dst;
-  constexpr bool kTwo = LAYOUT == EQAT_ROTARY_HALVES || WIDE == 1;         // an item that turns has two parts
+  constexpr bool kTwo = LAYOUT == EQAT_ROTARY_HALVES, kNarrow = WIDE < 8;  // an item that turns has two parts
   // first and (kTwo) second part of an item that turns; place of one that is handed on
-  const int ea = !turns ? p.rotary_dim + (c - p.turned) * WIDE : LAYOUT == EQAT_ROTARY_PAIRS && WIDE == 1 ? 2 * c : c * WIDE;
-  const int eb = LAYOUT == EQAT_ROTARY_HALVES ? ea + pairs : ea + 1;
+  const int up = (p.rotary_dim + 7) & ~7, words = (up - p.rotary_dim) >> 1, r = c - p.turned;
+  const int ea = turns || !kNarrow ? c * WIDE + (kTwo && !turns ? pairs : 0) : r < words ? p.rotary_dim + 2 * r : up + 8 * (r - words);
+  const int eb = ea + pairs;
   ptx::grid_dependency_wait();
   Piece<WIDE> va[kRows], vb[kTwo ? kRows : 1];
+  Piece<8> vr[kNarrow ? kRows : 1];
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
     const eqat_bf16* const in = src + i * src_pitch;
-    if (i < nrows && (turns || rests)) va[i] = load_piece<WIDE>(in + ea);
+    if (i < nrows && (turns || (rests && !kNarrow))) va[i] = load_piece<WIDE>(in + ea);
     if constexpr (kTwo)
       if (i < nrows && turns) vb[i] = load_piece<WIDE>(in + eb);
+    if constexpr (kNarrow)
+      if (i < nrows && rests) {
+        if (r < words) vr[i].w[0] = load_piece<2>(in + ea).w[0];
+        else vr[i] = load_piece<8>(in + ea);
+      }
   }
   if (warp < nrows) {
     int pos = 0;
@@ -113,7 +123,11 @@ __global__ void __launch_bounds__(max_threads(WIDE)) rotary_kernel(const RotaryP
   for (int i = 0; i < kRows; ++i) {
     if (i >= nrows || !s_live[i]) continue;
     eqat_bf16* const out = dst + i * dst_pitch;
-    if (rests) store_piece(out + ea, va[i]);
+    if (rests) {
+      if constexpr (!kNarrow) store_piece(out + ea, va[i]);
+      else if (r < words) store_piece(out + ea, Piece<2>{{vr[i].w[0]}});
+      else store_piece(out + ea, vr[i]);
+    }
     if (!turns) continue;
     if constexpr (WIDE == 1) {
       const float a = __uint_as_float((uint32_t)va[i].w << 16), b = __uint_as_float((uint32_t)vb[i].w << 16);
@@ -139,6 +153,10 @@ __global__ void __launch_bounds__(max_threads(WIDE)) rotary_kernel(const RotaryP
       } else {
 #pragma unroll
         for (int e = 0; e < WIDE / 2; ++e) {
+          if (PART && ea / 2 + e >= pairs) {
+            oa.w[e] = va[i].w[e];
+            continue;
+          }
           const float2 t = turn[e];
           float a, b;
           halves_of(va[i].w[e], a, b);
@@ -154,10 +172,11 @@ template <int WIDE>
 int launch_pieces(const eqat_rotary_desc& d, const RotaryRows& rows, RotaryParams& p, int sms, cudaStream_t st) {
   const bool halves = d.layout == EQAT_ROTARY_HALVES;
   const bool in_place = rows.q == rows.q_out && (d.kv_heads == 0 || rows.k == rows.k_out);
-  p.turned = halves || WIDE == 1 ? d.rotary_dim / 2 / WIDE : d.rotary_dim / WIDE;
-  p.rest = in_place ? 0 : (d.head_dim - d.rotary_dim) / WIDE;
+  p.turned = halves ? d.rotary_dim / 2 / WIDE : (d.rotary_dim + WIDE - 1) / WIDE;
+  const int up = (d.rotary_dim + 7) & ~7;
+  p.rest = in_place ? 0 : WIDE < 8 ? (up - d.rotary_dim) / 2 + (d.head_dim - up) / 8 : d.head_dim / WIDE - (halves ? 2 : 1) * p.turned;
   constexpr int kMost = max_threads(WIDE);
-  const int64_t items = (int64_t)p.heads * (p.turned + p.rest), chunks = (items + kMost - 1) / kMost;   // below 2^16: 2^15 heads of 511 / 256 items
+  const int64_t items = (int64_t)p.heads * (p.turned + p.rest), chunks = (items + kMost - 1) / kMost;   // below 2^16: 2^15 heads of 260 / 256 items
   // threads enough for a row in as many blocks, and a warp for each row's position
   const int even = (int)((items + chunks - 1) / chunks + 31) / 32 * 32, least = 32 * max_rows(WIDE);
   const dim3 threads(WIDE != 16 ? kMost : even > least ? even : least);
@@ -166,8 +185,11 @@ int launch_pieces(const eqat_rotary_desc& d, const RotaryRows& rows, RotaryParam
   p.block_rows = (int)(per < 1 ? 1 : per > max_rows(WIDE) ? max_rows(WIDE) : per);
   const dim3 grid((unsigned)((d.rows + p.block_rows - 1) / p.block_rows), (unsigned)chunks);
   const size_t smem = (size_t)p.block_rows * (d.rotary_dim / 2) * sizeof(float2);
-  return halves ? launch_overlapped(rotary_kernel<EQAT_ROTARY_HALVES, WIDE>, grid, threads, smem, st, p)
-                : launch_overlapped(rotary_kernel<EQAT_ROTARY_PAIRS, WIDE>, grid, threads, smem, st, p);
+  if constexpr (WIDE >= 8)
+    if (!halves)
+      return d.rotary_dim % WIDE == 0 ? launch_overlapped(rotary_kernel<EQAT_ROTARY_PAIRS, WIDE, false>, grid, threads, smem, st, p)
+                                      : launch_overlapped(rotary_kernel<EQAT_ROTARY_PAIRS, WIDE, true>, grid, threads, smem, st, p);
+  return launch_overlapped(rotary_kernel<EQAT_ROTARY_HALVES, WIDE, false>, grid, threads, smem, st, p);
 }
 
 }  // namespace
@@ -185,12 +207,14 @@ int launch_rotary(const eqat_rotary_desc& d, const RotaryRows& rows, bool backwa
   p.rotary_dim = d.rotary_dim;
   p.amplitude = d.amplitude;
   p.sine = backward ? -d.amplitude : d.amplitude;
-  const int part = d.layout == EQAT_ROTARY_HALVES ? d.rotary_dim / 2 : d.rotary_dim;             // what has to be whole pieces
+  const int part = d.layout == EQAT_ROTARY_HALVES ? d.rotary_dim / 2 : 0;          // what has to be whole pieces
   const bool keys = d.kv_heads > 0;
   if (part % 16 == 0 && d.head_dim % 16 == 0 && (rows.q_pitch | rows.q_out_pitch) % 16 == 0 && aligned32(rows.q, rows.q_out) &&
       (!keys || ((rows.k_pitch | rows.k_out_pitch) % 16 == 0 && aligned32(rows.k, rows.k_out))))
     return launch_pieces<16>(d, rows, p, sms, st);
-  return part % 8 == 0 ? launch_pieces<8>(d, rows, p, sms, st) : launch_pieces<1>(d, rows, p, sms, st);
+  if (part % 8 == 0) return launch_pieces<8>(d, rows, p, sms, st);
+  if (part % 4 == 0) return launch_pieces<4>(d, rows, p, sms, st);
+  return part % 2 == 0 ? launch_pieces<2>(d, rows, p, sms, st) : launch_pieces<1>(d, rows, p, sms, st);
 }
 
 }  // namespace eqat

@@ -269,3 +269,73 @@ def test_a_padded_batch(eqat, T):
     for other in got[1:]:
         assert all(torch.equal(a, b) for a, b in zip(other, got[0]))
     assert all(torch.isfinite(t.float()).all() for t in got[0])
+
+
+# ---------------------------------------------------------------------------------------------- parts of a head
+@pytest.mark.parametrize("layout", ["halves", "pairs"])
+@pytest.mark.parametrize("head_dim,rotary_dim", [(64, 12), (80, 20), (128, 4), (128, 34), (256, 252), (64, 48), (72, 72), (96, 40), (512, 510), (128, 64)])
+@pytest.mark.parametrize("rows,q_heads,kv_heads", [(3, 5, 1), (700, 8, 8)])
+def test_any_part_of_a_head(eqat, layout, head_dim, rotary_dim, rows, q_heads, kv_heads):
+    """Pieces of every size, on any 16 bytes, in place or not: the same bits; what does not turn is handed on as it is, NaN or not."""
+    from test_gpu_rotary import check, heads, layout_code
+    turns = eqat.rotary_turns(rotary_dim, 10000.0)
+    positions = [17 * i - 40 for i in range(rows)]
+    pos = torch.tensor(positions, dtype=torch.int32, device="cuda")
+    d = eqat.make_rotary_desc(rows, q_heads, kv_heads, head_dim, rotary_dim, layout_code(eqat, layout), 0.5)
+    src = [heads(rows, h, head_dim, i) for i, h in enumerate((q_heads, kv_heads))]
+    for t in src:
+        t[..., rotary_dim:][..., ::3] = float("nan")
+        t[..., rotary_dim:][..., 1::3] = float("inf")
+    buf, got = Guarded(), []
+    for shift in (0, 16, 32):
+        given, out = ([buf.empty(*t.shape, dtype=torch.bfloat16, shift_bytes=shift) for t in src] for _ in range(2))
+        for a, b in zip(given, src):
+            a.copy_(b)
+        eqat.eqat_rotary_fwd(d, *given, turns.cuda(), *out, pos)
+        for a, b in zip(given, src):
+            assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+        eqat.eqat_rotary_fwd(d, *given, turns.cuda(), *given, pos)
+        mixed = [given[0].clone(), torch.empty_like(src[1])]                 # queries in place, keys not
+        mixed[0].copy_(src[0])
+        eqat.eqat_rotary_fwd(d, mixed[0], src[1], turns.cuda(), *mixed, pos)
+        got += [out, given, mixed]
+    buf.check()
+    for pair in got:
+        for x, y, want in zip(src, pair, got[0]):
+            assert torch.equal(y.view(torch.int16), want.view(torch.int16))
+            assert torch.equal(y[..., rotary_dim:].reshape(-1).view(torch.int16), x[..., rotary_dim:].reshape(-1).view(torch.int16))
+    some = sorted({0, rows // 2, rows - 1})
+    for x, y in zip(src, got[0]):
+        check(y[some][..., :rotary_dim], x[some][..., :rotary_dim], turns, [positions[i] for i in some], layout, 1, 0.5)
+
+
+@pytest.mark.parametrize("rows,n", [(3, 1000), (700, 4096), (5, 16), (64, 8208)])
+def test_gated_on_any_16_bytes(eqat, rows, n):
+    """Pieces of 16 and of 8: the same bits."""
+    src, d, buf, got = [normal(rows, n, seed=i, std=1.5) for i in range(3)], eqat.make_gated_desc(rows, n, eqat.EQAT_ACT_GELU), Guarded(), []
+    for shift in (0, 16):
+        given = [buf.empty(rows, n, dtype=torch.bfloat16, shift_bytes=shift) for _ in src]
+        for a, b in zip(given, src):
+            a.copy_(b)
+        out = [buf.empty(rows, n, dtype=torch.bfloat16, shift_bytes=shift) for _ in range(3)]
+        eqat.eqat_gated_fwd(d, given[0], given[1], out[0])
+        eqat.eqat_gated_bwd(d, given[2], given[0], given[1], out[1], out[2])
+        got.append(out)
+    buf.check()
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("rows,n,group", [(3, 256, 32), (700, 4096, 128), (33, 5120, 5120), (50, 1040, 1040), (9, 16384, 64), (2, 32768, 256), (11, 384, 128)])
+def test_norm_on_any_16_bytes(eqat, rows, n, group):
+    """The order of a sum hangs on the shape alone."""
+    src, W, buf, got = [rows_of(rows, n, i) for i in range(2)], weight_of(n, 3), Guarded(), []
+    for shift in (0, 16):
+        x, r, h, y, h2, y2 = (buf.empty(rows, n, dtype=torch.bfloat16, shift_bytes=shift) for _ in range(6))
+        x.copy_(src[0])
+        r.copy_(src[1])
+        eqat.eqat_rms_norm_fwd(eqat.make_norm_desc(rows, n, EPS), x, r, W, h, y)
+        codes, scales = buf.empty(rows, n, dtype=torch.int8, shift_bytes=shift), buf.empty(rows, n // group, shift_bytes=shift)
+        eqat.eqat_rms_norm_fwd(eqat.make_norm_desc(rows, n, EPS, eqat.EQAT_CODES_INT8, group), x, r, W, h2, y2, codes, scales)
+        got.append((h, y, h2, y2, codes, scales))
+    buf.check()
+    assert all(torch.equal(a, b) for a, b in zip(*got))
