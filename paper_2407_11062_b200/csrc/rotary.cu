@@ -24,6 +24,12 @@ namespace {
 __host__ __device__ constexpr int max_rows(int wide) { return wide == 16 ? 2 : 4; }
 __host__ __device__ constexpr int max_threads(int wide) { return wide == 16 ? 128 : 256; }
 
+// Place of a pair's cosine and sine among a row's: 16 bytes stay free behind those of each piece (of 16 or 8 elements), or the threads of a
+// head, which read at the same place of pieces of their own, would meet in one bank (4096 rows of 64 heads of 128, all of it turned: 20.5 us,
+// without those bytes 26.8; of 32 heads of 256 20.9 and 40.9).
+__host__ __device__ constexpr int piece_pairs(int layout, int wide) { return wide < 8 ? 1 << 20 : layout == EQAT_ROTARY_HALVES ? wide : wide / 2; }
+__host__ __device__ constexpr int turn_place(int piece, int pair) { return pair + pair / piece * 2; }
+
 struct RotaryParams : RotaryRows {
   int rows, sequences, q_heads, heads, head_dim, rotary_dim;
   int block_rows, turned, rest;                      // rows of a block; items of a head that turn, and that are handed on
@@ -65,9 +71,10 @@ __global__ void __launch_bounds__(max_threads(WIDE)) rotary_kernel(const RotaryP
   constexpr int kRows = max_rows(WIDE);
   __shared__ int s_pos[kRows];
   __shared__ bool s_live[kRows];
-  extern __shared__ __align__(16) float2 s_turn[];   // [block_rows][rotary_dim / 2]: cosine, sine, times the amplitude
+  extern __shared__ __align__(16) float2 s_turn[];   // [block_rows][turn_place(rotary_dim / 2)]: cosine, sine, times the amplitude
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int pairs = p.rotary_dim >> 1;
+  constexpr int kPiece = piece_pairs(LAYOUT, WIDE);
+  const int pairs = p.rotary_dim >> 1, turn_pitch = turn_place(kPiece, pairs);
   const int row0 = (int)blockIdx.x * p.block_rows, nrows = min(p.block_rows, p.rows - row0);
   // this thread's item: the c-th of a head, turned ones first, then those handed on
   const int item = (int)(blockIdx.y * blockDim.x + threadIdx.x), items = p.turned + p.rest;
@@ -115,7 +122,7 @@ __global__ void __launch_bounds__(max_threads(WIDE)) rotary_kernel(const RotaryP
     const uint64_t angle = (uint64_t)(int64_t)s_pos[r] * (((uint64_t)f.y << 32) | f.x) + 0x80000000ull;
     float sn, cs;
     sincospif((float)(int32_t)(angle >> 32) * 0x1p-31f, &sn, &cs);
-    s_turn[i] = make_float2(cs * p.amplitude, sn * p.sine);
+    s_turn[r * turn_pitch + turn_place(kPiece, k)] = make_float2(cs * p.amplitude, sn * p.sine);
   }
   __syncthreads();
   ptx::grid_dependents_launch();
@@ -131,12 +138,12 @@ __global__ void __launch_bounds__(max_threads(WIDE)) rotary_kernel(const RotaryP
     if (!turns) continue;
     if constexpr (WIDE == 1) {
       const float a = __uint_as_float((uint32_t)va[i].w << 16), b = __uint_as_float((uint32_t)vb[i].w << 16);
-      const float2 t = s_turn[i * pairs + c];
+      const float2 t = s_turn[i * turn_pitch + c];
       const uint32_t o = pack_bf16x2(a * t.x - b * t.y, b * t.x + a * t.y);
       out[ea] = (eqat_bf16)(o & 0xFFFFu);
       out[eb] = (eqat_bf16)(o >> 16);
     } else {
-      const float2* const turn = s_turn + i * pairs + (kTwo ? ea : ea / 2);
+      const float2* const turn = s_turn + i * turn_pitch + turn_place(kPiece, kTwo ? ea : ea / 2);
       Piece<WIDE> oa;
       if constexpr (kTwo) {
         Piece<WIDE> ob;
@@ -179,12 +186,12 @@ int launch_pieces(const eqat_rotary_desc& d, const RotaryRows& rows, RotaryParam
   const int64_t items = (int64_t)p.heads * (p.turned + p.rest), chunks = (items + kMost - 1) / kMost;   // below 2^16: 2^15 heads of 260 / 256 items
   // threads enough for a row in as many blocks, and a warp for each row's position
   const int even = (int)((items + chunks - 1) / chunks + 31) / 32 * 32, least = 32 * max_rows(WIDE);
-  const dim3 threads(WIDE != 16 ? kMost : even > least ? even : least);
+  const dim3 threads(WIDE != 16 && chunks > 1 ? kMost : even > least ? even : least);
   // several rows a block where there are enough blocks all the same
   const int64_t per = d.rows * chunks / ((int64_t)sms * 8);
   p.block_rows = (int)(per < 1 ? 1 : per > max_rows(WIDE) ? max_rows(WIDE) : per);
   const dim3 grid((unsigned)((d.rows + p.block_rows - 1) / p.block_rows), (unsigned)chunks);
-  const size_t smem = (size_t)p.block_rows * (d.rotary_dim / 2) * sizeof(float2);
+  const size_t smem = (size_t)p.block_rows * turn_place(piece_pairs(d.layout, WIDE), d.rotary_dim / 2) * sizeof(float2);
   if constexpr (WIDE >= 8)
     if (!halves)
       return d.rotary_dim % WIDE == 0 ? launch_overlapped(rotary_kernel<EQAT_ROTARY_PAIRS, WIDE, false>, grid, threads, smem, st, p)
