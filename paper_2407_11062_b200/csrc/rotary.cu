@@ -7,10 +7,10 @@
 // 4 bytes an element cross HBM, which bounds long calls.  A thread owns one item of a row, the same in each of the block's rows:
 // 2 x 16 elements of a head (HALVES: a piece of each half; PAIRS: one piece; 8 each where alignment says so), whose places it works out
 // once.  It asks for the pieces of all its rows first; while they are on their way the block's warps look the rows' positions up, and
-// its threads compute the rows' sines and cosines into shared memory.  4094 rows of 80 heads of 128, a quarter of each turned: 28.2 us,
-// 0.91 of a copy's bandwidth (a thread on every 256th item of eight rows, one load at a time: 62.3; items kept, positions first: 43.6;
+// its threads compute the rows' sines and cosines into shared memory.  4094 rows of 80 heads of 128, a quarter of each turned: 28.3 us,
+// 0.90 of a copy's bandwidth (a thread on every 256th item of eight rows, one load at a time: 62.3; items kept, positions first: 43.6;
 // 16 bytes at a time, four rows of 256 threads: 29.3; 32 bytes and up to 64, 192, 280 threads: 28.8, 28.7, 30.2; one row of 192:
-// 32.4); 64 rows of 72 heads 3.0 us, a launch and two waits for memory.  4096 rows of 40 heads of 128, 34 elements of each turned: 25.2 us as
+// 32.4); 64 rows of 72 heads 3.0 us, a launch and two waits for memory.  4096 rows of 40 heads of 128, 34 elements of each turned: 25.3 us as
 // halves, 14.4 as pairs (element by element 55.7 and 51.5).
 #include "between.cuh"
 #include "common.cuh"
@@ -20,9 +20,10 @@
 namespace eqat {
 namespace {
 
-// Elements of a piece: 16 or 8, and of halves that are not whole pieces of 8 also 4, 2 or 1.  Rows of a block, all of whose pieces a thread has on their way, and its threads at most.
+// Elements of a piece: 16 or 8, and of halves that are not whole pieces of 8 also 4, 2 or 1.  Rows of a block, all of whose pieces a
+// thread has on their way, and its threads at most (128 against 256 for pieces of 8 and less: -15 % to +3 %; singles +10 %).
 __host__ __device__ constexpr int max_rows(int wide) { return wide == 16 ? 2 : 4; }
-__host__ __device__ constexpr int max_threads(int wide) { return wide == 16 ? 128 : 256; }
+__host__ __device__ constexpr int max_threads(int wide) { return wide > 1 ? 128 : 256; }
 
 // Place of a pair's cosine and sine among a row's: 16 bytes stay free behind those of each piece (of 16 or 8 elements), or the threads of a
 // head, which read at the same place of pieces of their own, would meet in one bank (4096 rows of 64 heads of 128, all of it turned: 20.5 us,
@@ -186,7 +187,7 @@ int launch_pieces(const eqat_rotary_desc& d, const RotaryRows& rows, RotaryParam
   const int64_t items = (int64_t)p.heads * (p.turned + p.rest), chunks = (items + kMost - 1) / kMost;   // below 2^16: 2^15 heads of 260 / 256 items
   // threads enough for a row in as many blocks, and a warp for each row's position
   const int even = (int)((items + chunks - 1) / chunks + 31) / 32 * 32, least = 32 * max_rows(WIDE);
-  const dim3 threads(WIDE != 16 && chunks > 1 ? kMost : even > least ? even : least);
+  const dim3 threads(even > least ? even : least);
   // several rows a block where there are enough blocks all the same
   const int64_t per = d.rows * chunks / ((int64_t)sms * 8);
   p.block_rows = (int)(per < 1 ? 1 : per > max_rows(WIDE) ? max_rows(WIDE) : per);
