@@ -465,7 +465,8 @@ int eqat_cache_attention(const eqat_cache_desc* desc, const eqat_attention_desc*
  * with a NaN gives NaN in y and the scales, one with an infinity NaN where it
  * stands (its group) and zeros elsewhere; codes of such groups may be anything.  A
  * row whose sum of squares passes binary32 gives zeros (NaN where h * w passes it
- * too), with eps = 0 a row of zeros gives NaN.
+ * too), with eps = 0 a row of zeros gives NaN, and one whose root mean square is
+ * below 2^-66 loses bits with its squares.
  *
  * features: a multiple of 8, at most 32768.  group (with codes): 32, 64, 128 or 256
  * dividing features, or features itself; 0 without codes. */

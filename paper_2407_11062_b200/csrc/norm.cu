@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_bwd_kernel(c
     }
     s = reduce_row<WARP>(s, red, turn);
     const float c = rsqrtf(fmaf(s.a, p.inverse_n, p.eps));
-    const float k = c * c * (s.b * p.inverse_n);
+    const float k = c * (s.b * p.inverse_n);           // c^2 by itself would leave binary32 where c passes 2^64
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       float (&hh)[8] = h[i % kHeld], (&yy)[8] = y[i % kHeld];
@@ -339,8 +339,9 @@ __global__ void __launch_bounds__(WARP ? kBlock : kMaxThreads) norm_bwd_kernel(c
       unpack(residual ? vector_of(2, i) : make_uint4(0u, 0u, 0u, 0u), r);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        dw[i][e] = fmaf(yy[e], hh[e] * c, dw[i][e]);
-        r[e] = fmaf(c, fmaf(-hh[e], k, yy[e] * g[e]), r[e]);
+        const float hc = hh[e] * c;
+        dw[i][e] = fmaf(yy[e], hc, dw[i][e]);
+        r[e] = fmaf(c, fmaf(-hc, k, yy[e] * g[e]), r[e]);
       }
       if (at + i * span < p.vecs) reinterpret_cast<uint4*>(p.dX)[(size_t)row * p.vecs + at + i * span] = pack(r);
     }
