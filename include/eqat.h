@@ -447,8 +447,8 @@ int eqat_cache_attention(const eqat_cache_desc* desc, const eqat_attention_desc*
  * with its backward pass.  Sizes are on the host; nothing is allocated, and calls
  * can be captured.  Statistics, angles and sums are held in 32 bits or more and
  * every output is rounded once, where nothing else is said.  In place means the
- * very same array (and pitch); arrays that overlap in any other way give undefined
- * values. */
+ * very same array and, with more than one row, the same pitch (EQAT_ERR_SHAPE
+ * otherwise); arrays that overlap in any other way give undefined values. */
 
 /* ---- root-mean-square norm of the residual stream
  *

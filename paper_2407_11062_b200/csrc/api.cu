@@ -155,6 +155,11 @@ inline bool workspace_ok(const void* workspace, size_t bytes, size_t need) {
   return need == 0 || (workspace != nullptr && bytes >= need && (reinterpret_cast<uintptr_t>(workspace) & 255u) == 0);
 }
 
+// An output in place of an input keeps its pitch; with another one rows would overwrite rows that are still to be read.
+inline bool overwrites_rows(int64_t rows, const eqat_bf16* in, int64_t in_pitch, const eqat_bf16* out, int64_t out_pitch) {
+  return rows > 1 && in == out && in_pitch != out_pitch;
+}
+
 int check_norm_desc(const eqat_norm_desc* d) {
   if (d == nullptr) return EQAT_ERR_NULL;
   if (d->rows <= 0 || d->rows > (int64_t)1 << 30) return EQAT_ERR_SHAPE;
@@ -193,7 +198,9 @@ int rotary(const eqat_rotary_desc* d, const RotaryRows& r, bool backward, void* 
   if (d->kv_heads > 0) {
     if (!pitch_ok(r.k_pitch, d->kv_heads, d->head_dim) || !pitch_ok(r.k_out_pitch, d->kv_heads, d->head_dim)) return EQAT_ERR_SHAPE;
     if ((rc = check_ptrs(r.k, r.k_out)) != EQAT_OK) return rc;
+    if (overwrites_rows(d->rows, r.k, r.k_pitch, r.k_out, r.k_out_pitch)) return EQAT_ERR_SHAPE;
   }
+  if (overwrites_rows(d->rows, r.q, r.q_pitch, r.q_out, r.q_out_pitch)) return EQAT_ERR_SHAPE;
   // one of the two ways to give positions
   if (r.positions != nullptr) {
     if (r.row_offsets != nullptr || r.lengths != nullptr) return EQAT_ERR_UNSUPPORTED;
@@ -632,6 +639,7 @@ int eqat_gated_fwd(const eqat_gated_desc* d, const eqat_bf16* G, int64_t g_pitch
   EQAT_TRY(check_gated_desc(d));
   if (!pitch_ok(g_pitch, 1, d->features) || !pitch_ok(u_pitch, 1, d->features)) return EQAT_ERR_SHAPE;
   EQAT_TRY(check_ptrs(G, U, H));
+  if (overwrites_rows(d->rows, G, g_pitch, H, d->features) || overwrites_rows(d->rows, U, u_pitch, H, d->features)) return EQAT_ERR_SHAPE;
   return launch_gated_fwd(*d, G, g_pitch, U, u_pitch, H, as_stream(stream));
 }
 
@@ -641,6 +649,9 @@ int eqat_gated_bwd(const eqat_gated_desc* d, const eqat_bf16* dH, const eqat_bf1
   if (!pitch_ok(g_pitch, 1, d->features) || !pitch_ok(u_pitch, 1, d->features)) return EQAT_ERR_SHAPE;
   if (!pitch_ok(dg_pitch, 1, d->features) || !pitch_ok(du_pitch, 1, d->features)) return EQAT_ERR_SHAPE;
   EQAT_TRY(check_ptrs(dH, G, U, dG, dU));
+  const struct { const eqat_bf16* at; int64_t pitch; } in[] = {{dH, d->features}, {G, g_pitch}, {U, u_pitch}};
+  for (const auto& i : in)
+    if (overwrites_rows(d->rows, i.at, i.pitch, dG, dg_pitch) || overwrites_rows(d->rows, i.at, i.pitch, dU, du_pitch)) return EQAT_ERR_SHAPE;
   return launch_gated_bwd(*d, dH, G, g_pitch, U, u_pitch, dG, dg_pitch, dU, du_pitch, as_stream(stream));
 }
 
