@@ -175,8 +175,8 @@ int check_norm_desc(const eqat_norm_desc* d) {
 int check_rotary_desc(const eqat_rotary_desc* d) {
   if (d == nullptr) return EQAT_ERR_NULL;
   if (d->rows <= 0 || d->rows > (int64_t)1 << 30) return EQAT_ERR_SHAPE;
-  if (d->q_heads <= 0 || d->q_heads > 1 << 14 || d->kv_heads < 0 || d->kv_heads > 1 << 14) return EQAT_ERR_SHAPE;
-  if (d->head_dim <= 0 || d->head_dim % 8 != 0 || d->head_dim > 512) return EQAT_ERR_SHAPE;
+  if (d->q_heads <= 0 || d->q_heads > kMaxRotaryHeads || d->kv_heads < 0 || d->kv_heads > kMaxRotaryHeads) return EQAT_ERR_SHAPE;
+  if (d->head_dim <= 0 || d->head_dim % 8 != 0 || d->head_dim > kMaxRotaryHeadDim) return EQAT_ERR_SHAPE;
   if (d->rotary_dim <= 0 || d->rotary_dim % 2 != 0 || d->rotary_dim > d->head_dim) return EQAT_ERR_SHAPE;
   if (d->layout != EQAT_ROTARY_HALVES && d->layout != EQAT_ROTARY_PAIRS) return EQAT_ERR_UNSUPPORTED;
   if (d->sequences < 0 || d->sequences > 1 << 20) return EQAT_ERR_SHAPE;

@@ -15,6 +15,7 @@ size_t norm_workspace(const eqat_norm_desc& d, int sms);
 int launch_norm_bwd(const eqat_norm_desc& d, const eqat_bf16* dY, const eqat_bf16* H, const eqat_bf16* W, const eqat_bf16* dR,
                     eqat_bf16* dX, float* dW, void* workspace, cudaStream_t st);
 
+constexpr int kMaxRotaryHeads = 1 << 14, kMaxRotaryHeadDim = 512;       // of queries, and of keys
 struct RotaryRows {
   const eqat_bf16 *q, *k;
   int64_t q_pitch, k_pitch;

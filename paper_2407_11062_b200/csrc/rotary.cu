@@ -176,15 +176,42 @@ __global__ void __launch_bounds__(max_threads(WIDE)) rotary_kernel(const RotaryP
   }
 }
 
+// Items of a head that turn, and that are handed on where a result is not in place.
+constexpr int turned_items(int layout, int wide, int rotary_dim) {
+  return layout == EQAT_ROTARY_HALVES ? rotary_dim / 2 / wide : (rotary_dim + wide - 1) / wide;
+}
+constexpr int rest_items(int layout, int wide, int head_dim, int rotary_dim) {
+  const int up = (rotary_dim + 7) & ~7;
+  return wide < 8 ? (up - rotary_dim) / 2 + (head_dim - up) / 8
+                  : head_dim / wide - (layout == EQAT_ROTARY_HALVES ? 2 : 1) * turned_items(layout, wide, rotary_dim);
+}
+// The largest piece that a half of `part` elements consists of (0: no halves), where 32 bytes at a time cannot be had.
+constexpr int piece_of(int part) { return part % 8 == 0 ? 8 : part % 4 == 0 ? 4 : part % 2 == 0 ? 2 : 1; }
+
+// A row's items go over the grid's second dimension, at most 65535 blocks: 256 items a head over 256 threads (510 elements as halves) and
+// 129 over 128 (508) are the most there are.
+constexpr bool rows_fit_the_grid() {
+  for (int layout : {EQAT_ROTARY_HALVES, EQAT_ROTARY_PAIRS})
+    for (int dim = 2; dim <= kMaxRotaryHeadDim; dim += 2) {
+      const int part = layout == EQAT_ROTARY_HALVES ? dim / 2 : 0;
+      for (int wide : {piece_of(part), 16}) {
+        if (part % wide != 0) continue;
+        const int64_t items = 2ll * kMaxRotaryHeads * (turned_items(layout, wide, dim) + rest_items(layout, wide, kMaxRotaryHeadDim, dim));
+        if ((items + max_threads(wide) - 1) / max_threads(wide) > 65535) return false;
+      }
+    }
+  return true;
+}
+static_assert(rows_fit_the_grid(), "blocks of a row");
+
 template <int WIDE>
 int launch_pieces(const eqat_rotary_desc& d, const RotaryRows& rows, RotaryParams& p, int sms, cudaStream_t st) {
   const bool halves = d.layout == EQAT_ROTARY_HALVES;
   const bool in_place = rows.q == rows.q_out && (d.kv_heads == 0 || rows.k == rows.k_out);
-  p.turned = halves ? d.rotary_dim / 2 / WIDE : (d.rotary_dim + WIDE - 1) / WIDE;
-  const int up = (d.rotary_dim + 7) & ~7;
-  p.rest = in_place ? 0 : WIDE < 8 ? (up - d.rotary_dim) / 2 + (d.head_dim - up) / 8 : d.head_dim / WIDE - (halves ? 2 : 1) * p.turned;
+  p.turned = turned_items(d.layout, WIDE, d.rotary_dim);
+  p.rest = in_place ? 0 : rest_items(d.layout, WIDE, d.head_dim, d.rotary_dim);
   constexpr int kMost = max_threads(WIDE);
-  const int64_t items = (int64_t)p.heads * (p.turned + p.rest), chunks = (items + kMost - 1) / kMost;   // below 2^16: 2^15 heads of 260 / 256 items
+  const int64_t items = (int64_t)p.heads * (p.turned + p.rest), chunks = (items + kMost - 1) / kMost;
   // threads enough for a row in as many blocks, and a warp for each row's position
   const int even = (int)((items + chunks - 1) / chunks + 31) / 32 * 32, least = 32 * max_rows(WIDE);
   const dim3 threads(even > least ? even : least);
@@ -220,9 +247,12 @@ int launch_rotary(const eqat_rotary_desc& d, const RotaryRows& rows, bool backwa
   if (part % 16 == 0 && d.head_dim % 16 == 0 && (rows.q_pitch | rows.q_out_pitch) % 16 == 0 && aligned32(rows.q, rows.q_out) &&
       (!keys || ((rows.k_pitch | rows.k_out_pitch) % 16 == 0 && aligned32(rows.k, rows.k_out))))
     return launch_pieces<16>(d, rows, p, sms, st);
-  if (part % 8 == 0) return launch_pieces<8>(d, rows, p, sms, st);
-  if (part % 4 == 0) return launch_pieces<4>(d, rows, p, sms, st);
-  return part % 2 == 0 ? launch_pieces<2>(d, rows, p, sms, st) : launch_pieces<1>(d, rows, p, sms, st);
+  switch (piece_of(part)) {
+    case 8: return launch_pieces<8>(d, rows, p, sms, st);
+    case 4: return launch_pieces<4>(d, rows, p, sms, st);
+    case 2: return launch_pieces<2>(d, rows, p, sms, st);
+    default: return launch_pieces<1>(d, rows, p, sms, st);
+  }
 }
 
 }  // namespace eqat
