@@ -513,8 +513,9 @@ int eqat_rms_norm_bwd(const eqat_norm_desc* desc, const eqat_bf16* dY, const eqa
  *     (a cos pf - b sin pf, b cos pf + a sin pf) * amplitude.
  * The other elements are handed on.  Frequencies are given as fractions of a turn
  * per position, in units of 2^-64: turns[i] = round(2^64 f_i / 2 pi) mod 2^64, so
- * that p * turns[i] mod 2^64 is the angle whatever the position; what remains is
- * rounded to 2^-32 of a turn. */
+ * that p * turns[i] mod 2^64 is the angle whatever the position; that is rounded to
+ * 2^-32 of a turn, between -1/2 and 1/2, and then to binary32: together at most
+ * 2^-26 + 2^-33 of a turn, 1e-7 radians, for any position. */
 enum { EQAT_ROTARY_HALVES = 0, EQAT_ROTARY_PAIRS = 1 };
 
 typedef struct {
