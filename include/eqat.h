@@ -627,6 +627,14 @@ int qlinear_packed_gated_fwd(const eqat_desc* desc, int activation, const eqat_b
  * expected to be faster than two projections.  `sms` as in eqat_packed_fwd_route. */
 int eqat_packed_gated_route(const eqat_desc* desc, int sms);
 
+/* The output tiles of both weights' contractions (a diagnostic): `op` is
+ * EQAT_OP_PACKED_GATED_FWD, for the tiled kernel, whether or not the call takes it, or
+ * EQAT_OP_PACKED_GATED_BWD.  h_tile receives the three numbers of eqat_gemm_tile (columns
+ * of a forward tile: half of them of either weight) and the parts that the contraction is
+ * split into, whose sums pass through the workspace where there is more than one.  `sms`
+ * as in eqat_packed_fwd_route. */
+int eqat_packed_gated_tile(const eqat_desc* desc, int op, int sms, int* h_tile);
+
 /* dG and dU as in eqat_gated_bwd, and
  *     dX = dG * W_gate + dU * W_up
  * of them as they are stored, one contraction over the features of both.  The step

@@ -136,6 +136,7 @@ def _load():
         "eqat_gated_fwd": (c_int, [G, P, c_int64, P, c_int64, P, P]),
         "eqat_gated_bwd": (c_int, [G, P, P, c_int64, P, c_int64, P, c_int64, P, c_int64, P]),
         "eqat_packed_gated_route": (c_int, [D, c_int]),
+        "eqat_packed_gated_tile": (c_int, [D, c_int, c_int, POINTER(c_int)]),
         "qlinear_packed_gated_fwd": (c_int, [D, c_int, P, W, W, P, P, P, P, c_size_t, P]),
         "qlinear_packed_gated_bwd": (c_int, [D, c_int, P, P, P, W, W, P, P, P, P, c_size_t, P]),
         "eqat_block_ap_step": (c_int, [POINTER(eqat_block_ap_linear), c_int, POINTER(c_int), P]),
@@ -443,6 +444,13 @@ def eqat_packed_gated_route(desc, sms=0) -> int:
     if route < 0:
         raise EqatError(route, "eqat_packed_gated_route")
     return route
+
+
+def eqat_packed_gated_tile(desc, op, sms=0):
+    """Tiles of both weights' contraction (EQAT_OP_PACKED_GATED_FWD, _BWD): rows per CTA, columns, CTAs that share a tile, parts of K."""
+    tile = (c_int * 4)()
+    _check(lib.eqat_packed_gated_tile(ctypes.byref(desc), int(op), int(sms), tile), "eqat_packed_gated_tile")
+    return tuple(tile)
 
 
 # A weight: (Wq_packed, s16, z).

@@ -661,6 +661,20 @@ int eqat_packed_gated_route(const eqat_desc* d, int sms) {
   return gated_route(*d, sms).kernel;
 }
 
+int eqat_packed_gated_tile(const eqat_desc* d, int op, int sms, int* h_tile) {
+  if (op != EQAT_OP_PACKED_GATED_FWD && op != EQAT_OP_PACKED_GATED_BWD) return EQAT_ERR_UNSUPPORTED;
+  EQAT_TRY(check_gated_desc(d));
+  if (h_tile == nullptr) return EQAT_ERR_NULL;
+  if (sms < 0) return EQAT_ERR_SHAPE;
+  if (sms == 0) sms = sms_or_148();
+  const JointPlan t = op == EQAT_OP_PACKED_GATED_BWD ? joint_plan(*d, sms) : JointPlan{packed_shape((int)d->tokens, 2 * d->out_features, sms), 1};
+  h_tile[0] = 128 * t.shape.mt;
+  h_tile[1] = t.shape.bn;
+  h_tile[2] = t.shape.pair ? 2 : 1;
+  h_tile[3] = t.split;
+  return EQAT_OK;
+}
+
 int qlinear_packed_gated_fwd(const eqat_desc* d, int activation, const eqat_bf16* X, const eqat_packed_weight* gate,
                              const eqat_packed_weight* up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, void* workspace,
                              size_t workspace_bytes, void* stream) {

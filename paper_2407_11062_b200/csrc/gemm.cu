@@ -1333,17 +1333,11 @@ int launch_packed_gated(const eqat_desc& d, int activation, const eqat_bf16* X, 
   }
 }
 
-namespace {
-
-// Tiles of dX of two weights, and the parts of their K.
-struct JointPlan {
-  TileShape shape;
-  int split;
-};
-// The least expected time over the three shapes of packed tiles and up to eight parts of at least 16 K blocks.  A K block of 64
-// takes a cluster 0.42 / 0.49 / 0.47 us (2 / 3 / 4-bit codes) on tiles of 128 x 128, 0.88 / 1.13 / 1.15 on 256 x 256, 0.65 / 0.72 / 0.67
-// on the 512 x 256 of a pair, as in the forward (wide.cu); a tile's epilogue about 3 us; the parts' sums, at most 64 MB so that they
-// stay in L2, are written and read at about 5 TB/s.  2 x 11008 x 4096, 2 bits, 1 / 256 / 512 / 1200 tokens: 137, 140, 144, 228 us with K whole, 45, 61, 84, 211 split.
+// Tiles of dX of two weights, and the parts of their K: the least expected time over the three shapes of packed tiles and up to eight
+// parts of at least 16 K blocks.  A K block of 64 takes a cluster 0.42 / 0.49 / 0.47 us (2 / 3 / 4-bit codes) on tiles of 128 x 128,
+// 0.88 / 1.13 / 1.15 on 256 x 256, 0.65 / 0.72 / 0.67 on the 512 x 256 of a pair, as in the forward (wide.cu); a tile's epilogue about
+// 3 us; the parts' sums, at most 64 MB so that they stay in L2, are written and read at about 5 TB/s.  2 x 11008 x 4096, 2 bits, 1 / 256 /
+// 512 / 1200 tokens: 137, 140, 144, 228 us with K whole, 45, 61, 84, 211 split.
 JointPlan joint_plan(const eqat_desc& d, int sms) {
   const int T = (int)d.tokens, in = d.in_features, kb = 2 * (d.out_features / BK);
   const TileShape shapes[3] = {{1, false, 128}, {2, false, kBN}, {2, true, kBN}};
@@ -1367,8 +1361,6 @@ JointPlan joint_plan(const eqat_desc& d, int sms) {
   }
   return best;
 }
-
-}  // namespace
 
 size_t packed_gated_dx_workspace(const eqat_desc& d, int sms) {
   const int split = joint_plan(d, sms).split;

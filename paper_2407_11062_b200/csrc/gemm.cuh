@@ -58,6 +58,11 @@ int launch_packed_dx(const eqat_desc& d, const eqat_bf16* dY, const uint8_t* Wq,
 int launch_packed_gated(const eqat_desc& d, int activation, const eqat_bf16* X, const eqat_packed_weight& gate,
                         const eqat_packed_weight& up, eqat_bf16* H, eqat_bf16* G, eqat_bf16* U, cudaStream_t st);
 // dX = dG * dequant(gate) + dU * dequant(up) in one contraction.  Few tokens need scratch, for sums over parts of K.
+struct JointPlan {
+  TileShape shape;
+  int split;                 // parts of K
+};
+JointPlan joint_plan(const eqat_desc& d, int sms);
 size_t packed_gated_dx_workspace(const eqat_desc& d, int sms);
 int launch_packed_gated_dx(const eqat_desc& d, const eqat_bf16* dG, const eqat_bf16* dU, const eqat_packed_weight& gate,
                            const eqat_packed_weight& up, eqat_bf16* dX, void* workspace, cudaStream_t st);
