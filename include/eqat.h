@@ -613,6 +613,10 @@ typedef struct {              /* a weight as qlinear_packed_fwd takes it: device
  * qlinear_packed_fwd and one of eqat_gated_fwd, through G and U or, where these are
  * NULL, through the workspace; H is then that of G and U as they are rounded.  What
  * is said of qlinear_packed_fwd, of how weights enter the products and of bits, holds.
+ * So H of random numbers is off, in relative norm, by its own rounding where codes
+ * enter as integers (1.7e-3, up to 64 tokens), by the rounding of both weights too on
+ * EQAT_ROUTE_TILED (2.9e-3), and by that of G and U besides on
+ * EQAT_ROUTE_WEIGHT_ROW_PAIRS (3.8e-3).
  * Without G and U it needs eqat_workspace_bytes(desc, EQAT_OP_PACKED_GATED_FWD) bytes
  * of scratch on the current device (0: workspace may be NULL; with G and U it always
  * may).  Calls that may overlap need a workspace each, here and in the backward pass.

@@ -51,7 +51,7 @@ __device__ __forceinline__ void activate_with_slope(float g, float& a, float& sl
   }
 }
 
-// For every activation: f(std::integral_constant<int, ACT>).
+// Runs the statements with kAct, a constant, as the activation that `act` says at run time.
 #define EQAT_WITH_ACTIVATION(act, ...)                                                     \
   do {                                                                                     \
     if ((act) == EQAT_ACT_SILU) { constexpr int kAct = EQAT_ACT_SILU; __VA_ARGS__; }       \

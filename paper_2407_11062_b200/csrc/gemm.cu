@@ -1337,7 +1337,12 @@ int launch_packed_gated(const eqat_desc& d, int activation, const eqat_bf16* X, 
 // parts of at least 16 K blocks.  A K block of 64 takes a cluster 0.42 / 0.49 / 0.47 us (2 / 3 / 4-bit codes) on tiles of 128 x 128,
 // 0.88 / 1.13 / 1.15 on 256 x 256, 0.65 / 0.72 / 0.67 on the 512 x 256 of a pair, as in the forward (wide.cu); a tile's epilogue about
 // 3 us; the parts' sums, at most 64 MB so that they stay in L2, are written and read at about 5 TB/s.  2 x 11008 x 4096, 2 bits, 1 / 256 /
-// 512 / 1200 tokens: 137, 140, 144, 228 us with K whole, 45, 61, 84, 211 split.
+// 512 / 1200 tokens: 137, 140, 144, 228 us with K whole, 45, 61, 84, 211 split.  (The price of 128 x 128 is what it takes; the line that
+// wide.cu draws is a little above it, since its own estimate is high there.)
+// Against every plan there is, 180 calls of 1 to 2048 tokens, five shapes from 2 x 1408 x 2048 to 2 x 28672 x 8192, 2, 3 and 4 bits: the
+// plans picked take 0.7 % more than the fastest, 147 are it, 19 take more than 5 % longer.  Worst: 5504 x 2048, 192 to 384 tokens, 7 to
+// 34 % (256 tokens, 2 bits: pairs in eight parts 41.9 us, 128 x 128 in four 31.1); 28672 x 8192, 1 token, 11 to 17 %; 13824 x 5120, 700 tokens,
+// 3 bits, 17 %.
 JointPlan joint_plan(const eqat_desc& d, int sms) {
   const int T = (int)d.tokens, in = d.in_features, kb = 2 * (d.out_features / BK);
   const TileShape shapes[3] = {{1, false, 128}, {2, false, kBN}, {2, true, kBN}};
