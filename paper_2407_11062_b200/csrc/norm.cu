@@ -400,34 +400,25 @@ RowShape row_shape(int vecs, int pairs) {
   return {vpt, ((vecs + vpt - 1) / vpt + 31) / 32 * 32};
 }
 
-// How a call goes out: blocks, and stages of the ring.
+// How the backward pass goes out: blocks, and stages of the ring.
 struct Launch {
   int blocks, stages;
   size_t smem;
 };
-// `tensors` in the ring; `busy`: threads of an SM that the kernel's registers leave room for; `stages`: at most.
-Launch launch_shape(int64_t rows, const RowShape& s, int tensors, int busy, int stages, int sms) {
+Launch backward_shape(const eqat_norm_desc& d, int sms) {
+  constexpr int kBusy = 512, kMostStages = 3;          // threads of an SM that the kernel's registers leave room for
+  const RowShape s = row_shape(d.features / 8, kMaxThreads);
   const int threads = s.threads == 32 ? kBlock : s.threads, rows_of_block = s.threads == 32 ? kBlock / 32 : 1;
-  const int stage = threads * s.vpt * tensors * 16;
-  int per_sm = busy / threads < 1 ? 1 : busy / threads;
+  const int stage = threads * s.vpt * 3 * 16;          // of H, dY and dR
+  int per_sm = kBusy / threads < 1 ? 1 : kBusy / threads, stages = kMostStages;
   // all stages, if need be with fewer blocks; fewer stages where they do not fit an SM
   while (per_sm > 1 && per_sm * stages * stage > kRingBytes) --per_sm;
   while (stages > 1 && stages * stage > kRingBytes) --stages;
-  const int64_t need = (rows + rows_of_block - 1) / rows_of_block, most = (int64_t)sms * per_sm;
-  return {(int)(need < most ? need : most), stages, (size_t)stages * stage};
-}
-Launch backward_shape(const eqat_norm_desc& d, int sms) {
-  const RowShape s = row_shape(d.features / 8, kMaxThreads);
-  Launch l = launch_shape(d.rows, s, 3, 512, 3, sms);
+  const int64_t need = (d.rows + rows_of_block - 1) / rows_of_block, most = (int64_t)sms * per_sm;
+  Launch l{(int)(need < most ? need : most), stages, (size_t)stages * stage};
   const size_t share = (size_t)(kBlock / 32) * d.features * sizeof(float);
   if (s.threads == 32 && l.smem < share) l.smem = share;
   return l;
-}
-
-template <typename... P, typename... A>
-int launch_with(void (*kernel)(P...), SmemOptIn& opt_in, const Launch& l, int threads, cudaStream_t st, A... args) {
-  if (l.smem > 40000 && !opt_in.ensure(kernel, kRingBytes)) return EQAT_ERR_CUDA;
-  return launch_overlapped(kernel, dim3(l.blocks), dim3(threads), l.smem, st, args...);
 }
 
 template <int VPT, bool WARP, bool LOOP, int CODES>
@@ -453,7 +444,8 @@ int launch_fwd(const eqat_norm_desc& d, const NormFwd& p, const RowShape& s, int
 template <int VPT, bool WARP>
 int launch_bwd(const NormBwd& p, const RowShape& s, const Launch& l, cudaStream_t st) {
   static SmemOptIn opt_in;
-  return launch_with(norm_bwd_kernel<VPT, WARP>, opt_in, l, WARP ? kBlock : s.threads, st, p, l.stages);
+  if (l.smem > 40000 && !opt_in.ensure(norm_bwd_kernel<VPT, WARP>, kRingBytes)) return EQAT_ERR_CUDA;
+  return launch_overlapped(norm_bwd_kernel<VPT, WARP>, dim3(l.blocks), dim3(WARP ? kBlock : s.threads), l.smem, st, p, l.stages);
 }
 
 }  // namespace
