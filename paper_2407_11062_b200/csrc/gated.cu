@@ -3,10 +3,11 @@
 // projections pass through memory and come here too.)
 //
 // Element-wise: 6 bytes an element forward and 10 backward, which HBM bounds: 4096 x 11008 forward 40.3 us (1.02 of a copy's
-// bandwidth), 4095 x 13824 backward 82.0 to 85.3 us (1.01 to 1.05; runs on one GPU and another).  A thread takes 16 elements, 32 bytes of
+// bandwidth), 4095 x 13824 backward 82.0 to 86.8 us (1.00 to 1.05; one GPU and another).  A thread takes 16 elements, 32 bytes of
 // each tensor, and is done: backward with a loop around it, which costs registers and so threads of an SM, 85.3 to 93.8 us where this
-// took 82.0; blocks that stay, eight an SM, 42.7 and 93.8, sixteen 41.4 and 87.9.  Where rows or places are multiples of 16 bytes only, a thread takes 8 at a time and blocks stay (44.1 and 98.0; a
-// block for every 2048 elements 49.4 and 99.6); it follows row and column by addition, not by a division for each piece.
+// took 82.0; blocks that stay, eight an SM, 42.7 and 93.8, sixteen 41.4 and 87.9.  Where rows or places are multiples of 16 bytes only, a
+// thread takes 8 at a time and blocks stay (44.1 and 98.0; a block for every 2048 elements 49.4 and 99.6); it follows row and column by
+// addition, not by a division for each piece.
 #include "activation.cuh"
 #include "between.cuh"
 #include "common.cuh"
